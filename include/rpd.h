@@ -346,6 +346,61 @@ int rpd_step_noalloc(const void *W_head, const void *g_norm, int d, int V, int K
  * is ignored. */
 void rpd_destroy(rpd_ctx *ctx);
 
+/* Element types of the operators below. */
+#define RPD_TYPE_BF16 0
+#define RPD_TYPE_F16 1
+#define RPD_TYPE_F32 2
+
+/* A head in 4 bits: products of a few activation rows with a [V][d] matrix whose elements are 4-bit
+ * codes with a scale, and optionally a zero point, for every `group` columns of a row.  (The paper
+ * has no counterpart: its heads are bf16.  A step with few rows is bound by reading the head, which
+ * in 4 bits is a quarter as long.)
+ *
+ *   y[r][v] = rho_r * sum over groups G of s[v][G] * sum over k in G of (q[v][k] - z[v][G]) * u[r][k]
+ *
+ * with u = x and rho = 1, or, with a gain g, the readout's normalisation as rpd_step applies it:
+ * u = g * x rounded to the type of x, rho_r = (mean_k x[r][k]^2 + eps)^(-1/2) applied after the
+ * sum.  Products and sums are fp32 (q - z and the scales enter exactly), and the logits are rounded
+ * once, to the type of `out`.  Inputs must be finite.
+ *
+ * rpd_quant_create: a head of d columns and V rows with groups of 32, 64 or 128 columns (others:
+ * RPD_ERR_UNSUPPORTED) on the current device; 1 <= d <= 65536, 1 <= V <= 2^24.  d need not be a
+ * multiple of the group: the last group is then shorter.  NULL on failure. */
+typedef struct rpd_quant rpd_quant; /* opaque, owned by the library */
+rpd_quant *rpd_quant_create(int d, int V, int group);
+
+/* Copy the weights into the head's own layout (V * d / 2 bytes and the scales, padded to 128 rows
+ * and whole groups); nothing of the caller's is read after the call returns.
+ *   codes  [V][(d + 1) / 2] uint8, device: column 2i in the lower four bits of byte i, column 2i + 1
+ *          in the upper ones (with odd d the last byte's upper bits are ignored);
+ *   scales [V][ceil(d / group)] bf16 or fp16 (scale_type), device;
+ *   zeros  [V][ceil(d / group)] uint8, device, lower four bits used; NULL: every zero point is 8.
+ * The copy runs on `stream`, and the call waits for it; no call on this head may be running or be
+ * captured in a graph that is used again (the layout is reallocated). */
+int rpd_quant_set_weights(rpd_quant *head, const void *codes, const void *scales, int scale_type,
+                          const void *zeros, void *stream);
+
+/* Device bytes of workspace that rpd_quant_logits needs for that many rows (0: none); -1 for a NULL
+ * head or rows < 0. */
+int64_t rpd_quant_workspace(const rpd_quant *head, int rows);
+
+/* Logits of `rows` activations, asynchronously on `stream` (a cudaStream_t, NULL = legacy default).
+ *   x    [rows][d] bf16 or fp16 (x_type), device, rows x_stride elements apart;
+ *   gain [d], type of x, device, or NULL for the plain product (eps is then ignored);
+ *   out  [rows][V] bf16, fp16 or fp32 (out_type), device, rows out_stride elements apart; elements
+ *        between the rows stay as they were; out may not overlap the inputs;
+ *   workspace  at least rpd_quant_workspace(head, rows) bytes of device memory, 256-byte aligned,
+ *        that no other call uses at the same time; NULL where that is 0.
+ * Strides are >= d and >= V (of no matter with one row); rows = 0 is a no-op.  Vectors are read 16
+ * bytes at a time where x and its stride allow it.  The head is only read: calls on several streams
+ * and from several threads may overlap. */
+int rpd_quant_logits(const rpd_quant *head, const void *x, int x_type, int64_t x_stride, int rows,
+                     const void *gain, float eps, void *out, int out_type, int64_t out_stride,
+                     void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Free the head (no call on it may be running).  NULL is ignored. */
+void rpd_quant_destroy(rpd_quant *head);
+
 /* Message of the last failing call on this host thread ("" if none). */
 const char *rpd_last_error(void);
 

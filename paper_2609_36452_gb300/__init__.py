@@ -19,6 +19,7 @@ __all__ = [
     "rpd_step_batched", "rpd_step_host", "rpd_step_noalloc", "rpd_set_vocab_shard",
     "rpd_step_shard_partials", "rpd_step_shard_finish", "rpd_profile_enable", "rpd_kernel_times",
     "rpd_build_decode_loop", "rpd_build_decode_loop_batched", "rpd_decode_loop_launch", "rpd_decode_loop_destroy", "DecodeLoop",
+    "rpd_quant_create", "rpd_quant_set_weights", "rpd_quant_workspace", "rpd_quant_logits", "rpd_quant_destroy", "QuantHead",
     "rpd_destroy", "rpd_last_error", "rpd_version", "Rpd", "RULE_PROFILES", "KERNEL_NAMES",
 ]
 
@@ -79,6 +80,12 @@ RPD_HEAD_BORROWED = 1
 HEAD_LAYOUTS = {"tiled": RPD_HEAD_TILED, "borrowed": RPD_HEAD_BORROWED}
 
 
+RPD_TYPE_BF16 = 0
+RPD_TYPE_F16 = 1
+RPD_TYPE_F32 = 2
+ELEMENT_TYPES = {"torch.bfloat16": RPD_TYPE_BF16, "torch.float16": RPD_TYPE_F16, "torch.float32": RPD_TYPE_F32}
+
+
 class RpdError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"rpd error {code}: {msg}")
@@ -122,6 +129,12 @@ def _load():
         "rpd_profile_enable": (i32, [vp, i32]),
         "rpd_kernel_times": (i32, [vp, ctypes.POINTER(ctypes.c_double),
                                    ctypes.POINTER(ctypes.c_int64), i32]),
+        "rpd_quant_create": (vp, [i32, i32, i32]),
+        "rpd_quant_set_weights": (i32, [vp, vp, vp, i32, vp, vp]),
+        "rpd_quant_workspace": (ctypes.c_int64, [vp, i32]),
+        "rpd_quant_logits": (i32, [vp, vp, i32, ctypes.c_int64, i32, vp, f32, vp, i32, ctypes.c_int64,
+                                   vp, ctypes.c_int64, vp]),
+        "rpd_quant_destroy": (None, [vp]),
         "rpd_destroy": (None, [vp]),
         "rpd_last_error": (ctypes.c_char_p, []),
         "rpd_version": (ctypes.c_char_p, []),
@@ -160,6 +173,11 @@ rpd_step_shard_partials = lib.rpd_step_shard_partials
 rpd_step_shard_finish = lib.rpd_step_shard_finish
 rpd_profile_enable = lib.rpd_profile_enable
 rpd_kernel_times = lib.rpd_kernel_times
+rpd_quant_create = lib.rpd_quant_create
+rpd_quant_set_weights = lib.rpd_quant_set_weights
+rpd_quant_workspace = lib.rpd_quant_workspace
+rpd_quant_logits = lib.rpd_quant_logits
+rpd_quant_destroy = lib.rpd_quant_destroy
 rpd_destroy = lib.rpd_destroy
 rpd_last_error = lib.rpd_last_error
 rpd_version = lib.rpd_version
@@ -189,6 +207,35 @@ def _arg(t, name: str, dtype: str, numel: int = None, cuda: bool = True):
     if numel is not None and t.numel() != numel:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: {t.numel()} elements, expected {numel}")
     return _ptr(t)
+
+
+def _rows_arg(t, name: str, types, shape):
+    """A CUDA tensor of the given shape whose innermost dimension is contiguous; its outer strides
+    (in elements) are the caller's.  Returns (pointer, RPD_TYPE_* or None, strides)."""
+    if t is None or not hasattr(t, "data_ptr"):
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: a tensor is required")
+    if not t.is_cuda:
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: must be a CUDA tensor")
+    dtype = str(t.dtype)
+    if dtype[6:] not in types:
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: dtype must be {' or '.join(types)}, not {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    strides = t.stride()
+    if shape[-1] > 1 and strides[-1] != 1 and t.numel():
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: its innermost dimension must be contiguous")
+    return _ptr(t), ELEMENT_TYPES.get(dtype), strides
+
+
+def _stream(device):
+    import torch
+    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: on {t.device}, expected {device}")
 
 
 _DEBUG_DTYPES = {"conf": "float32", "entropy": "float32", "persist": "int32", "drop": "float32",
@@ -429,3 +476,62 @@ def stats_dict(t) -> dict:
     """Decode one rpd_stats (an int32 tensor/array of STATS_WORDS) into a dict."""
     vals = [int(x) for x in (t.tolist() if hasattr(t, "tolist") else t)]
     return dict(zip(STATS_FIELDS, vals))
+
+
+class QuantHead:
+    """A [V][d] head of 4-bit codes with a scale (and optionally a zero point) for every ``group``
+    columns of a row (rpd_quant_*), on the device that is current when it is made."""
+
+    def __init__(self, d: int, V: int, group: int = 128):
+        self.d, self.V, self.group = d, V, group
+        self.handle = None
+        h = rpd_quant_create(d, V, group)
+        if not h:
+            raise RpdError(RPD_ERR_INVALID_ARGUMENT, rpd_last_error().decode())
+        self.handle = ctypes.c_void_p(h)
+        import torch
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def close(self):
+        if getattr(self, "handle", None):
+            rpd_quant_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def set_weights(self, codes, scales, zeros=None):
+        """codes [V][(d + 1) // 2] uint8 (the even column in the lower four bits), scales
+        [V][ceil(d / group)] bf16 or fp16, zeros like scales in uint8 (None: 8 everywhere); contiguous
+        CUDA tensors, copied."""
+        groups = -(-self.d // self.group)
+        kind = str(getattr(scales, "dtype", None))[6:]
+        if kind not in ("bfloat16", "float16"):
+            raise RpdError(RPD_ERR_INVALID_ARGUMENT, "scales: dtype must be bfloat16 or float16")
+        args = (_arg(codes, "codes", "uint8", self.V * ((self.d + 1) // 2)),
+                _arg(scales, "scales", kind, self.V * groups),
+                _arg(zeros, "zeros", "uint8", self.V * groups) if zeros is not None else None)
+        _same_device(self.device, codes=codes, scales=scales, zeros=zeros)
+        _check(rpd_quant_set_weights(self.handle, args[0], args[1], ELEMENT_TYPES[str(scales.dtype)], args[2],
+                                     _stream(self.device)))
+
+    def logits(self, x, out, gain=None, eps=1e-6, workspace=None):
+        """out[r] = W x[r], or with ``gain`` the readout of the normalised x[r]: x [rows][d] bf16 or
+        fp16, out [rows][V] bf16, fp16 or float32, gain [d] like x; rows may lie apart.  Runs on the
+        device's current stream.  ``workspace``: a uint8 CUDA tensor of rpd_quant_workspace bytes
+        (allocated where it is needed and None)."""
+        rows = x.shape[0] if hasattr(x, "shape") and len(x.shape) == 2 else 0
+        px, xt, xs = _rows_arg(x, "x", ("bfloat16", "float16"), (rows, self.d))
+        po, ot, os_ = _rows_arg(out, "out", ("bfloat16", "float16", "float32"), (rows, self.V))
+        pg = _arg(gain, "gain", str(x.dtype)[6:], self.d) if gain is not None else None
+        _same_device(self.device, x=x, out=out, gain=gain, workspace=workspace)
+        need = rpd_quant_workspace(self.handle, rows)
+        if need > 0 and workspace is None:
+            import torch
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        pw = _arg(workspace, "workspace", "uint8") if workspace is not None else None
+        _check(rpd_quant_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw,
+                                workspace.numel() if workspace is not None else 0, _stream(self.device)))

@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "head_plan.h"
+#include "op_host.h"
 #include "rpd_internal.h"
 
 using namespace rpd;
@@ -59,25 +60,6 @@ EncodeTiledFn encode_fn() {
     }();
     return fn;
 }
-
-// Entry points that touch the GPU run with the context's device current and its primary
-// context bound to the calling thread - cudaSetDevice does both; a host thread that has not
-// used the CUDA runtime yet has no context, and the driver's tensor-map encoder then fails -
-// and give the thread its previous device back when they return.
-struct DeviceGuard {
-    int prev = -1;
-    cudaError_t err = cudaSuccess;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        err = cudaSetDevice(dev);
-    }
-    ~DeviceGuard() {
-        int now = -1;
-        if (prev >= 0 && cudaGetDevice(&now) == cudaSuccess && now != prev) cudaSetDevice(prev);
-    }
-    DeviceGuard(const DeviceGuard &) = delete;
-    DeviceGuard &operator=(const DeviceGuard &) = delete;
-};
 
 // Row-major bf16 matrix [rows][cols] -> 2-D tensor map with a (64 x box_rows) box and
 // 128-byte swizzling; out-of-range elements read as zero.
