@@ -401,6 +401,62 @@ int rpd_quant_logits(const rpd_quant *head, const void *x, int x_type, int64_t x
 /* Free the head (no call on it may be running).  NULL is ignored. */
 void rpd_quant_destroy(rpd_quant *head);
 
+/* Drafted tokens checked against a target model, from given random numbers.  (The paper has no
+ * counterpart: rpd_step decides from one model's own confidence which positions to fill; this decides
+ * which of a sequence's drafted tokens - a draft model's, or a block that rpd_step committed - a
+ * second, autoregressive model would have drawn as well.)
+ *
+ * Sequence b has n = lengths[b] drafted tokens x_0 .. x_{n-1} and n + 1 rows of target logits, row i
+ * for the token behind x_{i-1}.  With p_i the softmax of row i at temperature T = temperature[b] over
+ * the allowed tokens, and q_i the softmax of the draft model's row i at the same temperature (without
+ * draft rows: 1 at x_i), draft i is accepted while
+ *     uniform[b][i] * q_i(x_i) < p_i(x_i).
+ * At the first rejection j the next token is drawn from the residual max(p_j - q_j, 0), after n
+ * acceptances from p_n; the accepted tokens and the next one are then distributed as if drawn from the
+ * target.  A token is drawn as argmax_v w(v) / noise[b][v] (the lowest v on a tie), which with
+ * exponential variates is a draw with the weights w.  T = 0 puts p_i at its largest logit (the lowest
+ * index on a tie): a draft is accepted where it is that token, and draft rows and random numbers are
+ * not read.  D = 0, or lengths of 0, is sampling.
+ *
+ * Sizes: B sequences, at most D drafts each, V tokens; 0 <= D <= 1024, 1 <= V <= 2^24 (larger, or
+ * more than 2^26 rows of logits: RPD_ERR_UNSUPPORTED).  B = 0 is a no-op. */
+typedef struct rpd_verify_args {
+    const void *target;         /* [B][D + 1][V] logits of `type`; rows behind a sequence's n + 1 are not read */
+    const void *draft;          /* [B][D][V] logits of `type`, or NULL */
+    const int32_t *tokens;      /* [B][D] (NULL if D = 0); one outside 0 .. V - 1 is rejected */
+    const int32_t *lengths;     /* [B] numbers of drafts, or NULL: D each */
+    const float *temperature;   /* [B] >= 0, or NULL: 1 each */
+    const uint32_t *allowed;    /* [B][D + 1][ceil(V / 32)] bits, 1 = allowed, bit v % 32 of word v / 32; or
+                                   NULL.  Logits of other tokens may hold anything */
+    const float *uniform;       /* [B][D] in [0, 1) */
+    const float *noise;         /* [B][V] exponential variates (>= 0; others never win) */
+    int32_t *out_accepted;      /* [B] accepted drafts */
+    int32_t *out_token;         /* [B][D + 1] the accepted drafts, the next token, then -1 */
+    int32_t *out_status;        /* [B] RPD_OK; or RPD_ERR_INVALID_ARGUMENT, with -1 for the next token, where
+                                   the sequence ends at a row without a distribution (no allowed finite
+                                   logit, or a NaN or +infinity among the allowed ones), or - nothing
+                                   accepted - n is not in 0 .. D, T is negative or NaN, or random numbers
+                                   that T > 0 needs are NULL */
+    float *out_prob;            /* [B][D] p_i(x_i), 0 behind the sequence's drafts; or NULL */
+    int64_t target_seq_stride;  /* elements between sequences and between rows; >= 0 (equal rows may be */
+    int64_t target_row_stride;  /* shared), the tokens of a row are contiguous */
+    int64_t draft_seq_stride;
+    int64_t draft_row_stride;
+    int64_t noise_stride;       /* elements between the sequences' variates */
+    int32_t type;               /* RPD_TYPE_* of both kinds of logits */
+    int32_t B, D, V;
+} rpd_verify_args;
+
+/* Device bytes of workspace that rpd_verify needs; -1 for negative sizes. */
+int64_t rpd_verify_workspace(int B, int D);
+
+/* Runs asynchronously on `stream` (a cudaStream_t of the device that holds `target`; NULL = legacy
+ * default).  Every buffer is device memory of that device; workspace: at least rpd_verify_workspace(B, D)
+ * bytes, 16-byte aligned, that no other call uses at the same time (its contents need no preparation).
+ * uniform (if D > 0) and noise may be NULL only where temperature is given and 0 throughout.  Outputs
+ * may not overlap the inputs. */
+int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Message of the last failing call on this host thread ("" if none). */
 const char *rpd_last_error(void);
 

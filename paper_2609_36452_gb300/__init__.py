@@ -20,6 +20,7 @@ __all__ = [
     "rpd_step_shard_partials", "rpd_step_shard_finish", "rpd_profile_enable", "rpd_kernel_times",
     "rpd_build_decode_loop", "rpd_build_decode_loop_batched", "rpd_decode_loop_launch", "rpd_decode_loop_destroy", "DecodeLoop",
     "rpd_quant_create", "rpd_quant_set_weights", "rpd_quant_workspace", "rpd_quant_logits", "rpd_quant_destroy", "QuantHead",
+    "rpd_verify_workspace", "rpd_verify", "verify", "RpdVerifyArgs",
     "rpd_destroy", "rpd_last_error", "rpd_version", "Rpd", "RULE_PROFILES", "KERNEL_NAMES",
 ]
 
@@ -63,6 +64,14 @@ class RpdDebug(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "conf", "entropy", "persist", "drop", "stability", "candidate", "layer_argmax",
         "layer_pmax")]
+
+
+class RpdVerifyArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "target", "draft", "tokens", "lengths", "temperature", "allowed", "uniform", "noise",
+        "out_accepted", "out_token", "out_status", "out_prob")] + [(n, ctypes.c_int64) for n in (
+            "target_seq_stride", "target_row_stride", "draft_seq_stride", "draft_row_stride", "noise_stride")] + [
+        (n, ctypes.c_int32) for n in ("type", "B", "D", "V")]
 
 
 STATS_FIELDS = [f[0] for f in RpdStats._fields_]
@@ -135,6 +144,8 @@ def _load():
         "rpd_quant_logits": (i32, [vp, vp, i32, ctypes.c_int64, i32, vp, f32, vp, i32, ctypes.c_int64,
                                    vp, ctypes.c_int64, vp]),
         "rpd_quant_destroy": (None, [vp]),
+        "rpd_verify_workspace": (ctypes.c_int64, [i32, i32]),
+        "rpd_verify": (i32, [ctypes.POINTER(RpdVerifyArgs), vp, ctypes.c_int64, vp]),
         "rpd_destroy": (None, [vp]),
         "rpd_last_error": (ctypes.c_char_p, []),
         "rpd_version": (ctypes.c_char_p, []),
@@ -178,6 +189,8 @@ rpd_quant_set_weights = lib.rpd_quant_set_weights
 rpd_quant_workspace = lib.rpd_quant_workspace
 rpd_quant_logits = lib.rpd_quant_logits
 rpd_quant_destroy = lib.rpd_quant_destroy
+rpd_verify_workspace = lib.rpd_verify_workspace
+rpd_verify = lib.rpd_verify
 rpd_destroy = lib.rpd_destroy
 rpd_last_error = lib.rpd_last_error
 rpd_version = lib.rpd_version
@@ -535,3 +548,49 @@ class QuantHead:
         pw = _arg(workspace, "workspace", "uint8") if workspace is not None else None
         _check(rpd_quant_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw,
                                 workspace.numel() if workspace is not None else 0, _stream(self.device)))
+
+
+def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, out_prob=None, draft=None,
+           lengths=None, temperature=None, allowed=None, workspace=None):
+    """Which drafted tokens a target model accepts, and the token that follows them (rpd_verify).
+
+    target [B][D + 1][V] and draft [B][D][V] (None: the drafts were chosen outright) are logits in
+    bf16, fp16 or float32 whose rows may lie apart; tokens [B][D] int32; uniform [B][D] and noise [B][V]
+    float32, given uniform and exponential variates (None where every temperature is 0); lengths [B]
+    int32 and temperature [B] float32 (None: D and 1); allowed [B][D + 1][ceil(V / 32)] int32 bit masks.
+    Outputs: out_accepted [B], out_token [B][D + 1], out_status [B] int32 and out_prob [B][D] float32.
+    Runs on the current stream of the logits' device.  ``workspace``: a uint8 CUDA tensor of
+    rpd_verify_workspace bytes (allocated if None)."""
+    if getattr(target, "dim", None) is None or target.dim() != 3 or target.shape[1] < 1:
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, "target: a tensor of [B][D + 1][V] logits is required")
+    B, D, V = target.shape[0], target.shape[1] - 1, target.shape[2]
+    logits = ("bfloat16", "float16", "float32")
+    a = RpdVerifyArgs()
+    a.B, a.D, a.V = B, D, V
+    a.target, a.type, st = _rows_arg(target, "target", logits, (B, D + 1, V))
+    a.target_seq_stride, a.target_row_stride = st[0], st[1]
+    if draft is not None:
+        a.draft, _, st = _rows_arg(draft, "draft", (str(target.dtype)[6:],), (B, D, V))
+        a.draft_seq_stride, a.draft_row_stride = st[0], st[1]
+    if noise is not None:
+        a.noise, _, st = _rows_arg(noise, "noise", ("float32",), (B, V))
+        a.noise_stride = st[0]
+    a.tokens = _arg(tokens, "tokens", "int32", B * D)
+    words = (V + 31) // 32
+    for name, t, dtype, numel in (("uniform", uniform, "float32", B * D), ("lengths", lengths, "int32", B),
+                                  ("temperature", temperature, "float32", B),
+                                  ("allowed", allowed, "int32", B * (D + 1) * words),
+                                  ("out_prob", out_prob, "float32", B * D)):
+        if t is not None:
+            setattr(a, name, _arg(t, name, dtype, numel))
+    a.out_accepted = _arg(out_accepted, "out_accepted", "int32", B)
+    a.out_token = _arg(out_token, "out_token", "int32", B * (D + 1))
+    a.out_status = _arg(out_status, "out_status", "int32", B)
+    _same_device(target.device, tokens=tokens, uniform=uniform, noise=noise, out_accepted=out_accepted,
+                 out_token=out_token, out_status=out_status, out_prob=out_prob, draft=draft, lengths=lengths,
+                 temperature=temperature, allowed=allowed, workspace=workspace)
+    if workspace is None:
+        import torch
+        workspace = torch.empty(rpd_verify_workspace(B, D), dtype=torch.uint8, device=target.device)
+    _check(rpd_verify(ctypes.byref(a), _arg(workspace, "workspace", "uint8"), workspace.numel(),
+                      _stream(target.device)))
