@@ -360,11 +360,12 @@ void rpd_destroy(rpd_ctx *ctx);
  *
  * with u = x and rho = 1, or, with a gain g, the readout's normalisation as rpd_step applies it:
  * u = g * x rounded to the type of x, rho_r = (mean_k x[r][k]^2 + eps)^(-1/2) applied after the
- * sum.  Products and sums are fp32 (q - z and the scales enter exactly), and the logits are rounded
- * once, to the type of `out`.  Inputs must be finite.
+ * sum.  Codes, zero points and scales enter exactly, u with at least 24 binary places below the row's
+ * largest (a smaller element is off by at most 2^-35 of that); products and sums are fp32, and the logits
+ * are rounded once, to the type of `out`.  Inputs must be finite.
  *
  * rpd_quant_create: a head of d columns and V rows with groups of 32, 64 or 128 columns (others:
- * RPD_ERR_UNSUPPORTED) on the current device; 1 <= d <= 65536, 1 <= V <= 2^24.  d need not be a
+ * RPD_ERR_UNSUPPORTED) on the current device; 1 <= d <= 32768, 1 <= V <= 2^24.  d need not be a
  * multiple of the group: the last group is then shorter.  NULL on failure. */
 typedef struct rpd_quant rpd_quant; /* opaque, owned by the library */
 rpd_quant *rpd_quant_create(int d, int V, int group);

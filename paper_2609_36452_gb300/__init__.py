@@ -222,6 +222,18 @@ def _arg(t, name: str, dtype: str, numel: int = None, cuda: bool = True):
     return _ptr(t)
 
 
+_torch_module = None
+
+
+def _torch():
+    """torch, imported by the first call that is given tensors."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 def _rows_arg(t, name: str, types, shape):
     """A CUDA tensor of the given shape whose innermost dimension is contiguous; its outer strides
     (in elements) are the caller's.  Returns (pointer, RPD_TYPE_* or None, strides)."""
@@ -232,23 +244,35 @@ def _rows_arg(t, name: str, types, shape):
     dtype = str(t.dtype)
     if dtype[6:] not in types:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: dtype must be {' or '.join(types)}, not {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     strides = t.stride()
-    if shape[-1] > 1 and strides[-1] != 1 and t.numel():
+    if strides[-1] != 1 and shape[-1] > 1 and t.numel():
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: its innermost dimension must be contiguous")
-    return _ptr(t), ELEMENT_TYPES.get(dtype), strides
+    return t.data_ptr(), ELEMENT_TYPES.get(dtype), strides
 
 
-def _stream(device):
-    import torch
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+def _dense_arg(t, name: str, dtype: str, numel: int, device: int):
+    """The address of a contiguous CUDA tensor of one device; the same checks as _arg and
+    _same_device, in the order that is quickest for a good argument."""
+    if (type(t) is _torch().Tensor and t.get_device() == device and t.dtype is getattr(_torch_module, dtype)
+            and t.is_contiguous() and t.numel() == numel):
+        return t.data_ptr()
+    _arg(t, name, dtype, numel)
+    _same_device(device, **{name: t})
+    return t.data_ptr()
 
 
-def _same_device(device, **tensors):
+def _same_device(device: int, **tensors):
     for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: on {t.device}, expected {device}")
+        if t is not None and t.get_device() != device:
+            raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: on {t.device}, expected device {device}")
+
+
+def _stream(device: int):
+    """The device's current stream (as torch.cuda.current_stream(device).cuda_stream, without the
+    object around it)."""
+    return _torch()._C._cuda_getCurrentRawStream(device)
 
 
 _DEBUG_DTYPES = {"conf": "float32", "entropy": "float32", "persist": "int32", "drop": "float32",
@@ -502,8 +526,7 @@ class QuantHead:
         if not h:
             raise RpdError(RPD_ERR_INVALID_ARGUMENT, rpd_last_error().decode())
         self.handle = ctypes.c_void_p(h)
-        import torch
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.device = _torch().cuda.current_device()
 
     def close(self):
         if getattr(self, "handle", None):
@@ -524,10 +547,9 @@ class QuantHead:
         kind = str(getattr(scales, "dtype", None))[6:]
         if kind not in ("bfloat16", "float16"):
             raise RpdError(RPD_ERR_INVALID_ARGUMENT, "scales: dtype must be bfloat16 or float16")
-        args = (_arg(codes, "codes", "uint8", self.V * ((self.d + 1) // 2)),
-                _arg(scales, "scales", kind, self.V * groups),
-                _arg(zeros, "zeros", "uint8", self.V * groups) if zeros is not None else None)
-        _same_device(self.device, codes=codes, scales=scales, zeros=zeros)
+        args = (_dense_arg(codes, "codes", "uint8", self.V * ((self.d + 1) // 2), self.device),
+                _dense_arg(scales, "scales", kind, self.V * groups, self.device),
+                _dense_arg(zeros, "zeros", "uint8", self.V * groups, self.device) if zeros is not None else None)
         _check(rpd_quant_set_weights(self.handle, args[0], args[1], ELEMENT_TYPES[str(scales.dtype)], args[2],
                                      _stream(self.device)))
 
@@ -539,15 +561,14 @@ class QuantHead:
         rows = x.shape[0] if hasattr(x, "shape") and len(x.shape) == 2 else 0
         px, xt, xs = _rows_arg(x, "x", ("bfloat16", "float16"), (rows, self.d))
         po, ot, os_ = _rows_arg(out, "out", ("bfloat16", "float16", "float32"), (rows, self.V))
-        pg = _arg(gain, "gain", str(x.dtype)[6:], self.d) if gain is not None else None
-        _same_device(self.device, x=x, out=out, gain=gain, workspace=workspace)
+        _same_device(self.device, x=x, out=out)
+        pg = _dense_arg(gain, "gain", str(x.dtype)[6:], self.d, self.device) if gain is not None else None
         need = rpd_quant_workspace(self.handle, rows)
         if need > 0 and workspace is None:
-            import torch
-            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-        pw = _arg(workspace, "workspace", "uint8") if workspace is not None else None
+            workspace = _torch().empty(need, dtype=_torch_module.uint8, device=x.device)
+        pw = _dense_arg(workspace, "workspace", "uint8", workspace.numel(), self.device) if workspace is not None else None
         _check(rpd_quant_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw,
-                                workspace.numel() if workspace is not None else 0, _stream(self.device)))
+                                need if pw is None else workspace.numel(), _stream(self.device)))
 
 
 def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, out_prob=None, draft=None,
@@ -569,28 +590,30 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
     a.B, a.D, a.V = B, D, V
     a.target, a.type, st = _rows_arg(target, "target", logits, (B, D + 1, V))
     a.target_seq_stride, a.target_row_stride = st[0], st[1]
+    dev = target.get_device()
     if draft is not None:
         a.draft, _, st = _rows_arg(draft, "draft", (str(target.dtype)[6:],), (B, D, V))
         a.draft_seq_stride, a.draft_row_stride = st[0], st[1]
+        _same_device(dev, draft=draft)
     if noise is not None:
         a.noise, _, st = _rows_arg(noise, "noise", ("float32",), (B, V))
         a.noise_stride = st[0]
-    a.tokens = _arg(tokens, "tokens", "int32", B * D)
-    words = (V + 31) // 32
-    for name, t, dtype, numel in (("uniform", uniform, "float32", B * D), ("lengths", lengths, "int32", B),
-                                  ("temperature", temperature, "float32", B),
-                                  ("allowed", allowed, "int32", B * (D + 1) * words),
-                                  ("out_prob", out_prob, "float32", B * D)):
-        if t is not None:
-            setattr(a, name, _arg(t, name, dtype, numel))
-    a.out_accepted = _arg(out_accepted, "out_accepted", "int32", B)
-    a.out_token = _arg(out_token, "out_token", "int32", B * (D + 1))
-    a.out_status = _arg(out_status, "out_status", "int32", B)
-    _same_device(target.device, tokens=tokens, uniform=uniform, noise=noise, out_accepted=out_accepted,
-                 out_token=out_token, out_status=out_status, out_prob=out_prob, draft=draft, lengths=lengths,
-                 temperature=temperature, allowed=allowed, workspace=workspace)
+        _same_device(dev, noise=noise)
+    a.tokens = _dense_arg(tokens, "tokens", "int32", B * D, dev)
+    if uniform is not None:
+        a.uniform = _dense_arg(uniform, "uniform", "float32", B * D, dev)
+    if lengths is not None:
+        a.lengths = _dense_arg(lengths, "lengths", "int32", B, dev)
+    if temperature is not None:
+        a.temperature = _dense_arg(temperature, "temperature", "float32", B, dev)
+    if allowed is not None:
+        a.allowed = _dense_arg(allowed, "allowed", "int32", B * (D + 1) * ((V + 31) // 32), dev)
+    if out_prob is not None:
+        a.out_prob = _dense_arg(out_prob, "out_prob", "float32", B * D, dev)
+    a.out_accepted = _dense_arg(out_accepted, "out_accepted", "int32", B, dev)
+    a.out_token = _dense_arg(out_token, "out_token", "int32", B * (D + 1), dev)
+    a.out_status = _dense_arg(out_status, "out_status", "int32", B, dev)
     if workspace is None:
-        import torch
-        workspace = torch.empty(rpd_verify_workspace(B, D), dtype=torch.uint8, device=target.device)
-    _check(rpd_verify(ctypes.byref(a), _arg(workspace, "workspace", "uint8"), workspace.numel(),
-                      _stream(target.device)))
+        workspace = _torch().empty(rpd_verify_workspace(B, D), dtype=_torch_module.uint8, device=target.device)
+    _check(rpd_verify(a, _dense_arg(workspace, "workspace", "uint8", workspace.numel(), dev), workspace.numel(),
+                      _stream(dev)))

@@ -7,18 +7,21 @@
 // u = rn(g * x) in the activations' type and rho_r = (mean_k x^2 + eps)^-1/2, applied after the
 // sum, as the 16-bit head does it.
 //
-// Precision.  q - z is a whole number of at most 5 bits: exact in bf16 and fp16, and so is its product
-// with u in fp32.  A group's products are summed in fp32 by the tensor core, the sum is multiplied by
-// the scale and added to the row's running sum in fp32.  Scales are never rounded into the weights.
+// Precision.  Codes enter the tensor core as fp16 subnormals q 2^-24, which costs one AND for two of them
+// (a shift more for the upper four of a word), activations as fp16 numbers that a power of two a row has
+// brought into range (quant_internal.h: scale_u).  Products and sums of a group are fp32, the zero point's
+// part -z sum u is what the sum starts from, and a group's sum is multiplied by its scale and added to the
+// row's in fp32: nothing is rounded into the weights.
 //
-// What bounds it: reading the codes once.  One row of a 126464 x 4096 head is 259 MB of codes and 8 MB
-// of scales.  Dequantising on the way to the multipliers costs about 1.4 instructions a weight and lane
-// (shift, mask and bias in one LOP3, subtraction in pairs), 20 us of the device's issue slots.
+// What bounds it: reading the codes once (one row of a 126464 x 4096 head is 259 MB of codes and 8 MB of
+// scales: 39 us), if the instructions a code costs stay below.  As bf16 numbers 128 + q less 128 + z (three
+// instructions a pair, 87 for 512 bytes of codes in all) they took 66 us.
 //
 // k_quant_rows: up to 16 rows.  A warp multiplies tiles of 16 matrix rows (M of the m16n8k16 MMA) by 8
-// or 16 activation rows (N), so that a dequantised fragment is used for all of them from registers.  The
-// codes are stored in fragment order, 512 contiguous bytes for 16 rows x 64 columns, which every lane
-// reads as one 16-byte vector, several of them ahead.  A CTA owns a range of tiles and its warps
+// or 16 activation rows (N), so that a fragment of codes is used for all of them from registers.  The
+// codes are stored in fragment order, 512 contiguous bytes for 16 rows x 64 columns, which a warp copies
+// through a ring of its own in shared memory (asked for in registers instead, the copies in flight are
+// limited by the six scoreboards of a warp: 66 us again).  A CTA owns a range of tiles and its warps
 // divide the range's column blocks evenly, over tile borders: one tile's row sums then come from
 // several warps and are joined in shared memory in warp order.
 #include <cuda_bf16.h>
@@ -70,7 +73,7 @@ __global__ void k_quant_pack(const uint8_t *codes, uint4 *packed, int V, int d, 
 }
 
 // Scales (and zero points) in the order of the tiles: [tile][group][g][2] for rows g and g + 8.  With
-// zero points an entry is 32 bits: the scale, and the zero point in the upper half.
+// zero points an entry is 32 bits: the scale, and the zero point as a bf16 number in the upper half.
 template <bool kZeros>
 __global__ void k_quant_pack_scales(const uint16_t *scales, const uint8_t *zeros, void *packed, int V, int groups,
                                     int tiles, int padded_groups) {
@@ -85,7 +88,9 @@ __global__ void k_quant_pack_scales(const uint16_t *scales, const uint8_t *zeros
         const long long at = static_cast<long long>(v) * groups + grp;
         const uint32_t s = in ? scales[at] : 0u;
         if (kZeros)
-            static_cast<uint32_t *>(packed)[i] = s | (in ? static_cast<uint32_t>(zeros[at]) & 15u : 8u) << 16;
+            static_cast<uint32_t *>(packed)[i] =
+                s |
+                static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(in ? zeros[at] & 15 : 0))) << 16;
         else
             static_cast<uint16_t *>(packed)[i] = static_cast<uint16_t>(s);
     }
@@ -96,15 +101,7 @@ __global__ void k_quant_pack_scales(const uint16_t *scales, const uint8_t *zeros
 constexpr int kRowsWarps = 16;
 constexpr int kRowsThreads = 32 * kRowsWarps;
 
-__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1,
-                                          __nv_bfloat16) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
-        " {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
         " {%0, %1, %2, %3};"
@@ -112,33 +109,99 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The lane's part of the activations into shared memory: rows of u, `row_bytes` apart, zero beyond
-// column d, and the factors rho.  Every thread takes part; ends with a barrier.
-template <typename T>
-__device__ void stage_rows(const QuantParams &p, uint8_t *xs, int row_bytes, float *red, float *rho) {
+// cp.async: 16 bytes a lane, past L1; commit closes a group of copies, wait<N> returns once all but the
+// last N groups have landed.
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// The launch's activations in shared memory: rows of `row_bytes` as scale_u leaves them, zero beyond column
+// d; sums[group][n] of a group's elements times 2^-24 (rows rounded up to an even number); and what a
+// row's logits are multiplied with.  The warps divide the rows, or a row, evenly.  Ends with a barrier.
+struct RowsSmem {
+    uint8_t *x;
+    float *sums, *factor, *red;
+    int row_bytes, sum_rows;
+};
+
+// f(chunk index, u) for the chunks of 8 columns of a row that fall to this lane: 32 neighbouring chunks a
+// warp at a time, the lane's next ones asked for before the first is used.  Lanes beyond the last chunk
+// get zeros.
+template <typename T, typename F>
+__device__ __forceinline__ void for_chunks(const QuantParams &p, const T *x, int first, int step, const F &f) {
+    constexpr int kBatch = 4;
+    const int chunks = p.blocks * 8;
     const T *gain = static_cast<const T *>(p.gain);
-    const int chunks = p.blocks * 8;  // of 8 elements
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int r = 0; r < p.rows; ++r) {
-        const T *x = static_cast<const T *>(p.x) + r * p.x_stride;
-        float ss = 0.f;
-        for (int c = threadIdx.x; c < chunks; c += kRowsThreads) {
-            uint4 v = load_chunk(x, c * 8, p.d, p.x_vectors);
-            if (gain) ss += norm_chunk<T>(v, load_chunk(gain, c * 8, p.d, p.gain_vectors));
-            *reinterpret_cast<uint4 *>(xs + static_cast<size_t>(r) * row_bytes + c * 16) = v;
-        }
-        if (gain) {
+    for (int c0 = first; c0 < chunks; c0 += kBatch * step) {
+        uint4 v[kBatch], g[kBatch];
 #pragma unroll
-            for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            if (lane == 0) red[r * kRowsWarps + warp] = ss;
+        for (int j = 0; j < kBatch; ++j) {
+            const int c = c0 + j * step + (threadIdx.x & 31);
+            v[j] = g[j] = make_uint4(0, 0, 0, 0);
+            if (c < chunks) {
+                v[j] = load_chunk(x, c * 8, p.d, p.x_vectors);
+                if (gain) g[j] = load_chunk(gain, c * 8, p.d, p.gain_vectors);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (c0 + j * step < chunks) f(c0 + j * step + static_cast<int>(threadIdx.x & 31), v[j], g[j]);
+    }
+}
+
+template <typename T, int kGroup>
+__device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
+    const int chunks = p.blocks * 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int per_row = kRowsWarps;  // warps that share a row
+    while (per_row * p.rows > kRowsWarps && per_row > 1) per_row >>= 1;
+    const int part = warp % per_row;
+    for (int r = warp / per_row; r < p.rows; r += kRowsWarps / per_row) {
+        float ss = 0.f, top = 0.f;
+        for_chunks(p, static_cast<const T *>(p.x) + r * p.x_stride, part * 32, per_row * 32,
+                   [&](int, const uint4 &v, const uint4 &g) {
+                       float2 u[4];
+                       ss += make_u<T>(v, p.gain != nullptr, g, u);
+#pragma unroll
+                       for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(u[i].x), fabsf(u[i].y)));
+                   });
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        }
+        if (lane == 0) {
+            s.red[(r * kRowsWarps + part) * 2] = ss;
+            s.red[(r * kRowsWarps + part) * 2 + 1] = top;
         }
     }
     __syncthreads();
-    if (threadIdx.x < p.rows) {
-        float ss = 0.f;
-        if (gain)
-            for (int w = 0; w < kRowsWarps; ++w) ss += red[threadIdx.x * kRowsWarps + w];
-        rho[threadIdx.x] = gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f;
+    for (int r = warp / per_row; r < p.rows; r += kRowsWarps / per_row) {
+        float ss = 0.f, top = 0.f;
+        for (int w = 0; w < per_row; ++w) {
+            ss += s.red[(r * kRowsWarps + w) * 2];
+            top = fmaxf(top, s.red[(r * kRowsWarps + w) * 2 + 1]);
+        }
+        const int E = exponent_of(top);
+        if (part == 0 && lane == 0)
+            s.factor[r] = ldexpf(p.gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f, E);
+        uint8_t *xs = s.x + static_cast<size_t>(r) * s.row_bytes;
+        for_chunks(p, static_cast<const T *>(p.x) + r * p.x_stride, part * 32, per_row * 32,
+                   [&](int c, const uint4 &v, const uint4 &g) {
+                       float2 u[4];
+                       uint4 w;
+                       make_u<T>(v, p.gain != nullptr, g, u);
+                       float sum = scale_u(u, E, w);
+                       if (c < chunks) *reinterpret_cast<uint4 *>(xs + c * 16) = w;
+#pragma unroll
+                       for (int o = 1; o < kGroup / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                       if (c < chunks && c % (kGroup / 8) == 0) s.sums[c / (kGroup / 8) * s.sum_rows + r] = sum;
+                   });
     }
     __syncthreads();
 }
@@ -146,30 +209,45 @@ __device__ void stage_rows(const QuantParams &p, uint8_t *xs, int row_bytes, flo
 // A finished tile's logits: fragment element (g, 2t) of the MMA's result is matrix row g, activation 2t.
 template <int kN8>
 __device__ __forceinline__ void store_tile(const QuantParams &p, int tile, const float (&run)[kN8][4],
-                                           const float *rho, int g, int t) {
+                                           const float *factor, int g, int t) {
 #pragma unroll
     for (int n = 0; n < kN8; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = n * 8 + 2 * t + (i & 1), v = tile * kQuantTileRows + g + (i >> 1) * 8;
-            if (r < p.rows && v < p.V) store_out(p.out, p.out_type, r * p.out_stride + v, run[n][i] * rho[r]);
+            if (r < p.rows && v < p.V)
+                store_out(p.out, p.out_type, r * p.out_stride + v, run[n][i] * kRowFactor * factor[r]);
         }
 }
 
-template <typename T, int kGroup, int kN8, bool kZeros>
-__global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParams p) {
-    constexpr int kUnitBlocks = kGroup == 128 ? 2 : 1;  // 64-column blocks of a unit of work
-    constexpr int kUnitGroups = kGroup == 32 ? 2 : 1;
-    constexpr int kAhead = kGroup == 128 ? 4 : 6;       // units whose codes are in flight
-    typedef typename MetaVec<kZeros>::type Meta;        // scales (and zero points) of rows g and g + 8
+// Units (groups, or for groups of 32 columns two) that a warp copies and waits for at a time: 2 KB of codes.
+template <int kGroup, bool kZeros>
+struct RowsStage {
+    static constexpr int kUnitBlocks = kGroup == 128 ? 2 : 1;  // 64-column blocks of a unit of work
+    static constexpr int kUnitGroups = kGroup == 32 ? 2 : 1;
+    static constexpr int kUnits = 4 / kUnitBlocks;
+    static constexpr int kCodeBytes = 2048;
+    static constexpr int kMetaUnit = kUnitGroups * (kZeros ? 64 : 32);
+    static constexpr int kBytes = kCodeBytes + kUnits * kMetaUnit;
+};
+
+template <int kGroup, int kN8, bool kZeros, bool kF16>
+__global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParams p, const int depth) {
+    typedef RowsStage<kGroup, kZeros> Stage;
+    typedef typename MetaVec<kZeros>::type Meta;  // scales (and zero points) of rows g and g + 8
+    constexpr int kUnitBlocks = Stage::kUnitBlocks, kUnitGroups = Stage::kUnitGroups;
     extern __shared__ __align__(128) uint8_t smem[];
     float *join = reinterpret_cast<float *>(smem);  // [warp][4 kN8][lane]
-    float *red = join + kRowsWarps * 4 * kN8 * 32;
-    float *rho = red + 16 * kRowsWarps;
-    uint8_t *xs = reinterpret_cast<uint8_t *>(rho + 16);
-    // a row and 64 bytes: the two rows that a quarter of a warp reads at once lie in different banks
-    const int row_bytes = p.blocks * 128 + 64;
+    RowsSmem sm;
+    sm.red = join + kRowsWarps * 4 * kN8 * 32;
+    sm.factor = sm.red + 2 * 16 * kRowsWarps;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    uint8_t *ring = reinterpret_cast<uint8_t *>(sm.factor + 16) + warp * depth * Stage::kBytes;
+    sm.x = reinterpret_cast<uint8_t *>(sm.factor + 16) + kRowsWarps * depth * Stage::kBytes;
+    // a row and 64 bytes: the two rows that a quarter of a warp reads at once lie in different banks
+    sm.row_bytes = p.blocks * 128 + 64;
+    sm.sum_rows = (p.rows + 1) & ~1;
+    sm.sums = reinterpret_cast<float *>(sm.x + static_cast<size_t>(p.rows) * sm.row_bytes);
 
     pdl_trigger();
     // this CTA's tiles, this warp's units of them
@@ -178,24 +256,35 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     const int per_tile = p.blocks / kUnitBlocks;
     const int units = (tile1 - tile0) * per_tile;
     const int u0 = units * warp / kRowsWarps, u1 = units * (warp + 1) / kRowsWarps;
-    const uint4 *codes = p.codes + (static_cast<long long>(tile0) * p.blocks) * 32 + t * 8 + g;
-    const Meta *meta = static_cast<const Meta *>(p.meta) + static_cast<long long>(tile0) * p.groups * 8 + g;
-
-    uint4 code[kAhead][kUnitBlocks];
-    Meta m[kAhead][kUnitGroups];
-    auto fetch = [&](int slot, int u) {
-        if (u < u1) {
+    // Both streams are contiguous over the CTA's tiles.  A lane copies the vectors of codes that it reads.
+    const int place = (t * 8 + g) * 16;
+    const uint8_t *codes = reinterpret_cast<const uint8_t *>(p.codes) +
+                           (static_cast<long long>(tile0) * p.blocks + static_cast<long long>(u0) * kUnitBlocks) * 512 + place;
+    const uint8_t *meta = static_cast<const uint8_t *>(p.meta) +
+                          (static_cast<long long>(tile0) * per_tile + u0) * Stage::kMetaUnit + lane * 16;
+    const uint32_t ring_at = smem_u32(ring);
+    int ahead = u1 - u0;  // units that are not yet asked for
+    auto fetch = [&](int slot) {
+        if (ahead > 0) {
+            const uint32_t to = ring_at + slot * Stage::kBytes;
 #pragma unroll
-            for (int b = 0; b < kUnitBlocks; ++b) code[slot][b] = ld_stream(codes + static_cast<long long>(u * kUnitBlocks + b) * 32);
-#pragma unroll
-            for (int k = 0; k < kUnitGroups; ++k) m[slot][k] = __ldg(meta + static_cast<long long>(u * kUnitGroups + k) * 8);
+            for (int b = 0; b < 4; ++b)
+                if (b / kUnitBlocks < ahead) copy_async(to + b * 512 + place, codes + b * 512);
+            if (lane * 16 < min(ahead, Stage::kUnits) * Stage::kMetaUnit)
+                copy_async(to + Stage::kCodeBytes + lane * 16, meta);
+            codes += Stage::kCodeBytes;
+            meta += Stage::kUnits * Stage::kMetaUnit;
+            ahead -= Stage::kUnits;
         }
+        copy_commit();
     };
-#pragma unroll
-    for (int s = 0; s < kAhead; ++s) fetch(s, u0 + s);
+    for (int s = 0; s < depth - 1; ++s) fetch(s);
 
     pdl_wait();  // the weights were laid out long ago; the activations may be the predecessor's
-    stage_rows<T>(p, xs, row_bytes, red, rho);
+    if (p.x_type == RPD_TYPE_BF16)
+        stage_rows<__nv_bfloat16, kGroup>(p, sm);
+    else
+        stage_rows<__half, kGroup>(p, sm);
 
     float run[kN8][4];
 #pragma unroll
@@ -204,73 +293,91 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
         for (int i = 0; i < 4; ++i) run[n][i] = 0.f;
     int in_tile = u0 % per_tile, tile = tile0 + u0 / per_tile;
     bool head = in_tile != 0;  // the tile at hand was begun by an earlier warp
-    const uint8_t *xrow = xs + static_cast<size_t>(g) * row_bytes + t * 16;
+    // Lanes of activations beyond the last read the last one's elements: their columns of the result
+    // are never stored.
+    const uint8_t *xrow[kN8];
+    const float *srow[kN8];
+#pragma unroll
+    for (int n = 0; n < kN8; ++n) {
+        xrow[n] = sm.x + static_cast<size_t>(min(n * 8 + g, p.rows - 1)) * sm.row_bytes + t * 16;
+        srow[n] = sm.sums + min(n * 8 + 2 * t, sm.sum_rows - 2);
+    }
 
-    for (int u = u0; u < u1; u += kAhead) {
+    int slot = 0, refill = depth - 1;
+    for (int u = u0; u < u1; u += Stage::kUnits) {
+        if (depth >= 6)
+            copy_wait<4>();
+        else if (depth >= 4)
+            copy_wait<2>();
+        else
+            copy_wait<0>();
+        __syncwarp();  // every lane's copies are seen, and every lane is done with the slot before
+        fetch(refill);
+        const uint8_t *stage = ring + slot * Stage::kBytes;
+        refill = slot;
+        slot = slot + 1 == depth ? 0 : slot + 1;
+        const int count = min(Stage::kUnits, u1 - u);
+        for (int j = 0; j < count; ++j) {
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) {
-            if (u + s < u1) {
+            for (int k = 0; k < kUnitGroups; ++k) {
+                float s_lo, s_hi, z_lo, z_hi;
+                unpack_meta<kF16>(*(reinterpret_cast<const Meta *>(stage + Stage::kCodeBytes) +
+                                    (j * kUnitGroups + k) * 8 + g),
+                                  s_lo, s_hi, z_lo, z_hi);
+                float c[kN8][4];
 #pragma unroll
-                for (int k = 0; k < kUnitGroups; ++k) {
-                    float c[kN8][4];
+                for (int n = 0; n < kN8; ++n) {
+                    const float2 sum =
+                        *reinterpret_cast<const float2 *>(srow[n] + (in_tile * kUnitGroups + k) * sm.sum_rows);
+                    c[n][0] = -z_lo * sum.x;
+                    c[n][1] = -z_lo * sum.y;
+                    c[n][2] = -z_hi * sum.x;
+                    c[n][3] = -z_hi * sum.y;
+                }
+                // 32-column halves of this group: (block, half)
+#pragma unroll
+                for (int h = 0; h < kGroup / 32; ++h) {
+                    const int b = kGroup == 32 ? 0 : h >> 1, half = kGroup == 32 ? k : h & 1;
+                    const uint4 q = *reinterpret_cast<const uint4 *>(stage + (j * kUnitBlocks + b) * 512 + place);
+                    const uint32_t lo = half ? q.y : q.x, hi = half ? q.w : q.z;
+                    uint4 xv[kN8];
 #pragma unroll
                     for (int n = 0; n < kN8; ++n)
+                        xv[n] = *reinterpret_cast<const uint4 *>(xrow[n] + (in_tile * kUnitBlocks + b) * 128 +
+                                                                 half * 64);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) c[n][i] = 0.f;
-                    float s_lo, s_hi;
-                    uint32_t z_lo, z_hi;
-                    unpack_meta<T>(m[s][k], p.scale_f16, s_lo, s_hi, z_lo, z_hi);
-                    // 32-column halves of this group: (block, half)
-#pragma unroll
-                    for (int h = 0; h < kGroup / 32; ++h) {
-                        const int b = kGroup == 32 ? 0 : h >> 1, half = kGroup == 32 ? k : h & 1;
-                        const uint4 q = code[s][b];
-                        const uint32_t lo = half ? q.y : q.x, hi = half ? q.w : q.z;
-                        uint4 xv[kN8];
-#pragma unroll
-                        for (int n = 0; n < kN8; ++n) {
-                            xv[n] = make_uint4(0, 0, 0, 0);
-                            if (n * 8 + g < p.rows)
-                                xv[n] = *reinterpret_cast<const uint4 *>(
-                                    xrow + static_cast<size_t>(n) * 8 * row_bytes +
-                                    (in_tile * kUnitBlocks + b) * 128 + half * 64);
-                        }
-#pragma unroll
-                        for (int step = 0; step < 2; ++step) {
-                            const uint32_t a[4] = {dequant_pair<T>(lo, 2 * step, z_lo), dequant_pair<T>(hi, 2 * step, z_hi),
-                                                   dequant_pair<T>(lo, 2 * step + 1, z_lo),
-                                                   dequant_pair<T>(hi, 2 * step + 1, z_hi)};
-#pragma unroll
-                            for (int n = 0; n < kN8; ++n)
-                                mma_16816(c[n], a, step ? xv[n].z : xv[n].x, step ? xv[n].w : xv[n].y, T());
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < kN8; ++n) {
-                        run[n][0] = fmaf(c[n][0], s_lo, run[n][0]);
-                        run[n][1] = fmaf(c[n][1], s_lo, run[n][1]);
-                        run[n][2] = fmaf(c[n][2], s_hi, run[n][2]);
-                        run[n][3] = fmaf(c[n][3], s_hi, run[n][3]);
-                    }
-                }
-                fetch(s, u + s + kAhead);
-                if (++in_tile == per_tile) {  // the tile's last columns
-                    if (head) {
+                    for (int step = 0; step < 2; ++step) {
+                        const uint32_t a[4] = {code_pair(lo, 2 * step), code_pair(hi, 2 * step),
+                                               code_pair(lo, 2 * step + 1), code_pair(hi, 2 * step + 1)};
 #pragma unroll
                         for (int n = 0; n < kN8; ++n)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) join[((warp * kN8 + n) * 4 + i) * 32 + lane] = run[n][i];
-                    } else {
-                        store_tile<kN8>(p, tile, run, rho, g, t);
+                            mma_16816(c[n], a, step ? xv[n].z : xv[n].x, step ? xv[n].w : xv[n].y);
                     }
-                    head = false;
-                    in_tile = 0;
-                    ++tile;
+                }
+#pragma unroll
+                for (int n = 0; n < kN8; ++n) {
+                    run[n][0] = fmaf(c[n][0], s_lo, run[n][0]);
+                    run[n][1] = fmaf(c[n][1], s_lo, run[n][1]);
+                    run[n][2] = fmaf(c[n][2], s_hi, run[n][2]);
+                    run[n][3] = fmaf(c[n][3], s_hi, run[n][3]);
+                }
+            }
+            if (++in_tile == per_tile) {  // the tile's last columns
+                if (head) {
 #pragma unroll
                     for (int n = 0; n < kN8; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) run[n][i] = 0.f;
+                        for (int i = 0; i < 4; ++i) join[((warp * kN8 + n) * 4 + i) * 32 + lane] = run[n][i];
+                } else {
+                    store_tile<kN8>(p, tile, run, sm.factor, g, t);
                 }
+                head = false;
+                in_tile = 0;
+                ++tile;
+#pragma unroll
+                for (int n = 0; n < kN8; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) run[n][i] = 0.f;
             }
         }
     }
@@ -290,40 +397,47 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 #pragma unroll
                 for (int i = 0; i < 4; ++i) run[n][i] += join[((w * kN8 + n) * 4 + i) * 32 + lane];
         }
-        store_tile<kN8>(p, tile, run, rho, g, t);
+        store_tile<kN8>(p, tile, run, sm.factor, g, t);
     }
 }
 
 constexpr int kRowsMax = 16;                 // activation rows of a launch
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 
-size_t rows_smem(int n8, int rows, int blocks) {
-    return static_cast<size_t>(kRowsWarps) * 4 * n8 * 32 * 4 + 16 * kRowsWarps * 4 + 16 * 4 +
-           static_cast<size_t>(rows) * (blocks * 128 + 64);
+// Shared memory besides the ring of codes.
+size_t rows_smem(int n8, int rows, int blocks, int groups) {
+    return (static_cast<size_t>(kRowsWarps) * 4 * n8 * 32 + 2 * 16 * kRowsWarps + 16) * 4 +
+           static_cast<size_t>(rows) * (blocks * 128 + 64) + static_cast<size_t>((rows + 1) & ~1) * groups * 4;
 }
 
-template <typename T, int kGroup, int kN8, bool kZeros>
+constexpr int kRowsRing = kRowsWarps * 2 * (2048 + 8 * 64);  // its least: two stages of any kind a warp
+
+template <int kGroup, int kN8, bool kZeros, bool kF16>
 cudaError_t launch_rows(const QuantParams &p, int num_sms, cudaStream_t s) {
-    void (*kernel)(QuantParams) = k_quant_rows<T, kGroup, kN8, kZeros>;
+    void (*kernel)(QuantParams, int) = k_quant_rows<kGroup, kN8, kZeros, kF16>;
     // (cheap, and per device: set on every call)
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(std::min(num_sms, p.row_tiles)), dim3(kRowsThreads),
-                      rows_smem(kN8, p.rows, p.blocks), s, p);
+    const size_t fixed = rows_smem(kN8, p.rows, p.blocks, p.groups);
+    const int stage = kRowsWarps * RowsStage<kGroup, kZeros>::kBytes;
+    const int fits = static_cast<int>((kRowsSmem - fixed) / stage);
+    const int depth = fits >= 6 ? 6 : fits >= 4 ? 4 : 2;
+    return launch_pdl(kernel, dim3(std::min(num_sms, p.row_tiles)), dim3(kRowsThreads), fixed + depth * stage, s, p,
+                      depth);
 }
 
-template <typename T, int kGroup>
-cudaError_t launch_rows_group(const QuantParams &p, bool zeros, int num_sms, cudaStream_t s) {
-    if (p.rows <= 8)
-        return zeros ? launch_rows<T, kGroup, 1, true>(p, num_sms, s) : launch_rows<T, kGroup, 1, false>(p, num_sms, s);
-    return zeros ? launch_rows<T, kGroup, 2, true>(p, num_sms, s) : launch_rows<T, kGroup, 2, false>(p, num_sms, s);
+template <int kGroup, int kN8>
+cudaError_t launch_rows_scales(const QuantParams &p, bool zeros, bool f16, int num_sms, cudaStream_t s) {
+    if (f16)
+        return zeros ? launch_rows<kGroup, kN8, true, true>(p, num_sms, s) : launch_rows<kGroup, kN8, false, true>(p, num_sms, s);
+    return zeros ? launch_rows<kGroup, kN8, true, false>(p, num_sms, s) : launch_rows<kGroup, kN8, false, false>(p, num_sms, s);
 }
 
-template <typename T>
-cudaError_t launch_rows_type(const QuantParams &p, int group, bool zeros, int num_sms, cudaStream_t s) {
-    return group == 32   ? launch_rows_group<T, 32>(p, zeros, num_sms, s)
-           : group == 64 ? launch_rows_group<T, 64>(p, zeros, num_sms, s)
-                         : launch_rows_group<T, 128>(p, zeros, num_sms, s);
+template <int kN8>
+cudaError_t launch_rows_group(const QuantParams &p, int group, bool zeros, bool f16, int num_sms, cudaStream_t s) {
+    return group == 32   ? launch_rows_scales<32, kN8>(p, zeros, f16, num_sms, s)
+           : group == 64 ? launch_rows_scales<64, kN8>(p, zeros, f16, num_sms, s)
+                         : launch_rows_scales<128, kN8>(p, zeros, f16, num_sms, s);
 }
 
 }  // namespace
@@ -470,7 +584,7 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.row_tiles = q->row_tiles;
     p.blocks = q->blocks;
     p.groups = q->groups;
-    p.scale_f16 = q->scale_f16 ? 1 : 0;
+    p.x_type = x_type;
     p.d = q->d;
     p.V = q->V;
     p.gain = gain;
@@ -481,16 +595,16 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.out_stride = out_stride;
     p.out_type = out_type;
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
-    // as many rows a launch as their activations fit into shared memory (at d = 65536 it is one)
+    // as many rows a launch as their activations fit into shared memory (at d = 32768 it is one)
     int most = kRowsMax;
-    while (rows_smem(2, most, q->blocks) > kRowsSmem) --most;
+    while (rows_smem(most > 8 ? 2 : 1, most, q->blocks, q->groups) + kRowsRing > kRowsSmem) --most;
     for (int r = 0; r < rows; r += most) {
         p.rows = std::min(most, rows - r);
         p.x = static_cast<const uint16_t *>(x) + r * x_stride;
         p.out = static_cast<char *>(out) + r * out_stride * type_size(out_type);
-        const cudaError_t e = x_type == RPD_TYPE_BF16
-                                  ? launch_rows_type<__nv_bfloat16>(p, q->group, q->zeros, q->num_sms, s)
-                                  : launch_rows_type<__half>(p, q->group, q->zeros, q->num_sms, s);
+        const cudaError_t e =
+            p.rows <= 8 ? launch_rows_group<1>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s)
+                        : launch_rows_group<2>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s);
         if (e != cudaSuccess) return op_cuda_fail(e, "4-bit head launch");
     }
     return RPD_OK;

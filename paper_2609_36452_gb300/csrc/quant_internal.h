@@ -10,7 +10,7 @@
 
 namespace rpd {
 
-constexpr int kQuantMaxD = 65536;       // a row of activations fits a CTA's shared memory
+constexpr int kQuantMaxD = 32768;       // a row of activations fits a CTA's shared memory
 constexpr int kQuantMaxV = 1 << 24;
 constexpr int kQuantTileRows = 16;      // matrix rows of a tile of the packed codes
 constexpr int kQuantPadTiles = 8;       // tiles are padded to a multiple of this many (128 rows)
@@ -21,7 +21,6 @@ struct QuantParams {
     int row_tiles;       // tiles of 16 matrix rows that hold a row
     int blocks;          // 64-column blocks of a row, a whole number of groups
     int groups;          // groups of a row, padding included
-    int scale_f16;       // the scales are fp16, else bf16
     int d, V;
     const void *x;       // [rows] rows, x_stride elements apart
     const void *gain;    // [d] or null
@@ -34,10 +33,6 @@ struct QuantParams {
     int out_type;
 };
 
-constexpr uint32_t kBiasBf16 = 0x43004300u;  // 128: adding q in 0..15 is setting its lowest four bits
-constexpr uint32_t kBiasHalf = 0x64006400u;  // 1024, likewise
-constexpr uint32_t kZeroDefault = 0x00080008u;
-
 template <bool kZeros>
 struct MetaVec {
     typedef uint32_t type;  // two 16-bit scales
@@ -47,62 +42,36 @@ struct MetaVec<true> {
     typedef uint2 type;  // scale and zero point of a row in each word
 };
 
-// Codes are read once a call: their lines are not kept in L1.
-__device__ __forceinline__ uint4 ld_stream(const uint4 *p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p));
-    return v;
+template <bool kF16>
+__device__ __forceinline__ float scale_low(uint32_t word) {
+    return kF16 ? __low2float(*reinterpret_cast<const __half2 *>(&word)) : __uint_as_float(word << 16);
+}
+template <bool kF16>
+__device__ __forceinline__ float scale_high(uint32_t word) {
+    return kF16 ? __high2float(*reinterpret_cast<const __half2 *>(&word)) : __uint_as_float(word & 0xFFFF0000u);
 }
 
-__device__ __forceinline__ float scale_value(uint32_t bits16, int f16) {
-    return f16 ? __half2float(__ushort_as_half(static_cast<unsigned short>(bits16)))
-               : __uint_as_float(bits16 << 16);
+// Scales of rows g and g + 8 of a tile, and their zero points (8 where none are stored).  A stored zero
+// point is a bf16 number in the upper half of its row's word.
+template <bool kF16>
+__device__ __forceinline__ void unpack_meta(uint32_t m, float &s_lo, float &s_hi, float &z_lo, float &z_hi) {
+    s_lo = scale_low<kF16>(m);
+    s_hi = scale_high<kF16>(m);
+    z_lo = z_hi = 8.f;
+}
+template <bool kF16>
+__device__ __forceinline__ void unpack_meta(uint2 m, float &s_lo, float &s_hi, float &z_lo, float &z_hi) {
+    s_lo = scale_low<kF16>(m.x);
+    s_hi = scale_low<kF16>(m.y);
+    z_lo = __uint_as_float(m.x & 0xFFFF0000u);
+    z_hi = __uint_as_float(m.y & 0xFFFF0000u);
 }
 
-template <typename T>
-constexpr uint32_t quant_bias() {
-    return kBiasBf16;
-}
-template <>
-constexpr uint32_t quant_bias<__half>() {
-    return kBiasHalf;
-}
-
-// Scales of rows g and g + 8 of a tile, and their zero points with the bias of the dequantisation.
-template <typename T>
-__device__ __forceinline__ void unpack_meta(uint32_t m, int f16, float &s_lo, float &s_hi, uint32_t &z_lo,
-                                            uint32_t &z_hi) {
-    s_lo = scale_value(m & 0xFFFFu, f16);
-    s_hi = scale_value(m >> 16, f16);
-    z_lo = z_hi = quant_bias<T>() | kZeroDefault;
-}
-template <typename T>
-__device__ __forceinline__ void unpack_meta(uint2 m, int f16, float &s_lo, float &s_hi, uint32_t &z_lo,
-                                            uint32_t &z_hi) {
-    s_lo = scale_value(m.x & 0xFFFFu, f16);
-    s_hi = scale_value(m.y & 0xFFFFu, f16);
-    z_lo = quant_bias<T>() | (m.x >> 16) * 0x00010001u;
-    z_hi = quant_bias<T>() | (m.y >> 16) * 0x00010001u;
-}
-
-// Two neighbouring columns (pair i of a word) of the codes as q - z in the activations' type; exact.
-template <typename T>
-__device__ __forceinline__ uint32_t dequant_pair(uint32_t word, int i, uint32_t bias_zero);
-template <>
-__device__ __forceinline__ uint32_t dequant_pair<__nv_bfloat16>(uint32_t word, int i, uint32_t bias_zero) {
-    const uint32_t v = ((word >> (4 * i)) & 0x000F000Fu) | kBiasBf16;
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v),
-                                     *reinterpret_cast<const __nv_bfloat162 *>(&bias_zero));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-template <>
-__device__ __forceinline__ uint32_t dequant_pair<__half>(uint32_t word, int i, uint32_t bias_zero) {
-    const uint32_t v = ((word >> (4 * i)) & 0x000F000Fu) | kBiasHalf;
-    const __half2 r =
-        __hsub2(*reinterpret_cast<const __half2 *>(&v), *reinterpret_cast<const __half2 *>(&bias_zero));
-    return *reinterpret_cast<const uint32_t *>(&r);
+// Pair i (columns 2i, 2i + 1) of a word of codes as two fp16 numbers: masked in place, they are the
+// subnormals q 2^-24 (pairs 0 and 2) and q 2^-20 (1 and 3) - exact, and for the tensor core numbers like any
+// others.  Activations of the odd pairs carry the missing 2^-4.
+__device__ __forceinline__ uint32_t code_pair(uint32_t word, int i) {
+    return (i < 2 ? word : word >> 8) & (i & 1 ? 0x00F000F0u : 0x000F000Fu);
 }
 
 // Elements [col, col + 8) of a row of d 16-bit elements, zero beyond its end.
@@ -125,31 +94,55 @@ __device__ __forceinline__ float2 pair_value(uint32_t v, __nv_bfloat16) {
 __device__ __forceinline__ float2 pair_value(uint32_t v, __half) {
     return __half22float2(*reinterpret_cast<const __half2 *>(&v));
 }
-__device__ __forceinline__ uint32_t pair_round(float2 f, __nv_bfloat16) {
-    const __nv_bfloat162 r = __floats2bfloat162_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t *>(&r);
+__device__ __forceinline__ float2 pair_round(float2 f, __nv_bfloat16) {
+    return __bfloat1622float2(__floats2bfloat162_rn(f.x, f.y));
 }
-__device__ __forceinline__ uint32_t pair_round(float2 f, __half) {
-    const __half2 r = __floats2half2_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
+__device__ __forceinline__ float2 pair_round(float2 f, __half) { return __half22float2(__floats2half2_rn(f.x, f.y)); }
 
-// v = rn(v * gain), returning the sum of v^2 before: the operand of a readout with a norm is
-// rounded to the activations' type (the product of two such numbers is exact in fp32), the factor rho is
-// not.
+// Eight columns of u from those of x, with a gain rn(g x): the operand of a readout with a norm is rounded to
+// the activations' type (the product of two such numbers is exact in fp32), its factor rho is not.  Returns
+// the sum of x^2.
 template <typename T>
-__device__ __forceinline__ float norm_chunk(uint4 &v, const uint4 &gain) {
-    uint32_t *w = reinterpret_cast<uint32_t *>(&v);
-    const uint32_t *gw = reinterpret_cast<const uint32_t *>(&gain);
+__device__ __forceinline__ float make_u(const uint4 &x, bool has_gain, const uint4 &gain, float2 (&u)[4]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w}, gw[4] = {gain.x, gain.y, gain.z, gain.w};
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 x = pair_value(w[i], T()), gf = pair_value(gw[i], T());
-        ss = fmaf(x.x, x.x, fmaf(x.y, x.y, ss));
-        w[i] = pair_round(make_float2(x.x * gf.x, x.y * gf.y), T());
+        u[i] = pair_value(w[i], T());
+        if (has_gain) {
+            const float2 gf = pair_value(gw[i], T());
+            ss = fmaf(u[i].x, u[i].x, fmaf(u[i].y, u[i].y, ss));
+            u[i] = pair_round(make_float2(u[i].x * gf.x, u[i].y * gf.y), T());
+        }
     }
     return ss;
 }
+
+// The power of two at or below x (1 for 0).
+__device__ __forceinline__ int exponent_of(float x) { return x > 0.f ? ilogbf(x) : 0; }
+
+// Activations as the tensor core gets them: u 2^(14 - E) in fp16, E the exponent of the row's largest u, and
+// the odd pairs 2^-4 of that.  Exact from 2^-24 of the largest element on; a smaller one is off by at
+// most 2^-35 of the largest.  Returns the sum of the eight elements as they then are, times 2^-24.
+__device__ __forceinline__ float scale_u(const float2 (&u)[4], int E, uint4 &out) {
+    const int e = 14 - E;  // in two factors: the power itself may lie outside fp32
+    const float f0 = ldexpf(1.f, e / 2), f1 = ldexpf(1.f, e - e / 2);
+    uint32_t w[4];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float f = i & 1 ? f1 * 0.0625f : f1;
+        const __half2 h = __floats2half2_rn(u[i].x * f0 * f, u[i].y * f0 * f);
+        const float2 v = __half22float2(h);
+        sum += (v.x + v.y) * (i & 1 ? 16.f : 1.f);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+    out = make_uint4(w[0], w[1], w[2], w[3]);
+    return sum * 0x1p-24f;
+}
+
+// What a row's sums are multiplied with, in two factors: 2^10 and 2^E rho.
+constexpr float kRowFactor = 1024.f;
 
 __device__ __forceinline__ void store_out(void *out, int type, long long at, float v) {
     if (type == RPD_TYPE_F32)

@@ -1,12 +1,13 @@
 """The 4-bit head (rpd_quant_*): refusals (no GPU), and its logits against the definition in 64 bits.
 
-Tolerance.  One logit is a sum of d products s (q - z) u.  The kernels multiply exactly, sum a group's
-products in fp32 in steps of 16 columns (the tensor core may cut its addends off instead of rounding
-them: 2^-22 of the sum of their sizes for every step), add the groups' sums in fp32 and join at most 16
-partial sums.  No rounding is larger than 2^-22 of the sum S of the products' sizes, and a logit sees at
-most group / 16 + d / group + 20 of them.  The factor rho is right to 48 * 2^-24 (a chain of at most
-40 additions under a square root, rsqrtf's two last places and a division).  The logit itself is rounded
-once to the type of the output, by half of its eps or of its smallest subnormal."""
+Tolerance.  A logit is a sum over groups of s (sum q u - z sum u).  The products are exact in fp32, and a
+group is summed in fp32 in steps of 16 columns (the tensor core may cut its addends off instead of rounding
+them: 2^-23 of the sum S of the sizes s (q + z) |u| for every step), the groups' sums are added up in fp32, as
+are the sums of u, and at most 16 partial sums are joined.  A logit sees at most
+group / 16 + d / group + 28 such roundings.  The activations enter as fp16 numbers scaled by a power of two:
+exact down to 2^-24 of the row's largest, smaller ones off by at most 2^-35 of it.  The factor rho is right to
+48 * 2^-24 (a chain of at most 40 additions under a square root, rsqrtf's two last places and a division).
+The logit itself is rounded once to the type of the output, by half of its eps or of its smallest subnormal."""
 import ctypes
 import os
 import threading
@@ -26,7 +27,7 @@ HALF_SUBNORMAL = {"bf16": 2.0 ** -134, "f16": 2.0 ** -25, "f32": 2.0 ** -150}
 
 @pytest.mark.parametrize("d,V,group,code", [(0, 16, 32, "INVALID_ARGUMENT"), (64, 0, 32, "INVALID_ARGUMENT"),
                                             (64, 16, 16, "UNSUPPORTED"), (64, 16, 100, "UNSUPPORTED"),
-                                            (65537, 16, 32, "UNSUPPORTED"), (64, (1 << 24) + 1, 32, "UNSUPPORTED")])
+                                            (32769, 16, 32, "UNSUPPORTED"), (64, (1 << 24) + 1, 32, "UNSUPPORTED")])
 def test_create_refuses_bad_shapes(d, V, group, code):
     assert not rpd.rpd_quant_create(d, V, group)
     assert rpd.rpd_last_error() != b""
@@ -108,13 +109,14 @@ def make(d, V, rows, group, zeros, norm, x="bf16", out="f32", scale="bf16", pad=
     return c
 
 
-def weights(c):
-    """(q - z) s in 64 bits, [V][d]."""
+def weights(c, sign=-1):
+    """(q - z) s, or the sizes (q + z) |s|, in 64 bits, [V][d]."""
     k = torch.arange(c["d"], device="cuda")
     byte = c["codes"][:, k // 2].long()
     q = torch.where(k % 2 == 0, byte & 15, byte >> 4)
     z = 8 if c["zeros"] is None else c["zeros"][:, k // c["group"]].long()
-    return (q - z).double() * c["scales"][:, k // c["group"]].double()
+    s = c["scales"][:, k // c["group"]].double()
+    return (q - z).double() * s if sign < 0 else (q + z).double() * s.abs()
 
 
 def reference(c):
@@ -125,9 +127,11 @@ def reference(c):
         u = (c["x"].float() * c["gain"].float()).to(c["x"].dtype).double()
     w = weights(c)
     y = (u @ w.t()) * rho
-    size = (u.abs() @ w.abs().t()) * rho
-    steps = c["group"] / 16 + c["d"] / c["group"] + 20
-    bound = steps * 2.0 ** -22 * size + 48 * 2.0 ** -24 * y.abs()
+    sizes = weights(c, 1)
+    size = (u.abs() @ sizes.t()) * rho
+    steps = c["group"] / 16 + c["d"] / c["group"] + 28
+    bound = steps * 2.0 ** -23 * size + 48 * 2.0 ** -24 * y.abs()
+    bound += 2.0 ** -35 * u.abs().amax(1, keepdim=True) * rho * sizes.sum(1)
     bound += torch.finfo(TYPES[c["outtype"]]).eps / 2 * (y.abs() + bound) + HALF_SUBNORMAL[c["outtype"]]
     return y, bound
 
@@ -168,8 +172,8 @@ SHAPES = [
     (4096, 2433, 128, 128, False, True, "bf16", "bf16", "bf16", 0),
     (4096, 999, 129, 32, True, True, "f16", "f32", "f16", 8),
     (8192, 300, 14, 64, False, True, "bf16", "f32", "bf16", 0),
-    (65536, 40, 3, 128, True, True, "bf16", "f32", "bf16", 0),
-    (65535, 33, 2, 32, False, False, "f16", "f32", "f16", 1),
+    (32768, 40, 3, 128, True, True, "bf16", "f32", "bf16", 0),
+    (32767, 33, 2, 32, False, False, "f16", "f32", "f16", 1),
 ]
 
 
