@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "librpd.so")
 CHECKED_BUILD = os.path.join(HERE, "_build_checked")
 CHECKED_LIB = os.path.join(HERE, "librpd_checked.so")
 SOURCES = ["rpd_host.cu", "k_compact.cu", "k_head_stats.cu", "k_merge_commit.cu",
-           "rpd_noalloc.cu", "k_quant.cu", "k_verify.cu"]
+           "rpd_noalloc.cu", "k_quant.cu", "k_quant_wide.cu", "k_verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -17,7 +17,7 @@
 // scales: 39 us), if the instructions a code costs stay below.  As bf16 numbers 128 + q less 128 + z (three
 // instructions a pair, 87 for 512 bytes of codes in all) they took 66 us.
 //
-// k_quant_rows: up to 16 rows.  A warp multiplies tiles of 16 matrix rows (M of the m16n8k16 MMA) by 8
+// k_quant_rows: up to 16 rows (more: k_quant_wide.cu).  A warp multiplies tiles of 16 matrix rows (M of the m16n8k16 MMA) by 8
 // or 16 activation rows (N), so that a fragment of codes is used for all of them from registers.  The
 // codes are stored in fragment order, 512 contiguous bytes for 16 rows x 64 columns, which a warp copies
 // through a ring of its own in shared memory (asked for in registers instead, the copies in flight are
@@ -295,12 +295,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     bool head = in_tile != 0;  // the tile at hand was begun by an earlier warp
     // Lanes of activations beyond the last read the last one's elements: their columns of the result
     // are never stored.
-    const uint8_t *xrow[kN8];
-    const float *srow[kN8];
+    uint32_t xrow[kN8], srow[kN8];
 #pragma unroll
     for (int n = 0; n < kN8; ++n) {
-        xrow[n] = sm.x + static_cast<size_t>(min(n * 8 + g, p.rows - 1)) * sm.row_bytes + t * 16;
-        srow[n] = sm.sums + min(n * 8 + 2 * t, sm.sum_rows - 2);
+        xrow[n] = smem_u32(sm.x) + min(n * 8 + g, p.rows - 1) * sm.row_bytes + t * 16;
+        srow[n] = smem_u32(sm.sums) + min(n * 8 + 2 * t, sm.sum_rows - 2) * 4;
     }
 
     int slot = 0, refill = depth - 1;
@@ -313,7 +312,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
             copy_wait<0>();
         __syncwarp();  // every lane's copies are seen, and every lane is done with the slot before
         fetch(refill);
-        const uint8_t *stage = ring + slot * Stage::kBytes;
+        const uint32_t stage = ring_at + slot * Stage::kBytes;
         refill = slot;
         slot = slot + 1 == depth ? 0 : slot + 1;
         const int count = min(Stage::kUnits, u1 - u);
@@ -321,30 +320,28 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 #pragma unroll
             for (int k = 0; k < kUnitGroups; ++k) {
                 float s_lo, s_hi, z_lo, z_hi;
-                unpack_meta<kF16>(*(reinterpret_cast<const Meta *>(stage + Stage::kCodeBytes) +
-                                    (j * kUnitGroups + k) * 8 + g),
-                                  s_lo, s_hi, z_lo, z_hi);
+                Meta m;
+                lds_meta(stage + Stage::kCodeBytes + ((j * kUnitGroups + k) * 8 + g) * sizeof(Meta), m);
+                unpack_meta<kF16>(m, s_lo, s_hi, z_lo, z_hi);
                 float c[kN8][4];
 #pragma unroll
                 for (int n = 0; n < kN8; ++n) {
-                    const float2 sum =
-                        *reinterpret_cast<const float2 *>(srow[n] + (in_tile * kUnitGroups + k) * sm.sum_rows);
-                    c[n][0] = -z_lo * sum.x;
-                    c[n][1] = -z_lo * sum.y;
-                    c[n][2] = -z_hi * sum.x;
-                    c[n][3] = -z_hi * sum.y;
+                    const uint2 sum = lds64(srow[n] + (in_tile * kUnitGroups + k) * sm.sum_rows * 4);
+                    c[n][0] = -z_lo * __uint_as_float(sum.x);
+                    c[n][1] = -z_lo * __uint_as_float(sum.y);
+                    c[n][2] = -z_hi * __uint_as_float(sum.x);
+                    c[n][3] = -z_hi * __uint_as_float(sum.y);
                 }
                 // 32-column halves of this group: (block, half)
 #pragma unroll
                 for (int h = 0; h < kGroup / 32; ++h) {
                     const int b = kGroup == 32 ? 0 : h >> 1, half = kGroup == 32 ? k : h & 1;
-                    const uint4 q = *reinterpret_cast<const uint4 *>(stage + (j * kUnitBlocks + b) * 512 + place);
+                    const uint4 q = lds128(stage + (j * kUnitBlocks + b) * 512 + place);
                     const uint32_t lo = half ? q.y : q.x, hi = half ? q.w : q.z;
                     uint4 xv[kN8];
 #pragma unroll
                     for (int n = 0; n < kN8; ++n)
-                        xv[n] = *reinterpret_cast<const uint4 *>(xrow[n] + (in_tile * kUnitBlocks + b) * 128 +
-                                                                 half * 64);
+                        xv[n] = lds128(xrow[n] + (in_tile * kUnitBlocks + b) * 128 + half * 64);
 #pragma unroll
                     for (int step = 0; step < 2; ++step) {
                         const uint32_t a[4] = {code_pair(lo, 2 * step), code_pair(hi, 2 * step),
@@ -402,6 +399,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 }
 
 constexpr int kRowsMax = 16;                 // activation rows of a launch
+constexpr int kRowsMost = 16;                // more are the other kernel's
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 
 // Shared memory besides the ring of codes.
@@ -452,7 +450,27 @@ struct rpd_quant {
     uint4 *codes = nullptr;
     void *meta = nullptr;
     bool set = false, zeros = false, scale_f16 = false;
+    CUtensorMap maps[2];  // the codes as rows of a tile's columns
 };
+
+namespace {
+
+// Boxes of 8 and of 4 tiles x 128 columns of the packed codes.
+int encode_codes(rpd_quant *q) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(q->blocks) * 128, static_cast<cuuint64_t>(q->pad_tiles)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(q->blocks) * 512};
+    cuuint32_t box[2] = {256, 8}, step[2] = {1, 1};
+    CUresult r = CUDA_SUCCESS;
+    for (int i = 0; i < 2 && r == CUDA_SUCCESS; ++i, box[1] /= 2)
+        r = fn(&q->maps[i], CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, q->codes, dims, strides, box, step,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -489,8 +507,7 @@ rpd_quant *rpd_quant_create(int d, int V, int group) {
     q->d = d;
     q->V = V;
     q->group = group;
-    const int unit = group > 64 ? group : 64;
-    q->blocks = (d + unit - 1) / unit * (unit / 64);
+    q->blocks = (d + 127) / 128 * 2;
     q->groups = q->blocks * 64 / group;
     q->row_tiles = (V + kQuantTileRows - 1) / kQuantTileRows;
     q->pad_tiles = (q->row_tiles + kQuantPadTiles - 1) / kQuantPadTiles * kQuantPadTiles;
@@ -540,6 +557,7 @@ int rpd_quant_set_weights(rpd_quant *q, const void *codes, const void *scales, i
         q->meta = nullptr;
         return op_cuda_fail(e, "layout of the 4-bit weights");
     }
+    if (const int rc = encode_codes(q)) return rc;
     q->zeros = zeros != nullptr;
     q->scale_f16 = scale_type == RPD_TYPE_F16;
     q->set = true;
@@ -551,7 +569,7 @@ int64_t rpd_quant_workspace(const rpd_quant *q, int rows) {
         op_fail(RPD_ERR_INVALID_ARGUMENT, "null head or negative rows");
         return -1;
     }
-    return 0;
+    return rows > kRowsMost ? quant_wide_workspace(rows, q->blocks, q->groups) : 0;
 }
 
 int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_stride, int rows, const void *gain,
@@ -571,13 +589,15 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "eps must be finite and >= 0");
     if (!aligned_to(x, 2) || (gain && !aligned_to(gain, 2)) || !aligned_to(out, type_size(out_type)))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "x, gain and out must be aligned to their elements");
-    (void)workspace;
-    (void)workspace_bytes;
+    const int64_t need = rpd_quant_workspace(q, rows);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned_to(workspace, 256)))
+        return op_fail(RPD_ERR_INVALID_ARGUMENT, "workspace: %lld bytes at a 256-byte boundary needed",
+                       static_cast<long long>(need));
     DeviceGuard dg(q->device);
     if (dg.err != cudaSuccess) return op_cuda_fail(dg.err, "cudaSetDevice");
     if (!pointer_usable(x, q->device, false) || !pointer_usable(out, q->device, false) ||
-        (gain && !pointer_usable(gain, q->device, false)))
-        return op_fail(RPD_ERR_INVALID_ARGUMENT, "x, gain and out must be device memory on the head's device");
+        (gain && !pointer_usable(gain, q->device, false)) || (need > 0 && !pointer_usable(workspace, q->device, false)))
+        return op_fail(RPD_ERR_INVALID_ARGUMENT, "x, gain, out and workspace must be device memory on the head's device");
     QuantParams p{};
     p.codes = q->codes;
     p.meta = q->meta;
@@ -595,6 +615,13 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.out_stride = out_stride;
     p.out_type = out_type;
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
+    if (rows > kRowsMost) {
+        p.x = x;
+        p.out = out;
+        p.rows = rows;
+        const cudaError_t e = quant_wide(q->maps, p, q->group, q->zeros, q->scale_f16, q->num_sms, workspace, s);
+        return e == cudaSuccess ? RPD_OK : op_cuda_fail(e, "4-bit head launch");
+    }
     // as many rows a launch as their activations fit into shared memory (at d = 32768 it is one)
     int most = kRowsMax;
     while (rows_smem(most > 8 ? 2 : 1, most, q->blocks, q->groups) + kRowsRing > kRowsSmem) --most;

@@ -1,0 +1,650 @@
+// k_quant_wide.cu - the 4-bit head for more than a few activations: the same sums as k_quant_rows
+// (k_quant.cu), on the fifth-generation tensor cores.
+//
+// The codes of 128 matrix rows are the MMA's A operand (M), read from tensor memory where four warps have
+// put them as fp16 subnormals, a thread a matrix row; the activations are B (N: 32 or 64 of them a pass), as
+// scale_u leaves them, staged in shared memory with 128-byte swizzling.  A group's product is summed in
+// TMEM; eight other warps read it, take the zero point's part off, and add it, scaled, to running sums in
+// registers, so that scales and zero points stay exact as in the kernel for few rows.
+//
+// A CTA (one an SM, persistent) owns a contiguous range of 16-row tiles and works on 256 rows at a time, as two
+// halves that share every stage of activations: a stage is 128 columns of both (16 KB of codes, 8 or 16 KB of
+// activations).  What bounds it is the instructions that a stage costs each role, a few hundred one after the other
+// whatever the stage's height: with 128 rows at a time a pass took as long a stage, with twice as many stages.
+//
+// Roles: warps 0-3 codes to TMEM (lanes by warp % 4), warps 4-11 epilogue (half = warp / 4 - 1), warps 12 and 13 TMA (codes;
+// activations), warp 14 MMA issue and TMEM.  Every wait is bounded; where one runs out the CTA's remaining logits
+// are NaN.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "ptx.cuh"
+#include "quant_internal.h"
+
+namespace rpd {
+namespace {
+
+constexpr int kWideThreads = 15 * 32;
+constexpr int kWideTmaCodes = 12, kWideTmaRows = 13, kWideMma = 14;  // warps
+constexpr int kWideHalfTiles = 8;                   // 16-row tiles of a half (128 TMEM lanes)
+constexpr int kWideUnitTiles = 2 * kWideHalfTiles;
+constexpr int kWideTileBytes = 1024;                // codes of a tile and stage
+constexpr int kWideCodeBytes = kWideUnitTiles * kWideTileBytes;
+constexpr int kWideMaxStages = 8;
+constexpr int kWideSlots = 2;                       // A operands in TMEM: 128 columns each (two halves)
+constexpr int kWideAccCols = 256;                   // TMEM columns before the A operands: two accumulators
+constexpr int kWideSmem = 226 * 1024;
+constexpr int kMetaChunk = 4;                       // groups whose scales an epilogue warp copies at a time
+constexpr int kMetaSlots = 4;
+constexpr int kMetaWarps = 8;
+constexpr long long kWideWaitCycles = 4000000000ll;  // two seconds
+
+struct WideParams {
+    QuantParams q;           // rows of this pass, their first output row
+    const uint8_t *x;        // [blocks][n][128 bytes], swizzled
+    const float *sums;       // [groups][n]
+    const float *factor;     // [n]
+    int stages;              // at least kWideSlots
+};
+
+// ------------------------------------------------------------------------------ activations
+
+// One row of a pass: its fp16 elements in the order of the main kernel's stages, its groups' sums, its
+// factor.  Rows that pad the pass are zero.
+template <typename T, int kGroup>
+__global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int per_pass, int n, uint8_t *xs, float *sums,
+                                                      float *factor) {
+    __shared__ float red[2][8];
+    const int slot = blockIdx.x % n, pass = blockIdx.x / n, r = pass * per_pass + slot;
+    const bool live = slot < per_pass && r < p.rows;
+    const int chunks = p.blocks * 8, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const T *x = static_cast<const T *>(p.x) + r * p.x_stride;
+    const T *gain = static_cast<const T *>(p.gain);
+    pdl_trigger();
+    pdl_wait();
+    float ss = 0.f, top = 0.f;
+    if (live)
+        for (int c = threadIdx.x; c < chunks; c += 256) {
+            float2 u[4];
+            ss += make_u<T>(load_chunk(x, c * 8, p.d, p.x_vectors), gain != nullptr,
+                            gain ? load_chunk(gain, c * 8, p.d, p.gain_vectors) : make_uint4(0, 0, 0, 0), u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(u[i].x), fabsf(u[i].y)));
+        }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    if (lane == 0) {
+        red[0][warp] = ss;
+        red[1][warp] = top;
+    }
+    __syncthreads();
+    ss = top = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        ss += red[0][w];
+        top = fmaxf(top, red[1][w]);
+    }
+    const int E = exponent_of(top);
+    if (threadIdx.x == 0)
+        factor[pass * n + slot] = ldexpf(gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f, E);
+    for (int c0 = warp * 32; c0 < chunks; c0 += 256) {
+        const int c = c0 + lane;
+        float sum = 0.f;
+        if (c < chunks) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (live) {
+                float2 u[4];
+                make_u<T>(load_chunk(x, c * 8, p.d, p.x_vectors), gain != nullptr,
+                          gain ? load_chunk(gain, c * 8, p.d, p.gain_vectors) : make_uint4(0, 0, 0, 0), u);
+                sum = scale_u(u, E, w);
+            }
+            const long long row = (static_cast<long long>(pass) * p.blocks + c / 8) * n + slot;
+            *reinterpret_cast<uint4 *>(xs + row * 128 + ((c % 8) ^ (slot % 8)) * 16) = w;
+        }
+#pragma unroll
+        for (int o = 1; o < kGroup / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (c < chunks && c % (kGroup / 8) == 0)
+            sums[(static_cast<long long>(pass) * p.groups + c / (kGroup / 8)) * n + slot] = sum;
+    }
+}
+
+// ------------------------------------------------------------------------------ PTX
+
+__device__ __forceinline__ void bulk_copy(void *to, const void *from, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     smem_u32(to)),
+                 "l"(from), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_copy_2d(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
+            "r"(smem_u32(to)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols) : "memory");
+}
+// D (+)= A (tensor memory) * B^T (shared memory), issued from a converged warp by its elected lane.
+__device__ __forceinline__ void umma_f16_ts_warp(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc,
+                                                 uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        " .reg .pred e, p;\n"
+        " elect.sync _|e, 0xffffffff;\n"
+        " setp.ne.b32 p, %4, 0;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "r"(a), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_commit_warp(uint64_t *bar) {
+    asm volatile(
+        "{\n"
+        " .reg .pred e;\n"
+        " elect.sync _|e, 0xffffffff;\n"
+        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
+        "}\n" ::"r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t at, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0],"
+        " {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16,"
+        " %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// kind::f16: fp32 accumulator, fp16 A and B, M = 128.
+__device__ __forceinline__ uint32_t idesc_f16(int n) {
+    return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (128u >> 4 << 24);
+}
+
+// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after two
+// seconds or once another role has raised it.
+__device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  // sleeps up to 2 us
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        " .reg .pred p;\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        " selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(2000)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    const uint32_t a = smem_u32(bar);
+    if (try_wait_long(a, parity)) return true;
+    const long long t0 = clock64();
+    while (!try_wait_long(a, parity)) {
+        if (*abort) return false;
+        if (clock64() - t0 > kWideWaitCycles) {
+            *abort = 1;
+            return false;
+        }
+    }
+    return true;
+}
+// By a converged warp, which stays so.
+__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort));
+}
+// On the way out: whatever the abort flag says.
+__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity) {
+    const uint32_t a = smem_u32(bar);
+    const long long t0 = clock64();
+    while (!mbar_try_wait(a, parity) && clock64() - t0 < kWideWaitCycles) {
+    }
+}
+
+// ------------------------------------------------------------------------------ the product
+
+// cp.async, as in k_quant.cu.
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A place in a ring of barriers.
+struct Cursor {
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int n, int by = 1) {
+        at += by;
+        if (at >= n) {
+            at -= n;
+            phase ^= 1u;
+        }
+    }
+};
+
+// Scale and zero point of a matrix row and group from shared memory.
+template <bool kZeros, bool kF16>
+__device__ __forceinline__ void row_meta(uint32_t at, float &scale, float &minus_zero) {
+    if (kZeros) {
+        const uint32_t m = lds32(at);
+        scale = scale_low<kF16>(m);
+        minus_zero = -__uint_as_float(m & 0xFFFF0000u);
+    } else {
+        scale = scale_low<kF16>(lds16(at));
+        minus_zero = -8.f;
+    }
+}
+
+constexpr int meta_group_bytes(bool zeros) { return zeros ? 64 : 32; }  // of a tile and group
+// a warp's slot: the scales of its two tiles, and the sums of its activations
+constexpr int meta_slot_bytes(bool zeros, int n) { return kMetaChunk * (2 * meta_group_bytes(zeros) + n * 4); }
+constexpr int meta_ring_bytes(bool zeros, int n) { return kMetaWarps * kMetaSlots * meta_slot_bytes(zeros, n); }
+
+template <int kGroup, bool kZeros, bool kF16, int n>
+__global__ void __launch_bounds__(kWideThreads, 1)
+    k_quant_wide(const __grid_constant__ CUtensorMap map8, const __grid_constant__ CUtensorMap map4, const WideParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    // done: the stage's MMAs are complete (its memory, its A operand and, with groups of 128 columns, the accumulator)
+    __shared__ uint64_t full[kWideMaxStages], done[kWideMaxStages], a_full[kWideSlots], acc_full[2], acc_empty[2],
+        drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ float factor[kWideMaxRows];
+    __shared__ int abort_flag;
+    volatile int *abort = &abort_flag;
+    uint8_t *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int stage_bytes = n * 256 + kWideCodeBytes;
+    const int steps = p.q.blocks / 2;  // stages of a unit
+    uint8_t *meta_ring = smem + p.stages * stage_bytes;
+    const int tile0 = static_cast<int>(static_cast<long long>(p.q.row_tiles) * blockIdx.x / gridDim.x);
+    const int tile1 = static_cast<int>(static_cast<long long>(p.q.row_tiles) * (blockIdx.x + 1) / gridDim.x);
+
+    pdl_trigger();
+    if (warp == kWideMma) tmem_alloc(&tmem_slot, 512);
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int i = 0; i < p.stages; ++i) {
+            mbar_init(&full[i], 2);
+            mbar_init(&done[i], 1);
+        }
+        for (int i = 0; i < kWideSlots; ++i) mbar_init(&a_full[i], 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&acc_full[i], 1);
+            mbar_init(&acc_empty[i], 8);
+        }
+        mbar_init(&drained, 1);
+        fence_mbar_init();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp == kWideTmaCodes || warp == kWideTmaRows) {
+        // ---- TMA, a warp for the codes and one for the activations (a copy takes its thread some 120 cycles)
+        if (lane == 0) {
+            const bool codes = warp == kWideTmaCodes;
+            if (!codes) {  // codes were laid out long ago: theirs need not wait
+                pdl_wait();
+                proxy_fence_global();
+            }
+            Cursor s;
+            int issued = 0;
+            bool ok = true;
+            for (int unit = tile0; unit < tile1 && ok; unit += kWideUnitTiles) {
+                const int tiles = min(tile1 - unit, kWideUnitTiles);
+                const int rest = tiles % 8;  // copies of eight tiles; of four where no more are left
+                const int bytes = (tiles - rest + (rest > 4 ? 8 : rest ? 4 : 0)) * kWideTileBytes;
+                for (int kb = 0; kb < steps; ++kb) {
+                    if (issued >= p.stages) ok = wait_phase(&done[s.at], s.phase ^ 1u, abort);
+                    if (!ok) break;
+                    uint8_t *to = smem + s.at * stage_bytes;
+                    if (codes) {
+                        mbar_arrive_expect_tx(&full[s.at], bytes);
+                        for (int t = 0; t < tiles; t += 8)
+                            tensor_copy_2d(to + n * 256 + t * kWideTileBytes, tiles - t > 4 ? &map8 : &map4, kb * 256, unit + t,
+                                           &full[s.at]);
+                    } else {
+                        mbar_arrive_expect_tx(&full[s.at], n * 256);
+                        bulk_copy(to, p.x + static_cast<long long>(kb) * n * 256, n * 256, &full[s.at]);
+                    }
+                    ++issued;
+                    s.next(p.stages);
+                }
+            }
+            if (!ok || *abort) {  // the copies in flight land before the memory goes (no wait can tell with the other
+                                  // warp's copies missing: a millisecond is a thousand times what they take)
+                const long long t0 = clock64();
+                while (clock64() - t0 < 2000000) {
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == kWideMma) {
+        // ---- MMA issue (every branch is warp-uniform)
+        // A stage is straight-line code: what it waits for, sixteen MMAs (or eight), commits.
+        constexpr int kGroups = 128 / kGroup, kSteps = 8 / kGroups;  // groups of a stage, 16-column steps of a group
+        const uint32_t idesc = idesc_f16(n), base = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint64_t b_base = smem_desc_sw128(smem_u32(smem));
+        Cursor s, a;
+        uint32_t acc_phase = 1;  // of the two accumulators: they are used in turn
+        int acc_next = 0;
+        bool ok = true;
+        for (int unit = tile0; unit < tile1 && ok; unit += kWideUnitTiles) {
+            const bool two = tile1 - unit > kWideHalfTiles;
+            for (int kb = 0; kb < steps; ++kb) {
+                // (the warps that arrive here have seen the whole stage land, activations too)
+                ok = wait_phase_warp(&a_full[a.at], a.phase, abort);
+                if (!ok) break;
+                const uint64_t b = b_base + static_cast<uint32_t>(s.at * stage_bytes) / 16;
+                const uint32_t a_at = base + kWideAccCols + a.at * 128;
+#pragma unroll 1
+                for (int grp = 0; grp < kGroups; ++grp) {
+                    ok = ok && wait_phase_warp(&acc_empty[acc_next], acc_phase, abort);
+                    if (ok) {
+                        tc_fence_after_sync();
+                        const uint32_t d = base + acc_next * 128;
+#pragma unroll
+                        for (int j = 0; j < kSteps; ++j) {
+                            const int k = grp * kSteps + j;  // columns 16 k .. of the stage
+                            umma_f16_ts_warp(d, a_at + k * 8, b + (k / 4) * (n * 8) + (k % 4) * 2, idesc, j != 0);
+                        }
+                        if (two)
+#pragma unroll
+                            for (int j = 0; j < kSteps; ++j) {
+                                const int k = grp * kSteps + j;
+                                umma_f16_ts_warp(d + 64, a_at + 64 + k * 8, b + (k / 4) * (n * 8) + (k % 4) * 2, idesc, j != 0);
+                            }
+                        if (kGroup != 128) umma_commit_warp(&acc_full[acc_next]);
+                        acc_phase ^= acc_next;
+                        acc_next ^= 1;
+                    }
+                }
+                if (!ok) break;
+                umma_commit_warp(&done[s.at]);
+                s.next(p.stages);
+                a.next(kWideSlots);
+            }
+        }
+        // everything issued has to be done before TMEM is given back
+        umma_commit_warp(&drained);
+        wait_drained(&drained, 0);
+        __syncwarp();
+    } else if (warp < 4) {
+        // ---- codes to TMEM: a thread a matrix row of each half
+        const int row = warp * 32 + lane;
+        // words 2 hi and 2 hi + 1 of the vectors of lanes (t, g), t = 0..3
+        const uint32_t place = smem_u32(smem) + n * 256 + (row >> 4) * kWideTileBytes + (row & 7) * 16 + ((row >> 3) & 1) * 8;
+        const uint32_t to = tmem + (static_cast<uint32_t>(warp * 32) << 16) + kWideAccCols;
+        Cursor s, a, before;  // before: the stage that had the A operand last, two ago
+        int i = 0;
+        bool ok = true;
+        for (int unit = tile0; unit < tile1 && ok; unit += kWideUnitTiles) {
+            const bool two = tile1 - unit > kWideHalfTiles;
+            for (int kb = 0; kb < steps; ++kb, ++i) {
+                ok = wait_phase_warp(&full[s.at], s.phase, abort);
+                if (!ok) break;
+                const uint32_t from = place + s.at * stage_bytes;
+                uint2 w[16];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) w[t] = lds64(from + t * 128);
+                if (two)
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) w[8 + t] = lds64(from + kWideHalfTiles * kWideTileBytes + t * 128);
+                if (i >= kWideSlots) {
+                    ok = wait_phase_warp(&done[before.at], before.phase, abort);
+                    if (!ok) break;
+                    before.next(p.stages);
+                    tc_fence_after_sync();
+                }
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    if (b < 2 || two) {
+                        uint32_t v[32];
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                v[t * 4 + k] = code_pair(w[4 * b + t].x, k);
+                                v[16 + t * 4 + k] = code_pair(w[4 * b + t].y, k);
+                            }
+                        tmem_st_32x32b_x32(to + a.at * 128 + b * 32, v);
+                    }
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&a_full[a.at]);
+                s.next(p.stages);
+                a.next(kWideSlots);
+            }
+        }
+    } else {
+        // ---- epilogue: a thread a matrix row, all activations
+        constexpr int cols = n;
+        const int half = (warp >> 2) - 1, row = (warp & 3) * 32 + lane;
+        const uint32_t from = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
+        // Scales and the activations' sums come in chunks of kMetaChunk groups (of the warp's two tiles, and of its
+        // activations), kMetaSlots - 1 chunks ahead and on into the next unit.
+        constexpr int kGroupBytes = meta_group_bytes(kZeros), kTileBytes = kMetaChunk * kGroupBytes;
+        constexpr int kSumBytes = cols * 4, kSlotBytes = meta_slot_bytes(kZeros, n);
+        const int groups = p.q.groups, per_unit = (groups + kMetaChunk - 1) / kMetaChunk;
+        const uint32_t ring = smem_u32(meta_ring) + (warp - 4) * kMetaSlots * kSlotBytes;
+        const uint8_t *meta = static_cast<const uint8_t *>(p.q.meta);
+        int fetch_unit = tile0, fetch_chunk = 0, fetch_slot = 0;
+        auto fetch = [&] {
+            if (fetch_unit < tile1) {
+                const int first = fetch_unit + half * kWideHalfTiles + (warp & 3) * 2, count = min(kMetaChunk, groups - fetch_chunk * kMetaChunk);
+                const uint32_t to = ring + fetch_slot * kSlotBytes;
+#pragma unroll
+                for (int i = 0; i < (2 * kTileBytes + 511) / 512; ++i) {
+                    const int at = i * 512 + lane * 16, t = at / kTileBytes, in = at % kTileBytes;
+                    const long long tile = min(first + t, p.q.row_tiles - 1);
+                    if (t < 2 && in < count * kGroupBytes)
+                        copy_async(to + at, meta + (tile * groups + fetch_chunk * kMetaChunk) * kGroupBytes + in);
+                }
+#pragma unroll
+                for (int i = 0; i < (kMetaChunk * kSumBytes + 511) / 512; ++i) {
+                    const int at = i * 512 + lane * 16;
+                    if (at < count * kSumBytes)
+                        copy_async(to + 2 * kTileBytes + at,
+                                   p.sums + static_cast<size_t>(fetch_chunk * kMetaChunk + at / kSumBytes) * n +
+                                       at % kSumBytes / 4);
+                }
+                if (++fetch_chunk == per_unit) {
+                    fetch_chunk = 0;
+                    fetch_unit += kWideUnitTiles;
+                }
+                fetch_slot = (fetch_slot + 1) % kMetaSlots;
+            }
+            copy_commit();
+        };
+        pdl_wait();  // sums and factors are the predecessor's
+        for (int i = 0; i < kMetaSlots - 1; ++i) fetch();
+        if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[threadIdx.x - 128];
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const uint32_t entry = ((row & 7) * 2 + ((row >> 3) & 1)) * (kGroupBytes / 16) + (lane >> 4) * kTileBytes;
+        int slot = 0;
+        Cursor acc, s;
+        bool ok = true;
+        for (int unit = tile0; unit < tile1; unit += kWideUnitTiles) {
+            f32x2 run[cols / 2];
+#pragma unroll
+            for (int i = 0; i < cols / 2; ++i) run[i] = pack2(0.f, 0.f);
+            for (int first = 0; first < groups && ok; first += kMetaChunk) {
+                copy_wait<kMetaSlots - 2>();
+                __syncwarp();  // every lane's copies are seen, and every lane is done with the chunk before
+                fetch();
+                uint32_t meta_at = ring + slot * kSlotBytes + entry, sum_at = ring + slot * kSlotBytes + 2 * kTileBytes;
+                slot = (slot + 1) % kMetaSlots;
+                const int count = min(kMetaChunk, groups - first);
+                for (int j = 0; j < count; ++j) {
+                    // all that does not hang on the product is read before the wait for it
+                    float scale, minus_zero;
+                    row_meta<kZeros, kF16>(meta_at, scale, minus_zero);
+                    const f32x2 s2 = pack2(scale, scale), z2 = pack2(minus_zero, minus_zero);
+                    f32x2 zs[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 su = lds128(sum_at + i * 16);
+                        zs[2 * i] = pack2(__uint_as_float(su.x), __uint_as_float(su.y));
+                        zs[2 * i + 1] = pack2(__uint_as_float(su.z), __uint_as_float(su.w));
+                    }
+                    ok = kGroup == 128 ? wait_phase_warp(&done[s.at], s.phase, abort)
+                                       : wait_phase_warp(&acc_full[acc.at], acc.phase, abort);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int c = 0; c < cols / 32; ++c) {
+                        float v[32];
+                        tmem_ld_32x32b_x32(from + acc.at * 128 + c * 32, v);
+                        if (c == cols / 32 - 1) {  // all of the accumulator is read
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&acc_empty[acc.at]);
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            f32x2 *r = run + c * 16 + h * 8;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                r[i] = fma2(s2, fma2(z2, zs[i], pack2(v[h * 16 + 2 * i], v[h * 16 + 2 * i + 1])), r[i]);
+                            if (c * 2 + h + 1 < cols / 16)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint4 su = lds128(sum_at + (c * 2 + h + 1) * 64 + i * 16);
+                                    zs[2 * i] = pack2(__uint_as_float(su.x), __uint_as_float(su.y));
+                                    zs[2 * i + 1] = pack2(__uint_as_float(su.z), __uint_as_float(su.w));
+                                }
+                        }
+                    }
+                    meta_at += kGroupBytes;
+                    sum_at += kSumBytes;
+                    acc.next(2);
+                    s.next(p.stages);
+                }
+            }
+            const int tile = unit + half * kWideHalfTiles + (row >> 4), v = tile * kQuantTileRows + (row & 15);
+            if (tile < tile1 && v < p.q.V) {
+#pragma unroll
+                for (int i = 0; i < cols / 2; ++i) {
+                    float y[2];
+                    unpack2(run[i], y[0], y[1]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int r = 2 * i + k;
+                        if (r < p.q.rows)
+                            store_out(p.q.out, p.q.out_type, r * p.q.out_stride + v,
+                                      ok ? y[k] * kRowFactor * factor[r] : __int_as_float(0x7FFFFFFF));
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == kWideMma) tmem_free(tmem, 512);
+}
+
+template <int kGroup, bool kZeros, bool kF16, int n>
+cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int num_sms, cudaStream_t s) {
+    void (*kernel)(const CUtensorMap, const CUtensorMap, const WideParams) = k_quant_wide<kGroup, kZeros, kF16, n>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem);
+    if (e != cudaSuccess) return e;
+    constexpr int stage = n * 256 + kWideCodeBytes, ring = meta_ring_bytes(kZeros, n);
+    constexpr int stages = (kWideSmem - 1024 - ring) / stage;
+    static_assert(stages >= kWideSlots, "an A operand's last stage is still in the ring when it is waited for");
+    p.stages = std::min(kWideMaxStages, stages);
+    return launch_pdl(kernel, dim3(std::min(num_sms, p.q.row_tiles)), dim3(kWideThreads),
+                      static_cast<size_t>(p.stages) * stage + ring + 1024, s, maps[0], maps[1], p);
+}
+
+template <int kGroup, int n>
+cudaError_t launch_wide_scales(const CUtensorMap *maps, const WideParams &p, bool zeros, bool f16, int num_sms,
+                               cudaStream_t s) {
+    if (f16)
+        return zeros ? launch_wide<kGroup, true, true, n>(maps, p, num_sms, s) : launch_wide<kGroup, false, true, n>(maps, p, num_sms, s);
+    return zeros ? launch_wide<kGroup, true, false, n>(maps, p, num_sms, s) : launch_wide<kGroup, false, false, n>(maps, p, num_sms, s);
+}
+
+template <int n>
+cudaError_t launch_wide_group(const CUtensorMap *maps, const WideParams &p, int group, bool zeros, bool f16, int num_sms,
+                              cudaStream_t s) {
+    return group == 32   ? launch_wide_scales<32, n>(maps, p, zeros, f16, num_sms, s)
+           : group == 64 ? launch_wide_scales<64, n>(maps, p, zeros, f16, num_sms, s)
+                         : launch_wide_scales<128, n>(maps, p, zeros, f16, num_sms, s);
+}
+
+template <int kGroup>
+cudaError_t launch_x(const QuantParams &p, int per_pass, int n, int passes, uint8_t *xs, float *sums, float *factor,
+                     cudaStream_t s) {
+    return p.x_type == RPD_TYPE_BF16
+               ? launch_pdl(k_quant_wide_x<__nv_bfloat16, kGroup>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs,
+                            sums, factor)
+               : launch_pdl(k_quant_wide_x<__half, kGroup>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs, sums,
+                            factor);
+}
+
+// Passes over the codes, their rows and what these are padded to.
+struct WidePasses {
+    int passes, per_pass, n;
+    explicit WidePasses(int rows) {
+        passes = (rows + kWideMaxRows - 1) / kWideMaxRows;
+        per_pass = (rows + passes - 1) / passes;
+        n = per_pass <= 32 ? 32 : 64;
+    }
+};
+
+}  // namespace
+
+long long quant_wide_workspace(int rows, int blocks, int groups) {
+    const WidePasses w(rows);
+    return static_cast<long long>(w.passes) * w.n * (blocks * 128ll + groups * 4ll + 4ll);
+}
+
+cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
+                       void *workspace, cudaStream_t s) {
+    const WidePasses w(p.rows);
+    uint8_t *xs = static_cast<uint8_t *>(workspace);
+    float *sums = reinterpret_cast<float *>(xs + static_cast<size_t>(w.passes) * w.n * p.blocks * 128);
+    float *factor = sums + static_cast<size_t>(w.passes) * w.n * p.groups;
+    cudaError_t e = group == 32   ? launch_x<32>(p, w.per_pass, w.n, w.passes, xs, sums, factor, s)
+                    : group == 64 ? launch_x<64>(p, w.per_pass, w.n, w.passes, xs, sums, factor, s)
+                                  : launch_x<128>(p, w.per_pass, w.n, w.passes, xs, sums, factor, s);
+    for (int i = 0; i < w.passes && e == cudaSuccess; ++i) {
+        WideParams q{};
+        q.q = p;
+        q.q.rows = std::min(w.per_pass, p.rows - i * w.per_pass);
+        q.q.out = static_cast<char *>(p.out) + i * w.per_pass * p.out_stride * (p.out_type == RPD_TYPE_F32 ? 4 : 2);
+        q.x = xs + static_cast<size_t>(i) * w.n * p.blocks * 128;
+        q.sums = sums + static_cast<size_t>(i) * w.n * p.groups;
+        q.factor = factor + static_cast<size_t>(i) * w.n;
+        e = w.n == 32 ? launch_wide_group<32>(maps, q, group, zeros, f16, num_sms, s)
+                      : launch_wide_group<64>(maps, q, group, zeros, f16, num_sms, s);
+    }
+    return e;
+}
+
+}  // namespace rpd

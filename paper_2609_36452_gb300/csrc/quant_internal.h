@@ -1,6 +1,7 @@
 // quant_internal.h - the 4-bit head's parameters and the device helpers that its kernels share.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -19,7 +20,7 @@ struct QuantParams {
     const uint4 *codes;  // [row_tiles][blocks][32]
     const void *meta;    // scales (and zero points), [row_tiles][groups][8][2]
     int row_tiles;       // tiles of 16 matrix rows that hold a row
-    int blocks;          // 64-column blocks of a row, a whole number of groups
+    int blocks;          // 64-column blocks of a row, an even number
     int groups;          // groups of a row, padding included
     int d, V;
     const void *x;       // [rows] rows, x_stride elements apart
@@ -41,6 +42,31 @@ template <>
 struct MetaVec<true> {
     typedef uint2 type;  // scale and zero point of a row in each word
 };
+
+// Loads from shared memory by its own addresses (a pointer that the compiler cannot trace back to shared memory is
+// read by generic loads, which wait like those from global memory).
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t at) {
+    unsigned short v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ void lds_meta(uint32_t at, uint32_t &m) { m = lds32(at); }
+__device__ __forceinline__ void lds_meta(uint32_t at, uint2 &m) { m = lds64(at); }
 
 template <bool kF16>
 __device__ __forceinline__ float scale_low(uint32_t word) {
@@ -152,5 +178,12 @@ __device__ __forceinline__ void store_out(void *out, int type, long long at, flo
     else
         static_cast<__half *>(out)[at] = __float2half_rn(v);
 }
+
+// The kernel for more rows (k_quant_wide.cu): as many passes over the codes as there are `kWideMaxRows` rows.
+constexpr int kWideMaxRows = 64;
+// maps: boxes of 8 and of 4 tiles x 128 columns of the packed codes.
+long long quant_wide_workspace(int rows, int blocks, int groups);
+cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
+                       void *workspace, cudaStream_t s);
 
 }  // namespace rpd

@@ -43,24 +43,6 @@ int cuda_fail(cudaError_t e, const char *what) {
                 what, cudaGetErrorString(e));
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static const EncodeTiledFn fn = [] {  // initialised once, thread-safely
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000,
-                                             cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(ptr);
-        return static_cast<EncodeTiledFn>(nullptr);
-    }();
-    return fn;
-}
-
 // Row-major bf16 matrix [rows][cols] -> 2-D tensor map with a (64 x box_rows) box and
 // 128-byte swizzling; out-of-range elements read as zero.
 int encode_bf16_2d(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols,
