@@ -448,12 +448,13 @@ typedef struct rpd_verify_args {
     int32_t B, D, V;
 } rpd_verify_args;
 
-/* Device bytes of workspace that rpd_verify needs; -1 for negative sizes. */
+/* Device bytes of workspace that rpd_verify needs (0 for D = 0); -1 for negative sizes. */
 int64_t rpd_verify_workspace(int B, int D);
 
 /* Runs asynchronously on `stream` (a cudaStream_t of the device that holds `target`; NULL = legacy
  * default).  Every buffer is device memory of that device; workspace: at least rpd_verify_workspace(B, D)
- * bytes, 16-byte aligned, that no other call uses at the same time (its contents need no preparation).
+ * bytes, 16-byte aligned, that no other call uses at the same time (its contents need no preparation); NULL
+ * where that is 0.
  * uniform (if D > 0) and noise may be NULL only where temperature is given and 0 throughout.  Outputs
  * may not overlap the inputs. */
 int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_bytes, void *stream);

@@ -223,6 +223,7 @@ def _arg(t, name: str, dtype: str, numel: int = None, cuda: bool = True):
 
 
 _torch_module = None
+_DTYPES = {}  # name -> torch dtype, and torch dtype -> RPD_TYPE_*
 
 
 def _torch():
@@ -230,6 +231,9 @@ def _torch():
     global _torch_module
     if _torch_module is None:
         import torch
+        for n in ("bfloat16", "float16", "float32", "int32", "uint8"):
+            _DTYPES[n] = getattr(torch, n)
+            _DTYPES[getattr(torch, n)] = ELEMENT_TYPES.get("torch." + n)
         _torch_module = torch
     return _torch_module
 
@@ -237,25 +241,29 @@ def _torch():
 def _rows_arg(t, name: str, types, shape):
     """A CUDA tensor of the given shape whose innermost dimension is contiguous; its outer strides
     (in elements) are the caller's.  Returns (pointer, RPD_TYPE_* or None, strides)."""
+    if t.__class__ is _torch().Tensor and t.is_cuda and t.shape == shape and t.dtype in types:
+        strides = t.stride()
+        if strides[-1] == 1 or shape[-1] <= 1 or not t.numel():
+            return t.data_ptr(), _DTYPES[t.dtype], strides
     if t is None or not hasattr(t, "data_ptr"):
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: a tensor is required")
     if not t.is_cuda:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: must be a CUDA tensor")
-    dtype = str(t.dtype)
-    if dtype[6:] not in types:
-        raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: dtype must be {' or '.join(types)}, not {t.dtype}")
+    if t.dtype not in types:
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT,
+                       f"{name}: dtype must be {' or '.join(str(x)[6:] for x in types)}, not {t.dtype}")
     if t.shape != shape:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     strides = t.stride()
     if strides[-1] != 1 and shape[-1] > 1 and t.numel():
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, f"{name}: its innermost dimension must be contiguous")
-    return t.data_ptr(), ELEMENT_TYPES.get(dtype), strides
+    return t.data_ptr(), _DTYPES[t.dtype], strides
 
 
 def _dense_arg(t, name: str, dtype: str, numel: int, device: int):
     """The address of a contiguous CUDA tensor of one device; the same checks as _arg and
     _same_device, in the order that is quickest for a good argument."""
-    if (type(t) is _torch().Tensor and t.get_device() == device and t.dtype is getattr(_torch_module, dtype)
+    if (t.__class__ is _torch().Tensor and t.get_device() == device and t.dtype is _DTYPES[dtype]
             and t.is_contiguous() and t.numel() == numel):
         return t.data_ptr()
     _arg(t, name, dtype, numel)
@@ -559,8 +567,9 @@ class QuantHead:
         device's current stream.  ``workspace``: a uint8 CUDA tensor of rpd_quant_workspace bytes
         (allocated where it is needed and None)."""
         rows = x.shape[0] if hasattr(x, "shape") and len(x.shape) == 2 else 0
-        px, xt, xs = _rows_arg(x, "x", ("bfloat16", "float16"), (rows, self.d))
-        po, ot, os_ = _rows_arg(out, "out", ("bfloat16", "float16", "float32"), (rows, self.V))
+        T = _torch()
+        px, xt, xs = _rows_arg(x, "x", (T.bfloat16, T.float16), (rows, self.d))
+        po, ot, os_ = _rows_arg(out, "out", (T.bfloat16, T.float16, T.float32), (rows, self.V))
         _same_device(self.device, x=x, out=out)
         pg = _dense_arg(gain, "gain", str(x.dtype)[6:], self.d, self.device) if gain is not None else None
         need = rpd_quant_workspace(self.handle, rows)
@@ -582,38 +591,37 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
     Outputs: out_accepted [B], out_token [B][D + 1], out_status [B] int32 and out_prob [B][D] float32.
     Runs on the current stream of the logits' device.  ``workspace``: a uint8 CUDA tensor of
     rpd_verify_workspace bytes (allocated if None)."""
-    if getattr(target, "dim", None) is None or target.dim() != 3 or target.shape[1] < 1:
+    shape = getattr(target, "shape", ())
+    if len(shape) != 3 or shape[1] < 1:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, "target: a tensor of [B][D + 1][V] logits is required")
-    B, D, V = target.shape[0], target.shape[1] - 1, target.shape[2]
-    logits = ("bfloat16", "float16", "float32")
-    a = RpdVerifyArgs()
-    a.B, a.D, a.V = B, D, V
-    a.target, a.type, st = _rows_arg(target, "target", logits, (B, D + 1, V))
-    a.target_seq_stride, a.target_row_stride = st[0], st[1]
+    B, D, V = shape[0], shape[1] - 1, shape[2]
+    T = _torch()
+    pt, kind, ts = _rows_arg(target, "target", (T.bfloat16, T.float16, T.float32), (B, D + 1, V))
     dev = target.get_device()
+    pd, ds = None, (0, 0)
     if draft is not None:
-        a.draft, _, st = _rows_arg(draft, "draft", (str(target.dtype)[6:],), (B, D, V))
-        a.draft_seq_stride, a.draft_row_stride = st[0], st[1]
+        pd, _, ds = _rows_arg(draft, "draft", (target.dtype,), (B, D, V))
         _same_device(dev, draft=draft)
+    pn, ns = None, (0,)
     if noise is not None:
-        a.noise, _, st = _rows_arg(noise, "noise", ("float32",), (B, V))
-        a.noise_stride = st[0]
+        pn, _, ns = _rows_arg(noise, "noise", (T.float32,), (B, V))
         _same_device(dev, noise=noise)
-    a.tokens = _dense_arg(tokens, "tokens", "int32", B * D, dev)
-    if uniform is not None:
-        a.uniform = _dense_arg(uniform, "uniform", "float32", B * D, dev)
-    if lengths is not None:
-        a.lengths = _dense_arg(lengths, "lengths", "int32", B, dev)
-    if temperature is not None:
-        a.temperature = _dense_arg(temperature, "temperature", "float32", B, dev)
-    if allowed is not None:
-        a.allowed = _dense_arg(allowed, "allowed", "int32", B * (D + 1) * ((V + 31) // 32), dev)
-    if out_prob is not None:
-        a.out_prob = _dense_arg(out_prob, "out_prob", "float32", B * D, dev)
-    a.out_accepted = _dense_arg(out_accepted, "out_accepted", "int32", B, dev)
-    a.out_token = _dense_arg(out_token, "out_token", "int32", B * (D + 1), dev)
-    a.out_status = _dense_arg(out_status, "out_status", "int32", B, dev)
+    a = RpdVerifyArgs(
+        pt, pd, _dense_arg(tokens, "tokens", "int32", B * D, dev),
+        None if lengths is None else _dense_arg(lengths, "lengths", "int32", B, dev),
+        None if temperature is None else _dense_arg(temperature, "temperature", "float32", B, dev),
+        None if allowed is None else _dense_arg(allowed, "allowed", "int32", B * (D + 1) * ((V + 31) // 32), dev),
+        None if uniform is None else _dense_arg(uniform, "uniform", "float32", B * D, dev), pn,
+        _dense_arg(out_accepted, "out_accepted", "int32", B, dev),
+        _dense_arg(out_token, "out_token", "int32", B * (D + 1), dev),
+        _dense_arg(out_status, "out_status", "int32", B, dev),
+        None if out_prob is None else _dense_arg(out_prob, "out_prob", "float32", B * D, dev),
+        ts[0], ts[1], ds[0], ds[1], ns[0], kind, B, D, V)
     if workspace is None:
-        workspace = _torch().empty(rpd_verify_workspace(B, D), dtype=_torch_module.uint8, device=target.device)
-    _check(rpd_verify(a, _dense_arg(workspace, "workspace", "uint8", workspace.numel(), dev), workspace.numel(),
-                      _stream(dev)))
+        size = rpd_verify_workspace(B, D)
+        workspace = target.new_empty(size, dtype=T.uint8) if size else None  # (held until the call is enqueued)
+    else:
+        size = workspace.numel()
+        _dense_arg(workspace, "workspace", "uint8", size, dev)
+    pw = None if workspace is None else workspace.data_ptr()
+    _check(rpd_verify(a, pw, size, _stream(dev)))

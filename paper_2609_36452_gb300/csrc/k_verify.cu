@@ -28,7 +28,8 @@ namespace {
 
 constexpr int kVerifyThreads = 256;
 constexpr int kVerifyWarps = kVerifyThreads / 32;
-constexpr int kVerifyCluster = 8;     // CTAs that scan one sequence's row
+constexpr int kDecideResident = 1024;  // threads an SM of the kernels that work in clusters
+constexpr int kVerifyMaxCluster = 8;  // CTAs that scan one sequence's row, at most
 constexpr int kVerifyMaxDrafts = 1024;
 constexpr int kVerifyMaxSplits = 32;
 
@@ -88,6 +89,12 @@ __device__ __forceinline__ uint32_t allowed_bits(const uint32_t *mask, int at, i
     return __funnelshift_r(lo, hi, at & 31);
 }
 
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 constexpr float kNoLogit = -__builtin_huge_valf();
 
 // 1 / T in units of log2, so that e^(x / T) = 2^(x c).  Within bounds where infinite logits give 0 and the
@@ -98,10 +105,12 @@ __device__ __forceinline__ float exponent_scale(float T) {
 
 // ------------------------------------------------------------------------------ statistics of the rows
 
-// Running maximum and sum.  A sum that is not finite and positive marks a row without a distribution: a
-// NaN or an infinite logit makes it NaN, and a row without any finite logit leaves it 0.
+// Running maximum and sum (in two halves, for the packed operations).  A sum that is not finite and positive marks a
+// row without a distribution: a NaN or an infinite logit makes it NaN, and a row without any finite logit leaves
+// it 0.
 struct Stat {
-    float m = kNoLogit, s = 0.f;
+    float m = kNoLogit;
+    f32x2 s = 0;  // two zeros
     template <int N>
     __device__ __forceinline__ void add(const float (&z)[N], float c) {
         float top = m;
@@ -110,26 +119,38 @@ struct Stat {
         if (top == kNoLogit) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (z[i] != z[i]) s = z[i];
+                if (z[i] != z[i]) s = pack2(z[i], z[i]);
             return;
         }
         if (top > m) {
-            s *= ex2((m - top) * c);
+            const float f = ex2((m - top) * c);
+            s = mul2(s, pack2(f, f));
             m = top;
         }
+        const f32x2 minus_m = pack2(-m, -m), c2 = pack2(c, c);
 #pragma unroll
-        for (int i = 0; i < N; ++i) s += ex2((z[i] - m) * c);
+        for (int i = 0; i + 1 < N; i += 2) {
+            float x, y;
+            unpack2(mul2(add2(pack2(z[i], z[i + 1]), minus_m), c2), x, y);
+            s = add2(s, pack2(ex2(x), ex2(y)));
+        }
+        if (N % 2) s = add2(s, pack2(ex2((z[N - 1] - m) * c), 0.f));
+    }
+    __device__ __forceinline__ float sum() const {
+        float x, y;
+        unpack2(s, x, y);
+        return x + y;
     }
     __device__ __forceinline__ void join(float m2, float s2, float c) {
         const float top = fmaxf(m, m2);
         if (top == kNoLogit) {
-            s += s2;
+            s = pack2(sum() + s2, 0.f);
         } else {
-            s = s * ex2((m - top) * c) + s2 * ex2((m2 - top) * c);
+            s = pack2(sum() * ex2((m - top) * c) + s2 * ex2((m2 - top) * c), 0.f);
             m = top;
         }
     }
-    __device__ __forceinline__ bool ok() const { return s > 0.f && s < -kNoLogit; }
+    __device__ __forceinline__ bool ok() const { return sum() > 0.f && sum() < -kNoLogit; }
 };
 
 // The largest logit and its lowest index.
@@ -154,7 +175,7 @@ struct Best {
 
 // Calls f(z, first index) for the thread's vectors of slice `split` of a row, with the tokens that are
 // not allowed at -infinity, and g(z, index) for the elements that no vector holds.
-template <typename T, bool kMask, typename F, typename G>
+template <typename T, bool kMask, int kThreads, typename F, typename G>
 __device__ __forceinline__ void walk_slice(const Row<T> &row, const uint32_t *mask, int words, int split, int splits,
                                            const F &f, const G &g) {
     constexpr int N = Row<T>::kVec;
@@ -162,14 +183,14 @@ __device__ __forceinline__ void walk_slice(const Row<T> &row, const uint32_t *ma
     const int v0 = static_cast<int>(static_cast<long long>(row.vecs) * split / splits);
     const int v1 = static_cast<int>(static_cast<long long>(row.vecs) * (split + 1) / splits);
     const uint4 *body = reinterpret_cast<const uint4 *>(row.p + row.peel);
-    for (int v = v0 + threadIdx.x; v < v1; v += kVerifyThreads * kUnroll) {
+    for (int v = v0 + threadIdx.x; v < v1; v += kThreads * kUnroll) {
         uint4 raw[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
-            if (v + u * kVerifyThreads < v1) raw[u] = body[v + u * kVerifyThreads];
+            if (v + u * kThreads < v1) raw[u] = body[v + u * kThreads];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int at = v + u * kVerifyThreads;
+            const int at = v + u * kThreads;
             if (at < v1) {
                 float z[N];
                 unpack(raw[u], z, T());
@@ -214,35 +235,35 @@ __device__ __forceinline__ const uint32_t *mask_row(const rpd_verify_args &a, in
 }
 
 // A slice of a row: rows 0..D are the target's, D + 1 .. 2 D the draft model's.
-template <typename T, bool kMask>
-__device__ __forceinline__ void row_slice(const rpd_verify_args &a, const VerifyParams &p, int b, int i, int split,
+template <typename T, bool kMask, int kWarps>
+__device__ __forceinline__ void row_slice(const rpd_verify_args &a, const VerifyParams &p, int b, int i, int split, int splits,
                                           const void *base, long long offset, float temperature, float4 *out) {
     const Row<T> row(base, offset, a.V);
     const uint32_t *mask = kMask ? mask_row(a, p.words, b, i) : nullptr;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    __shared__ float4 part[kVerifyWarps];
+    __shared__ float4 part[kWarps];
     if (temperature > 0.f) {
         const float c = exponent_scale(temperature);
         Stat st;
-        walk_slice<T, kMask>(
-            row, mask, p.words, split, p.splits, [&](const auto &z, int) { st.add(z, c); },
+        walk_slice<T, kMask, kWarps * 32>(
+            row, mask, p.words, split, splits, [&](const auto &z, int) { st.add(z, c); },
             [&](float z, int) {
                 const float one[1] = {z};
                 st.add(one, c);
             });
 #pragma unroll
         for (int o = 16; o; o >>= 1)
-            st.join(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), c);
-        if (lane == 0) part[warp] = make_float4(st.m, st.s, 0.f, 0.f);
+            st.join(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.sum(), o), c);
+        if (lane == 0) part[warp] = make_float4(st.m, st.sum(), 0.f, 0.f);
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < kVerifyWarps; ++w) st.join(part[w].x, part[w].y, c);
-            *out = make_float4(st.m, st.s, 0.f, 0.f);
+            for (int w = 1; w < kWarps; ++w) st.join(part[w].x, part[w].y, c);
+            *out = make_float4(st.m, st.sum(), 0.f, 0.f);
         }
     } else {
         Best best;
-        walk_slice<T, kMask>(
-            row, mask, p.words, split, p.splits,
+        walk_slice<T, kMask, kWarps * 32>(
+            row, mask, p.words, split, splits,
             [&](const auto &z, int first) {
 #pragma unroll
                 for (int k = 0; k < Row<T>::kVec; ++k) best.add(z[k], first + k);
@@ -255,7 +276,7 @@ __device__ __forceinline__ void row_slice(const rpd_verify_args &a, const Verify
         if (lane == 0) part[warp] = make_float4(best.m, best.bad ? 1.f : 0.f, __int_as_float(best.at), 0.f);
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < kVerifyWarps; ++w) {
+            for (int w = 1; w < kWarps; ++w) {
                 best.join(part[w].x, __float_as_int(part[w].z));
                 best.bad |= part[w].y != 0.f;
             }
@@ -267,92 +288,404 @@ __device__ __forceinline__ void row_slice(const rpd_verify_args &a, const Verify
 template <typename T, bool kMask>
 __global__ void __launch_bounds__(kVerifyThreads) k_verify_rows(const VerifyParams p) {
     const rpd_verify_args &a = p.a;
-    pdl_trigger();
     const int kinds = a.draft ? 2 * a.D + 1 : a.D + 1;
     const int split = blockIdx.x % p.splits, r = blockIdx.x / p.splits % kinds, b = blockIdx.x / p.splits / kinds;
     const bool is_draft = r > a.D;
     const int i = is_draft ? r - a.D - 1 : r;
     pdl_wait();
+    pdl_trigger();  // not before: k_verify_decide reads the call's inputs ahead of its own wait
     const int n = draft_count(a, b);
     const float temperature = temperature_of(a, b);
     // rows behind a sequence's last one are never read, nor a draft model's where the choice is greedy
     if (n < 0 || n > a.D || !(temperature >= 0.f) || (is_draft ? i >= n || temperature == 0.f : i > n)) return;
     float4 *out = p.partials + (static_cast<long long>(b) * (2 * a.D + 1) + r) * p.splits + split;
     if (is_draft)
-        row_slice<T, false>(a, p, b, i, split, a.draft, draft_offset(a, b, i), temperature, out);
+        row_slice<T, false, kVerifyWarps>(a, p, b, i, split, p.splits, a.draft, draft_offset(a, b, i), temperature, out);
     else
-        row_slice<T, kMask>(a, p, b, i, split, a.target, target_offset(a, b, i), temperature, out);
+        row_slice<T, kMask, kVerifyWarps>(a, p, b, i, split, p.splits, a.target, target_offset(a, b, i), temperature, out);
 }
 
 // ------------------------------------------------------------------------------ decision
 
-// Weight and variate of the race's leader: w / e is the largest so far, the lowest index on a tie.
-// Compared by cross products, so that a variate of 0 wins against any other.
+// The race's leader: the largest w / e so far, the lowest index on a tie.  Quotients are w times the reciprocal
+// (both right to a last place or two): a variate of 0 wins against any other, one that is negative or no number,
+// and a weight that is not positive, never.
 struct Race {
-    float w = 0.f, e = 1.f;
+    float best = 0.f;
     int at = 0x7FFFFFFF;
-    __device__ __forceinline__ void add(float w2, float e2, int at2) {  // a thread's indices rise
-        if (w2 > 0.f && e2 >= 0.f && w2 * e > w * e2) {
-            w = w2;
-            e = e2;
-            at = at2;
+    __device__ __forceinline__ void add(float score, int i) {  // a thread's indices rise
+        if (score > best) {
+            best = score;
+            at = i;
         }
     }
-    __device__ __forceinline__ void join(float w2, float e2, int at2) {
-        const float x = w2 * e, y = w * e2;
-        if (w2 > 0.f && (x > y || (x == y && at2 < at) || w == 0.f)) {
-            w = w2;
-            e = e2;
-            at = at2;
+    template <int N>
+    __device__ __forceinline__ void add(const float (&score)[N], int first) {
+        float top = score[0];
+#pragma unroll
+        for (int k = 1; k < N; ++k) top = fmaxf(top, score[k]);
+        if (top > best) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) add(score[k], first + k);
+        }
+    }
+    __device__ __forceinline__ void join(float score, int i) {
+        if (score > best || (score == best && i < at)) {
+            best = score;
+            at = i;
         }
     }
     __device__ __forceinline__ void join_warp() {
 #pragma unroll
         for (int o = 16; o; o >>= 1)
-            join(__shfl_xor_sync(0xffffffffu, w, o), __shfl_xor_sync(0xffffffffu, e, o),
-                 __shfl_xor_sync(0xffffffffu, at, o));
+            join(__shfl_xor_sync(0xffffffffu, best, o), __shfl_xor_sync(0xffffffffu, at, o));
     }
 };
 
-// Shared memory: for rows 0..D of the target largest logit, sum and argmax, for those of the draft
-// model largest logit and sum.
+// Shared memory: for rows 0..D of the target largest logit, sum and argmax, for those of the draft model largest
+// logit and sum; for every draft its logit in both.
 struct DecideRows {
-    float *tm, *ts, *dm, *ds;
+    float *tm, *ts, *dm, *ds, *zx, *zq;
     int *arg;
 };
+constexpr int kDecideRowBytes = 28;
 
-template <typename T, bool kMask>
-__global__ void __cluster_dims__(kVerifyCluster) __launch_bounds__(kVerifyThreads)
-    k_verify_decide(const VerifyParams p) {
+// The CTA's part of a row of variates on its way to L2, while the statistics are still being made.
+__device__ __forceinline__ void prefetch_slice(const float *row, int V, int split, int splits) {
+    const uintptr_t first = (reinterpret_cast<uintptr_t>(row + static_cast<long long>(V) * split / splits) + 15) & ~uintptr_t(15);
+    const uintptr_t last = reinterpret_cast<uintptr_t>(row + static_cast<long long>(V) * (split + 1) / splits) & ~uintptr_t(15);
+    if (last > first)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(first), "r"(static_cast<uint32_t>(last - first))
+                     : "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+
+// What the race is run over: p (all drafts accepted), p without the rejected token, or max(p - q, 0).
+enum Residual { kAll, kOthers, kExcess };
+
+// The row that the next token is drawn from, at the place in it where a vector begins.
+template <typename T>
+struct Contest {
+    const T *p, *q;
+    const float *noise;
+    const uint32_t *mask;
+    int words, V, rejected;             // rejected: the token, for kOthers
+    float c, tm, t_inv, dm, d_inv;      // exponent scale; largest logits and 1 / sums
+    __device__ __forceinline__ float weight(float z) const { return ex2((z - tm) * c); }  // p times the sum
+    __device__ __forceinline__ float other(float z) const { return ex2((z - dm) * c) * d_inv; }
+};
+
+// A token's score in the race and, for kExcess, in the one over p itself (should no excess be positive: p = q but for
+// roundings).
+template <int kKind, typename T>
+__device__ __forceinline__ void contend(const Contest<T> &s, float z, float zq, float e, int at, float &score, float &plain) {
+    const float w = s.weight(z), r = reciprocal(e);
+    score = (kKind == kExcess ? fmaf(w, s.t_inv, -s.other(zq)) : w) * r;
+    if (kKind == kOthers && at == s.rejected) score = 0.f;
+    if (kKind == kExcess) plain = w * r;
+}
+
+// This CTA's slice of the race.  Where variates and draft logits have the target's alignment, they are read in vectors
+// too; otherwise a thread takes single tokens, neighbours side by side.
+template <int kKind, bool kMask, int kThreads, typename T>
+__device__ __forceinline__ void run_race(const Contest<T> &s, int split, int splits, Race &race, Race &plain) {
+    constexpr int N = Row<T>::kVec, kUnroll = N == 4 ? 4 : 2;
+    const Row<T> row(s.p, 0, s.V);
+    const bool vectors = (reinterpret_cast<uintptr_t>(s.noise + row.peel) & 15) == 0 &&
+                         (kKind != kExcess || (reinterpret_cast<uintptr_t>(s.q + row.peel) & 15) == 0);
+    if (!vectors) {
+        const int i0 = static_cast<int>(static_cast<long long>(s.V) * split / splits);
+        const int i1 = static_cast<int>(static_cast<long long>(s.V) * (split + 1) / splits);
+#pragma unroll 4
+        for (int i = i0 + threadIdx.x; i < i1; i += kThreads) {
+            float z = value(s.p[i]);
+            if (kMask && !((s.mask[i >> 5] >> (i & 31)) & 1u)) z = kNoLogit;
+            float score, other = 0.f;
+            contend<kKind>(s, z, kKind == kExcess ? value(s.q[i]) : 0.f, s.noise[i], i, score, other);
+            race.add(score, i);
+            if (kKind == kExcess) plain.add(other, i);
+        }
+        return;
+    }
+    const int v0 = static_cast<int>(static_cast<long long>(row.vecs) * split / splits);
+    const int v1 = static_cast<int>(static_cast<long long>(row.vecs) * (split + 1) / splits);
+    const uint4 *pv = reinterpret_cast<const uint4 *>(s.p + row.peel);
+    const uint4 *qv = reinterpret_cast<const uint4 *>(s.q + row.peel);
+    const float4 *ev = reinterpret_cast<const float4 *>(s.noise + row.peel);
+    for (int v = v0 + threadIdx.x; v < v1; v += kThreads * kUnroll) {
+        uint4 raw[kUnroll], raw_q[kUnroll];
+        float4 e[kUnroll][N / 4];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int at = min(v + u * kThreads, v1 - 1);
+            raw[u] = pv[at];
+            if (kKind == kExcess) raw_q[u] = qv[at];
+#pragma unroll
+            for (int k = 0; k < N / 4; ++k) e[u][k] = ev[at * (N / 4) + k];
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (v + u * kThreads < v1) {
+                const int first = row.peel + (v + u * kThreads) * N;
+                float z[N], zq[N];
+                unpack(raw[u], z, T());
+                if (kKind == kExcess) unpack(raw_q[u], zq, T());
+                const uint32_t bits = kMask ? allowed_bits(s.mask, first, s.words) : 0u;
+                float score[N], other[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float4 &f = e[u][k / 4];
+                    const float en = k % 4 == 0 ? f.x : k % 4 == 1 ? f.y : k % 4 == 2 ? f.z : f.w;
+                    contend<kKind>(s, kMask && !((bits >> k) & 1u) ? kNoLogit : z[k], kKind == kExcess ? zq[k] : 0.f, en,
+                                   first + k, score[k], other[k]);
+                }
+                race.add(score, first);
+                if (kKind == kExcess) plain.add(other, first);
+            }
+        }
+    }
+    const int loose = split == 0 ? row.peel : 0, behind = row.peel + row.vecs * N;
+    const int count = loose + (split == splits - 1 ? s.V - behind : 0);
+    if (static_cast<int>(threadIdx.x) < count) {
+        const int i = static_cast<int>(threadIdx.x) < loose ? threadIdx.x : behind + threadIdx.x - loose;
+        float z = value(s.p[i]);
+        if (kMask && !((s.mask[i >> 5] >> (i & 31)) & 1u)) z = kNoLogit;
+        float score, other = 0.f;
+        contend<kKind>(s, z, kKind == kExcess ? value(s.q[i]) : 0.f, s.noise[i], i, score, other);
+        race.join(score, i);
+        if (kKind == kExcess) plain.join(other, i);
+    }
+}
+
+// ------------------------------------------------------------------------------ nothing drafted
+
+// Statistics of a slice and the race over it in one pass, both relative to the running maximum.
+struct Draw {
+    Stat st;
+    Race race;
+    template <int N>
+    __device__ __forceinline__ void add(const float (&z)[N], const float (&e)[N], int first, float c) {
+        float top = st.m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = fmaxf(top, z[i]);
+        if (top > st.m) {
+            const float f = ex2((st.m - top) * c);
+            st.s = mul2(st.s, pack2(f, f));
+            race.best = f > 0.f ? race.best * f : 0.f;
+            st.m = top;
+        }
+        if (top == kNoLogit) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (z[i] != z[i]) st.s = pack2(z[i], z[i]);
+            return;
+        }
+        const f32x2 minus_m = pack2(-st.m, -st.m), c2 = pack2(c, c);
+        float score[N];
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            float x, y;
+            unpack2(mul2(add2(pack2(z[i], i + 1 < N ? z[(i + 1) % N] : kNoLogit), minus_m), c2), x, y);
+            x = ex2(x);
+            y = ex2(y);
+            st.s = add2(st.s, pack2(x, y));
+            score[i] = x * reciprocal(e[i]);
+            if (i + 1 < N) score[(i + 1) % N] = y * reciprocal(e[(i + 1) % N]);
+        }
+        race.add(score, first);
+    }
+    __device__ __forceinline__ void join(float m2, float s2, float best2, int at2, float c) {
+        const float top = fmaxf(st.m, m2);
+        float f1 = 1.f, f2 = 1.f;
+        if (top > kNoLogit) {
+            f1 = ex2((st.m - top) * c);
+            f2 = ex2((m2 - top) * c);
+        }
+        race.best = f1 > 0.f ? race.best * f1 : 0.f;
+        race.join(f2 > 0.f ? best2 * f2 : 0.f, at2);
+        st.s = pack2(st.sum() * f1 + s2 * f2, 0.f);
+        st.m = top;
+    }
+};
+
+template <typename T, bool kMask, int kThreads>
+__device__ __forceinline__ void draw_slice(const T *p, const uint32_t *mask, int words, const float *noise, int V, float c,
+                                           int split, int splits, Draw &draw) {
+    constexpr int N = Row<T>::kVec, kUnroll = N == 4 ? 4 : 2;
+    const Row<T> row(p, 0, V);
+    if (reinterpret_cast<uintptr_t>(noise + row.peel) & 15) {  // single tokens, neighbours side by side
+        const int i0 = static_cast<int>(static_cast<long long>(V) * split / splits);
+        const int i1 = static_cast<int>(static_cast<long long>(V) * (split + 1) / splits);
+#pragma unroll 4
+        for (int i = i0 + threadIdx.x; i < i1; i += kThreads) {
+            const float z[1] = {kMask && !((mask[i >> 5] >> (i & 31)) & 1u) ? kNoLogit : value(p[i])}, e[1] = {noise[i]};
+            draw.add(z, e, i, c);
+        }
+        return;
+    }
+    const int v0 = static_cast<int>(static_cast<long long>(row.vecs) * split / splits);
+    const int v1 = static_cast<int>(static_cast<long long>(row.vecs) * (split + 1) / splits);
+    const int loose = split == 0 ? row.peel : 0, behind = row.peel + row.vecs * N;
+    const int count = loose + (split == splits - 1 ? V - behind : 0);
+    if (static_cast<int>(threadIdx.x) < loose) {  // (a thread's indices rise)
+        const int i = threadIdx.x;
+        const float z[1] = {kMask && !((mask[i >> 5] >> (i & 31)) & 1u) ? kNoLogit : value(p[i])}, e[1] = {noise[i]};
+        draw.add(z, e, i, c);
+    }
+    const uint4 *pv = reinterpret_cast<const uint4 *>(p + row.peel);
+    const float4 *ev = reinterpret_cast<const float4 *>(noise + row.peel);
+    for (int v = v0 + threadIdx.x; v < v1; v += kThreads * kUnroll) {
+        uint4 raw[kUnroll];
+        float4 f[kUnroll][N / 4];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int at = min(v + u * kThreads, v1 - 1);
+            raw[u] = pv[at];
+#pragma unroll
+            for (int k = 0; k < N / 4; ++k) f[u][k] = ev[at * (N / 4) + k];
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (v + u * kThreads < v1) {
+                const int first = row.peel + (v + u * kThreads) * N;
+                float z[N], e[N];
+                unpack(raw[u], z, T());
+                const uint32_t bits = kMask ? allowed_bits(mask, first, words) : 0u;
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    if (kMask) z[k] = (bits >> k) & 1u ? z[k] : kNoLogit;
+                    const float4 &g = f[u][k / 4];
+                    e[k] = k % 4 == 0 ? g.x : k % 4 == 1 ? g.y : k % 4 == 2 ? g.z : g.w;
+                }
+                draw.add(z, e, first, c);
+            }
+        }
+    }
+    if (static_cast<int>(threadIdx.x) >= loose && static_cast<int>(threadIdx.x) < count) {
+        const int i = behind + threadIdx.x - loose;
+        const float z[1] = {kMask && !((mask[i >> 5] >> (i & 31)) & 1u) ? kNoLogit : value(p[i])}, e[1] = {noise[i]};
+        draw.add(z, e, i, c);
+    }
+}
+
+// One cluster a sequence draws from its only row: every CTA a slice, joined in the first one.
+template <typename T, bool kMask, int kThreads>
+__global__ void __launch_bounds__(kThreads, kDecideResident / kThreads) k_sample(const VerifyParams p) {
     const rpd_verify_args &a = p.a;
-    extern __shared__ float rows_smem[];
-    __shared__ int first_stop;
-    __shared__ Race warp_race[2][kVerifyWarps];
-    __shared__ Race cta_race[2][kVerifyCluster];  // of the whole cluster, in its first CTA
-    const DecideRows s{rows_smem, rows_smem + (a.D + 1), rows_smem + 2 * (a.D + 1), rows_smem + 3 * (a.D + 1),
-                       reinterpret_cast<int *>(rows_smem + 4 * (a.D + 1))};
+    __shared__ float4 warp_part[kThreads / 32];
+    __shared__ float4 cta_part[kVerifyMaxCluster];  // of the whole cluster, in its first CTA
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.x / kVerifyCluster, rank = cluster_ctarank();
+    const int ranks = static_cast<int>(cluster_size()), b = blockIdx.x / ranks;
+    const int rank = static_cast<int>(cluster_ctarank());
     pdl_trigger();
     cluster_sync();  // every CTA of the cluster runs: their shared memory may be written
     pdl_wait();
+    const int n = draft_count(a, b);
+    const float temperature = temperature_of(a, b);
+    const bool greedy = temperature == 0.f, usable = n == 0 && temperature >= 0.f && (greedy || a.noise);
+    const float c = greedy ? 1.f : exponent_scale(temperature);
+    if (usable) {
+        if (greedy) {
+            row_slice<T, kMask, kThreads / 32>(a, p, b, 0, rank, ranks, a.target, target_offset(a, b, 0), 0.f, warp_part);
+        } else {
+            Draw draw;
+            draw_slice<T, kMask, kThreads>(static_cast<const T *>(a.target) + target_offset(a, b, 0),
+                                 kMask ? mask_row(a, p.words, b, 0) : nullptr, p.words, a.noise + b * a.noise_stride, a.V, c, rank,
+                                 ranks, draw);
+#pragma unroll
+            for (int o = 16; o; o >>= 1)
+                draw.join(__shfl_xor_sync(0xffffffffu, draw.st.m, o), __shfl_xor_sync(0xffffffffu, draw.st.sum(), o),
+                          __shfl_xor_sync(0xffffffffu, draw.race.best, o), __shfl_xor_sync(0xffffffffu, draw.race.at, o), c);
+            if (lane == 0) warp_part[warp] = make_float4(draw.st.m, draw.st.sum(), draw.race.best, __int_as_float(draw.race.at));
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                for (int w = 1; w < kThreads / 32; ++w)
+                    draw.join(warp_part[w].x, warp_part[w].y, warp_part[w].z, __float_as_int(warp_part[w].w), c);
+                warp_part[0] = make_float4(draw.st.m, draw.st.sum(), draw.race.best, __int_as_float(draw.race.at));
+            }
+        }
+        if (threadIdx.x == 0) {
+            const uint32_t to = mapa_shared(smem_u32(&cta_part[rank]), 0);
+            st_shared_cluster(to, __float_as_int(warp_part[0].x));
+            st_shared_cluster(to + 4, __float_as_int(warp_part[0].y));
+            st_shared_cluster(to + 8, __float_as_int(warp_part[0].z));
+            st_shared_cluster(to + 12, __float_as_int(warp_part[0].w));
+        }
+    }
+    cluster_sync();
+    if (rank != 0 || threadIdx.x != 0) return;
+    int next = -1;
+    if (usable && greedy) {
+        Best best;
+        bool nan = false;
+        for (int r = 0; r < ranks; ++r) {
+            best.join(cta_part[r].x, __float_as_int(cta_part[r].z));
+            nan = nan || cta_part[r].y != 0.f;
+        }
+        if (!nan && best.m > kNoLogit && best.m < -kNoLogit) next = best.at;
+    } else if (usable) {
+        Draw draw;
+        for (int r = 0; r < ranks; ++r)
+            draw.join(cta_part[r].x, cta_part[r].y, cta_part[r].z, __float_as_int(cta_part[r].w), c);
+        if (draw.st.ok() && draw.race.best > 0.f) next = draw.race.at;
+    }
+    a.out_accepted[b] = 0;
+    a.out_token[b] = next;
+    a.out_status[b] = next < 0 ? RPD_ERR_INVALID_ARGUMENT : RPD_OK;
+}
+
+template <typename T, bool kMask, int kThreads>
+__global__ void __launch_bounds__(kThreads, kDecideResident / kThreads) k_verify_decide(const VerifyParams p) {
+    const rpd_verify_args &a = p.a;
+    extern __shared__ float rows_smem[];
+    __shared__ int first_stop;
+    __shared__ Race warp_race[2][kThreads / 32];
+    __shared__ Race cta_race[2][kVerifyMaxCluster];  // of the whole cluster, in its first CTA
+    const int rows = a.D + 1;
+    const DecideRows s{rows_smem,            rows_smem + rows,     rows_smem + 2 * rows, rows_smem + 3 * rows,
+                       rows_smem + 4 * rows, rows_smem + 5 * rows, reinterpret_cast<int *>(rows_smem + 6 * rows)};
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int ranks = static_cast<int>(cluster_size()), b = blockIdx.x / ranks;
+    const int rank = static_cast<int>(cluster_ctarank());
+    pdl_trigger();
+    // The rows kernel has seen its predecessors done before this one could start: the inputs may be read while it runs.
     const int n = draft_count(a, b);
     const float T_seq = temperature_of(a, b);
     const bool greedy = T_seq == 0.f;
     const bool usable = n >= 0 && n <= a.D && T_seq >= 0.f && (greedy || (a.noise && (n == 0 || a.uniform)));
     const float c = greedy ? 1.f : exponent_scale(T_seq);
     const bool drafts = a.draft && !greedy;
+    const int32_t *tokens = a.tokens + static_cast<long long>(b) * a.D;
+    if (threadIdx.x == 0) first_stop = usable ? n : 0;
+    if (threadIdx.x == 32 && usable && !greedy) prefetch_slice(a.noise + b * a.noise_stride, a.V, rank, ranks);
+    if (usable)
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const int x = tokens[i];
+            const bool in = x >= 0 && x < a.V;
+            float zx = kNoLogit, zq = kNoLogit;
+            if (in && (!kMask || ((mask_row(a, p.words, b, i)[x >> 5] >> (x & 31)) & 1u)))
+                zx = value(static_cast<const T *>(a.target)[target_offset(a, b, i) + x]);
+            if (in && drafts) zq = value(static_cast<const T *>(a.draft)[draft_offset(a, b, i) + x]);
+            s.zx[i] = zx;
+            s.zq[i] = zq;
+        }
+    cluster_sync();  // every CTA of the cluster runs: their shared memory may be written
+    pdl_wait();
     int stop = 0, next = -1;
     bool bad = true;
-    if (threadIdx.x == 0) first_stop = usable ? n : 0;
     if (usable) {
         // the slices of every row joined, a warp a row
         const float4 *partials = p.partials + static_cast<long long>(b) * (2 * a.D + 1) * p.splits;
         const int count = n + 1 + (drafts ? n : 0);
-        for (int k = warp; k < count; k += kVerifyWarps) {
+        for (int k = warp; k < count; k += kThreads / 32) {
             const int r = k <= n ? k : a.D + 1 + (k - n - 1);
-            float4 v = lane < p.splits ? partials[static_cast<long long>(r) * p.splits + lane]
-                                       : make_float4(kNoLogit, 0.f, __int_as_float(0x7FFFFFFF), 0.f);
+            const float4 v = lane < p.splits ? partials[static_cast<long long>(r) * p.splits + lane]
+                                             : make_float4(kNoLogit, 0.f, __int_as_float(0x7FFFFFFF), 0.f);
             if (greedy) {
                 Best best;
                 best.m = v.x;
@@ -369,44 +702,26 @@ __global__ void __cluster_dims__(kVerifyCluster) __launch_bounds__(kVerifyThread
             } else {
                 Stat st;
                 st.m = v.x;
-                st.s = v.y;
+                st.s = pack2(v.y, 0.f);
 #pragma unroll
                 for (int o = 16; o; o >>= 1)
-                    st.join(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), c);
+                    st.join(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.sum(), o), c);
                 if (lane == 0) {
-                    const float sum = st.ok() ? st.s : 0.f;
-                    if (k <= n) {
-                        s.tm[k] = st.m;
-                        s.ts[k] = sum;
-                    } else {
-                        s.dm[k - n - 1] = st.m;
-                        s.ds[k - n - 1] = sum;
-                    }
+                    (k <= n ? s.tm[k] : s.dm[k - n - 1]) = st.m;
+                    (k <= n ? s.ts[k] : s.ds[k - n - 1]) = st.ok() ? st.sum() : 0.f;
                 }
             }
         }
         __syncthreads();
         // every draft's verdict; the first rejection counts
-        for (int i = threadIdx.x; i < n; i += kVerifyThreads) {
-            const int x = a.tokens[static_cast<long long>(b) * a.D + i];
-            const bool in = x >= 0 && x < a.V;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const int x = tokens[i];
             bool sound = s.ts[i] > 0.f;
-            float px = 0.f, qx = 1.f;
-            if (in && sound) {
-                if (greedy) {
-                    px = x == s.arg[i] ? 1.f : 0.f;
-                } else if (!kMask || ((mask_row(a, p.words, b, i)[x >> 5] >> (x & 31)) & 1u)) {
-                    const float z = value(static_cast<const T *>(a.target)[target_offset(a, b, i) + x]);
-                    px = ex2((z - s.tm[i]) * c) / s.ts[i];
-                }
-            }
+            const float px = !sound ? 0.f : greedy ? (x == s.arg[i] ? 1.f : 0.f) : ex2((s.zx[i] - s.tm[i]) * c) / s.ts[i];
+            float qx = 1.f;
             if (drafts) {
                 sound = sound && s.ds[i] > 0.f;
-                qx = 0.f;
-                if (in && sound) {
-                    const float z = value(static_cast<const T *>(a.draft)[draft_offset(a, b, i) + x]);
-                    qx = ex2((z - s.dm[i]) * c) / s.ds[i];
-                }
+                qx = sound ? ex2((s.zq[i] - s.dm[i]) * c) / s.ds[i] : 0.f;
             }
             const bool accept =
                 sound && (greedy ? px > 0.f : a.uniform[static_cast<long long>(b) * a.D + i] * qx < px);
@@ -420,30 +735,19 @@ __global__ void __cluster_dims__(kVerifyCluster) __launch_bounds__(kVerifyThread
         if (!bad && greedy) {
             next = s.arg[stop];
         } else if (!bad) {
-            // the race: its weights, and - should no residual be positive (p = q but for roundings) -
-            // the target's own probabilities
             Race race, plain;
-            const Row<T> row(a.target, target_offset(a, b, stop), a.V);
-            const uint32_t *mask = kMask ? mask_row(a, p.words, b, stop) : nullptr;
-            const float *noise = a.noise + b * a.noise_stride;
-            const T *q = rejected && drafts ? static_cast<const T *>(a.draft) + draft_offset(a, b, stop) : nullptr;
-            const int x = rejected && !drafts ? a.tokens[static_cast<long long>(b) * a.D + stop] : -1;
-            const float tm = s.tm[stop], t_inv = 1.f / s.ts[stop];
-            const float dm = q ? s.dm[stop] : 0.f, d_inv = q ? 1.f / s.ds[stop] : 0.f;
-            auto one = [&](float z, int at) {
-                const float w = ex2((z - tm) * c) * t_inv, e = noise[at];
-                float left = at == x ? 0.f : w;
-                if (q) left = w - ex2((value(q[at]) - dm) * c) * d_inv;
-                race.add(left, e, at);
-                if (rejected) plain.add(w, e, at);
-            };
-            walk_slice<T, kMask>(
-                row, mask, p.words, rank, kVerifyCluster,
-                [&](const auto &z, int first) {
-#pragma unroll
-                    for (int k = 0; k < Row<T>::kVec; ++k) one(z[k], first + k);
-                },
-                one);
+            const Contest<T> contest{static_cast<const T *>(a.target) + target_offset(a, b, stop),
+                                     rejected && drafts ? static_cast<const T *>(a.draft) + draft_offset(a, b, stop) : nullptr,
+                                     a.noise + b * a.noise_stride, kMask ? mask_row(a, p.words, b, stop) : nullptr, p.words, a.V,
+                                     rejected ? tokens[stop] : -1, c, s.tm[stop],
+                                     1.f / s.ts[stop], rejected && drafts ? s.dm[stop] : 0.f,
+                                     rejected && drafts ? 1.f / s.ds[stop] : 0.f};
+            if (!rejected)
+                run_race<kAll, kMask, kThreads>(contest, rank, ranks, race, plain);
+            else if (drafts)
+                run_race<kExcess, kMask, kThreads>(contest, rank, ranks, race, plain);
+            else
+                run_race<kOthers, kMask, kThreads>(contest, rank, ranks, race, plain);
             race.join_warp();
             plain.join_warp();
             if (lane == 0) {
@@ -453,14 +757,13 @@ __global__ void __cluster_dims__(kVerifyCluster) __launch_bounds__(kVerifyThread
             __syncthreads();
             if (threadIdx.x < 2) {
                 Race r = warp_race[threadIdx.x][0];
-                for (int w = 1; w < kVerifyWarps; ++w) {
+                for (int w = 1; w < kThreads / 32; ++w) {
                     const Race &o = warp_race[threadIdx.x][w];
-                    r.join(o.w, o.e, o.at);
+                    r.join(o.best, o.at);
                 }
                 const uint32_t to = mapa_shared(smem_u32(&cta_race[threadIdx.x][rank]), 0);
-                st_shared_cluster(to, __float_as_int(r.w));
-                st_shared_cluster(to + 4, __float_as_int(r.e));
-                st_shared_cluster(to + 8, r.at);
+                st_shared_cluster(to, __float_as_int(r.best));
+                st_shared_cluster(to + 4, r.at);
             }
         }
     }
@@ -468,15 +771,14 @@ __global__ void __cluster_dims__(kVerifyCluster) __launch_bounds__(kVerifyThread
     if (rank != 0) return;
     if (usable && !bad && !greedy) {
         Race r;
-        for (int kind = 0; kind < 2 && r.w == 0.f; ++kind)
-            for (int k = 0; k < kVerifyCluster; ++k)
-                r.join(cta_race[kind][k].w, cta_race[kind][k].e, cta_race[kind][k].at);
-        next = r.w > 0.f ? r.at : -1;
+        for (int kind = 0; kind < 2 && r.best == 0.f; ++kind)
+            for (int k = 0; k < ranks; ++k) r.join(cta_race[kind][k].best, cta_race[kind][k].at);
+        next = r.best > 0.f ? r.at : -1;
         bad = next < 0;
     }
-    for (int i = threadIdx.x; i <= a.D; i += kVerifyThreads) {
+    for (int i = threadIdx.x; i <= a.D; i += kThreads) {
         const long long row = static_cast<long long>(b) * (a.D + 1);
-        a.out_token[row + i] = i < stop ? a.tokens[static_cast<long long>(b) * a.D + i] : i == stop ? next : -1;
+        a.out_token[row + i] = i < stop ? tokens[i] : i == stop ? next : -1;
         if (a.out_prob && i < a.D && i >= (usable ? n : 0)) a.out_prob[static_cast<long long>(b) * a.D + i] = 0.f;
     }
     if (threadIdx.x == 0) {
@@ -492,18 +794,50 @@ int verify_splits(long long rows, long long row_bytes, int num_sms) {
     return static_cast<int>(std::max(1ll, std::min({wanted, most, static_cast<long long>(kVerifyMaxSplits)})));
 }
 
+// CTAs that share a sequence: up to eight, as long as all of them run at once.
+int verify_cluster(int B, int threads, int num_sms) {
+    int ranks = kVerifyMaxCluster;
+    while (ranks > 1 && static_cast<long long>(B) * ranks > static_cast<long long>(kDecideResident / threads) * num_sms)
+        ranks >>= 1;
+    return ranks;
+}
+
+template <typename T, bool kMask, int kThreads>
+cudaError_t launch_clusters(const VerifyParams &p, int num_sms, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    const int ranks = verify_cluster(p.a.B, kThreads, num_sms);
+    cfg.gridDim = dim3(static_cast<unsigned>(p.a.B) * ranks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = p.a.D > 0 ? static_cast<size_t>(p.a.D + 1) * kDecideRowBytes : 0;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = t_no_pdl ? 1 : 2;
+    return p.a.D > 0 ? cudaLaunchKernelEx(&cfg, k_verify_decide<T, kMask, kThreads>, p)
+                     : cudaLaunchKernelEx(&cfg, k_sample<T, kMask, kThreads>, p);
+}
+
 template <typename T, bool kMask>
-cudaError_t launch_verify(const VerifyParams &p, long long rows, cudaStream_t s) {
-    cudaError_t e = launch_pdl(k_verify_rows<T, kMask>, dim3(static_cast<unsigned>(rows * p.splits)),
-                               dim3(kVerifyThreads), 0, s, p);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(k_verify_decide<T, kMask>, dim3(static_cast<unsigned>(p.a.B) * kVerifyCluster),
-                      dim3(kVerifyThreads), static_cast<size_t>(p.a.D + 1) * 20, s, p);
+cudaError_t launch_verify(const VerifyParams &p, long long rows, int num_sms, cudaStream_t s) {
+    if (p.a.D > 0) {
+        const cudaError_t e = launch_pdl(k_verify_rows<T, kMask>, dim3(static_cast<unsigned>(rows * p.splits)),
+                                         dim3(kVerifyThreads), 0, s, p);
+        if (e != cudaSuccess) return e;
+    }
+    // few sequences: twice the threads a CTA
+    return static_cast<long long>(p.a.B) * kVerifyMaxCluster * 512 <= static_cast<long long>(kDecideResident) * num_sms
+               ? launch_clusters<T, kMask, 512>(p, num_sms, s)
+               : launch_clusters<T, kMask, 256>(p, num_sms, s);
 }
 
 template <typename T>
-cudaError_t launch_verify_type(const VerifyParams &p, long long rows, cudaStream_t s) {
-    return p.a.allowed ? launch_verify<T, true>(p, rows, s) : launch_verify<T, false>(p, rows, s);
+cudaError_t launch_verify_type(const VerifyParams &p, long long rows, int num_sms, cudaStream_t s) {
+    return p.a.allowed ? launch_verify<T, true>(p, rows, num_sms, s) : launch_verify<T, false>(p, rows, num_sms, s);
 }
 
 const char *verify_shape_error(int B, int D, int V) {
@@ -523,7 +857,7 @@ int64_t rpd_verify_workspace(int B, int D) {
         op_fail(RPD_ERR_INVALID_ARGUMENT, "%s", m);
         return -1;
     }
-    return static_cast<int64_t>(B) * (2 * static_cast<int64_t>(D) + 1) * kVerifyMaxSplits * 16;
+    return D == 0 ? 0 : static_cast<int64_t>(B) * (2 * static_cast<int64_t>(D) + 1) * kVerifyMaxSplits * 16;
 }
 
 int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_bytes, void *stream_ptr) {
@@ -534,16 +868,17 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
     if (a.D > kVerifyMaxDrafts || a.V > (1 << 24))
         return op_fail(RPD_ERR_UNSUPPORTED, "D must be <= %d and V <= %d", kVerifyMaxDrafts, 1 << 24);
     const long long rows = static_cast<long long>(a.B) * (a.draft ? 2 * a.D + 1 : a.D + 1);
-    if (rows * kVerifyMaxSplits > 0x7FFFFFFFll || a.B > (0x7FFFFFFF / kVerifyCluster))
+    if (rows * kVerifyMaxSplits > 0x7FFFFFFFll || a.B > (0x7FFFFFFF / kVerifyMaxCluster))
         return op_fail(RPD_ERR_UNSUPPORTED, "too many rows (%lld)", rows);
     if (a.B == 0) return RPD_OK;
-    if (!a.target || !a.out_accepted || !a.out_token || !a.out_status || !workspace || (a.D > 0 && !a.tokens))
+    if (!a.target || !a.out_accepted || !a.out_token || !a.out_status || (a.D > 0 && !a.tokens))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "null buffer");
     if (!a.temperature && (!a.noise || (a.D > 0 && !a.uniform)))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "uniform and noise are needed unless every temperature is 0");
-    if (workspace_bytes < rpd_verify_workspace(a.B, a.D) || !aligned16(workspace))
+    const int64_t need = rpd_verify_workspace(a.B, a.D);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "workspace: %lld bytes at a 16-byte boundary needed",
-                       static_cast<long long>(rpd_verify_workspace(a.B, a.D)));
+                       static_cast<long long>(need));
     if (a.target_seq_stride < 0 || a.target_row_stride < 0 || a.draft_seq_stride < 0 || a.draft_row_stride < 0 ||
         a.noise_stride < 0)
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "strides must be >= 0");
@@ -565,7 +900,7 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
     if (dg.err != cudaSuccess) return op_cuda_fail(dg.err, "cudaSetDevice");
     if (const int rc = check_device(at.device)) return rc;
     const void *device[] = {a.draft, a.tokens, a.lengths, a.temperature, a.allowed, a.uniform, a.noise,
-                            a.out_accepted, a.out_token, a.out_status, a.out_prob, workspace};
+                            a.out_accepted, a.out_token, a.out_status, a.out_prob, need > 0 ? workspace : nullptr};
     for (const void *d : device)
         if (d && !pointer_usable(d, at.device, false))
             return op_fail(RPD_ERR_INVALID_ARGUMENT, "every buffer must be device memory on the device of the target");
@@ -580,9 +915,9 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
     p.splits = verify_splits(rows, static_cast<long long>(a.V) * size, num_sms);
     p.words = (a.V + 31) / 32;
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
-    e = a.type == RPD_TYPE_F32    ? launch_verify_type<float>(p, rows, s)
-        : a.type == RPD_TYPE_BF16 ? launch_verify_type<__nv_bfloat16>(p, rows, s)
-                                  : launch_verify_type<__half>(p, rows, s);
+    e = a.type == RPD_TYPE_F32    ? launch_verify_type<float>(p, rows, num_sms, s)
+        : a.type == RPD_TYPE_BF16 ? launch_verify_type<__nv_bfloat16>(p, rows, num_sms, s)
+                                  : launch_verify_type<__half>(p, rows, num_sms, s);
     if (e != cudaSuccess) return op_cuda_fail(e, "verification launch");
     return RPD_OK;
 }

@@ -52,9 +52,9 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
     """The row checks of the binding, which come before any call into the library."""
     t = torch.zeros(3, 8, dtype=torch.bfloat16)
     with pytest.raises(rpd.RpdError, match="CUDA"):
-        rpd._rows_arg(t, "x", ("bfloat16",), (3, 8))
+        rpd._rows_arg(t, "x", (torch.bfloat16,), (3, 8))
     with pytest.raises(rpd.RpdError, match="required"):
-        rpd._rows_arg(None, "x", ("bfloat16",), (3, 8))
+        rpd._rows_arg(None, "x", (torch.bfloat16,), (3, 8))
 
 
 @gpu
