@@ -619,7 +619,8 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
         ts[0], ts[1], ds[0], ds[1], ns[0], kind, B, D, V)
     if workspace is None:
         size = rpd_verify_workspace(B, D)
-        workspace = target.new_empty(size, dtype=T.uint8) if size else None  # (held until the call is enqueued)
+        # (held until the call is enqueued)
+        workspace = T.empty(size, dtype=T.uint8, device=target.device) if size else None
     else:
         size = workspace.numel()
         _dense_arg(workspace, "workspace", "uint8", size, dev)

@@ -17,12 +17,13 @@
 // scales: 39 us), if the instructions a code costs stay below.  As bf16 numbers 128 + q less 128 + z (three
 // instructions a pair, 87 for 512 bytes of codes in all) they took 66 us.
 //
-// k_quant_rows: up to 16 rows (more: k_quant_wide.cu).  A warp multiplies tiles of 16 matrix rows (M of the m16n8k16 MMA) by 8
-// or 16 activation rows (N), so that a fragment of codes is used for all of them from registers.  The
-// codes are stored in fragment order, 512 contiguous bytes for 16 rows x 64 columns, which a warp copies
-// through a ring of its own in shared memory (asked for in registers instead, the copies in flight are
-// limited by the six scoreboards of a warp: 66 us again).  A CTA owns a range of tiles and its warps
-// divide the range's column blocks evenly, over tile borders: one tile's row sums then come from
+// k_quant_rows: up to 16 rows (more: k_quant_wide.cu).  A warp multiplies pairs of tiles of 16 matrix rows (M of the
+// m16n8k16 MMA) by 8 or 16 activation rows (N), so that a fragment of codes is used for all of these, and a
+// fragment of activations for both tiles, from registers (with one tile at a time shared memory was the limit: 52.6
+// us).  The codes are stored in fragment order, 1 KB for 32 rows x 64 columns, which a warp copies through a
+// ring of its own in shared memory (asked for in registers instead, the copies in flight are
+// limited by the six scoreboards of a warp: 66 us again).  A CTA owns a range of pairs and its warps
+// divide the range's column blocks evenly, over their borders: a pair's sums then may come from
 // several warps and are joined in shared memory in warp order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -41,23 +42,22 @@ namespace {
 
 // ------------------------------------------------------------------------------ layout of the codes
 
-// One 16-byte vector of the packed codes a thread: the place of lane (t, g) of tile (vt, kb) holds
-// rows 16 vt + g (words 0, 1) and 16 vt + g + 8 (words 2, 3), columns 64 kb + 8 t + {0..7} (words 0, 2)
-// and 32 columns further (words 1, 3).  Nibble i of a word is column 2i, nibble i + 4 column 2i + 1, so
-// that (word >> 4i) & 0x000F000F is a pair of neighbouring columns in the halves of a register.
-__global__ void k_quant_pack(const uint8_t *codes, uint4 *packed, int V, int d, int tiles, int blocks) {
-    const long long n = static_cast<long long>(tiles) * blocks * 32;
+// One 16-byte vector of the packed codes a thread: the place of lane (t, g) of tile `which` of (pair, kb) holds rows
+// 32 pair + 16 which + g (words 0, 1) and 8 rows further (words 2, 3), columns 64 kb + 8 t + {0..7} (words 0, 2)
+// and 32 columns further (words 1, 3).  Nibble i of a word is column 2i, nibble i + 4 column 2i + 1, so that
+// (word >> 4i) & 0x000F000F is a pair of neighbouring columns in the halves of a register.
+__global__ void k_quant_pack(const uint8_t *codes, uint4 *packed, int V, int d, int pairs, int blocks) {
+    const long long n = static_cast<long long>(pairs) * blocks * 64;
     const int row_bytes = (d + 1) / 2;
     for (long long i = blockIdx.x * static_cast<long long>(blockDim.x) + threadIdx.x; i < n;
          i += static_cast<long long>(gridDim.x) * blockDim.x) {
-        const int place = static_cast<int>(i & 31), t = place >> 3, g = place & 7;
-        const long long tile = i >> 5;
-        const int kb = static_cast<int>(tile % blocks);
-        const int vt = static_cast<int>(tile / blocks);
+        const int place = static_cast<int>(i & 31), t = place >> 3, g = place & 7, which = static_cast<int>(i >> 5) & 1;
+        const int kb = static_cast<int>((i >> 6) % blocks);
+        const int pair = static_cast<int>((i >> 6) / blocks);
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int v = vt * 16 + g + (j >> 1) * 8;
+            const int v = pair * kQuantPairRows + which * 16 + g + (j >> 1) * 8;
             const int byte = (kb * 64 + (j & 1) * 32 + t * 8) / 2;
             uint32_t word = 0;
 #pragma unroll
@@ -72,25 +72,23 @@ __global__ void k_quant_pack(const uint8_t *codes, uint4 *packed, int V, int d, 
     }
 }
 
-// Scales (and zero points) in the order of the tiles: [tile][group][g][2] for rows g and g + 8.  With
-// zero points an entry is 32 bits: the scale, and the zero point as a bf16 number in the upper half.
+// Scales (and zero points) in the order of the pairs: [pair][group][tile][g][2] for rows g and g + 8 of a tile.
+// With zero points an entry is 32 bits: the scale, and the zero point as a bf16 number in the upper half.
 template <bool kZeros>
 __global__ void k_quant_pack_scales(const uint16_t *scales, const uint8_t *zeros, void *packed, int V, int groups,
-                                    int tiles, int padded_groups) {
-    const long long n = static_cast<long long>(tiles) * padded_groups * 16;
+                                    int pairs, int padded_groups) {
+    const long long n = static_cast<long long>(pairs) * padded_groups * 32;
     for (long long i = blockIdx.x * static_cast<long long>(blockDim.x) + threadIdx.x; i < n;
          i += static_cast<long long>(gridDim.x) * blockDim.x) {
-        const int hi = static_cast<int>(i & 1), g = static_cast<int>(i >> 1) & 7;
-        const long long tg = i >> 4;
-        const int grp = static_cast<int>(tg % padded_groups);
-        const int v = static_cast<int>(tg / padded_groups) * 16 + hi * 8 + g;
+        const int hi = static_cast<int>(i & 1), g = static_cast<int>(i >> 1) & 7, which = static_cast<int>(i >> 4) & 1;
+        const int grp = static_cast<int>((i >> 5) % padded_groups);
+        const int v = static_cast<int>((i >> 5) / padded_groups) * kQuantPairRows + which * 16 + hi * 8 + g;
         const bool in = v < V && grp < groups;
         const long long at = static_cast<long long>(v) * groups + grp;
         const uint32_t s = in ? scales[at] : 0u;
         if (kZeros)
             static_cast<uint32_t *>(packed)[i] =
-                s |
-                static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(in ? zeros[at] & 15 : 0))) << 16;
+                s | static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(in ? zeros[at] & 15 : 0))) << 16;
         else
             static_cast<uint16_t *>(packed)[i] = static_cast<uint16_t>(s);
     }
@@ -154,6 +152,11 @@ __device__ __forceinline__ void for_chunks(const QuantParams &p, const T *x, int
     }
 }
 
+// Floats of the sums, what follows them aligned to 64 bytes.
+__host__ __device__ constexpr size_t sums_floats(int rows, int groups) {
+    return (static_cast<size_t>((rows + 1) & ~1) * groups + 15) & ~size_t(15);
+}
+
 template <typename T, int kGroup>
 __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
     const int chunks = p.blocks * 8;
@@ -206,18 +209,20 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
     __syncthreads();
 }
 
-// A finished tile's logits: fragment element (g, 2t) of the MMA's result is matrix row g, activation 2t.
+// A finished pair's logits: fragment element (g, 2t) of the MMA's result is matrix row g, activation 2t.
 template <int kN8>
-__device__ __forceinline__ void store_tile(const QuantParams &p, int tile, const float (&run)[kN8][4],
+__device__ __forceinline__ void store_pair(const QuantParams &p, int pair, const float (&run)[2][kN8][4],
                                            const float *factor, int g, int t) {
 #pragma unroll
-    for (int n = 0; n < kN8; ++n)
+    for (int which = 0; which < 2; ++which)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = n * 8 + 2 * t + (i & 1), v = tile * kQuantTileRows + g + (i >> 1) * 8;
-            if (r < p.rows && v < p.V)
-                store_out(p.out, p.out_type, r * p.out_stride + v, run[n][i] * kRowFactor * factor[r]);
-        }
+        for (int n = 0; n < kN8; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = n * 8 + 2 * t + (i & 1), v = pair * kQuantPairRows + which * 16 + g + (i >> 1) * 8;
+                if (r < p.rows && v < p.V)
+                    store_out(p.out, p.out_type, r * p.out_stride + v, run[which][n][i] * kRowFactor * factor[r]);
+            }
 }
 
 // Units (groups, or for groups of 32 columns two) that a warp copies and waits for at a time: 2 KB of codes.
@@ -225,9 +230,9 @@ template <int kGroup, bool kZeros>
 struct RowsStage {
     static constexpr int kUnitBlocks = kGroup == 128 ? 2 : 1;  // 64-column blocks of a unit of work
     static constexpr int kUnitGroups = kGroup == 32 ? 2 : 1;
-    static constexpr int kUnits = 4 / kUnitBlocks;
+    static constexpr int kUnits = 2 / kUnitBlocks;
     static constexpr int kCodeBytes = 2048;
-    static constexpr int kMetaUnit = kUnitGroups * (kZeros ? 64 : 32);
+    static constexpr int kMetaUnit = kUnitGroups * (kZeros ? 128 : 64);
     static constexpr int kBytes = kCodeBytes + kUnits * kMetaUnit;
 };
 
@@ -237,39 +242,39 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     typedef typename MetaVec<kZeros>::type Meta;  // scales (and zero points) of rows g and g + 8
     constexpr int kUnitBlocks = Stage::kUnitBlocks, kUnitGroups = Stage::kUnitGroups;
     extern __shared__ __align__(128) uint8_t smem[];
-    float *join = reinterpret_cast<float *>(smem);  // [warp][4 kN8][lane]
     RowsSmem sm;
-    sm.red = join + kRowsWarps * 4 * kN8 * 32;
+    sm.red = reinterpret_cast<float *>(smem);
     sm.factor = sm.red + 2 * 16 * kRowsWarps;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    uint8_t *ring = reinterpret_cast<uint8_t *>(sm.factor + 16) + warp * depth * Stage::kBytes;
-    sm.x = reinterpret_cast<uint8_t *>(sm.factor + 16) + kRowsWarps * depth * Stage::kBytes;
     // a row and 64 bytes: the two rows that a quarter of a warp reads at once lie in different banks
     sm.row_bytes = p.blocks * 128 + 64;
     sm.sum_rows = (p.rows + 1) & ~1;
-    sm.sums = reinterpret_cast<float *>(sm.x + static_cast<size_t>(p.rows) * sm.row_bytes);
+    sm.sums = sm.factor + 16;
+    uint8_t *ring = reinterpret_cast<uint8_t *>(sm.sums + sums_floats(p.rows, p.groups));
+    sm.x = ring + kRowsWarps * depth * Stage::kBytes;
+    float *join = reinterpret_cast<float *>(sm.x);  // [warp][8 kN8][lane], when nobody reads the activations any more
 
     pdl_trigger();
-    // this CTA's tiles, this warp's units of them
-    const int tile0 = static_cast<int>(static_cast<long long>(p.row_tiles) * blockIdx.x / gridDim.x);
-    const int tile1 = static_cast<int>(static_cast<long long>(p.row_tiles) * (blockIdx.x + 1) / gridDim.x);
-    const int per_tile = p.blocks / kUnitBlocks;
-    const int units = (tile1 - tile0) * per_tile;
+    // this CTA's pairs of tiles, this warp's units of them
+    const int pair0 = static_cast<int>(static_cast<long long>(p.pairs) * blockIdx.x / gridDim.x);
+    const int pair1 = static_cast<int>(static_cast<long long>(p.pairs) * (blockIdx.x + 1) / gridDim.x);
+    const int per_pair = p.blocks / kUnitBlocks;
+    const int units = (pair1 - pair0) * per_pair;
     const int u0 = units * warp / kRowsWarps, u1 = units * (warp + 1) / kRowsWarps;
-    // Both streams are contiguous over the CTA's tiles.  A lane copies the vectors of codes that it reads.
+    // Both streams are contiguous over the CTA's pairs.  A lane copies the vectors of codes that it reads.
     const int place = (t * 8 + g) * 16;
     const uint8_t *codes = reinterpret_cast<const uint8_t *>(p.codes) +
-                           (static_cast<long long>(tile0) * p.blocks + static_cast<long long>(u0) * kUnitBlocks) * 512 + place;
+                           (static_cast<long long>(pair0) * p.blocks + static_cast<long long>(u0) * kUnitBlocks) * 1024 + place;
     const uint8_t *meta = static_cast<const uint8_t *>(p.meta) +
-                          (static_cast<long long>(tile0) * per_tile + u0) * Stage::kMetaUnit + lane * 16;
-    const uint32_t ring_at = smem_u32(ring);
+                          (static_cast<long long>(pair0) * per_pair + u0) * Stage::kMetaUnit + lane * 16;
+    const uint32_t ring_at = smem_u32(ring) + warp * depth * Stage::kBytes;
     int ahead = u1 - u0;  // units that are not yet asked for
     auto fetch = [&](int slot) {
         if (ahead > 0) {
             const uint32_t to = ring_at + slot * Stage::kBytes;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                if (b / kUnitBlocks < ahead) copy_async(to + b * 512 + place, codes + b * 512);
+                if (b / (2 * kUnitBlocks) < ahead) copy_async(to + b * 512 + place, codes + b * 512);
             if (lane * 16 < min(ahead, Stage::kUnits) * Stage::kMetaUnit)
                 copy_async(to + Stage::kCodeBytes + lane * 16, meta);
             codes += Stage::kCodeBytes;
@@ -286,13 +291,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     else
         stage_rows<__half, kGroup>(p, sm);
 
-    float run[kN8][4];
+    float run[2][kN8][4], first[2][kN8][4];  // first: of a pair that an earlier warp began
 #pragma unroll
-    for (int n = 0; n < kN8; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) run[n][i] = 0.f;
-    int in_tile = u0 % per_tile, tile = tile0 + u0 / per_tile;
-    bool head = in_tile != 0;  // the tile at hand was begun by an earlier warp
+    for (int i = 0; i < 8 * kN8; ++i) run[i / (4 * kN8)][i / 4 % kN8][i % 4] = first[i / (4 * kN8)][i / 4 % kN8][i % 4] = 0.f;
+    int in_pair = u0 % per_pair, pair = pair0 + u0 / per_pair;
+    const bool joins = in_pair != 0;
+    bool head = joins;  // the pair at hand was begun by an earlier warp
     // Lanes of activations beyond the last read the last one's elements: their columns of the result
     // are never stored.
     uint32_t xrow[kN8], srow[kN8];
@@ -301,6 +305,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
         xrow[n] = smem_u32(sm.x) + min(n * 8 + g, p.rows - 1) * sm.row_bytes + t * 16;
         srow[n] = smem_u32(sm.sums) + min(n * 8 + 2 * t, sm.sum_rows - 2) * 4;
     }
+    const uint32_t sum_step = sm.sum_rows * 4;
 
     int slot = 0, refill = depth - 1;
     for (int u = u0; u < u1; u += Stage::kUnits) {
@@ -315,86 +320,93 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
         const uint32_t stage = ring_at + slot * Stage::kBytes;
         refill = slot;
         slot = slot + 1 == depth ? 0 : slot + 1;
-        const int count = min(Stage::kUnits, u1 - u);
-        for (int j = 0; j < count; ++j) {
 #pragma unroll
-            for (int k = 0; k < kUnitGroups; ++k) {
-                float s_lo, s_hi, z_lo, z_hi;
-                Meta m;
-                lds_meta(stage + Stage::kCodeBytes + ((j * kUnitGroups + k) * 8 + g) * sizeof(Meta), m);
-                unpack_meta<kF16>(m, s_lo, s_hi, z_lo, z_hi);
-                float c[kN8][4];
+        for (int j = 0; j < Stage::kUnits; ++j) {
+            if (u + j < u1) {
+                uint4 q[2];
 #pragma unroll
-                for (int n = 0; n < kN8; ++n) {
-                    const uint2 sum = lds64(srow[n] + (in_tile * kUnitGroups + k) * sm.sum_rows * 4);
-                    c[n][0] = -z_lo * __uint_as_float(sum.x);
-                    c[n][1] = -z_lo * __uint_as_float(sum.y);
-                    c[n][2] = -z_hi * __uint_as_float(sum.x);
-                    c[n][3] = -z_hi * __uint_as_float(sum.y);
-                }
-                // 32-column halves of this group: (block, half)
+                for (int k = 0; k < kUnitGroups; ++k) {
+                    float s_lo[2], s_hi[2], c[2][kN8][4];
 #pragma unroll
-                for (int h = 0; h < kGroup / 32; ++h) {
-                    const int b = kGroup == 32 ? 0 : h >> 1, half = kGroup == 32 ? k : h & 1;
-                    const uint4 q = lds128(stage + (j * kUnitBlocks + b) * 512 + place);
-                    const uint32_t lo = half ? q.y : q.x, hi = half ? q.w : q.z;
-                    uint4 xv[kN8];
+                    for (int n = 0; n < kN8; ++n) {
+                        const uint2 sum = lds64(srow[n] + (in_pair * kUnitGroups + k) * sum_step);
 #pragma unroll
-                    for (int n = 0; n < kN8; ++n)
-                        xv[n] = lds128(xrow[n] + (in_tile * kUnitBlocks + b) * 128 + half * 64);
+                        for (int which = 0; which < 2; ++which) {
+                            float z_lo, z_hi;
+                            Meta m;
+                            lds_meta(stage + Stage::kCodeBytes +
+                                         (((j * kUnitGroups + k) * 2 + which) * 8 + g) * sizeof(Meta), m);
+                            unpack_meta<kF16>(m, s_lo[which], s_hi[which], z_lo, z_hi);
+                            c[which][n][0] = -z_lo * __uint_as_float(sum.x);
+                            c[which][n][1] = -z_lo * __uint_as_float(sum.y);
+                            c[which][n][2] = -z_hi * __uint_as_float(sum.x);
+                            c[which][n][3] = -z_hi * __uint_as_float(sum.y);
+                        }
+                    }
+                    // 32-column halves of this group: (block, half); a fragment of activations for both tiles
 #pragma unroll
-                    for (int step = 0; step < 2; ++step) {
-                        const uint32_t a[4] = {code_pair(lo, 2 * step), code_pair(hi, 2 * step),
-                                               code_pair(lo, 2 * step + 1), code_pair(hi, 2 * step + 1)};
+                    for (int h = 0; h < kGroup / 32; ++h) {
+                        const int b = kGroup == 32 ? 0 : h >> 1, half = kGroup == 32 ? k : h & 1;
+                        uint4 xv[kN8];
 #pragma unroll
                         for (int n = 0; n < kN8; ++n)
-                            mma_16816(c[n], a, step ? xv[n].z : xv[n].x, step ? xv[n].w : xv[n].y);
+                            xv[n] = lds128(xrow[n] + (in_pair * kUnitBlocks + b) * 128 + half * 64);
+#pragma unroll
+                        for (int which = 0; which < 2; ++which) {
+                            if (kGroup == 32 ? k == 0 : half == 0)
+                                q[which] = lds128(stage + (j * kUnitBlocks + b) * 1024 + which * 512 + place);
+                            const uint32_t lo = half ? q[which].y : q[which].x, hi = half ? q[which].w : q[which].z;
+#pragma unroll
+                            for (int step = 0; step < 2; ++step) {
+                                const uint32_t a[4] = {code_pair(lo, 2 * step), code_pair(hi, 2 * step),
+                                                       code_pair(lo, 2 * step + 1), code_pair(hi, 2 * step + 1)};
+#pragma unroll
+                                for (int n = 0; n < kN8; ++n)
+                                    mma_16816(c[which][n], a, step ? xv[n].z : xv[n].x, step ? xv[n].w : xv[n].y);
+                            }
+                        }
                     }
+#pragma unroll
+                    for (int which = 0; which < 2; ++which)
+#pragma unroll
+                        for (int n = 0; n < kN8; ++n) {
+                            run[which][n][0] = fmaf(c[which][n][0], s_lo[which], run[which][n][0]);
+                            run[which][n][1] = fmaf(c[which][n][1], s_lo[which], run[which][n][1]);
+                            run[which][n][2] = fmaf(c[which][n][2], s_hi[which], run[which][n][2]);
+                            run[which][n][3] = fmaf(c[which][n][3], s_hi[which], run[which][n][3]);
+                        }
                 }
+                if (++in_pair == per_pair) {  // the pair's last columns
+                    if (!head) store_pair<kN8>(p, pair, run, sm.factor, g, t);
 #pragma unroll
-                for (int n = 0; n < kN8; ++n) {
-                    run[n][0] = fmaf(c[n][0], s_lo, run[n][0]);
-                    run[n][1] = fmaf(c[n][1], s_lo, run[n][1]);
-                    run[n][2] = fmaf(c[n][2], s_hi, run[n][2]);
-                    run[n][3] = fmaf(c[n][3], s_hi, run[n][3]);
+                    for (int i = 0; i < 8 * kN8; ++i) {
+                        float &r = run[i / (4 * kN8)][i / 4 % kN8][i % 4];
+                        if (head) first[i / (4 * kN8)][i / 4 % kN8][i % 4] = r;
+                        r = 0.f;
+                    }
+                    head = false;
+                    in_pair = 0;
+                    ++pair;
                 }
-            }
-            if (++in_tile == per_tile) {  // the tile's last columns
-                if (head) {
-#pragma unroll
-                    for (int n = 0; n < kN8; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) join[((warp * kN8 + n) * 4 + i) * 32 + lane] = run[n][i];
-                } else {
-                    store_tile<kN8>(p, tile, run, sm.factor, g, t);
-                }
-                head = false;
-                in_tile = 0;
-                ++tile;
-#pragma unroll
-                for (int n = 0; n < kN8; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) run[n][i] = 0.f;
             }
         }
-    }
-    if (head && in_tile) {  // the warp's whole range lies inside one tile
-#pragma unroll
-        for (int n = 0; n < kN8; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) join[((warp * kN8 + n) * 4 + i) * 32 + lane] = run[n][i];
     }
     __syncthreads();
-    if (!head && in_tile) {  // a tile that this warp began and later warps went on with
-        const int end = (tile - tile0 + 1) * per_tile;
+    if (joins) {  // (where the warp's whole range lies inside one pair, its sums are still in run)
+#pragma unroll
+        for (int i = 0; i < 8 * kN8; ++i)
+            join[(warp * 8 * kN8 + i) * 32 + lane] =
+                head ? run[i / (4 * kN8)][i / 4 % kN8][i % 4] : first[i / (4 * kN8)][i / 4 % kN8][i % 4];
+    }
+    __syncthreads();
+    if (!head && in_pair) {  // a pair that this warp began and later warps went on with
+        const int end = (pair - pair0 + 1) * per_pair;
         for (int w = warp + 1; w < kRowsWarps; ++w) {
-            if (units * w / kRowsWarps >= end) break;  // (a warp without units in the tile has left zeros)
+            if (units * w / kRowsWarps >= end) break;  // (a warp without units in the pair has left zeros)
 #pragma unroll
-            for (int n = 0; n < kN8; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) run[n][i] += join[((w * kN8 + n) * 4 + i) * 32 + lane];
+            for (int i = 0; i < 8 * kN8; ++i) run[i / (4 * kN8)][i / 4 % kN8][i % 4] += join[(w * 8 * kN8 + i) * 32 + lane];
         }
-        store_tile<kN8>(p, tile, run, sm.factor, g, t);
+        store_pair<kN8>(p, pair, run, sm.factor, g, t);
     }
 }
 
@@ -402,13 +414,13 @@ constexpr int kRowsMax = 16;                 // activation rows of a launch
 constexpr int kRowsMost = 16;                // more are the other kernel's
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 
-// Shared memory besides the ring of codes.
+// Shared memory besides the ring of codes (the activations' part is big enough for the partial sums that follow).
 size_t rows_smem(int n8, int rows, int blocks, int groups) {
-    return (static_cast<size_t>(kRowsWarps) * 4 * n8 * 32 + 2 * 16 * kRowsWarps + 16) * 4 +
-           static_cast<size_t>(rows) * (blocks * 128 + 64) + static_cast<size_t>((rows + 1) & ~1) * groups * 4;
+    return (2 * 16 * kRowsWarps + 16 + sums_floats(rows, groups)) * 4 +
+           std::max(static_cast<size_t>(rows) * (blocks * 128 + 64), static_cast<size_t>(kRowsWarps) * 8 * n8 * 32 * 4);
 }
 
-constexpr int kRowsRing = kRowsWarps * 2 * (2048 + 8 * 64);  // its least: two stages of any kind a warp
+constexpr int kRowsRing = kRowsWarps * 2 * (2048 + 4 * 128);  // its least: two stages of any kind a warp
 
 template <int kGroup, int kN8, bool kZeros, bool kF16>
 cudaError_t launch_rows(const QuantParams &p, int num_sms, cudaStream_t s) {
@@ -420,7 +432,7 @@ cudaError_t launch_rows(const QuantParams &p, int num_sms, cudaStream_t s) {
     const int stage = kRowsWarps * RowsStage<kGroup, kZeros>::kBytes;
     const int fits = static_cast<int>((kRowsSmem - fixed) / stage);
     const int depth = fits >= 6 ? 6 : fits >= 4 ? 4 : 2;
-    return launch_pdl(kernel, dim3(std::min(num_sms, p.row_tiles)), dim3(kRowsThreads), fixed + depth * stage, s, p,
+    return launch_pdl(kernel, dim3(std::min(num_sms, p.pairs)), dim3(kRowsThreads), fixed + depth * stage, s, p,
                       depth);
 }
 
@@ -446,25 +458,25 @@ using namespace rpd;
 struct rpd_quant {
     int d = 0, V = 0, group = 0;
     int device = 0, num_sms = 0;
-    int row_tiles = 0, pad_tiles = 0, blocks = 0, groups = 0;  // groups: padding included
+    int pairs = 0, pad_pairs = 0, blocks = 0, groups = 0;  // groups: padding included
     uint4 *codes = nullptr;
     void *meta = nullptr;
     bool set = false, zeros = false, scale_f16 = false;
-    CUtensorMap maps[2];  // the codes as rows of a tile's columns
+    CUtensorMap maps[2];  // the codes, a row a pair
 };
 
 namespace {
 
-// Boxes of 8 and of 4 tiles x 128 columns of the packed codes.
+// Boxes of 4 and of 2 pairs x 128 columns of the packed codes.
 int encode_codes(rpd_quant *q) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
-    cuuint64_t dims[2] = {static_cast<cuuint64_t>(q->blocks) * 128, static_cast<cuuint64_t>(q->pad_tiles)};
-    cuuint64_t strides[1] = {static_cast<cuuint64_t>(q->blocks) * 512};
-    cuuint32_t box[2] = {256, 8}, step[2] = {1, 1};
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(q->blocks) * 128, static_cast<cuuint64_t>(q->pad_pairs)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(q->blocks) * 1024};
+    cuuint32_t box[2] = {256, 4}, step[2] = {1, 1};
     CUresult r = CUDA_SUCCESS;
     for (int i = 0; i < 2 && r == CUDA_SUCCESS; ++i, box[1] /= 2)
-        r = fn(&q->maps[i], CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, q->codes, dims, strides, box, step,
+        r = fn(&q->maps[i], CU_TENSOR_MAP_DATA_TYPE_UINT64, 2, q->codes, dims, strides, box, step,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
@@ -509,8 +521,8 @@ rpd_quant *rpd_quant_create(int d, int V, int group) {
     q->group = group;
     q->blocks = (d + 127) / 128 * 2;
     q->groups = q->blocks * 64 / group;
-    q->row_tiles = (V + kQuantTileRows - 1) / kQuantTileRows;
-    q->pad_tiles = (q->row_tiles + kQuantPadTiles - 1) / kQuantPadTiles * kQuantPadTiles;
+    q->pairs = (V + kQuantPairRows - 1) / kQuantPairRows;
+    q->pad_pairs = (q->pairs + kQuantPadPairs - 1) / kQuantPadPairs * kQuantPadPairs;
     return q;
 }
 
@@ -526,8 +538,8 @@ int rpd_quant_set_weights(rpd_quant *q, const void *codes, const void *scales, i
         (zeros && !pointer_usable(zeros, q->device, false)))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "codes, scales and zeros must be device memory on the head's device");
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
-    const size_t code_bytes = static_cast<size_t>(q->pad_tiles) * q->blocks * 512;
-    const size_t meta_bytes = static_cast<size_t>(q->pad_tiles) * q->groups * (zeros ? 64 : 32);
+    const size_t code_bytes = static_cast<size_t>(q->pad_pairs) * q->blocks * 1024;
+    const size_t meta_bytes = static_cast<size_t>(q->pad_pairs) * q->groups * (zeros ? 128 : 64);
     // Freeing the previous layout waits for the device: no call may still be reading it.
     q->set = false;
     if (q->codes) cudaFree(q->codes);
@@ -539,14 +551,14 @@ int rpd_quant_set_weights(rpd_quant *q, const void *codes, const void *scales, i
     if (e == cudaSuccess) {
         const int groups = (q->d + q->group - 1) / q->group;
         k_quant_pack<<<q->num_sms * 8, 256, 0, s>>>(static_cast<const uint8_t *>(codes), q->codes, q->V, q->d,
-                                                    q->pad_tiles, q->blocks);
+                                                    q->pad_pairs, q->blocks);
         if (zeros)
             k_quant_pack_scales<true><<<q->num_sms * 4, 256, 0, s>>>(static_cast<const uint16_t *>(scales),
                                                                      static_cast<const uint8_t *>(zeros), q->meta,
-                                                                     q->V, groups, q->pad_tiles, q->groups);
+                                                                     q->V, groups, q->pad_pairs, q->groups);
         else
             k_quant_pack_scales<false><<<q->num_sms * 4, 256, 0, s>>>(static_cast<const uint16_t *>(scales), nullptr,
-                                                                      q->meta, q->V, groups, q->pad_tiles, q->groups);
+                                                                      q->meta, q->V, groups, q->pad_pairs, q->groups);
         e = cudaGetLastError();
         if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     }
@@ -601,7 +613,7 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     QuantParams p{};
     p.codes = q->codes;
     p.meta = q->meta;
-    p.row_tiles = q->row_tiles;
+    p.pairs = q->pairs;
     p.blocks = q->blocks;
     p.groups = q->groups;
     p.x_type = x_type;

@@ -7,7 +7,7 @@
 // TMEM; eight other warps read it, take the zero point's part off, and add it, scaled, to running sums in
 // registers, so that scales and zero points stay exact as in the kernel for few rows.
 //
-// A CTA (one an SM, persistent) owns a contiguous range of 16-row tiles and works on 256 rows at a time, as two
+// A CTA (one an SM, persistent) owns a contiguous range of pairs of 16-row tiles and works on 256 rows at a time, as two
 // halves that share every stage of activations: a stage is 128 columns of both (16 KB of codes, 8 or 16 KB of
 // activations).  What bounds it is the instructions that a stage costs each role, a few hundred one after the other
 // whatever the stage's height: with 128 rows at a time a pass took as long a stage, with twice as many stages.
@@ -30,10 +30,10 @@ namespace {
 
 constexpr int kWideThreads = 15 * 32;
 constexpr int kWideTmaCodes = 12, kWideTmaRows = 13, kWideMma = 14;  // warps
-constexpr int kWideHalfTiles = 8;                   // 16-row tiles of a half (128 TMEM lanes)
-constexpr int kWideUnitTiles = 2 * kWideHalfTiles;
-constexpr int kWideTileBytes = 1024;                // codes of a tile and stage
-constexpr int kWideCodeBytes = kWideUnitTiles * kWideTileBytes;
+constexpr int kWideHalf = 4;                        // pairs of tiles (32 matrix rows) of a half (128 TMEM lanes)
+constexpr int kWideUnit = 2 * kWideHalf;
+constexpr int kWidePairBytes = 2048;                // codes of a pair and stage: [block][tile][512 bytes]
+constexpr int kWideCodeBytes = kWideUnit * kWidePairBytes;
 constexpr int kWideMaxStages = 8;
 constexpr int kWideSlots = 2;                       // A operands in TMEM: 128 columns each (two halves)
 constexpr int kWideAccCols = 256;                   // TMEM columns before the A operands: two accumulators
@@ -256,14 +256,14 @@ __device__ __forceinline__ void row_meta(uint32_t at, float &scale, float &minus
     }
 }
 
-constexpr int meta_group_bytes(bool zeros) { return zeros ? 64 : 32; }  // of a tile and group
-// a warp's slot: the scales of its two tiles, and the sums of its activations
-constexpr int meta_slot_bytes(bool zeros, int n) { return kMetaChunk * (2 * meta_group_bytes(zeros) + n * 4); }
+constexpr int meta_group_bytes(bool zeros) { return zeros ? 128 : 64; }  // of a pair and group
+// a warp's slot: the scales of its pair, and the sums of the activations
+constexpr int meta_slot_bytes(bool zeros, int n) { return kMetaChunk * (meta_group_bytes(zeros) + n * 4); }
 constexpr int meta_ring_bytes(bool zeros, int n) { return kMetaWarps * kMetaSlots * meta_slot_bytes(zeros, n); }
 
 template <int kGroup, bool kZeros, bool kF16, int n>
 __global__ void __launch_bounds__(kWideThreads, 1)
-    k_quant_wide(const __grid_constant__ CUtensorMap map8, const __grid_constant__ CUtensorMap map4, const WideParams p) {
+    k_quant_wide(const __grid_constant__ CUtensorMap map4, const __grid_constant__ CUtensorMap map2, const WideParams p) {
     extern __shared__ uint8_t smem_raw[];
     // done: the stage's MMAs are complete (its memory, its A operand and, with groups of 128 columns, the accumulator)
     __shared__ uint64_t full[kWideMaxStages], done[kWideMaxStages], a_full[kWideSlots], acc_full[2], acc_empty[2],
@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     constexpr int stage_bytes = n * 256 + kWideCodeBytes;
     const int steps = p.q.blocks / 2;  // stages of a unit
     uint8_t *meta_ring = smem + p.stages * stage_bytes;
-    const int tile0 = static_cast<int>(static_cast<long long>(p.q.row_tiles) * blockIdx.x / gridDim.x);
-    const int tile1 = static_cast<int>(static_cast<long long>(p.q.row_tiles) * (blockIdx.x + 1) / gridDim.x);
+    const int pair0 = static_cast<int>(static_cast<long long>(p.q.pairs) * blockIdx.x / gridDim.x);
+    const int pair1 = static_cast<int>(static_cast<long long>(p.q.pairs) * (blockIdx.x + 1) / gridDim.x);
 
     pdl_trigger();
     if (warp == kWideMma) tmem_alloc(&tmem_slot, 512);
@@ -312,18 +312,18 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             Cursor s;
             int issued = 0;
             bool ok = true;
-            for (int unit = tile0; unit < tile1 && ok; unit += kWideUnitTiles) {
-                const int tiles = min(tile1 - unit, kWideUnitTiles);
-                const int rest = tiles % 8;  // copies of eight tiles; of four where no more are left
-                const int bytes = (tiles - rest + (rest > 4 ? 8 : rest ? 4 : 0)) * kWideTileBytes;
+            for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
+                const int pairs = min(pair1 - unit, kWideUnit);
+                const int rest = pairs % 4;  // copies of four pairs; of two where no more are left
+                const int bytes = (pairs - rest + (rest > 2 ? 4 : rest ? 2 : 0)) * kWidePairBytes;
                 for (int kb = 0; kb < steps; ++kb) {
                     if (issued >= p.stages) ok = wait_phase(&done[s.at], s.phase ^ 1u, abort);
                     if (!ok) break;
                     uint8_t *to = smem + s.at * stage_bytes;
                     if (codes) {
                         mbar_arrive_expect_tx(&full[s.at], bytes);
-                        for (int t = 0; t < tiles; t += 8)
-                            tensor_copy_2d(to + n * 256 + t * kWideTileBytes, tiles - t > 4 ? &map8 : &map4, kb * 256, unit + t,
+                        for (int t = 0; t < pairs; t += 4)
+                            tensor_copy_2d(to + n * 256 + t * kWidePairBytes, pairs - t > 2 ? &map4 : &map2, kb * 256, unit + t,
                                            &full[s.at]);
                     } else {
                         mbar_arrive_expect_tx(&full[s.at], n * 256);
@@ -351,8 +351,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         uint32_t acc_phase = 1;  // of the two accumulators: they are used in turn
         int acc_next = 0;
         bool ok = true;
-        for (int unit = tile0; unit < tile1 && ok; unit += kWideUnitTiles) {
-            const bool two = tile1 - unit > kWideHalfTiles;
+        for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
+            const bool two = pair1 - unit > kWideHalf;
             for (int kb = 0; kb < steps; ++kb) {
                 // (the warps that arrive here have seen the whole stage land, activations too)
                 ok = wait_phase_warp(&a_full[a.at], a.phase, abort);
@@ -395,23 +395,25 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // ---- codes to TMEM: a thread a matrix row of each half
         const int row = warp * 32 + lane;
         // words 2 hi and 2 hi + 1 of the vectors of lanes (t, g), t = 0..3
-        const uint32_t place = smem_u32(smem) + n * 256 + (row >> 4) * kWideTileBytes + (row & 7) * 16 + ((row >> 3) & 1) * 8;
+        const uint32_t place = smem_u32(smem) + n * 256 + (row >> 5) * kWidePairBytes + ((row >> 4) & 1) * 512 +
+                               (row & 7) * 16 + ((row >> 3) & 1) * 8;
         const uint32_t to = tmem + (static_cast<uint32_t>(warp * 32) << 16) + kWideAccCols;
         Cursor s, a, before;  // before: the stage that had the A operand last, two ago
         int i = 0;
         bool ok = true;
-        for (int unit = tile0; unit < tile1 && ok; unit += kWideUnitTiles) {
-            const bool two = tile1 - unit > kWideHalfTiles;
+        for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
+            const bool two = pair1 - unit > kWideHalf;
             for (int kb = 0; kb < steps; ++kb, ++i) {
                 ok = wait_phase_warp(&full[s.at], s.phase, abort);
                 if (!ok) break;
                 const uint32_t from = place + s.at * stage_bytes;
                 uint2 w[16];
 #pragma unroll
-                for (int t = 0; t < 8; ++t) w[t] = lds64(from + t * 128);
+                for (int t = 0; t < 8; ++t) w[t] = lds64(from + (t >> 2) * 1024 + (t & 3) * 128);
                 if (two)
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) w[8 + t] = lds64(from + kWideHalfTiles * kWideTileBytes + t * 128);
+                    for (int t = 0; t < 8; ++t)
+                        w[8 + t] = lds64(from + kWideHalf * kWidePairBytes + (t >> 2) * 1024 + (t & 3) * 128);
                 if (i >= kWideSlots) {
                     ok = wait_phase_warp(&done[before.at], before.phase, abort);
                     if (!ok) break;
@@ -445,36 +447,36 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         constexpr int cols = n;
         const int half = (warp >> 2) - 1, row = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
-        // Scales and the activations' sums come in chunks of kMetaChunk groups (of the warp's two tiles, and of its
+        // Scales and the activations' sums come in chunks of kMetaChunk groups (of the warp's pair of tiles, and of all
         // activations), kMetaSlots - 1 chunks ahead and on into the next unit.
-        constexpr int kGroupBytes = meta_group_bytes(kZeros), kTileBytes = kMetaChunk * kGroupBytes;
+        constexpr int kGroupBytes = meta_group_bytes(kZeros), kMetaBytes = kMetaChunk * kGroupBytes;
         constexpr int kSumBytes = cols * 4, kSlotBytes = meta_slot_bytes(kZeros, n);
         const int groups = p.q.groups, per_unit = (groups + kMetaChunk - 1) / kMetaChunk;
         const uint32_t ring = smem_u32(meta_ring) + (warp - 4) * kMetaSlots * kSlotBytes;
         const uint8_t *meta = static_cast<const uint8_t *>(p.q.meta);
-        int fetch_unit = tile0, fetch_chunk = 0, fetch_slot = 0;
+        int fetch_unit = pair0, fetch_chunk = 0, fetch_slot = 0;
         auto fetch = [&] {
-            if (fetch_unit < tile1) {
-                const int first = fetch_unit + half * kWideHalfTiles + (warp & 3) * 2, count = min(kMetaChunk, groups - fetch_chunk * kMetaChunk);
+            if (fetch_unit < pair1) {
+                const long long pair = min(fetch_unit + half * kWideHalf + (warp & 3), p.q.pairs - 1);
+                const int count = min(kMetaChunk, groups - fetch_chunk * kMetaChunk);
                 const uint32_t to = ring + fetch_slot * kSlotBytes;
 #pragma unroll
-                for (int i = 0; i < (2 * kTileBytes + 511) / 512; ++i) {
-                    const int at = i * 512 + lane * 16, t = at / kTileBytes, in = at % kTileBytes;
-                    const long long tile = min(first + t, p.q.row_tiles - 1);
-                    if (t < 2 && in < count * kGroupBytes)
-                        copy_async(to + at, meta + (tile * groups + fetch_chunk * kMetaChunk) * kGroupBytes + in);
+                for (int i = 0; i < (kMetaBytes + 511) / 512; ++i) {
+                    const int at = i * 512 + lane * 16;
+                    if (at < count * kGroupBytes)
+                        copy_async(to + at, meta + (pair * groups + fetch_chunk * kMetaChunk) * kGroupBytes + at);
                 }
 #pragma unroll
                 for (int i = 0; i < (kMetaChunk * kSumBytes + 511) / 512; ++i) {
                     const int at = i * 512 + lane * 16;
                     if (at < count * kSumBytes)
-                        copy_async(to + 2 * kTileBytes + at,
+                        copy_async(to + kMetaBytes + at,
                                    p.sums + static_cast<size_t>(fetch_chunk * kMetaChunk + at / kSumBytes) * n +
                                        at % kSumBytes / 4);
                 }
                 if (++fetch_chunk == per_unit) {
                     fetch_chunk = 0;
-                    fetch_unit += kWideUnitTiles;
+                    fetch_unit += kWideUnit;
                 }
                 fetch_slot = (fetch_slot + 1) % kMetaSlots;
             }
@@ -484,11 +486,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         for (int i = 0; i < kMetaSlots - 1; ++i) fetch();
         if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[threadIdx.x - 128];
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        const uint32_t entry = ((row & 7) * 2 + ((row >> 3) & 1)) * (kGroupBytes / 16) + (lane >> 4) * kTileBytes;
+        const uint32_t entry = ((lane >> 4) * 16 + (row & 7) * 2 + ((row >> 3) & 1)) * (kGroupBytes / 32);
         int slot = 0;
         Cursor acc, s;
         bool ok = true;
-        for (int unit = tile0; unit < tile1; unit += kWideUnitTiles) {
+        for (int unit = pair0; unit < pair1; unit += kWideUnit) {
             f32x2 run[cols / 2];
 #pragma unroll
             for (int i = 0; i < cols / 2; ++i) run[i] = pack2(0.f, 0.f);
@@ -496,7 +498,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 copy_wait<kMetaSlots - 2>();
                 __syncwarp();  // every lane's copies are seen, and every lane is done with the chunk before
                 fetch();
-                uint32_t meta_at = ring + slot * kSlotBytes + entry, sum_at = ring + slot * kSlotBytes + 2 * kTileBytes;
+                uint32_t meta_at = ring + slot * kSlotBytes + entry, sum_at = ring + slot * kSlotBytes + kMetaBytes;
                 slot = (slot + 1) % kMetaSlots;
                 const int count = min(kMetaChunk, groups - first);
                 for (int j = 0; j < count; ++j) {
@@ -545,8 +547,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     s.next(p.stages);
                 }
             }
-            const int tile = unit + half * kWideHalfTiles + (row >> 4), v = tile * kQuantTileRows + (row & 15);
-            if (tile < tile1 && v < p.q.V) {
+            const int pair = unit + half * kWideHalf + (row >> 5), v = pair * kQuantPairRows + lane;
+            if (pair < pair1 && v < p.q.V) {
 #pragma unroll
                 for (int i = 0; i < cols / 2; ++i) {
                     float y[2];
@@ -577,7 +579,7 @@ cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int num_sms, cuda
     constexpr int stages = (kWideSmem - 1024 - ring) / stage;
     static_assert(stages >= kWideSlots, "an A operand's last stage is still in the ring when it is waited for");
     p.stages = std::min(kWideMaxStages, stages);
-    return launch_pdl(kernel, dim3(std::min(num_sms, p.q.row_tiles)), dim3(kWideThreads),
+    return launch_pdl(kernel, dim3(std::min(num_sms, p.q.pairs)), dim3(kWideThreads),
                       static_cast<size_t>(p.stages) * stage + ring + 1024, s, maps[0], maps[1], p);
 }
 

@@ -13,13 +13,13 @@ namespace rpd {
 
 constexpr int kQuantMaxD = 32768;       // a row of activations fits a CTA's shared memory
 constexpr int kQuantMaxV = 1 << 24;
-constexpr int kQuantTileRows = 16;      // matrix rows of a tile of the packed codes
-constexpr int kQuantPadTiles = 8;       // tiles are padded to a multiple of this many (128 rows)
+constexpr int kQuantPairRows = 32;      // matrix rows of a pair of tiles of the packed codes
+constexpr int kQuantPadPairs = 4;       // pairs are padded to a multiple of this many (128 rows)
 
 struct QuantParams {
-    const uint4 *codes;  // [row_tiles][blocks][32]
-    const void *meta;    // scales (and zero points), [row_tiles][groups][8][2]
-    int row_tiles;       // tiles of 16 matrix rows that hold a row
+    const uint4 *codes;  // [pairs][blocks][2][32]: a pair's tiles of 16 rows x 64 columns
+    const void *meta;    // scales (and zero points), [pairs][groups][2][8][2]
+    int pairs;           // pairs of tiles that hold a row
     int blocks;          // 64-column blocks of a row, an even number
     int groups;          // groups of a row, padding included
     int d, V;
@@ -181,7 +181,7 @@ __device__ __forceinline__ void store_out(void *out, int type, long long at, flo
 
 // The kernel for more rows (k_quant_wide.cu): as many passes over the codes as there are `kWideMaxRows` rows.
 constexpr int kWideMaxRows = 64;
-// maps: boxes of 8 and of 4 tiles x 128 columns of the packed codes.
+// maps: boxes of 4 and of 2 pairs x 128 columns of the packed codes.
 long long quant_wide_workspace(int rows, int blocks, int groups);
 cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
                        void *workspace, cudaStream_t s);
