@@ -142,8 +142,8 @@ __device__ __forceinline__ void for_chunks(const QuantParams &p, const T *x, int
             const int c = c0 + j * step + (threadIdx.x & 31);
             v[j] = g[j] = make_uint4(0, 0, 0, 0);
             if (c < chunks) {
-                v[j] = load_chunk(x, c * 8, p.d, p.x_vectors);
-                if (gain) g[j] = load_chunk(gain, c * 8, p.d, p.gain_vectors);
+                v[j] = load_chunk(x, c * 8, p.d, p.x_align);
+                if (gain) g[j] = load_chunk(gain, c * 8, p.d, p.gain_align);
             }
         }
 #pragma unroll
@@ -467,6 +467,9 @@ struct rpd_quant {
 
 namespace {
 
+// The largest of 16, 8, 4 and 2 that divides an address (and whatever is or-ed into it).
+int common_align(uintptr_t bits) { return bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16; }
+
 // Boxes of 4 and of 2 pairs x 128 columns of the packed codes.
 int encode_codes(rpd_quant *q) {
     EncodeTiledFn fn = encode_fn();
@@ -621,8 +624,8 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.V = q->V;
     p.gain = gain;
     p.x_stride = x_stride;
-    p.x_vectors = aligned16(x) && (rows == 1 || x_stride % 8 == 0);
-    p.gain_vectors = gain && aligned16(gain);
+    p.x_align = common_align(reinterpret_cast<uintptr_t>(x) | (rows > 1 ? static_cast<uintptr_t>(x_stride) * 2 : 0));
+    p.gain_align = common_align(reinterpret_cast<uintptr_t>(gain));
     p.eps = eps;
     p.out_stride = out_stride;
     p.out_type = out_type;

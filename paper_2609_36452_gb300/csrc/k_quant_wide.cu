@@ -70,8 +70,8 @@ __global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int p
     if (live)
         for (int c = threadIdx.x; c < chunks; c += 256) {
             float2 u[4];
-            ss += make_u<T>(load_chunk(x, c * 8, p.d, p.x_vectors), gain != nullptr,
-                            gain ? load_chunk(gain, c * 8, p.d, p.gain_vectors) : make_uint4(0, 0, 0, 0), u);
+            ss += make_u<T>(load_chunk(x, c * 8, p.d, p.x_align), gain != nullptr,
+                            gain ? load_chunk(gain, c * 8, p.d, p.gain_align) : make_uint4(0, 0, 0, 0), u);
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(u[i].x), fabsf(u[i].y)));
         }
@@ -101,8 +101,8 @@ __global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int p
             uint4 w = make_uint4(0, 0, 0, 0);
             if (live) {
                 float2 u[4];
-                make_u<T>(load_chunk(x, c * 8, p.d, p.x_vectors), gain != nullptr,
-                          gain ? load_chunk(gain, c * 8, p.d, p.gain_vectors) : make_uint4(0, 0, 0, 0), u);
+                make_u<T>(load_chunk(x, c * 8, p.d, p.x_align), gain != nullptr,
+                          gain ? load_chunk(gain, c * 8, p.d, p.gain_align) : make_uint4(0, 0, 0, 0), u);
                 sum = scale_u(u, E, w);
             }
             const long long row = (static_cast<long long>(pass) * p.blocks + c / 8) * n + slot;

@@ -26,7 +26,7 @@ struct QuantParams {
     const void *x;       // [rows] rows, x_stride elements apart
     const void *gain;    // [d] or null
     long long x_stride;
-    int x_type, x_vectors, gain_vectors;  // RPD_TYPE_*; rows (the gain) can be read 16 bytes at a time
+    int x_type, x_align, gain_align;  // RPD_TYPE_*; bytes (16, 8, 4, 2) at whose multiples rows (the gain) begin
     int rows;
     float eps;
     void *out;           // [rows] rows of V, out_stride elements apart
@@ -100,10 +100,19 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t word, int i) {
     return (i < 2 ? word : word >> 8) & (i & 1 ? 0x00F000F0u : 0x000F000Fu);
 }
 
-// Elements [col, col + 8) of a row of d 16-bit elements, zero beyond its end.
+// Elements [col, col + 8) of a row of d 16-bit elements, zero beyond its end; `align`: bytes (16, 8, 4 or 2) at whose
+// multiples every row begins.
 template <typename T>
-__device__ __forceinline__ uint4 load_chunk(const T *row, int col, int d, int vectors) {
-    if (vectors && col + 8 <= d) return *reinterpret_cast<const uint4 *>(row + col);
+__device__ __forceinline__ uint4 load_chunk(const T *row, int col, int d, int align) {
+    if (col + 8 <= d && align > 2) {
+        if (align == 16) return *reinterpret_cast<const uint4 *>(row + col);
+        if (align == 8) {
+            const uint2 *v = reinterpret_cast<const uint2 *>(row + col);
+            return make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+        }
+        const uint32_t *v = reinterpret_cast<const uint32_t *>(row + col);
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
     const uint16_t *e = reinterpret_cast<const uint16_t *>(row);
     uint32_t w[4];
 #pragma unroll
