@@ -223,14 +223,16 @@ def _arg(t, name: str, dtype: str, numel: int = None, cuda: bool = True):
 
 
 _torch_module = None
+_Tensor = None
 _DTYPES = {}  # name -> torch dtype, and torch dtype -> RPD_TYPE_*
 
 
 def _torch():
     """torch, imported by the first call that is given tensors."""
-    global _torch_module
+    global _torch_module, _Tensor
     if _torch_module is None:
         import torch
+        _Tensor = torch.Tensor
         for n in ("bfloat16", "float16", "float32", "int32", "uint8"):
             _DTYPES[n] = getattr(torch, n)
             _DTYPES[getattr(torch, n)] = ELEMENT_TYPES.get("torch." + n)
@@ -241,7 +243,7 @@ def _torch():
 def _rows_arg(t, name: str, types, shape):
     """A CUDA tensor of the given shape whose innermost dimension is contiguous; its outer strides
     (in elements) are the caller's.  Returns (pointer, RPD_TYPE_* or None, strides)."""
-    if t.__class__ is _torch().Tensor and t.is_cuda and t.shape == shape and t.dtype in types:
+    if t.__class__ is _Tensor and t.is_cuda and t.shape == shape and t.dtype in types:
         strides = t.stride()
         if strides[-1] == 1 or shape[-1] <= 1 or not t.numel():
             return t.data_ptr(), _DTYPES[t.dtype], strides
@@ -263,7 +265,7 @@ def _rows_arg(t, name: str, types, shape):
 def _dense_arg(t, name: str, dtype: str, numel: int, device: int):
     """The address of a contiguous CUDA tensor of one device; the same checks as _arg and
     _same_device, in the order that is quickest for a good argument."""
-    if (t.__class__ is _torch().Tensor and t.get_device() == device and t.dtype is _DTYPES[dtype]
+    if (t.__class__ is _Tensor and t.get_device() == device and t.dtype is _DTYPES[dtype]
             and t.is_contiguous() and t.numel() == numel):
         return t.data_ptr()
     _arg(t, name, dtype, numel)
@@ -280,7 +282,7 @@ def _same_device(device: int, **tensors):
 def _stream(device: int):
     """The device's current stream (as torch.cuda.current_stream(device).cuda_stream, without the
     object around it)."""
-    return _torch()._C._cuda_getCurrentRawStream(device)
+    return _torch_module._C._cuda_getCurrentRawStream(device)
 
 
 _DEBUG_DTYPES = {"conf": "float32", "entropy": "float32", "persist": "int32", "drop": "float32",
@@ -601,11 +603,13 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
     pd, ds = None, (0, 0)
     if draft is not None:
         pd, _, ds = _rows_arg(draft, "draft", (target.dtype,), (B, D, V))
-        _same_device(dev, draft=draft)
+        if draft.get_device() != dev:
+            _same_device(dev, draft=draft)
     pn, ns = None, (0,)
     if noise is not None:
         pn, _, ns = _rows_arg(noise, "noise", (T.float32,), (B, V))
-        _same_device(dev, noise=noise)
+        if noise.get_device() != dev:
+            _same_device(dev, noise=noise)
     a = RpdVerifyArgs(
         pt, pd, _dense_arg(tokens, "tokens", "int32", B * D, dev),
         None if lengths is None else _dense_arg(lengths, "lengths", "int32", B, dev),

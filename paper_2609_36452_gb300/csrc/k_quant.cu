@@ -541,6 +541,11 @@ int rpd_quant_set_weights(rpd_quant *q, const void *codes, const void *scales, i
         (zeros && !pointer_usable(zeros, q->device, false)))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "codes, scales and zeros must be device memory on the head's device");
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(s, &capturing);
+    if (e != cudaSuccess) return op_cuda_fail(e, "cudaStreamIsCapturing");
+    if (capturing != cudaStreamCaptureStatusNone)
+        return op_fail(RPD_ERR_INVALID_ARGUMENT, "the weights cannot be set while the stream is being captured");
     const size_t code_bytes = static_cast<size_t>(q->pad_pairs) * q->blocks * 1024;
     const size_t meta_bytes = static_cast<size_t>(q->pad_pairs) * q->groups * (zeros ? 128 : 64);
     // Freeing the previous layout waits for the device: no call may still be reading it.
@@ -549,7 +554,7 @@ int rpd_quant_set_weights(rpd_quant *q, const void *codes, const void *scales, i
     if (q->meta) cudaFree(q->meta);
     q->codes = nullptr;
     q->meta = nullptr;
-    cudaError_t e = cudaMalloc(&q->codes, code_bytes);
+    e = cudaMalloc(&q->codes, code_bytes);
     if (e == cudaSuccess) e = cudaMalloc(&q->meta, meta_bytes);
     if (e == cudaSuccess) {
         const int groups = (q->d + q->group - 1) / q->group;

@@ -90,6 +90,41 @@ def test_refusals_with_a_head():
     h.close()
 
 
+@gpu
+@needs_gpu
+def test_workspace_refusals_and_weights_under_capture():
+    c = make(256, 300, 40, 64, False, False)
+    h = head_of(c)
+    need = rpd.rpd_quant_workspace(h.handle, 40)
+    assert need > 0 and rpd.rpd_quant_workspace(h.handle, 16) == 0 and rpd.rpd_quant_workspace(h.handle, -1) == -1
+    ws = torch.zeros(need + 256, dtype=torch.uint8, device="cuda")
+    for bad in (ws[:need - 1], ws[8:], ws.cpu(), ws.int()):
+        with pytest.raises(rpd.RpdError) as e:
+            h.logits(c["x"], c["out"], workspace=bad)
+        assert e.value.code == rpd.RPD_ERR_INVALID_ARGUMENT
+    assert rpd.rpd_quant_logits(h.handle, c["x"].data_ptr(), 0, 256, 40, None, 0.0, c["out"].data_ptr(), 2, 300, None, 0,
+                                None) == rpd.RPD_ERR_INVALID_ARGUMENT
+    torch.cuda.synchronize()
+    assert (c["buffer"] == 77).all()
+    ws.fill_(0xFF)  # whatever the workspace holds
+    h.logits(c["x"], c["out"], workspace=ws)
+    torch.cuda.synchronize()
+    check(c)
+    # new weights wait for the device, which a capture forbids: refused, and the old ones stay
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c["out"].zero_()
+        with pytest.raises(rpd.RpdError) as e:
+            h.set_weights(c["codes"], c["scales"])
+        h.logits(c["x"], c["out"])
+    assert e.value.code == rpd.RPD_ERR_INVALID_ARGUMENT
+    g.replay()
+    torch.cuda.synchronize()
+    check(c)
+    del g
+    h.close()
+
+
 # ------------------------------------------------------------------------------ numerics
 
 def make(d, V, rows, group, zeros, norm, x="bf16", out="f32", scale="bf16", pad=0, seed=0):
@@ -232,6 +267,31 @@ def test_a_row_that_is_not_finite_stays_alone(rows):
     keep = [r for r in range(rows) if r != 1]
     assert torch.equal(c["out"][keep], before[keep])
     assert torch.isnan(c["out"][1]).all()
+    h.close()
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("rows", [5, 20])
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+def test_rows_of_any_magnitude(rows, x):
+    """Activations from the type's smallest to its largest numbers, rows of zeros, and rows whose elements
+    span its range: a power of two a row brings them into the tensor core's."""
+    c = make(192, 260, rows, 64, True, False, x=x)
+    low, high = (-120, 100) if x == "bf16" else (-20, 8)
+    power = torch.linspace(low, high, rows, device="cuda").round()
+    c["x"].copy_((torch.randn(rows, 192, device="cuda").double() * torch.exp2(power.double())[:, None]).to(TYPES[x]))
+    c["x"][1] = 0
+    c["x"][2] = torch.exp2(torch.linspace(low, high, 192, device="cuda").round()).to(TYPES[x])
+    c["x"][3] = 0
+    c["x"][3, 77] = torch.finfo(TYPES[x]).max
+    h = head_of(c)
+    c["scales"].mul_(2.0 ** -10)
+    h.set_weights(c["codes"], c["scales"], c["zeros"])
+    h.logits(c["x"], c["out"])
+    torch.cuda.synchronize()
+    assert (c["out"][1] == 0).all()
+    check(c)
     h.close()
 
 

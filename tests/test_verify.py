@@ -234,6 +234,9 @@ SHAPES = [
     (64, 5, 3000, "bf16", True, 8, True, False, 0),
     (33, 0, 5000, "f32", False, 5, False, True, 2),
     (1, 257, 300, "f32", False, 0, False, False, 0),
+    (1, 1024, 40, "bf16", True, 0, False, True, 0),
+    (40, 3, 2000, "f16", True, 7, True, False, 0),
+    (200, 0, 900, "f32", False, 9, False, False, 1),
     (2, 5, 50021, "bf16", True, 0, False, True, 3),
     (1, 5, 126464, "bf16", True, 0, False, False, 0),
     (3, 2, 152064, "f32", True, 0, False, False, 0),
@@ -359,6 +362,32 @@ def test_bad_lengths_temperatures_and_tokens_end_a_sequence_not_the_call():
     n.noise = None
     got = n.run()
     assert got["status"].tolist() == [0, 1]
+
+
+@gpu
+@needs_gpu
+def test_nothing_drafted():
+    """D = 0: rows that are empty or hold no number, offsets of logits that grow along the row, lengths that are
+    not 0, and temperatures, as with drafts."""
+    c = Case(9, 0, 777, "bf16", False, allowed=True)
+    c.temperature.copy_(torch.tensor([1.0, 0.0, 1.0, 0.0, 1.0, 1e-30, math.inf, -1.0, 1.0]))
+    c.target[2, 0, 776] = math.nan
+    c.on[2, 0, 776] = True
+    c.target[3, 0, 5] = math.inf
+    c.on[3, 0, 5] = True
+    c.on[4] = False
+    c.target[5, 0, 388] = 1000.0
+    c.pack()
+    c.lengths = torch.tensor([0, 0, 0, 0, 0, 0, 0, 0, 1], dtype=torch.int32, device="cuda")
+    got = c.run()
+    assert got["status"].tolist() == [0, 0, 1, 1, 1, 0, 0, 1, 1]
+    assert (got["accepted"] == 0).all() and got["token"][5, 0] == 388
+    assert (got["token"][got["status"] == 1] == -1).all()
+    d = Case(3, 0, 60000, "f32", False)
+    d.target += torch.linspace(-300, 300, 60000, device="cuda")  # the maximum rises in every thread's part
+    d.check(d.run())
+    d.target.copy_(d.target.flip(2))
+    d.check(d.run())
 
 
 @gpu
