@@ -7,24 +7,26 @@
 // u = rn(g * x) in the activations' type and rho_r = (mean_k x^2 + eps)^-1/2, applied after the
 // sum, as the 16-bit head does it.
 //
-// Precision.  Codes enter the tensor core as fp16 subnormals q 2^-24, which costs one AND for two of them
-// (a shift more for the upper four of a word), activations as fp16 numbers that a power of two a row has
-// brought into range (quant_internal.h: scale_u).  Products and sums of a group are fp32, the zero point's
-// part -z sum u is what the sum starts from, and a group's sum is multiplied by its scale and added to the
-// row's in fp32: nothing is rounded into the weights.
+// Precision.  A pair of codes, masked in place, is two fp16 subnormals q 2^-24 (or 2^-20), and one fused multiply-add
+// makes (q - z) 2^-9 of both, exactly.  Activations are fp16 numbers that a power of two a row has brought into range
+// (quant_internal.h: scale_u).  Products and sums of a group are fp32, and a group's sum is multiplied by its scale and
+// added to the row's in fp32: nothing is rounded into the weights.  One row's logits are up to 1.3e-7 of their norm off.
+// (Without the multiply-add, the subnormals themselves to the tensor core and the zero point's part -z sum u added to
+// the sum, it was up to 1.7e-6: the tensor core lines its addends up by the operands' exponents, and a
+// subnormal's has up to ten places less than that says.  It was no faster.)
 //
-// What bounds it: reading the codes once (one row of a 126464 x 4096 head is 259 MB of codes and 8 MB of
-// scales: 39 us), if the instructions a code costs stay below.  As bf16 numbers 128 + q less 128 + z (three
-// instructions a pair, 87 for 512 bytes of codes in all) they took 66 us.
+// What bounds it: reading the codes once.  One row of a 126464 x 4096 head in groups of 128 is 259 MB of codes and 8 MB
+// of scales, 39.4 us at 6780 GB/s; it takes 45.5 (5.9 TB/s), 8 rows 49.3, 9 rows 65.6, 16 rows 67.3.  As bf16 numbers
+// 128 + q less 128 + z (three instructions a pair of codes, 87 for 512 bytes in all) one row took 66 us.
 //
 // k_quant_rows: up to 16 rows (more: k_quant_wide.cu).  A warp multiplies pairs of tiles of 16 matrix rows (M of the
 // m16n8k16 MMA) by 8 or 16 activation rows (N), so that a fragment of codes is used for all of these, and a
-// fragment of activations for both tiles, from registers (with one tile at a time shared memory was the limit: 52.6
-// us).  The codes are stored in fragment order, 1 KB for 32 rows x 64 columns, which a warp copies through a
-// ring of its own in shared memory (asked for in registers instead, the copies in flight are
-// limited by the six scoreboards of a warp: 66 us again).  A CTA owns a range of pairs and its warps
-// divide the range's column blocks evenly, over their borders: a pair's sums then may come from
-// several warps and are joined in shared memory in warp order.
+// fragment of activations for both tiles, from registers (with one tile at a time the reads of shared memory were the
+// limit: 52.6 us).  The codes are stored in fragment order, 1 KB for 32 rows x 64 columns, which a warp copies through
+// a ring of its own in shared memory (asked for in registers instead, the copies in flight are limited by the six
+// scoreboards of a warp: 66 us again).  A CTA owns a range of pairs and its warps divide the range's column blocks
+// evenly, over their borders: a pair's sums then may come from several warps and are joined in shared memory in
+// warp order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -73,7 +75,7 @@ __global__ void k_quant_pack(const uint8_t *codes, uint4 *packed, int V, int d, 
 }
 
 // Scales (and zero points) in the order of the pairs: [pair][group][tile][g][2] for rows g and g + 8 of a tile.
-// With zero points an entry is 32 bits: the scale, and the zero point as a bf16 number in the upper half.
+// With zero points an entry is 32 bits: the scale, and in the upper half -z 2^-9 in fp16.
 template <bool kZeros>
 __global__ void k_quant_pack_scales(const uint16_t *scales, const uint8_t *zeros, void *packed, int V, int groups,
                                     int pairs, int padded_groups) {
@@ -88,7 +90,7 @@ __global__ void k_quant_pack_scales(const uint16_t *scales, const uint8_t *zeros
         const uint32_t s = in ? scales[at] : 0u;
         if (kZeros)
             static_cast<uint32_t *>(packed)[i] =
-                s | static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(in ? zeros[at] & 15 : 0))) << 16;
+                s | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(in ? (zeros[at] & 15) * -0x1p-9f : 0.f))) << 16;
         else
             static_cast<uint16_t *>(packed)[i] = static_cast<uint16_t>(s);
     }
@@ -118,13 +120,12 @@ __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The launch's activations in shared memory: rows of `row_bytes` as scale_u leaves them, zero beyond column
-// d; sums[group][n] of a group's elements times 2^-24 (rows rounded up to an even number); and what a
-// row's logits are multiplied with.  The warps divide the rows, or a row, evenly.  Ends with a barrier.
+// The launch's activations in shared memory: rows of `row_bytes` as scale_u leaves them, zero beyond column d; and
+// what a row's logits are multiplied with.  The warps divide the rows, or a row, evenly.  Ends with a barrier.
 struct RowsSmem {
     uint8_t *x;
-    float *sums, *factor, *red;
-    int row_bytes, sum_rows;
+    float *factor, *red;
+    int row_bytes;
 };
 
 // f(chunk index, u) for the chunks of 8 columns of a row that fall to this lane: 32 neighbouring chunks a
@@ -152,12 +153,7 @@ __device__ __forceinline__ void for_chunks(const QuantParams &p, const T *x, int
     }
 }
 
-// Floats of the sums, what follows them aligned to 64 bytes.
-__host__ __device__ constexpr size_t sums_floats(int rows, int groups) {
-    return (static_cast<size_t>((rows + 1) & ~1) * groups + 15) & ~size_t(15);
-}
-
-template <typename T, int kGroup>
+template <typename T>
 __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
     const int chunks = p.blocks * 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -199,11 +195,8 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
                        float2 u[4];
                        uint4 w;
                        make_u<T>(v, p.gain != nullptr, g, u);
-                       float sum = scale_u(u, E, w);
+                       scale_u<false>(u, E, w);
                        if (c < chunks) *reinterpret_cast<uint4 *>(xs + c * 16) = w;
-#pragma unroll
-                       for (int o = 1; o < kGroup / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                       if (c < chunks && c % (kGroup / 8) == 0) s.sums[c / (kGroup / 8) * s.sum_rows + r] = sum;
                    });
     }
     __syncthreads();
@@ -221,7 +214,7 @@ __device__ __forceinline__ void store_pair(const QuantParams &p, int pair, const
             for (int i = 0; i < 4; ++i) {
                 const int r = n * 8 + 2 * t + (i & 1), v = pair * kQuantPairRows + which * 16 + g + (i >> 1) * 8;
                 if (r < p.rows && v < p.V)
-                    store_out(p.out, p.out_type, r * p.out_stride + v, run[which][n][i] * kRowFactor * factor[r]);
+                    store_out(p.out, p.out_type, r * p.out_stride + v, run[which][n][i] * kWeightFactor * factor[r]);
             }
 }
 
@@ -248,9 +241,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     // a row and 64 bytes: the two rows that a quarter of a warp reads at once lie in different banks
     sm.row_bytes = p.blocks * 128 + 64;
-    sm.sum_rows = (p.rows + 1) & ~1;
-    sm.sums = sm.factor + 16;
-    uint8_t *ring = reinterpret_cast<uint8_t *>(sm.sums + sums_floats(p.rows, p.groups));
+    uint8_t *ring = reinterpret_cast<uint8_t *>(sm.factor + 16);
     sm.x = ring + kRowsWarps * depth * Stage::kBytes;
     float *join = reinterpret_cast<float *>(sm.x);  // [warp][8 kN8][lane], when nobody reads the activations any more
 
@@ -287,9 +278,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 
     pdl_wait();  // the weights were laid out long ago; the activations may be the predecessor's
     if (p.x_type == RPD_TYPE_BF16)
-        stage_rows<__nv_bfloat16, kGroup>(p, sm);
+        stage_rows<__nv_bfloat16>(p, sm);
     else
-        stage_rows<__half, kGroup>(p, sm);
+        stage_rows<__half>(p, sm);
 
     float run[2][kN8][4], first[2][kN8][4];  // first: of a pair that an earlier warp began
 #pragma unroll
@@ -299,13 +290,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     bool head = joins;  // the pair at hand was begun by an earlier warp
     // Lanes of activations beyond the last read the last one's elements: their columns of the result
     // are never stored.
-    uint32_t xrow[kN8], srow[kN8];
+    uint32_t xrow[kN8];
 #pragma unroll
-    for (int n = 0; n < kN8; ++n) {
+    for (int n = 0; n < kN8; ++n)
         xrow[n] = smem_u32(sm.x) + min(n * 8 + g, p.rows - 1) * sm.row_bytes + t * 16;
-        srow[n] = smem_u32(sm.sums) + min(n * 8 + 2 * t, sm.sum_rows - 2) * 4;
-    }
-    const uint32_t sum_step = sm.sum_rows * 4;
 
     int slot = 0, refill = depth - 1;
     for (int u = u0; u < u1; u += Stage::kUnits) {
@@ -327,21 +315,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 #pragma unroll
                 for (int k = 0; k < kUnitGroups; ++k) {
                     float s_lo[2], s_hi[2], c[2][kN8][4];
+                    uint32_t z_lo[2], z_hi[2];
 #pragma unroll
-                    for (int n = 0; n < kN8; ++n) {
-                        const uint2 sum = lds64(srow[n] + (in_pair * kUnitGroups + k) * sum_step);
+                    for (int which = 0; which < 2; ++which) {
+                        Meta m;
+                        lds_meta(stage + Stage::kCodeBytes + (((j * kUnitGroups + k) * 2 + which) * 8 + g) * sizeof(Meta), m);
+                        unpack_meta<kF16>(m, s_lo[which], s_hi[which], z_lo[which], z_hi[which]);
 #pragma unroll
-                        for (int which = 0; which < 2; ++which) {
-                            float z_lo, z_hi;
-                            Meta m;
-                            lds_meta(stage + Stage::kCodeBytes +
-                                         (((j * kUnitGroups + k) * 2 + which) * 8 + g) * sizeof(Meta), m);
-                            unpack_meta<kF16>(m, s_lo[which], s_hi[which], z_lo, z_hi);
-                            c[which][n][0] = -z_lo * __uint_as_float(sum.x);
-                            c[which][n][1] = -z_lo * __uint_as_float(sum.y);
-                            c[which][n][2] = -z_hi * __uint_as_float(sum.x);
-                            c[which][n][3] = -z_hi * __uint_as_float(sum.y);
-                        }
+                        for (int n = 0; n < kN8; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) c[which][n][i] = 0.f;
                     }
                     // 32-column halves of this group: (block, half); a fragment of activations for both tiles
 #pragma unroll
@@ -358,8 +341,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
                             const uint32_t lo = half ? q[which].y : q[which].x, hi = half ? q[which].w : q[which].z;
 #pragma unroll
                             for (int step = 0; step < 2; ++step) {
-                                const uint32_t a[4] = {code_pair(lo, 2 * step), code_pair(hi, 2 * step),
-                                                       code_pair(lo, 2 * step + 1), code_pair(hi, 2 * step + 1)};
+                                const uint32_t a[4] = {
+                                    weight_pair(lo, 2 * step, z_lo[which]), weight_pair(hi, 2 * step, z_hi[which]),
+                                    weight_pair(lo, 2 * step + 1, z_lo[which]), weight_pair(hi, 2 * step + 1, z_hi[which])};
 #pragma unroll
                                 for (int n = 0; n < kN8; ++n)
                                     mma_16816(c[which][n], a, step ? xv[n].z : xv[n].x, step ? xv[n].w : xv[n].y);
@@ -411,12 +395,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 }
 
 constexpr int kRowsMax = 16;                 // activation rows of a launch
-constexpr int kRowsMost = 16;                // more are the other kernel's
+// More rows are the other kernel's.  126464 x 4096: 16 rows 67.3 us here (92 there), 17 rows 92.6 there (two launches
+// here: 113); 15872 x 4096: 22.0 (27), and 27.4 (33).
+constexpr int kRowsMost = 16;
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 
 // Shared memory besides the ring of codes (the activations' part is big enough for the partial sums that follow).
-size_t rows_smem(int n8, int rows, int blocks, int groups) {
-    return (2 * 16 * kRowsWarps + 16 + sums_floats(rows, groups)) * 4 +
+size_t rows_smem(int n8, int rows, int blocks) {
+    return (2 * 16 * kRowsWarps + 16) * 4 +
            std::max(static_cast<size_t>(rows) * (blocks * 128 + 64), static_cast<size_t>(kRowsWarps) * 8 * n8 * 32 * 4);
 }
 
@@ -428,7 +414,7 @@ cudaError_t launch_rows(const QuantParams &p, int num_sms, cudaStream_t s) {
     // (cheap, and per device: set on every call)
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem);
     if (e != cudaSuccess) return e;
-    const size_t fixed = rows_smem(kN8, p.rows, p.blocks, p.groups);
+    const size_t fixed = rows_smem(kN8, p.rows, p.blocks);
     const int stage = kRowsWarps * RowsStage<kGroup, kZeros>::kBytes;
     const int fits = static_cast<int>((kRowsSmem - fixed) / stage);
     const int depth = fits >= 6 ? 6 : fits >= 4 ? 4 : 2;
@@ -642,9 +628,9 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
         const cudaError_t e = quant_wide(q->maps, p, q->group, q->zeros, q->scale_f16, q->num_sms, workspace, s);
         return e == cudaSuccess ? RPD_OK : op_cuda_fail(e, "4-bit head launch");
     }
-    // as many rows a launch as their activations fit into shared memory (at d = 32768 it is one)
+    // as many rows a launch as their activations fit into shared memory (16 up to d = 4096, one at d = 32768)
     int most = kRowsMax;
-    while (rows_smem(most > 8 ? 2 : 1, most, q->blocks, q->groups) + kRowsRing > kRowsSmem) --most;
+    while (rows_smem(most > 8 ? 2 : 1, most, q->blocks) + kRowsRing > kRowsSmem) --most;
     for (int r = 0; r < rows; r += most) {
         p.rows = std::min(most, rows - r);
         p.x = static_cast<const uint16_t *>(x) + r * x_stride;

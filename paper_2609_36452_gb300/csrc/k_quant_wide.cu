@@ -4,13 +4,20 @@
 // The codes of 128 matrix rows are the MMA's A operand (M), read from tensor memory where four warps have
 // put them as fp16 subnormals, a thread a matrix row; the activations are B (N: 32 or 64 of them a pass), as
 // scale_u leaves them, staged in shared memory with 128-byte swizzling.  A group's product is summed in
-// TMEM; eight other warps read it, take the zero point's part off, and add it, scaled, to running sums in
-// registers, so that scales and zero points stay exact as in the kernel for few rows.
+// TMEM; eight other warps read it, take the zero point's part -z sum u off, and add it, scaled, to running sums in
+// registers, so that scales and zero points stay exact as in the kernel for few rows.  (Subnormals cost the
+// tensor core's sums some places, see there: 17 and more rows are up to 9.3e-7 of their norm off.)
 //
 // A CTA (one an SM, persistent) owns a contiguous range of pairs of 16-row tiles and works on 256 rows at a time, as two
 // halves that share every stage of activations: a stage is 128 columns of both (16 KB of codes, 8 or 16 KB of
-// activations).  What bounds it is the instructions that a stage costs each role, a few hundred one after the other
-// whatever the stage's height: with 128 rows at a time a pass took as long a stage, with twice as many stages.
+// activations).
+//
+// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us, 17 rows take 92.8, 32 rows 94.6, 33 rows 104, 64
+// rows 108), nor the tensor cores (an MMA of M = 128 and N = 32 / 64 with A in TMEM takes 18 / 32 cycles, 15 us a
+// pass in all), but what a stage costs its roles one after the other: 1550 cycles where the codes' share of HBM is
+// 700.  Leaving out the stores to TMEM, 22 us of it go, the epilogue's arithmetic 6, the MMAs 5; copies and
+// hand-overs alone take 59 us.  Tried and no faster: two sets of warps for the codes, two issuers, three operands in
+// flight, 128 rows at a time with six operands in flight (109 us).
 //
 // Roles: warps 0-3 codes to TMEM (lanes by warp % 4), warps 4-11 epilogue (half = warp / 4 - 1), warps 12 and 13 TMA (codes;
 // activations), warp 14 MMA issue and TMEM.  Every wait is bounded; where one runs out the CTA's remaining logits
@@ -103,7 +110,7 @@ __global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int p
                 float2 u[4];
                 make_u<T>(load_chunk(x, c * 8, p.d, p.x_align), gain != nullptr,
                           gain ? load_chunk(gain, c * 8, p.d, p.gain_align) : make_uint4(0, 0, 0, 0), u);
-                sum = scale_u(u, E, w);
+                sum = scale_u<true>(u, E, w);
             }
             const long long row = (static_cast<long long>(pass) * p.blocks + c / 8) * n + slot;
             *reinterpret_cast<uint4 *>(xs + row * 128 + ((c % 8) ^ (slot % 8)) * 16) = w;
@@ -249,7 +256,7 @@ __device__ __forceinline__ void row_meta(uint32_t at, float &scale, float &minus
     if (kZeros) {
         const uint32_t m = lds32(at);
         scale = scale_low<kF16>(m);
-        minus_zero = -__uint_as_float(m & 0xFFFF0000u);
+        minus_zero = minus_zero_value(m);
     } else {
         scale = scale_low<kF16>(lds16(at));
         minus_zero = -8.f;
@@ -558,7 +565,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         const int r = 2 * i + k;
                         if (r < p.q.rows)
                             store_out(p.q.out, p.q.out_type, r * p.q.out_stride + v,
-                                      ok ? y[k] * kRowFactor * factor[r] : __int_as_float(0x7FFFFFFF));
+                                      ok ? y[k] * kCodeFactor * factor[r] : __int_as_float(0x7FFFFFFF));
                     }
                 }
             }
@@ -609,7 +616,8 @@ cudaError_t launch_x(const QuantParams &p, int per_pass, int n, int passes, uint
                             factor);
 }
 
-// Passes over the codes, their rows and what these are padded to.
+// Passes over the codes, their rows and what these are padded to (as 64, 32 rows of the 126464 x 4096 head take 103
+// us in place of 94.6).
 struct WidePasses {
     int passes, per_pass, n;
     explicit WidePasses(int rows) {

@@ -77,27 +77,39 @@ __device__ __forceinline__ float scale_high(uint32_t word) {
     return kF16 ? __high2float(*reinterpret_cast<const __half2 *>(&word)) : __uint_as_float(word & 0xFFFF0000u);
 }
 
-// Scales of rows g and g + 8 of a tile, and their zero points (8 where none are stored).  A stored zero
-// point is a bf16 number in the upper half of its row's word.
+// Scales of rows g and g + 8 of a tile, and -z 2^-9 twice as fp16 (z = 8 where no zero points are stored).  A stored
+// zero point is that fp16 number in the upper half of its row's word.
+constexpr uint32_t kMinusZeroDefault = 0xA400A400u;  // -2^-6 twice
+
 template <bool kF16>
-__device__ __forceinline__ void unpack_meta(uint32_t m, float &s_lo, float &s_hi, float &z_lo, float &z_hi) {
+__device__ __forceinline__ void unpack_meta(uint32_t m, float &s_lo, float &s_hi, uint32_t &z_lo, uint32_t &z_hi) {
     s_lo = scale_low<kF16>(m);
     s_hi = scale_high<kF16>(m);
-    z_lo = z_hi = 8.f;
+    z_lo = z_hi = kMinusZeroDefault;
 }
 template <bool kF16>
-__device__ __forceinline__ void unpack_meta(uint2 m, float &s_lo, float &s_hi, float &z_lo, float &z_hi) {
+__device__ __forceinline__ void unpack_meta(uint2 m, float &s_lo, float &s_hi, uint32_t &z_lo, uint32_t &z_hi) {
     s_lo = scale_low<kF16>(m.x);
     s_hi = scale_low<kF16>(m.y);
-    z_lo = __uint_as_float(m.x & 0xFFFF0000u);
-    z_hi = __uint_as_float(m.y & 0xFFFF0000u);
+    z_lo = __byte_perm(m.x, 0, 0x3232);
+    z_hi = __byte_perm(m.y, 0, 0x3232);
+}
+__device__ __forceinline__ float minus_zero_value(uint32_t m) {  // -z, of a row's word
+    return 512.f * __high2float(*reinterpret_cast<const __half2 *>(&m));
 }
 
-// Pair i (columns 2i, 2i + 1) of a word of codes as two fp16 numbers: masked in place, they are the
-// subnormals q 2^-24 (pairs 0 and 2) and q 2^-20 (1 and 3) - exact, and for the tensor core numbers like any
-// others.  Activations of the odd pairs carry the missing 2^-4.
+// Pair i (columns 2i, 2i + 1) of a word of codes as two fp16 numbers: masked in place, they are the subnormals q 2^-24
+// (pairs 0 and 2) and q 2^-20 (1 and 3), exact.
 __device__ __forceinline__ uint32_t code_pair(uint32_t word, int i) {
     return (i < 2 ? word : word >> 8) & (i & 1 ? 0x00F000F0u : 0x000F000Fu);
+}
+
+// The pair as (q - z) 2^-9, exact too (one fused multiply-add for both).
+__device__ __forceinline__ uint32_t weight_pair(uint32_t word, int i, uint32_t minus_zero) {
+    const uint32_t q = code_pair(word, i), up = i & 1 ? 0x68006800u : 0x78007800u;  // 2^11, 2^15
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2 *>(&q), *reinterpret_cast<const __half2 *>(&up),
+                              *reinterpret_cast<const __half2 *>(&minus_zero));
+    return *reinterpret_cast<const uint32_t *>(&r);
 }
 
 // Elements [col, col + 8) of a row of d 16-bit elements, zero beyond its end; `align`: bytes (16, 8, 4 or 2) at whose
@@ -156,9 +168,10 @@ __device__ __forceinline__ float make_u(const uint4 &x, bool has_gain, const uin
 // The power of two at or below x (1 for 0).
 __device__ __forceinline__ int exponent_of(float x) { return x > 0.f ? ilogbf(x) : 0; }
 
-// Activations as the tensor core gets them: u 2^(14 - E) in fp16, E the exponent of the row's largest u, and
-// the odd pairs 2^-4 of that.  Exact from 2^-24 of the largest element on; a smaller one is off by at
-// most 2^-35 of the largest.  Returns the sum of the eight elements as they then are, times 2^-24.
+// Activations as the tensor core gets them: u 2^(14 - E) in fp16, E the exponent of the row's largest u.  Exact from 2^-24
+// of the largest element on; a smaller one is off by at most 2^-35 of the largest.  With kOddLess the odd pairs,
+// whose codes are 2^4 too large, are 2^-4 of that.  Returns the sum of the eight elements before that, times 2^-24.
+template <bool kOddLess>
 __device__ __forceinline__ float scale_u(const float2 (&u)[4], int E, uint4 &out) {
     const int e = 14 - E;  // in two factors: the power itself may lie outside fp32
     const float f0 = ldexpf(1.f, e / 2), f1 = ldexpf(1.f, e - e / 2);
@@ -166,18 +179,18 @@ __device__ __forceinline__ float scale_u(const float2 (&u)[4], int E, uint4 &out
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float f = i & 1 ? f1 * 0.0625f : f1;
+        const float f = kOddLess && (i & 1) ? f1 * 0.0625f : f1;
         const __half2 h = __floats2half2_rn(u[i].x * f0 * f, u[i].y * f0 * f);
         const float2 v = __half22float2(h);
-        sum += (v.x + v.y) * (i & 1 ? 16.f : 1.f);
+        sum += (v.x + v.y) * (kOddLess && (i & 1) ? 16.f : 1.f);
         w[i] = *reinterpret_cast<const uint32_t *>(&h);
     }
     out = make_uint4(w[0], w[1], w[2], w[3]);
     return sum * 0x1p-24f;
 }
 
-// What a row's sums are multiplied with, in two factors: 2^10 and 2^E rho.
-constexpr float kRowFactor = 1024.f;
+// What a row's sums are multiplied with besides 2^E rho: with weights (q - z) 2^-9, and with codes q 2^-24.
+constexpr float kWeightFactor = 0.03125f, kCodeFactor = 1024.f;
 
 __device__ __forceinline__ void store_out(void *out, int type, long long at, float v) {
     if (type == RPD_TYPE_F32)
