@@ -360,8 +360,8 @@ void rpd_destroy(rpd_ctx *ctx);
  *
  * with u = x and rho = 1, or, with a gain g, the readout's normalisation as rpd_step applies it:
  * u = g * x rounded to the type of x, rho_r = (mean_k x[r][k]^2 + eps)^(-1/2) applied after the
- * sum.  Codes, zero points and scales enter exactly, u with at least 24 binary places below the row's
- * largest (a smaller element is off by at most 2^-35 of that); products and sums are fp32, and the logits
+ * sum.  Codes, zero points and scales enter exactly, u exactly down to 2^-28 of the row's
+ * largest (a smaller element is off by at most 2^-39 of that); products and sums are fp32, and the logits
  * are rounded once, to the type of `out`.  Inputs must be finite.
  *
  * rpd_quant_create: a head of d columns and V rows with groups of 32, 64 or 128 columns (others:

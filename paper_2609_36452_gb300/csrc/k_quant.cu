@@ -10,9 +10,9 @@
 // Precision.  A pair of codes, masked in place, is two fp16 subnormals q 2^-24 (or 2^-20), and one fused multiply-add
 // makes (q - z) 2^-9 of both, exactly.  Activations are fp16 numbers that a power of two a row has brought into range
 // (quant_internal.h: scale_u).  Products and sums of a group are fp32, and a group's sum is multiplied by its scale and
-// added to the row's in fp32: nothing is rounded into the weights.  One row's logits are up to 1.3e-7 of their norm off.
+// added to the row's in fp32: nothing is rounded into the weights.  Logits of d = 4096 are up to 1.3e-7 of their norm off.
 // (Without the multiply-add, the subnormals themselves to the tensor core and the zero point's part -z sum u added to
-// the sum, it was up to 1.7e-6: the tensor core lines its addends up by the operands' exponents, and a
+// the sum, they were up to 1.7e-6 off: the tensor core lines its addends up by the operands' exponents, and a
 // subnormal's has up to ten places less than that says.  It was no faster.)
 //
 // What bounds it: reading the codes once.  One row of a 126464 x 4096 head in groups of 128 is 259 MB of codes and 8 MB
@@ -195,7 +195,7 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
                        float2 u[4];
                        uint4 w;
                        make_u<T>(v, p.gain != nullptr, g, u);
-                       scale_u<false>(u, E, w);
+                       scale_u(u, E, w);
                        if (c < chunks) *reinterpret_cast<uint4 *>(xs + c * 16) = w;
                    });
     }
@@ -395,8 +395,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 }
 
 constexpr int kRowsMax = 16;                 // activation rows of a launch
-// More rows are the other kernel's.  126464 x 4096: 16 rows 67.3 us here (92 there), 17 rows 92.6 there (two launches
-// here: 113); 15872 x 4096: 22.0 (27), and 27.4 (33).
+// More rows are the other kernel's.  126464 x 4096: 16 rows 67.3 us here (95 there), 17 rows 95.5 there (two launches
+// here: 113); 15872 x 4096: 22.0 (27), and 26.6 (33).
 constexpr int kRowsMost = 16;
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 
@@ -575,7 +575,7 @@ int64_t rpd_quant_workspace(const rpd_quant *q, int rows) {
         op_fail(RPD_ERR_INVALID_ARGUMENT, "null head or negative rows");
         return -1;
     }
-    return rows > kRowsMost ? quant_wide_workspace(rows, q->blocks, q->groups) : 0;
+    return rows > kRowsMost ? quant_wide_workspace(rows, q->blocks) : 0;
 }
 
 int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_stride, int rows, const void *gain,
@@ -628,7 +628,7 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
         const cudaError_t e = quant_wide(q->maps, p, q->group, q->zeros, q->scale_f16, q->num_sms, workspace, s);
         return e == cudaSuccess ? RPD_OK : op_cuda_fail(e, "4-bit head launch");
     }
-    // as many rows a launch as their activations fit into shared memory (16 up to d = 4096, one at d = 32768)
+    // as many rows a launch as their activations fit into shared memory (16 up to d = 4096, two at d = 32768)
     int most = kRowsMax;
     while (rows_smem(most > 8 ? 2 : 1, most, q->blocks) + kRowsRing > kRowsSmem) --most;
     for (int r = 0; r < rows; r += most) {

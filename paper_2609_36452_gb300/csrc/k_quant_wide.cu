@@ -1,25 +1,29 @@
 // k_quant_wide.cu - the 4-bit head for more than a few activations: the same sums as k_quant_rows
 // (k_quant.cu), on the fifth-generation tensor cores.
 //
-// The codes of 128 matrix rows are the MMA's A operand (M), read from tensor memory where four warps have
-// put them as fp16 subnormals, a thread a matrix row; the activations are B (N: 32 or 64 of them a pass), as
-// scale_u leaves them, staged in shared memory with 128-byte swizzling.  A group's product is summed in
-// TMEM; eight other warps read it, take the zero point's part -z sum u off, and add it, scaled, to running sums in
-// registers, so that scales and zero points stay exact as in the kernel for few rows.  (Subnormals cost the
-// tensor core's sums some places, see there: 17 and more rows are up to 9.3e-7 of their norm off.)
+// The weights of 128 matrix rows are the MMA's A operand (M), read from tensor memory where four warps have put
+// (q - z) 2^-9 as fp16, exactly, a thread a matrix row; the activations are B (N: 32 or 64 of them a pass), as scale_u
+// leaves them, staged in shared memory with 128-byte swizzling.  A group's product is summed in TMEM; eight other
+// warps read it and add it, scaled, to running sums in registers, so that scales stay exact as in the kernel for few
+// rows.
 //
 // A CTA (one an SM, persistent) owns a contiguous range of pairs of 16-row tiles and works on 256 rows at a time, as two
 // halves that share every stage of activations: a stage is 128 columns of both (16 KB of codes, 8 or 16 KB of
 // activations).
 //
-// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us, 17 rows take 92.8, 32 rows 94.6, 33 rows 104, 64
-// rows 108), nor the tensor cores (an MMA of M = 128 and N = 32 / 64 with A in TMEM takes 18 / 32 cycles, 15 us a
-// pass in all), but what a stage costs its roles one after the other: 1550 cycles where the codes' share of HBM is
-// 700.  Leaving out the stores to TMEM, 22 us of it go, the epilogue's arithmetic 6, the MMAs 5; copies and
-// hand-overs alone take 59 us.  Tried and no faster: two sets of warps for the codes, two issuers, three operands in
-// flight, 128 rows at a time with six operands in flight (109 us).
+// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us; 17 rows take 95.5, 32 rows 98.1, 33 rows 107, 64
+// rows 111, and with stored zero points 20 rows 105), nor the tensor cores (an MMA of M = 128 and N = 32 / 64 with A in
+// TMEM takes 18 / 32 cycles, 15 us a pass in all), but what a stage costs its roles one after the other: 1550 cycles
+// where the codes' share of HBM is 700.  Of 93 us, measured when the operand still was the masked codes, 22 went without
+// the stores to TMEM, 6 without the epilogue's arithmetic, 5 without the MMAs; copies and hand-overs alone took 59.
+// Tried and no faster: two sets of warps for the operand, two issuers, three operands in flight, 128 rows at a time
+// with six in flight (109 us).
 //
-// Roles: warps 0-3 codes to TMEM (lanes by warp % 4), warps 4-11 epilogue (half = warp / 4 - 1), warps 12 and 13 TMA (codes;
+// (The masked codes themselves as subnormal operands, and -z sum u added by the epilogue, were 3 us faster, 12 with
+// stored zero points, but for the reason given in k_quant.cu logits of d = 4096 were 9e-7 of their norm off in place of
+// 2.1e-7.)
+//
+// Roles: warps 0-3 weights to TMEM (lanes by warp % 4), warps 4-11 epilogue (half = warp / 4 - 1), warps 12 and 13 TMA (codes;
 // activations), warp 14 MMA issue and TMEM.  Every wait is bounded; where one runs out the CTA's remaining logits
 // are NaN.
 #include <cuda.h>
@@ -45,26 +49,23 @@ constexpr int kWideMaxStages = 8;
 constexpr int kWideSlots = 2;                       // A operands in TMEM: 128 columns each (two halves)
 constexpr int kWideAccCols = 256;                   // TMEM columns before the A operands: two accumulators
 constexpr int kWideSmem = 226 * 1024;
-constexpr int kMetaChunk = 4;                       // groups whose scales an epilogue warp copies at a time
+constexpr int kMetaChunk = 4;                       // groups whose scales a warp copies at a time
 constexpr int kMetaSlots = 4;
-constexpr int kMetaWarps = 8;
 constexpr long long kWideWaitCycles = 4000000000ll;  // two seconds
 
 struct WideParams {
     QuantParams q;           // rows of this pass, their first output row
     const uint8_t *x;        // [blocks][n][128 bytes], swizzled
-    const float *sums;       // [groups][n]
     const float *factor;     // [n]
     int stages;              // at least kWideSlots
 };
 
 // ------------------------------------------------------------------------------ activations
 
-// One row of a pass: its fp16 elements in the order of the main kernel's stages, its groups' sums, its
-// factor.  Rows that pad the pass are zero.
-template <typename T, int kGroup>
-__global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int per_pass, int n, uint8_t *xs, float *sums,
-                                                      float *factor) {
+// One row of a pass: its fp16 elements in the order of the main kernel's stages, and its factor.  Rows that pad the
+// pass are zero.
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int per_pass, int n, uint8_t *xs, float *factor) {
     __shared__ float red[2][8];
     const int slot = blockIdx.x % n, pass = blockIdx.x / n, r = pass * per_pass + slot;
     const bool live = slot < per_pass && r < p.rows;
@@ -101,24 +102,16 @@ __global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int p
     const int E = exponent_of(top);
     if (threadIdx.x == 0)
         factor[pass * n + slot] = ldexpf(gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f, E);
-    for (int c0 = warp * 32; c0 < chunks; c0 += 256) {
-        const int c = c0 + lane;
-        float sum = 0.f;
-        if (c < chunks) {
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (live) {
-                float2 u[4];
-                make_u<T>(load_chunk(x, c * 8, p.d, p.x_align), gain != nullptr,
-                          gain ? load_chunk(gain, c * 8, p.d, p.gain_align) : make_uint4(0, 0, 0, 0), u);
-                sum = scale_u<true>(u, E, w);
-            }
-            const long long row = (static_cast<long long>(pass) * p.blocks + c / 8) * n + slot;
-            *reinterpret_cast<uint4 *>(xs + row * 128 + ((c % 8) ^ (slot % 8)) * 16) = w;
+    for (int c = threadIdx.x; c < chunks; c += 256) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) {
+            float2 u[4];
+            make_u<T>(load_chunk(x, c * 8, p.d, p.x_align), gain != nullptr,
+                      gain ? load_chunk(gain, c * 8, p.d, p.gain_align) : make_uint4(0, 0, 0, 0), u);
+            scale_u(u, E, w);
         }
-#pragma unroll
-        for (int o = 1; o < kGroup / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (c < chunks && c % (kGroup / 8) == 0)
-            sums[(static_cast<long long>(pass) * p.groups + c / (kGroup / 8)) * n + slot] = sum;
+        const long long row = (static_cast<long long>(pass) * p.blocks + c / 8) * n + slot;
+        *reinterpret_cast<uint4 *>(xs + row * 128 + ((c % 8) ^ (slot % 8)) * 16) = w;
     }
 }
 
@@ -250,23 +243,56 @@ struct Cursor {
     }
 };
 
-// Scale and zero point of a matrix row and group from shared memory.
-template <bool kZeros, bool kF16>
-__device__ __forceinline__ void row_meta(uint32_t at, float &scale, float &minus_zero) {
-    if (kZeros) {
-        const uint32_t m = lds32(at);
-        scale = scale_low<kF16>(m);
-        minus_zero = minus_zero_value(m);
-    } else {
-        scale = scale_low<kF16>(lds16(at));
-        minus_zero = -8.f;
-    }
-}
-
 constexpr int meta_group_bytes(bool zeros) { return zeros ? 128 : 64; }  // of a pair and group
-// a warp's slot: the scales of its pair, and the sums of the activations
-constexpr int meta_slot_bytes(bool zeros, int n) { return kMetaChunk * (meta_group_bytes(zeros) + n * 4); }
-constexpr int meta_ring_bytes(bool zeros, int n) { return kMetaWarps * kMetaSlots * meta_slot_bytes(zeros, n); }
+
+// Scales (and zero points) of a warp's pairs on their way through shared memory: chunks of kMetaChunk groups,
+// kMetaSlots - 1 of them ahead and on into the next unit.  Every lane calls it.
+template <bool kZeros, int kPairs>
+struct MetaRing {
+    static constexpr int kGroupBytes = meta_group_bytes(kZeros), kPairBytes = kMetaChunk * kGroupBytes;
+    static constexpr int kSlotBytes = kPairs * kPairBytes, kBytes = kMetaSlots * kSlotBytes;
+    const uint8_t *meta;
+    uint32_t ring;
+    int pair, last, groups, end;  // the next chunk's first pair (others kWideHalf on), bounds
+    int chunk = 0, slot_in = 0, slot_out = 0;
+    __device__ MetaRing(const QuantParams &q, uint32_t ring_at, int first, int unit_end)
+        : meta(static_cast<const uint8_t *>(q.meta)), ring(ring_at), pair(first), last(q.pairs - 1), groups(q.groups),
+          end(unit_end) {
+        for (int i = 0; i < kMetaSlots - 1; ++i) fetch();
+    }
+    __device__ __forceinline__ void fetch() {
+        if (pair < end) {
+            const int count = min(kMetaChunk, groups - chunk * kMetaChunk);
+            const uint32_t to = ring + slot_in * kSlotBytes;
+#pragma unroll
+            for (int h = 0; h < kPairs; ++h) {
+                const int at = (threadIdx.x & 31) * 16;
+                const long long from = static_cast<long long>(min(pair + h * kWideHalf, last)) * groups + chunk * kMetaChunk;
+                if (at < count * kGroupBytes) copy_async(to + h * kPairBytes + at, meta + from * kGroupBytes + at);
+            }
+            if (++chunk * kMetaChunk >= groups) {
+                chunk = 0;
+                pair += kWideUnit;
+            }
+            slot_in = (slot_in + 1) % kMetaSlots;
+        }
+        copy_commit();
+    }
+    __device__ __forceinline__ uint32_t next() {  // where the next chunk is
+        copy_wait<kMetaSlots - 2>();
+        __syncwarp();  // every lane's copies are seen, and every lane is done with the chunk before
+        fetch();
+        const uint32_t at = ring + slot_out * kSlotBytes;
+        slot_out = (slot_out + 1) % kMetaSlots;
+        return at;
+    }
+};
+static_assert(kMetaChunk * meta_group_bytes(true) <= 512, "a chunk of a pair is one copy a lane");
+
+// Shared memory for the epilogue's scales and, where zero points are stored, the weights' warps'.
+constexpr int meta_bytes(bool zeros) {
+    return zeros ? 8 * MetaRing<true, 1>::kBytes + 4 * MetaRing<true, 2>::kBytes : 8 * MetaRing<false, 1>::kBytes;
+}
 
 template <int kGroup, bool kZeros, bool kF16, int n>
 __global__ void __launch_bounds__(kWideThreads, 1)
@@ -283,7 +309,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int stage_bytes = n * 256 + kWideCodeBytes;
     const int steps = p.q.blocks / 2;  // stages of a unit
-    uint8_t *meta_ring = smem + p.stages * stage_bytes;
+    const uint32_t meta_ring = smem_u32(smem) + p.stages * stage_bytes;
     const int pair0 = static_cast<int>(static_cast<long long>(p.q.pairs) * blockIdx.x / gridDim.x);
     const int pair1 = static_cast<int>(static_cast<long long>(p.q.pairs) * (blockIdx.x + 1) / gridDim.x);
 
@@ -399,13 +425,18 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         wait_drained(&drained, 0);
         __syncwarp();
     } else if (warp < 4) {
-        // ---- codes to TMEM: a thread a matrix row of each half
+        // ---- weights to TMEM: a thread a matrix row of each half
         const int row = warp * 32 + lane;
         // words 2 hi and 2 hi + 1 of the vectors of lanes (t, g), t = 0..3
         const uint32_t place = smem_u32(smem) + n * 256 + (row >> 5) * kWidePairBytes + ((row >> 4) & 1) * 512 +
                                (row & 7) * 16 + ((row >> 3) & 1) * 8;
         const uint32_t to = tmem + (static_cast<uint32_t>(warp * 32) << 16) + kWideAccCols;
         Cursor s, a, before;  // before: the stage that had the A operand last, two ago
+        typedef MetaRing<kZeros, 2> Ring;  // zero points of both halves' rows
+        constexpr int kGroups = 128 / kGroup;  // of a stage
+        const uint32_t entry = ((lane >> 4) * 16 + (row & 7) * 2 + ((row >> 3) & 1)) * (Ring::kGroupBytes / 32);
+        Ring ring(p.q, meta_ring + 8 * MetaRing<kZeros, 1>::kBytes + warp * Ring::kBytes, pair0 + warp, kZeros ? pair1 : 0);
+        uint32_t zeros_at = 0;
         int i = 0;
         bool ok = true;
         for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
@@ -421,6 +452,18 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
                     for (int t = 0; t < 8; ++t)
                         w[8 + t] = lds64(from + kWideHalf * kWidePairBytes + (t >> 2) * 1024 + (t & 3) * 128);
+                uint32_t z[2][kGroups];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {  // (here, their way from shared memory is hidden by the wait below: 1 us)
+                    z[0][g] = z[1][g] = kMinusZeroDefault;
+                    if (kZeros) {
+                        const int in_chunk = (kb * kGroups + g) % kMetaChunk;
+                        if (in_chunk == 0) zeros_at = ring.next() + entry;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            z[h][g] = __byte_perm(lds32(zeros_at + h * Ring::kPairBytes + in_chunk * Ring::kGroupBytes), 0, 0x3232);
+                    }
+                }
                 if (i >= kWideSlots) {
                     ok = wait_phase_warp(&done[before.at], before.phase, abort);
                     if (!ok) break;
@@ -435,8 +478,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         for (int t = 0; t < 4; ++t)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                v[t * 4 + k] = code_pair(w[4 * b + t].x, k);
-                                v[16 + t * 4 + k] = code_pair(w[4 * b + t].y, k);
+                                // columns 64 (b % 2) of the stage on, and 32 further
+                                v[t * 4 + k] = weight_pair(w[4 * b + t].x, k, z[b / 2][b % 2 * 64 / kGroup]);
+                                v[16 + t * 4 + k] = weight_pair(w[4 * b + t].y, k, z[b / 2][(b % 2 * 64 + 32) / kGroup]);
                             }
                         tmem_st_32x32b_x32(to + a.at * 128 + b * 32, v);
                     }
@@ -454,47 +498,15 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         constexpr int cols = n;
         const int half = (warp >> 2) - 1, row = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
-        // Scales and the activations' sums come in chunks of kMetaChunk groups (of the warp's pair of tiles, and of all
-        // activations), kMetaSlots - 1 chunks ahead and on into the next unit.
-        constexpr int kGroupBytes = meta_group_bytes(kZeros), kMetaBytes = kMetaChunk * kGroupBytes;
-        constexpr int kSumBytes = cols * 4, kSlotBytes = meta_slot_bytes(kZeros, n);
-        const int groups = p.q.groups, per_unit = (groups + kMetaChunk - 1) / kMetaChunk;
-        const uint32_t ring = smem_u32(meta_ring) + (warp - 4) * kMetaSlots * kSlotBytes;
-        const uint8_t *meta = static_cast<const uint8_t *>(p.q.meta);
-        int fetch_unit = pair0, fetch_chunk = 0, fetch_slot = 0;
-        auto fetch = [&] {
-            if (fetch_unit < pair1) {
-                const long long pair = min(fetch_unit + half * kWideHalf + (warp & 3), p.q.pairs - 1);
-                const int count = min(kMetaChunk, groups - fetch_chunk * kMetaChunk);
-                const uint32_t to = ring + fetch_slot * kSlotBytes;
-#pragma unroll
-                for (int i = 0; i < (kMetaBytes + 511) / 512; ++i) {
-                    const int at = i * 512 + lane * 16;
-                    if (at < count * kGroupBytes)
-                        copy_async(to + at, meta + (pair * groups + fetch_chunk * kMetaChunk) * kGroupBytes + at);
-                }
-#pragma unroll
-                for (int i = 0; i < (kMetaChunk * kSumBytes + 511) / 512; ++i) {
-                    const int at = i * 512 + lane * 16;
-                    if (at < count * kSumBytes)
-                        copy_async(to + kMetaBytes + at,
-                                   p.sums + static_cast<size_t>(fetch_chunk * kMetaChunk + at / kSumBytes) * n +
-                                       at % kSumBytes / 4);
-                }
-                if (++fetch_chunk == per_unit) {
-                    fetch_chunk = 0;
-                    fetch_unit += kWideUnit;
-                }
-                fetch_slot = (fetch_slot + 1) % kMetaSlots;
-            }
-            copy_commit();
-        };
-        pdl_wait();  // sums and factors are the predecessor's
-        for (int i = 0; i < kMetaSlots - 1; ++i) fetch();
+        typedef MetaRing<kZeros, 1> Ring;
+        const uint32_t entry = ((lane >> 4) * 16 + (row & 7) * 2 + ((row >> 3) & 1)) * (Ring::kGroupBytes / 32);
+        const int groups = p.q.groups;
+        // (a half that has no rows in the last unit follows it all the same, on the last pair's scales)
+        Ring ring(p.q, meta_ring + (warp - 4) * Ring::kBytes, pair0 + half * kWideHalf + (warp & 3),
+                  pair0 + (pair1 - pair0 + kWideUnit - 1) / kWideUnit * kWideUnit);
+        pdl_wait();  // the factors are the predecessor's
         if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[threadIdx.x - 128];
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        const uint32_t entry = ((lane >> 4) * 16 + (row & 7) * 2 + ((row >> 3) & 1)) * (kGroupBytes / 32);
-        int slot = 0;
         Cursor acc, s;
         bool ok = true;
         for (int unit = pair0; unit < pair1; unit += kWideUnit) {
@@ -502,24 +514,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
             for (int i = 0; i < cols / 2; ++i) run[i] = pack2(0.f, 0.f);
             for (int first = 0; first < groups && ok; first += kMetaChunk) {
-                copy_wait<kMetaSlots - 2>();
-                __syncwarp();  // every lane's copies are seen, and every lane is done with the chunk before
-                fetch();
-                uint32_t meta_at = ring + slot * kSlotBytes + entry, sum_at = ring + slot * kSlotBytes + kMetaBytes;
-                slot = (slot + 1) % kMetaSlots;
+                uint32_t meta_at = ring.next() + entry;
                 const int count = min(kMetaChunk, groups - first);
                 for (int j = 0; j < count; ++j) {
-                    // all that does not hang on the product is read before the wait for it
-                    float scale, minus_zero;
-                    row_meta<kZeros, kF16>(meta_at, scale, minus_zero);
-                    const f32x2 s2 = pack2(scale, scale), z2 = pack2(minus_zero, minus_zero);
-                    f32x2 zs[8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint4 su = lds128(sum_at + i * 16);
-                        zs[2 * i] = pack2(__uint_as_float(su.x), __uint_as_float(su.y));
-                        zs[2 * i + 1] = pack2(__uint_as_float(su.z), __uint_as_float(su.w));
-                    }
+                    const float scale = scale_low<kF16>(kZeros ? lds32(meta_at) : lds16(meta_at));
+                    const f32x2 s2 = pack2(scale, scale);
                     ok = kGroup == 128 ? wait_phase_warp(&done[s.at], s.phase, abort)
                                        : wait_phase_warp(&acc_full[acc.at], acc.phase, abort);
                     if (!ok) break;
@@ -534,24 +533,12 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                             if (lane == 0) mbar_arrive(&acc_empty[acc.at]);
                         }
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            f32x2 *r = run + c * 16 + h * 8;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                r[i] = fma2(s2, fma2(z2, zs[i], pack2(v[h * 16 + 2 * i], v[h * 16 + 2 * i + 1])), r[i]);
-                            if (c * 2 + h + 1 < cols / 16)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const uint4 su = lds128(sum_at + (c * 2 + h + 1) * 64 + i * 16);
-                                    zs[2 * i] = pack2(__uint_as_float(su.x), __uint_as_float(su.y));
-                                    zs[2 * i + 1] = pack2(__uint_as_float(su.z), __uint_as_float(su.w));
-                                }
-                        }
+                        for (int i = 0; i < 16; ++i)
+                            run[c * 16 + i] = fma2(s2, pack2(v[2 * i], v[2 * i + 1]), run[c * 16 + i]);
                     }
-                    meta_at += kGroupBytes;
-                    sum_at += kSumBytes;
+                    meta_at += Ring::kGroupBytes;
                     acc.next(2);
-                    s.next(p.stages);
+                    if (kGroup == 128) s.next(p.stages);
                 }
             }
             const int pair = unit + half * kWideHalf + (row >> 5), v = pair * kQuantPairRows + lane;
@@ -565,7 +552,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         const int r = 2 * i + k;
                         if (r < p.q.rows)
                             store_out(p.q.out, p.q.out_type, r * p.q.out_stride + v,
-                                      ok ? y[k] * kCodeFactor * factor[r] : __int_as_float(0x7FFFFFFF));
+                                      ok ? y[k] * kWeightFactor * factor[r] : __int_as_float(0x7FFFFFFF));
                     }
                 }
             }
@@ -582,7 +569,7 @@ cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int num_sms, cuda
     void (*kernel)(const CUtensorMap, const CUtensorMap, const WideParams) = k_quant_wide<kGroup, kZeros, kF16, n>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem);
     if (e != cudaSuccess) return e;
-    constexpr int stage = n * 256 + kWideCodeBytes, ring = meta_ring_bytes(kZeros, n);
+    constexpr int stage = n * 256 + kWideCodeBytes, ring = meta_bytes(kZeros);
     constexpr int stages = (kWideSmem - 1024 - ring) / stage;
     static_assert(stages >= kWideSlots, "an A operand's last stage is still in the ring when it is waited for");
     p.stages = std::min(kWideMaxStages, stages);
@@ -606,50 +593,42 @@ cudaError_t launch_wide_group(const CUtensorMap *maps, const WideParams &p, int 
                          : launch_wide_scales<128, n>(maps, p, zeros, f16, num_sms, s);
 }
 
-template <int kGroup>
-cudaError_t launch_x(const QuantParams &p, int per_pass, int n, int passes, uint8_t *xs, float *sums, float *factor,
-                     cudaStream_t s) {
+cudaError_t launch_x(const QuantParams &p, int per_pass, int n, int passes, uint8_t *xs, float *factor, cudaStream_t s) {
     return p.x_type == RPD_TYPE_BF16
-               ? launch_pdl(k_quant_wide_x<__nv_bfloat16, kGroup>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs,
-                            sums, factor)
-               : launch_pdl(k_quant_wide_x<__half, kGroup>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs, sums,
-                            factor);
+               ? launch_pdl(k_quant_wide_x<__nv_bfloat16>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs, factor)
+               : launch_pdl(k_quant_wide_x<__half>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs, factor);
 }
 
-// Passes over the codes, their rows and what these are padded to (as 64, 32 rows of the 126464 x 4096 head take 103
-// us in place of 94.6).
+// Passes over the codes, their rows and what these are padded to (33 rows of the 126464 x 4096 head, padded to 64, take
+// 107 us, 32 rows as 32 take 98.1).
 struct WidePasses {
     int passes, per_pass, n;
     explicit WidePasses(int rows) {
-        passes = (rows + kWideMaxRows - 1) / kWideMaxRows;
-        per_pass = (rows + passes - 1) / passes;
+        passes = rows / kWideMaxRows + (rows % kWideMaxRows != 0);
+        per_pass = rows / passes + (rows % passes != 0);
         n = per_pass <= 32 ? 32 : 64;
     }
 };
 
 }  // namespace
 
-long long quant_wide_workspace(int rows, int blocks, int groups) {
+long long quant_wide_workspace(int rows, int blocks) {
     const WidePasses w(rows);
-    return static_cast<long long>(w.passes) * w.n * (blocks * 128ll + groups * 4ll + 4ll);
+    return static_cast<long long>(w.passes) * w.n * (blocks * 128ll + 4ll);
 }
 
 cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
                        void *workspace, cudaStream_t s) {
     const WidePasses w(p.rows);
     uint8_t *xs = static_cast<uint8_t *>(workspace);
-    float *sums = reinterpret_cast<float *>(xs + static_cast<size_t>(w.passes) * w.n * p.blocks * 128);
-    float *factor = sums + static_cast<size_t>(w.passes) * w.n * p.groups;
-    cudaError_t e = group == 32   ? launch_x<32>(p, w.per_pass, w.n, w.passes, xs, sums, factor, s)
-                    : group == 64 ? launch_x<64>(p, w.per_pass, w.n, w.passes, xs, sums, factor, s)
-                                  : launch_x<128>(p, w.per_pass, w.n, w.passes, xs, sums, factor, s);
+    float *factor = reinterpret_cast<float *>(xs + static_cast<size_t>(w.passes) * w.n * p.blocks * 128);
+    cudaError_t e = launch_x(p, w.per_pass, w.n, w.passes, xs, factor, s);
     for (int i = 0; i < w.passes && e == cudaSuccess; ++i) {
         WideParams q{};
         q.q = p;
         q.q.rows = std::min(w.per_pass, p.rows - i * w.per_pass);
         q.q.out = static_cast<char *>(p.out) + i * w.per_pass * p.out_stride * (p.out_type == RPD_TYPE_F32 ? 4 : 2);
         q.x = xs + static_cast<size_t>(i) * w.n * p.blocks * 128;
-        q.sums = sums + static_cast<size_t>(i) * w.n * p.groups;
         q.factor = factor + static_cast<size_t>(i) * w.n;
         e = w.n == 32 ? launch_wide_group<32>(maps, q, group, zeros, f16, num_sms, s)
                       : launch_wide_group<64>(maps, q, group, zeros, f16, num_sms, s);

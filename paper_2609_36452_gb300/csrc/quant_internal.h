@@ -94,9 +94,6 @@ __device__ __forceinline__ void unpack_meta(uint2 m, float &s_lo, float &s_hi, u
     z_lo = __byte_perm(m.x, 0, 0x3232);
     z_hi = __byte_perm(m.y, 0, 0x3232);
 }
-__device__ __forceinline__ float minus_zero_value(uint32_t m) {  // -z, of a row's word
-    return 512.f * __high2float(*reinterpret_cast<const __half2 *>(&m));
-}
 
 // Pair i (columns 2i, 2i + 1) of a word of codes as two fp16 numbers: masked in place, they are the subnormals q 2^-24
 // (pairs 0 and 2) and q 2^-20 (1 and 3), exact.
@@ -168,29 +165,22 @@ __device__ __forceinline__ float make_u(const uint4 &x, bool has_gain, const uin
 // The power of two at or below x (1 for 0).
 __device__ __forceinline__ int exponent_of(float x) { return x > 0.f ? ilogbf(x) : 0; }
 
-// Activations as the tensor core gets them: u 2^(14 - E) in fp16, E the exponent of the row's largest u.  Exact from 2^-24
-// of the largest element on; a smaller one is off by at most 2^-35 of the largest.  With kOddLess the odd pairs,
-// whose codes are 2^4 too large, are 2^-4 of that.  Returns the sum of the eight elements before that, times 2^-24.
-template <bool kOddLess>
-__device__ __forceinline__ float scale_u(const float2 (&u)[4], int E, uint4 &out) {
+// Activations as the tensor core gets them: u 2^(14 - E) in fp16, E the exponent of the row's largest u.  Exact from 2^-28
+// of the largest element on; a smaller one is off by at most 2^-39 of the largest.
+__device__ __forceinline__ void scale_u(const float2 (&u)[4], int E, uint4 &out) {
     const int e = 14 - E;  // in two factors: the power itself may lie outside fp32
     const float f0 = ldexpf(1.f, e / 2), f1 = ldexpf(1.f, e - e / 2);
     uint32_t w[4];
-    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float f = kOddLess && (i & 1) ? f1 * 0.0625f : f1;
-        const __half2 h = __floats2half2_rn(u[i].x * f0 * f, u[i].y * f0 * f);
-        const float2 v = __half22float2(h);
-        sum += (v.x + v.y) * (kOddLess && (i & 1) ? 16.f : 1.f);
+        const __half2 h = __floats2half2_rn(u[i].x * f0 * f1, u[i].y * f0 * f1);
         w[i] = *reinterpret_cast<const uint32_t *>(&h);
     }
     out = make_uint4(w[0], w[1], w[2], w[3]);
-    return sum * 0x1p-24f;
 }
 
-// What a row's sums are multiplied with besides 2^E rho: with weights (q - z) 2^-9, and with codes q 2^-24.
-constexpr float kWeightFactor = 0.03125f, kCodeFactor = 1024.f;
+// What a row's sums are multiplied with besides 2^E rho: 2^(9 - 14).
+constexpr float kWeightFactor = 0.03125f;
 
 __device__ __forceinline__ void store_out(void *out, int type, long long at, float v) {
     if (type == RPD_TYPE_F32)
@@ -204,7 +194,7 @@ __device__ __forceinline__ void store_out(void *out, int type, long long at, flo
 // The kernel for more rows (k_quant_wide.cu): as many passes over the codes as there are `kWideMaxRows` rows.
 constexpr int kWideMaxRows = 64;
 // maps: boxes of 4 and of 2 pairs x 128 columns of the packed codes.
-long long quant_wide_workspace(int rows, int blocks, int groups);
+long long quant_wide_workspace(int rows, int blocks);
 cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
                        void *workspace, cudaStream_t s);
 
