@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 
 __all__ = [
     "RPD_OK", "RPD_ERR_INVALID_ARGUMENT", "RPD_ERR_NO_HEAD", "RPD_ERR_CUDA",
@@ -283,6 +284,25 @@ def _stream(device: int):
     """The device's current stream (as torch.cuda.current_stream(device).cuda_stream, without the
     object around it)."""
     return _torch_module._C._cuda_getCurrentRawStream(device)
+
+
+_SCRATCH_KEPT = 1 << 22
+_scratch = threading.local()
+
+
+def _workspace(size: int, device: int, stream: int):
+    """(address, bytes, owner to hold until the call is enqueued) of at least ``size`` bytes of workspace.
+    On the default stream, whose calls run one after another, it is a buffer that the thread keeps (another
+    thread's calls may be enqueued between the launches of one): making a tensor takes 8 us, the
+    rest of a small call 12.  Elsewhere, and so under capture, it is new."""
+    if stream or size > _SCRATCH_KEPT:
+        t = _torch_module.empty(size, dtype=_torch_module.uint8, device=device)
+        return t.data_ptr(), size, t
+    kept = _scratch.__dict__.get(device)
+    if kept is None:
+        t = _torch_module.empty(_SCRATCH_KEPT, dtype=_torch_module.uint8, device=device)
+        kept = _scratch.__dict__[device] = (t.data_ptr(), _SCRATCH_KEPT, t)
+    return kept
 
 
 _DEBUG_DTYPES = {"conf": "float32", "entropy": "float32", "persist": "int32", "drop": "float32",
@@ -567,19 +587,22 @@ class QuantHead:
         """out[r] = W x[r], or with ``gain`` the readout of the normalised x[r]: x [rows][d] bf16 or
         fp16, out [rows][V] bf16, fp16 or float32, gain [d] like x; rows may lie apart.  Runs on the
         device's current stream.  ``workspace``: a uint8 CUDA tensor of rpd_quant_workspace bytes
-        (allocated where it is needed and None)."""
+        (None: the binding's own, on the default stream one that the thread keeps)."""
         rows = x.shape[0] if hasattr(x, "shape") and len(x.shape) == 2 else 0
         T = _torch()
         px, xt, xs = _rows_arg(x, "x", (T.bfloat16, T.float16), (rows, self.d))
         po, ot, os_ = _rows_arg(out, "out", (T.bfloat16, T.float16, T.float32), (rows, self.V))
         _same_device(self.device, x=x, out=out)
         pg = _dense_arg(gain, "gain", str(x.dtype)[6:], self.d, self.device) if gain is not None else None
-        need = rpd_quant_workspace(self.handle, rows)
-        if need > 0 and workspace is None:
-            workspace = _torch().empty(need, dtype=_torch_module.uint8, device=x.device)
-        pw = _dense_arg(workspace, "workspace", "uint8", workspace.numel(), self.device) if workspace is not None else None
-        _check(rpd_quant_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw,
-                                need if pw is None else workspace.numel(), _stream(self.device)))
+        stream, pw, size = _stream(self.device), None, 0
+        if workspace is not None:
+            size = workspace.numel()
+            pw = _dense_arg(workspace, "workspace", "uint8", size, self.device)
+        else:
+            need = rpd_quant_workspace(self.handle, rows)
+            if need > 0:
+                pw, size, workspace = _workspace(need, self.device, stream)
+        _check(rpd_quant_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw, size, stream))
 
 
 def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, out_prob=None, draft=None,
@@ -592,7 +615,7 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
     int32 and temperature [B] float32 (None: D and 1); allowed [B][D + 1][ceil(V / 32)] int32 bit masks.
     Outputs: out_accepted [B], out_token [B][D + 1], out_status [B] int32 and out_prob [B][D] float32.
     Runs on the current stream of the logits' device.  ``workspace``: a uint8 CUDA tensor of
-    rpd_verify_workspace bytes (allocated if None)."""
+    rpd_verify_workspace bytes (None: the binding's own, on the default stream one that the thread keeps)."""
     shape = getattr(target, "shape", ())
     if len(shape) != 3 or shape[1] < 1:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, "target: a tensor of [B][D + 1][V] logits is required")
@@ -621,12 +644,12 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
         _dense_arg(out_status, "out_status", "int32", B, dev),
         None if out_prob is None else _dense_arg(out_prob, "out_prob", "float32", B * D, dev),
         ts[0], ts[1], ds[0], ds[1], ns[0], kind, B, D, V)
-    if workspace is None:
-        size = rpd_verify_workspace(B, D)
-        # (held until the call is enqueued)
-        workspace = T.empty(size, dtype=T.uint8, device=target.device) if size else None
-    else:
+    stream, pw = _stream(dev), None
+    if workspace is not None:
         size = workspace.numel()
-        _dense_arg(workspace, "workspace", "uint8", size, dev)
-    pw = None if workspace is None else workspace.data_ptr()
-    _check(rpd_verify(a, pw, size, _stream(dev)))
+        pw = _dense_arg(workspace, "workspace", "uint8", size, dev)
+    else:
+        size = rpd_verify_workspace(B, D)
+        if size > 0:
+            pw, size, workspace = _workspace(size, dev, stream)
+    _check(rpd_verify(a, pw, size, stream))

@@ -9,6 +9,7 @@ division is one more: in all (2.1 |x| + V / 256 + 140) * 2^-24 of the value.  A 
 the next token, may differ from the definition's only where the two sides lie closer than their errors."""
 import ctypes
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -489,6 +490,52 @@ def test_graphs_streams_and_repeats_agree():
     torch.cuda.synchronize()
     c.check({k: v.cpu().numpy() for k, v in zip(("accepted", "token", "status", "prob"), outs[0])})
     del graphs
+
+
+@gpu
+@needs_gpu
+def test_threads_and_streams_without_workspaces_given():
+    """Calls of several threads on the default stream, one of them with a head in between, and one's on a
+    stream of its own: each works in a workspace that no other call is using."""
+    cases = [Case(5, 4, 20011, "bf16", True, 2, True, seed=s) for s in range(3)]
+    want = [c.run() for c in cases]
+    V, d = 3001, 256
+    head = rpd.QuantHead(d, V, 64)
+    head.set_weights(torch.randint(0, 256, (V, d // 2), dtype=torch.uint8, device="cuda"),
+                     torch.rand(V, d // 64, device="cuda").bfloat16())
+    x = torch.randn(20, d, device="cuda").bfloat16()
+    logits = torch.empty(20, V, device="cuda")
+    head.logits(x, logits)
+    want_logits = logits.clone()
+    own, failures = torch.cuda.Stream(), []
+
+    def work(c, want, stream, with_head):
+        try:
+            o = [torch.zeros(40, *shape, dtype=t, device="cuda") for shape, t in (
+                ((5,), torch.int32), ((5, 5), torch.int32), ((5,), torch.int32), ((5, 4), torch.float32))]
+            y = torch.zeros(40, 20, V, device="cuda")
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                for i in range(40):
+                    rpd.verify(c.target, c.tokens, c.uniform, c.noise, *[t[i] for t in o], draft=c.draft,
+                               lengths=c.lengths, temperature=c.temperature)
+                    if with_head:
+                        head.logits(x, y[i])
+            torch.cuda.synchronize()
+            for k, t in zip(("accepted", "token", "status", "prob"), o):
+                assert all(np.array_equal(r, want[k]) for r in t.cpu().numpy()), k
+            assert not with_head or all(torch.equal(r, want_logits) for r in y)
+        except BaseException as e:
+            failures.append(e)
+
+    threads = [threading.Thread(target=work, args=(c, w, s, h)) for c, w, s, h in zip(
+        cases, want, (torch.cuda.default_stream(), torch.cuda.default_stream(), own), (False, True, False))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    head.close()
+    assert not failures, failures
 
 
 @gpu
