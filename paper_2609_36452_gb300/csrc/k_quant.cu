@@ -154,15 +154,15 @@ __device__ __forceinline__ void for_chunks(const QuantParams &p, const T *x, int
 }
 
 template <typename T>
-__device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
+__device__ void stage_rows(const QuantParams &p, const RowsSmem &s, int first, int rows) {
     const int chunks = p.blocks * 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int per_row = kRowsWarps;  // warps that share a row
-    while (per_row * p.rows > kRowsWarps && per_row > 1) per_row >>= 1;
+    while (per_row * rows > kRowsWarps && per_row > 1) per_row >>= 1;
     const int part = warp % per_row;
-    for (int r = warp / per_row; r < p.rows; r += kRowsWarps / per_row) {
+    for (int r = warp / per_row; r < rows; r += kRowsWarps / per_row) {
         float ss = 0.f, top = 0.f;
-        for_chunks(p, static_cast<const T *>(p.x) + r * p.x_stride, part * 32, per_row * 32,
+        for_chunks(p, static_cast<const T *>(p.x) + (first + r) * p.x_stride, part * 32, per_row * 32,
                    [&](int, const uint4 &v, const uint4 &g) {
                        float2 u[4];
                        ss += make_u<T>(v, p.gain != nullptr, g, u);
@@ -180,7 +180,7 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
         }
     }
     __syncthreads();
-    for (int r = warp / per_row; r < p.rows; r += kRowsWarps / per_row) {
+    for (int r = warp / per_row; r < rows; r += kRowsWarps / per_row) {
         float ss = 0.f, top = 0.f;
         for (int w = 0; w < per_row; ++w) {
             ss += s.red[(r * kRowsWarps + w) * 2];
@@ -190,7 +190,7 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
         if (part == 0 && lane == 0)
             s.factor[r] = ldexpf(p.gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f, E);
         uint8_t *xs = s.x + static_cast<size_t>(r) * s.row_bytes;
-        for_chunks(p, static_cast<const T *>(p.x) + r * p.x_stride, part * 32, per_row * 32,
+        for_chunks(p, static_cast<const T *>(p.x) + (first + r) * p.x_stride, part * 32, per_row * 32,
                    [&](int c, const uint4 &v, const uint4 &g) {
                        float2 u[4];
                        uint4 w;
@@ -205,7 +205,7 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s) {
 // A finished pair's logits: fragment element (g, 2t) of the MMA's result is matrix row g, activation 2t.
 template <int kN8>
 __device__ __forceinline__ void store_pair(const QuantParams &p, int pair, const float (&run)[2][kN8][4],
-                                           const float *factor, int g, int t) {
+                                           const float *factor, int first, int rows, int g, int t) {
 #pragma unroll
     for (int which = 0; which < 2; ++which)
 #pragma unroll
@@ -213,8 +213,8 @@ __device__ __forceinline__ void store_pair(const QuantParams &p, int pair, const
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = n * 8 + 2 * t + (i & 1), v = pair * kQuantPairRows + which * 16 + g + (i >> 1) * 8;
-                if (r < p.rows && v < p.V)
-                    store_out(p.out, p.out_type, r * p.out_stride + v, run[which][n][i] * kWeightFactor * factor[r]);
+                if (r < rows && v < p.V)
+                    store_out(p.out, p.out_type, (first + r) * p.out_stride + v, run[which][n][i] * kWeightFactor * factor[r]);
             }
 }
 
@@ -246,6 +246,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     float *join = reinterpret_cast<float *>(sm.x);  // [warp][8 kN8][lane], when nobody reads the activations any more
 
     pdl_trigger();
+    const int row0 = blockIdx.y * p.per, rows = min(p.per, p.rows - row0);
     // this CTA's pairs of tiles, this warp's units of them
     const int pair0 = static_cast<int>(static_cast<long long>(p.pairs) * blockIdx.x / gridDim.x);
     const int pair1 = static_cast<int>(static_cast<long long>(p.pairs) * (blockIdx.x + 1) / gridDim.x);
@@ -278,9 +279,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 
     pdl_wait();  // the weights were laid out long ago; the activations may be the predecessor's
     if (p.x_type == RPD_TYPE_BF16)
-        stage_rows<__nv_bfloat16>(p, sm);
+        stage_rows<__nv_bfloat16>(p, sm, row0, rows);
     else
-        stage_rows<__half>(p, sm);
+        stage_rows<__half>(p, sm, row0, rows);
 
     float run[2][kN8][4], first[2][kN8][4];  // first: of a pair that an earlier warp began
 #pragma unroll
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
     uint32_t xrow[kN8];
 #pragma unroll
     for (int n = 0; n < kN8; ++n)
-        xrow[n] = smem_u32(sm.x) + min(n * 8 + g, p.rows - 1) * sm.row_bytes + t * 16;
+        xrow[n] = smem_u32(sm.x) + min(n * 8 + g, rows - 1) * sm.row_bytes + t * 16;
 
     int slot = 0, refill = depth - 1;
     for (int u = u0; u < u1; u += Stage::kUnits) {
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
                         }
                 }
                 if (++in_pair == per_pair) {  // the pair's last columns
-                    if (!head) store_pair<kN8>(p, pair, run, sm.factor, g, t);
+                    if (!head) store_pair<kN8>(p, pair, run, sm.factor, row0, rows, g, t);
 #pragma unroll
                     for (int i = 0; i < 8 * kN8; ++i) {
                         float &r = run[i / (4 * kN8)][i / 4 % kN8][i % 4];
@@ -390,13 +391,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 #pragma unroll
             for (int i = 0; i < 8 * kN8; ++i) run[i / (4 * kN8)][i / 4 % kN8][i % 4] += join[(w * 8 * kN8 + i) * 32 + lane];
         }
-        store_pair<kN8>(p, pair, run, sm.factor, g, t);
+        store_pair<kN8>(p, pair, run, sm.factor, row0, rows, g, t);
     }
 }
 
-constexpr int kRowsMax = 16;                 // activation rows of a launch
-// More rows are the other kernel's.  126464 x 4096: 16 rows 67.3 us here (95 there), 17 rows 95.5 there (two launches
-// here: 113); 15872 x 4096: 22.0 (27), and 26.6 (33).
+constexpr int kRowsMax = 16;                 // activation rows of a CTA
+// More rows are the other kernel's, unless every CTA for them has an SM to itself (rows_of_cta).  126464 x 4096: 16 rows
+// 67.3 us here (95 there), 17 rows 95.5 there (two launches here: 113); 15872 x 4096: 22.0 (27), and 26.6 (33).
 constexpr int kRowsMost = 16;
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 
@@ -414,11 +415,11 @@ cudaError_t launch_rows(const QuantParams &p, int num_sms, cudaStream_t s) {
     // (cheap, and per device: set on every call)
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem);
     if (e != cudaSuccess) return e;
-    const size_t fixed = rows_smem(kN8, p.rows, p.blocks);
+    const size_t fixed = rows_smem(kN8, p.per, p.blocks);
     const int stage = kRowsWarps * RowsStage<kGroup, kZeros>::kBytes;
     const int fits = static_cast<int>((kRowsSmem - fixed) / stage);
     const int depth = fits >= 6 ? 6 : fits >= 4 ? 4 : 2;
-    return launch_pdl(kernel, dim3(std::min(num_sms, p.pairs)), dim3(kRowsThreads), fixed + depth * stage, s, p,
+    return launch_pdl(kernel, dim3(std::min(num_sms, p.pairs), (p.rows + p.per - 1) / p.per), dim3(kRowsThreads), fixed + depth * stage, s, p,
                       depth);
 }
 
@@ -455,6 +456,18 @@ namespace {
 
 // The largest of 16, 8, 4 and 2 that divides an address (and whatever is or-ed into it).
 int common_align(uintptr_t bits) { return bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16; }
+
+long long rows_ctas(const rpd_quant *q, int rows, int per) {
+    return ((rows - 1ll) / per + 1) * std::min(q->pairs, q->num_sms);
+}
+
+// Activation rows of a CTA of k_quant_rows: as many as fit into its shared memory (16 up to d = 4096, two at d = 32768), but
+// eight where every CTA has an SM to itself all the same (2000 x 4096: 16 rows 10.7 us, as one CTA's 16.1).
+int rows_of_cta(const rpd_quant *q, int rows) {
+    int most = std::min(kRowsMax, std::max(rows, 1));
+    while (rows_smem(most > 8 ? 2 : 1, most, q->blocks) + kRowsRing > kRowsSmem) --most;
+    return most > 8 && rows_ctas(q, rows, 8) <= q->num_sms ? 8 : most;
+}
 
 // Boxes of 4 and of 2 pairs x 128 columns of the packed codes.
 int encode_codes(rpd_quant *q) {
@@ -575,7 +588,9 @@ int64_t rpd_quant_workspace(const rpd_quant *q, int rows) {
         op_fail(RPD_ERR_INVALID_ARGUMENT, "null head or negative rows");
         return -1;
     }
-    return rows > kRowsMost ? quant_wide_workspace(rows, q->blocks) : 0;
+    return rows <= kRowsMost || rows_ctas(q, rows, rows_of_cta(q, rows)) <= q->num_sms
+               ? 0
+               : quant_wide_workspace(rows, q->blocks, q->pairs, q->num_sms);
 }
 
 int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_stride, int rows, const void *gain,
@@ -620,27 +635,19 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.eps = eps;
     p.out_stride = out_stride;
     p.out_type = out_type;
+    p.x = x;
+    p.out = out;
+    p.rows = rows;
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
-    if (rows > kRowsMost) {
-        p.x = x;
-        p.out = out;
-        p.rows = rows;
-        const cudaError_t e = quant_wide(q->maps, p, q->group, q->zeros, q->scale_f16, q->num_sms, workspace, s);
-        return e == cudaSuccess ? RPD_OK : op_cuda_fail(e, "4-bit head launch");
+    cudaError_t e;
+    if (need > 0) {
+        e = quant_wide(q->maps, p, q->group, q->zeros, q->scale_f16, q->num_sms, workspace, s);
+    } else {
+        p.per = rows_of_cta(q, rows);
+        e = p.per <= 8 ? launch_rows_group<1>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s)
+                       : launch_rows_group<2>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s);
     }
-    // as many rows a launch as their activations fit into shared memory (16 up to d = 4096, two at d = 32768)
-    int most = kRowsMax;
-    while (rows_smem(most > 8 ? 2 : 1, most, q->blocks) + kRowsRing > kRowsSmem) --most;
-    for (int r = 0; r < rows; r += most) {
-        p.rows = std::min(most, rows - r);
-        p.x = static_cast<const uint16_t *>(x) + r * x_stride;
-        p.out = static_cast<char *>(out) + r * out_stride * type_size(out_type);
-        const cudaError_t e =
-            p.rows <= 8 ? launch_rows_group<1>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s)
-                        : launch_rows_group<2>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s);
-        if (e != cudaSuccess) return op_cuda_fail(e, "4-bit head launch");
-    }
-    return RPD_OK;
+    return e == cudaSuccess ? RPD_OK : op_cuda_fail(e, "4-bit head launch");
 }
 
 void rpd_quant_destroy(rpd_quant *q) {

@@ -54,9 +54,9 @@ constexpr int kMetaSlots = 4;
 constexpr long long kWideWaitCycles = 4000000000ll;  // two seconds
 
 struct WideParams {
-    QuantParams q;           // rows of this pass, their first output row
-    const uint8_t *x;        // [blocks][n][128 bytes], swizzled
-    const float *factor;     // [n]
+    QuantParams q;           // q.per rows a pass: blockIdx.y's
+    const uint8_t *x;        // [passes][blocks][n][128 bytes], swizzled
+    const float *factor;     // [passes][n]
     int stages;              // at least kWideSlots
 };
 
@@ -65,10 +65,10 @@ struct WideParams {
 // One row of a pass: its fp16 elements in the order of the main kernel's stages, and its factor.  Rows that pad the
 // pass are zero.
 template <typename T>
-__global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int per_pass, int n, uint8_t *xs, float *factor) {
+__global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int n, uint8_t *xs, float *factor) {
     __shared__ float red[2][8];
-    const int slot = blockIdx.x % n, pass = blockIdx.x / n, r = pass * per_pass + slot;
-    const bool live = slot < per_pass && r < p.rows;
+    const int slot = blockIdx.x % n, pass = blockIdx.x / n, r = pass * p.per + slot;
+    const bool live = slot < p.per && r < p.rows;
     const int chunks = p.blocks * 8, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const T *x = static_cast<const T *>(p.x) + r * p.x_stride;
     const T *gain = static_cast<const T *>(p.gain);
@@ -338,6 +338,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // ---- TMA, a warp for the codes and one for the activations (a copy takes its thread some 120 cycles)
         if (lane == 0) {
             const bool codes = warp == kWideTmaCodes;
+            const uint8_t *x = p.x + static_cast<long long>(blockIdx.y) * p.q.blocks * n * 128;
             if (!codes) {  // codes were laid out long ago: theirs need not wait
                 pdl_wait();
                 proxy_fence_global();
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                                            &full[s.at]);
                     } else {
                         mbar_arrive_expect_tx(&full[s.at], n * 256);
-                        bulk_copy(to, p.x + static_cast<long long>(kb) * n * 256, n * 256, &full[s.at]);
+                        bulk_copy(to, x + static_cast<long long>(kb) * n * 256, n * 256, &full[s.at]);
                     }
                     ++issued;
                     s.next(p.stages);
@@ -505,7 +506,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         Ring ring(p.q, meta_ring + (warp - 4) * Ring::kBytes, pair0 + half * kWideHalf + (warp & 3),
                   pair0 + (pair1 - pair0 + kWideUnit - 1) / kWideUnit * kWideUnit);
         pdl_wait();  // the factors are the predecessor's
-        if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[threadIdx.x - 128];
+        if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[blockIdx.y * n + threadIdx.x - 128];
         asm volatile("bar.sync 1, 256;" ::: "memory");
         Cursor acc, s;
         bool ok = true;
@@ -543,6 +544,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             }
             const int pair = unit + half * kWideHalf + (row >> 5), v = pair * kQuantPairRows + lane;
             if (pair < pair1 && v < p.q.V) {
+                int pass;  // (read here: kept in a register through the loop above, it cost 20 rows 3 us)
+                asm volatile("mov.u32 %0, %%ctaid.y;" : "=r"(pass));
+                const int row0 = pass * p.q.per, rows = min(p.q.per, p.q.rows - row0);
 #pragma unroll
                 for (int i = 0; i < cols / 2; ++i) {
                     float y[2];
@@ -550,8 +554,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const int r = 2 * i + k;
-                        if (r < p.q.rows)
-                            store_out(p.q.out, p.q.out_type, r * p.q.out_stride + v,
+                        if (r < rows)
+                            store_out(p.q.out, p.q.out_type, (row0 + r) * p.q.out_stride + v,
                                       ok ? y[k] * kWeightFactor * factor[r] : __int_as_float(0x7FFFFFFF));
                     }
                 }
@@ -565,7 +569,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 }
 
 template <int kGroup, bool kZeros, bool kF16, int n>
-cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int num_sms, cudaStream_t s) {
+cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int passes, int num_sms, cudaStream_t s) {
     void (*kernel)(const CUtensorMap, const CUtensorMap, const WideParams) = k_quant_wide<kGroup, kZeros, kF16, n>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem);
     if (e != cudaSuccess) return e;
@@ -573,67 +577,66 @@ cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int num_sms, cuda
     constexpr int stages = (kWideSmem - 1024 - ring) / stage;
     static_assert(stages >= kWideSlots, "an A operand's last stage is still in the ring when it is waited for");
     p.stages = std::min(kWideMaxStages, stages);
-    return launch_pdl(kernel, dim3(std::min(num_sms, p.q.pairs)), dim3(kWideThreads),
+    return launch_pdl(kernel, dim3(std::min(num_sms, p.q.pairs), passes), dim3(kWideThreads),
                       static_cast<size_t>(p.stages) * stage + ring + 1024, s, maps[0], maps[1], p);
 }
 
 template <int kGroup, int n>
-cudaError_t launch_wide_scales(const CUtensorMap *maps, const WideParams &p, bool zeros, bool f16, int num_sms,
-                               cudaStream_t s) {
+cudaError_t launch_wide_scales(const CUtensorMap *maps, const WideParams &p, bool zeros, bool f16, int passes,
+                               int num_sms, cudaStream_t s) {
     if (f16)
-        return zeros ? launch_wide<kGroup, true, true, n>(maps, p, num_sms, s) : launch_wide<kGroup, false, true, n>(maps, p, num_sms, s);
-    return zeros ? launch_wide<kGroup, true, false, n>(maps, p, num_sms, s) : launch_wide<kGroup, false, false, n>(maps, p, num_sms, s);
+        return zeros ? launch_wide<kGroup, true, true, n>(maps, p, passes, num_sms, s) : launch_wide<kGroup, false, true, n>(maps, p, passes, num_sms, s);
+    return zeros ? launch_wide<kGroup, true, false, n>(maps, p, passes, num_sms, s) : launch_wide<kGroup, false, false, n>(maps, p, passes, num_sms, s);
 }
 
 template <int n>
-cudaError_t launch_wide_group(const CUtensorMap *maps, const WideParams &p, int group, bool zeros, bool f16, int num_sms,
-                              cudaStream_t s) {
-    return group == 32   ? launch_wide_scales<32, n>(maps, p, zeros, f16, num_sms, s)
-           : group == 64 ? launch_wide_scales<64, n>(maps, p, zeros, f16, num_sms, s)
-                         : launch_wide_scales<128, n>(maps, p, zeros, f16, num_sms, s);
+cudaError_t launch_wide_group(const CUtensorMap *maps, const WideParams &p, int group, bool zeros, bool f16, int passes,
+                              int num_sms, cudaStream_t s) {
+    return group == 32   ? launch_wide_scales<32, n>(maps, p, zeros, f16, passes, num_sms, s)
+           : group == 64 ? launch_wide_scales<64, n>(maps, p, zeros, f16, passes, num_sms, s)
+                         : launch_wide_scales<128, n>(maps, p, zeros, f16, passes, num_sms, s);
 }
 
-cudaError_t launch_x(const QuantParams &p, int per_pass, int n, int passes, uint8_t *xs, float *factor, cudaStream_t s) {
+cudaError_t launch_x(const QuantParams &p, int n, int passes, uint8_t *xs, float *factor, cudaStream_t s) {
     return p.x_type == RPD_TYPE_BF16
-               ? launch_pdl(k_quant_wide_x<__nv_bfloat16>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs, factor)
-               : launch_pdl(k_quant_wide_x<__half>, dim3(passes * n), dim3(256), 0, s, p, per_pass, n, xs, factor);
+               ? launch_pdl(k_quant_wide_x<__nv_bfloat16>, dim3(passes * n), dim3(256), 0, s, p, n, xs, factor)
+               : launch_pdl(k_quant_wide_x<__half>, dim3(passes * n), dim3(256), 0, s, p, n, xs, factor);
 }
 
-// Passes over the codes, their rows and what these are padded to (33 rows of the 126464 x 4096 head, padded to 64, take
-// 107 us, 32 rows as 32 take 98.1).
+// Passes over the codes, their rows and what these are padded to: 64, or 32 where that makes no more passes or they all
+// run side by side.  (126464 x 4096: 33 rows, padded to 64, take 107 us, 32 rows as 32 take 98.1.)
 struct WidePasses {
     int passes, per_pass, n;
-    explicit WidePasses(int rows) {
-        passes = rows / kWideMaxRows + (rows % kWideMaxRows != 0);
+    WidePasses(int rows, int pairs, int num_sms) {
+        passes = rows / 32 + (rows % 32 != 0);
+        n = static_cast<long long>(passes) * pairs <= num_sms ? 32 : kWideMaxRows;
+        if (n == kWideMaxRows) passes = rows / n + (rows % n != 0);
         per_pass = rows / passes + (rows % passes != 0);
-        n = per_pass <= 32 ? 32 : 64;
+        if (per_pass <= 32) n = 32;
     }
 };
 
 }  // namespace
 
-long long quant_wide_workspace(int rows, int blocks) {
-    const WidePasses w(rows);
+long long quant_wide_workspace(int rows, int blocks, int pairs, int num_sms) {
+    const WidePasses w(rows, pairs, num_sms);
     return static_cast<long long>(w.passes) * w.n * (blocks * 128ll + 4ll);
 }
 
 cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
                        void *workspace, cudaStream_t s) {
-    const WidePasses w(p.rows);
+    const WidePasses w(p.rows, p.pairs, num_sms);
     uint8_t *xs = static_cast<uint8_t *>(workspace);
+    WideParams q{};
+    q.q = p;
+    q.q.per = w.per_pass;
+    q.x = xs;
     float *factor = reinterpret_cast<float *>(xs + static_cast<size_t>(w.passes) * w.n * p.blocks * 128);
-    cudaError_t e = launch_x(p, w.per_pass, w.n, w.passes, xs, factor, s);
-    for (int i = 0; i < w.passes && e == cudaSuccess; ++i) {
-        WideParams q{};
-        q.q = p;
-        q.q.rows = std::min(w.per_pass, p.rows - i * w.per_pass);
-        q.q.out = static_cast<char *>(p.out) + i * w.per_pass * p.out_stride * (p.out_type == RPD_TYPE_F32 ? 4 : 2);
-        q.x = xs + static_cast<size_t>(i) * w.n * p.blocks * 128;
-        q.factor = factor + static_cast<size_t>(i) * w.n;
-        e = w.n == 32 ? launch_wide_group<32>(maps, q, group, zeros, f16, num_sms, s)
-                      : launch_wide_group<64>(maps, q, group, zeros, f16, num_sms, s);
-    }
-    return e;
+    q.factor = factor;
+    const cudaError_t e = launch_x(q.q, w.n, w.passes, xs, factor, s);
+    if (e != cudaSuccess) return e;
+    return w.n == 32 ? launch_wide_group<32>(maps, q, group, zeros, f16, w.passes, num_sms, s)
+                     : launch_wide_group<64>(maps, q, group, zeros, f16, w.passes, num_sms, s);
 }
 
 }  // namespace rpd

@@ -27,7 +27,7 @@ struct QuantParams {
     const void *gain;    // [d] or null
     long long x_stride;
     int x_type, x_align, gain_align;  // RPD_TYPE_*; bytes (16, 8, 4, 2) at whose multiples rows (the gain) begin
-    int rows;
+    int rows, per;       // activation rows; of them, as many as a CTA (or a pass) works on: blockIdx.y's
     float eps;
     void *out;           // [rows] rows of V, out_stride elements apart
     long long out_stride;
@@ -194,7 +194,7 @@ __device__ __forceinline__ void store_out(void *out, int type, long long at, flo
 // The kernel for more rows (k_quant_wide.cu): as many passes over the codes as there are `kWideMaxRows` rows.
 constexpr int kWideMaxRows = 64;
 // maps: boxes of 4 and of 2 pairs x 128 columns of the packed codes.
-long long quant_wide_workspace(int rows, int blocks);
+long long quant_wide_workspace(int rows, int blocks, int pairs, int num_sms);
 cudaError_t quant_wide(const CUtensorMap *maps, const QuantParams &p, int group, bool zeros, bool f16, int num_sms,
                        void *workspace, cudaStream_t s);
 

@@ -93,7 +93,7 @@ def test_refusals_with_a_head():
 @gpu
 @needs_gpu
 def test_workspace_refusals_and_weights_under_capture():
-    c = make(256, 300, 40, 64, False, False)
+    c = make(256, 5003, 40, 64, False, False)
     h = head_of(c)
     need = rpd.rpd_quant_workspace(h.handle, 40)
     assert need > 0 and rpd.rpd_quant_workspace(h.handle, 16) == 0 and rpd.rpd_quant_workspace(h.handle, -1) == -1
@@ -102,7 +102,7 @@ def test_workspace_refusals_and_weights_under_capture():
         with pytest.raises(rpd.RpdError) as e:
             h.logits(c["x"], c["out"], workspace=bad)
         assert e.value.code == rpd.RPD_ERR_INVALID_ARGUMENT
-    assert rpd.rpd_quant_logits(h.handle, c["x"].data_ptr(), 0, 256, 40, None, 0.0, c["out"].data_ptr(), 2, 300, None, 0,
+    assert rpd.rpd_quant_logits(h.handle, c["x"].data_ptr(), 0, 256, 40, None, 0.0, c["out"].data_ptr(), 2, 5003, None, 0,
                                 None) == rpd.RPD_ERR_INVALID_ARGUMENT
     torch.cuda.synchronize()
     assert (c["buffer"] == 77).all()
@@ -207,6 +207,15 @@ SHAPES = [
     (4096, 2433, 128, 128, False, True, "bf16", "bf16", "bf16", 0),
     (4096, 999, 129, 32, True, True, "f16", "f32", "f16", 8),
     (8192, 300, 14, 64, False, True, "bf16", "f32", "bf16", 0),
+    (8192, 300, 100, 64, True, True, "bf16", "f32", "bf16", 0),
+    (256, 5000, 20, 32, False, True, "bf16", "f32", "bf16", 0),
+    (700, 5000, 40, 32, True, True, "f16", "f32", "f16", 3),
+    (700, 4900, 100, 64, False, False, "bf16", "f32", "f16", 8),
+    (129, 4865, 17, 128, True, True, "bf16", "bf16", "bf16", 0),
+    (200, 4877, 33, 128, False, False, "f16", "f16", "f16", 5),
+    (1254, 1022, 80, 64, True, False, "bf16", "f32", "f16", 0),
+    (20000, 513, 40, 128, False, True, "bf16", "f32", "bf16", 0),
+    (32768, 40, 35, 32, False, True, "f16", "f32", "bf16", 0),
     (32768, 40, 3, 128, True, True, "bf16", "f32", "bf16", 0),
     (32767, 33, 2, 32, False, False, "f16", "f32", "f16", 1),
 ]
@@ -226,9 +235,13 @@ def test_logits_match_the_definition(shape):
 
 @gpu
 @needs_gpu
-@pytest.mark.parametrize("rows", list(range(1, 20)) + [24, 31, 32, 33, 47, 48, 49, 63, 64, 65, 96, 127, 128, 130, 257])
-def test_every_row_count(rows):
-    c = make(384, 700, rows, 128, True, True, seed=rows)
+@pytest.mark.parametrize("V,rows", [(700, r) for r in list(range(1, 20)) + [
+    24, 31, 32, 33, 47, 48, 49, 63, 64, 65, 96, 127, 128, 130, 257]] + [(4999, r) for r in (
+        9, 16, 17, 18, 24, 31, 32, 33, 47, 48, 49, 63, 64, 65, 96, 127, 128, 130, 257)] + [(1022, r) for r in (
+            32, 33, 38, 39, 64, 65, 80, 96, 127, 128, 129, 130)])
+def test_every_row_count(V, rows):
+    """Small heads, whose rows run side by side, and larger ones, by the kernel for many rows."""
+    c = make(384, V, rows, 128, True, True, seed=rows)
     h = head_of(c)
     h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
     torch.cuda.synchronize()
@@ -238,11 +251,11 @@ def test_every_row_count(rows):
 
 @gpu
 @needs_gpu
-@pytest.mark.parametrize("rows", [2, 40])
-def test_one_column_at_a_time_lands_in_its_place(rows):
+@pytest.mark.parametrize("rows,V", [(2, 130), (40, 130), (40, 5003)])
+def test_one_column_at_a_time_lands_in_its_place(rows, V):
     """Unit activations read single columns of the matrix: every code, scale and zero point in place,
     exactly (one product, no sum)."""
-    c = make(97, 130, rows, 32, True, False, seed=5)
+    c = make(97, V, rows, 32, True, False, seed=5)
     w = weights(c)
     h = head_of(c)
     for first in range(0, 97, rows):
@@ -256,9 +269,9 @@ def test_one_column_at_a_time_lands_in_its_place(rows):
 
 @gpu
 @needs_gpu
-@pytest.mark.parametrize("rows", [3, 33])
-def test_a_row_that_is_not_finite_stays_alone(rows):
-    c = make(256, 300, rows, 64, False, True)
+@pytest.mark.parametrize("rows,V", [(3, 300), (33, 300), (33, 5003)])
+def test_a_row_that_is_not_finite_stays_alone(rows, V):
+    c = make(256, V, rows, 64, False, True)
     h = head_of(c)
     h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
     before = c["out"].clone()
@@ -272,12 +285,12 @@ def test_a_row_that_is_not_finite_stays_alone(rows):
 
 @gpu
 @needs_gpu
-@pytest.mark.parametrize("rows", [5, 20])
+@pytest.mark.parametrize("rows,V", [(5, 260), (20, 260), (20, 5003)])
 @pytest.mark.parametrize("x", ["bf16", "f16"])
-def test_rows_of_any_magnitude(rows, x):
+def test_rows_of_any_magnitude(rows, V, x):
     """Activations from the type's smallest to its largest numbers, rows of zeros, and rows whose elements
     span its range: a power of two a row brings them into the tensor core's."""
-    c = make(192, 260, rows, 64, True, False, x=x)
+    c = make(192, V, rows, 64, True, False, x=x)
     low, high = (-120, 100) if x == "bf16" else (-20, 8)
     power = torch.linspace(low, high, rows, device="cuda").round()
     c["x"].copy_((torch.randn(rows, 192, device="cuda").double() * torch.exp2(power.double())[:, None]).to(TYPES[x]))
