@@ -19,7 +19,7 @@
 // of scales, 39.4 us at 6780 GB/s; it takes 45.5 (5.9 TB/s), 8 rows 49.3, 9 rows 65.6, 16 rows 67.3.  As bf16 numbers
 // 128 + q less 128 + z (three instructions a pair of codes, 87 for 512 bytes in all) one row took 66 us.
 //
-// k_quant_rows: up to 16 rows (more: k_quant_wide.cu).  A warp multiplies pairs of tiles of 16 matrix rows (M of the
+// k_quant_rows: up to 16 rows a CTA (many rows of a head that fills the device: k_quant_wide.cu).  A warp multiplies pairs of tiles of 16 matrix rows (M of the
 // m16n8k16 MMA) by 8 or 16 activation rows (N), so that a fragment of codes is used for all of these, and a
 // fragment of activations for both tiles, from registers (with one tile at a time the reads of shared memory were the
 // limit: 52.6 us).  The codes are stored in fragment order, 1 KB for 32 rows x 64 columns, which a warp copies through
@@ -397,7 +397,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 
 constexpr int kRowsMax = 16;                 // activation rows of a CTA
 // More rows are the other kernel's, unless every CTA for them has an SM to itself (rows_of_cta).  126464 x 4096: 16 rows
-// 67.3 us here (95 there), 17 rows 95.5 there (two launches here: 113); 15872 x 4096: 22.0 (27), and 26.6 (33).
+// 65.8 us here (95 there), 17 rows 96.3 there (120 here); 15872 x 4096: 21.8 (27), and 26.7 (34).  2000 x 4096: 32 rows,
+// 126 CTAs, 16.4 us here (23.6), 48 rows, which would be 189, 24.5 there (31.4).
 constexpr int kRowsMost = 16;
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 

@@ -7,13 +7,13 @@
 // warps read it and add it, scaled, to running sums in registers, so that scales stay exact as in the kernel for few
 // rows.
 //
-// A CTA (one an SM, persistent) owns a contiguous range of pairs of 16-row tiles and works on 256 rows at a time, as two
-// halves that share every stage of activations: a stage is 128 columns of both (16 KB of codes, 8 or 16 KB of
-// activations).
+// A CTA (one an SM) has a pass of up to 64 activation rows and a contiguous range of pairs of 16-row tiles.  It works
+// on 256 matrix rows at a time, as two halves that share every stage of activations: a stage is 128 columns of both (16 KB
+// of codes, 8 or 16 KB of activations).
 //
-// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us; 17 rows take 95.5, 32 rows 98.1, 33 rows 107, 64
-// rows 111, and with stored zero points 20 rows 105), nor the tensor cores (an MMA of M = 128 and N = 32 / 64 with A in
-// TMEM takes 18 / 32 cycles, 15 us a pass in all), but what a stage costs its roles one after the other: 1550 cycles
+// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us; 17 rows take 96.3, 32 rows 98.9, 33 rows 108, 64
+// rows 113, 128 rows 218, and with stored zero points 20 rows 106), nor the tensor cores (an MMA of M = 128 and N =
+// 32 / 64 with A in TMEM takes 18 / 32 cycles, 15 us a pass in all), but what a stage costs its roles one after the other: 1550 cycles
 // where the codes' share of HBM is 700.  Of 93 us, measured when the operand still was the masked codes, 22 went without
 // the stores to TMEM, 6 without the epilogue's arithmetic, 5 without the MMAs; copies and hand-overs alone took 59.
 // Tried and no faster: two sets of warps for the operand, two issuers, three operands in flight, 128 rows at a time
@@ -54,7 +54,7 @@ constexpr int kMetaSlots = 4;
 constexpr long long kWideWaitCycles = 4000000000ll;  // two seconds
 
 struct WideParams {
-    QuantParams q;           // q.per rows a pass: blockIdx.y's
+    QuantParams q;           // q.per rows a pass: blockIdx.x's
     const uint8_t *x;        // [passes][blocks][n][128 bytes], swizzled
     const float *factor;     // [passes][n]
     int stages;              // at least kWideSlots
@@ -310,8 +310,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     constexpr int stage_bytes = n * 256 + kWideCodeBytes;
     const int steps = p.q.blocks / 2;  // stages of a unit
     const uint32_t meta_ring = smem_u32(smem) + p.stages * stage_bytes;
-    const int pair0 = static_cast<int>(static_cast<long long>(p.q.pairs) * blockIdx.x / gridDim.x);
-    const int pair1 = static_cast<int>(static_cast<long long>(p.q.pairs) * (blockIdx.x + 1) / gridDim.x);
+    const int pair0 = static_cast<int>(static_cast<long long>(p.q.pairs) * blockIdx.y / gridDim.y);
+    const int pair1 = static_cast<int>(static_cast<long long>(p.q.pairs) * (blockIdx.y + 1) / gridDim.y);
 
     pdl_trigger();
     if (warp == kWideMma) tmem_alloc(&tmem_slot, 512);
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // ---- TMA, a warp for the codes and one for the activations (a copy takes its thread some 120 cycles)
         if (lane == 0) {
             const bool codes = warp == kWideTmaCodes;
-            const uint8_t *x = p.x + static_cast<long long>(blockIdx.y) * p.q.blocks * n * 128;
+            const uint8_t *x = p.x + static_cast<long long>(blockIdx.x) * p.q.blocks * n * 128;
             if (!codes) {  // codes were laid out long ago: theirs need not wait
                 pdl_wait();
                 proxy_fence_global();
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         Ring ring(p.q, meta_ring + (warp - 4) * Ring::kBytes, pair0 + half * kWideHalf + (warp & 3),
                   pair0 + (pair1 - pair0 + kWideUnit - 1) / kWideUnit * kWideUnit);
         pdl_wait();  // the factors are the predecessor's
-        if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[blockIdx.y * n + threadIdx.x - 128];
+        if (threadIdx.x - 128 < n) factor[threadIdx.x - 128] = p.factor[static_cast<long long>(blockIdx.x) * n + threadIdx.x - 128];
         asm volatile("bar.sync 1, 256;" ::: "memory");
         Cursor acc, s;
         bool ok = true;
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             const int pair = unit + half * kWideHalf + (row >> 5), v = pair * kQuantPairRows + lane;
             if (pair < pair1 && v < p.q.V) {
                 int pass;  // (read here: kept in a register through the loop above, it cost 20 rows 3 us)
-                asm volatile("mov.u32 %0, %%ctaid.y;" : "=r"(pass));
+                asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(pass));
                 const int row0 = pass * p.q.per, rows = min(p.q.per, p.q.rows - row0);
 #pragma unroll
                 for (int i = 0; i < cols / 2; ++i) {
@@ -577,7 +577,7 @@ cudaError_t launch_wide(const CUtensorMap *maps, WideParams p, int passes, int n
     constexpr int stages = (kWideSmem - 1024 - ring) / stage;
     static_assert(stages >= kWideSlots, "an A operand's last stage is still in the ring when it is waited for");
     p.stages = std::min(kWideMaxStages, stages);
-    return launch_pdl(kernel, dim3(std::min(num_sms, p.q.pairs), passes), dim3(kWideThreads),
+    return launch_pdl(kernel, dim3(passes, std::min(num_sms, p.q.pairs)), dim3(kWideThreads),
                       static_cast<size_t>(p.stages) * stage + ring + 1024, s, maps[0], maps[1], p);
 }
 
@@ -604,7 +604,8 @@ cudaError_t launch_x(const QuantParams &p, int n, int passes, uint8_t *xs, float
 }
 
 // Passes over the codes, their rows and what these are padded to: 64, or 32 where that makes no more passes or they all
-// run side by side.  (126464 x 4096: 33 rows, padded to 64, take 107 us, 32 rows as 32 take 98.1.)
+// run side by side.  (126464 x 4096: 33 rows, padded to 64, take 108 us, 32 rows as 32 take 98.9; 1022 x 1254: 80
+// rows 12.6, as two passes of 64 in turn 26.6.)
 struct WidePasses {
     int passes, per_pass, n;
     WidePasses(int rows, int pairs, int num_sms) {

@@ -27,7 +27,7 @@ struct QuantParams {
     const void *gain;    // [d] or null
     long long x_stride;
     int x_type, x_align, gain_align;  // RPD_TYPE_*; bytes (16, 8, 4, 2) at whose multiples rows (the gain) begin
-    int rows, per;       // activation rows; of them, as many as a CTA (or a pass) works on: blockIdx.y's
+    int rows, per;       // activation rows; of them, as many as a CTA works on at a time
     float eps;
     void *out;           // [rows] rows of V, out_stride elements apart
     long long out_stride;

@@ -251,6 +251,18 @@ def test_every_row_count(V, rows):
 
 @gpu
 @needs_gpu
+def test_millions_of_rows():
+    """More passes than a grid has places in its second and third dimension (65535)."""
+    c = make(8, 5, 65536 * 64 + 17, 32, True, True)
+    h = head_of(c)
+    h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    torch.cuda.synchronize()
+    check(c)
+    h.close()
+
+
+@gpu
+@needs_gpu
 @pytest.mark.parametrize("rows,V", [(2, 130), (40, 130), (40, 5003)])
 def test_one_column_at_a_time_lands_in_its_place(rows, V):
     """Unit activations read single columns of the matrix: every code, scale and zero point in place,
