@@ -98,6 +98,15 @@ __device__ __forceinline__ float reciprocal(float x) {
     return r;
 }
 
+// 1 / e of variates, right to a last place or two.  -0 is made 0 first: it is not negative (-log(1 - u) gives it where u
+// is 0), so it wins, which its own reciprocal of -infinity would not.
+__device__ __forceinline__ float inverse_variate(float e) { return reciprocal(e + 0.f); }
+__device__ __forceinline__ void inverse_variates(float e0, float e1, float &r0, float &r1) {
+    unpack2(add2(pack2(e0, e1), 0ull), r0, r1);
+    r0 = reciprocal(r0);
+    r1 = reciprocal(r1);
+}
+
 constexpr float kNoLogit = -__builtin_huge_valf();
 
 // 1 / T in units of log2, so that e^(x / T) = 2^(x c).  Within bounds where infinite logits give 0 and the
@@ -383,12 +392,13 @@ struct Contest {
     __device__ __forceinline__ float other(float z) const { return ex2((z - dm) * c) * d_inv; }
 };
 
-// A token's score in the race and, for kExcess, in the one over p itself (should no excess be positive: p = q but for
-// roundings).
+// A token's score in the race (r: 1 / its variate) and, for kExcess, in the one over p itself (should no excess be
+// positive: p = q but for roundings).  An excess below 0 is none: with its sign, and that of a negative variate, it
+// would win.
 template <int kKind, typename T>
-__device__ __forceinline__ void contend(const Contest<T> &s, float z, float zq, float e, int at, float &score, float &plain) {
-    const float w = s.weight(z), r = reciprocal(e);
-    score = (kKind == kExcess ? fmaf(w, s.t_inv, -s.other(zq)) : w) * r;
+__device__ __forceinline__ void contend(const Contest<T> &s, float z, float zq, float r, int at, float &score, float &plain) {
+    const float w = s.weight(z);
+    score = (kKind == kExcess ? fmaxf(fmaf(w, s.t_inv, -s.other(zq)), 0.f) : w) * r;
     if (kKind == kOthers && at == s.rejected) score = 0.f;
     if (kKind == kExcess) plain = w * r;
 }
@@ -409,7 +419,7 @@ __device__ __forceinline__ void run_race(const Contest<T> &s, int split, int spl
             float z = value(s.p[i]);
             if (kMask && !((s.mask[i >> 5] >> (i & 31)) & 1u)) z = kNoLogit;
             float score, other = 0.f;
-            contend<kKind>(s, z, kKind == kExcess ? value(s.q[i]) : 0.f, s.noise[i], i, score, other);
+            contend<kKind>(s, z, kKind == kExcess ? value(s.q[i]) : 0.f, inverse_variate(s.noise[i]), i, score, other);
             race.add(score, i);
             if (kKind == kExcess) plain.add(other, i);
         }
@@ -439,14 +449,16 @@ __device__ __forceinline__ void run_race(const Contest<T> &s, int split, int spl
                 unpack(raw[u], z, T());
                 if (kKind == kExcess) unpack(raw_q[u], zq, T());
                 const uint32_t bits = kMask ? allowed_bits(s.mask, first, s.words) : 0u;
-                float score[N], other[N];
+                float score[N], other[N], r[N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const float4 &f = e[u][k / 4];
-                    const float en = k % 4 == 0 ? f.x : k % 4 == 1 ? f.y : k % 4 == 2 ? f.z : f.w;
-                    contend<kKind>(s, kMask && !((bits >> k) & 1u) ? kNoLogit : z[k], kKind == kExcess ? zq[k] : 0.f, en,
-                                   first + k, score[k], other[k]);
+                for (int k = 0; k < N / 4; ++k) {
+                    inverse_variates(e[u][k].x, e[u][k].y, r[4 * k], r[4 * k + 1]);
+                    inverse_variates(e[u][k].z, e[u][k].w, r[4 * k + 2], r[4 * k + 3]);
                 }
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    contend<kKind>(s, kMask && !((bits >> k) & 1u) ? kNoLogit : z[k], kKind == kExcess ? zq[k] : 0.f, r[k],
+                                   first + k, score[k], other[k]);
                 race.add(score, first);
                 if (kKind == kExcess) plain.add(other, first);
             }
@@ -459,7 +471,7 @@ __device__ __forceinline__ void run_race(const Contest<T> &s, int split, int spl
         float z = value(s.p[i]);
         if (kMask && !((s.mask[i >> 5] >> (i & 31)) & 1u)) z = kNoLogit;
         float score, other = 0.f;
-        contend<kKind>(s, z, kKind == kExcess ? value(s.q[i]) : 0.f, s.noise[i], i, score, other);
+        contend<kKind>(s, z, kKind == kExcess ? value(s.q[i]) : 0.f, inverse_variate(s.noise[i]), i, score, other);
         race.join(score, i);
         if (kKind == kExcess) plain.join(other, i);
     }
@@ -497,8 +509,14 @@ struct Draw {
             x = ex2(x);
             y = ex2(y);
             st.s = add2(st.s, pack2(x, y));
-            score[i] = x * reciprocal(e[i]);
-            if (i + 1 < N) score[(i + 1) % N] = y * reciprocal(e[(i + 1) % N]);
+            if (i + 1 < N) {
+                float r0, r1;
+                inverse_variates(e[i], e[(i + 1) % N], r0, r1);
+                score[i] = x * r0;
+                score[(i + 1) % N] = y * r1;
+            } else {
+                score[i] = x * inverse_variate(e[i]);
+            }
         }
         race.add(score, first, step);
     }
