@@ -186,9 +186,15 @@ __device__ void stage_rows(const QuantParams &p, const RowsSmem &s, int first, i
             ss += s.red[(r * kRowsWarps + w) * 2];
             top = fmaxf(top, s.red[(r * kRowsWarps + w) * 2 + 1]);
         }
-        const int E = exponent_of(top);
-        if (part == 0 && lane == 0)
-            s.factor[r] = ldexpf(p.gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f, E);
+        int E = exponent_of(top);
+        if (p.gain && norm_unusual(ss, top, p.eps, E)) {  // (the row's warps all do it, for E)
+            const NormFactor f = norm_factor_unusual(static_cast<const T *>(p.x) + (first + r) * p.x_stride, chunks, p.d,
+                                                     p.x_align, p.eps, top, E);
+            E = f.E;
+            if (part == 0 && lane == 0) s.factor[r] = f.factor;
+        } else if (part == 0 && lane == 0) {
+            s.factor[r] = p.gain ? norm_factor(ss, static_cast<float>(p.d), p.eps, E) : ldexpf(1.f, E);
+        }
         uint8_t *xs = s.x + static_cast<size_t>(r) * s.row_bytes;
         for_chunks(p, static_cast<const T *>(p.x) + (first + r) * p.x_stride, part * 32, per_row * 32,
                    [&](int c, const uint4 &v, const uint4 &g) {

@@ -99,9 +99,14 @@ __global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int n
         ss += red[0][w];
         top = fmaxf(top, red[1][w]);
     }
-    const int E = exponent_of(top);
-    if (threadIdx.x == 0)
-        factor[pass * n + slot] = ldexpf(gain ? rsqrtf(ss / static_cast<float>(p.d) + p.eps) : 1.f, E);
+    int E = exponent_of(top);
+    if (gain && live && norm_unusual(ss, top, p.eps, E)) {
+        const NormFactor f = norm_factor_unusual(x, chunks, p.d, p.x_align, p.eps, top, E);
+        E = f.E;
+        if (threadIdx.x == 0) factor[pass * n + slot] = f.factor;
+    } else if (threadIdx.x == 0) {
+        factor[pass * n + slot] = gain ? norm_factor(ss, static_cast<float>(p.d), p.eps, E) : ldexpf(1.f, E);
+    }
     for (int c = threadIdx.x; c < chunks; c += 256) {
         uint4 w = make_uint4(0, 0, 0, 0);
         if (live) {

@@ -165,6 +165,65 @@ __device__ __forceinline__ float make_u(const uint4 &x, bool has_gain, const uin
 // The power of two at or below x (1 for 0).
 __device__ __forceinline__ int exponent_of(float x) { return x > 0.f ? ilogbf(x) : 0; }
 
+// A row's factor rho 2^E under a norm, rho = (ss / d + eps)^-1/2, as it usually is.  ss: the sum of x^2 as make_u adds it
+// up, top: the largest |u|.
+__device__ __forceinline__ float norm_factor(float ss, float d, float eps, int E) { return ldexpf(rsqrtf(ss / d + eps), E); }
+
+// Whether it is not: fp32 has not held the sum (it is infinite, or below 2^-90, where squares under 2^-126 may be what counts;
+// above, what 32768 of these lose is below 2^-44 of it), or rho 2^E may lie under 2^-126 (rho itself is at least 2^-64).
+// Rows of zeros, such as a batch is padded with, have products of 0 whatever finite rho is.
+__device__ __forceinline__ bool norm_unusual(float ss, float top, float eps, int E) {
+    return (!(ss >= 0x1p-90f && ss <= 3e38f) || E < -62) && ss == ss && !(top == 0.f && eps > 0.f);
+}
+
+// Then the warp, all of it, goes through the row twice more, for (x 2^-F)^2 with F the exponent of its largest |x|.  E is
+// raised until rho 2^E is a normal number: smaller, it would lose bits that a logit has.  (Activations are then
+// smaller by as much and off by up to 2^-39 2^E, which times rho is some 2^-165: under half of fp32's smallest number for
+// weights of a sum below 2^15.)
+struct NormFactor {
+    float factor;
+    int E;
+};
+template <typename T>
+__device__ __noinline__ NormFactor norm_factor_unusual(const T *x, int chunks, int d, int align, float eps, float top, int E) {
+    const int lane = threadIdx.x & 31;
+    float most = 0.f;
+    for (int c = lane; c < chunks; c += 32) {
+        const uint4 v = load_chunk(x, c * 8, d, align);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = pair_value(w[i], T());
+            most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (top == 0.f) return {most > 0.f ? 1.f : rsqrtf(eps), E};  // (eps = 0: products of 0, and 0 / 0 for a row of zeros)
+    const int F = exponent_of(fminf(most, 3e38f));
+    const float f0 = ldexpf(1.f, -F / 2), f1 = ldexpf(1.f, -F + F / 2);  // (2^-F itself may lie outside fp32)
+    float sum = 0.f;
+    for (int c = lane; c < chunks; c += 32) {
+        const uint4 v = load_chunk(x, c * 8, d, align);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = pair_value(w[i], T());
+            const float a = f.x * f0 * f1, b = f.y * f0 * f1;
+            sum = fmaf(a, a, fmaf(b, b, sum));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    // rho = 2^-F (sum / d + eps 2^-2F)^-1/2, the sum at least 1; where eps 2^-2F leaves fp32, eps is all that counts
+    const float e = ldexpf(eps, -2 * F);
+    const bool held = e <= 3e38f;
+    const float r = held ? rsqrtf(sum / static_cast<float>(d) + e) : rsqrtf(eps);
+    const int R = held ? -F : 0;  // rho = r 2^R
+    E = max(E, -126 - R - ilogbf(r));
+    return {ldexpf(r, R + E), E};
+}
+
 // Activations as the tensor core gets them: u 2^(14 - E) in fp16, E the exponent of the row's largest u.  Exact from 2^-28
 // of the largest element on; a smaller one is off by at most 2^-39 of the largest.
 __device__ __forceinline__ void scale_u(const float2 (&u)[4], int E, uint4 &out) {
