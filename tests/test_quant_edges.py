@@ -1,9 +1,10 @@
-"""The 4-bit head (rpd_quant_*) at its edges: activations of any size under a norm.  Bounds as in test_quant_head.py."""
+"""The 4-bit head (rpd_quant_*) at its edges: activations of any size under a norm, the accuracy that is promised, calls
+that fail or give up.  Where not said otherwise, bounds are those of test_quant_head.py."""
 import pytest
 import torch
 
 import paper_2609_36452_gb300 as rpd
-from test_quant_head import TYPES, check, head_of, make
+from test_quant_head import TYPES, check, head_of, make, reference, weights
 
 gpu = pytest.mark.gpu
 needs_gpu = pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA GPU")
@@ -44,3 +45,75 @@ def test_normalised_rows_of_any_magnitude(d, rows, V, x, eps):
         c["out"][zero] = c["out"][0]
     check(c)
     h.close()
+
+
+def rounding_steps(d, group, norm):
+    """The error of a logit in units of 2^-23 of the logits' norm, as the root of a sum of squares.  A group is summed in
+    n = group / 16 steps, the sum after step i having i / n of the variance of a group's: each cuts off at most 2^-23 of it.
+    The m = d / group groups are added up with a rounding of at most half of that each.  The group's scale and the two
+    factors round a logit three times more; rho, under a norm, is a chain of 40 roundings of at most half of that each."""
+    n, m = group // 16, -(-d // group)
+    inside = sum(i / n for i in range(1, n + 1))
+    outside = sum(i / m for i in range(1, m + 1)) / 4
+    return (inside + outside + 3 / 4 + (40 / 4 if norm else 0)) ** 0.5
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("rows,V", [(1, 4096), (16, 4096), (20, 20000), (64, 20000), (128, 20000)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+def test_error_in_units_of_the_logits_norm(rows, V, group, zeros, norm):
+    """At d = 4096 the fp32 logits' error lies below what fp32 sums of exact products may leave, relative to the logits'
+    norm: weights rounded to 16 bits, group sums in 16 bits (both some 10^-3) or operands that the tensor core
+    lines up worse (1.7e-6 with groups of 128) lie above it."""
+    c = make(4096, V, rows, group, zeros, norm, seed=group + rows)
+    h = head_of(c)
+    h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    torch.cuda.synchronize()
+    y, _ = reference(c)
+    off = (c["out"].double() - y).norm() / y.norm()
+    print(f"off {off.item():.3g}")
+    assert off <= rounding_steps(4096, group, norm) * 2.0 ** -23
+    h.close()
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("rows,V", [(3, 600), (20, 600), (20, 5003)])
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+def test_small_elements_beside_a_large_one(rows, V, x):
+    """A row's largest element meets weights of 0: what is 2^-28 of it and more enters exactly, and a smaller one is off by
+    at most 2^-39 of the largest."""
+    d, group = 256, 64
+    c = make(d, V, rows, group, True, False, x=x)
+    c["zeros"].fill_(5)
+    c["codes"][:, 32] = 0x55  # columns 64 and 65
+    c["scales"].fill_(1.0)
+    top = 2.0 ** 100 if x == "bf16" else 2.0 ** 15
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    small = (1 + torch.rand(rows, d, device="cuda", generator=gen)).to(TYPES[x]).double()
+    if x == "bf16":
+        small *= top * 2.0 ** -28
+    else:  # (fp16 has nothing smaller that is exact)
+        small = (small * 2.0 ** -13).to(TYPES[x]).double()
+    small[:, 64:66] = 0
+    for j in range(2):
+        xs = small.clone() if j == 0 or x == "f16" else small * 2.0 ** -9
+        xs[:, 64] = top
+        c["x"].copy_(xs.to(TYPES[x]))
+        assert torch.equal(c["x"].double(), xs)
+        h = head_of(c)
+        h.logits(c["x"], c["out"])
+        torch.cuda.synchronize()
+        w = weights(c)
+        assert (w[:, 64:66] == 0).all()
+        y = xs @ w.t()
+        xs[:, 64] = 0
+        # the sums' own roundings, of sums of the sizes of the small products alone
+        bound = (group / 16 + d / group + 28) * 2.0 ** -23 * (xs.abs() @ w.abs().t())
+        if j and x == "bf16":
+            bound += 2.0 ** -39 * top * w.abs().sum(1)
+        assert ((c["out"].double() - y).abs() <= bound).all()
+        h.close()
