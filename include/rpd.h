@@ -400,6 +400,16 @@ int rpd_quant_logits(const rpd_quant *head, const void *x, int x_type, int64_t x
                      const void *gain, float eps, void *out, int out_type, int64_t out_stride,
                      void *workspace, int64_t workspace_bytes, void *stream);
 
+/* Diagnostics, as rpd_set_wait_limit and rpd_inject_stall.  The waits inside the kernel for more than a few rows are
+ * bounded; where one runs out the kernel stops, drains what it has in flight, frees its tensor memory, and the
+ * logits that it had not finished are NaN (rpd_quant_logits itself has long returned); the head stays usable.
+ *   rpd_quant_set_wait_limit: the bound, in microseconds (default 2 000 000), 1000 .. 60 000 000.
+ *   rpd_quant_inject_stall:   while on, that kernel never asks for its activations, so that its waits run
+ *                             out; used to test the path (the kernel for a few rows is not affected).
+ * Both apply to calls that follow; no call on this head may be running. */
+int rpd_quant_set_wait_limit(rpd_quant *head, int64_t microseconds);
+int rpd_quant_inject_stall(rpd_quant *head, int on);
+
 /* Free the head (no call on it may be running).  NULL is ignored. */
 void rpd_quant_destroy(rpd_quant *head);
 

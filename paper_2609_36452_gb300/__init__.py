@@ -21,6 +21,7 @@ __all__ = [
     "rpd_step_shard_partials", "rpd_step_shard_finish", "rpd_profile_enable", "rpd_kernel_times",
     "rpd_build_decode_loop", "rpd_build_decode_loop_batched", "rpd_decode_loop_launch", "rpd_decode_loop_destroy", "DecodeLoop",
     "rpd_quant_create", "rpd_quant_set_weights", "rpd_quant_workspace", "rpd_quant_logits", "rpd_quant_destroy", "QuantHead",
+    "rpd_quant_set_wait_limit", "rpd_quant_inject_stall",
     "rpd_verify_workspace", "rpd_verify", "verify", "RpdVerifyArgs",
     "rpd_destroy", "rpd_last_error", "rpd_version", "Rpd", "RULE_PROFILES", "KERNEL_NAMES",
 ]
@@ -144,6 +145,8 @@ def _load():
         "rpd_quant_workspace": (ctypes.c_int64, [vp, i32]),
         "rpd_quant_logits": (i32, [vp, vp, i32, ctypes.c_int64, i32, vp, f32, vp, i32, ctypes.c_int64,
                                    vp, ctypes.c_int64, vp]),
+        "rpd_quant_set_wait_limit": (i32, [vp, ctypes.c_int64]),
+        "rpd_quant_inject_stall": (i32, [vp, i32]),
         "rpd_quant_destroy": (None, [vp]),
         "rpd_verify_workspace": (ctypes.c_int64, [i32, i32]),
         "rpd_verify": (i32, [ctypes.POINTER(RpdVerifyArgs), vp, ctypes.c_int64, vp]),
@@ -189,6 +192,8 @@ rpd_quant_create = lib.rpd_quant_create
 rpd_quant_set_weights = lib.rpd_quant_set_weights
 rpd_quant_workspace = lib.rpd_quant_workspace
 rpd_quant_logits = lib.rpd_quant_logits
+rpd_quant_set_wait_limit = lib.rpd_quant_set_wait_limit
+rpd_quant_inject_stall = lib.rpd_quant_inject_stall
 rpd_quant_destroy = lib.rpd_quant_destroy
 rpd_verify_workspace = lib.rpd_verify_workspace
 rpd_verify = lib.rpd_verify
@@ -582,6 +587,14 @@ class QuantHead:
                 _dense_arg(zeros, "zeros", "uint8", self.V * groups, self.device) if zeros is not None else None)
         _check(rpd_quant_set_weights(self.handle, args[0], args[1], ELEMENT_TYPES[str(scales.dtype)], args[2],
                                      _stream(self.device)))
+
+    def set_wait_limit(self, microseconds: int):
+        _check(rpd_quant_set_wait_limit(self.handle, int(microseconds)))
+
+    def inject_stall(self, on: bool = True):
+        """Diagnostics: while on, the kernel for more than a few rows asks for no activations; its bounded waits run
+        out and the logits are NaN."""
+        _check(rpd_quant_inject_stall(self.handle, 1 if on else 0))
 
     def logits(self, x, out, gain=None, eps=1e-6, workspace=None):
         """out[r] = W x[r], or with ``gain`` the readout of the normalised x[r]: x [rows][d] bf16 or

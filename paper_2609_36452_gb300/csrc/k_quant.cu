@@ -456,10 +456,15 @@ struct rpd_quant {
     uint4 *codes = nullptr;
     void *meta = nullptr;
     bool set = false, zeros = false, scale_f16 = false;
+    int64_t wait_us = 2000000;  // of the wide kernel's waits
+    bool stall = false;
     CUtensorMap maps[2];  // the codes, a row a pair
 };
 
 namespace {
+
+constexpr int64_t kQuantCyclesPerUs = 2000;         // the limit of a wait is counted in cycles of some 2 GHz
+constexpr int64_t kQuantMaxWaitUs = 60000000;
 
 // The largest of 16, 8, 4 and 2 that divides an address (and whatever is or-ed into it).
 int common_align(uintptr_t bits) { return bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16; }
@@ -645,6 +650,8 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.x = x;
     p.out = out;
     p.rows = rows;
+    p.wait_cycles = q->wait_us * kQuantCyclesPerUs;
+    p.stall = q->stall ? 1 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
     cudaError_t e;
     if (need > 0) {
@@ -655,6 +662,20 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
                        : launch_rows_group<2>(p, q->group, q->zeros, q->scale_f16, q->num_sms, s);
     }
     return e == cudaSuccess ? RPD_OK : op_cuda_fail(e, "4-bit head launch");
+}
+
+int rpd_quant_set_wait_limit(rpd_quant *q, int64_t microseconds) {
+    if (!q) return op_fail(RPD_ERR_INVALID_ARGUMENT, "null head");
+    if (microseconds < 1000 || microseconds > kQuantMaxWaitUs)
+        return op_fail(RPD_ERR_INVALID_ARGUMENT, "the wait limit must be 1000 .. %lld us", static_cast<long long>(kQuantMaxWaitUs));
+    q->wait_us = microseconds;
+    return RPD_OK;
+}
+
+int rpd_quant_inject_stall(rpd_quant *q, int on) {
+    if (!q) return op_fail(RPD_ERR_INVALID_ARGUMENT, "null head");
+    q->stall = on != 0;
+    return RPD_OK;
 }
 
 void rpd_quant_destroy(rpd_quant *q) {

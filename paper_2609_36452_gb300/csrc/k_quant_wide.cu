@@ -24,8 +24,8 @@
 // 2.1e-7.)
 //
 // Roles: warps 0-3 weights to TMEM (lanes by warp % 4), warps 4-11 epilogue (half = warp / 4 - 1), warps 12 and 13 TMA (codes;
-// activations), warp 14 MMA issue and TMEM.  Every wait is bounded; where one runs out the CTA's remaining logits
-// are NaN.
+// activations), warp 14 MMA issue and TMEM.  Every wait is bounded (from when the kernels before this one are done: a role
+// waits for these before its first bounded wait); where one runs out the CTA's remaining logits are NaN.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -51,7 +51,6 @@ constexpr int kWideAccCols = 256;                   // TMEM columns before the A
 constexpr int kWideSmem = 226 * 1024;
 constexpr int kMetaChunk = 4;                       // groups whose scales a warp copies at a time
 constexpr int kMetaSlots = 4;
-constexpr long long kWideWaitCycles = 4000000000ll;  // two seconds
 
 struct WideParams {
     QuantParams q;           // q.per rows a pass: blockIdx.x's
@@ -183,8 +182,8 @@ __device__ __forceinline__ uint32_t idesc_f16(int n) {
     return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (128u >> 4 << 24);
 }
 
-// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after two
-// seconds or once another role has raised it.
+// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after `limit` cycles
+// or once another role has raised it.
 __device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  // sleeps up to 2 us
     uint32_t ok;
     asm volatile(
@@ -198,13 +197,13 @@ __device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  
         : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort) {
+__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
     const uint32_t a = smem_u32(bar);
     if (try_wait_long(a, parity)) return true;
     const long long t0 = clock64();
     while (!try_wait_long(a, parity)) {
         if (*abort) return false;
-        if (clock64() - t0 > kWideWaitCycles) {
+        if (clock64() - t0 > limit) {
             *abort = 1;
             return false;
         }
@@ -212,14 +211,14 @@ __device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volat
     return true;
 }
 // By a converged warp, which stays so.
-__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort));
+__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
+    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort, limit));
 }
 // On the way out: whatever the abort flag says.
-__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity) {
+__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, long long limit) {
     const uint32_t a = smem_u32(bar);
     const long long t0 = clock64();
-    while (!mbar_try_wait(a, parity) && clock64() - t0 < kWideWaitCycles) {
+    while (!mbar_try_wait(a, parity) && clock64() - t0 < limit) {
     }
 }
 
@@ -350,13 +349,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             }
             Cursor s;
             int issued = 0;
-            bool ok = true;
+            bool ok = codes || !p.q.stall;
             for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
                 const int pairs = min(pair1 - unit, kWideUnit);
                 const int rest = pairs % 4;  // copies of four pairs; of two where no more are left
                 const int bytes = (pairs - rest + (rest > 2 ? 4 : rest ? 2 : 0)) * kWidePairBytes;
                 for (int kb = 0; kb < steps; ++kb) {
-                    if (issued >= p.stages) ok = wait_phase(&done[s.at], s.phase ^ 1u, abort);
+                    if (issued == p.stages) pdl_wait();
+                    if (issued >= p.stages) ok = wait_phase(&done[s.at], s.phase ^ 1u, abort, p.q.wait_cycles);
                     if (!ok) break;
                     uint8_t *to = smem + s.at * stage_bytes;
                     if (codes) {
@@ -390,17 +390,18 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         uint32_t acc_phase = 1;  // of the two accumulators: they are used in turn
         int acc_next = 0;
         bool ok = true;
+        pdl_wait();
         for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
             const bool two = pair1 - unit > kWideHalf;
             for (int kb = 0; kb < steps; ++kb) {
                 // (the warps that arrive here have seen the whole stage land, activations too)
-                ok = wait_phase_warp(&a_full[a.at], a.phase, abort);
+                ok = wait_phase_warp(&a_full[a.at], a.phase, abort, p.q.wait_cycles);
                 if (!ok) break;
                 const uint64_t b = b_base + static_cast<uint32_t>(s.at * stage_bytes) / 16;
                 const uint32_t a_at = base + kWideAccCols + a.at * 128;
 #pragma unroll 1
                 for (int grp = 0; grp < kGroups; ++grp) {
-                    ok = ok && wait_phase_warp(&acc_empty[acc_next], acc_phase, abort);
+                    ok = ok && wait_phase_warp(&acc_empty[acc_next], acc_phase, abort, p.q.wait_cycles);
                     if (ok) {
                         tc_fence_after_sync();
                         const uint32_t d = base + acc_next * 128;
@@ -428,7 +429,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         }
         // everything issued has to be done before TMEM is given back
         umma_commit_warp(&drained);
-        wait_drained(&drained, 0);
+        wait_drained(&drained, 0, p.q.wait_cycles);
         __syncwarp();
     } else if (warp < 4) {
         // ---- weights to TMEM: a thread a matrix row of each half
@@ -445,10 +446,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         uint32_t zeros_at = 0;
         int i = 0;
         bool ok = true;
+        pdl_wait();
         for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
             const bool two = pair1 - unit > kWideHalf;
             for (int kb = 0; kb < steps; ++kb, ++i) {
-                ok = wait_phase_warp(&full[s.at], s.phase, abort);
+                ok = wait_phase_warp(&full[s.at], s.phase, abort, p.q.wait_cycles);
                 if (!ok) break;
                 const uint32_t from = place + s.at * stage_bytes;
                 uint2 w[16];
@@ -471,7 +473,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                 }
                 if (i >= kWideSlots) {
-                    ok = wait_phase_warp(&done[before.at], before.phase, abort);
+                    ok = wait_phase_warp(&done[before.at], before.phase, abort, p.q.wait_cycles);
                     if (!ok) break;
                     before.next(p.stages);
                     tc_fence_after_sync();
@@ -499,6 +501,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 a.next(kWideSlots);
             }
         }
+        copy_wait<0>();  // (after a wait that ran out, chunks may be on their way)
     } else {
         // ---- epilogue: a thread a matrix row, all activations
         constexpr int cols = n;
@@ -525,8 +528,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 for (int j = 0; j < count; ++j) {
                     const float scale = scale_low<kF16>(kZeros ? lds32(meta_at) : lds16(meta_at));
                     const f32x2 s2 = pack2(scale, scale);
-                    ok = kGroup == 128 ? wait_phase_warp(&done[s.at], s.phase, abort)
-                                       : wait_phase_warp(&acc_full[acc.at], acc.phase, abort);
+                    ok = kGroup == 128 ? wait_phase_warp(&done[s.at], s.phase, abort, p.q.wait_cycles)
+                                       : wait_phase_warp(&acc_full[acc.at], acc.phase, abort, p.q.wait_cycles);
                     if (!ok) break;
                     tc_fence_after_sync();
 #pragma unroll
@@ -566,6 +569,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 }
             }
         }
+        copy_wait<0>();
     }
     tc_fence_before_sync();
     __syncthreads();

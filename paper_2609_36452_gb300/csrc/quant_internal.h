@@ -32,6 +32,8 @@ struct QuantParams {
     void *out;           // [rows] rows of V, out_stride elements apart
     long long out_stride;
     int out_type;
+    long long wait_cycles;  // of the wide kernel's waits
+    int stall;              // diagnostics: its activations are not asked for
 };
 
 template <bool kZeros>

@@ -117,3 +117,41 @@ def test_small_elements_beside_a_large_one(rows, V, x):
             bound += 2.0 ** -39 * top * w.abs().sum(1)
         assert ((c["out"].double() - y).abs() <= bound).all()
         h.close()
+
+
+def test_wait_limits_of_no_head_are_refused():
+    assert rpd.rpd_quant_set_wait_limit(None, 5000) == rpd.RPD_ERR_INVALID_ARGUMENT
+    assert rpd.rpd_quant_inject_stall(None, 1) == rpd.RPD_ERR_INVALID_ARGUMENT
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("d,V,rows,group,zeros", [(384, 5003, 20, 128, False), (1024, 40003, 64, 128, True),
+                                                  (1024, 40003, 128, 32, True), (8192, 3000, 33, 64, False)])
+def test_a_wait_that_runs_out_leaves_nan_and_a_usable_head(d, V, rows, group, zeros):
+    """A role of the kernel for many rows that never gets its copies: every other one gives up within the limit, in
+    one unit of matrix rows and in several."""
+    c = make(d, V, rows, group, zeros, True, pad=8)
+    h = head_of(c)
+    h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    torch.cuda.synchronize()
+    check(c)
+    before = c["out"].clone()
+    for bad in (0, -5, 999, 60000001):
+        with pytest.raises(rpd.RpdError) as e:
+            h.set_wait_limit(bad)
+        assert e.value.code == rpd.RPD_ERR_INVALID_ARGUMENT
+    h.set_wait_limit(2000)
+    h.inject_stall()
+    for _ in range(2):
+        h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    few = torch.zeros(8, V, device="cuda")
+    h.logits(c["x"][:8], few, gain=c["gain"], eps=c["eps"])  # (the other kernel has no such waits)
+    torch.cuda.synchronize()
+    assert torch.isnan(c["out"]).all() and torch.isfinite(few).all()
+    assert (c["buffer"][rows:] == 77).all() and (c["buffer"][:, V:] == 77).all()
+    h.inject_stall(False)
+    h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    torch.cuda.synchronize()
+    assert torch.equal(c["out"], before)
+    h.close()
