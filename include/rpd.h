@@ -376,9 +376,10 @@ rpd_quant *rpd_quant_create(int d, int V, int group);
  *          in the upper ones (with odd d the last byte's upper bits are ignored);
  *   scales [V][ceil(d / group)] bf16 or fp16 (scale_type), device;
  *   zeros  [V][ceil(d / group)] uint8, device, lower four bits used; NULL: every zero point is 8.
- * The copy runs on `stream` (which may not be under capture: RPD_ERR_INVALID_ARGUMENT), and the call waits
- * for it; no call on this head may be running or be captured in a graph that is used again (the layout
- * is reallocated). */
+ * The copy runs on `stream` (which may not be under capture: RPD_ERR_INVALID_ARGUMENT; another stream may be), and the
+ * call waits for it; no call on this head may be running or be captured in a graph that is used again
+ * (the layout is reallocated).  A head that has weights keeps them where the call fails, unless the
+ * device has no room for both: the old ones are then freed first. */
 int rpd_quant_set_weights(rpd_quant *head, const void *codes, const void *scales, int scale_type,
                           const void *zeros, void *stream);
 

@@ -34,6 +34,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 
 #include "op_host.h"
 #include "ptx.cuh"
@@ -449,12 +450,32 @@ cudaError_t launch_rows_group(const QuantParams &p, int group, bool zeros, bool 
 
 using namespace rpd;
 
+// The weights of a head in its own order, in device memory.
+struct QuantLayout {
+    uint4 *codes = nullptr;
+    void *meta = nullptr;
+    cudaError_t allocate(size_t code_bytes, size_t meta_bytes) {  // both or neither
+        cudaError_t e = cudaMalloc(&codes, code_bytes);
+        if (e == cudaSuccess) e = cudaMalloc(&meta, meta_bytes);
+        if (e != cudaSuccess) release();
+        return e;
+    }
+    cudaError_t release() {  // what could not be freed is kept
+        cudaError_t e = cudaFree(codes);
+        if (e == cudaSuccess) {
+            codes = nullptr;
+            e = cudaFree(meta);
+            if (e == cudaSuccess) meta = nullptr;
+        }
+        return e;
+    }
+};
+
 struct rpd_quant {
     int d = 0, V = 0, group = 0;
     int device = 0, num_sms = 0;
     int pairs = 0, pad_pairs = 0, blocks = 0, groups = 0;  // groups: padding included
-    uint4 *codes = nullptr;
-    void *meta = nullptr;
+    QuantLayout layout;
     bool set = false, zeros = false, scale_f16 = false;
     int64_t wait_us = 2000000;  // of the wide kernel's waits
     bool stall = false;
@@ -465,6 +486,16 @@ namespace {
 
 constexpr int64_t kQuantCyclesPerUs = 2000;         // the limit of a wait is counted in cycles of some 2 GHz
 constexpr int64_t kQuantMaxWaitUs = 60000000;
+
+// A launch without attributes, with its own error (not one that an earlier call has left behind).
+template <typename... KArgs, typename... Args>
+cudaError_t launch_plain(void (*kernel)(KArgs...), int grid, int block, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = s;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 // The largest of 16, 8, 4 and 2 that divides an address (and whatever is or-ed into it).
 int common_align(uintptr_t bits) { return bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16; }
@@ -482,7 +513,7 @@ int rows_of_cta(const rpd_quant *q, int rows) {
 }
 
 // Boxes of 4 and of 2 pairs x 128 columns of the packed codes.
-int encode_codes(rpd_quant *q) {
+int encode_codes(const rpd_quant *q, uint4 *codes, CUtensorMap *maps) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
     cuuint64_t dims[2] = {static_cast<cuuint64_t>(q->blocks) * 128, static_cast<cuuint64_t>(q->pad_pairs)};
@@ -490,9 +521,9 @@ int encode_codes(rpd_quant *q) {
     cuuint32_t box[2] = {256, 4}, step[2] = {1, 1};
     CUresult r = CUDA_SUCCESS;
     for (int i = 0; i < 2 && r == CUDA_SUCCESS; ++i, box[1] /= 2)
-        r = fn(&q->maps[i], CU_TENSOR_MAP_DATA_TYPE_UINT64, 2, q->codes, dims, strides, box, step,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        r = fn(&maps[i], CU_TENSOR_MAP_DATA_TYPE_UINT64, 2, codes, dims, strides, box, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
 }
 
@@ -559,39 +590,40 @@ int rpd_quant_set_weights(rpd_quant *q, const void *codes, const void *scales, i
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "the weights cannot be set while the stream is being captured");
     const size_t code_bytes = static_cast<size_t>(q->pad_pairs) * q->blocks * 1024;
     const size_t meta_bytes = static_cast<size_t>(q->pad_pairs) * q->groups * (zeros ? 128 : 64);
-    // Freeing the previous layout waits for the device: no call may still be reading it.
-    q->set = false;
-    if (q->codes) cudaFree(q->codes);
-    if (q->meta) cudaFree(q->meta);
-    q->codes = nullptr;
-    q->meta = nullptr;
-    e = cudaMalloc(&q->codes, code_bytes);
-    if (e == cudaSuccess) e = cudaMalloc(&q->meta, meta_bytes);
-    if (e == cudaSuccess) {
-        const int groups = (q->d + q->group - 1) / q->group;
-        k_quant_pack<<<q->num_sms * 8, 256, 0, s>>>(static_cast<const uint8_t *>(codes), q->codes, q->V, q->d,
-                                                    q->pad_pairs, q->blocks);
-        if (zeros)
-            k_quant_pack_scales<true><<<q->num_sms * 4, 256, 0, s>>>(static_cast<const uint16_t *>(scales),
-                                                                     static_cast<const uint8_t *>(zeros), q->meta,
-                                                                     q->V, groups, q->pad_pairs, q->groups);
-        else
-            k_quant_pack_scales<false><<<q->num_sms * 4, 256, 0, s>>>(static_cast<const uint16_t *>(scales), nullptr,
-                                                                      q->meta, q->V, groups, q->pad_pairs, q->groups);
-        e = cudaGetLastError();
-        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    RelaxedCapture rc;
+    // The new layout is made beside the one that is there, which a failure then leaves as it was.  Only where the device
+    // has no room for both is the old one freed first.
+    QuantLayout made;
+    e = made.allocate(code_bytes, meta_bytes);
+    if (e == cudaErrorMemoryAllocation && q->set) {
+        cudaGetLastError();
+        q->set = false;
+        e = q->layout.release();
+        if (e == cudaSuccess) e = made.allocate(code_bytes, meta_bytes);
     }
-    if (e != cudaSuccess) {
-        if (q->codes) cudaFree(q->codes);
-        if (q->meta) cudaFree(q->meta);
-        q->codes = nullptr;
-        q->meta = nullptr;
-        return op_cuda_fail(e, "layout of the 4-bit weights");
+    if (e != cudaSuccess) return op_cuda_fail(e, "memory for the 4-bit weights");
+    const int groups = (q->d + q->group - 1) / q->group;
+    e = launch_plain(k_quant_pack, q->num_sms * 8, 256, s, static_cast<const uint8_t *>(codes), made.codes, q->V, q->d,
+                     q->pad_pairs, q->blocks);
+    if (e == cudaSuccess)
+        e = launch_plain(zeros ? k_quant_pack_scales<true> : k_quant_pack_scales<false>, q->num_sms * 4, 256, s,
+                         static_cast<const uint16_t *>(scales), static_cast<const uint8_t *>(zeros), made.meta, q->V,
+                         groups, q->pad_pairs, q->groups);
+    const cudaError_t done = cudaStreamSynchronize(s);  // (whatever was launched may not outlive its memory)
+    if (e == cudaSuccess) e = done;
+    CUtensorMap maps[2];
+    const int code = e != cudaSuccess ? op_cuda_fail(e, "layout of the 4-bit weights") : encode_codes(q, made.codes, maps);
+    if (code != RPD_OK) {
+        made.release();
+        return code;
     }
-    if (const int rc = encode_codes(q)) return rc;
+    std::swap(q->layout, made);
+    std::copy(maps, maps + 2, q->maps);
     q->zeros = zeros != nullptr;
     q->scale_f16 = scale_type == RPD_TYPE_F16;
     q->set = true;
+    made.release();  // waits for the device: no call may still be reading it
+    cudaGetLastError();
     return RPD_OK;
 }
 
@@ -632,8 +664,8 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
         (gain && !pointer_usable(gain, q->device, false)) || (need > 0 && !pointer_usable(workspace, q->device, false)))
         return op_fail(RPD_ERR_INVALID_ARGUMENT, "x, gain, out and workspace must be device memory on the head's device");
     QuantParams p{};
-    p.codes = q->codes;
-    p.meta = q->meta;
+    p.codes = q->layout.codes;
+    p.meta = q->layout.meta;
     p.pairs = q->pairs;
     p.blocks = q->blocks;
     p.groups = q->groups;
@@ -681,8 +713,9 @@ int rpd_quant_inject_stall(rpd_quant *q, int on) {
 void rpd_quant_destroy(rpd_quant *q) {
     if (!q) return;
     DeviceGuard dg(q->device);
-    if (q->codes) cudaFree(q->codes);
-    if (q->meta) cudaFree(q->meta);
+    RelaxedCapture rc;
+    q->layout.release();
+    cudaGetLastError();
     delete q;
 }
 

@@ -61,9 +61,20 @@ inline int op_fail(int code, const char *fmt, ...) {
 }
 
 inline int op_cuda_fail(cudaError_t e, const char *what) {
+    cudaGetLastError();  // reported here: it is not the next call's
     return op_fail(e == cudaErrorMemoryAllocation ? RPD_ERR_OUT_OF_MEMORY : RPD_ERR_CUDA, "%s: %s", what,
                    cudaGetErrorString(e));
 }
+
+// While it lives, this thread's allocations and frees are allowed although some stream is being captured in the global mode
+// (without it they would fail, and end that capture).
+struct RelaxedCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    RelaxedCapture(const RelaxedCapture &) = delete;
+    RelaxedCapture &operator=(const RelaxedCapture &) = delete;
+};
 
 // Bytes of an element of one of the RPD_TYPE_* types, 0 for anything else.
 inline int type_size(int type) {

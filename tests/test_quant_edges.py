@@ -1,5 +1,7 @@
 """The 4-bit head (rpd_quant_*) at its edges: activations of any size under a norm, the accuracy that is promised, calls
 that fail or give up.  Where not said otherwise, bounds are those of test_quant_head.py."""
+import ctypes
+
 import pytest
 import torch
 
@@ -155,3 +157,104 @@ def test_a_wait_that_runs_out_leaves_nan_and_a_usable_head(d, V, rows, group, ze
     torch.cuda.synchronize()
     assert torch.equal(c["out"], before)
     h.close()
+
+
+class Capture:
+    """A stream under capture in the global mode, by the driver's own calls; `blocking`: one that the legacy default stream
+    waits for.  What ends it says whether it was still sound."""
+
+    def __init__(self, blocking):
+        self.cu = ctypes.CDLL("libcuda.so.1")
+        self.stream, self.graph = ctypes.c_void_p(), ctypes.c_void_p()
+        assert self.cu.cuStreamCreate(ctypes.byref(self.stream), 0 if blocking else 1) == 0
+        assert self.cu.cuStreamBeginCapture_v2(self.stream, 0) == 0
+
+    def end(self):
+        rc = self.cu.cuStreamEndCapture(self.stream, ctypes.byref(self.graph))
+        if rc == 0:
+            self.cu.cuGraphDestroy(self.graph)
+        self.cu.cuStreamDestroy_v2(self.stream)
+        return rc
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("rows", [3, 20])
+def test_weights_are_set_and_heads_closed_while_another_stream_is_captured(rows):
+    c, c2 = make(256, 5003, rows, 64, False, True), make(256, 5003, rows, 64, True, True, seed=1)
+    h, other = head_of(c), head_of(c)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (torch.cuda.default_stream(), side):
+        for case in (c2, c):
+            capture = Capture(blocking=False)
+            try:
+                with torch.cuda.stream(stream):
+                    h.set_weights(case["codes"], case["scales"], case["zeros"])
+                if other.handle:
+                    other.close()
+            finally:
+                rc = capture.end()
+            assert rc == 0  # (neither call has ended it)
+            h.logits(case["x"], case["out"], gain=case["gain"], eps=case["eps"])
+            torch.cuda.synchronize()
+            check(case)
+    h.close()
+
+
+@gpu
+@needs_gpu
+def test_a_refused_call_leaves_the_weights_and_no_error_behind():
+    """The legacy default stream cannot be asked for anything while a stream that it waits for is being captured: the call
+    fails, the weights stay, and the next call does not report the failure again."""
+    c, c2 = make(256, 1000, 5, 64, False, True), make(256, 1000, 5, 64, True, True, seed=1)
+    h = head_of(c)
+    torch.cuda.synchronize()
+    capture = Capture(blocking=True)
+    try:
+        with pytest.raises(rpd.RpdError) as e:
+            h.set_weights(c2["codes"], c2["scales"], c2["zeros"])
+    finally:
+        capture.end()
+    assert e.value.code == rpd.RPD_ERR_CUDA
+    h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    torch.cuda.synchronize()
+    check(c)
+    h.set_weights(c2["codes"], c2["scales"], c2["zeros"])
+    h.logits(c2["x"], c2["out"], gain=c2["gain"], eps=c2["eps"])
+    torch.cuda.synchronize()
+    check(c2)
+    h.close()
+
+
+@gpu
+@needs_gpu
+def test_new_weights_where_there_is_no_room_for_two_layouts():
+    """2.4 GB of weights on a device with some 1 GB left: the old ones are freed first; a head that has none fails,
+    and works once there is room."""
+    c = make(1024, 1 << 22, 2, 32, False, False, out="bf16")
+    h, empty = head_of(c), rpd.QuantHead(1024, 1 << 22, 32)
+    ref, zeros = c["out"].clone(), torch.full((1 << 22, 32), 8, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    filler = torch.empty(torch.cuda.mem_get_info()[0] - (1200 << 20), dtype=torch.uint8, device="cuda")
+    assert torch.cuda.mem_get_info()[0] < 1300 << 20
+    with pytest.raises(rpd.RpdError) as e:
+        empty.set_weights(c["codes"], c["scales"])
+    assert e.value.code == rpd.RPD_ERR_OUT_OF_MEMORY
+    h.logits(c["x"], c["out"])
+    ref.copy_(c["out"])
+    h.set_weights(c["codes"], c["scales"], zeros)
+    c["out"].zero_()
+    h.logits(c["x"], c["out"])
+    torch.cuda.synchronize()
+    assert torch.equal(c["out"], ref)
+    del filler
+    torch.cuda.empty_cache()
+    empty.set_weights(c["codes"], c["scales"])
+    c["out"].zero_()
+    empty.logits(c["x"], c["out"])
+    torch.cuda.synchronize()
+    assert torch.equal(c["out"], ref)
+    h.close()
+    empty.close()
