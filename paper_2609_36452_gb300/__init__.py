@@ -279,6 +279,13 @@ def _dense_arg(t, name: str, dtype: str, numel: int, device: int):
     return t.data_ptr()
 
 
+def _size(n: int, name: str) -> int:
+    """A size that the C ABI takes in 32 bits (ctypes would cut off the rest of a larger one)."""
+    if not -(1 << 31) <= n < 1 << 31:
+        raise RpdError(RPD_ERR_UNSUPPORTED, f"{name}: {n} does not fit 32 bits")
+    return n
+
+
 def _same_device(device: int, **tensors):
     for name, t in tensors.items():
         if t is not None and t.get_device() != device:
@@ -557,7 +564,7 @@ class QuantHead:
     def __init__(self, d: int, V: int, group: int = 128):
         self.d, self.V, self.group = d, V, group
         self.handle = None
-        h = rpd_quant_create(d, V, group)
+        h = rpd_quant_create(_size(d, "d"), _size(V, "V"), _size(group, "group"))
         if not h:
             raise RpdError(RPD_ERR_INVALID_ARGUMENT, rpd_last_error().decode())
         self.handle = ctypes.c_void_p(h)
@@ -601,7 +608,7 @@ class QuantHead:
         fp16, out [rows][V] bf16, fp16 or float32, gain [d] like x; rows may lie apart.  Runs on the
         device's current stream.  ``workspace``: a uint8 CUDA tensor of rpd_quant_workspace bytes
         (None: the binding's own, on the default stream one that the thread keeps)."""
-        rows = x.shape[0] if hasattr(x, "shape") and len(x.shape) == 2 else 0
+        rows = _size(x.shape[0], "rows of x") if hasattr(x, "shape") and len(x.shape) == 2 else 0
         T = _torch()
         px, xt, xs = _rows_arg(x, "x", (T.bfloat16, T.float16), (rows, self.d))
         po, ot, os_ = _rows_arg(out, "out", (T.bfloat16, T.float16, T.float32), (rows, self.V))
@@ -632,7 +639,7 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
     shape = getattr(target, "shape", ())
     if len(shape) != 3 or shape[1] < 1:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, "target: a tensor of [B][D + 1][V] logits is required")
-    B, D, V = shape[0], shape[1] - 1, shape[2]
+    B, D, V = _size(shape[0], "B"), _size(shape[1] - 1, "D"), _size(shape[2], "V")
     T = _torch()
     pt, kind, ts = _rows_arg(target, "target", (T.bfloat16, T.float16, T.float32), (B, D + 1, V))
     dev = target.get_device()

@@ -258,3 +258,26 @@ def test_new_weights_where_there_is_no_room_for_two_layouts():
     assert torch.equal(c["out"], ref)
     h.close()
     empty.close()
+
+
+@pytest.mark.parametrize("d,V,group", [((1 << 32) + 64, 100, 32), (64, (1 << 32) + 100, 32), (64, 100, (1 << 32) + 32),
+                                       (64, 1 << 31, 32)])
+def test_sizes_beyond_32_bits_make_no_head(d, V, group):
+    with pytest.raises(rpd.RpdError, match="32 bits") as e:
+        rpd.QuantHead(d, V, group)
+    assert e.value.code == rpd.RPD_ERR_UNSUPPORTED
+
+
+@gpu
+@needs_gpu
+def test_rows_beyond_32_bits_are_refused():
+    """2^32 + 1 rows of which the C ABI would see one."""
+    c = make(64, 40, 1, 32, False, False)
+    h = head_of(c)
+    for rows in ((1 << 32) + 1, 1 << 31):
+        with pytest.raises(rpd.RpdError) as e:
+            h.logits(c["x"].expand(rows, 64), c["out"].expand(rows, 40))
+        assert e.value.code == rpd.RPD_ERR_UNSUPPORTED
+    torch.cuda.synchronize()
+    assert (c["buffer"] == 77).all()
+    h.close()

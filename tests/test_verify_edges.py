@@ -84,3 +84,12 @@ def test_a_variate_of_minus_zero_is_zero(dtype, single, kind):
     got = c.run()
     assert got["token"][:, row].tolist() == best[:, 0].tolist()
     assert (got["status"] == 0).all() and (got["accepted"] == row).all()
+
+
+@pytest.mark.parametrize("shape", [((1 << 32) + 1, 1, 1), (1, (1 << 32) + 1, 1), (1, 1, (1 << 32) + 1), (1 << 31, 1, 1)])
+def test_sizes_beyond_32_bits_are_refused(shape):
+    """Of 2^32 + 1 sequences, drafts or tokens the C ABI would see one."""
+    z = torch.zeros(1, 1, 1).expand(shape)
+    with pytest.raises(rpd.RpdError, match="32 bits") as e:
+        rpd.verify(z, None, None, None, None, None, None)
+    assert e.value.code == rpd.RPD_ERR_UNSUPPORTED
