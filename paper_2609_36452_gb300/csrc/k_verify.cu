@@ -35,6 +35,7 @@ constexpr int kDecideResident = 1024;  // threads an SM of the kernels that work
 constexpr int kVerifyMaxCluster = 8;  // CTAs that scan one sequence's row, at most
 constexpr int kVerifyMaxDrafts = 1024;
 constexpr int kVerifyMaxSplits = 32;
+constexpr long long kVerifyMaxRows = 1 << 26;  // a grid has as many CTAs: of so many rows none is divided (verify_splits)
 
 struct VerifyParams {
     rpd_verify_args a;
@@ -900,7 +901,7 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
     if (a.D > kVerifyMaxDrafts || a.V > (1 << 24))
         return op_fail(RPD_ERR_UNSUPPORTED, "D must be <= %d and V <= %d", kVerifyMaxDrafts, 1 << 24);
     const long long rows = static_cast<long long>(a.B) * (a.draft ? 2 * a.D + 1 : a.D + 1);
-    if (rows * kVerifyMaxSplits > 0x7FFFFFFFll || a.B > (0x7FFFFFFF / kVerifyMaxCluster))
+    if (rows > kVerifyMaxRows)
         return op_fail(RPD_ERR_UNSUPPORTED, "too many rows (%lld)", rows);
     if (a.B == 0) return RPD_OK;
     if (!a.target || !a.out_accepted || !a.out_token || !a.out_status || (a.D > 0 && !a.tokens))

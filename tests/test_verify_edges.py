@@ -1,12 +1,13 @@
 """Verification of drafted tokens (rpd_verify) at its edges: variates and probabilities at the ends of their
 ranges, sizes beyond 32 bits.  Decisions are held against the definition in 64 bits, with test_verify.py's bounds."""
+import ctypes
 import math
 
 import pytest
 import torch
 
 import paper_2609_36452_gb300 as rpd
-from test_verify import TYPES, Case
+from test_verify import Case, args_of
 
 gpu = pytest.mark.gpu
 needs_gpu = pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA GPU")
@@ -93,3 +94,29 @@ def test_sizes_beyond_32_bits_are_refused(shape):
     with pytest.raises(rpd.RpdError, match="32 bits") as e:
         rpd.verify(z, None, None, None, None, None, None)
     assert e.value.code == rpd.RPD_ERR_UNSUPPORTED
+
+
+def test_as_many_rows_as_promised_are_taken():
+    """2^26 rows of logits and no more: drafts' rows count too."""
+    for kw, ok in ((dict(B=1 << 26, D=0), True), (dict(B=(1 << 26) + 1, D=0), False), (dict(B=1 << 24, D=3), True),
+                   (dict(B=(1 << 24) + 1, D=3), False), (dict(B=1 << 23, D=3, draft=4096), True),
+                   (dict(B=1 << 24, D=2, draft=4096), False)):
+        a = args_of(target=None, **kw)  # what comes after the sizes is refused in any case
+        want = rpd.RPD_ERR_INVALID_ARGUMENT if ok else rpd.RPD_ERR_UNSUPPORTED
+        assert rpd.rpd_verify(ctypes.byref(a), 4096, 1 << 60, None) == want, kw
+
+
+@gpu
+@needs_gpu
+def test_the_most_rows():
+    """2^26 sequences of one token, and 2^25 of one draft each, which is accepted."""
+    for B, D in ((1 << 26, 0), (1 << 25, 1)):
+        target = torch.zeros(1, 1, 2, device="cuda").expand(B, D + 1, 2)
+        tokens = torch.zeros(B, D, dtype=torch.int32, device="cuda")
+        uniform = torch.full((B, D), 0.25, device="cuda")
+        noise = torch.tensor([[1.0, 2.0]], device="cuda").expand(B, 2)
+        o = [torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((B,), (B, D + 1), (B,))]
+        rpd.verify(target, tokens, uniform, noise, *o)
+        assert (o[0] == D).all() and (o[1] == 0).all() and (o[2] == 0).all()
+        del target, tokens, uniform, noise, o
+        torch.cuda.empty_cache()
