@@ -429,7 +429,8 @@ void rpd_quant_destroy(rpd_quant *head);
  * target.  A token is drawn as argmax_v w(v) / noise[b][v] (the lowest v on a tie), which with
  * exponential variates is a draw with the weights w.  T = 0 puts p_i at its largest logit (the lowest
  * index on a tie): a draft is accepted where it is that token, and draft rows and random numbers are
- * not read.  D = 0, or lengths of 0, is sampling.
+ * not read; other T count as at least 1.45e-30 and at most
+ * 1.44e37.  D = 0, or lengths of 0, is sampling.
  *
  * Sizes: B sequences, at most D drafts each, V tokens; 0 <= D <= 1024, 1 <= V <= 2^24 (larger, or
  * more than 2^26 rows of logits: RPD_ERR_UNSUPPORTED).  B = 0 is a no-op. */

@@ -116,6 +116,10 @@ __device__ __forceinline__ float exponent_scale(float T) {
     return fminf(fmaxf(1.4426950408889634f / T, 1e-37f), 1e30f);
 }
 
+// A draft's own probability, of which there is one a row: exp2f goes down to fp32's smallest number (the terms' 2^x ends
+// at 2^-126; p = 0 would reject a draft although u = 0).
+__device__ __forceinline__ float probability(float z, float m, float c, float sum) { return exp2f((z - m) * c) / sum; }
+
 // ------------------------------------------------------------------------------ statistics of the rows
 
 // Running maximum and sum (in two halves, for the packed operations).  A sum that is not finite and positive marks a
@@ -748,11 +752,11 @@ __global__ void __launch_bounds__(kThreads, kDecideResident / kThreads) k_verify
         for (int i = threadIdx.x; i < n; i += kThreads) {
             const int x = tokens[i];
             bool sound = s.ts[i] > 0.f;
-            const float px = !sound ? 0.f : greedy ? (x == s.arg[i] ? 1.f : 0.f) : ex2((s.zx[i] - s.tm[i]) * c) / s.ts[i];
+            const float px = !sound ? 0.f : greedy ? (x == s.arg[i] ? 1.f : 0.f) : probability(s.zx[i], s.tm[i], c, s.ts[i]);
             float qx = 1.f;
             if (drafts) {
                 sound = sound && s.ds[i] > 0.f;
-                qx = sound ? ex2((s.zq[i] - s.dm[i]) * c) / s.ds[i] : 0.f;
+                qx = sound ? probability(s.zq[i], s.dm[i], c, s.ds[i]) : 0.f;
             }
             const bool accept =
                 sound && (greedy ? px > 0.f : a.uniform[static_cast<long long>(b) * a.D + i] * qx < px);

@@ -120,3 +120,75 @@ def test_the_most_rows():
         assert (o[0] == D).all() and (o[1] == 0).all() and (o[2] == 0).all()
         del target, tokens, uniform, noise, o
         torch.cuda.empty_cache()
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("draft", [True, False])
+def test_probabilities_down_to_the_smallest_number(dtype, draft):
+    """Drafts whose probability lies between 2^-149 and 2^-126: it is what the definition says to half of fp32's smallest
+    number (and the tolerance of the value), and u = 0 accepts them."""
+    c = Case(16, 1, 700, dtype, draft, spread=0.5)
+    c.temperature.fill_(0.5)
+    c.tokens.fill_(33)
+    c.target[:, 0, 33] = c.target[:, 0].amax(1) - torch.linspace(38, 46, 16, device="cuda").to(c.dtype)
+    if draft:
+        c.draft[:, 0, 33] = c.draft[:, 0].amax(1) - 40
+    c.uniform.fill_(0.0)
+    got = c.run()
+    assert (got["accepted"] == 1).all() and (got["status"] == 0).all()
+    p = torch.softmax(c.target[:, 0].double() / 0.5, 1)[:, 33].cpu().numpy()
+    assert (p < 2.0 ** -110).all() and (p > 2.0 ** -149).all() and (p < 2.0 ** -126).any()
+    x = c.target[:, 0, 33].double() - c.target[:, 0].double().amax(1)
+    bound = c.tolerance(x.cpu().numpy() * 2 / math.log(2)) * p + 2.0 ** -150
+    assert (abs(got["prob"][:, 0].astype(float) - p) <= bound).all()
+    c.check(got)
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("D", [0, 2])
+def test_temperatures_beyond_their_bounds_count_as_these(D):
+    """Infinite and huge temperatures over logits that span all of fp32, and vanishing ones: the same as at the largest and
+    the smallest that count, probabilities, verdicts and draws alike, so that the probabilities still add up to 1."""
+    runs = []
+    most, least = 1 / math.log(2) * 1e37, 1 / math.log(2) * 1e-30
+    for T in ((math.inf, 1e38, 2e37, 1e-40, 1e-33, 1e-30), (1e38, math.inf, math.inf, 1e-31, 1e-42, 1e-32)):
+        c = Case(6, D, 700, "f32", False)
+        c.target[:, :, ::2] = torch.finfo(torch.float32).min
+        c.target[:, :, 1::2] *= 1e36
+        c.target[3:] = (c.target[3:] / 1e36).clamp(min=-4).round() * 1e-30
+        c.temperature.copy_(torch.tensor(T))
+        c.tokens.fill_(7)
+        runs.append(c.run())
+        c.temperature.copy_(torch.tensor((most,) * 3 + (least,) * 3))
+        c.check(runs[-1])
+    for k in runs[0]:
+        assert (runs[0][k] == runs[1][k]).all(), k
+    assert (runs[0]["status"] == 0).all()
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_error_of_the_probabilities(dtype):
+    """Relative errors of the drafts' probabilities: the roundings of z - m, of 1 / T and of their product move the
+    exponent, and so the value, by 3 * 2^-24 |x|; exp2f is right to 2^-22, the quotient to 2^-24.  The sum: ex2's
+    2^-22, and a term's exponent, three times rounded, |x| of which the weights of the sum average; its
+    additions have no common sign."""
+    c = Case(16, 8, 50021, dtype, False, seed=4)
+    c.tokens = torch.where(torch.rand(16, 8, device="cuda") < 0.5, c.target[:, :8].float().argmax(2).int(), c.tokens)
+    got = c.run()
+    t = c.temperature.double().view(-1, 1, 1)
+    z = c.target[:, :8].double()
+    p = torch.softmax(z / t, 2)
+    x = (z - z.amax(2, keepdim=True)) / t
+    mean = (p * x.abs()).sum(2)  # |x| of the terms as the sum weighs them
+    at = c.tokens.long().unsqueeze(2)
+    p, x = p.gather(2, at).squeeze(2), x.gather(2, at).squeeze(2).abs()
+    chain = (50021 / 256 + 64) ** 0.5
+    bound = (3 * x + 5 + 4 + 3 * mean + chain) * 2.0 ** -24
+    off = (torch.tensor(got["prob"], device="cuda").double() / p - 1).abs()
+    print(f"off {off.max().item():.3g}, of the bound {(off / bound).max().item():.3g}")
+    assert (off <= bound).all()
