@@ -337,13 +337,13 @@ struct Race {
         }
     }
     template <int N>
-    __device__ __forceinline__ void add(const float (&score)[N], int first, int step = 1) {
+    __device__ __forceinline__ void add(const float (&score)[N], int first) {
         float top = score[0];
 #pragma unroll
         for (int k = 1; k < N; ++k) top = fmaxf(top, score[k]);
         if (top > best) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) add(score[k], first + k * step);
+            for (int k = 0; k < N; ++k) add(score[k], first + k);
         }
     }
     __device__ __forceinline__ void join(float score, int i) {
@@ -484,12 +484,31 @@ __device__ __forceinline__ void run_race(const Contest<T> &s, int split, int spl
 
 // ------------------------------------------------------------------------------ nothing drafted
 
-// Statistics of a slice and the race over it in one pass, both relative to the running maximum.
+// The row and its variates, for a score that has to be made anew.
+template <typename T>
+struct DrawRow {
+    const T *p;
+    const float *noise;
+    float c;
+    __device__ __forceinline__ float score(int at, float m) const {
+        const float r = inverse_variate(noise[at]);
+        return r < -kNoLogit ? ex2((value(p[at]) - m) * c) * r : r;
+    }
+};
+
+// Statistics of a slice and the race over it in one pass, both relative to the running maximum.  A leader's score that has
+// been multiplied on depends, in its last places, on the maxima that it has met; where another comes within 2^-10 of
+// it, it is made anew from its logit and variate, so that of equal tokens the first one wins.  (To keep both with
+// every leader made 128 rows 1 us slower.)
+constexpr float kDrawNear = 0x1p-10f;
+
 struct Draw {
     Stat st;
     Race race;
-    template <int N>
-    __device__ __forceinline__ void add(const float (&z)[N], const float (&e)[N], int first, float c, int step = 1) {
+    template <int N, typename T>
+    __device__ __forceinline__ void add(const float (&z)[N], const float (&e)[N], int first, const DrawRow<T> &row,
+                                        int step = 1) {
+        const float c = row.c;
         float top = st.m;
 #pragma unroll
         for (int i = 0; i < N; ++i) top = fmaxf(top, z[i]);
@@ -523,43 +542,82 @@ struct Draw {
                 score[i] = x * inverse_variate(e[i]);
             }
         }
-        race.add(score, first, step);
-    }
-    __device__ __forceinline__ void join(float m2, float s2, float best2, int at2, float c) {
-        const float top = fmaxf(st.m, m2);
-        float f1 = 1.f, f2 = 1.f;
-        if (top > kNoLogit) {
-            f1 = ex2((st.m - top) * c);
-            f2 = ex2((m2 - top) * c);
+        float best = score[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) best = fmaxf(best, score[i]);
+        if (best > race.best * (1.f - kDrawNear)) {
+            if (best < race.best * (1.f + kDrawNear)) race.best = row.score(race.at, st.m);
+#pragma unroll
+            for (int i = 0; i < N; ++i) race.add(score[i], first + i * step);
         }
-        race.best = f1 > 0.f ? race.best * f1 : 0.f;
-        race.join(f2 > 0.f ? best2 * f2 : 0.f, at2);
-        st.s = pack2(st.sum() * f1 + s2 * f2, 0.f);
+    }
+    // Of all lanes of a warp, for all of them.
+    template <typename T>
+    __device__ __forceinline__ void join_warp(const DrawRow<T> &row) {
+        float top = st.m, sum = st.sum();
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float f = top > kNoLogit ? ex2((st.m - top) * row.c) : 1.f;
+        sum *= f;
+        race.best = f > 0.f ? race.best * f : 0.f;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        float most = most_of_warp(race.best);
+        const bool near = race.best > 0.f && race.best >= most * (1.f - kDrawNear);
+        if (__popc(__ballot_sync(0xffffffffu, near)) > 1) {
+            if (near) race.best = row.score(race.at, top);
+            most = most_of_warp(race.best);
+        }
+        race.at = __reduce_min_sync(0xffffffffu, race.best == most ? race.at : 0x7FFFFFFF);
+        race.best = most;
         st.m = top;
+        st.s = pack2(sum, 0.f);
+    }
+    static __device__ __forceinline__ float most_of_warp(float score) {  // scores are at least 0: ordered as their bits are
+        return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(score)));
+    }
+    __device__ __forceinline__ float4 part() const { return make_float4(st.m, st.sum(), race.best, __int_as_float(race.at)); }
+    __device__ __forceinline__ void set(const float4 &part) {
+        st.m = part.x;
+        st.s = pack2(part.y, 0.f);
+        race.best = part.z;
+        race.at = __float_as_int(part.w);
     }
 };
 
 template <typename T, bool kMask, int kThreads>
-__device__ __forceinline__ void draw_slice(const T *p, const uint32_t *mask, int words, const float *noise, int V, float c,
-                                           int split, int splits, Draw &draw) {
+__device__ __forceinline__ void draw_slice(const DrawRow<T> &source, const uint32_t *mask, int words, int V, int split,
+                                           int splits, Draw &draw) {
+    const T *p = source.p;
+    const float *noise = source.noise;
     constexpr int N = Row<T>::kVec, kUnroll = N == 4 ? 4 : 2;
-    // single tokens that a thread asks for at a time (39 rows of 136321 with a stride that the variates do not have: 12.0
-    // us, one after the other 26)
+    // single tokens that a thread asks for at a time, and the next ones before it scores these (39 rows of 136321 with a
+    // stride that the variates do not have, from HBM: 14.1 us, the next ones only then 16.3)
     constexpr int kBatch = 8;
     const Row<T> row(p, 0, V);
     if (reinterpret_cast<uintptr_t>(noise + row.peel) & 15) {  // single tokens, neighbours side by side
         const int i0 = static_cast<int>(static_cast<long long>(V) * split / splits);
         const int i1 = static_cast<int>(static_cast<long long>(V) * (split + 1) / splits);
-        for (int i = i0 + threadIdx.x; i < i1; i += kThreads * kBatch) {
-            float z[kBatch], e[kBatch];
+        float z[kBatch], e[kBatch], z_next[kBatch], e_next[kBatch];
+        auto load = [&](int i, float (&zs)[kBatch], float (&es)[kBatch]) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const int at = i + k * kThreads, from = at < i1 ? at : i;
-                z[k] = value(p[from]);
-                e[k] = noise[from];
-                if (at >= i1 || (kMask && !((mask[from >> 5] >> (from & 31)) & 1u))) z[k] = kNoLogit;
+                const int at = i + k * kThreads, from = min(at, i1 - 1);
+                zs[k] = value(p[from]);
+                es[k] = noise[from];
+                if (at >= i1 || (kMask && !((mask[from >> 5] >> (from & 31)) & 1u))) zs[k] = kNoLogit;
             }
-            draw.add(z, e, i, c, kThreads);
+        };
+        int i = i0 + threadIdx.x;
+        if (i < i1) load(i, z, e);
+        for (; i < i1; i += kThreads * kBatch) {
+            if (i + kThreads * kBatch < i1) load(i + kThreads * kBatch, z_next, e_next);
+            draw.add(z, e, i, source, kThreads);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                z[k] = z_next[k];
+                e[k] = e_next[k];
+            }
         }
         return;
     }
@@ -570,7 +628,7 @@ __device__ __forceinline__ void draw_slice(const T *p, const uint32_t *mask, int
     if (static_cast<int>(threadIdx.x) < loose) {  // (a thread's indices rise)
         const int i = threadIdx.x;
         const float z[1] = {kMask && !((mask[i >> 5] >> (i & 31)) & 1u) ? kNoLogit : value(p[i])}, e[1] = {noise[i]};
-        draw.add(z, e, i, c);
+        draw.add(z, e, i, source);
     }
     const uint4 *pv = reinterpret_cast<const uint4 *>(p + row.peel);
     const float4 *ev = reinterpret_cast<const float4 *>(noise + row.peel);
@@ -597,14 +655,14 @@ __device__ __forceinline__ void draw_slice(const T *p, const uint32_t *mask, int
                     const float4 &g = f[u][k / 4];
                     e[k] = k % 4 == 0 ? g.x : k % 4 == 1 ? g.y : k % 4 == 2 ? g.z : g.w;
                 }
-                draw.add(z, e, first, c);
+                draw.add(z, e, first, source);
             }
         }
     }
     if (static_cast<int>(threadIdx.x) >= loose && static_cast<int>(threadIdx.x) < count) {
         const int i = behind + threadIdx.x - loose;
         const float z[1] = {kMask && !((mask[i >> 5] >> (i & 31)) & 1u) ? kNoLogit : value(p[i])}, e[1] = {noise[i]};
-        draw.add(z, e, i, c);
+        draw.add(z, e, i, source);
     }
 }
 
@@ -624,24 +682,21 @@ __global__ void __launch_bounds__(kThreads, kDecideResident / kThreads) k_sample
     const float temperature = temperature_of(a, b);
     const bool greedy = temperature == 0.f, usable = n == 0 && temperature >= 0.f && (greedy || a.noise);
     const float c = greedy ? 1.f : exponent_scale(temperature);
+    const DrawRow<T> row{static_cast<const T *>(a.target) + target_offset(a, b, 0), a.noise + b * a.noise_stride, c};
     if (usable) {
         if (greedy) {
             row_slice<T, kMask, kThreads / 32>(a, p, b, 0, rank, ranks, a.target, target_offset(a, b, 0), 0.f, warp_part);
         } else {
             Draw draw;
-            draw_slice<T, kMask, kThreads>(static_cast<const T *>(a.target) + target_offset(a, b, 0),
-                                 kMask ? mask_row(a, p.words, b, 0) : nullptr, p.words, a.noise + b * a.noise_stride, a.V, c, rank,
-                                 ranks, draw);
-#pragma unroll
-            for (int o = 16; o; o >>= 1)
-                draw.join(__shfl_xor_sync(0xffffffffu, draw.st.m, o), __shfl_xor_sync(0xffffffffu, draw.st.sum(), o),
-                          __shfl_xor_sync(0xffffffffu, draw.race.best, o), __shfl_xor_sync(0xffffffffu, draw.race.at, o), c);
-            if (lane == 0) warp_part[warp] = make_float4(draw.st.m, draw.st.sum(), draw.race.best, __int_as_float(draw.race.at));
+            draw_slice<T, kMask, kThreads>(row, kMask ? mask_row(a, p.words, b, 0) : nullptr, p.words, a.V, rank, ranks, draw);
+            draw.join_warp(row);
+            if (lane == 0) warp_part[warp] = draw.part();
             __syncthreads();
-            if (threadIdx.x == 0) {
-                for (int w = 1; w < kThreads / 32; ++w)
-                    draw.join(warp_part[w].x, warp_part[w].y, warp_part[w].z, __float_as_int(warp_part[w].w), c);
-                warp_part[0] = make_float4(draw.st.m, draw.st.sum(), draw.race.best, __int_as_float(draw.race.at));
+            if (warp == 0) {
+                draw = Draw();
+                if (lane < kThreads / 32) draw.set(warp_part[lane]);
+                draw.join_warp(row);
+                if (lane == 0) warp_part[0] = draw.part();
             }
         }
         if (threadIdx.x == 0) {
@@ -653,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, kDecideResident / kThreads) k_sample
         }
     }
     cluster_sync();
-    if (rank != 0 || threadIdx.x != 0) return;
+    if (rank != 0 || warp != 0) return;
     int next = -1;
     if (usable && greedy) {
         Best best;
@@ -665,10 +720,11 @@ __global__ void __launch_bounds__(kThreads, kDecideResident / kThreads) k_sample
         if (!nan && best.m > kNoLogit && best.m < -kNoLogit) next = best.at;
     } else if (usable) {
         Draw draw;
-        for (int r = 0; r < ranks; ++r)
-            draw.join(cta_part[r].x, cta_part[r].y, cta_part[r].z, __float_as_int(cta_part[r].w), c);
+        if (lane < ranks) draw.set(cta_part[lane]);
+        draw.join_warp(row);
         if (draw.st.ok() && draw.race.best > 0.f) next = draw.race.at;
     }
+    if (lane != 0) return;
     a.out_accepted[b] = 0;
     a.out_token[b] = next;
     a.out_status[b] = next < 0 ? RPD_ERR_INVALID_ARGUMENT : RPD_OK;

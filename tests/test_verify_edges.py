@@ -192,3 +192,32 @@ def test_error_of_the_probabilities(dtype):
     off = (torch.tensor(got["prob"], device="cuda").double() / p - 1).abs()
     print(f"off {off.max().item():.3g}, of the bound {(off / bound).max().item():.3g}")
     assert (off <= bound).all()
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("single", [False, True])
+@pytest.mark.parametrize("draft", [None, False, True])
+def test_a_tie_anywhere_in_the_row_goes_to_the_lowest_index(dtype, single, draft):
+    """Two tokens with the same logits and the same variate, by far the smallest of the row: wherever they lie, and whatever
+    the largest logits of their parts of the row are."""
+    B, V = 150, 6008
+    c = Case(B, 0 if draft is None else 1, V, dtype, draft, spread=4.0, seed=2)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    pair = torch.rand(B, V, device="cuda", generator=gen).topk(2, 1).indices.sort(1).values
+    row = 0
+    c.temperature.fill_(1.0)
+    if draft is not None:
+        row = 1 if draft else 0  # behind an accepted draft, or in a rejected one's place
+        c.uniform.fill_(0.0 if draft else 1 - 2.0 ** -24)
+        c.tokens = c.target[:, :1].float().argmin(2).int()
+    below = 6 * torch.rand(B, 1, device="cuda", generator=gen)  # at least e^-6 2^27 in the race, others at most 100
+    c.target[:, row].scatter_(1, pair, (c.target[:, row].float().amax(1, keepdim=True) - below).to(c.dtype).expand(B, 2))
+    c.noise.clamp_(min=0.01)
+    c.noise.scatter_(1, pair, (2.0 ** -28 * (1 + torch.rand(B, 1, device="cuda", generator=gen))).expand(B, 2))
+    if single:
+        read_singly(c)
+    got = c.run()
+    assert (got["status"] == 0).all() and (got["accepted"] == row).all()
+    assert got["token"][:, row].tolist() == pair[:, 0].tolist()
