@@ -110,17 +110,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// cp.async: 16 bytes a lane, past L1; commit closes a group of copies, wait<N> returns once all but the
-// last N groups have landed.
-__device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // The launch's activations in shared memory: rows of `row_bytes` as scale_u leaves them, zero beyond column d; and
 // what a row's logits are multiplied with.  The warps divide the rows, or a row, evenly.  Ends with a barrier.
 struct RowsSmem {

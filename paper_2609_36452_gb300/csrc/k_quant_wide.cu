@@ -224,16 +224,6 @@ __device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, lon
 
 // ------------------------------------------------------------------------------ the product
 
-// cp.async, as in k_quant.cu.
-__device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // A place in a ring of barriers.
 struct Cursor {
     int at = 0;

@@ -910,7 +910,7 @@ cudaError_t launch_clusters(const VerifyParams &p, int num_sms, cudaStream_t s) 
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = t_no_pdl ? 1 : 2;
+    cfg.numAttrs = 2;
     return p.a.D > 0 ? cudaLaunchKernelEx(&cfg, k_verify_decide<T, kMask, kThreads>, p)
                      : cudaLaunchKernelEx(&cfg, k_sample<T, kMask, kThreads>, p);
 }

@@ -45,6 +45,17 @@ struct MetaVec<true> {
     typedef uint2 type;  // scale and zero point of a row in each word
 };
 
+// cp.async: 16 bytes a lane, past L1; commit closes a group of copies, wait<N> returns once all but the
+// last N groups have landed.
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // Loads from shared memory by its own addresses (a pointer that the compiler cannot trace back to shared memory is
 // read by generic loads, which wait like those from global memory).
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
