@@ -182,8 +182,9 @@ __device__ __forceinline__ uint32_t idesc_f16(int n) {
     return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (128u >> 4 << 24);
 }
 
-// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after `limit` cycles
-// or once another role has raised it.
+// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after abort[1] times 1024
+// cycles or once another role has raised it.  (The limit is read where it is needed: as a number of 64 bits from the
+// parameters it cost the loops of 64 rows registers, 152064 x 3584 in groups of 32 7 us of 170.)
 __device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  // sleeps up to 2 us
     uint32_t ok;
     asm volatile(
@@ -197,13 +198,13 @@ __device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  
         : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
+__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort) {
     const uint32_t a = smem_u32(bar);
     if (try_wait_long(a, parity)) return true;
     const long long t0 = clock64();
     while (!try_wait_long(a, parity)) {
         if (*abort) return false;
-        if (clock64() - t0 > limit) {
+        if (clock64() - t0 > static_cast<long long>(abort[1]) << 10) {
             *abort = 1;
             return false;
         }
@@ -211,14 +212,14 @@ __device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volat
     return true;
 }
 // By a converged warp, which stays so.
-__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
-    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort, limit));
+__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort));
 }
 // On the way out: whatever the abort flag says.
-__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, long long limit) {
+__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, volatile int *abort) {
     const uint32_t a = smem_u32(bar);
     const long long t0 = clock64();
-    while (!mbar_try_wait(a, parity) && clock64() - t0 < limit) {
+    while (!mbar_try_wait(a, parity) && clock64() - t0 < static_cast<long long>(abort[1]) << 10) {
     }
 }
 
@@ -297,8 +298,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         drained;
     __shared__ uint32_t tmem_slot;
     __shared__ float factor[kWideMaxRows];
-    __shared__ int abort_flag;
-    volatile int *abort = &abort_flag;
+    __shared__ int give_up[2];  // whether a wait has run out, and its limit in 1024 cycles
+    volatile int *abort = give_up;
     uint8_t *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int stage_bytes = n * 256 + kWideCodeBytes;
@@ -310,7 +311,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     pdl_trigger();
     if (warp == kWideMma) tmem_alloc(&tmem_slot, 512);
     if (threadIdx.x == 0) {
-        abort_flag = 0;
+        give_up[0] = 0;
+        give_up[1] = static_cast<int>(p.q.wait_cycles >> 10);
         for (int i = 0; i < p.stages; ++i) {
             mbar_init(&full[i], 2);
             mbar_init(&done[i], 1);
@@ -346,7 +348,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 const int bytes = (pairs - rest + (rest > 2 ? 4 : rest ? 2 : 0)) * kWidePairBytes;
                 for (int kb = 0; kb < steps; ++kb) {
                     if (issued == p.stages) pdl_wait();
-                    if (issued >= p.stages) ok = wait_phase(&done[s.at], s.phase ^ 1u, abort, p.q.wait_cycles);
+                    if (issued >= p.stages) ok = wait_phase(&done[s.at], s.phase ^ 1u, abort);
                     if (!ok) break;
                     uint8_t *to = smem + s.at * stage_bytes;
                     if (codes) {
@@ -385,13 +387,13 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             const bool two = pair1 - unit > kWideHalf;
             for (int kb = 0; kb < steps; ++kb) {
                 // (the warps that arrive here have seen the whole stage land, activations too)
-                ok = wait_phase_warp(&a_full[a.at], a.phase, abort, p.q.wait_cycles);
+                ok = wait_phase_warp(&a_full[a.at], a.phase, abort);
                 if (!ok) break;
                 const uint64_t b = b_base + static_cast<uint32_t>(s.at * stage_bytes) / 16;
                 const uint32_t a_at = base + kWideAccCols + a.at * 128;
 #pragma unroll 1
                 for (int grp = 0; grp < kGroups; ++grp) {
-                    ok = ok && wait_phase_warp(&acc_empty[acc_next], acc_phase, abort, p.q.wait_cycles);
+                    ok = ok && wait_phase_warp(&acc_empty[acc_next], acc_phase, abort);
                     if (ok) {
                         tc_fence_after_sync();
                         const uint32_t d = base + acc_next * 128;
@@ -419,7 +421,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         }
         // everything issued has to be done before TMEM is given back
         umma_commit_warp(&drained);
-        wait_drained(&drained, 0, p.q.wait_cycles);
+        wait_drained(&drained, 0, abort);
         __syncwarp();
     } else if (warp < 4) {
         // ---- weights to TMEM: a thread a matrix row of each half
@@ -440,7 +442,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         for (int unit = pair0; unit < pair1 && ok; unit += kWideUnit) {
             const bool two = pair1 - unit > kWideHalf;
             for (int kb = 0; kb < steps; ++kb, ++i) {
-                ok = wait_phase_warp(&full[s.at], s.phase, abort, p.q.wait_cycles);
+                ok = wait_phase_warp(&full[s.at], s.phase, abort);
                 if (!ok) break;
                 const uint32_t from = place + s.at * stage_bytes;
                 uint2 w[16];
@@ -463,7 +465,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                 }
                 if (i >= kWideSlots) {
-                    ok = wait_phase_warp(&done[before.at], before.phase, abort, p.q.wait_cycles);
+                    ok = wait_phase_warp(&done[before.at], before.phase, abort);
                     if (!ok) break;
                     before.next(p.stages);
                     tc_fence_after_sync();
@@ -518,8 +520,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 for (int j = 0; j < count; ++j) {
                     const float scale = scale_low<kF16>(kZeros ? lds32(meta_at) : lds16(meta_at));
                     const f32x2 s2 = pack2(scale, scale);
-                    ok = kGroup == 128 ? wait_phase_warp(&done[s.at], s.phase, abort, p.q.wait_cycles)
-                                       : wait_phase_warp(&acc_full[acc.at], acc.phase, abort, p.q.wait_cycles);
+                    ok = kGroup == 128 ? wait_phase_warp(&done[s.at], s.phase, abort)
+                                       : wait_phase_warp(&acc_full[acc.at], acc.phase, abort);
                     if (!ok) break;
                     tc_fence_after_sync();
 #pragma unroll
