@@ -353,16 +353,18 @@ void rpd_destroy(rpd_ctx *ctx);
 
 /* A head in 4 bits: products of a few activation rows with a [V][d] matrix whose elements are 4-bit
  * codes with a scale, and optionally a zero point, for every `group` columns of a row.  (The paper
- * has no counterpart: its heads are bf16.  A step with few rows is bound by reading the head, which
- * in 4 bits is a quarter as long.)
+ * has no counterpart: its heads are bf16, and its step takes no other.  These are a drafter's or a
+ * target's logits, for rpd_verify below: with few rows they are bound by reading the head, which in
+ * 4 bits is a quarter as long.)
  *
  *   y[r][v] = rho_r * sum over groups G of s[v][G] * sum over k in G of (q[v][k] - z[v][G]) * u[r][k]
  *
  * with u = x and rho = 1, or, with a gain g, the readout's normalisation as rpd_step applies it:
  * u = g * x rounded to the type of x, rho_r = (mean_k x[r][k]^2 + eps)^(-1/2) applied after the
  * sum.  Codes, zero points and scales enter exactly, u exactly down to 2^-28 of the row's
- * largest (a smaller element is off by at most 2^-39 of that); products and sums are fp32, and the logits
- * are rounded once, to the type of `out`.  Inputs must be finite.
+ * largest (a smaller element is off by at most 2^-39 of that; under a norm of 2^-126 / rho, where that
+ * is more); products and sums are fp32, and the logits are rounded once, to the type of `out`.  The
+ * inputs and u must be finite, and scales below 2^110.
  *
  * rpd_quant_create: a head of d columns and V rows with groups of 32, 64 or 128 columns (others:
  * RPD_ERR_UNSUPPORTED) on the current device; 1 <= d <= 32768, 1 <= V <= 2^24.  d need not be a
@@ -376,10 +378,10 @@ rpd_quant *rpd_quant_create(int d, int V, int group);
  *          in the upper ones (with odd d the last byte's upper bits are ignored);
  *   scales [V][ceil(d / group)] bf16 or fp16 (scale_type), device;
  *   zeros  [V][ceil(d / group)] uint8, device, lower four bits used; NULL: every zero point is 8.
- * The copy runs on `stream` (which may not be under capture: RPD_ERR_INVALID_ARGUMENT; another stream may be), and the
- * call waits for it; no call on this head may be running or be captured in a graph that is used again
- * (the layout is reallocated).  A head that has weights keeps them where the call fails, unless the
- * device has no room for both: the old ones are then freed first. */
+ * The copy runs on `stream` (which may not be under capture: RPD_ERR_INVALID_ARGUMENT; another
+ * stream may be), and the call waits for it; no call on this head may be running or be captured in a
+ * graph that is used again (the layout is reallocated).  A head that has weights keeps them where the
+ * call fails, unless the device has no room for both: the old ones are then freed first. */
 int rpd_quant_set_weights(rpd_quant *head, const void *codes, const void *scales, int scale_type,
                           const void *zeros, void *stream);
 
@@ -401,12 +403,14 @@ int rpd_quant_logits(const rpd_quant *head, const void *x, int x_type, int64_t x
                      const void *gain, float eps, void *out, int out_type, int64_t out_stride,
                      void *workspace, int64_t workspace_bytes, void *stream);
 
-/* Diagnostics, as rpd_set_wait_limit and rpd_inject_stall.  The waits inside the kernel for more than a few rows are
- * bounded; where one runs out the kernel stops, drains what it has in flight, frees its tensor memory, and the
- * logits that it had not finished are NaN (rpd_quant_logits itself has long returned); the head stays usable.
- *   rpd_quant_set_wait_limit: the bound, in microseconds (default 2 000 000), 1000 .. 60 000 000.
- *   rpd_quant_inject_stall:   while on, that kernel never asks for its activations, so that its waits run
- *                             out; used to test the path (the kernel for a few rows is not affected).
+/* Diagnostics, as rpd_set_wait_limit and rpd_inject_stall.  The waits inside the kernel for more than
+ * a few rows are bounded; where one runs out the kernel stops, drains what it has in flight, frees its
+ * tensor memory, and the logits that it had not finished are NaN (rpd_quant_logits itself has long
+ * returned); the head stays usable.
+ *   rpd_quant_set_wait_limit: the bound, in microseconds of a 2 GHz clock (default 2 000 000),
+ *                             1000 .. 60 000 000.
+ *   rpd_quant_inject_stall:   while on, that kernel never asks for its activations, so that its waits
+ *                             run out; used to test the path (the kernel for a few rows has no waits).
  * Both apply to calls that follow; no call on this head may be running. */
 int rpd_quant_set_wait_limit(rpd_quant *head, int64_t microseconds);
 int rpd_quant_inject_stall(rpd_quant *head, int on);
@@ -429,8 +433,14 @@ void rpd_quant_destroy(rpd_quant *head);
  * target.  A token is drawn as argmax_v w(v) / noise[b][v] (the lowest v on a tie), which with
  * exponential variates is a draw with the weights w.  T = 0 puts p_i at its largest logit (the lowest
  * index on a tie): a draft is accepted where it is that token, and draft rows and random numbers are
- * not read; other T count as at least 1.45e-30 and at most
- * 1.44e37.  D = 0, or lengths of 0, is sampling.
+ * not read; other T count as at least 1.45e-30 and at most 1.44e37.  D = 0, or lengths of 0, is
+ * sampling.
+ * In the race, weights below 2^-126 of the row's largest may count as 0, variates below 2^-126 do (0, and
+ * -0, wins against any other), and variates above 2^126 never win.
+ * q_i has no mask and no temperature of its own: it is the draft model's distribution, and the tokens are
+ * distributed like the target's, only where the drafts were drawn from that.  A draft model that drew
+ * under a mask has its other tokens' logits set to -infinity by the caller, and one that drew at
+ * another temperature T' has its logits multiplied by T / T'.
  *
  * Sizes: B sequences, at most D drafts each, V tokens; 0 <= D <= 1024, 1 <= V <= 2^24 (larger, or
  * more than 2^26 rows of logits: RPD_ERR_UNSUPPORTED).  B = 0 is a no-op. */
@@ -443,7 +453,7 @@ typedef struct rpd_verify_args {
     const uint32_t *allowed;    /* [B][D + 1][ceil(V / 32)] bits, 1 = allowed, bit v % 32 of word v / 32; or
                                    NULL.  Logits of other tokens may hold anything */
     const float *uniform;       /* [B][D] in [0, 1) */
-    const float *noise;         /* [B][V] exponential variates (>= 0; others never win) */
+    const float *noise;         /* [B][V] exponential variates (>= 0; negative ones and NaN never win) */
     int32_t *out_accepted;      /* [B] accepted drafts */
     int32_t *out_token;         /* [B][D + 1] the accepted drafts, the next token, then -1 */
     int32_t *out_status;        /* [B] RPD_OK; or RPD_ERR_INVALID_ARGUMENT, with -1 for the next token, where

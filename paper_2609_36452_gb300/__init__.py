@@ -596,11 +596,12 @@ class QuantHead:
                                      _stream(self.device)))
 
     def set_wait_limit(self, microseconds: int):
+        """The bound of a wait inside the kernel for more than a few rows (default two seconds)."""
         _check(rpd_quant_set_wait_limit(self.handle, int(microseconds)))
 
     def inject_stall(self, on: bool = True):
-        """Diagnostics: while on, the kernel for more than a few rows asks for no activations; its bounded waits run
-        out and the logits are NaN."""
+        """Diagnostics: while on, the kernel for more than a few rows asks for no activations; its bounded
+        waits run out and the logits are NaN."""
         _check(rpd_quant_inject_stall(self.handle, 1 if on else 0))
 
     def logits(self, x, out, gain=None, eps=1e-6, workspace=None):
@@ -635,7 +636,8 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
     int32 and temperature [B] float32 (None: D and 1); allowed [B][D + 1][ceil(V / 32)] int32 bit masks.
     Outputs: out_accepted [B], out_token [B][D + 1], out_status [B] int32 and out_prob [B][D] float32.
     Runs on the current stream of the logits' device.  ``workspace``: a uint8 CUDA tensor of
-    rpd_verify_workspace bytes (None: the binding's own, on the default stream one that the thread keeps)."""
+    rpd_verify_workspace bytes (None: the binding's own, on the default stream one that the thread keeps).
+    draft's rows are taken as they are: where the drafts were drawn under a mask, set the other tokens to -inf."""
     shape = getattr(target, "shape", ())
     if len(shape) != 3 or shape[1] < 1:
         raise RpdError(RPD_ERR_INVALID_ARGUMENT, "target: a tensor of [B][D + 1][V] logits is required")

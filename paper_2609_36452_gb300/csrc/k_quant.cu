@@ -16,7 +16,7 @@
 // subnormal's has up to ten places less than that says.  It was no faster.)
 //
 // What bounds it: reading the codes once.  One row of a 126464 x 4096 head in groups of 128 is 259 MB of codes and 8 MB
-// of scales, 39.4 us at 6780 GB/s; it takes 45.5 (5.9 TB/s), 8 rows 49.3, 9 rows 65.6, 16 rows 67.3.  As bf16 numbers
+// of scales, 39.4 us at 6780 GB/s; it takes 45.8 (5.8 TB/s), 8 rows 49.4, 9 rows 63.7, 16 rows 66.0.  As bf16 numbers
 // 128 + q less 128 + z (three instructions a pair of codes, 87 for 512 bytes in all) one row took 66 us.
 //
 // k_quant_rows: up to 16 rows a CTA (many rows of a head that fills the device: k_quant_wide.cu).  A warp multiplies pairs of tiles of 16 matrix rows (M of the
@@ -393,8 +393,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_quant_rows(const QuantParam
 
 constexpr int kRowsMax = 16;                 // activation rows of a CTA
 // More rows are the other kernel's, unless every CTA for them has an SM to itself (rows_of_cta).  126464 x 4096: 16 rows
-// 65.8 us here (95 there), 17 rows 96.3 there (120 here); 15872 x 4096: 21.8 (27), and 26.7 (34).  2000 x 4096: 32 rows,
-// 126 CTAs, 16.4 us here (23.6), 48 rows, which would be 189, 24.5 there (31.4).
+// 66.0 us here (95 there), 17 rows 96.2 there (120 here); 15872 x 4096: 21.9 (27), and 26.7 (34).  2000 x 4096: 32 rows,
+// 126 CTAs, 16.6 us here (23.6), 48 rows, which would be 189, 24.7 there (31.4).  From d = 4480 on 16 rows are two groups
+// here and more, each of which reads the codes again; that is not weighed.
 constexpr int kRowsMost = 16;
 constexpr int kRowsSmem = 224 * 1024;        // of the 227 KB a CTA may have
 

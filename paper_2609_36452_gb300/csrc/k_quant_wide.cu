@@ -11,8 +11,8 @@
 // on 256 matrix rows at a time, as two halves that share every stage of activations: a stage is 128 columns of both (16 KB
 // of codes, 8 or 16 KB of activations).
 //
-// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us; 17 rows take 96.3, 32 rows 98.9, 33 rows 108, 64
-// rows 113, 128 rows 218, and with stored zero points 20 rows 106), nor the tensor cores (an MMA of M = 128 and N =
+// What bounds it: not HBM (one pass over a 126464 x 4096 head is 39 us; 17 rows take 96.2, 32 rows 98.7, 33 rows 109, 64
+// rows 113, 128 rows 218, and with stored zero points 20 rows 107), nor the tensor cores (an MMA of M = 128 and N =
 // 32 / 64 with A in TMEM takes 18 / 32 cycles, 15 us a pass in all), but what a stage costs its roles one after the other: 1550 cycles
 // where the codes' share of HBM is 700.  Of 93 us, measured when the operand still was the masked codes, 22 went without
 // the stores to TMEM, 6 without the epilogue's arithmetic, 5 without the MMAs; copies and hand-overs alone took 59.
@@ -605,7 +605,7 @@ cudaError_t launch_x(const QuantParams &p, int n, int passes, uint8_t *xs, float
 }
 
 // Passes over the codes, their rows and what these are padded to: 64, or 32 where that makes no more passes or they all
-// run side by side.  (126464 x 4096: 33 rows, padded to 64, take 108 us, 32 rows as 32 take 98.9; 1022 x 1254: 80
+// run side by side.  (126464 x 4096: 33 rows, padded to 64, take 109 us, 32 rows as 32 take 98.7; 1022 x 1254: 80
 // rows 12.6, as two passes of 64 in turn 26.6.)
 struct WidePasses {
     int passes, per_pass, n;

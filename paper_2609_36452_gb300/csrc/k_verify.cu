@@ -16,7 +16,8 @@
 // us, of which 4 are a chain of waits (partial sums, verdicts, scan, join).  Statistics are fp32; differences z - m come
 // before the multiplication by 1 / T (with bf16 and fp16 logits they are exact or nearly so).  Without drafts
 // (k_sample) a cluster makes the statistics and runs the race in one pass: 128 rows of 126464 bf16 logits under a
-// mask, with their variates 99 MB, in 18.0 us (5.5 TB/s; as statistics and a second pass 45).
+// mask, with their variates 99 MB, in 21.1 us from HBM (4.7 TB/s; 18.4 where the same inputs come again and part of them is
+// still in L2; as statistics and a second pass 45).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

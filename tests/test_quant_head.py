@@ -1,13 +1,15 @@
 """The 4-bit head (rpd_quant_*): refusals (no GPU), and its logits against the definition in 64 bits.
 
-Tolerance.  A logit is a sum over groups of s sum (q - z) u, with more than 16 rows of s (sum q u - z sum u).  The
-products are exact in fp32, and a group is summed in fp32 in steps of 16 columns (the tensor core may cut its
-addends off instead of rounding them: 2^-23 of the sum S of the sizes s (q + z) |u| for every step), the groups'
+Tolerance.  A logit is a sum over groups of s sum (q - z) u.  The bound is that of s (sum q u - z sum u), a form with
+larger sums: the products are exact in fp32, and a group is summed in fp32 in steps of 16 columns (the tensor core may
+cut its addends off instead of rounding them: 2^-23 of the sum S of the sizes s (q + z) |u| for every step), the groups'
 sums are added up in fp32, as are the sums of u, and at most 16 partial sums are joined.  A logit sees at most
-group / 16 + d / group + 28 such roundings.  The activations enter as fp16 numbers scaled by a power of two:
-exact down to 2^-24 of the row's largest, smaller ones off by at most 2^-35 of it.  The factor rho is right to
-48 * 2^-24 (a chain of at most 40 additions under a square root, rsqrtf's two last places and a division).
-The logit itself is rounded once to the type of the output, by half of its eps or of its smallest subnormal."""
+group / 16 + d / group + 28 such roundings.  The activations enter as fp16 numbers scaled by a power of two; the bound
+takes them for exact down to 2^-24 of the row's largest, and smaller ones for off by at most 2^-35 of it.  The
+kernels sum (q - z) u and are exact down to 2^-28, with 2^-39 below: test_quant_edges.py holds them to that.  The
+factor rho is right to 48 * 2^-24 (a chain of at most 40 additions under a square root, rsqrtf's two last places and
+a division).  The logit itself is rounded once to the type of the output, by half of its eps or of its smallest
+subnormal."""
 import ctypes
 import os
 import threading

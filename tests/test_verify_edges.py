@@ -3,6 +3,7 @@ ranges, sizes beyond 32 bits.  Decisions are held against the definition in 64 b
 import ctypes
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -221,3 +222,29 @@ def test_a_tie_anywhere_in_the_row_goes_to_the_lowest_index(dtype, single, draft
     got = c.run()
     assert (got["status"] == 0).all() and (got["accepted"] == row).all()
     assert got["token"][:, row].tolist() == pair[:, 0].tolist()
+
+
+@gpu
+@needs_gpu
+def test_drafts_drawn_under_the_target_s_mask():
+    """A draft model that drew under a mask, its other logits at -infinity: the first token that a sequence yields is a draw
+    from the masked target; 20000 sequences, every frequency within five standard deviations."""
+    B, V = 20000, 6
+    g = torch.Generator(device="cuda").manual_seed(11)
+    dev = dict(device="cuda", generator=g)
+    on = torch.tensor([True, False, True, True, False, True], device="cuda")
+    z = torch.tensor([0.0, 5.0, -1.0, 1.0, math.nan, 0.5], device="cuda")
+    y = torch.where(on, torch.randn(V, **dev), -math.inf)
+    c = Case(2, 1, V)
+    c.B, c.on = B, on.expand(B, 2, V)
+    c.pack()
+    c.target, c.draft, c.temperature = z.expand(B, 2, V), y.expand(B, 1, V), None
+    e = torch.empty(B, V, device="cuda").exponential_(generator=g)
+    c.tokens = (y - e.log()).argmax(1).int().view(B, 1)
+    c.uniform = torch.rand(B, 1, **dev)
+    c.noise = torch.empty(B, V, device="cuda").exponential_(generator=g)
+    got = c.run()
+    assert (got["status"] == 0).all()
+    p = torch.softmax(torch.where(on, z, -math.inf).double(), 0).cpu().numpy()
+    first = np.bincount(got["token"][:, 0], minlength=V) / B
+    assert (abs(first - p) <= 5 * (p * (1 - p) / B) ** 0.5).all(), (first, p)
