@@ -225,6 +225,14 @@ __device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, vol
 
 // ------------------------------------------------------------------------------ the product
 
+// Copies in flight land before the memory goes.  Stages that only one of the two TMA warps has asked for lack an arrival;
+// neither is more than `stages` of them ahead.
+__device__ __noinline__ void drain_copies(uint64_t *full, int stages, const int *issued_of, volatile int *abort) {
+    const int both = min(issued_of[0], issued_of[1]), any = max(issued_of[0], issued_of[1]);
+    for (int i = both; i < any; ++i) mbar_arrive(&full[i % stages]);
+    for (int i = max(0, any - stages); i < any; ++i) wait_drained(&full[i % stages], (i / stages) & 1, abort);
+}
+
 // A place in a ring of barriers.
 struct Cursor {
     int at = 0;
@@ -298,6 +306,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         drained;
     __shared__ uint32_t tmem_slot;
     __shared__ float factor[kWideMaxRows];
+    __shared__ int issued_of[2];  // stages that the TMA warps have asked for: codes; activations
     __shared__ int give_up[2];  // whether a wait has run out, and its limit in 1024 cycles
     volatile int *abort = give_up;
     uint8_t *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
@@ -312,6 +321,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     if (warp == kWideMma) tmem_alloc(&tmem_slot, 512);
     if (threadIdx.x == 0) {
         give_up[0] = 0;
+        issued_of[0] = issued_of[1] = (pair1 - pair0 + kWideUnit - 1) / kWideUnit * steps;  // unless a wait runs out
         give_up[1] = static_cast<int>(p.q.wait_cycles >> 10);
         for (int i = 0; i < p.stages; ++i) {
             mbar_init(&full[i], 2);
@@ -364,12 +374,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     s.next(p.stages);
                 }
             }
-            if (!ok || *abort) {  // the copies in flight land before the memory goes (no wait can tell with the other
-                                  // warp's copies missing: a millisecond is a thousand times what they take)
-                const long long t0 = clock64();
-                while (clock64() - t0 < 2000000) {
-                }
-            }
+            if (!ok) issued_of[codes ? 0 : 1] = issued;
         }
         __syncwarp();
     } else if (warp == kWideMma) {
@@ -566,6 +571,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    if (*abort && threadIdx.x == 0) drain_copies(full, p.stages, issued_of, abort);
     if (warp == kWideMma) tmem_free(tmem, 512);
 }
 
