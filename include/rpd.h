@@ -418,6 +418,60 @@ int rpd_quant_inject_stall(rpd_quant *head, int on);
 /* Free the head (no call on it may be running).  NULL is ignored. */
 void rpd_quant_destroy(rpd_quant *head);
 
+/* A head in 8 bits: products of activation rows, from one to thousands, with a [V][d] matrix of e4m3
+ * codes that has an fp32 scale for every 128 x 128 of them (rpd_fp8_quantize makes both).  As the 4-bit
+ * head above it yields the logits that rpd_sample and rpd_verify take; its codes are twice as long,
+ * and with many rows it runs at the tensor cores' 8-bit rate.
+ *
+ *   y[r][v] = rho_r * sum over blocks B of 128 columns of
+ *                     sw[v / 128][B] * sx[r][B] * sum over k in B of qw[v][k] * qx[r][k]
+ *
+ * u = x and rho = 1, or with a gain g u = g * x rounded to the type of x and rho_r = (mean_k x[r][k]^2 +
+ * eps)^(-1/2), as for the 4-bit head.  The activations are brought to e4m3 by the call: sx[r][B] = the largest
+ * |u[r][k]| of the block / 448, qx = u / sx, both divisions in fp32, the quotient rounded to the nearest
+ * e4m3 number (ties to even; a block whose scale is 0 has codes of 0).  Sums are fp32; the logits are
+ * rounded once, to the type of `out`.  Inputs and u must be finite, codes no NaN, scales 0 or within
+ * 2^-100 .. 2^110 in size.
+ *
+ * rpd_fp8_create: a head of d columns and V rows on the current device; 1 <= d <= 32768, 1 <= V <= 2^24 and
+ * fewer than 256 GB of codes.  NULL on failure. */
+typedef struct rpd_fp8 rpd_fp8; /* opaque, owned by the library */
+rpd_fp8 *rpd_fp8_create(int d, int V);
+
+/* Copy the weights into the head's own layout (V * d bytes and the scales, padded to 256 rows and whole
+ * blocks); nothing of the caller's is read after the call returns.
+ *   codes  [V][d] e4m3 bytes, device;  scales [ceil(V / 128)][ceil(d / 128)] fp32, device.
+ * The copy runs on `stream` (which may not be under capture: RPD_ERR_INVALID_ARGUMENT; another stream may
+ * be), and the call waits for it; no call on this head may be running.  The layout stays where it is: graphs
+ * that have captured calls use the new weights when they run again. */
+int rpd_fp8_set_weights(rpd_fp8 *head, const void *codes, const float *scales, void *stream);
+
+/* Device bytes of workspace that rpd_fp8_logits needs for that many rows; -1 for a NULL head or rows < 0. */
+int64_t rpd_fp8_workspace(const rpd_fp8 *head, int rows);
+
+/* Logits of `rows` activations; arguments and conditions as for rpd_quant_logits. */
+int rpd_fp8_logits(const rpd_fp8 *head, const void *x, int x_type, int64_t x_stride, int rows,
+                   const void *gain, float eps, void *out, int out_type, int64_t out_stride,
+                   void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Diagnostics, as rpd_quant_set_wait_limit and rpd_quant_inject_stall; here every call has waits. */
+int rpd_fp8_set_wait_limit(rpd_fp8 *head, int64_t microseconds);
+int rpd_fp8_inject_stall(rpd_fp8 *head, int on);
+
+/* Free the head (no call on it may be running).  NULL is ignored. */
+void rpd_fp8_destroy(rpd_fp8 *head);
+
+/* Bring a matrix to e4m3 with an fp32 scale for every 128 columns of block_rows rows (1: activations, 128:
+ * the head's weights), asynchronously on `stream` (a cudaStream_t of the device that holds x; NULL = legacy
+ * default): scale = largest |x| of the block / 448, code = x / scale to the nearest e4m3 number, as above.
+ *   x      [rows][cols] bf16, fp16 or fp32 (x_type), device, rows x_stride elements apart; finite;
+ *   codes  [rows][cols] bytes, device, rows codes_stride apart; bytes between the rows stay as they were;
+ *   scales [ceil(rows / block_rows)][ceil(cols / 128)] fp32, device.
+ * Strides are >= cols (of no matter with one row); rows = 0 or cols = 0 is a no-op; a block_rows other than 1
+ * and 128 is RPD_ERR_UNSUPPORTED.  Outputs may not overlap x. */
+int rpd_fp8_quantize(const void *x, int x_type, int64_t x_stride, int rows, int cols, int block_rows,
+                     void *codes, int64_t codes_stride, float *scales, void *stream);
+
 /* Drafted tokens checked against a target model, from given random numbers.  (The paper has no
  * counterpart: rpd_step decides from one model's own confidence which positions to fill; this decides
  * which of a sequence's drafted tokens - a draft model's, or a block that rpd_step committed - a

@@ -22,6 +22,8 @@ __all__ = [
     "rpd_build_decode_loop", "rpd_build_decode_loop_batched", "rpd_decode_loop_launch", "rpd_decode_loop_destroy", "DecodeLoop",
     "rpd_quant_create", "rpd_quant_set_weights", "rpd_quant_workspace", "rpd_quant_logits", "rpd_quant_destroy", "QuantHead",
     "rpd_quant_set_wait_limit", "rpd_quant_inject_stall",
+    "rpd_fp8_create", "rpd_fp8_set_weights", "rpd_fp8_workspace", "rpd_fp8_logits", "rpd_fp8_set_wait_limit",
+    "rpd_fp8_inject_stall", "rpd_fp8_destroy", "rpd_fp8_quantize", "Fp8Head", "quantize_fp8",
     "rpd_verify_workspace", "rpd_verify", "verify", "RpdVerifyArgs",
     "rpd_destroy", "rpd_last_error", "rpd_version", "Rpd", "RULE_PROFILES", "KERNEL_NAMES",
 ]
@@ -148,6 +150,15 @@ def _load():
         "rpd_quant_set_wait_limit": (i32, [vp, ctypes.c_int64]),
         "rpd_quant_inject_stall": (i32, [vp, i32]),
         "rpd_quant_destroy": (None, [vp]),
+        "rpd_fp8_create": (vp, [i32, i32]),
+        "rpd_fp8_set_weights": (i32, [vp, vp, vp, vp]),
+        "rpd_fp8_workspace": (ctypes.c_int64, [vp, i32]),
+        "rpd_fp8_logits": (i32, [vp, vp, i32, ctypes.c_int64, i32, vp, f32, vp, i32, ctypes.c_int64,
+                                 vp, ctypes.c_int64, vp]),
+        "rpd_fp8_set_wait_limit": (i32, [vp, ctypes.c_int64]),
+        "rpd_fp8_inject_stall": (i32, [vp, i32]),
+        "rpd_fp8_destroy": (None, [vp]),
+        "rpd_fp8_quantize": (i32, [vp, i32, ctypes.c_int64, i32, i32, i32, vp, ctypes.c_int64, vp, vp]),
         "rpd_verify_workspace": (ctypes.c_int64, [i32, i32]),
         "rpd_verify": (i32, [ctypes.POINTER(RpdVerifyArgs), vp, ctypes.c_int64, vp]),
         "rpd_destroy": (None, [vp]),
@@ -195,6 +206,14 @@ rpd_quant_logits = lib.rpd_quant_logits
 rpd_quant_set_wait_limit = lib.rpd_quant_set_wait_limit
 rpd_quant_inject_stall = lib.rpd_quant_inject_stall
 rpd_quant_destroy = lib.rpd_quant_destroy
+rpd_fp8_create = lib.rpd_fp8_create
+rpd_fp8_set_weights = lib.rpd_fp8_set_weights
+rpd_fp8_workspace = lib.rpd_fp8_workspace
+rpd_fp8_logits = lib.rpd_fp8_logits
+rpd_fp8_set_wait_limit = lib.rpd_fp8_set_wait_limit
+rpd_fp8_inject_stall = lib.rpd_fp8_inject_stall
+rpd_fp8_destroy = lib.rpd_fp8_destroy
+rpd_fp8_quantize = lib.rpd_fp8_quantize
 rpd_verify_workspace = lib.rpd_verify_workspace
 rpd_verify = lib.rpd_verify
 rpd_destroy = lib.rpd_destroy
@@ -239,7 +258,7 @@ def _torch():
     if _torch_module is None:
         import torch
         _Tensor = torch.Tensor
-        for n in ("bfloat16", "float16", "float32", "int32", "uint8"):
+        for n in ("bfloat16", "float16", "float32", "int32", "uint8", "float8_e4m3fn"):
             _DTYPES[n] = getattr(torch, n)
             _DTYPES[getattr(torch, n)] = ELEMENT_TYPES.get("torch." + n)
         _torch_module = torch
@@ -557,14 +576,12 @@ def stats_dict(t) -> dict:
     return dict(zip(STATS_FIELDS, vals))
 
 
-class QuantHead:
-    """A [V][d] head of 4-bit codes with a scale (and optionally a zero point) for every ``group``
-    columns of a row (rpd_quant_*), on the device that is current when it is made."""
+class _ReducedHead:
+    """What the heads in reduced precision share: a handle of the library's, and the readout through it.
+    A subclass names its entry points (rpd_quant_*, rpd_fp8_*)."""
+    handle = None
 
-    def __init__(self, d: int, V: int, group: int = 128):
-        self.d, self.V, self.group = d, V, group
-        self.handle = None
-        h = rpd_quant_create(_size(d, "d"), _size(V, "V"), _size(group, "group"))
+    def _made(self, h):
         if not h:
             raise RpdError(RPD_ERR_INVALID_ARGUMENT, rpd_last_error().decode())
         self.handle = ctypes.c_void_p(h)
@@ -572,7 +589,7 @@ class QuantHead:
 
     def close(self):
         if getattr(self, "handle", None):
-            rpd_quant_destroy(self.handle)
+            self._c_destroy(self.handle)
             self.handle = None
 
     def __del__(self):
@@ -580,6 +597,47 @@ class QuantHead:
             self.close()
         except Exception:
             pass
+
+    def set_wait_limit(self, microseconds: int):
+        """The bound of a wait inside the kernels that have waits (default two seconds)."""
+        _check(self._c_set_wait_limit(self.handle, int(microseconds)))
+
+    def inject_stall(self, on: bool = True):
+        """Diagnostics: while on, kernels that have waits ask for no activations; their bounded waits run out and
+        the logits are NaN."""
+        _check(self._c_inject_stall(self.handle, 1 if on else 0))
+
+    def logits(self, x, out, gain=None, eps=1e-6, workspace=None):
+        """out[r] = W x[r], or with ``gain`` the readout of the normalised x[r]: x [rows][d] bf16 or
+        fp16, out [rows][V] bf16, fp16 or float32, gain [d] like x; rows may lie apart.  Runs on the
+        device's current stream.  ``workspace``: a uint8 CUDA tensor of rpd_quant_workspace or
+        rpd_fp8_workspace bytes (None: the binding's own, on the default stream one that the thread keeps)."""
+        rows = _size(x.shape[0], "rows of x") if hasattr(x, "shape") and len(x.shape) == 2 else 0
+        T = _torch()
+        px, xt, xs = _rows_arg(x, "x", (T.bfloat16, T.float16), (rows, self.d))
+        po, ot, os_ = _rows_arg(out, "out", (T.bfloat16, T.float16, T.float32), (rows, self.V))
+        _same_device(self.device, x=x, out=out)
+        pg = _dense_arg(gain, "gain", str(x.dtype)[6:], self.d, self.device) if gain is not None else None
+        stream, pw, size = _stream(self.device), None, 0
+        if workspace is not None:
+            size = workspace.numel()
+            pw = _dense_arg(workspace, "workspace", "uint8", size, self.device)
+        else:
+            need = self._c_workspace(self.handle, rows)
+            if need > 0:
+                pw, size, workspace = _workspace(need, self.device, stream)
+        _check(self._c_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw, size, stream))
+
+
+class QuantHead(_ReducedHead):
+    """A [V][d] head of 4-bit codes with a scale (and optionally a zero point) for every ``group``
+    columns of a row (rpd_quant_*), on the device that is current when it is made."""
+    _c_logits, _c_workspace, _c_destroy = rpd_quant_logits, rpd_quant_workspace, rpd_quant_destroy
+    _c_set_wait_limit, _c_inject_stall = rpd_quant_set_wait_limit, rpd_quant_inject_stall
+
+    def __init__(self, d: int, V: int, group: int = 128):
+        self.d, self.V, self.group = d, V, group
+        self._made(rpd_quant_create(_size(d, "d"), _size(V, "V"), _size(group, "group")))
 
     def set_weights(self, codes, scales, zeros=None):
         """codes [V][(d + 1) // 2] uint8 (the even column in the lower four bits), scales
@@ -595,35 +653,44 @@ class QuantHead:
         _check(rpd_quant_set_weights(self.handle, args[0], args[1], ELEMENT_TYPES[str(scales.dtype)], args[2],
                                      _stream(self.device)))
 
-    def set_wait_limit(self, microseconds: int):
-        """The bound of a wait inside the kernel for more than a few rows (default two seconds)."""
-        _check(rpd_quant_set_wait_limit(self.handle, int(microseconds)))
 
-    def inject_stall(self, on: bool = True):
-        """Diagnostics: while on, the kernel for more than a few rows asks for no activations; its bounded
-        waits run out and the logits are NaN."""
-        _check(rpd_quant_inject_stall(self.handle, 1 if on else 0))
+class Fp8Head(_ReducedHead):
+    """A [V][d] head of e4m3 codes with a float32 scale for every 128 x 128 of them (rpd_fp8_*), on the device
+    that is current when it is made.  ``quantize_fp8`` makes its weights."""
+    _c_logits, _c_workspace, _c_destroy = rpd_fp8_logits, rpd_fp8_workspace, rpd_fp8_destroy
+    _c_set_wait_limit, _c_inject_stall = rpd_fp8_set_wait_limit, rpd_fp8_inject_stall
 
-    def logits(self, x, out, gain=None, eps=1e-6, workspace=None):
-        """out[r] = W x[r], or with ``gain`` the readout of the normalised x[r]: x [rows][d] bf16 or
-        fp16, out [rows][V] bf16, fp16 or float32, gain [d] like x; rows may lie apart.  Runs on the
-        device's current stream.  ``workspace``: a uint8 CUDA tensor of rpd_quant_workspace bytes
-        (None: the binding's own, on the default stream one that the thread keeps)."""
-        rows = _size(x.shape[0], "rows of x") if hasattr(x, "shape") and len(x.shape) == 2 else 0
-        T = _torch()
-        px, xt, xs = _rows_arg(x, "x", (T.bfloat16, T.float16), (rows, self.d))
-        po, ot, os_ = _rows_arg(out, "out", (T.bfloat16, T.float16, T.float32), (rows, self.V))
-        _same_device(self.device, x=x, out=out)
-        pg = _dense_arg(gain, "gain", str(x.dtype)[6:], self.d, self.device) if gain is not None else None
-        stream, pw, size = _stream(self.device), None, 0
-        if workspace is not None:
-            size = workspace.numel()
-            pw = _dense_arg(workspace, "workspace", "uint8", size, self.device)
-        else:
-            need = rpd_quant_workspace(self.handle, rows)
-            if need > 0:
-                pw, size, workspace = _workspace(need, self.device, stream)
-        _check(rpd_quant_logits(self.handle, px, xt, xs[0], rows, pg, eps, po, ot, os_[0], pw, size, stream))
+    def __init__(self, d: int, V: int):
+        self.d, self.V = d, V
+        self._made(rpd_fp8_create(_size(d, "d"), _size(V, "V")))
+
+    def set_weights(self, codes, scales):
+        """codes [V][d] float8_e4m3fn (or uint8, the same bytes), scales [ceil(V / 128)][ceil(d / 128)] float32;
+        contiguous CUDA tensors, copied."""
+        kind = "uint8" if str(getattr(codes, "dtype", None)) == "torch.uint8" else "float8_e4m3fn"
+        pc = _dense_arg(codes, "codes", kind, self.V * self.d, self.device)
+        ps = _dense_arg(scales, "scales", "float32", -(-self.V // 128) * -(-self.d // 128), self.device)
+        _check(rpd_fp8_set_weights(self.handle, pc, ps, _stream(self.device)))
+
+
+def quantize_fp8(x, codes, scales, block_rows=1):
+    """x [rows][cols] (bf16, fp16 or float32) as e4m3 codes with a scale for every 128 columns of ``block_rows`` rows,
+    1 (activations) or 128 (an Fp8Head's weights): codes [rows][cols] float8_e4m3fn or uint8, scales
+    [ceil(rows / block_rows)][ceil(cols / 128)] float32, contiguous.  Rows of x and codes may lie apart.  Runs on
+    the current stream of x's device."""
+    shape = getattr(x, "shape", ())
+    if len(shape) != 2:
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, "x: a tensor of [rows][cols] is required")
+    if block_rows not in (1, 128):
+        raise RpdError(RPD_ERR_UNSUPPORTED, f"block_rows must be 1 or 128 (got {block_rows})")
+    rows, cols = _size(shape[0], "rows"), _size(shape[1], "cols")
+    T = _torch()
+    px, kind, xs = _rows_arg(x, "x", (T.bfloat16, T.float16, T.float32), (rows, cols))
+    dev = x.get_device()
+    pc, _, cs = _rows_arg(codes, "codes", (T.float8_e4m3fn, T.uint8), (rows, cols))
+    _same_device(dev, codes=codes)
+    ps = _dense_arg(scales, "scales", "float32", -(-rows // block_rows) * -(-cols // 128), dev)
+    _check(rpd_fp8_quantize(px, kind, xs[0], rows, cols, block_rows, pc, cs[0], ps, _stream(dev)))
 
 
 def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, out_prob=None, draft=None,

@@ -474,22 +474,6 @@ struct rpd_quant {
 
 namespace {
 
-constexpr int64_t kQuantCyclesPerUs = 2000;         // the limit of a wait is counted in cycles of some 2 GHz
-constexpr int64_t kQuantMaxWaitUs = 60000000;
-
-// A launch without attributes, with its own error (not one that an earlier call has left behind).
-template <typename... KArgs, typename... Args>
-cudaError_t launch_plain(void (*kernel)(KArgs...), int grid, int block, cudaStream_t s, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(block);
-    cfg.stream = s;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
-// The largest of 16, 8, 4 and 2 that divides an address (and whatever is or-ed into it).
-int common_align(uintptr_t bits) { return bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16; }
-
 long long rows_ctas(const rpd_quant *q, int rows, int per) {
     return ((rows - 1ll) / per + 1) * std::min(q->pairs, q->num_sms);
 }
@@ -672,7 +656,7 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
     p.x = x;
     p.out = out;
     p.rows = rows;
-    p.wait_cycles = q->wait_us * kQuantCyclesPerUs;
+    p.wait_cycles = q->wait_us * kWaitCyclesPerUs;
     p.stall = q->stall ? 1 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
     cudaError_t e;
@@ -688,8 +672,8 @@ int rpd_quant_logits(const rpd_quant *q, const void *x, int x_type, int64_t x_st
 
 int rpd_quant_set_wait_limit(rpd_quant *q, int64_t microseconds) {
     if (!q) return op_fail(RPD_ERR_INVALID_ARGUMENT, "null head");
-    if (microseconds < 1000 || microseconds > kQuantMaxWaitUs)
-        return op_fail(RPD_ERR_INVALID_ARGUMENT, "the wait limit must be 1000 .. %lld us", static_cast<long long>(kQuantMaxWaitUs));
+    if (microseconds < 1000 || microseconds > kMaxWaitUs)
+        return op_fail(RPD_ERR_INVALID_ARGUMENT, "the wait limit must be 1000 .. %lld us", static_cast<long long>(kMaxWaitUs));
     q->wait_us = microseconds;
     return RPD_OK;
 }

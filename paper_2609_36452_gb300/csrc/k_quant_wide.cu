@@ -121,27 +121,6 @@ __global__ void __launch_bounds__(256) k_quant_wide_x(const QuantParams p, int n
 
 // ------------------------------------------------------------------------------ PTX
 
-__device__ __forceinline__ void bulk_copy(void *to, const void *from, uint32_t bytes, uint64_t *bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                     smem_u32(to)),
-                 "l"(from), "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
-__device__ __forceinline__ void tensor_copy_2d(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
-            "r"(smem_u32(to)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
-        : "memory");
-}
-__device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t cols) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols) : "memory");
-}
 // D (+)= A (tensor memory) * B^T (shared memory), issued from a converged warp by its elected lane.
 __device__ __forceinline__ void umma_f16_ts_warp(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc,
                                                  uint32_t accumulate) {
@@ -153,15 +132,6 @@ __device__ __forceinline__ void umma_f16_ts_warp(uint32_t d, uint32_t a, uint64_
         " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
         "}\n" ::"r"(d),
         "r"(a), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-__device__ __forceinline__ void umma_commit_warp(uint64_t *bar) {
-    asm volatile(
-        "{\n"
-        " .reg .pred e;\n"
-        " elect.sync _|e, 0xffffffff;\n"
-        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
-        "}\n" ::"r"(smem_u32(bar))
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t at, const uint32_t (&r)[32]) {
@@ -182,47 +152,6 @@ __device__ __forceinline__ uint32_t idesc_f16(int n) {
     return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (128u >> 4 << 24);
 }
 
-// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after abort[1] times 1024
-// cycles or once another role has raised it.  (The limit is read where it is needed: as a number of 64 bits from the
-// parameters it cost the loops of 64 rows registers, 152064 x 3584 in groups of 32 7 us of 170.)
-__device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  // sleeps up to 2 us
-    uint32_t ok;
-    asm volatile(
-        "{\n"
-        " .reg .pred p;\n"
-        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-        " selp.u32 %0, 1, 0, p;\n"
-        "}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(2000)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    const uint32_t a = smem_u32(bar);
-    if (try_wait_long(a, parity)) return true;
-    const long long t0 = clock64();
-    while (!try_wait_long(a, parity)) {
-        if (*abort) return false;
-        if (clock64() - t0 > static_cast<long long>(abort[1]) << 10) {
-            *abort = 1;
-            return false;
-        }
-    }
-    return true;
-}
-// By a converged warp, which stays so.
-__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort));
-}
-// On the way out: whatever the abort flag says.
-__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    const uint32_t a = smem_u32(bar);
-    const long long t0 = clock64();
-    while (!mbar_try_wait(a, parity) && clock64() - t0 < static_cast<long long>(abort[1]) << 10) {
-    }
-}
-
 // ------------------------------------------------------------------------------ the product
 
 // Copies in flight land before the memory goes.  Stages that only one of the two TMA warps has asked for lack an arrival;
@@ -232,19 +161,6 @@ __device__ __noinline__ void drain_copies(uint64_t *full, int stages, const int 
     for (int i = both; i < any; ++i) mbar_arrive(&full[i % stages]);
     for (int i = max(0, any - stages); i < any; ++i) wait_drained(&full[i % stages], (i / stages) & 1, abort);
 }
-
-// A place in a ring of barriers.
-struct Cursor {
-    int at = 0;
-    uint32_t phase = 0;
-    __device__ __forceinline__ void next(int n, int by = 1) {
-        at += by;
-        if (at >= n) {
-            at -= n;
-            phase ^= 1u;
-        }
-    }
-};
 
 constexpr int meta_group_bytes(bool zeros) { return zeros ? 128 : 64; }  // of a pair and group
 

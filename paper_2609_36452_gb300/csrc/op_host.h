@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdarg>
+#include <cstdint>
 #include <cstdio>
 
 #include "rpd_internal.h"
@@ -76,6 +77,9 @@ struct RelaxedCapture {
     RelaxedCapture &operator=(const RelaxedCapture &) = delete;
 };
 
+constexpr int64_t kWaitCyclesPerUs = 2000;  // the limit of a wait in a kernel is counted in cycles of some 2 GHz
+constexpr int64_t kMaxWaitUs = 60000000;
+
 // Bytes of an element of one of the RPD_TYPE_* types, 0 for anything else.
 inline int type_size(int type) {
     return type == RPD_TYPE_F32 ? 4 : type == RPD_TYPE_BF16 || type == RPD_TYPE_F16 ? 2 : 0;
@@ -92,5 +96,18 @@ inline int check_device(int device) {
         return op_fail(RPD_ERR_UNSUPPORTED, "device is sm_%d%d; this library is built for sm_103a", major, minor);
     return RPD_OK;
 }
+
+// A launch without attributes, with its own error (not one that an earlier call has left behind).
+template <typename... KArgs, typename... Args>
+cudaError_t launch_plain(void (*kernel)(KArgs...), int grid, int block, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = s;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// The largest of 16, 8, 4 and 2 that divides an address (and whatever is or-ed into it).
+inline int common_align(uintptr_t bits) { return bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16; }
 
 }  // namespace rpd

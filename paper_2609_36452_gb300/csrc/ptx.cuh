@@ -386,4 +386,92 @@ __device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, float (&v)[32
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// ------------------------------------------------------------------------------ one CTA's copies, tensor memory, waits
+
+// Contiguous bytes (both addresses and the size multiples of 16) and a box of a tensor, signalled on `bar`.
+__device__ __forceinline__ void bulk_copy(void *to, const void *from, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     smem_u32(to)),
+                 "l"(from), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_copy_2d(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
+            "r"(smem_u32(to)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols) : "memory");
+}
+// Arrive on `bar` when every tcgen05.mma that the elected lane has issued is complete; from a converged warp.
+__device__ __forceinline__ void umma_commit_warp(uint64_t *bar) {
+    asm volatile(
+        "{\n"
+        " .reg .pred e;\n"
+        " elect.sync _|e, 0xffffffff;\n"
+        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
+        "}\n" ::"r"(smem_u32(bar))
+        : "memory");
+}
+// Bounded waits for the phase of parity `parity`, by the SM's clock: give up, and raise *abort, after abort[1] times 1024
+// cycles or once another role has raised it.  (The limit is read where it is needed: as a number of 64 bits from the
+// parameters it cost the loops of 64 rows registers, 152064 x 3584 in groups of 32 7 us of 170.)
+__device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {  // sleeps up to 2 us
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        " .reg .pred p;\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        " selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(2000)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool wait_phase(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    const uint32_t a = smem_u32(bar);
+    if (try_wait_long(a, parity)) return true;
+    const long long t0 = clock64();
+    while (!try_wait_long(a, parity)) {
+        if (*abort) return false;
+        if (clock64() - t0 > static_cast<long long>(abort[1]) << 10) {
+            *abort = 1;
+            return false;
+        }
+    }
+    return true;
+}
+// By a converged warp, which stays so.
+__device__ __forceinline__ bool wait_phase_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    return __all_sync(0xffffffffu, wait_phase(bar, parity, abort));
+}
+// On the way out: whatever the abort flag says.
+__device__ __forceinline__ void wait_drained(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    const uint32_t a = smem_u32(bar);
+    const long long t0 = clock64();
+    while (!mbar_try_wait(a, parity) && clock64() - t0 < static_cast<long long>(abort[1]) << 10) {
+    }
+}
+
+// A place in a ring of barriers.
+struct Cursor {
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int n, int by = 1) {
+        at += by;
+        if (at >= n) {
+            at -= n;
+            phase ^= 1u;
+        }
+    }
+};
+
 }  // namespace rpd
