@@ -536,6 +536,50 @@ int64_t rpd_verify_workspace(int B, int D);
  * may not overlap the inputs. */
 int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_bytes, void *stream);
 
+/* A token from every row of logits, by one given random number a row and under limits.  (The paper has no
+ * counterpart.  rpd_verify without drafts draws too, by V random numbers a row and under a mask alone;
+ * out_allowed is a mask that it takes: a target model's rows under these limits.)
+ *
+ * The tokens of row r that are allowed and whose logits are finite are ordered by their logits, of equal ones the
+ * lower index first; w = e^((z - largest z) / T), T = temperature[r].
+ *   top_k: the first top_k[r] tokens are kept (< 1: all of them);
+ *   top_p: of these, a token while the weights before it are less than top_p[r] times the sum of these (>= 1: all of
+ *          them; the first token always);
+ *   min_p: of these, a token with w >= min_p[r] (<= 0: all of them).
+ * The token is the first, in that order, at which the sum of the kept weights up to and with it exceeds
+ * uniform[r] times the sum of all that are kept.  T = 0 keeps the first token alone, whatever the limits;
+ * other T count as at least 1.45e-30 and at most 1.44e37.
+ * Weights are right to some 2^-31 each, without bias, those of 2^-10 of their sum and more to 2^-50; sums of them
+ * are exact.  Results do not depend on the launch's shape.
+ *
+ * 1 <= V <= 2^24, 0 <= rows <= 2^26 (larger: RPD_ERR_UNSUPPORTED; 0 is a no-op).  A row that fits eight SMs' shared
+ * memory (400 KB a CTA pair; 800 000 bf16 logits) is read once. */
+typedef struct rpd_sample_args {
+    const void *logits;         /* [rows][V] of `type`, device, rows row_stride elements apart */
+    const uint32_t *allowed;    /* [rows][ceil(V / 32)] bits, 1 = allowed, as rpd_verify's; or NULL.  Logits of other
+                                   tokens may hold anything */
+    const float *temperature;   /* [rows] >= 0, or NULL: 1 each */
+    const int32_t *top_k;       /* [rows] or NULL: no limit */
+    const float *top_p;         /* [rows] or NULL */
+    const float *min_p;         /* [rows] <= 1, or NULL */
+    const float *uniform;       /* [rows] in [0, 1); NULL only where temperature is given and 0 throughout */
+    int32_t *out_token;         /* [rows] */
+    int32_t *out_status;        /* [rows] RPD_OK; or RPD_ERR_INVALID_ARGUMENT, with token -1, nothing kept and
+                                   probability 0, where a row has no allowed finite logit or a NaN or +infinity among
+                                   the allowed ones, T is negative or NaN, uniform outside [0, 1) while T > 0, top_p
+                                   NaN, or min_p NaN or above 1 */
+    int32_t *out_kept;          /* [rows] number of kept tokens, or NULL */
+    float *out_prob;            /* [rows] the token's weight over the sum of the kept ones, or NULL */
+    uint32_t *out_allowed;      /* [rows][ceil(V / 32)] the kept tokens as such bits, 0 beyond V; or NULL */
+    int64_t row_stride;         /* >= 0 (equal rows may be shared); the tokens of a row are contiguous */
+    int32_t type;               /* RPD_TYPE_* of the logits */
+    int32_t rows, V;
+} rpd_sample_args;
+
+/* Runs asynchronously on `stream` (a cudaStream_t of the device that holds the logits; NULL = legacy default).
+ * Every buffer is device memory of that device; outputs may not overlap the inputs.  No workspace. */
+int rpd_sample(const rpd_sample_args *args, void *stream);
+
 /* Message of the last failing call on this host thread ("" if none). */
 const char *rpd_last_error(void);
 

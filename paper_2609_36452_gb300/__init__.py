@@ -24,7 +24,7 @@ __all__ = [
     "rpd_quant_set_wait_limit", "rpd_quant_inject_stall",
     "rpd_fp8_create", "rpd_fp8_set_weights", "rpd_fp8_workspace", "rpd_fp8_logits", "rpd_fp8_set_wait_limit",
     "rpd_fp8_inject_stall", "rpd_fp8_destroy", "rpd_fp8_quantize", "Fp8Head", "quantize_fp8",
-    "rpd_verify_workspace", "rpd_verify", "verify", "RpdVerifyArgs",
+    "rpd_verify_workspace", "rpd_verify", "verify", "RpdVerifyArgs", "rpd_sample", "sample", "RpdSampleArgs",
     "rpd_destroy", "rpd_last_error", "rpd_version", "Rpd", "RULE_PROFILES", "KERNEL_NAMES",
 ]
 
@@ -76,6 +76,13 @@ class RpdVerifyArgs(ctypes.Structure):
         "out_accepted", "out_token", "out_status", "out_prob")] + [(n, ctypes.c_int64) for n in (
             "target_seq_stride", "target_row_stride", "draft_seq_stride", "draft_row_stride", "noise_stride")] + [
         (n, ctypes.c_int32) for n in ("type", "B", "D", "V")]
+
+
+class RpdSampleArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "logits", "allowed", "temperature", "top_k", "top_p", "min_p", "uniform", "out_token", "out_status", "out_kept",
+        "out_prob", "out_allowed")] + [("row_stride", ctypes.c_int64)] + [
+            (n, ctypes.c_int32) for n in ("type", "rows", "V")]
 
 
 STATS_FIELDS = [f[0] for f in RpdStats._fields_]
@@ -161,6 +168,7 @@ def _load():
         "rpd_fp8_quantize": (i32, [vp, i32, ctypes.c_int64, i32, i32, i32, vp, ctypes.c_int64, vp, vp]),
         "rpd_verify_workspace": (ctypes.c_int64, [i32, i32]),
         "rpd_verify": (i32, [ctypes.POINTER(RpdVerifyArgs), vp, ctypes.c_int64, vp]),
+        "rpd_sample": (i32, [ctypes.POINTER(RpdSampleArgs), vp]),
         "rpd_destroy": (None, [vp]),
         "rpd_last_error": (ctypes.c_char_p, []),
         "rpd_version": (ctypes.c_char_p, []),
@@ -216,6 +224,7 @@ rpd_fp8_destroy = lib.rpd_fp8_destroy
 rpd_fp8_quantize = lib.rpd_fp8_quantize
 rpd_verify_workspace = lib.rpd_verify_workspace
 rpd_verify = lib.rpd_verify
+rpd_sample = lib.rpd_sample
 rpd_destroy = lib.rpd_destroy
 rpd_last_error = lib.rpd_last_error
 rpd_version = lib.rpd_version
@@ -742,3 +751,34 @@ def verify(target, tokens, uniform, noise, out_accepted, out_token, out_status, 
         if size > 0:
             pw, size, workspace = _workspace(size, dev, stream)
     _check(rpd_verify(a, pw, size, stream))
+
+
+def sample(logits, uniform, out_token, out_status, temperature=None, top_k=None, top_p=None, min_p=None, allowed=None,
+           out_kept=None, out_prob=None, out_allowed=None):
+    """A token from every row of logits, by one given random number a row and under limits (rpd_sample).
+
+    logits [rows][V] bf16, fp16 or float32, rows may lie apart; uniform [rows] float32 in [0, 1) (None where every
+    temperature is 0); temperature, top_p, min_p [rows] float32 and top_k [rows] int32 (None: 1, and no limits); allowed
+    [rows][ceil(V / 32)] int32 bit masks.  Outputs: out_token, out_status [rows] int32; out_kept [rows] int32, the number
+    of tokens within the limits, out_prob [rows] float32, the token's share of their weights, and out_allowed, the
+    tokens themselves as a bit mask such as ``verify`` takes (each may be None).  Runs on the current stream of the
+    logits' device."""
+    shape = getattr(logits, "shape", ())
+    if len(shape) != 2 or shape[1] < 1:
+        raise RpdError(RPD_ERR_INVALID_ARGUMENT, "logits: a tensor of [rows][V] is required")
+    rows, V = _size(shape[0], "rows"), _size(shape[1], "V")
+    T = _torch()
+    pl, kind, strides = _rows_arg(logits, "logits", (T.bfloat16, T.float16, T.float32), (rows, V))
+    dev, words = logits.get_device(), rows * ((V + 31) // 32)
+
+    def dense(t, name, dtype, numel=rows):
+        return None if t is None else _dense_arg(t, name, dtype, numel, dev)
+
+    a = RpdSampleArgs(
+        pl, dense(allowed, "allowed", "int32", words), dense(temperature, "temperature", "float32"),
+        dense(top_k, "top_k", "int32"), dense(top_p, "top_p", "float32"), dense(min_p, "min_p", "float32"),
+        dense(uniform, "uniform", "float32"), _dense_arg(out_token, "out_token", "int32", rows, dev),
+        _dense_arg(out_status, "out_status", "int32", rows, dev), dense(out_kept, "out_kept", "int32"),
+        dense(out_prob, "out_prob", "float32"), dense(out_allowed, "out_allowed", "int32", words),
+        strides[0], kind, rows, V)
+    _check(rpd_sample(a, _stream(dev)))
