@@ -28,6 +28,12 @@ constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleMaxCluster = 8;
 constexpr int kSampleTable = 512;
+constexpr int kSampleBins = 4096;          // of the first histogram
+constexpr int kBinParts = 256;             // parts of a bin, of which the mean is kept
+constexpr int kBinOctaves = 64;            // what the bins span at most: a bin is a 64th of an octave of weights, or less
+constexpr float kBinError = 0x1p-14f;      // of a sum of bins' weights, taken at their tokens' mean places: at most 2^-16 for
+                                           // the spread around the mean and 2^-15.5 for the parts
+constexpr int kSampleList = 2048;          // tokens that are sorted
 constexpr float kLowest = -3.402823466e38f;
 
 struct SampleParams {
@@ -35,6 +41,8 @@ struct SampleParams {
     int words;       // 32-bit words of a row of masks
     int slice;       // tokens of a CTA, a multiple of 32
     int sum_bits;    // units of a row's sum of weights: 2^-sum_bits of the largest
+    int thread_bits; // of a thread's
+    int list_at;     // in shared memory, where the histogram and then the lists are
 };
 
 // 2^(i / 512) in units of 2^-31.
@@ -195,20 +203,24 @@ struct SampleWeights {
         rest = __fadd_rn(__fsub_rn(y, __fsub_rn(t, kShift)), fmaf(d, c_lo, fmaf(d, c_hi, -y)));
         return __float_as_int(t);
     }
-    __device__ void set(float top_logit, double T) {
-        top = top_logit;
+    __device__ void set_temperature(double T) {
         inverse_T = 1.0 / T;
         const double c64 = 1.4426950408889634 / T;
         c_hi = c = static_cast<float>(c64);
         c_lo = static_cast<float>(c64 - c_hi);
+    }
+    __device__ void set_top(float top_logit) {
+        top = top_logit;
         A = fabsf(top_logit) * c < 0x1p12f ? 0.f : top_logit;
         k_top = split(top_logit - A, rest_top);
         big = -kNoLogit;
     }
     // Logits at and below `floor` weigh nothing: under 2^-bits.
-    __device__ void set_floor(int bits) { floor = fmaxf(kLowest, __double2float_rd(top - bits / static_cast<double>(c))); }
+    __device__ void set_floor(int bits) {
+        floor = fmaxf(kLowest, __fsub_rd(static_cast<float>(top), __fdiv_ru(static_cast<float>(bits), c)));
+    }
     // Of a sum of about `sum` times the largest weight, those that hold 2^-10 and more.
-    __device__ void set_big(float sum) { big = static_cast<float>(top - (10.0 - log2f(sum)) / c); }
+    __device__ void set_big(float sum) { big = static_cast<float>(top) - (10.f - log2f(sum)) / c; }
     __device__ __forceinline__ uint64_t of(float z, int bits, const uint32_t *table) const {
         float r;
         const int k = split(fmaxf(z, floor) - A, r) - k_top;
@@ -237,11 +249,39 @@ struct SampleCut {
     __device__ __forceinline__ bool keeps(uint32_t k, int v) const { return k > key || (k == key && v <= last); }
 };
 
+// A bin at which a running count or sum passes something, with both before and behind it.
+struct SampleFound {
+    int bin, count0, count1;
+    float sum0, sum1;
+};
+// What the first histogram leaves to be found out.
+struct SamplePlan {
+    int slow;               // nothing but the four passes will do
+    int gather;             // top-k: every token before `draw1` is listed, and all is decided there
+    int by_list;            // top-p: the cut is in the bins from cut0 to cut1
+    int by_edge;            // min-p: tokens from `edge` on are kept, and there is no other cut
+    float draw0, draw1, cut0, cut1;  // places, in parts of bins
+    float scale;
+    int cut_count;          // tokens before cut0
+    float sum;              // about that of all weights
+};
+struct SampleResult {
+    int slow;
+    SampleCut cut;
+    int token, kept;
+    double prob;
+};
+
 struct SampleShared {
     uint32_t table[kSampleTable];
     SampleWeights w;
-    uint64_t mass[256];
-    uint32_t count[256];
+    // what lies where the first histogram was, and the lists will be
+    struct Scratch {
+        uint64_t mass[256];
+        uint32_t count[256];
+        float scan[kSampleThreads + 1];
+        int scan_count[kSampleThreads + 1];
+    } *x;
     float range[2][kSampleWarps];
     float top, low;            // the slice's, then the row's
     int bad;
@@ -254,6 +294,17 @@ struct SampleShared {
     uint64_t bin_mass;
     int above_count, bin_count, bin;
     int tie;                   // the token of a tie that the border falls on
+    double min_log;            // T log(min_p): min-p keeps logits from so far below the largest on
+    // the quick way
+    int binned, tail;          // a slice's tokens in the bins, and below them
+    int listed[2];             // entries of the lists
+    SampleFound found[4];
+    SamplePlan plan;
+    SampleResult result;
+    double sums64[3][kSampleWarps];
+    double part[3];            // a slice's weights: of all that count, above the cut's bins, above the draw's
+    int part_count;
+    int first;
 };
 
 __device__ __forceinline__ double ld_cluster_f64(uint32_t a) {
@@ -303,8 +354,8 @@ __device__ __noinline__ SampleCut find_border(const S &s, SampleShared &sm, int 
     uint64_t bin_mass = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = threadIdx.x; i < 256; i += kSampleThreads) {
-            sm.mass[i] = 0;
-            sm.count[i] = 0;
+            sm.x->mass[i] = 0;
+            sm.x->count[i] = 0;
         }
         __syncthreads();
         int run = -1, run_count = 0;  // neighbours that fall into one bin are added at once
@@ -315,8 +366,8 @@ __device__ __noinline__ SampleCut find_border(const S &s, SampleShared &sm, int 
             const int b = static_cast<int>(key >> shift) & 255;
             if (b != run) {
                 if (run >= 0) {
-                    atomicAdd(&sm.count[run], run_count);
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sm.mass[run]), static_cast<unsigned long long>(run_mass));
+                    atomicAdd(&sm.x->count[run], run_count);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sm.x->mass[run]), static_cast<unsigned long long>(run_mass));
                 }
                 run = b;
                 run_count = 0;
@@ -326,8 +377,8 @@ __device__ __noinline__ SampleCut find_border(const S &s, SampleShared &sm, int 
             run_mass += sm.w.exact_of(z, bits, sm.table);
         });
         if (run >= 0) {
-            atomicAdd(&sm.count[run], run_count);
-            atomicAdd(reinterpret_cast<unsigned long long *>(&sm.mass[run]), static_cast<unsigned long long>(run_mass));
+            atomicAdd(&sm.x->count[run], run_count);
+            atomicAdd(reinterpret_cast<unsigned long long *>(&sm.x->mass[run]), static_cast<unsigned long long>(run_mass));
         }
         row_sync(ranks);
         if (rank == 0) {
@@ -335,30 +386,30 @@ __device__ __noinline__ SampleCut find_border(const S &s, SampleShared &sm, int 
                 uint64_t m = 0;
                 uint32_t c = 0;
                 for (int r = 0; r < ranks; ++r) {
-                    m += ld_cluster_u64(peer(&sm.mass[threadIdx.x], r));
-                    c += ld_cluster_u32(peer(&sm.count[threadIdx.x], r));
+                    m += ld_cluster_u64(peer(&sm.x->mass[threadIdx.x], r));
+                    c += ld_cluster_u32(peer(&sm.x->count[threadIdx.x], r));
                 }
-                sm.mass[threadIdx.x] = m;
-                sm.count[threadIdx.x] = c;
+                sm.x->mass[threadIdx.x] = m;
+                sm.x->count[threadIdx.x] = c;
             }
             __syncthreads();
             if (threadIdx.x == 0) {
                 uint64_t m = above;
                 int c = above_count, found = -1;
                 for (int b = 255; b >= 0; --b) {
-                    const int bc = static_cast<int>(sm.count[b]);
+                    const int bc = static_cast<int>(sm.x->count[b]);
                     if (bc == 0) continue;
                     found = b;
                     sm.above = m;
                     sm.above_count = c;
-                    m += sm.mass[b];
+                    m += sm.x->mass[b];
                     c += bc;
                     const double at = static_cast<double>(m);
                     if (t.by_count ? c >= t.count : t.strictly ? at > t.mass : at >= t.mass) break;
                 }
                 sm.bin = found;  // (the last one that is not empty where roundings let none reach it)
-                sm.bin_count = static_cast<int>(sm.count[found]);
-                sm.bin_mass = sm.mass[found];
+                sm.bin_count = static_cast<int>(sm.x->count[found]);
+                sm.bin_mass = sm.x->mass[found];
             }
         }
         row_sync(ranks);
@@ -435,7 +486,7 @@ __device__ __noinline__ double kept_mass(const S &s, SampleShared &sm, int ranks
         c += __shfl_xor_sync(0xffffffffu, c, o);
     }
     if ((threadIdx.x & 31) == 0) {
-        sm.mass[threadIdx.x >> 5] = m;
+        sm.x->mass[threadIdx.x >> 5] = m;
         sm.counts[threadIdx.x >> 5] = c;
     }
     row_sync(ranks);
@@ -443,7 +494,7 @@ __device__ __noinline__ double kept_mass(const S &s, SampleShared &sm, int ranks
     c = 0;
     for (int r = 0; r < ranks; ++r)
         for (int w = 0; w < kSampleWarps; ++w) {
-            m += ld_cluster_u64(peer(&sm.mass[w], r));
+            m += ld_cluster_u64(peer(&sm.x->mass[w], r));
             c += static_cast<int>(ld_cluster_u32(peer(&sm.counts[w], r)));
         }
     row_sync(ranks);
@@ -451,25 +502,529 @@ __device__ __noinline__ double kept_mass(const S &s, SampleShared &sm, int ranks
     return static_cast<double>(m);
 }
 
+// Every border in four passes.  Leaves the result in every CTA.
+template <typename S>
+__device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ranks, int rank, int bits, float top, float edge, int top_k,
+                                           float top_p, float u) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) sm.w.set_floor(bits);
+    __syncthreads();
+    float sum = 0.f;
+    s.each([&](float z, int) { sum += ex2((z - top) * sm.w.c); });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) sm.sums[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.f;
+        for (int w = 0; w < kSampleWarps; ++w) sum += sm.sums[w];
+        sm.sum = sum;
+    }
+    row_sync(ranks);
+    if (threadIdx.x == 0) {
+        sum = 0.f;
+        for (int q = 0; q < ranks; ++q) sum += __uint_as_float(ld_cluster_u32(peer(&sm.sum, q)));
+        sm.w.set_big(fmaxf(sum, 1.f));
+    }
+    row_sync(ranks);
+    SampleCut cut{0u, 0x7FFFFFFF};
+    int n, place;
+    double mass = kept_mass(s, sm, ranks, bits, cut, n), weight, upto;
+    if (top_k > 0 && top_k < n) cut = find_border(s, sm, ranks, rank, bits, cut, {true, false, top_k, 0.0}, n, mass, weight);
+    if (top_p < 1.f) cut = find_border(s, sm, ranks, rank, bits, cut, {false, false, 0, top_p * mass}, n, mass, weight);
+    if (edge != kNoLogit && order_key(edge) > cut.key) {
+        cut = {order_key(edge), 0x7FFFFFFF};
+        mass = kept_mass(s, sm, ranks, bits, cut, n);
+    }
+    const SampleCut token = find_border(s, sm, ranks, rank, bits, cut, {false, true, 0, u * mass}, place, upto, weight);
+    if (threadIdx.x == 0) sm.result = {0, cut, token.last, n, weight / mass};
+    __syncthreads();
+}
+
+// ------------------------------------------------------------------------------ the quick way
+
+// A place in the order, in parts of bins: 0 at the largest logit.
+__device__ __forceinline__ float sample_place(float z, float top, float scale) { return (top - z) * scale; }
+
+// Entries in ascending order are tokens in theirs.
+__device__ __forceinline__ uint64_t sample_entry(float z, int v) { return static_cast<uint64_t>(~order_key(z)) << 32 | static_cast<uint32_t>(v); }
+
+// n entries, padded to a power of two (returned), by the CTA.
+__device__ __forceinline__ int sort_entries(uint64_t *list, int n) {
+    int size = 32;
+    while (size < n) size <<= 1;
+    for (int i = n + threadIdx.x; i < size; i += kSampleThreads) list[i] = ~0ull;
+    __syncthreads();
+    for (int k = 2; k <= size; k <<= 1)
+        for (int j = k >> 1; j; j >>= 1) {
+            for (int i = threadIdx.x; i < size / 2; i += kSampleThreads) {
+                const int a = 2 * i - (i & (j - 1)), b = a + j;
+                const uint64_t x = list[a], y = list[b];
+                if ((x > y) == ((a & k) == 0)) {
+                    list[a] = y;
+                    list[b] = x;
+                }
+            }
+            __syncthreads();
+        }
+    return size;
+}
+
+constexpr int kSamplePer = kSampleList / kSampleThreads;  // entries of a thread
+
+// Sums of the threads' numbers before each, and of all, in the threads' order.
+__device__ __forceinline__ double scan_block(double mine, double *warps, double &all) {
+    double upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double up = __shfl_up_sync(0xffffffffu, upto, o);
+        if ((threadIdx.x & 31) >= o) upto += up;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 31) warps[threadIdx.x >> 5] = upto;
+    __syncthreads();
+    double before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kSampleWarps; ++w) {
+        if (w == static_cast<int>(threadIdx.x >> 5)) before = all;
+        all += warps[w];
+    }
+    return before + upto - mine;
+}
+
+// A sorted list in the threads' registers: neighbouring entries, their weights, and the sum of those before.
+struct SampleSorted {
+    uint64_t entry[kSamplePer];
+    double w[kSamplePer], before, all;
+    int first, per;
+    __device__ void read(const uint64_t *list, int n, int size, SampleShared &sm) {
+        per = max(1, size / kSampleThreads);
+        first = threadIdx.x * per;
+        double mine = 0;
+#pragma unroll
+        for (int i = 0; i < kSamplePer; ++i) {
+            const bool in = i < per && first + i < n;
+            entry[i] = in ? list[first + i] : ~0ull;
+            w[i] = in ? static_cast<double>(sm.w.exact_of(key_value(~static_cast<uint32_t>(entry[i] >> 32)), 54, sm.table)) * 0x1p-54 : 0.0;
+            mine += w[i];
+        }
+        before = scan_block(mine, sm.sum64, all);
+    }
+    // Smallest number of an entry for which f(number, running sum before it, its weight) holds; kSampleList if none.
+    template <typename F>
+    __device__ int find(int n, int &slot, F f) const {
+        __syncthreads();
+        if (threadIdx.x == 0) slot = kSampleList;
+        __syncthreads();
+        double at = before;
+        int found = kSampleList;
+#pragma unroll
+        for (int i = 0; i < kSamplePer; ++i) {
+            if (i < per && first + i < n && found == kSampleList && f(first + i, at, w[i], entry[i])) found = first + i;
+            at += w[i];
+        }
+        if (found < kSampleList) atomicMin(&slot, found);
+        __syncthreads();
+        return slot;
+    }
+    // Weights of the first m entries.
+    __device__ double sum_of(int m, SampleShared &sm) const {
+        double mine = 0, total;
+#pragma unroll
+        for (int i = 0; i < kSamplePer; ++i)
+            if (i < per && first + i < m) mine += w[i];
+        scan_block(mine, sm.sum64, total);
+        return total;
+    }
+};
+
+// The first histogram's bins in the threads of the row's first CTA, eight neighbours each, with the running count and
+// sum before them.
+struct SampleBins {
+    static constexpr int kPer = kSampleBins / kSampleThreads;
+    int count[kPer];
+    float sum[kPer];
+    // The first bin at whose end f(count, sum) holds; bin = kSampleBins if at none.
+    template <typename F>
+    __device__ void find(SampleShared &sm, SampleFound &to, F f) const {
+        if (threadIdx.x == 0 && !f(sm.x->scan_count[kSampleThreads], sm.x->scan[kSampleThreads]))
+            to = {kSampleBins, sm.x->scan_count[kSampleThreads], sm.x->scan_count[kSampleThreads], sm.x->scan[kSampleThreads], sm.x->scan[kSampleThreads]};
+        const bool before = threadIdx.x && f(sm.x->scan_count[threadIdx.x], sm.x->scan[threadIdx.x]);
+        if (before || !f(sm.x->scan_count[threadIdx.x + 1], sm.x->scan[threadIdx.x + 1])) return;
+        int c = sm.x->scan_count[threadIdx.x];
+        float e = sm.x->scan[threadIdx.x];
+        for (int i = 0; i < kPer; ++i) {
+            if (i == kPer - 1 || f(c + count[i], e + sum[i])) {
+                to = {static_cast<int>(threadIdx.x) * kPer + i, c, c + count[i], e, e + sum[i]};
+                return;
+            }
+            c += count[i];
+            e += sum[i];
+        }
+    }
+};
+
+// Which bins the borders are in, by the running counts and sums of bins: the first CTA of the row.  Sums are kBinError off
+// at most, so that a border may be in either of two bins, or more.
+__device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const uint8_t *own, float top, float edge, float scale, int top_k,
+                                             float top_p, float u) {
+    constexpr int kPer = SampleBins::kPer;
+    SampleBins bins;
+    const int per_rank = kSampleBins / ranks, first = threadIdx.x * kPer;
+    int c = 0;
+    float e = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const uint64_t v = ld_cluster_u64(mapa_shared(smem_u32(own + (first + i) % per_rank * 8), (first + i) / per_rank));
+        bins.count[i] = static_cast<int>(v);
+        bins.sum[i] = __uint_as_float(static_cast<uint32_t>(v >> 32));
+        c += bins.count[i];
+        e += bins.sum[i];
+    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int c_upto = c;
+    float e_upto = e;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int cu = __shfl_up_sync(0xffffffffu, c_upto, o);
+        const float eu = __shfl_up_sync(0xffffffffu, e_upto, o);
+        if (lane >= o) {
+            c_upto += cu;
+            e_upto += eu;
+        }
+    }
+    if (lane == 31) {
+        sm.counts[warp] = c_upto;
+        sm.sums[warp] = e_upto;
+    }
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) {
+        c_upto += sm.counts[w];
+        e_upto += sm.sums[w];
+    }
+    if (threadIdx.x == 0) {
+        sm.x->scan_count[0] = 0;
+        sm.x->scan[0] = 0.f;
+    }
+    sm.x->scan_count[threadIdx.x + 1] = c_upto;
+    sm.x->scan[threadIdx.x + 1] = e_upto;
+    __syncthreads();
+    const int binned = sm.x->scan_count[kSampleThreads];
+    const float sum = sm.x->scan[kSampleThreads], error = kBinError * sum;
+    int expected = 0, tail = 0;
+    for (int q = 0; q < ranks; ++q) {
+        expected += static_cast<int>(ld_cluster_u32(peer(&sm.binned, q)));
+        tail += static_cast<int>(ld_cluster_u32(peer(&sm.tail, q)));
+    }
+    SamplePlan plan{};
+    plan.scale = scale;
+    plan.sum = fmaxf(sum, 1.f);
+    plan.cut0 = plan.cut1 = -1.f;
+    plan.slow = binned != expected;  // a bin had more tokens than it can count
+    constexpr float kEnd = static_cast<float>(kSampleBins) * kBinParts;
+    const auto place_of = [](int bin) { return static_cast<float>(bin) * kBinParts; };
+    if (top_k > 0 && top_k < binned + tail) {
+        bins.find(sm, sm.found[0], [&](int n, float) { return n >= top_k; });
+        __syncthreads();
+        plan.gather = 1;
+        plan.draw1 = place_of(sm.found[0].bin + 1);
+        plan.slow |= sm.found[0].bin == kSampleBins || sm.found[0].count1 > kSampleList;
+    } else {
+        float least = sum, most = sum;  // of the kept weights
+        int last = kSampleBins - 1;     // bin of a kept token
+        const float edge_place = edge == kNoLogit ? kEnd : fminf(sample_place(edge, top, scale), kEnd);
+        plan.by_edge = edge != kNoLogit;
+        if (top_p < 1.f) {
+            bins.find(sm, sm.found[0], [&](int, float m) { return m >= top_p * sum - error; });
+            bins.find(sm, sm.found[1], [&](int, float m) { return m >= top_p * sum + error; });
+            __syncthreads();
+            const int b0 = sm.found[0].bin, b1 = min(sm.found[1].bin, kSampleBins - 1);
+            if (edge_place >= place_of(b0)) {
+                plan.by_list = 1;
+                plan.by_edge = 0;
+                plan.cut0 = place_of(b0);
+                plan.cut1 = place_of(b1 + 1);
+                plan.cut_count = sm.found[0].count0;
+                least = sm.found[0].sum0;
+                most = sm.found[1].sum1;
+                last = b1;
+                plan.slow |= sm.found[1].count1 - sm.found[0].count0 > kSampleList / 2 || b0 > b1;
+            }
+        }
+        if (plan.by_edge && edge_place < kEnd) {
+            last = static_cast<int>(edge_place) / kBinParts;
+            if (static_cast<int>(threadIdx.x) == last / kPer) {
+                int n = sm.x->scan_count[threadIdx.x];
+                float m = sm.x->scan[threadIdx.x];
+                for (int i = 0; i < last % kPer; ++i) {
+                    n += bins.count[i];
+                    m += bins.sum[i];
+                }
+                sm.found[0] = {last, n, n + bins.count[last % kPer], m, m + bins.sum[last % kPer]};
+            }
+            __syncthreads();
+            least = sm.found[0].sum0;
+            most = sm.found[0].sum1;
+        }
+        least = u * least - error;
+        most = u * most + error;
+        bins.find(sm, sm.found[2], [&](int, float m) { return m > least; });
+        bins.find(sm, sm.found[3], [&](int, float m) { return m > most; });
+        __syncthreads();
+        const bool past = sm.found[3].bin > last;
+        const int b0 = min(sm.found[2].bin, last), b1 = past ? last : sm.found[3].bin;
+        plan.draw0 = place_of(b0);
+        plan.draw1 = place_of(b1 + 1);
+        plan.slow |= sm.found[2].bin > last || (past ? sm.x->scan_count[min(kSampleThreads, b1 / kPer + 1)] : sm.found[3].count1) - sm.found[2].count0 > kSampleList / 2;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) sm.plan = plan;
+}
+
+// A first histogram of the row over 4096 bins, equally wide in the logit, says in which one or two of them each border is;
+// a second pass adds the weights before these up, exactly, and lists the tokens in them, which the first CTA sorts.
+// With top-k all tokens that may be kept are listed.  False: the row is not like that (so many equal logits that a
+// bin's count or a list runs over, or a k of thousands).  Leaves the result in every CTA.
+template <typename S>
+__device__ __forceinline__ bool sample_quickly(const S &s, SampleShared &sm, const SampleParams &p, uint8_t *buffer, int ranks, int rank,
+                                               float top, float low, float edge, int top_k, float top_p, float u) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t *hist = reinterpret_cast<uint32_t *>(buffer + p.list_at);
+    uint64_t *lists = reinterpret_cast<uint64_t *>(buffer + p.list_at);
+    uint8_t *own = buffer + p.list_at + kSampleList * 8;  // this CTA's bins of the row: counts and sums; then the sorted list
+    static_assert(kSampleBins * 4 <= kSampleList * 8 && sizeof(SampleShared::Scratch) <= kSampleList * 8, "lists take their place");
+    const auto list_token = [&](int which, int room, float z, int v) {
+        const int at = atomicAdd(&sm.listed[which], 1);
+        if (at < room) lists[which * (kSampleList / 2) + at] = sample_entry(z, v);
+    };
+    const float c = sm.w.c;
+    const float span = fminf(fminf(kBinOctaves / c, top - low), 3e38f);
+    const float scale = span > 0.f ? fminf((kSampleBins * kBinParts - kBinParts / 2) / span, 1e38f) : 0.f;
+    if (threadIdx.x == 0) {
+        sm.binned = sm.tail = 0;
+        sm.listed[0] = sm.listed[1] = 0;
+    }
+    for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    int binned = 0, tail = 0;
+    s.each([&](float z, int) {
+        if (z >= kLowest) {
+            const int at = static_cast<int>(sample_place(z, top, scale));
+            if (at < kSampleBins * kBinParts) {
+                atomicAdd(&hist[at / kBinParts], (1u << 20) | (at % kBinParts));  // 4095 tokens fit
+                ++binned;
+            } else {
+                ++tail;
+            }
+        }
+    });
+    binned = __reduce_add_sync(0xffffffffu, binned);
+    tail = __reduce_add_sync(0xffffffffu, tail);
+    if (lane == 0) {
+        atomicAdd(&sm.binned, binned);
+        atomicAdd(&sm.tail, tail);
+    }
+    row_sync(ranks);
+    // the slices' histograms become the row's, a part of the bins a CTA
+    const int per_rank = kSampleBins / ranks;
+    const float octaves = scale > 0.f ? c / scale : 0.f;  // of a part of a bin
+    for (int i = threadIdx.x; i < per_rank; i += kSampleThreads) {
+        const int b = rank * per_rank + i;
+        uint32_t n = 0, parts = 0;
+        for (int q = 0; q < ranks; ++q) {
+            const uint32_t v = ld_cluster_u32(peer(&hist[b], q));
+            n += v >> 20;
+            parts += v & 0xFFFFFu;
+        }
+        const float mean = n ? static_cast<float>(parts) / static_cast<float>(n) + 0.5f : 0.f;
+        const float sum = static_cast<float>(n) * ex2(-(static_cast<float>(b * kBinParts) + mean) * octaves);
+        reinterpret_cast<uint2 *>(own)[i] = make_uint2(n, __float_as_uint(sum));
+    }
+    row_sync(ranks);
+    if (rank == 0) plan_borders(sm, ranks, own, top, edge, scale, top_k, top_p, u);
+    row_sync(ranks);
+    if (rank != 0) {
+        if (threadIdx.x < sizeof(SamplePlan) / 4)
+            reinterpret_cast<uint32_t *>(&sm.plan)[threadIdx.x] = ld_cluster_u32(peer(reinterpret_cast<uint32_t *>(&sm.plan) + threadIdx.x, 0));
+        __syncthreads();
+    }
+    if (sm.plan.slow) {
+        row_sync(ranks);
+        return false;
+    }
+    const int bits = p.thread_bits;
+    if (threadIdx.x == 0) {
+        sm.w.set_floor(bits);
+        sm.w.set_big(sm.plan.sum);
+    }
+    __syncthreads();
+    const SamplePlan plan = sm.plan;
+    if (plan.gather) {
+        s.each([&](float z, int v) {
+            if (z >= kLowest && sample_place(z, top, scale) < plan.draw1) list_token(0, kSampleList, z, v);
+        });
+    } else {
+        const SampleWeights w = sm.w;
+        uint64_t all = 0, before_cut = 0, before_draw = 0;
+        int count = 0;
+        const float from = plan.by_edge ? edge : kLowest;
+        s.each([&](float z, int v) {
+            if (z >= from) {
+                ++count;
+                const uint64_t m = w.exact_of(z, bits, sm.table);
+                const float at = sample_place(z, top, scale);
+                all += m;
+                if (at < plan.cut0) before_cut += m;
+                if (at < plan.draw0) before_draw += m;
+                if (at >= plan.draw0 && at < plan.draw1) list_token(0, kSampleList / 2, z, v);
+                if (at >= plan.cut0 && at < plan.cut1) list_token(1, kSampleList / 2, z, v);
+            }
+        });
+        const double unit = 1.0 / static_cast<double>(1ull << bits);
+        double sums[3] = {static_cast<double>(all) * unit, static_cast<double>(before_cut) * unit, static_cast<double>(before_draw) * unit};
+        count = __reduce_add_sync(0xffffffffu, count);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
+            if (lane == 0) sm.sums64[i][warp] = sums[i];
+        }
+        if (lane == 0) sm.counts[warp] = count;
+        __syncthreads();
+        if (threadIdx.x < 4) {
+            double m = 0;
+            int n = 0;
+            for (int i = 0; i < kSampleWarps; ++i) {
+                n += sm.counts[i];
+                if (threadIdx.x < 3) m += sm.sums64[threadIdx.x][i];
+            }
+            if (threadIdx.x < 3) sm.part[threadIdx.x] = m;
+            if (threadIdx.x == 3) sm.part_count = n;
+        }
+    }
+    row_sync(ranks);
+    if (rank == 0) {
+        uint64_t *sorted = reinterpret_cast<uint64_t *>(own);
+        double sums[3] = {0, 0, 0};
+        int count = 0;
+        if (!plan.gather)
+            for (int q = 0; q < ranks; ++q) {
+                for (int i = 0; i < 3; ++i) sums[i] += ld_cluster_f64(peer(&sm.part[i], q));
+                count += static_cast<int>(ld_cluster_u32(peer(&sm.part_count, q)));
+            }
+        SampleResult res{};
+        const auto collect = [&](int which, int room) {  // the CTAs' parts of a list
+            int n = 0;
+            for (int q = 0; q < ranks; ++q) {
+                int m = static_cast<int>(ld_cluster_u32(peer(&sm.listed[which], q)));
+                if (n + m > room) {  // (the plan has counted them)
+                    res.slow = 1;
+                    m = 0;
+                }
+                for (int i = threadIdx.x; i < m; i += kSampleThreads)
+                    sorted[n + i] = ld_cluster_u64(peer(lists + which * (kSampleList / 2) + i, q));
+                n += m;
+            }
+            return n;
+        };
+        const auto logit_of = [](uint64_t entry) { return key_value(~static_cast<uint32_t>(entry >> 32)); };
+        SampleSorted list;
+        double mass, base;
+        int n, size;
+        if (plan.gather) {
+            n = collect(0, kSampleList);
+            size = sort_entries(sorted, n);
+            n = min(n, top_k);
+            list.read(sorted, n, size, sm);
+            const double target = top_p < 1.f ? top_p * list.all : 2 * list.all;
+            res.kept = list.find(n, sm.first, [&](int i, double before, double, uint64_t entry) {
+                return i && (before >= target || logit_of(entry) < edge);
+            });
+            res.kept = min(res.kept, n);
+            mass = list.sum_of(res.kept, sm);
+            base = 0;
+            n = res.kept;
+            const uint64_t last = sorted[res.kept - 1];
+            res.cut = {~static_cast<uint32_t>(last >> 32), static_cast<int>(last & 0xFFFFFFFFu)};
+        } else {
+            res.cut = {plan.by_edge ? order_key(edge) : 0u, 0x7FFFFFFF};
+            res.kept = count;
+            mass = sums[0];
+            if (plan.by_list) {
+                n = collect(1, kSampleList / 2);
+                size = sort_entries(sorted, n);
+                list.read(sorted, n, size, sm);
+                const double target = top_p * sums[0];
+                const int end = list.find(n, sm.first, [&](int i, double before, double, uint64_t entry) {
+                    return (i || plan.cut_count) && sums[1] + before >= target;
+                });
+                // the list holds the border if its first token is kept and the last one is not (or the row's last)
+                if (end == 0 || (end == kSampleList && plan.cut_count + n < count && sums[1] + list.all < target)) res.slow = 1;
+                const int by_edge = list.find(n, sm.first, [&](int, double, double, uint64_t entry) { return logit_of(entry) < edge; });
+                const int keep = min(min(end, by_edge), n);
+                res.kept = plan.cut_count + keep;
+                mass = sums[1] + list.sum_of(keep, sm);
+                if (by_edge <= min(end, n)) {
+                    res.cut = {order_key(edge), 0x7FFFFFFF};
+                } else if (keep) {
+                    const uint64_t last = sorted[keep - 1];
+                    res.cut = {~static_cast<uint32_t>(last >> 32), static_cast<int>(last & 0xFFFFFFFFu)};
+                }
+                __syncthreads();
+            }
+            n = collect(0, kSampleList / 2);
+            size = sort_entries(sorted, n);
+            list.read(sorted, n, size, sm);
+            base = sums[2];
+        }
+        const double target = u * mass;
+        const int place = list.find(n, sm.first, [&](int, double before, double w, uint64_t) { return base + before + w > target; });
+        if (place == kSampleList || base > target) res.slow = 1;
+#pragma unroll
+        for (int i = 0; i < kSamplePer; ++i)
+            if (i < list.per && list.first + i == place) {
+                res.token = static_cast<int>(list.entry[i] & 0xFFFFFFFFu);
+                res.prob = list.w[i] / mass;
+                sm.result = res;
+            }
+        if (res.slow && threadIdx.x == 0) sm.result = res;
+        __syncthreads();
+    }
+    row_sync(ranks);
+    if (rank != 0) {
+        if (threadIdx.x < sizeof(SampleResult) / 4)
+            reinterpret_cast<uint32_t *>(&sm.result)[threadIdx.x] = ld_cluster_u32(peer(reinterpret_cast<uint32_t *>(&sm.result) + threadIdx.x, 0));
+    }
+    row_sync(ranks);
+    return !sm.result.slow;
+}
+
 // ------------------------------------------------------------------------------ the kernel
 
 __device__ __forceinline__ float clamp_temperature(float T) { return fminf(fmaxf(T, 1.45e-30f), 1.44e37f); }
 
 template <typename T, bool kResident>
-__global__ void __launch_bounds__(kSampleThreads) k_sample_limits(const SampleParams p) {
+__global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const SampleParams p) {
     extern __shared__ __align__(16) uint8_t buffer[];
     __shared__ SampleShared sm;
     const int ranks = static_cast<int>(cluster_nctarank()), rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
     const long long r = blockIdx.x / ranks;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_trigger();
+    if (threadIdx.x == 0) sm.x = reinterpret_cast<SampleShared::Scratch *>(buffer + p.list_at);
     for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) sm.table[i] = g_sample_table.v[i];
     pdl_wait();
     const Slice<T, kResident> s(p, r, rank, buffer);
-    SampleRange range = load_slice(s);
     const float T_row = p.a.temperature ? p.a.temperature[r] : 1.f, u = p.a.uniform ? p.a.uniform[r] : 0.f;
     const float top_p = p.a.top_p ? p.a.top_p[r] : 1.f, min_p = p.a.min_p ? p.a.min_p[r] : 0.f;
     const int top_k = p.a.top_k ? p.a.top_k[r] : 0;
+    if (threadIdx.x == 0) {  // (on its way while the others load)
+        const float T_used = clamp_temperature(T_row);
+        sm.w.set_temperature(T_used);
+        sm.min_log = min_p > 0.f ? T_used * log(static_cast<double>(min_p)) : 0.0;
+    }
+    SampleRange range = load_slice(s);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         range.top = fmaxf(range.top, __shfl_xor_sync(0xffffffffu, range.top, o));
@@ -517,45 +1072,15 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_limits(const SamplePa
         prob = 1;
         row_sync(ranks);
     } else if (ok) {
-        const int bits = p.sum_bits;
-        const float T_used = clamp_temperature(T_row);
-        if (threadIdx.x == 0) {
-            sm.w.set(top, T_used);
-            sm.w.set_floor(bits);
+        if (threadIdx.x == 0) sm.w.set_top(top);
+        const float edge = min_p > 0.f ? __double2float_ru(top + sm.min_log) : kNoLogit;
+        if (!sample_quickly(s, sm, p, buffer, ranks, rank, top, low, edge, top_k, top_p, u)) {
+            sample_slowly(s, sm, ranks, rank, p.sum_bits, top, edge, top_k, top_p, u);
         }
-        __syncthreads();
-        float sum = 0.f;
-        s.each([&](float z, int) { sum += ex2((z - top) * sm.w.c); });
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) sm.sums[warp] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            sum = 0.f;
-            for (int w = 0; w < kSampleWarps; ++w) sum += sm.sums[w];
-            sm.sum = sum;
-        }
-        row_sync(ranks);
-        if (threadIdx.x == 0) {
-            sum = 0.f;
-            for (int q = 0; q < ranks; ++q) sum += __uint_as_float(ld_cluster_u32(peer(&sm.sum, q)));
-            sm.w.set_big(fmaxf(sum, 1.f));
-        }
-        row_sync(ranks);
-        int n;
-        double mass = kept_mass(s, sm, ranks, bits, all, n), weight;
-        if (top_k > 0 && top_k < n) cut = find_border(s, sm, ranks, rank, bits, cut, {true, false, top_k, 0.0}, n, mass, weight);
-        if (top_p < 1.f) cut = find_border(s, sm, ranks, rank, bits, cut, {false, false, 0, top_p * mass}, n, mass, weight);
-        if (min_p > 0.f) {
-            const float edge = __double2float_ru(top + T_used * log(static_cast<double>(min_p)));
-            if (order_key(edge) > cut.key) {
-                cut = {order_key(edge), 0x7FFFFFFF};
-                mass = kept_mass(s, sm, ranks, bits, cut, n);
-            }
-        }
-        kept = n;
-        token = find_border(s, sm, ranks, rank, bits, cut, {false, true, 0, u * mass}, n, prob, weight);
-        prob = weight / mass;
+        cut = sm.result.cut;
+        token = {0u, sm.result.token};
+        kept = sm.result.kept;
+        prob = sm.result.prob;
     }
     if (rank == 0 && threadIdx.x == 0) {
         p.a.out_token[r] = ok ? token.last : -1;
@@ -596,15 +1121,21 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t s) {
     const auto slice_of = [&](int n) { return ((p.words + n - 1) / n) * 32; };
     while (ranks < kSampleMaxCluster && slice_of(ranks) * static_cast<long long>(sizeof(T)) > 64 * 1024) ranks *= 2;
     p.slice = slice_of(ranks);
-    const long long bytes = p.slice * static_cast<long long>(sizeof(T)) + 32;
-    const bool resident = bytes <= kSampleSmem;
+    const long long lists = kSampleList * 8 + std::max(kSampleList * 8, kSampleBins / ranks * 8);
+    const long long slice_bytes = (p.slice * static_cast<long long>(sizeof(T)) + 47) / 16 * 16;
+    const bool resident = slice_bytes + lists <= kSampleSmem;
+    p.list_at = resident ? static_cast<int>(slice_bytes) : 0;
+    const long long bytes = p.list_at + lists;
+    int per = 0;  // tokens of a thread
+    while (kSampleThreads * static_cast<long long>(1 << per) < p.slice + 2 * kSampleThreads * 16) ++per;
+    p.thread_bits = std::min(54, 63 - per);
     void (*kernel)(const SampleParams) = resident ? k_sample_limits<T, true> : k_sample_limits<T, false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.a.rows) * ranks);
     cfg.blockDim = dim3(kSampleThreads);
-    cfg.dynamicSmemBytes = resident ? static_cast<size_t>(bytes) : 0;
+    cfg.dynamicSmemBytes = static_cast<size_t>(bytes);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
