@@ -41,26 +41,30 @@ struct SampleParams {
     int words;       // 32-bit words of a row of masks
     int slice;       // tokens of a CTA, a multiple of 32
     int sum_bits;    // units of a row's sum of weights: 2^-sum_bits of the largest
-    int thread_bits; // of a thread's
-    int list_at;     // in shared memory, where the histogram and then the lists are
+    int list_at;     // in shared memory, where the histogram and then the lists are; behind them this CTA's bins of the row
+    int upto_at;     // room for running sums of a list
 };
 
-// 2^(i / 512) in units of 2^-31.
+// 2^(i / 512) in units of 2^-31, and what is left of it in units of 2^-52 (signed).
 struct SampleTable {
     uint32_t v[kSampleTable];
-    constexpr SampleTable() : v() {
-        for (int i = 0; i < kSampleTable; ++i) {
-            const double x = i * (0.6931471805599453 / kSampleTable);
-            double term = 1, sum = 1;
-            for (int n = 1; n < 24; ++n) {
-                term *= x / n;
-                sum += term;
-            }
-            v[i] = static_cast<uint32_t>(sum * 2147483648.0 + 0.5);
-        }
-    }
+    int rest[kSampleTable];
 };
-__device__ const SampleTable g_sample_table;
+constexpr SampleTable sample_table() {
+    SampleTable t{};
+    for (int i = 0; i < kSampleTable; ++i) {
+        const double x = i * (0.6931471805599453 / kSampleTable);
+        double term = 1, sum = 1;
+        for (int n = 1; n < 24; ++n) {
+            term *= x / n;
+            sum += term;
+        }
+        t.v[i] = static_cast<uint32_t>(sum * 2147483648.0 + 0.5);
+        t.rest[i] = static_cast<int>((sum - t.v[i] / 2147483648.0) * 4503599627370496.0);
+    }
+    return t;
+}
+__device__ const SampleTable g_sample_table = sample_table();
 
 __device__ __forceinline__ uint32_t order_key(float z) {  // of floats, -0 as 0
     const uint32_t b = __float_as_uint(z + 0.f);
@@ -120,19 +124,29 @@ struct Slice {
     }
     __device__ __forceinline__ int loose() const { return row.V - row.vecs * N; }  // tokens outside vectors
     __device__ __forceinline__ int loose_at(int i) const { return i < row.peel ? i : i + row.vecs * N; }
-    // f(logit, token) for every token; threads interleave.
+    // f(logit, token) for every token; threads interleave.  (Eight bytes of a resident slice at a time: bodies of f for a whole
+    // vector are more code than the instruction caches hold, and every loop here runs some thirty times.)
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        for (int i = threadIdx.x; i < row.vecs; i += kSampleThreads) {
-            const uint4 raw = kResident ? *reinterpret_cast<const uint4 *>(buf + (row.peel + i * N) * sizeof(T))
-                                        : allowed_vec(global_vec(i), i);
+        constexpr int n = kResident ? N / 2 : N;
+        const int pieces = row.vecs * (N / n);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < pieces; i += kSampleThreads) {
+            const int first = row.peel + i * n;
             float z[N];
-            unpack(raw, z, T());
+            if (kResident) {
+                const uint2 raw = *reinterpret_cast<const uint2 *>(buf + first * sizeof(T));
+                unpack(make_uint4(raw.x, raw.y, 0, 0), z, T());
+            } else {
+                unpack(allowed_vec(global_vec(i), i), z, T());
+            }
 #pragma unroll
-            for (int k = 0; k < N; ++k) f(z[k], v0 + row.peel + i * N + k);
+            for (int k = 0; k < n; ++k) f(z[k], v0 + first + k);
         }
-        if (static_cast<int>(threadIdx.x) < loose()) {
-            const int j = loose_at(threadIdx.x);
+        const int rest = loose();
+#pragma unroll 1
+        for (int i = threadIdx.x; i < rest; i += kSampleThreads) {
+            const int j = loose_at(i);
             f(at(j), v0 + j);
         }
     }
@@ -193,8 +207,8 @@ __device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s) 
 struct SampleWeights {
     float A, c_hi, c_lo, rest_top, floor, big;
     int k_top;  // as the bits of the shifted product
-    float c;
-    double top, inverse_T;
+    int64_t rest64_top;
+    float c, top, temperature;
     static constexpr float kShift = 1.5f * (1 << 14);  // floats near it have steps of 1/512
     // y = d c to the nearest 1 / 512 (its bits), and the rest.  (Every operation rounds by itself: the largest logit's rest is
     // to be the same number wherever it is made.)
@@ -203,24 +217,27 @@ struct SampleWeights {
         rest = __fadd_rn(__fsub_rn(y, __fsub_rn(t, kShift)), fmaf(d, c_lo, fmaf(d, c_hi, -y)));
         return __float_as_int(t);
     }
-    __device__ void set_temperature(double T) {
-        inverse_T = 1.0 / T;
-        const double c64 = 1.4426950408889634 / T;
-        c_hi = c = static_cast<float>(c64);
-        c_lo = static_cast<float>(c64 - c_hi);
+    // log2 e / T in two floats: the quotient and what it leaves, divided again.
+    __device__ void set_temperature(float T) {
+        constexpr float kHigh = 1.44269502f, kLow = 1.92596303e-8f;  // log2 e
+        temperature = T;
+        c_hi = __fdiv_rn(kHigh, T);
+        c_lo = __fdiv_rn(fmaf(-c_hi, T, kHigh) + kLow, T);
+        c = c_hi;
     }
     __device__ void set_top(float top_logit) {
         top = top_logit;
         A = fabsf(top_logit) * c < 0x1p12f ? 0.f : top_logit;
         k_top = split(top_logit - A, rest_top);
+        rest64_top = rest64(top_logit - A, k_top);
         big = -kNoLogit;
     }
     // Logits at and below `floor` weigh nothing: under 2^-bits.
     __device__ void set_floor(int bits) {
-        floor = fmaxf(kLowest, __fsub_rd(static_cast<float>(top), __fdiv_ru(static_cast<float>(bits), c)));
+        floor = fmaxf(kLowest, __fsub_rd(top, __fdiv_ru(static_cast<float>(bits), c)));
     }
     // Of a sum of about `sum` times the largest weight, those that hold 2^-10 and more.
-    __device__ void set_big(float sum) { big = static_cast<float>(top) - (10.f - log2f(sum)) / c; }
+    __device__ void set_big(float sum) { big = top - (10.f - log2f(sum)) / c; }
     __device__ __forceinline__ uint64_t of(float z, int bits, const uint32_t *table) const {
         float r;
         const int k = split(fmaxf(z, floor) - A, r) - k_top;
@@ -233,10 +250,30 @@ struct SampleWeights {
         const uint64_t m = static_cast<uint64_t>(table[k & (kSampleTable - 1)]) * one_q;  // 2^62 to 2^63
         return m >> (62 - bits - (k >> 9));
     }
+    // The rest of y in units of 2^-52: the product's and its error.
+    __device__ __forceinline__ int64_t rest64(float d, int &k) const {
+        const float y = __fmul_rn(d, c_hi), t = __fadd_rn(y, kShift);
+        k = __float_as_int(t);
+        return __float2ll_rn(__fsub_rn(y, __fsub_rn(t, kShift)) * 0x1p52f) + __float2ll_rn(fmaf(d, c_lo, fmaf(d, c_hi, -y)) * 0x1p52f);
+    }
+    // The same weight with every step in 64 bits, right to some 2^-42.
+    __device__ __noinline__ uint64_t in_64_bits(float z, int bits, const SampleTable *table) const {
+        int k;
+        const int64_t r = rest64(z - A, k) - rest64_top;
+        k -= k_top;
+        const int64_t x = __mul64hi(r << 8, 0x58B90BFBE8E7BCD6ll) >> 7;  // r ln 2: ln 2 in units of 2^-63
+        const float xf = static_cast<float>(x) * 0x1p-52f;
+        const int64_t p = x + (__mul64hi(x << 6, x << 6) >> 1) + __float2ll_rn(xf * xf * xf * (0.16666667f + xf * 0.041666668f) * 0x1p52f);
+        const int at = k & (kSampleTable - 1);
+        const int64_t whole = (static_cast<int64_t>(table->v[at]) << 21) + table->rest[at];
+        const uint64_t m = static_cast<uint64_t>(whole + __mul64hi(whole << 5, p << 7));  // 2^52 to 2^53
+        const int down = 52 - bits - (k >> 9);
+        return down > 0 ? (m >> (down - 1)) + 1 >> 1 : m << -down;
+    }
     // With the big ones in 64 bits; 0 at the floor.
-    __device__ __forceinline__ uint64_t exact_of(float z, int bits, const uint32_t *table) const {
-        if (z >= big) return __double2ull_rn(exp((z - top) * inverse_T) * static_cast<double>(1ull << bits));
-        return z > floor ? of(z, bits, table) : 0ull;
+    __device__ __forceinline__ uint64_t exact_of(float z, int bits, const SampleTable &table) const {
+        if (z >= big) return in_64_bits(z, bits, &table);
+        return z > floor ? of(z, bits, table.v) : 0ull;
     }
 };
 
@@ -264,16 +301,22 @@ struct SamplePlan {
     float scale;
     int cut_count;          // tokens before cut0
     float sum;              // about that of all weights
+    int bits;               // units of sums: 2^-bits of the largest weight; all of them fit 62 bits
+};
+// An entry of a sorted list, and the weights before it.
+struct SampleHit {
+    int at;
+    uint64_t before, w, entry;
 };
 struct SampleResult {
     int slow;
     SampleCut cut;
     int token, kept;
-    double prob;
+    float prob;
 };
 
 struct SampleShared {
-    uint32_t table[kSampleTable];
+    SampleTable table;
     SampleWeights w;
     // what lies where the first histogram was, and the lists will be
     struct Scratch {
@@ -287,7 +330,6 @@ struct SampleShared {
     int bad;
     float sums[kSampleWarps];
     float sum;
-    double sum64[kSampleWarps];
     int counts[kSampleWarps];
     // what the first CTA of the cluster has found
     uint64_t above;            // of the bins above the border's
@@ -297,21 +339,17 @@ struct SampleShared {
     double min_log;            // T log(min_p): min-p keeps logits from so far below the largest on
     // the quick way
     int binned, tail;          // a slice's tokens in the bins, and below them
-    int listed[2];             // entries of the lists
     SampleFound found[4];
     SamplePlan plan;
     SampleResult result;
-    double sums64[3][kSampleWarps];
-    double part[3];            // a slice's weights: of all that count, above the cut's bins, above the draw's
-    int part_count;
-    int first;
+    // in the first CTA
+    int listed[2];             // entries of the lists
+    uint64_t part[kSampleMaxCluster][3];  // of every CTA: weights of all that count, above the cut's bins, above the draw's
+    int part_count[kSampleMaxCluster];
+    uint64_t warp_sums[3][kSampleWarps];
+    SampleHit hit;
 };
 
-__device__ __forceinline__ double ld_cluster_f64(uint32_t a) {
-    double v;
-    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(a) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
     uint64_t v;
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
@@ -322,6 +360,16 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
 }
+__device__ __forceinline__ void st_cluster_u64(uint32_t a, uint64_t v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+}
+__device__ __forceinline__ int add_cluster(uint32_t a, int n) {  // returns the value before
+    int old;
+    asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(n) : "memory");
+    return old;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 template <typename V>
 __device__ __forceinline__ uint32_t peer(const V *p, int rank) { return mapa_shared(smem_u32(p), rank); }
 
@@ -502,6 +550,25 @@ __device__ __noinline__ double kept_mass(const S &s, SampleShared &sm, int ranks
     return static_cast<double>(m);
 }
 
+// The tokens that `keep` holds for as bits: 32 tokens a warp and word; a lane keeps one of 32 words, so that they are
+// stored together.
+template <typename S, typename F>
+__device__ __forceinline__ void write_bits(const S &s, uint32_t *out, F keep) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, words = (s.row.V + 31) / 32;
+    out += s.v0 / 32;
+    for (int w0 = warp * 32; w0 < words; w0 += kSampleThreads) {
+        uint32_t mine = 0;
+#pragma unroll 8
+        for (int i = 0; i < 32; ++i) {
+            const int j = (w0 + i) * 32 + lane;
+            const float z = j < s.row.V ? s.at(j) : kNoLogit;
+            const uint32_t word = __ballot_sync(0xffffffffu, z >= kLowest && keep(z, s.v0 + j));
+            if (i == lane) mine = word;
+        }
+        if (w0 + lane < words) out[w0 + lane] = mine;
+    }
+}
+
 // Every border in four passes.  Leaves the result in every CTA.
 template <typename S>
 __device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ranks, int rank, int bits, float top, float edge, int top_k,
@@ -537,7 +604,7 @@ __device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ran
         mass = kept_mass(s, sm, ranks, bits, cut, n);
     }
     const SampleCut token = find_border(s, sm, ranks, rank, bits, cut, {false, true, 0, u * mass}, place, upto, weight);
-    if (threadIdx.x == 0) sm.result = {0, cut, token.last, n, weight / mass};
+    if (threadIdx.x == 0) sm.result = {0, cut, token.last, n, static_cast<float>(weight / mass)};
     __syncthreads();
 }
 
@@ -549,95 +616,147 @@ __device__ __forceinline__ float sample_place(float z, float top, float scale) {
 // Entries in ascending order are tokens in theirs.
 __device__ __forceinline__ uint64_t sample_entry(float z, int v) { return static_cast<uint64_t>(~order_key(z)) << 32 | static_cast<uint32_t>(v); }
 
-// n entries, padded to a power of two (returned), by the CTA.
-__device__ __forceinline__ int sort_entries(uint64_t *list, int n) {
-    int size = 32;
-    while (size < n) size <<= 1;
-    for (int i = n + threadIdx.x; i < size; i += kSampleThreads) list[i] = ~0ull;
-    __syncthreads();
+// Up to kSampleThreads entries of each of kLists lists, which lie `apart` entries apart: an entry a thread, exchanged by shuffles
+// where its partner is in the same warp.
+template <int kLists>
+__device__ __forceinline__ void sort_in_registers(uint64_t *list, int apart, int size) {
+    const int t = threadIdx.x;
+    uint64_t x[kLists];
+#pragma unroll
+    for (int l = 0; l < kLists; ++l) x[l] = t < size ? list[l * apart + t] : ~0ull;
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j; j >>= 1) {
-            for (int i = threadIdx.x; i < size / 2; i += kSampleThreads) {
-                const int a = 2 * i - (i & (j - 1)), b = a + j;
-                const uint64_t x = list[a], y = list[b];
-                if ((x > y) == ((a & k) == 0)) {
-                    list[a] = y;
-                    list[b] = x;
-                }
+            const bool low = ((t & k) == 0) == ((t & j) == 0);  // keeps the smaller one
+            uint64_t y[kLists];
+            if (j >= 32) {
+                __syncthreads();
+#pragma unroll
+                for (int l = 0; l < kLists; ++l)
+                    if (t < size) list[l * apart + t] = x[l];
+                __syncthreads();
+#pragma unroll
+                for (int l = 0; l < kLists; ++l) y[l] = t < size ? list[l * apart + (t ^ j)] : ~0ull;
+            } else {
+#pragma unroll
+                for (int l = 0; l < kLists; ++l) y[l] = __shfl_xor_sync(0xffffffffu, x[l], j);
             }
-            __syncthreads();
+#pragma unroll
+            for (int l = 0; l < kLists; ++l)
+                if ((y[l] < x[l]) == low) x[l] = y[l];
         }
+    __syncthreads();
+#pragma unroll
+    for (int l = 0; l < kLists; ++l)
+        if (t < size) list[l * apart + t] = x[l];
+    __syncthreads();
+}
+
+// n0 entries, and n1 from kSampleList / 2 on, by the CTA; each padded to `size`, a power of two (returned).
+__device__ __noinline__ int sort_entries(uint64_t *list, int n0, int n1) {
+    int size = 32;
+    while (size < n0 || size < n1) size <<= 1;
+    for (int i = n0 + threadIdx.x; i < size; i += kSampleThreads) list[i] = ~0ull;
+    if (n1)
+        for (int i = n1 + threadIdx.x; i < size; i += kSampleThreads) list[kSampleList / 2 + i] = ~0ull;
+    __syncthreads();
+    if (size <= kSampleThreads) {
+        if (n1)
+            sort_in_registers<2>(list, kSampleList / 2, size);
+        else
+            sort_in_registers<1>(list, 0, size);
+        return size;
+    }
+    for (int l = 0; l < (n1 ? 2 : 1); ++l, list += kSampleList / 2)
+        for (int k = 2; k <= size; k <<= 1)
+            for (int j = k >> 1; j; j >>= 1) {
+                for (int i = threadIdx.x; i < size / 2; i += kSampleThreads) {
+                    const int a = 2 * i - (i & (j - 1)), b = a + j;
+                    const uint64_t x = list[a], y = list[b];
+                    if ((x > y) == ((a & k) == 0)) {
+                        list[a] = y;
+                        list[b] = x;
+                    }
+                }
+                __syncthreads();
+            }
     return size;
 }
 
-constexpr int kSamplePer = kSampleList / kSampleThreads;  // entries of a thread
-
-// Sums of the threads' numbers before each, and of all, in the threads' order.
-__device__ __forceinline__ double scan_block(double mine, double *warps, double &all) {
-    double upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const double up = __shfl_up_sync(0xffffffffu, upto, o);
-        if ((threadIdx.x & 31) >= o) upto += up;
+// a f, f in [0, 1), rounded down or up.
+__device__ __forceinline__ uint64_t times_fraction(uint64_t a, float f, bool up) {
+    const uint32_t b = __float_as_uint(f), e = b >> 23;
+    const uint64_t m = e ? (b & 0x7FFFFFu) | 0x800000u : b & 0x7FFFFFu;
+    const int s = 150 - static_cast<int>(max(e, 1u));  // f = m 2^-s, s >= 24
+    const uint64_t hi = __umul64hi(a, m), lo = a * m;
+    if (s >= 128) return up && (hi | lo);
+    if (s >= 64) {
+        const uint64_t q = hi >> (s - 64);
+        return q + (up && (lo || (q << (s - 64)) != hi));
     }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 31) warps[threadIdx.x >> 5] = upto;
-    __syncthreads();
-    double before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kSampleWarps; ++w) {
-        if (w == static_cast<int>(threadIdx.x >> 5)) before = all;
-        all += warps[w];
-    }
-    return before + upto - mine;
+    return (hi << (64 - s) | lo >> s) + (up && lo << (64 - s));
 }
 
-// A sorted list in the threads' registers: neighbouring entries, their weights, and the sum of those before.
-struct SampleSorted {
-    uint64_t entry[kSamplePer];
-    double w[kSamplePer], before, all;
-    int first, per;
-    __device__ void read(const uint64_t *list, int n, int size, SampleShared &sm) {
-        per = max(1, size / kSampleThreads);
-        first = threadIdx.x * per;
-        double mine = 0;
+// a / b to the nearest fp32 number, nearly: numbers as two floats each, the quotient's rest divided again.
+__device__ __forceinline__ float quotient(uint64_t a, uint64_t b) {
+    const float a_hi = __ull2float_rz(a), b_hi = __ull2float_rz(b);
+    const float a_lo = __ull2float_rn(a - __float2ull_rz(a_hi)), b_lo = __ull2float_rn(b - __float2ull_rz(b_hi));
+    const float q = a_hi / b_hi;
+    return q + (fmaf(-q, b_hi, a_hi) + fmaf(-q, b_lo, a_lo)) / b_hi;
+}
+
+// Running sums of the weights of n sorted entries, up to and with each, in shared memory; the sum of all is returned.
+__device__ __forceinline__ uint64_t add_up(const uint64_t *list, int n, uint64_t *upto, int bits, SampleShared &sm) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint64_t before = 0;
+#pragma unroll 1
+    for (int first = 0; first < n; first += kSampleThreads) {
+        const int i = first + threadIdx.x;
+        uint64_t m = i < n ? sm.w.exact_of(key_value(~static_cast<uint32_t>(list[i] >> 32)), bits, sm.table) : 0ull;
 #pragma unroll
-        for (int i = 0; i < kSamplePer; ++i) {
-            const bool in = i < per && first + i < n;
-            entry[i] = in ? list[first + i] : ~0ull;
-            w[i] = in ? static_cast<double>(sm.w.exact_of(key_value(~static_cast<uint32_t>(entry[i] >> 32)), 54, sm.table)) * 0x1p-54 : 0.0;
-            mine += w[i];
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t up = __shfl_up_sync(0xffffffffu, m, o);
+            if (lane >= o) m += up;
         }
-        before = scan_block(mine, sm.sum64, all);
-    }
-    // Smallest number of an entry for which f(number, running sum before it, its weight) holds; kSampleList if none.
-    template <typename F>
-    __device__ int find(int n, int &slot, F f) const {
+        if (lane == 31) sm.warp_sums[0][warp] = m;
         __syncthreads();
-        if (threadIdx.x == 0) slot = kSampleList;
-        __syncthreads();
-        double at = before;
-        int found = kSampleList;
+        uint64_t all = before;
 #pragma unroll
-        for (int i = 0; i < kSamplePer; ++i) {
-            if (i < per && first + i < n && found == kSampleList && f(first + i, at, w[i], entry[i])) found = first + i;
-            at += w[i];
+        for (int w = 0; w < kSampleWarps; ++w) {
+            const uint64_t v = sm.warp_sums[0][w];
+            if (w < warp) before += v;
+            all += v;
         }
-        if (found < kSampleList) atomicMin(&slot, found);
+        if (i < n) upto[i] = before + m;
+        before = all;
         __syncthreads();
-        return slot;
     }
-    // Weights of the first m entries.
-    __device__ double sum_of(int m, SampleShared &sm) const {
-        double mine = 0, total;
-#pragma unroll
-        for (int i = 0; i < kSamplePer; ++i)
-            if (i < per && first + i < m) mine += w[i];
-        scan_block(mine, sm.sum64, total);
-        return total;
+    return before;
+}
+
+// The first entry at which the weights, `base` and those before it, reach `target`, or whose logit is below `edge`
+// (but not entry 0 if `spare`); or, `through`, the first with which they exceed `target`.  Number n if there is none.
+__device__ __forceinline__ SampleHit find_entry(const uint64_t *list, const uint64_t *upto, int n, uint64_t base, uint64_t target, bool through,
+                                                bool spare, float edge, SampleShared &sm) {
+    __syncthreads();
+    if (threadIdx.x == 0) sm.hit = {n, n ? upto[n - 1] : 0ull, 0, ~0ull};
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kSampleThreads) {
+        const uint64_t with = upto[i], before = i ? upto[i - 1] : 0ull;
+        bool now, earlier;  // whether it holds for this entry and for the one before (once it holds it does for all that follow)
+        if (through) {
+            now = base + with > target;
+            earlier = i && base + before > target;
+        } else {
+            const auto below = [&](int j) { return key_value(~static_cast<uint32_t>(list[j] >> 32)) < edge; };
+            now = (base + before >= target || below(i)) && !(spare && i == 0);
+            earlier = i && (base + (i > 1 ? upto[i - 2] : 0ull) >= target || below(i - 1)) && !(spare && i == 1);
+        }
+        if (now && !earlier) sm.hit = {i, before, with - before, list[i]};
     }
-};
+    __syncthreads();
+    return sm.hit;
+}
 
 // The first histogram's bins in the threads of the row's first CTA, eight neighbours each, with the running count and
 // sum before them.
@@ -645,15 +764,17 @@ struct SampleBins {
     static constexpr int kPer = kSampleBins / kSampleThreads;
     int count[kPer];
     float sum[kPer];
-    // The first bin at whose end f(count, sum) holds; bin = kSampleBins if at none.
-    template <typename F>
-    __device__ void find(SampleShared &sm, SampleFound &to, F f) const {
+    // The first bin up to whose end there are `least` tokens (by_count), or a sum of `least` or more (or of more); bin =
+    // kSampleBins if there is none.
+    __device__ __forceinline__ void find(SampleShared &sm, SampleFound &to, bool by_count, float least, bool more) const {
+        const auto f = [&](int n, float m) { return by_count ? n >= static_cast<int>(least) : more ? m > least : m >= least; };
         if (threadIdx.x == 0 && !f(sm.x->scan_count[kSampleThreads], sm.x->scan[kSampleThreads]))
             to = {kSampleBins, sm.x->scan_count[kSampleThreads], sm.x->scan_count[kSampleThreads], sm.x->scan[kSampleThreads], sm.x->scan[kSampleThreads]};
         const bool before = threadIdx.x && f(sm.x->scan_count[threadIdx.x], sm.x->scan[threadIdx.x]);
         if (before || !f(sm.x->scan_count[threadIdx.x + 1], sm.x->scan[threadIdx.x + 1])) return;
         int c = sm.x->scan_count[threadIdx.x];
         float e = sm.x->scan[threadIdx.x];
+#pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (i == kPer - 1 || f(c + count[i], e + sum[i])) {
                 to = {static_cast<int>(threadIdx.x) * kPer + i, c, c + count[i], e, e + sum[i]};
@@ -674,11 +795,14 @@ __device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const 
     const int per_rank = kSampleBins / ranks, first = threadIdx.x * kPer;
     int c = 0;
     float e = 0.f;
+    const uint32_t from = mapa_shared(smem_u32(own + first % per_rank * 8), first / per_rank);
+    uint64_t v[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = ld_cluster_u64(from + i * 8);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const uint64_t v = ld_cluster_u64(mapa_shared(smem_u32(own + (first + i) % per_rank * 8), (first + i) / per_rank));
-        bins.count[i] = static_cast<int>(v);
-        bins.sum[i] = __uint_as_float(static_cast<uint32_t>(v >> 32));
+        bins.count[i] = static_cast<int>(v[i]);
+        bins.sum[i] = __uint_as_float(static_cast<uint32_t>(v[i] >> 32));
         c += bins.count[i];
         e += bins.sum[i];
     }
@@ -713,19 +837,22 @@ __device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const 
     const int binned = sm.x->scan_count[kSampleThreads];
     const float sum = sm.x->scan[kSampleThreads], error = kBinError * sum;
     int expected = 0, tail = 0;
-    for (int q = 0; q < ranks; ++q) {
-        expected += static_cast<int>(ld_cluster_u32(peer(&sm.binned, q)));
-        tail += static_cast<int>(ld_cluster_u32(peer(&sm.tail, q)));
+    if (lane < ranks) {
+        expected = static_cast<int>(ld_cluster_u32(peer(&sm.binned, lane)));
+        tail = static_cast<int>(ld_cluster_u32(peer(&sm.tail, lane)));
     }
+    expected = __reduce_add_sync(0xffffffffu, expected);
+    tail = __reduce_add_sync(0xffffffffu, tail);
     SamplePlan plan{};
     plan.scale = scale;
     plan.sum = fmaxf(sum, 1.f);
+    plan.bits = min(54, 60 - ilogbf(plan.sum));
     plan.cut0 = plan.cut1 = -1.f;
     plan.slow = binned != expected;  // a bin had more tokens than it can count
     constexpr float kEnd = static_cast<float>(kSampleBins) * kBinParts;
     const auto place_of = [](int bin) { return static_cast<float>(bin) * kBinParts; };
     if (top_k > 0 && top_k < binned + tail) {
-        bins.find(sm, sm.found[0], [&](int n, float) { return n >= top_k; });
+        bins.find(sm, sm.found[0], true, static_cast<float>(top_k), false);
         __syncthreads();
         plan.gather = 1;
         plan.draw1 = place_of(sm.found[0].bin + 1);
@@ -736,8 +863,8 @@ __device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const 
         const float edge_place = edge == kNoLogit ? kEnd : fminf(sample_place(edge, top, scale), kEnd);
         plan.by_edge = edge != kNoLogit;
         if (top_p < 1.f) {
-            bins.find(sm, sm.found[0], [&](int, float m) { return m >= top_p * sum - error; });
-            bins.find(sm, sm.found[1], [&](int, float m) { return m >= top_p * sum + error; });
+            bins.find(sm, sm.found[0], false, top_p * sum - error, false);
+            bins.find(sm, sm.found[1], false, top_p * sum + error, false);
             __syncthreads();
             const int b0 = sm.found[0].bin, b1 = min(sm.found[1].bin, kSampleBins - 1);
             if (edge_place >= place_of(b0)) {
@@ -769,8 +896,8 @@ __device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const 
         }
         least = u * least - error;
         most = u * most + error;
-        bins.find(sm, sm.found[2], [&](int, float m) { return m > least; });
-        bins.find(sm, sm.found[3], [&](int, float m) { return m > most; });
+        bins.find(sm, sm.found[2], false, least, true);
+        bins.find(sm, sm.found[3], false, most, true);
         __syncthreads();
         const bool past = sm.found[3].bin > last;
         const int b0 = min(sm.found[2].bin, last), b1 = past ? last : sm.found[3].bin;
@@ -782,31 +909,24 @@ __device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const 
     if (threadIdx.x == 0) sm.plan = plan;
 }
 
+// A token's entry at the end of a list in the first CTA's shared memory.
+__device__ __noinline__ void list_token(uint32_t listed, uint32_t list, int room, float z, int v) {
+    const int at = add_cluster(listed, 1);
+    if (at < room) st_cluster_u64(list + at * 8, sample_entry(z, v));
+}
+
 // A first histogram of the row over 4096 bins, equally wide in the logit, says in which one or two of them each border is;
-// a second pass adds the weights before these up, exactly, and lists the tokens in them, which the first CTA sorts.
-// With top-k all tokens that may be kept are listed.  False: the row is not like that (so many equal logits that a
-// bin's count or a list runs over, or a k of thousands).  Leaves the result in every CTA.
+// a second pass adds the weights before these up, exactly, and lists the tokens in them in the first CTA's shared memory,
+// which sorts them (solve_lists).  With top-k all tokens that may be kept are listed.  False: the row is not like that (so many equal
+// logits that a bin's count or a list runs over, or a k of thousands).  `hist` is clear; kept tokens' bits go to out, those in
+// the cut's bins excepted.
 template <typename S>
-__device__ __forceinline__ bool sample_quickly(const S &s, SampleShared &sm, const SampleParams &p, uint8_t *buffer, int ranks, int rank,
-                                               float top, float low, float edge, int top_k, float top_p, float u) {
+__device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint32_t *hist, uint8_t *own, int ranks, int rank, float top,
+                                             float low, float edge, int top_k, float top_p, float u, uint32_t *out) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint32_t *hist = reinterpret_cast<uint32_t *>(buffer + p.list_at);
-    uint64_t *lists = reinterpret_cast<uint64_t *>(buffer + p.list_at);
-    uint8_t *own = buffer + p.list_at + kSampleList * 8;  // this CTA's bins of the row: counts and sums; then the sorted list
-    static_assert(kSampleBins * 4 <= kSampleList * 8 && sizeof(SampleShared::Scratch) <= kSampleList * 8, "lists take their place");
-    const auto list_token = [&](int which, int room, float z, int v) {
-        const int at = atomicAdd(&sm.listed[which], 1);
-        if (at < room) lists[which * (kSampleList / 2) + at] = sample_entry(z, v);
-    };
     const float c = sm.w.c;
     const float span = fminf(fminf(kBinOctaves / c, top - low), 3e38f);
     const float scale = span > 0.f ? fminf((kSampleBins * kBinParts - kBinParts / 2) / span, 1e38f) : 0.f;
-    if (threadIdx.x == 0) {
-        sm.binned = sm.tail = 0;
-        sm.listed[0] = sm.listed[1] = 0;
-    }
-    for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
     int binned = 0, tail = 0;
     s.each([&](float z, int) {
         if (z >= kLowest) {
@@ -831,13 +951,15 @@ __device__ __forceinline__ bool sample_quickly(const S &s, SampleShared &sm, con
     const float octaves = scale > 0.f ? c / scale : 0.f;  // of a part of a bin
     for (int i = threadIdx.x; i < per_rank; i += kSampleThreads) {
         const int b = rank * per_rank + i;
-        uint32_t n = 0, parts = 0;
-        for (int q = 0; q < ranks; ++q) {
-            const uint32_t v = ld_cluster_u32(peer(&hist[b], q));
-            n += v >> 20;
-            parts += v & 0xFFFFFu;
+        uint32_t v[kSampleMaxCluster], n = 0, parts = 0;
+#pragma unroll
+        for (int q = 0; q < kSampleMaxCluster; ++q) v[q] = q < ranks ? ld_cluster_u32(peer(&hist[b], q)) : 0u;
+#pragma unroll
+        for (int q = 0; q < kSampleMaxCluster; ++q) {
+            n += v[q] >> 20;
+            parts += v[q] & 0xFFFFFu;
         }
-        const float mean = n ? static_cast<float>(parts) / static_cast<float>(n) + 0.5f : 0.f;
+        const float mean = n ? __fdividef(static_cast<float>(parts), static_cast<float>(n)) + 0.5f : 0.f;
         const float sum = static_cast<float>(n) * ex2(-(static_cast<float>(b * kBinParts) + mean) * octaves);
         reinterpret_cast<uint2 *>(own)[i] = make_uint2(n, __float_as_uint(sum));
     }
@@ -853,151 +975,118 @@ __device__ __forceinline__ bool sample_quickly(const S &s, SampleShared &sm, con
         row_sync(ranks);
         return false;
     }
-    const int bits = p.thread_bits;
     if (threadIdx.x == 0) {
-        sm.w.set_floor(bits);
+        sm.w.set_floor(sm.plan.bits);
         sm.w.set_big(sm.plan.sum);
     }
     __syncthreads();
-    const SamplePlan plan = sm.plan;
-    if (plan.gather) {
+    const uint32_t lists = peer(reinterpret_cast<uint64_t *>(hist), 0), listed = peer(&sm.listed[0], 0);
+    const float draw0 = sm.plan.draw0, draw1 = sm.plan.draw1, cut0 = sm.plan.cut0, cut1 = sm.plan.cut1;
+    const float from = sm.plan.by_edge ? edge : kLowest;
+    if (sm.plan.gather) {
         s.each([&](float z, int v) {
-            if (z >= kLowest && sample_place(z, top, scale) < plan.draw1) list_token(0, kSampleList, z, v);
+            if (z >= kLowest && sample_place(z, top, scale) < draw1) list_token(listed, lists, kSampleList, z, v);
         });
     } else {
         const SampleWeights w = sm.w;
-        uint64_t all = 0, before_cut = 0, before_draw = 0;
+        const int bits = sm.plan.bits;
+        uint64_t sums[3] = {0, 0, 0};
         int count = 0;
-        const float from = plan.by_edge ? edge : kLowest;
         s.each([&](float z, int v) {
             if (z >= from) {
                 ++count;
-                const uint64_t m = w.exact_of(z, bits, sm.table);
+                const uint64_t m = z >= w.big ? sm.w.in_64_bits(z, bits, &sm.table) : z > w.floor ? w.of(z, bits, sm.table.v) : 0ull;
                 const float at = sample_place(z, top, scale);
-                all += m;
-                if (at < plan.cut0) before_cut += m;
-                if (at < plan.draw0) before_draw += m;
-                if (at >= plan.draw0 && at < plan.draw1) list_token(0, kSampleList / 2, z, v);
-                if (at >= plan.cut0 && at < plan.cut1) list_token(1, kSampleList / 2, z, v);
+                sums[0] += m;
+                sums[1] += at < cut0 ? m : 0;
+                sums[2] += at < draw0 ? m : 0;
+                if (at < fmaxf(cut1, draw1)) {
+                    if (at >= cut0 && at < cut1) list_token(listed + 4, lists + kSampleList * 4, kSampleList / 2, z, v);
+                    if (at >= draw0 && at < draw1) list_token(listed, lists, kSampleList / 2, z, v);
+                }
             }
         });
-        const double unit = 1.0 / static_cast<double>(1ull << bits);
-        double sums[3] = {static_cast<double>(all) * unit, static_cast<double>(before_cut) * unit, static_cast<double>(before_draw) * unit};
         count = __reduce_add_sync(0xffffffffu, count);
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
 #pragma unroll
             for (int o = 16; o; o >>= 1) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
-            if (lane == 0) sm.sums64[i][warp] = sums[i];
+            if (lane == 0) sm.warp_sums[i][warp] = sums[i];
         }
         if (lane == 0) sm.counts[warp] = count;
         __syncthreads();
         if (threadIdx.x < 4) {
-            double m = 0;
+            uint64_t m = 0;
             int n = 0;
+#pragma unroll
             for (int i = 0; i < kSampleWarps; ++i) {
                 n += sm.counts[i];
-                if (threadIdx.x < 3) m += sm.sums64[threadIdx.x][i];
+                m += sm.warp_sums[min(2, static_cast<int>(threadIdx.x))][i];
             }
-            if (threadIdx.x < 3) sm.part[threadIdx.x] = m;
-            if (threadIdx.x == 3) sm.part_count = n;
+            if (threadIdx.x < 3)
+                st_cluster_u64(peer(&sm.part[rank][threadIdx.x], 0), m);
+            else
+                st_shared_cluster(peer(&sm.part_count[rank], 0), n);
         }
     }
-    row_sync(ranks);
-    if (rank == 0) {
-        uint64_t *sorted = reinterpret_cast<uint64_t *>(own);
-        double sums[3] = {0, 0, 0};
-        int count = 0;
-        if (!plan.gather)
-            for (int q = 0; q < ranks; ++q) {
-                for (int i = 0; i < 3; ++i) sums[i] += ld_cluster_f64(peer(&sm.part[i], q));
-                count += static_cast<int>(ld_cluster_u32(peer(&sm.part_count, q)));
-            }
-        SampleResult res{};
-        const auto collect = [&](int which, int room) {  // the CTAs' parts of a list
-            int n = 0;
-            for (int q = 0; q < ranks; ++q) {
-                int m = static_cast<int>(ld_cluster_u32(peer(&sm.listed[which], q)));
-                if (n + m > room) {  // (the plan has counted them)
-                    res.slow = 1;
-                    m = 0;
-                }
-                for (int i = threadIdx.x; i < m; i += kSampleThreads)
-                    sorted[n + i] = ld_cluster_u64(peer(lists + which * (kSampleList / 2) + i, q));
-                n += m;
-            }
-            return n;
-        };
-        const auto logit_of = [](uint64_t entry) { return key_value(~static_cast<uint32_t>(entry >> 32)); };
-        SampleSorted list;
-        double mass, base;
-        int n, size;
-        if (plan.gather) {
-            n = collect(0, kSampleList);
-            size = sort_entries(sorted, n);
-            n = min(n, top_k);
-            list.read(sorted, n, size, sm);
-            const double target = top_p < 1.f ? top_p * list.all : 2 * list.all;
-            res.kept = list.find(n, sm.first, [&](int i, double before, double, uint64_t entry) {
-                return i && (before >= target || logit_of(entry) < edge);
-            });
-            res.kept = min(res.kept, n);
-            mass = list.sum_of(res.kept, sm);
-            base = 0;
-            n = res.kept;
-            const uint64_t last = sorted[res.kept - 1];
-            res.cut = {~static_cast<uint32_t>(last >> 32), static_cast<int>(last & 0xFFFFFFFFu)};
-        } else {
-            res.cut = {plan.by_edge ? order_key(edge) : 0u, 0x7FFFFFFF};
-            res.kept = count;
-            mass = sums[0];
-            if (plan.by_list) {
-                n = collect(1, kSampleList / 2);
-                size = sort_entries(sorted, n);
-                list.read(sorted, n, size, sm);
-                const double target = top_p * sums[0];
-                const int end = list.find(n, sm.first, [&](int i, double before, double, uint64_t entry) {
-                    return (i || plan.cut_count) && sums[1] + before >= target;
-                });
-                // the list holds the border if its first token is kept and the last one is not (or the row's last)
-                if (end == 0 || (end == kSampleList && plan.cut_count + n < count && sums[1] + list.all < target)) res.slow = 1;
-                const int by_edge = list.find(n, sm.first, [&](int, double, double, uint64_t entry) { return logit_of(entry) < edge; });
-                const int keep = min(min(end, by_edge), n);
-                res.kept = plan.cut_count + keep;
-                mass = sums[1] + list.sum_of(keep, sm);
-                if (by_edge <= min(end, n)) {
-                    res.cut = {order_key(edge), 0x7FFFFFFF};
-                } else if (keep) {
-                    const uint64_t last = sorted[keep - 1];
-                    res.cut = {~static_cast<uint32_t>(last >> 32), static_cast<int>(last & 0xFFFFFFFFu)};
-                }
-                __syncthreads();
-            }
-            n = collect(0, kSampleList / 2);
-            size = sort_entries(sorted, n);
-            list.read(sorted, n, size, sm);
-            base = sums[2];
+    if (out) {
+        const float end = sm.plan.gather ? 0.f : sm.plan.by_list ? cut0 : -kNoLogit;  // places from there on are not kept, or not yet
+        write_bits(s, out, [&](float z, int) { return z >= from && (end == -kNoLogit || sample_place(z, top, scale) < end); });
+    }
+    return true;
+}
+
+// The lists' tokens in order, and so the cut and the token: by the row's first CTA alone.  `upto`: room for running sums.  False:
+// a border is not where the histogram had it, which its bounds rule out.
+__device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, uint64_t *upto, int ranks, float edge, int top_k, float top_p,
+                                            float u, uint32_t *out) {
+    const bool gather = sm.plan.gather, by_list = sm.plan.by_list;
+    const int bits = sm.plan.bits, cut_count = sm.plan.cut_count;
+    int listed = min(sm.listed[0], gather ? kSampleList : kSampleList / 2);
+    const int cut_listed = min(sm.listed[1], kSampleList / 2);
+    sort_entries(lists, listed, cut_listed);
+    uint64_t all = 0, before_cut = 0, before_draw = 0, mass;
+    int kept = 0;
+    bool good = true;
+    if (!gather) {
+        for (int q = 0; q < ranks; ++q) {
+            all += sm.part[q][0];
+            before_cut += sm.part[q][1];
+            before_draw += sm.part[q][2];
+            kept += sm.part_count[q];
         }
-        const double target = u * mass;
-        const int place = list.find(n, sm.first, [&](int, double before, double w, uint64_t) { return base + before + w > target; });
-        if (place == kSampleList || base > target) res.slow = 1;
-#pragma unroll
-        for (int i = 0; i < kSamplePer; ++i)
-            if (i < list.per && list.first + i == place) {
-                res.token = static_cast<int>(list.entry[i] & 0xFFFFFFFFu);
-                res.prob = list.w[i] / mass;
-                sm.result = res;
+    }
+    mass = all;
+    if (gather || by_list) {
+        const uint64_t *list = gather ? lists : lists + kSampleList / 2;
+        const int n = gather ? min(listed, top_k) : cut_listed;
+        const uint64_t sum = add_up(list, n, upto, bits, sm);
+        const uint64_t target = top_p < 1.f ? times_fraction(gather ? sum : all, fmaxf(top_p, 0.f), true) : ~0ull;
+        const SampleHit end = find_entry(list, upto, n, before_cut, target, false, cut_count == 0, edge, sm);
+        if (by_list) {
+            // the border is here if the first token is before it and the last one is not (or the row's last)
+            if (cut_count && before_cut >= target) good = false;
+            if (end.at == n && cut_count + n < kept && before_cut + sum < target) good = false;
+        }
+        kept = cut_count + end.at;
+        mass = before_cut + end.before;
+        if (out)
+            for (int i = threadIdx.x; i < end.at; i += kSampleThreads) {
+                const int v = static_cast<int>(list[i] & 0xFFFFFFFFu);
+                atomicOr(&out[v >> 5], 1u << (v & 31));
             }
-        if (res.slow && threadIdx.x == 0) sm.result = res;
+        if (gather) listed = end.at;
+    }
+    if (!gather) {
         __syncthreads();
+        add_up(lists, listed, upto, bits, sm);
     }
-    row_sync(ranks);
-    if (rank != 0) {
-        if (threadIdx.x < sizeof(SampleResult) / 4)
-            reinterpret_cast<uint32_t *>(&sm.result)[threadIdx.x] = ld_cluster_u32(peer(reinterpret_cast<uint32_t *>(&sm.result) + threadIdx.x, 0));
-    }
-    row_sync(ranks);
-    return !sm.result.slow;
+    const uint64_t target = times_fraction(mass, u, false);
+    const SampleHit hit = find_entry(lists, upto, listed, before_draw, target, true, false, edge, sm);
+    if (hit.at == listed || before_draw > target) good = false;
+    if (threadIdx.x == 0) sm.result = {!good, {}, static_cast<int>(hit.entry & 0xFFFFFFFFu), kept, quotient(hit.w, mass)};
+    __syncthreads();
+    return good;
 }
 
 // ------------------------------------------------------------------------------ the kernel
@@ -1011,14 +1100,26 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     const int ranks = static_cast<int>(cluster_nctarank()), rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
     const long long r = blockIdx.x / ranks;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t *hist = reinterpret_cast<uint32_t *>(buffer + p.list_at);
+    uint8_t *own = buffer + p.list_at + kSampleList * 8;  // this CTA's bins of the row: counts and sums
+    static_assert(kSampleBins * 4 <= kSampleList * 8 && sizeof(SampleShared::Scratch) <= kSampleList * 8, "lists take their place");
     pdl_trigger();
-    if (threadIdx.x == 0) sm.x = reinterpret_cast<SampleShared::Scratch *>(buffer + p.list_at);
-    for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) sm.table[i] = g_sample_table.v[i];
+    for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) {
+        sm.table.v[i] = g_sample_table.v[i];
+        sm.table.rest[i] = g_sample_table.rest[i];
+    }
+    for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 0) {
+        sm.x = reinterpret_cast<SampleShared::Scratch *>(hist);
+        sm.binned = sm.tail = 0;
+        sm.listed[0] = sm.listed[1] = 0;
+    }
     pdl_wait();
     const Slice<T, kResident> s(p, r, rank, buffer);
     const float T_row = p.a.temperature ? p.a.temperature[r] : 1.f, u = p.a.uniform ? p.a.uniform[r] : 0.f;
     const float top_p = p.a.top_p ? p.a.top_p[r] : 1.f, min_p = p.a.min_p ? p.a.min_p[r] : 0.f;
     const int top_k = p.a.top_k ? p.a.top_k[r] : 0;
+    uint32_t *out = p.a.out_allowed ? reinterpret_cast<uint32_t *>(p.a.out_allowed) + r * p.words : nullptr;
     if (threadIdx.x == 0) {  // (on its way while the others load)
         const float T_used = clamp_temperature(T_row);
         sm.w.set_temperature(T_used);
@@ -1035,74 +1136,71 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         sm.range[0][warp] = range.top;
         sm.range[1][warp] = range.bad ? kNoLogit : range.low;  // a smallest logit of -infinity says so
     }
-    __syncthreads();
+    row_sync(ranks);
     float top = kNoLogit, low = -kNoLogit;
-    for (int w = 0; w < kSampleWarps; ++w) {
-        top = fmaxf(top, sm.range[0][w]);
-        low = fminf(low, sm.range[1][w]);
+    for (int i = lane; i < ranks * kSampleWarps; i += 32) {
+        top = fmaxf(top, __uint_as_float(ld_cluster_u32(peer(&sm.range[0][i % kSampleWarps], i / kSampleWarps))));
+        low = fminf(low, __uint_as_float(ld_cluster_u32(peer(&sm.range[1][i % kSampleWarps], i / kSampleWarps))));
     }
-    if (ranks > 1) {
-        if (threadIdx.x == 0) {
-            sm.top = top;
-            sm.low = low;
-        }
-        cluster_sync();
-        for (int q = 0; q < ranks; ++q) {
-            top = fmaxf(top, __uint_as_float(ld_cluster_u32(peer(&sm.top, q))));
-            low = fminf(low, __uint_as_float(ld_cluster_u32(peer(&sm.low, q))));
-        }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
     }
     const bool ok = low != kNoLogit && top != kNoLogit && T_row >= 0.f && (T_row == 0.f || (p.a.uniform && u >= 0.f && u < 1.f)) &&
                     top_p == top_p && min_p <= 1.f;
-    SampleCut all{0u, 0x7FFFFFFF}, cut = all, token{0u, -1};
-    int kept = 0;
-    double prob = 0;
-    if (ok && T_row == 0.f) {
+    bool done = false;  // the mask is written
+    SampleCut cut{0xFFFFFFFFu, -1};  // nothing
+    if (!ok) {
+        if (threadIdx.x == 0) sm.result = {0, cut, -1, 0, 0.f};
+    } else if (T_row == 0.f) {
         // the largest logit, and of several the first
-        cut = {order_key(top), 0x7FFFFFFF};
         if (threadIdx.x == 0) sm.tie = 0x7FFFFFFF;
         row_sync(ranks);
+        cut = {order_key(top), 0x7FFFFFFF};
         s.each([&](float z, int v) {
             if (order_key(z) == cut.key) atomicMin(&sm.tie, v);
         });
         row_sync(ranks);
         for (int q = 0; q < ranks; ++q) cut.last = min(cut.last, static_cast<int>(ld_cluster_u32(peer(&sm.tie, q))));
-        token = cut;
-        kept = 1;
-        prob = 1;
-        row_sync(ranks);
-    } else if (ok) {
+        if (threadIdx.x == 0) sm.result = {0, cut, cut.last, 1, 1.f};
+    } else {
         if (threadIdx.x == 0) sm.w.set_top(top);
+        __syncthreads();
         const float edge = min_p > 0.f ? __double2float_ru(top + sm.min_log) : kNoLogit;
-        if (!sample_quickly(s, sm, p, buffer, ranks, rank, top, low, edge, top_k, top_p, u)) {
+        if (list_borders(s, sm, hist, own, ranks, rank, top, low, edge, top_k, top_p, u, out)) {
+            // the rest is the first CTA's; the others' shared memory is not read any more
+            if (ranks > 1) {
+                cluster_arrive();
+                if (rank != 0) return;
+                cluster_wait();
+            } else {
+                __syncthreads();
+            }
+            done = solve_lists(sm, reinterpret_cast<uint64_t *>(hist), reinterpret_cast<uint64_t *>(buffer + p.upto_at), ranks, edge, top_k, top_p, u, out);
+            if (!done) {
+                SampleParams whole = p;
+                whole.slice = p.words * 32;
+                const Slice<T, false> row(whole, r, 0, buffer);
+                sample_slowly(row, sm, 1, 0, p.sum_bits, top, edge, top_k, top_p, u);
+                cut = sm.result.cut;
+                if (out) write_bits(row, out, [&](float z, int v) { return cut.keeps(order_key(z), v); });
+                done = true;
+            }
+        } else {
             sample_slowly(s, sm, ranks, rank, p.sum_bits, top, edge, top_k, top_p, u);
+            cut = sm.result.cut;
         }
-        cut = sm.result.cut;
-        token = {0u, sm.result.token};
-        kept = sm.result.kept;
-        prob = sm.result.prob;
     }
     if (rank == 0 && threadIdx.x == 0) {
-        p.a.out_token[r] = ok ? token.last : -1;
+        const SampleResult res = sm.result;
+        p.a.out_token[r] = res.token;
         p.a.out_status[r] = ok ? RPD_OK : RPD_ERR_INVALID_ARGUMENT;
-        if (p.a.out_kept) p.a.out_kept[r] = kept;
-        if (p.a.out_prob) p.a.out_prob[r] = static_cast<float>(prob);
+        if (p.a.out_kept) p.a.out_kept[r] = res.kept;
+        if (p.a.out_prob) p.a.out_prob[r] = res.prob;
     }
-    if (p.a.out_allowed) {
-        // 32 tokens a warp and word; a lane keeps one of 32 words, so that they are stored together
-        uint32_t *out = reinterpret_cast<uint32_t *>(p.a.out_allowed) + r * p.words + s.v0 / 32;
-        const int words = (s.row.V + 31) / 32;
-        for (int w0 = warp * 32; w0 < words; w0 += kSampleThreads) {
-            uint32_t mine = 0;
-            for (int i = 0; i < 32; ++i) {
-                const int j = (w0 + i) * 32 + lane;
-                const float z = j < s.row.V ? s.at(j) : kNoLogit;
-                const uint32_t word = __ballot_sync(0xffffffffu, ok && z >= kLowest && cut.keeps(order_key(z), s.v0 + j));
-                if (i == lane) mine = word;
-            }
-            if (w0 + lane < words) out[w0 + lane] = mine;
-        }
-    }
+    if (done) return;
+    if (out) write_bits(s, out, [&](float z, int v) { return cut.keeps(order_key(z), v); });
     if (ranks > 1) cluster_sync();  // shared memory is read by the others until here
 }
 
@@ -1121,14 +1219,13 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t s) {
     const auto slice_of = [&](int n) { return ((p.words + n - 1) / n) * 32; };
     while (ranks < kSampleMaxCluster && slice_of(ranks) * static_cast<long long>(sizeof(T)) > 64 * 1024) ranks *= 2;
     p.slice = slice_of(ranks);
-    const long long lists = kSampleList * 8 + std::max(kSampleList * 8, kSampleBins / ranks * 8);
     const long long slice_bytes = (p.slice * static_cast<long long>(sizeof(T)) + 47) / 16 * 16;
-    const bool resident = slice_bytes + lists <= kSampleSmem;
+    const int own_bytes = kSampleBins / ranks * 8;
+    const bool resident = slice_bytes + kSampleList * 16 <= kSampleSmem;
     p.list_at = resident ? static_cast<int>(slice_bytes) : 0;
-    const long long bytes = p.list_at + lists;
-    int per = 0;  // tokens of a thread
-    while (kSampleThreads * static_cast<long long>(1 << per) < p.slice + 2 * kSampleThreads * 16) ++per;
-    p.thread_bits = std::min(54, 63 - per);
+    // running sums lie where the slice was, or where this CTA's bins were
+    p.upto_at = p.list_at >= kSampleList * 8 ? 0 : p.list_at + kSampleList * 8;
+    const long long bytes = p.list_at + kSampleList * 8 + (p.upto_at ? std::max(own_bytes, kSampleList * 8) : own_bytes);
     void (*kernel)(const SampleParams) = resident ? k_sample_limits<T, true> : k_sample_limits<T, false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
     if (e != cudaSuccess) return e;
