@@ -70,6 +70,10 @@ __device__ __forceinline__ uint32_t order_key(float z) {  // of floats, -0 as 0
     const uint32_t b = __float_as_uint(z + 0.f);
     return b ^ (static_cast<uint32_t>(static_cast<int>(b) >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float before_float(float z) {  // the next smaller one
+    const uint32_t k = __float_as_uint(z + 0.f);
+    return __uint_as_float(k == 0 ? 0x80000001u : k & 0x80000000u ? k + 1 : k - 1);
+}
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
 // ------------------------------------------------------------------------------ a CTA's part of a row
@@ -153,18 +157,32 @@ struct Slice {
 };
 static_assert(kSampleThreads >= 2 * 8, "tokens outside vectors are a thread's each");
 
-// Largest and smallest logit of the slice, and whether one is NaN or +infinity.  A resident slice is copied on the way.
+// Of a thread's part of a slice: largest and smallest logit, whether one is NaN or +infinity, the number of finite ones, and
+// about the sum of the weights relative to the largest (free of charge: the row is on its way from HBM meanwhile).
 struct SampleRange {
-    float top = kNoLogit, low = -kNoLogit;
+    float top = kLowest, low = -kNoLogit, sum = 0.f;
+    int count = 0;
     bool bad = false;
-    __device__ __forceinline__ void add(float z) {
-        bad |= !(z < -kNoLogit);
-        top = fmaxf(top, z);
-        low = fminf(low, z < kLowest ? -kNoLogit : z);
+    template <int n>
+    __device__ __forceinline__ void add(const float (&z)[n], float c) {
+        float most = top;
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+            bad |= !(z[k] < -kNoLogit);
+            most = fmaxf(most, z[k]);
+            low = fminf(low, z[k] < kLowest ? -kNoLogit : z[k]);
+            count += z[k] >= kLowest;
+        }
+        if (most > top) {
+            sum *= ex2((top - most) * c);
+            top = most;
+        }
+#pragma unroll
+        for (int k = 0; k < n; ++k) sum += ex2((z[k] - top) * c);
     }
 };
 template <typename T, bool kResident>
-__device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s) {
+__device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s, float c) {
     constexpr int N = Row<T>::kVec, kUnroll = 4;
     SampleRange r;
     for (int i = threadIdx.x; i < s.row.vecs; i += kSampleThreads * kUnroll) {
@@ -180,20 +198,19 @@ __device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s) 
                 if (kResident) *reinterpret_cast<uint4 *>(s.buf + (s.row.peel + at * N) * sizeof(T)) = raw[u];
                 float z[N];
                 unpack(raw[u], z, T());
-#pragma unroll
-                for (int k = 0; k < N; ++k) r.add(z[k]);
+                r.add(z, c);
             }
         }
     }
     if (static_cast<int>(threadIdx.x) < s.loose()) {
         const int j = s.loose_at(threadIdx.x);
-        const float z = s.global_at(j);
+        const float z[1] = {s.global_at(j)};
         if (kResident) {
             const uint32_t none = no_logit_pair(T());
             T *to = reinterpret_cast<T *>(s.buf) + j;
-            *to = z == kNoLogit ? *reinterpret_cast<const T *>(&none) : s.row.p[j];
+            *to = z[0] == kNoLogit ? *reinterpret_cast<const T *>(&none) : s.row.p[j];
         }
-        r.add(z);
+        r.add(z, c);
     }
     return r;
 }
@@ -240,7 +257,7 @@ struct SampleWeights {
     __device__ void set_big(float sum) { big = top - (10.f - log2f(sum)) / c; }
     __device__ __forceinline__ uint64_t of(float z, int bits, const uint32_t *table) const {
         float r;
-        const int k = split(fmaxf(z, floor) - A, r) - k_top;
+        const int k = split(z - A, r) - k_top;
         r = __fsub_rn(r, rest_top);
         // r ln 2 + r^2 ln^2 2 / 2 + r^3 ln^3 2 / 6 in units of 2^-31, to the nearest
         float q = fmaf(r, 1.1919417e8f, 5.158825e8f);
@@ -248,7 +265,7 @@ struct SampleWeights {
         q = fmaf(r, q, 12582912.f);
         const uint32_t one_q = static_cast<uint32_t>(__float_as_int(q)) + (0x80000000u - 0x4B400000u);
         const uint64_t m = static_cast<uint64_t>(table[k & (kSampleTable - 1)]) * one_q;  // 2^62 to 2^63
-        return m >> (62 - bits - (k >> 9));
+        return m >> ((62 - bits - (k >> 9)) & 63);
     }
     // The rest of y in units of 2^-52: the product's and its error.
     __device__ __forceinline__ int64_t rest64(float d, int &k) const {
@@ -270,7 +287,7 @@ struct SampleWeights {
         const int down = 52 - bits - (k >> 9);
         return down > 0 ? (m >> (down - 1)) + 1 >> 1 : m << -down;
     }
-    // With the big ones in 64 bits; 0 at the floor.
+    // (Above: with logits above the floor.)  With the big ones in 64 bits; 0 at the floor.
     __device__ __forceinline__ uint64_t exact_of(float z, int bits, const SampleTable &table) const {
         if (z >= big) return in_64_bits(z, bits, &table);
         return z > floor ? of(z, bits, table.v) : 0ull;
@@ -325,9 +342,8 @@ struct SampleShared {
         float scan[kSampleThreads + 1];
         int scan_count[kSampleThreads + 1];
     } *x;
-    float range[2][kSampleWarps];
-    float top, low;            // the slice's, then the row's
-    int bad;
+    float range[4][kSampleWarps];  // largest, smallest, sum, least of the threads' largest
+    int finite[kSampleWarps];
     float sums[kSampleWarps];
     float sum;
     int counts[kSampleWarps];
@@ -338,7 +354,7 @@ struct SampleShared {
     int tie;                   // the token of a tie that the border falls on
     double min_log;            // T log(min_p): min-p keeps logits from so far below the largest on
     // the quick way
-    int binned, tail;          // a slice's tokens in the bins, and below them
+    int binned;                // a slice's tokens in the bins
     SampleFound found[4];
     SamplePlan plan;
     SampleResult result;
@@ -788,8 +804,8 @@ struct SampleBins {
 
 // Which bins the borders are in, by the running counts and sums of bins: the first CTA of the row.  Sums are kBinError off
 // at most, so that a border may be in either of two bins, or more.
-__device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const uint8_t *own, float top, float edge, float scale, int top_k,
-                                             float top_p, float u) {
+__device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const uint8_t *own, float top, float edge, float scale, float sum, int finite,
+                                             int top_k, float top_p, float u) {
     constexpr int kPer = SampleBins::kPer;
     SampleBins bins;
     const int per_rank = kSampleBins / ranks, first = threadIdx.x * kPer;
@@ -835,23 +851,18 @@ __device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const 
     sm.x->scan[threadIdx.x + 1] = e_upto;
     __syncthreads();
     const int binned = sm.x->scan_count[kSampleThreads];
-    const float sum = sm.x->scan[kSampleThreads], error = kBinError * sum;
-    int expected = 0, tail = 0;
-    if (lane < ranks) {
-        expected = static_cast<int>(ld_cluster_u32(peer(&sm.binned, lane)));
-        tail = static_cast<int>(ld_cluster_u32(peer(&sm.tail, lane)));
-    }
-    expected = __reduce_add_sync(0xffffffffu, expected);
-    tail = __reduce_add_sync(0xffffffffu, tail);
+    sum = fmaxf(sum, 1.f);
+    const float error = kBinError * sum;
+    const int expected = __reduce_add_sync(0xffffffffu, lane < ranks ? static_cast<int>(ld_cluster_u32(peer(&sm.binned, lane))) : 0);
     SamplePlan plan{};
     plan.scale = scale;
-    plan.sum = fmaxf(sum, 1.f);
-    plan.bits = min(54, 60 - ilogbf(plan.sum));
+    plan.sum = sum;
+    plan.bits = min(54, 59 - ilogbf(plan.sum));
     plan.cut0 = plan.cut1 = -1.f;
     plan.slow = binned != expected;  // a bin had more tokens than it can count
     constexpr float kEnd = static_cast<float>(kSampleBins) * kBinParts;
     const auto place_of = [](int bin) { return static_cast<float>(bin) * kBinParts; };
-    if (top_k > 0 && top_k < binned + tail) {
+    if (top_k > 0) {
         bins.find(sm, sm.found[0], true, static_cast<float>(top_k), false);
         __syncthreads();
         plan.gather = 1;
@@ -922,29 +933,25 @@ __device__ __noinline__ void list_token(uint32_t listed, uint32_t list, int room
 // the cut's bins excepted.
 template <typename S>
 __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint32_t *hist, uint8_t *own, int ranks, int rank, float top,
-                                             float low, float edge, int top_k, float top_p, float u, uint32_t *out) {
+                                             float low, float least, float sum, int finite, float edge, int top_k, float top_p, float u,
+                                             uint32_t *out) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float c = sm.w.c;
-    const float span = fminf(fminf(kBinOctaves / c, top - low), 3e38f);
+    const float span = fminf(fminf(kBinOctaves / c, top - fmaxf(low, least)), 3e38f);
     const float scale = span > 0.f ? fminf((kSampleBins * kBinParts - kBinParts / 2) / span, 1e38f) : 0.f;
-    int binned = 0, tail = 0;
+    int binned = 0;
+    least = fmaxf(least, kLowest);
     s.each([&](float z, int) {
-        if (z >= kLowest) {
+        if (z >= least) {
             const int at = static_cast<int>(sample_place(z, top, scale));
             if (at < kSampleBins * kBinParts) {
                 atomicAdd(&hist[at / kBinParts], (1u << 20) | (at % kBinParts));  // 4095 tokens fit
                 ++binned;
-            } else {
-                ++tail;
             }
         }
     });
     binned = __reduce_add_sync(0xffffffffu, binned);
-    tail = __reduce_add_sync(0xffffffffu, tail);
-    if (lane == 0) {
-        atomicAdd(&sm.binned, binned);
-        atomicAdd(&sm.tail, tail);
-    }
+    if (lane == 0) atomicAdd(&sm.binned, binned);
     row_sync(ranks);
     // the slices' histograms become the row's, a part of the bins a CTA
     const int per_rank = kSampleBins / ranks;
@@ -964,7 +971,7 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
         reinterpret_cast<uint2 *>(own)[i] = make_uint2(n, __float_as_uint(sum));
     }
     row_sync(ranks);
-    if (rank == 0) plan_borders(sm, ranks, own, top, edge, scale, top_k, top_p, u);
+    if (rank == 0) plan_borders(sm, ranks, own, top, edge, scale, sum, finite, top_k, top_p, u);
     row_sync(ranks);
     if (rank != 0) {
         if (threadIdx.x < sizeof(SamplePlan) / 4)
@@ -991,22 +998,24 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
         const SampleWeights w = sm.w;
         const int bits = sm.plan.bits;
         uint64_t sums[3] = {0, 0, 0};
+        const bool by_edge = sm.plan.by_edge;
         int count = 0;
+        const float last = fmaxf(cut1, draw1), weighs = by_edge ? fmaxf(w.floor, before_float(edge)) : w.floor;
         s.each([&](float z, int v) {
-            if (z >= from) {
-                ++count;
-                const uint64_t m = z >= w.big ? sm.w.in_64_bits(z, bits, &sm.table) : z > w.floor ? w.of(z, bits, sm.table.v) : 0ull;
-                const float at = sample_place(z, top, scale);
-                sums[0] += m;
-                sums[1] += at < cut0 ? m : 0;
-                sums[2] += at < draw0 ? m : 0;
-                if (at < fmaxf(cut1, draw1)) {
-                    if (at >= cut0 && at < cut1) list_token(listed + 4, lists + kSampleList * 4, kSampleList / 2, z, v);
-                    if (at >= draw0 && at < draw1) list_token(listed, lists, kSampleList / 2, z, v);
-                }
+            uint64_t m = w.of(z, bits, sm.table.v);  // (of a logit that does not count: anything)
+            if (z >= w.big) m = sm.w.in_64_bits(z, bits, &sm.table);
+            m = z > weighs ? m : 0ull;
+            sums[0] += m;
+            const float at = sample_place(z, top, scale);
+            if (at < last) {
+                if (at < cut0) sums[1] += m;
+                if (at < draw0) sums[2] += m;
+                if (at >= cut0 && at < cut1) list_token(listed + 4, lists + kSampleList * 4, kSampleList / 2, z, v);
+                if (at >= draw0 && at < draw1 && z >= from) list_token(listed, lists, kSampleList / 2, z, v);
             }
+            if (by_edge) count += z >= edge;
         });
-        count = __reduce_add_sync(0xffffffffu, count);
+        if (by_edge) count = __reduce_add_sync(0xffffffffu, count);
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
 #pragma unroll
@@ -1038,7 +1047,7 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
 
 // The lists' tokens in order, and so the cut and the token: by the row's first CTA alone.  `upto`: room for running sums.  False:
 // a border is not where the histogram had it, which its bounds rule out.
-__device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, uint64_t *upto, int ranks, float edge, int top_k, float top_p,
+__device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, uint64_t *upto, int ranks, int finite, float edge, int top_k, float top_p,
                                             float u, uint32_t *out) {
     const bool gather = sm.plan.gather, by_list = sm.plan.by_list;
     const int bits = sm.plan.bits, cut_count = sm.plan.cut_count;
@@ -1047,7 +1056,7 @@ __device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, u
     sort_entries(lists, listed, cut_listed);
     uint64_t all = 0, before_cut = 0, before_draw = 0, mass;
     int kept = 0;
-    bool good = true;
+    bool good = sm.listed[0] == listed && sm.listed[1] == cut_listed;
     if (!gather) {
         for (int q = 0; q < ranks; ++q) {
             all += sm.part[q][0];
@@ -1055,6 +1064,7 @@ __device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, u
             before_draw += sm.part[q][2];
             kept += sm.part_count[q];
         }
+        if (!sm.plan.by_edge) kept = finite;
     }
     mass = all;
     if (gather || by_list) {
@@ -1111,7 +1121,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) {
         sm.x = reinterpret_cast<SampleShared::Scratch *>(hist);
-        sm.binned = sm.tail = 0;
+        sm.binned = 0;
         sm.listed[0] = sm.listed[1] = 0;
     }
     pdl_wait();
@@ -1120,34 +1130,66 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     const float top_p = p.a.top_p ? p.a.top_p[r] : 1.f, min_p = p.a.min_p ? p.a.min_p[r] : 0.f;
     const int top_k = p.a.top_k ? p.a.top_k[r] : 0;
     uint32_t *out = p.a.out_allowed ? reinterpret_cast<uint32_t *>(p.a.out_allowed) + r * p.words : nullptr;
-    if (threadIdx.x == 0) {  // (on its way while the others load)
-        const float T_used = clamp_temperature(T_row);
+    const float T_used = clamp_temperature(T_row), c = 1.44269502f / T_used;
+    if (threadIdx.x == 0) {
         sm.w.set_temperature(T_used);
-        sm.min_log = min_p > 0.f ? T_used * log(static_cast<double>(min_p)) : 0.0;
+        sm.min_log = min_p > 0.f ? T_used * log(static_cast<double>(min_p)) : 0.0;  // (on its way while the others load)
     }
-    SampleRange range = load_slice(s);
+    SampleRange range = load_slice(s, c);
+    float top = range.top, low = range.bad ? kNoLogit : range.low;  // a smallest logit of -infinity says so
+    float least_top = top;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        range.top = fmaxf(range.top, __shfl_xor_sync(0xffffffffu, range.top, o));
-        range.low = fminf(range.low, __shfl_xor_sync(0xffffffffu, range.low, o));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+        least_top = fminf(least_top, __shfl_xor_sync(0xffffffffu, least_top, o));
     }
-    range.bad = __any_sync(0xffffffffu, range.bad);
+    float sum = range.sum * ex2((range.top - top) * c);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    int finite = __reduce_add_sync(0xffffffffu, range.count);
     if (lane == 0) {
-        sm.range[0][warp] = range.top;
-        sm.range[1][warp] = range.bad ? kNoLogit : range.low;  // a smallest logit of -infinity says so
+        sm.range[0][warp] = top;
+        sm.range[1][warp] = low;
+        sm.range[2][warp] = sum;
+        sm.range[3][warp] = least_top;
+        sm.finite[warp] = finite;
     }
     row_sync(ranks);
-    float top = kNoLogit, low = -kNoLogit;
-    for (int i = lane; i < ranks * kSampleWarps; i += 32) {
-        top = fmaxf(top, __uint_as_float(ld_cluster_u32(peer(&sm.range[0][i % kSampleWarps], i / kSampleWarps))));
-        low = fminf(low, __uint_as_float(ld_cluster_u32(peer(&sm.range[1][i % kSampleWarps], i / kSampleWarps))));
+    float tops[kSampleMaxCluster / 2], sums[kSampleMaxCluster / 2], least_warp = -kNoLogit;
+    top = kLowest;
+    low = least_top = -kNoLogit;
+    finite = 0;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSampleMaxCluster / 2; ++i) {  // two CTAs' warps at a time
+        const int q = 2 * i + lane / kSampleWarps, w = lane % kSampleWarps;
+        tops[i] = kLowest;
+        sums[i] = 0.f;
+        if (q < ranks) {
+            tops[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[0][w], q)));
+            sums[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[2][w], q)));
+            low = fminf(low, __uint_as_float(ld_cluster_u32(peer(&sm.range[1][w], q))));
+            least_top = fminf(least_top, __uint_as_float(ld_cluster_u32(peer(&sm.range[3][w], q))));
+            finite += static_cast<int>(ld_cluster_u32(peer(&sm.finite[w], q)));
+            least_warp = fminf(least_warp, tops[i]);
+        }
+        top = fmaxf(top, tops[i]);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+        least_top = fminf(least_top, __shfl_xor_sync(0xffffffffu, least_top, o));
+        least_warp = fminf(least_warp, __shfl_xor_sync(0xffffffffu, least_warp, o));
     }
-    const bool ok = low != kNoLogit && top != kNoLogit && T_row >= 0.f && (T_row == 0.f || (p.a.uniform && u >= 0.f && u < 1.f)) &&
+#pragma unroll
+    for (int i = 0; i < kSampleMaxCluster / 2; ++i) sum += sums[i] * ex2((tops[i] - top) * c);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    finite = __reduce_add_sync(0xffffffffu, finite);
+    static_assert(kSampleWarps == 16, "two CTAs' warps are a warp's lanes");
+    const bool ok = low != kNoLogit && finite > 0 && T_row >= 0.f && (T_row == 0.f || (p.a.uniform && u >= 0.f && u < 1.f)) &&
                     top_p == top_p && min_p <= 1.f;
     bool done = false;  // the mask is written
     SampleCut cut{0xFFFFFFFFu, -1};  // nothing
@@ -1168,7 +1210,24 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         if (threadIdx.x == 0) sm.w.set_top(top);
         __syncthreads();
         const float edge = min_p > 0.f ? __double2float_ru(top + sm.min_log) : kNoLogit;
-        if (list_borders(s, sm, hist, own, ranks, rank, top, low, edge, top_k, top_p, u, out)) {
+        // Logits that no border can be at.  Top-k: a warp's (or a thread's) largest logit is one of the row's, so that the least of
+        // so many of them is not above the k-th.  Top-p, or the draw where there is no limit: what follows a border holds
+        // 1 - q of the sum in V tokens at most, and none of these weighs more than the border's.  (2^-12 for the bins' error.)
+        float least = kLowest;
+        const bool by_k = top_k > 0 && top_k < finite;
+        if (by_k) {
+            if (top_k <= ranks * kSampleWarps)
+                least = least_warp;
+            else if (top_k <= ranks * kSampleThreads)
+                least = least_top;
+        } else {
+            const float q = top_p < 1.f ? fmaxf(top_p, 0.f) : u, rest = (1.f - q - 0x1p-12f) * sum / static_cast<float>(p.a.V);
+            if (edge != kNoLogit && top_p >= 1.f)
+                least = edge;
+            else if (rest > 0.f)
+                least = fmaxf(edge, top + __fdividef(log2f(rest) - 0x1p-6f, c));
+        }
+        if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out)) {
             // the rest is the first CTA's; the others' shared memory is not read any more
             if (ranks > 1) {
                 cluster_arrive();
@@ -1177,7 +1236,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
             } else {
                 __syncthreads();
             }
-            done = solve_lists(sm, reinterpret_cast<uint64_t *>(hist), reinterpret_cast<uint64_t *>(buffer + p.upto_at), ranks, edge, top_k, top_p, u, out);
+            done = solve_lists(sm, reinterpret_cast<uint64_t *>(hist), reinterpret_cast<uint64_t *>(buffer + p.upto_at), ranks, finite, edge, top_k, top_p, u, out);
             if (!done) {
                 SampleParams whole = p;
                 whole.slice = p.words * 32;
