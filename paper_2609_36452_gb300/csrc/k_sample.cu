@@ -70,10 +70,6 @@ __device__ __forceinline__ uint32_t order_key(float z) {  // of floats, -0 as 0
     const uint32_t b = __float_as_uint(z + 0.f);
     return b ^ (static_cast<uint32_t>(static_cast<int>(b) >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float before_float(float z) {  // the next smaller one
-    const uint32_t k = __float_as_uint(z + 0.f);
-    return __uint_as_float(k == 0 ? 0x80000001u : k & 0x80000000u ? k + 1 : k - 1);
-}
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
 // ------------------------------------------------------------------------------ a CTA's part of a row
@@ -128,6 +124,37 @@ struct Slice {
     }
     __device__ __forceinline__ int loose() const { return row.V - row.vecs * N; }  // tokens outside vectors
     __device__ __forceinline__ int loose_at(int i) const { return i < row.peel ? i : i + row.vecs * N; }
+    // f(logits, first token, how many) for every vector, and every token outside of them (then other logits are -infinity).
+    template <typename F>
+    __device__ __forceinline__ void each_vec(F f) const {
+        constexpr int kAhead = kResident ? 1 : 3;  // vectors on their way from L2 meanwhile
+        const int pieces = row.vecs + loose();
+        uint4 raw[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int i = threadIdx.x + a * kSampleThreads;
+            if (!kResident && i < row.vecs) raw[a] = global_vec(i);
+        }
+#pragma unroll 1
+        for (int i = threadIdx.x; i < pieces; i += kSampleThreads) {
+            float z[N];
+            int first = row.peel + i * N;
+            if (i < row.vecs) {
+                unpack(kResident ? *reinterpret_cast<const uint4 *>(buf + first * sizeof(T)) : allowed_vec(raw[0], i), z, T());
+            } else {
+                first = loose_at(i - row.vecs);
+                z[0] = at(first);
+#pragma unroll
+                for (int k = 1; k < N; ++k) z[k] = kNoLogit;
+            }
+            if (!kResident) {
+#pragma unroll
+                for (int a = 0; a + 1 < kAhead; ++a) raw[a] = raw[a + 1];
+                if (i + kAhead * kSampleThreads < row.vecs) raw[kAhead - 1] = global_vec(i + kAhead * kSampleThreads);
+            }
+            f(z, v0 + first);
+        }
+    }
     // f(logit, token) for every token; threads interleave.  (Eight bytes of a resident slice at a time: bodies of f for a whole
     // vector are more code than the instruction caches hold, and every loop here runs some thirty times.)
     template <typename F>
@@ -157,26 +184,28 @@ struct Slice {
 };
 static_assert(kSampleThreads >= 2 * 8, "tokens outside vectors are a thread's each");
 
-// Of a thread's part of a slice: largest and smallest logit, whether one is NaN or +infinity, the number of finite ones, and
-// about the sum of the weights relative to the largest (free of charge: the row is on its way from HBM meanwhile).
+// Of a thread's part of a slice: largest and smallest logit, the number of those that are -infinity, and about the sum of
+// the weights relative to the largest (free of charge: the row is on its way from HBM meanwhile).  The sum is no number where a
+// logit is NaN or +infinity.
 struct SampleRange {
     float top = kLowest, low = -kNoLogit, sum = 0.f;
-    int count = 0;
-    bool bad = false;
+    int gone = 0;
     template <int n>
     __device__ __forceinline__ void add(const float (&z)[n], float c) {
-        float most = top;
+        float most = top, least = z[0];
 #pragma unroll
         for (int k = 0; k < n; ++k) {
-            bad |= !(z[k] < -kNoLogit);
             most = fmaxf(most, z[k]);
-            low = fminf(low, z[k] < kLowest ? -kNoLogit : z[k]);
-            count += z[k] >= kLowest;
+            least = fminf(least, z[k]);
         }
         if (most > top) {
             sum *= ex2((top - most) * c);
             top = most;
         }
+        if (least < kLowest)
+#pragma unroll
+            for (int k = 0; k < n; ++k) gone += z[k] < kLowest;
+        low = fminf(low, least);
 #pragma unroll
         for (int k = 0; k < n; ++k) sum += ex2((z[k] - top) * c);
     }
@@ -222,7 +251,7 @@ __device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s, 
 // 2^(whole part of k) table[k mod 512] (1 + r ln 2 + ...).  A = 0, or the largest logit where that times c leaves
 // the range of k: logits that count are then within a factor of two of it, and the difference is exact.
 struct SampleWeights {
-    float A, c_hi, c_lo, rest_top, floor, big;
+    float A, c_hi, c_lo, rest_top, least, big;
     int k_top;  // as the bits of the shifted product
     int64_t rest64_top;
     float c, top, temperature;
@@ -249,23 +278,39 @@ struct SampleWeights {
         rest64_top = rest64(top_logit - A, k_top);
         big = -kNoLogit;
     }
-    // Logits at and below `floor` weigh nothing: under 2^-bits.
+    // Logits so far below weigh nothing: under 2^-bits.
     __device__ void set_floor(int bits) {
-        floor = fmaxf(kLowest, __fsub_rd(top, __fdiv_ru(static_cast<float>(bits), c)));
+        least = (top - A) - (static_cast<float>(bits) + 0.5f) / c;
     }
     // Of a sum of about `sum` times the largest weight, those that hold 2^-10 and more.
     __device__ void set_big(float sum) { big = top - (10.f - log2f(sum)) / c; }
     __device__ __forceinline__ uint64_t of(float z, int bits, const uint32_t *table) const {
-        float r;
-        const int k = split(z - A, r) - k_top;
-        r = __fsub_rn(r, rest_top);
+        uint64_t m[2];
+        two_of(z, kNoLogit, bits, table, m);
+        return m[0];
+    }
+    // Two at a time.  A logit at the floor and below gets the weight 0: its difference is taken for one of bits + 1/2 octaves,
+    // and the shift leaves nothing.
+    __device__ __forceinline__ void two_of(float z0, float z1, int bits, const uint32_t *table, uint64_t (&m)[2]) const {
+        const f32x2 d = pack2(fmaxf(z0 - A, least), fmaxf(z1 - A, least)), c2 = pack2(c_hi, c_hi), shift = pack2(kShift, kShift);
+        const f32x2 minus = pack2(-1.f, -1.f);
+        const f32x2 y = mul2(d, c2), t = add2(y, shift);
+        // (y - (t - shift)) + (d c_lo + (d c_hi - y)) - rest_top
+        const f32x2 head = fma2(minus, add2(t, pack2(-kShift, -kShift)), y);
+        const f32x2 r = add2(add2(head, fma2(d, pack2(c_lo, c_lo), fma2(d, c2, mul2(minus, y)))), pack2(-rest_top, -rest_top));
         // r ln 2 + r^2 ln^2 2 / 2 + r^3 ln^3 2 / 6 in units of 2^-31, to the nearest
-        float q = fmaf(r, 1.1919417e8f, 5.158825e8f);
-        q = fmaf(r, q, 1.488522236e9f);
-        q = fmaf(r, q, 12582912.f);
-        const uint32_t one_q = static_cast<uint32_t>(__float_as_int(q)) + (0x80000000u - 0x4B400000u);
-        const uint64_t m = static_cast<uint64_t>(table[k & (kSampleTable - 1)]) * one_q;  // 2^62 to 2^63
-        return m >> ((62 - bits - (k >> 9)) & 63);
+        f32x2 q = fma2(r, pack2(1.1919417e8f, 1.1919417e8f), pack2(5.158825e8f, 5.158825e8f));
+        q = fma2(r, q, pack2(1.488522236e9f, 1.488522236e9f));
+        q = fma2(r, q, pack2(12582912.f, 12582912.f));
+        float tf[2], qf[2];
+        unpack2(t, tf[0], tf[1]);
+        unpack2(q, qf[0], qf[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int k = __float_as_int(tf[i]) - k_top;
+            const uint32_t one_q = static_cast<uint32_t>(__float_as_int(qf[i])) + (0x80000000u - 0x4B400000u);
+            m[i] = static_cast<uint64_t>(table[k & (kSampleTable - 1)]) * one_q >> ((62 - bits - (k >> 9)) & 63);  // of 2^62 to 2^63
+        }
     }
     // The rest of y in units of 2^-52: the product's and its error.
     __device__ __forceinline__ int64_t rest64(float d, int &k) const {
@@ -287,10 +332,10 @@ struct SampleWeights {
         const int down = 52 - bits - (k >> 9);
         return down > 0 ? (m >> (down - 1)) + 1 >> 1 : m << -down;
     }
-    // (Above: with logits above the floor.)  With the big ones in 64 bits; 0 at the floor.
+    // With the big ones in 64 bits.
     __device__ __forceinline__ uint64_t exact_of(float z, int bits, const SampleTable &table) const {
         if (z >= big) return in_64_bits(z, bits, &table);
-        return z > floor ? of(z, bits, table.v) : 0ull;
+        return of(z, bits, table.v);
     }
 };
 
@@ -315,7 +360,6 @@ struct SamplePlan {
     int by_list;            // top-p: the cut is in the bins from cut0 to cut1
     int by_edge;            // min-p: tokens from `edge` on are kept, and there is no other cut
     float draw0, draw1, cut0, cut1;  // places, in parts of bins
-    float scale;
     int cut_count;          // tokens before cut0
     float sum;              // about that of all weights
     int bits;               // units of sums: 2^-bits of the largest weight; all of them fit 62 bits
@@ -339,11 +383,9 @@ struct SampleShared {
     struct Scratch {
         uint64_t mass[256];
         uint32_t count[256];
-        float scan[kSampleThreads + 1];
-        int scan_count[kSampleThreads + 1];
     } *x;
     float range[4][kSampleWarps];  // largest, smallest, sum, least of the threads' largest
-    int finite[kSampleWarps];
+    int finite[kSampleWarps], binned[kSampleWarps];
     float sums[kSampleWarps];
     float sum;
     int counts[kSampleWarps];
@@ -354,12 +396,12 @@ struct SampleShared {
     int tie;                   // the token of a tie that the border falls on
     double min_log;            // T log(min_p): min-p keeps logits from so far below the largest on
     // the quick way
-    int binned;                // a slice's tokens in the bins
-    SampleFound found[4];
+    SampleFound found[5];
+    float edges[4];            // the smallest logits before the plan's places
+    int listed[2], list_at[2]; // entries of this CTA's lists, and where they go in the first one's
     SamplePlan plan;
     SampleResult result;
     // in the first CTA
-    int listed[2];             // entries of the lists
     uint64_t part[kSampleMaxCluster][3];  // of every CTA: weights of all that count, above the cut's bins, above the draw's
     int part_count[kSampleMaxCluster];
     uint64_t warp_sums[3][kSampleWarps];
@@ -566,21 +608,29 @@ __device__ __noinline__ double kept_mass(const S &s, SampleShared &sm, int ranks
     return static_cast<double>(m);
 }
 
-// The tokens that `keep` holds for as bits: 32 tokens a warp and word; a lane keeps one of 32 words, so that they are
+// The tokens that `keep` holds for (or none) as bits: 32 tokens a warp and word; a lane keeps one of 32 words, so that they are
 // stored together.
 template <typename S, typename F>
-__device__ __forceinline__ void write_bits(const S &s, uint32_t *out, F keep) {
+__device__ __forceinline__ void write_bits(const S &s, uint32_t *out, bool none, F keep) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, words = (s.row.V + 31) / 32;
     out += s.v0 / 32;
     for (int w0 = warp * 32; w0 < words; w0 += kSampleThreads) {
         uint32_t mine = 0;
-#pragma unroll 8
-        for (int i = 0; i < 32; ++i) {
-            const int j = (w0 + i) * 32 + lane;
-            const float z = j < s.row.V ? s.at(j) : kNoLogit;
-            const uint32_t word = __ballot_sync(0xffffffffu, z >= kLowest && keep(z, s.v0 + j));
-            if (i == lane) mine = word;
-        }
+        if (!none)
+#pragma unroll 1
+            for (int i = 0; i < 32; i += 8) {
+                float z[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {  // (asked for together: word by word the answers are waited for one by one)
+                    const int j = (w0 + i + k) * 32 + lane;
+                    z[k] = j < s.row.V ? s.at(j) : kNoLogit;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t word = __ballot_sync(0xffffffffu, keep(z[k], s.v0 + (w0 + i + k) * 32 + lane));
+                    if (i + k == lane) mine = word;
+                }
+            }
         if (w0 + lane < words) out[w0 + lane] = mine;
     }
 }
@@ -774,188 +824,58 @@ __device__ __forceinline__ SampleHit find_entry(const uint64_t *list, const uint
     return sm.hit;
 }
 
-// The first histogram's bins in the threads of the row's first CTA, eight neighbours each, with the running count and
-// sum before them.
+// A CTA's bins of the row's histogram: counts and sums of weights, kPer neighbours a thread; and the running ones before each
+// thread's, of the row.
 struct SampleBins {
-    static constexpr int kPer = kSampleBins / kSampleThreads;
-    int count[kPer];
-    float sum[kPer];
-    // The first bin up to whose end there are `least` tokens (by_count), or a sum of `least` or more (or of more); bin =
-    // kSampleBins if there is none.
-    __device__ __forceinline__ void find(SampleShared &sm, SampleFound &to, bool by_count, float least, bool more) const {
+    const uint2 *own;
+    int per, first;    // bins of a thread, and the first of this one's among the row's
+    int count0, count1, all_count;  // before and behind this thread's, and of the row
+    float sum0, sum1, all_sum;
+    // The first bin up to whose end there are `least` tokens (by_count), or a sum of `least` or more (or of more), in every CTA's
+    // found[slot]; what was there stays where there is none.
+    __device__ __forceinline__ void find(SampleShared &sm, int slot, int ranks, bool by_count, float least, bool more) const {
         const auto f = [&](int n, float m) { return by_count ? n >= static_cast<int>(least) : more ? m > least : m >= least; };
-        if (threadIdx.x == 0 && !f(sm.x->scan_count[kSampleThreads], sm.x->scan[kSampleThreads]))
-            to = {kSampleBins, sm.x->scan_count[kSampleThreads], sm.x->scan_count[kSampleThreads], sm.x->scan[kSampleThreads], sm.x->scan[kSampleThreads]};
-        const bool before = threadIdx.x && f(sm.x->scan_count[threadIdx.x], sm.x->scan[threadIdx.x]);
-        if (before || !f(sm.x->scan_count[threadIdx.x + 1], sm.x->scan[threadIdx.x + 1])) return;
-        int c = sm.x->scan_count[threadIdx.x];
-        float e = sm.x->scan[threadIdx.x];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (i == kPer - 1 || f(c + count[i], e + sum[i])) {
-                to = {static_cast<int>(threadIdx.x) * kPer + i, c, c + count[i], e, e + sum[i]};
-                return;
-            }
-            c += count[i];
-            e += sum[i];
+        if ((first && f(count0, sum0)) || !f(count1, sum1)) return;
+        int i = 0, n = count0, n1 = n;
+        float m = sum0, m1 = m;
+        for (;; ++i) {
+            const uint2 v = own[i];
+            n1 = n + static_cast<int>(v.x);
+            m1 = m + __uint_as_float(v.y);
+            if (i == per - 1 || f(n1, m1)) break;
+            n = n1;
+            m = m1;
+        }
+        tell(sm, slot, ranks, {first + i, n, n1, m, m1});
+    }
+    // The same for a bin that is known.
+    __device__ __forceinline__ void find_bin(SampleShared &sm, int slot, int ranks, int bin) const {
+        if (bin < first || bin >= first + per) return;
+        int n = count0;
+        float m = sum0;
+        for (int i = 0; i < bin - first; ++i) {
+            n += static_cast<int>(own[i].x);
+            m += __uint_as_float(own[i].y);
+        }
+        const uint2 v = own[bin - first];
+        tell(sm, slot, ranks, {bin, n, n + static_cast<int>(v.x), m, m + __uint_as_float(v.y)});
+    }
+    __device__ __forceinline__ void tell(SampleShared &sm, int slot, int ranks, const SampleFound &f) const {
+        for (int q = 0; q < ranks; ++q) {
+            const uint32_t to = peer(&sm.found[slot], q);
+            st_shared_cluster(to, f.bin);
+            st_shared_cluster(to + 4, f.count0);
+            st_shared_cluster(to + 8, f.count1);
+            st_shared_cluster(to + 12, __float_as_int(f.sum0));
+            st_shared_cluster(to + 16, __float_as_int(f.sum1));
         }
     }
 };
 
-// Which bins the borders are in, by the running counts and sums of bins: the first CTA of the row.  Sums are kBinError off
-// at most, so that a border may be in either of two bins, or more.
-__device__ __forceinline__ void plan_borders(SampleShared &sm, int ranks, const uint8_t *own, float top, float edge, float scale, float sum, int finite,
-                                             int top_k, float top_p, float u) {
-    constexpr int kPer = SampleBins::kPer;
-    SampleBins bins;
-    const int per_rank = kSampleBins / ranks, first = threadIdx.x * kPer;
-    int c = 0;
-    float e = 0.f;
-    const uint32_t from = mapa_shared(smem_u32(own + first % per_rank * 8), first / per_rank);
-    uint64_t v[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = ld_cluster_u64(from + i * 8);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        bins.count[i] = static_cast<int>(v[i]);
-        bins.sum[i] = __uint_as_float(static_cast<uint32_t>(v[i] >> 32));
-        c += bins.count[i];
-        e += bins.sum[i];
-    }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int c_upto = c;
-    float e_upto = e;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int cu = __shfl_up_sync(0xffffffffu, c_upto, o);
-        const float eu = __shfl_up_sync(0xffffffffu, e_upto, o);
-        if (lane >= o) {
-            c_upto += cu;
-            e_upto += eu;
-        }
-    }
-    if (lane == 31) {
-        sm.counts[warp] = c_upto;
-        sm.sums[warp] = e_upto;
-    }
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) {
-        c_upto += sm.counts[w];
-        e_upto += sm.sums[w];
-    }
-    if (threadIdx.x == 0) {
-        sm.x->scan_count[0] = 0;
-        sm.x->scan[0] = 0.f;
-    }
-    sm.x->scan_count[threadIdx.x + 1] = c_upto;
-    sm.x->scan[threadIdx.x + 1] = e_upto;
-    __syncthreads();
-    const int binned = sm.x->scan_count[kSampleThreads];
-    sum = fmaxf(sum, 1.f);
-    const float error = kBinError * sum;
-    const int expected = __reduce_add_sync(0xffffffffu, lane < ranks ? static_cast<int>(ld_cluster_u32(peer(&sm.binned, lane))) : 0);
-    SamplePlan plan{};
-    plan.scale = scale;
-    plan.sum = sum;
-    plan.bits = min(54, 59 - ilogbf(plan.sum));
-    plan.cut0 = plan.cut1 = -1.f;
-    plan.slow = binned != expected;  // a bin had more tokens than it can count
-    constexpr float kEnd = static_cast<float>(kSampleBins) * kBinParts;
-    const auto place_of = [](int bin) { return static_cast<float>(bin) * kBinParts; };
-    if (top_k > 0) {
-        bins.find(sm, sm.found[0], true, static_cast<float>(top_k), false);
-        __syncthreads();
-        plan.gather = 1;
-        plan.draw1 = place_of(sm.found[0].bin + 1);
-        plan.slow |= sm.found[0].bin == kSampleBins || sm.found[0].count1 > kSampleList;
-    } else {
-        float least = sum, most = sum;  // of the kept weights
-        int last = kSampleBins - 1;     // bin of a kept token
-        const float edge_place = edge == kNoLogit ? kEnd : fminf(sample_place(edge, top, scale), kEnd);
-        plan.by_edge = edge != kNoLogit;
-        if (top_p < 1.f) {
-            bins.find(sm, sm.found[0], false, top_p * sum - error, false);
-            bins.find(sm, sm.found[1], false, top_p * sum + error, false);
-            __syncthreads();
-            const int b0 = sm.found[0].bin, b1 = min(sm.found[1].bin, kSampleBins - 1);
-            if (edge_place >= place_of(b0)) {
-                plan.by_list = 1;
-                plan.by_edge = 0;
-                plan.cut0 = place_of(b0);
-                plan.cut1 = place_of(b1 + 1);
-                plan.cut_count = sm.found[0].count0;
-                least = sm.found[0].sum0;
-                most = sm.found[1].sum1;
-                last = b1;
-                plan.slow |= sm.found[1].count1 - sm.found[0].count0 > kSampleList / 2 || b0 > b1;
-            }
-        }
-        if (plan.by_edge && edge_place < kEnd) {
-            last = static_cast<int>(edge_place) / kBinParts;
-            if (static_cast<int>(threadIdx.x) == last / kPer) {
-                int n = sm.x->scan_count[threadIdx.x];
-                float m = sm.x->scan[threadIdx.x];
-                for (int i = 0; i < last % kPer; ++i) {
-                    n += bins.count[i];
-                    m += bins.sum[i];
-                }
-                sm.found[0] = {last, n, n + bins.count[last % kPer], m, m + bins.sum[last % kPer]};
-            }
-            __syncthreads();
-            least = sm.found[0].sum0;
-            most = sm.found[0].sum1;
-        }
-        least = u * least - error;
-        most = u * most + error;
-        bins.find(sm, sm.found[2], false, least, true);
-        bins.find(sm, sm.found[3], false, most, true);
-        __syncthreads();
-        const bool past = sm.found[3].bin > last;
-        const int b0 = min(sm.found[2].bin, last), b1 = past ? last : sm.found[3].bin;
-        plan.draw0 = place_of(b0);
-        plan.draw1 = place_of(b1 + 1);
-        plan.slow |= sm.found[2].bin > last || (past ? sm.x->scan_count[min(kSampleThreads, b1 / kPer + 1)] : sm.found[3].count1) - sm.found[2].count0 > kSampleList / 2;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) sm.plan = plan;
-}
-
-// A token's entry at the end of a list in the first CTA's shared memory.
-__device__ __noinline__ void list_token(uint32_t listed, uint32_t list, int room, float z, int v) {
-    const int at = add_cluster(listed, 1);
-    if (at < room) st_cluster_u64(list + at * 8, sample_entry(z, v));
-}
-
-// A first histogram of the row over 4096 bins, equally wide in the logit, says in which one or two of them each border is;
-// a second pass adds the weights before these up, exactly, and lists the tokens in them in the first CTA's shared memory,
-// which sorts them (solve_lists).  With top-k all tokens that may be kept are listed.  False: the row is not like that (so many equal
-// logits that a bin's count or a list runs over, or a k of thousands).  `hist` is clear; kept tokens' bits go to out, those in
-// the cut's bins excepted.
-template <typename S>
-__device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint32_t *hist, uint8_t *own, int ranks, int rank, float top,
-                                             float low, float least, float sum, int finite, float edge, int top_k, float top_p, float u,
-                                             uint32_t *out) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float c = sm.w.c;
-    const float span = fminf(fminf(kBinOctaves / c, top - fmaxf(low, least)), 3e38f);
-    const float scale = span > 0.f ? fminf((kSampleBins * kBinParts - kBinParts / 2) / span, 1e38f) : 0.f;
-    int binned = 0;
-    least = fmaxf(least, kLowest);
-    s.each([&](float z, int) {
-        if (z >= least) {
-            const int at = static_cast<int>(sample_place(z, top, scale));
-            if (at < kSampleBins * kBinParts) {
-                atomicAdd(&hist[at / kBinParts], (1u << 20) | (at % kBinParts));  // 4095 tokens fit
-                ++binned;
-            }
-        }
-    });
-    binned = __reduce_add_sync(0xffffffffu, binned);
-    if (lane == 0) atomicAdd(&sm.binned, binned);
-    row_sync(ranks);
-    // the slices' histograms become the row's, a part of the bins a CTA
-    const int per_rank = kSampleBins / ranks;
-    const float octaves = scale > 0.f ? c / scale : 0.f;  // of a part of a bin
+// The slices' histograms become the row's, a part of the bins a CTA.
+__device__ __forceinline__ SampleBins make_bins(SampleShared &sm, const uint32_t *hist, uint8_t *own, int ranks, int rank, float octaves) {
+    const int per_rank = kSampleBins / ranks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint2 *mine = reinterpret_cast<uint2 *>(own);
     for (int i = threadIdx.x; i < per_rank; i += kSampleThreads) {
         const int b = rank * per_rank + i;
         uint32_t v[kSampleMaxCluster], n = 0, parts = 0;
@@ -967,80 +887,326 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
             parts += v[q] & 0xFFFFFu;
         }
         const float mean = n ? __fdividef(static_cast<float>(parts), static_cast<float>(n)) + 0.5f : 0.f;
-        const float sum = static_cast<float>(n) * ex2(-(static_cast<float>(b * kBinParts) + mean) * octaves);
-        reinterpret_cast<uint2 *>(own)[i] = make_uint2(n, __float_as_uint(sum));
+        mine[i] = make_uint2(n, __float_as_uint(static_cast<float>(n) * ex2(-(static_cast<float>(b * kBinParts) + mean) * octaves)));
+    }
+    __syncthreads();
+    SampleBins bins;
+    bins.per = per_rank / kSampleThreads;
+    bins.own = mine + threadIdx.x * bins.per;
+    bins.first = rank * per_rank + static_cast<int>(threadIdx.x) * bins.per;
+    int n = 0;
+    float m = 0.f;
+    for (int i = 0; i < bins.per; ++i) {
+        n += static_cast<int>(bins.own[i].x);
+        m += __uint_as_float(bins.own[i].y);
+    }
+    int n_upto = n;
+    float m_upto = m;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int nu = __shfl_up_sync(0xffffffffu, n_upto, o);
+        const float mu = __shfl_up_sync(0xffffffffu, m_upto, o);
+        if (lane >= o) {
+            n_upto += nu;
+            m_upto += mu;
+        }
+    }
+    if (lane == 31) {
+        sm.counts[warp] = n_upto;
+        sm.sums[warp] = m_upto;
     }
     row_sync(ranks);
-    if (rank == 0) plan_borders(sm, ranks, own, top, edge, scale, sum, finite, top_k, top_p, u);
-    row_sync(ranks);
-    if (rank != 0) {
-        if (threadIdx.x < sizeof(SamplePlan) / 4)
-            reinterpret_cast<uint32_t *>(&sm.plan)[threadIdx.x] = ld_cluster_u32(peer(reinterpret_cast<uint32_t *>(&sm.plan) + threadIdx.x, 0));
-        __syncthreads();
+    // totals of all warps before this one, in this CTA and those before
+    int n_before = 0, n_all = 0;
+    float m_before = 0.f, m_all = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSampleMaxCluster / 2; ++i) {
+        const int q = 2 * i + lane / kSampleWarps, w = lane % kSampleWarps;
+        if (q < ranks) {
+            const int nw = static_cast<int>(ld_cluster_u32(peer(&sm.counts[w], q)));
+            const float mw = __uint_as_float(ld_cluster_u32(peer(&sm.sums[w], q)));
+            n_all += nw;
+            m_all += mw;
+            if (q < rank || (q == rank && w < warp)) {
+                n_before += nw;
+                m_before += mw;
+            }
+        }
     }
-    if (sm.plan.slow) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        m_all += __shfl_xor_sync(0xffffffffu, m_all, o);
+        m_before += __shfl_xor_sync(0xffffffffu, m_before, o);
+    }
+    n_all = __reduce_add_sync(0xffffffffu, n_all);
+    n_before = __reduce_add_sync(0xffffffffu, n_before);
+    bins.count1 = n_before + n_upto;
+    bins.sum1 = m_before + m_upto;
+    // (what is before a thread is what is behind the one before it: the same number, so that one of them has a border)
+    bins.count0 = __shfl_up_sync(0xffffffffu, bins.count1, 1);
+    bins.sum0 = __shfl_up_sync(0xffffffffu, bins.sum1, 1);
+    if (lane == 0) {
+        bins.count0 = n_before;
+        bins.sum0 = m_before;
+    }
+    bins.all_count = n_all;
+    bins.all_sum = m_all;
+    return bins;
+}
+
+// Which bins the borders are in, by the running counts and sums of bins.  Sums are kBinError off at most, so that a border may
+// be in either of two bins, or more.  Every thread of the row calls it and knows the plan.
+__device__ __forceinline__ SamplePlan plan_borders(SampleShared &sm, const SampleBins &bins, int ranks, float top, float edge, float scale, float sum,
+                                                   int expected, int top_k, float top_p, float u) {
+    constexpr float kEnd = static_cast<float>(kSampleBins) * kBinParts;
+    const auto place_of = [](int bin) { return static_cast<float>(bin) * kBinParts; };
+    sum = fmaxf(sum, 1.f);
+    const float error = kBinError * sum;
+    const float edge_place = edge == kNoLogit ? kEnd : fminf(sample_place(edge, top, scale), kEnd);
+    SamplePlan plan{};
+    plan.sum = sum;
+    plan.bits = min(54, 59 - ilogbf(plan.sum));
+    plan.cut0 = plan.cut1 = -1.f;
+    plan.slow = bins.all_count != expected;  // a bin had more tokens than it can count
+    if (top_k > 0) {
+        bins.find(sm, 0, ranks, true, static_cast<float>(top_k), false);
+    } else {
+        if (top_p < 1.f) {
+            bins.find(sm, 0, ranks, false, top_p * sum - error, false);
+            bins.find(sm, 1, ranks, false, top_p * sum + error, false);
+        }
+        if (edge_place < kEnd) bins.find_bin(sm, 4, ranks, static_cast<int>(edge_place) / kBinParts);
+    }
+    row_sync(ranks);
+    if (top_k > 0) {
+        plan.gather = 1;
+        plan.draw1 = place_of(sm.found[0].bin + 1);
+        plan.slow |= sm.found[0].bin == kSampleBins || sm.found[0].count1 > kSampleList;
+        return plan;
+    }
+    float least = sum, most = sum;  // of the kept weights
+    int last = kSampleBins - 1, last_count = bins.all_count;  // bin of a kept token, and tokens up to its end
+    plan.by_edge = edge != kNoLogit;
+    if (top_p < 1.f) {
+        const SampleFound f0 = sm.found[0], f1 = sm.found[1];
+        if (edge_place >= place_of(f0.bin)) {
+            plan.by_list = 1;
+            plan.by_edge = 0;
+            plan.cut0 = place_of(f0.bin);
+            plan.cut1 = place_of(min(f1.bin + 1, kSampleBins));
+            plan.cut_count = f0.count0;
+            least = f0.sum0;
+            most = f1.bin < kSampleBins ? f1.sum1 : sum;
+            if (f1.bin < kSampleBins) {
+                last = f1.bin;
+                last_count = f1.count1;
+            }
+            plan.slow |= f0.bin == kSampleBins || last_count - f0.count0 > kSampleList / 2;
+        }
+    }
+    if (plan.by_edge && edge_place < kEnd) {
+        const SampleFound f = sm.found[4];
+        last = f.bin;
+        last_count = f.count1;
+        least = f.sum0;
+        most = f.sum1;
+    }
+    least = u * least - error;
+    most = u * most + error;
+    bins.find(sm, 2, ranks, false, least, true);
+    bins.find(sm, 3, ranks, false, most, true);
+    row_sync(ranks);
+    const SampleFound f0 = sm.found[2], f1 = sm.found[3];
+    plan.slow |= f0.bin > last;
+    plan.draw0 = place_of(min(f0.bin, last));
+    plan.draw1 = place_of(min(f1.bin, last) + 1);
+    plan.slow |= (f1.bin > last ? last_count : f1.count1) - f0.count0 > kSampleList / 2;
+    return plan;
+}
+
+// The smallest logit before a place (infinity: none is): by halves, of the few floats around it where these are enough.
+__device__ __forceinline__ float logit_before(float place, float top, float scale) {
+    if (!(place > 0.f)) return -kNoLogit;
+    const auto before = [&](uint32_t key) { return sample_place(key_value(key), top, scale) < place; };
+    const float about = top - place / scale, off = 0x1p-21f * fmaxf(fabsf(top), fabsf(about));
+    uint32_t no = order_key(kLowest) - 1, yes = order_key(top);  // not before it; before it
+    const float low = about - off, high = about + off;
+    if (low >= kLowest && !before(order_key(low))) no = order_key(low);
+    if (high < top && before(order_key(high))) yes = order_key(high);
+    while (yes - no > 1) {
+        const uint32_t mid = no + (yes - no) / 2;
+        if (before(mid))
+            yes = mid;
+        else
+            no = mid;
+    }
+    return key_value(yes);
+}
+
+// A token's entry at the end of a list of this CTA.
+__device__ __forceinline__ void list_token(int *listed, uint64_t *list, int room, float z, int v) {
+    const int at = atomicAdd(listed, 1);
+    if (at < room) list[at] = sample_entry(z, v);
+}
+
+template <int n>
+__device__ __forceinline__ float largest(const float (&z)[n]) {
+    float most = z[0];
+#pragma unroll
+    for (int k = 1; k < n; ++k) most = fmaxf(most, z[k]);
+    return most;
+}
+
+// A first histogram of the row over 4096 bins, equally wide in the logit, says in which one or two of them each border is;
+// a second pass adds the weights before these up, exactly, and lists the tokens in them; the lists go to the first CTA's shared
+// memory, which sorts them (solve_lists).  With top-k all tokens that may be kept are listed.  False: the row is not like that (so
+// many equal logits that a bin's count or a list runs over, or a k of thousands).  `hist` is clear; kept tokens' bits go to out,
+// those in the cut's bins excepted.
+template <typename S>
+__device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint32_t *hist, uint8_t *own, int ranks, int rank, float top,
+                                             float low, float least, float sum, int finite, float edge, int top_k, float top_p, float u,
+                                             uint32_t *out) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float c = sm.w.c;
+    least = fmaxf(least, kLowest);
+    const float span = fminf(fminf(kBinOctaves / c, top - fmaxf(low, least)), 3e38f);
+    const float scale = span > 0.f ? fminf((kSampleBins * kBinParts - kBinParts / 2) / span, 1e38f) : 0.f;
+    int binned = 0;
+    s.each_vec([&](const auto &z, int) {
+        if (largest(z) < least) return;
+#pragma unroll
+        for (int k = 0; k < S::N; ++k)
+            if (z[k] >= least) {
+                const int at = static_cast<int>(sample_place(z[k], top, scale));
+                if (at < kSampleBins * kBinParts) {
+                    atomicAdd(&hist[at / kBinParts], (1u << 20) | (at % kBinParts));  // 4095 tokens fit
+                    ++binned;
+                }
+            }
+    });
+    binned = __reduce_add_sync(0xffffffffu, binned);
+    if (lane == 0) sm.binned[warp] = binned;
+    row_sync(ranks);
+    int expected = 0;
+#pragma unroll
+    for (int i = 0; i < kSampleMaxCluster / 2; ++i) {
+        const int q = 2 * i + lane / kSampleWarps;
+        if (q < ranks) expected += static_cast<int>(ld_cluster_u32(peer(&sm.binned[lane % kSampleWarps], q)));
+    }
+    expected = __reduce_add_sync(0xffffffffu, expected);
+    const SampleBins bins = make_bins(sm, hist, own, ranks, rank, scale > 0.f ? c / scale : 0.f);
+    SamplePlan plan = plan_borders(sm, bins, ranks, top, edge, scale, sum, expected, top_k, top_p, u);
+    if (plan.slow) {
         row_sync(ranks);
         return false;
     }
+    if (threadIdx.x < 4) {
+        const float place = threadIdx.x == 0 ? plan.draw0 : threadIdx.x == 1 ? plan.draw1 : threadIdx.x == 2 ? plan.cut0 : plan.cut1;
+        sm.edges[threadIdx.x] = logit_before(place, top, scale);
+    }
     if (threadIdx.x == 0) {
-        sm.w.set_floor(sm.plan.bits);
-        sm.w.set_big(sm.plan.sum);
+        sm.plan = plan;
+        sm.w.set_floor(plan.bits);
+        sm.w.set_big(plan.sum);
     }
     __syncthreads();
-    const uint32_t lists = peer(reinterpret_cast<uint64_t *>(hist), 0), listed = peer(&sm.listed[0], 0);
-    const float draw0 = sm.plan.draw0, draw1 = sm.plan.draw1, cut0 = sm.plan.cut0, cut1 = sm.plan.cut1;
-    const float from = sm.plan.by_edge ? edge : kLowest;
-    if (sm.plan.gather) {
-        s.each([&](float z, int v) {
-            if (z >= kLowest && sample_place(z, top, scale) < draw1) list_token(listed, lists, kSampleList, z, v);
+    uint64_t *list = reinterpret_cast<uint64_t *>(hist), *cut_list = list + kSampleList / 2;
+    const float draw0 = sm.edges[0], draw1 = sm.edges[1], cut0 = sm.edges[2], cut1 = sm.edges[3];
+    const int bits = plan.bits;
+    uint64_t sums[3] = {0, 0, 0};
+    int count = 0;
+    if (plan.gather) {
+        s.each_vec([&](const auto &z, int v) {
+            if (largest(z) < draw1) return;
+#pragma unroll
+            for (int k = 0; k < S::N; ++k)
+                if (z[k] >= draw1) list_token(&sm.listed[0], list, kSampleList, z[k], v + k);
+        });
+    } else if (plan.by_edge) {
+        s.each_vec([&](const auto &z, int v) {
+            if (largest(z) < edge) return;
+#pragma unroll
+            for (int k = 0; k < S::N; ++k)
+                if (z[k] >= edge) {
+                    const uint64_t m = sm.w.exact_of(z[k], bits, sm.table);
+                    ++count;
+                    sums[0] += m;
+                    if (z[k] >= draw0)
+                        sums[2] += m;
+                    else if (z[k] >= draw1)
+                        list_token(&sm.listed[0], list, kSampleList / 2, z[k], v + k);
+                }
         });
     } else {
         const SampleWeights w = sm.w;
-        const int bits = sm.plan.bits;
-        uint64_t sums[3] = {0, 0, 0};
-        const bool by_edge = sm.plan.by_edge;
-        int count = 0;
-        const float last = fmaxf(cut1, draw1), weighs = by_edge ? fmaxf(w.floor, before_float(edge)) : w.floor;
-        s.each([&](float z, int v) {
-            uint64_t m = w.of(z, bits, sm.table.v);  // (of a logit that does not count: anything)
-            if (z >= w.big) m = sm.w.in_64_bits(z, bits, &sm.table);
-            m = z > weighs ? m : 0ull;
-            sums[0] += m;
-            const float at = sample_place(z, top, scale);
-            if (at < last) {
-                if (at < cut0) sums[1] += m;
-                if (at < draw0) sums[2] += m;
-                if (at >= cut0 && at < cut1) list_token(listed + 4, lists + kSampleList * 4, kSampleList / 2, z, v);
-                if (at >= draw0 && at < draw1 && z >= from) list_token(listed, lists, kSampleList / 2, z, v);
+        s.each_vec([&](const auto &z, int v) {
+            uint32_t special = 0;  // tokens that are listed, or weighed in 64 bits
+#pragma unroll
+            for (int k = 0; k < S::N; k += 2) {
+                uint64_t m[2];
+                w.two_of(z[k], z[k + 1], bits, sm.table.v, m);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float x = z[k + i];
+                    const bool before_cut = x >= cut0, before_draw = x >= draw0;
+                    sums[0] += m[i];
+                    if (before_cut) sums[1] += m[i];
+                    if (before_draw) sums[2] += m[i];
+                    if ((x >= cut1 && !before_cut) || (x >= draw1 && !before_draw) || x >= w.big) special |= 1u << (k + i);
+                }
             }
-            if (by_edge) count += z >= edge;
+            while (special) {
+                const int k = __ffs(special) - 1;
+                special &= special - 1;
+                const float x = s.at(v - s.v0 + k);
+                if (x >= w.big) {
+                    const uint64_t more = sm.w.in_64_bits(x, bits, &sm.table) - w.of(x, bits, sm.table.v);
+                    sums[0] += more;
+                    if (x >= cut0) sums[1] += more;
+                    if (x >= draw0) sums[2] += more;
+                }
+                if (x >= cut1 && x < cut0) list_token(&sm.listed[1], cut_list, kSampleList / 2, x, v + k);
+                if (x >= draw1 && x < draw0) list_token(&sm.listed[0], list, kSampleList / 2, x, v + k);
+            }
         });
-        if (by_edge) count = __reduce_add_sync(0xffffffffu, count);
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 3; ++i) {
 #pragma unroll
-            for (int o = 16; o; o >>= 1) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
-            if (lane == 0) sm.warp_sums[i][warp] = sums[i];
+        for (int o = 16; o; o >>= 1) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
+        if (lane == 0) sm.warp_sums[i][warp] = sums[i];
+    }
+    if (lane == 0) sm.counts[warp] = count;
+    __syncthreads();
+    if (threadIdx.x < 4) {
+        uint64_t m = 0;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) {
+            n += sm.counts[i];
+            m += sm.warp_sums[min(2, static_cast<int>(threadIdx.x))][i];
         }
-        if (lane == 0) sm.counts[warp] = count;
+        if (threadIdx.x < 3)
+            st_cluster_u64(peer(&sm.part[rank][threadIdx.x], 0), m);
+        else
+            st_shared_cluster(peer(&sm.part_count[rank], 0), n);
+    }
+    if (rank != 0) {  // the lists go behind what the first CTA has
+        if (threadIdx.x < 2) sm.list_at[threadIdx.x] = sm.listed[threadIdx.x] ? add_cluster(peer(&sm.listed[threadIdx.x], 0), sm.listed[threadIdx.x]) : 0;
         __syncthreads();
-        if (threadIdx.x < 4) {
-            uint64_t m = 0;
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < kSampleWarps; ++i) {
-                n += sm.counts[i];
-                m += sm.warp_sums[min(2, static_cast<int>(threadIdx.x))][i];
-            }
-            if (threadIdx.x < 3)
-                st_cluster_u64(peer(&sm.part[rank][threadIdx.x], 0), m);
-            else
-                st_shared_cluster(peer(&sm.part_count[rank], 0), n);
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which) {
+            const int room = plan.gather ? kSampleList : kSampleList / 2, at = sm.list_at[which];
+            const uint32_t to = peer(list + which * (kSampleList / 2), 0);
+            for (int i = threadIdx.x; i < min(sm.listed[which], room - at); i += kSampleThreads)
+                st_cluster_u64(to + (at + i) * 8, list[which * (kSampleList / 2) + i]);
         }
     }
     if (out) {
-        const float end = sm.plan.gather ? 0.f : sm.plan.by_list ? cut0 : -kNoLogit;  // places from there on are not kept, or not yet
-        write_bits(s, out, [&](float z, int) { return z >= from && (end == -kNoLogit || sample_place(z, top, scale) < end); });
+        // those before the cut's bins; of a list's none yet
+        const float from = plan.gather ? -kNoLogit : plan.by_list ? cut0 : plan.by_edge ? edge : kLowest;
+        write_bits(s, out, from == -kNoLogit, [&](float z, int) { return z >= from; });
     }
     return true;
 }
@@ -1121,8 +1287,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) {
         sm.x = reinterpret_cast<SampleShared::Scratch *>(hist);
-        sm.binned = 0;
         sm.listed[0] = sm.listed[1] = 0;
+        for (int i = 0; i < 5; ++i) sm.found[i] = {kSampleBins, 0, 0, 0.f, 0.f};
     }
     pdl_wait();
     const Slice<T, kResident> s(p, r, rank, buffer);
@@ -1136,7 +1302,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         sm.min_log = min_p > 0.f ? T_used * log(static_cast<double>(min_p)) : 0.0;  // (on its way while the others load)
     }
     SampleRange range = load_slice(s, c);
-    float top = range.top, low = range.bad ? kNoLogit : range.low;  // a smallest logit of -infinity says so
+    float top = range.top, low = fmaxf(range.low, kLowest);  // (of a row with -infinities: the lowest there is)
     float least_top = top;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -1147,7 +1313,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     float sum = range.sum * ex2((range.top - top) * c);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    int finite = __reduce_add_sync(0xffffffffu, range.count);
+    int finite = __reduce_add_sync(0xffffffffu, range.gone);  // those that are not, here
     if (lane == 0) {
         sm.range[0][warp] = top;
         sm.range[1][warp] = low;
@@ -1187,9 +1353,9 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     for (int i = 0; i < kSampleMaxCluster / 2; ++i) sum += sums[i] * ex2((tops[i] - top) * c);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    finite = __reduce_add_sync(0xffffffffu, finite);
+    finite = p.a.V - __reduce_add_sync(0xffffffffu, finite);
     static_assert(kSampleWarps == 16, "two CTAs' warps are a warp's lanes");
-    const bool ok = low != kNoLogit && finite > 0 && T_row >= 0.f && (T_row == 0.f || (p.a.uniform && u >= 0.f && u < 1.f)) &&
+    const bool ok = fabsf(sum) < -kNoLogit && finite > 0 && T_row >= 0.f && (T_row == 0.f || (p.a.uniform && u >= 0.f && u < 1.f)) &&
                     top_p == top_p && min_p <= 1.f;
     bool done = false;  // the mask is written
     SampleCut cut{0xFFFFFFFFu, -1};  // nothing
@@ -1243,7 +1409,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
                 const Slice<T, false> row(whole, r, 0, buffer);
                 sample_slowly(row, sm, 1, 0, p.sum_bits, top, edge, top_k, top_p, u);
                 cut = sm.result.cut;
-                if (out) write_bits(row, out, [&](float z, int v) { return cut.keeps(order_key(z), v); });
+                if (out) write_bits(row, out, false, [&](float z, int v) { return z >= kLowest && cut.keeps(order_key(z), v); });
                 done = true;
             }
         } else {
@@ -1259,7 +1425,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         if (p.a.out_prob) p.a.out_prob[r] = res.prob;
     }
     if (done) return;
-    if (out) write_bits(s, out, [&](float z, int v) { return cut.keeps(order_key(z), v); });
+    if (out) write_bits(s, out, !ok, [&](float z, int v) { return z >= kLowest && cut.keeps(order_key(z), v); });
     if (ranks > 1) cluster_sync();  // shared memory is read by the others until here
 }
 
