@@ -43,6 +43,7 @@ struct SampleParams {
     int sum_bits;    // units of a row's sum of weights: 2^-sum_bits of the largest
     int list_at;     // in shared memory, where the histogram and then the lists are; behind them this CTA's bins of the row
     int upto_at;     // room for running sums of a list
+    int bits_at;     // a slice's bits of the mask that goes out; 0 where these are too many
 };
 
 // 2^(i / 512) in units of 2^-31, and what is left of it in units of 2^-52 (signed).
@@ -1065,7 +1066,7 @@ __device__ __forceinline__ float largest(const float (&z)[n]) {
 template <typename S>
 __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint32_t *hist, uint8_t *own, int ranks, int rank, float top,
                                              float low, float least, float sum, int finite, float edge, int top_k, float top_p, float u,
-                                             uint32_t *out) {
+                                             uint32_t *out, uint32_t *kept_bits) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float c = sm.w.c;
     least = fmaxf(least, kLowest);
@@ -1115,6 +1116,17 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
     const int bits = plan.bits;
     uint64_t sums[3] = {0, 0, 0};
     int count = 0;
+    // Bits of the tokens before the cut's bins; of a list's none yet.
+    const auto keep = [&](uint32_t bits_of, int v) {
+        const int at = v - s.v0;
+        atomicOr(&kept_bits[at >> 5], bits_of << (at & 31));
+        if (at % 32 + S::N > 32 && bits_of >> (32 - at % 32)) atomicOr(&kept_bits[(at >> 5) + 1], bits_of >> (32 - at % 32));
+    };
+    const bool mark = out && kept_bits;
+    if (mark) {
+        for (int i = threadIdx.x; i < (s.row.V + 31) / 32; i += kSampleThreads) kept_bits[i] = 0;
+        __syncthreads();
+    }
     if (plan.gather) {
         s.each_vec([&](const auto &z, int v) {
             if (largest(z) < draw1) return;
@@ -1125,10 +1137,12 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
     } else if (plan.by_edge) {
         s.each_vec([&](const auto &z, int v) {
             if (largest(z) < edge) return;
+            uint32_t kept = 0;
 #pragma unroll
             for (int k = 0; k < S::N; ++k)
                 if (z[k] >= edge) {
                     const uint64_t m = sm.w.exact_of(z[k], bits, sm.table);
+                    kept |= 1u << k;
                     ++count;
                     sums[0] += m;
                     if (z[k] >= draw0)
@@ -1136,10 +1150,13 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
                     else if (z[k] >= draw1)
                         list_token(&sm.listed[0], list, kSampleList / 2, z[k], v + k);
                 }
+            if (mark) keep(kept, v);
         });
     } else {
         const SampleWeights w = sm.w;
+        const float from = plan.by_list ? cut0 : kLowest;
         s.each_vec([&](const auto &z, int v) {
+            uint32_t kept = 0;
             uint32_t special = 0;  // tokens that are listed, or weighed in 64 bits
 #pragma unroll
             for (int k = 0; k < S::N; k += 2) {
@@ -1152,9 +1169,11 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
                     sums[0] += m[i];
                     if (before_cut) sums[1] += m[i];
                     if (before_draw) sums[2] += m[i];
+                    if (x >= from) kept |= 1u << (k + i);
                     if ((x >= cut1 && !before_cut) || (x >= draw1 && !before_draw) || x >= w.big) special |= 1u << (k + i);
                 }
             }
+            if (kept && mark) keep(kept, v);
             while (special) {
                 const int k = __ffs(special) - 1;
                 special &= special - 1;
@@ -1203,10 +1222,11 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
                 st_cluster_u64(to + (at + i) * 8, list[which * (kSampleList / 2) + i]);
         }
     }
-    if (out) {
-        // those before the cut's bins; of a list's none yet
+    if (mark) {  // (behind the barrier that the sums have had)
+        for (int i = threadIdx.x; i < (s.row.V + 31) / 32; i += kSampleThreads) out[s.v0 / 32 + i] = kept_bits[i];
+    } else if (out) {
         const float from = plan.gather ? -kNoLogit : plan.by_list ? cut0 : plan.by_edge ? edge : kLowest;
-        write_bits(s, out, from == -kNoLogit, [&](float z, int) { return z >= from; });
+        write_bits(s, out, plan.gather, [&](float z, int) { return z >= from; });
     }
     return true;
 }
@@ -1393,7 +1413,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
             else if (rest > 0.f)
                 least = fmaxf(edge, top + __fdividef(log2f(rest) - 0x1p-6f, c));
         }
-        if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out)) {
+        if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out,
+                         p.bits_at ? reinterpret_cast<uint32_t *>(buffer + p.bits_at) : nullptr)) {
             // the rest is the first CTA's; the others' shared memory is not read any more
             if (ranks > 1) {
                 cluster_arrive();
@@ -1429,28 +1450,36 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     if (ranks > 1) cluster_sync();  // shared memory is read by the others until here
 }
 
-constexpr int kSampleSmem = 200 * 1024;  // of a slice that stays in shared memory
+constexpr int kSampleSmem = 200 * 1024;
+constexpr int kSampleSlice = 80 * 1024;  // that stays in shared memory, two of them beside each other; a longer one is read again
+constexpr int kSampleBits = 48 * 1024;   // of a slice, at most
 
-// CTAs of a row: up to eight, as long as all of them run at once and a CTA has some thousand tokens.
+// CTAs of a row, two of which an SM holds.  One row of 126464 tokens: 22.0 us with eight, 27.7 with four; 7 rows of 50021: 22.3
+// and 20.2; 128 rows of 126464: 88 with eight, 57 with four, 59 with two; 528 rows of 152064 in fp32 (no slice of a row in four
+// stays in shared memory beside another): 391 with four, 327 with two, 346 with one; one row of 4096: 12.6 with four, 13.5
+// with two, 14.3 with one.
 int sample_ranks(long long rows, int V, int num_sms) {
-    int ranks = kSampleMaxCluster;
-    while (ranks > 1 && (rows * ranks > 2 * num_sms || V < ranks * 2048)) ranks >>= 1;
+    int ranks = rows * 8 <= 2 * num_sms && V >= 8 * 8192 ? 8 : rows * 4 <= 4 * num_sms ? 4 : 2;
+    while (ranks > 1 && V < ranks * 1024) ranks >>= 1;
     return ranks;
 }
 
 template <typename T>
 cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t s) {
-    int ranks = sample_ranks(p.a.rows, p.a.V, num_sms);
-    const auto slice_of = [&](int n) { return ((p.words + n - 1) / n) * 32; };
-    while (ranks < kSampleMaxCluster && slice_of(ranks) * static_cast<long long>(sizeof(T)) > 64 * 1024) ranks *= 2;
-    p.slice = slice_of(ranks);
+    const int ranks = sample_ranks(p.a.rows, p.a.V, num_sms);
+    p.slice = (p.words + ranks - 1) / ranks * 32;
     const long long slice_bytes = (p.slice * static_cast<long long>(sizeof(T)) + 47) / 16 * 16;
     const int own_bytes = kSampleBins / ranks * 8;
-    const bool resident = slice_bytes + kSampleList * 16 <= kSampleSmem;
+    const bool resident = slice_bytes <= kSampleSlice;
     p.list_at = resident ? static_cast<int>(slice_bytes) : 0;
     // running sums lie where the slice was, or where this CTA's bins were
     p.upto_at = p.list_at >= kSampleList * 8 ? 0 : p.list_at + kSampleList * 8;
-    const long long bytes = p.list_at + kSampleList * 8 + (p.upto_at ? std::max(own_bytes, kSampleList * 8) : own_bytes);
+    p.bits_at = p.list_at + kSampleList * 8 + (p.upto_at ? std::max(own_bytes, kSampleList * 8) : own_bytes);
+    long long bytes = p.bits_at;
+    if (p.a.out_allowed && p.slice / 8 <= kSampleBits)
+        bytes += p.slice / 8;
+    else
+        p.bits_at = 0;
     void (*kernel)(const SampleParams) = resident ? k_sample_limits<T, true> : k_sample_limits<T, false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
     if (e != cudaSuccess) return e;

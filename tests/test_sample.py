@@ -148,7 +148,7 @@ def test_limits(rows, V, stride, limit, kind):
 
 @gpu
 @needs_gpu
-@pytest.mark.parametrize("rows,V,kind", [(1, 126464, "bf16"), (40, 126464, "bf16"), (3, 152064, "f32"), (2, 1500001, "f32"), (300, 5000, "f16")])
+@pytest.mark.parametrize("rows,V,kind", [(1, 126464, "bf16"), (40, 126464, "bf16"), (3, 152064, "f32"), (2, 1500001, "f32"), (1, 5000011, "bf16"), (300, 5000, "f16"), (160, 30000, "f32")])
 def test_sizes(rows, V, kind):
     g = gen(V)
     z = logits(rows, V, kind, rows)
