@@ -39,7 +39,7 @@ constexpr int kFp8ColsTile = 256;           // matrix rows of a tile (N)
 constexpr int kFp8TileBytes = kFp8ColsTile * kFp8Block;  // codes of a tile and block
 constexpr int kFp8RowsBytes = kFp8RowsTile * kFp8Block;
 constexpr int kFp8Threads = 12 * 32;        // three warpgroups, between which the registers are divided anew
-constexpr int kFp8EpilogueRegs = 216, kFp8OtherRegs = 56;  // 256 * 216 + 128 * 56 of the launch's 384 * 168
+constexpr int kFp8EpilogueRegs = 224, kFp8OtherRegs = 56;  // 256 * 224 + 128 * 56 of the launch's 384 * 168
 constexpr int kFp8TmaCodes = 8, kFp8TmaRows = 9, kFp8Mma = 10;  // warps; 0 - 7 are the epilogue
 constexpr int kFp8Smem = 226 * 1024;
 constexpr int kFp8MaxRows = 1 << 14;         // of a launch
@@ -84,12 +84,34 @@ __global__ void k_fp8_pack_scales(const float *scales, float *packed, int rows, 
 
 // ------------------------------------------------------------------------------ activations
 
-// Eight numbers over a scale as e4m3 codes.
-__device__ __forceinline__ uint2 fp8_codes(const float2 (&u)[4], float scale) {
+// Eight numbers over a scale as e4m3 codes: the fp32 quotient, rounded.  A product with the reciprocal is at most 2 of
+// fp32's last places off that, and the code hangs on it only where it is as close to the middle between two codes (bit 19 of
+// the number set, those below it clear); there, and where e4m3's own steps do not get smaller any more (below 2^-6), it is
+// divided.  (A division each took a head of 126464 x 4096 from 300 us to 865.)
+__device__ __forceinline__ bool fp8_close(float t) {
+    const uint32_t b = __float_as_uint(t);
+    return ((b + 3u - 0x80000u) & 0xFFFFFu) <= 6u || (fabsf(t) < 0x1p-6f && t != 0.f);
+}
+__device__ __forceinline__ uint2 fp8_codes(const float2 (&u)[4], float scale, float inverse) {
+    float2 t[4];
+    bool close = !(scale >= 0x1p-100f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        t[i] = make_float2(u[i].x * inverse, u[i].y * inverse);
+        close |= fp8_close(t[i].x) || fp8_close(t[i].y);
+    }
+    if (close)
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            const float2 from = i == 0 ? u[0] : i == 1 ? u[1] : i == 2 ? u[2] : u[3];
+            const float2 q = make_float2(from.x / scale, from.y / scale);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k == i) t[k] = q;
+        }
     uint32_t h[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        h[i] = __nv_cvt_float2_to_fp8x2(make_float2(u[i].x / scale, u[i].y / scale), __NV_SATFINITE, __NV_E4M3);
+    for (int i = 0; i < 4; ++i) h[i] = __nv_cvt_float2_to_fp8x2(t[i], __NV_SATFINITE, __NV_E4M3);
     return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
 }
 
@@ -136,7 +158,8 @@ __global__ void __launch_bounds__(256) k_fp8_rows(const Fp8RowsParams p) {
         if (c < chunks) {
             top = fmaxf(top, amax);
             const float scale = amax / kFp8Most;
-            const uint2 q = fp8_codes(u, scale > 0.f ? scale : 1.f);
+            const float by = scale > 0.f ? scale : 1.f;
+            const uint2 q = fp8_codes(u, by, 1.f / by);
             const int kb = c >> 4, piece = (c >> 1) & 7;
             *reinterpret_cast<uint2 *>(codes + static_cast<long long>(kb) * kFp8RowsBytes + (piece ^ (slot & 7)) * 16 + (c & 1) * 8) = q;
             if ((c & 15) == 0) scale_of[kb] = scale;
@@ -193,7 +216,7 @@ struct Fp8Params {
     float *partials;          // [worker][2][CTA of a pair][2][32][partial rows][4]
     void *out;
     long long out_stride;
-    int out_type, out_vec;    // out_vec: 16-byte stores fit
+    int out_type, out_vec;    // out_vec: 32-byte stores fit
     int rows, V;
     long long wait_cycles;
     int stall;
@@ -292,6 +315,24 @@ __device__ __forceinline__ bool fp8_wait_warp(uint64_t *bar, uint32_t parity, vo
     return __all_sync(0xffffffffu, fp8_wait<kPair>(bar, parity, abort));
 }
 
+// 16 columns of the accumulator on their way to a thread's registers, which are theirs after tmem_arrived.
+__device__ __forceinline__ void tmem_ask_x16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32"
+        " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
+
 __device__ __forceinline__ int ld_shared_cluster(uint32_t cluster_addr) {
     int v;
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
@@ -301,32 +342,43 @@ __device__ __forceinline__ void mbar_complete_tx(uint64_t *bar, uint32_t bytes) 
     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
 
-// Eight neighbouring logits of a row from column v on.
-__device__ __forceinline__ void fp8_store(const Fp8Params &p, long long row, int v, const float (&y)[8]) {
+__device__ __forceinline__ void store_256(void *to, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t pair_of(float a, float b, int type) {
+    if (type == RPD_TYPE_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Sixteen neighbouring logits of a row from column v on, 32 bytes a store where that fits (a whole sector: stores of half
+// a sector were read and written twice).
+__device__ __forceinline__ void fp8_store(const Fp8Params &p, long long row, int v, const float (&y)[16]) {
     const long long at = row * p.out_stride + v;
-    if (p.out_vec && v + 8 <= p.V) {
+    if (p.out_vec && v + 16 <= p.V) {
+        uint32_t w[8];
         if (p.out_type == RPD_TYPE_F32) {
-            float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at);
-            to[0] = make_float4(y[0], y[1], y[2], y[3]);
-            to[1] = make_float4(y[4], y[5], y[6], y[7]);
-        } else {
-            uint32_t w[4];
+            float *to = static_cast<float *>(p.out) + at;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (p.out_type == RPD_TYPE_BF16) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
-                    w[i] = *reinterpret_cast<const uint32_t *>(&h);
-                } else {
-                    const __half2 h = __floats2half2_rn(y[2 * i], y[2 * i + 1]);
-                    w[i] = *reinterpret_cast<const uint32_t *>(&h);
-                }
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(y[8 * h + i]);
+                store_256(to + 8 * h, w);
             }
-            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pair_of(y[2 * i], y[2 * i + 1], p.out_type);
+            store_256(static_cast<uint16_t *>(p.out) + at, w);
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 16; ++i)
         if (v + i < p.V) store_out(p.out, p.out_type, at + i, y[i]);
 }
 
@@ -518,22 +570,32 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 ok = fp8_wait_warp<kPair>(&sm.acc_full[acc], acc_phase, abort);
                 if (!ok) break;
                 tc_fence_after_sync();
-                if (reads) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float v[32];
-                        tmem_ld_32x32b_x32(from + acc * 256 + c * 32, v);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) run[c * 16 + i] = fma2(f2, pack2(v[2 * i], v[2 * i + 1]), run[c * 16 + i]);
+                const auto release = [&] {  // all of the accumulator is in registers
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (kPair)
+                            mbar_arrive_cluster(empty[acc]);
+                        else
+                            mbar_arrive(&sm.acc_empty[acc]);
                     }
-                }
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) {
-                    if (kPair)
-                        mbar_arrive_cluster(empty[acc]);
-                    else
-                        mbar_arrive(&sm.acc_empty[acc]);
+                };
+                if (reads) {
+                    uint32_t v[2][16];  // one half is multiplied while the next is on its way
+                    tmem_ask_x16(from + acc * 256, v[0]);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        tmem_arrived(v[c & 1]);
+                        if (c < 7)
+                            tmem_ask_x16(from + acc * 256 + (c + 1) * 16, v[(c + 1) & 1]);
+                        else
+                            release();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            run[c * 8 + i] = fma2(f2, pack2(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), run[c * 8 + i]);
+                    }
+                } else {
+                    release();
                 }
                 acc_phase ^= acc;
                 acc ^= 1;
@@ -582,13 +644,13 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 const int v0 = col_tile * kFp8ColsTile + half * 128;
                 const float factor = __ldcg(p.factor + row);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float y[8];
+                for (int i = 0; i < 8; ++i) {
+                    float y[16];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) unpack2(run[4 * i + j], y[2 * j], y[2 * j + 1]);
+                    for (int j = 0; j < 8; ++j) unpack2(run[8 * i + j], y[2 * j], y[2 * j + 1]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] *= factor;
-                    if (v0 + 8 * i < p.V) fp8_store(p, row, v0 + 8 * i, y);
+                    for (int j = 0; j < 16; ++j) y[j] *= factor;
+                    if (v0 + 16 * i < p.V) fp8_store(p, row, v0 + 16 * i, y);
                 }
             }
         }
@@ -690,23 +752,43 @@ cudaError_t launch_fp8(const CUtensorMap &codes, const CUtensorMap &x, const Fp8
 
 // ------------------------------------------------------------------------------ the quantiser
 
-__device__ __forceinline__ void load_eight(const float *row, int col, int cols, int align, float2 (&u)[4]) {
-    if (col + 8 <= cols && align >= 8) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const float2 *>(row + col + 2 * i);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        u[i] = make_float2(col + 2 * i < cols ? row[col + 2 * i] : 0.f, col + 2 * i + 1 < cols ? row[col + 2 * i + 1] : 0.f);
-}
+// Eight neighbouring numbers of a row as they are.
 template <typename T>
-__device__ __forceinline__ void load_eight(const T *row, int col, int cols, int align, float2 (&u)[4]) {
-    const uint4 v = load_chunk(row, col, cols, align);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+struct Eight {
+    uint4 v;
+    __device__ __forceinline__ void load(const T *row, int col, int cols, int align) { v = load_chunk(row, col, cols, align); }
+    __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float2 (&u)[4]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = pair_value(w[i], T());
-}
+        for (int i = 0; i < 4; ++i) u[i] = pair_value(w[i], T());
+    }
+};
+template <>
+struct Eight<float> {
+    float2 v[4];
+    __device__ __forceinline__ void load(const float *row, int col, int cols, int align) {
+        if (col + 8 <= cols && align == 16) {
+            const float4 a = reinterpret_cast<const float4 *>(row + col)[0], b = reinterpret_cast<const float4 *>(row + col)[1];
+            v[0] = make_float2(a.x, a.y);
+            v[1] = make_float2(a.z, a.w);
+            v[2] = make_float2(b.x, b.y);
+            v[3] = make_float2(b.z, b.w);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = make_float2(col + 2 * i < cols ? row[col + 2 * i] : 0.f, col + 2 * i + 1 < cols ? row[col + 2 * i + 1] : 0.f);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = make_float2(0.f, 0.f);
+    }
+    __device__ __forceinline__ void get(float2 (&u)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = v[i];
+    }
+};
 
 __device__ __forceinline__ void store_codes(uint8_t *row, int col, int cols, bool vec, uint2 q) {
     if (vec && col + 8 <= cols) {
@@ -741,19 +823,22 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantizeParams p)
         const bool live = i < rows * blocks;
         const int block = static_cast<int>(i % blocks);
         const long long row0 = kHigh == 1 ? i / blocks : i / blocks * kHigh + lanes;
-        float2 u[kRows][4];
+        Eight<T> x[kRows];
         float amax = 0.f;
 #pragma unroll
         for (int j = 0; j < kRows; ++j) {
             const long long row = row0 + j * 16;
-            if (live && row < p.rows) {
-                load_eight(static_cast<const T *>(p.x) + row * p.x_stride, block * kFp8Block + col, p.cols, p.x_align, u[j]);
-            } else {
+            if (live && row < p.rows)
+                x[j].load(static_cast<const T *>(p.x) + row * p.x_stride, block * kFp8Block + col, p.cols, p.x_align);
+            else
+                x[j].clear();
+        }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) u[j][k] = make_float2(0.f, 0.f);
-            }
+        for (int j = 0; j < kRows; ++j) {
+            float2 u[4];
+            x[j].get(u);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(fabsf(u[j][k].x), fabsf(u[j][k].y)));
+            for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(fabsf(u[k].x), fabsf(u[k].y)));
         }
 #pragma unroll
         for (int o = kHigh == 1 ? 8 : 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
@@ -764,13 +849,15 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantizeParams p)
             for (int w = 0; w < 8; ++w) amax = fmaxf(amax, red[w]);
             __syncthreads();
         }
-        const float scale = amax / kFp8Most, by = scale > 0.f ? scale : 1.f;
+        const float scale = amax / kFp8Most, by = scale > 0.f ? scale : 1.f, inverse = 1.f / by;
         if (live && (kHigh == 1 ? col == 0 : threadIdx.x == 0)) p.scales[i] = scale;
 #pragma unroll
         for (int j = 0; j < kRows; ++j) {
             const long long row = row0 + j * 16;
+            float2 u[4];
+            x[j].get(u);
             if (live && row < p.rows)
-                store_codes(p.codes + row * p.codes_stride, block * kFp8Block + col, p.cols, p.vec, fp8_codes(u[j], by));
+                store_codes(p.codes + row * p.codes_stride, block * kFp8Block + col, p.cols, p.vec, fp8_codes(u, by, inverse));
         }
     }
 }
@@ -948,7 +1035,7 @@ int rpd_fp8_logits(const rpd_fp8 *h, const void *x, int x_type, int64_t x_stride
         p.out = static_cast<uint8_t *>(out) + first * out_stride * type_size(out_type);
         p.out_stride = out_stride;
         p.out_type = out_type;
-        p.out_vec = aligned_to(out, 16) && (rows == 1 || out_stride * type_size(out_type) % 16 == 0);
+        p.out_vec = aligned_to(out, 32) && (rows == 1 || out_stride * type_size(out_type) % 32 == 0);
         p.rows = n;
         p.V = h->V;
         p.wait_cycles = h->wait_us * kWaitCyclesPerUs;
