@@ -294,25 +294,10 @@ __device__ __forceinline__ void fp8_commit(uint64_t *bar) {
         umma_commit_warp(bar);
 }
 
-// wait_phase_warp; in a pair with acquire semantics at cluster scope, for arrivals may come from the other CTA.
-template <bool kPair>
-__device__ __forceinline__ bool fp8_wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    if (!kPair) return wait_phase(bar, parity, abort);
-    const uint32_t a = smem_u32(bar);
-    if (mbar_try_wait_cluster(a, parity)) return true;
-    const long long t0 = clock64();
-    while (!mbar_try_wait_cluster(a, parity)) {
-        if (*abort) return false;
-        if (clock64() - t0 > static_cast<long long>(abort[1]) << 10) {
-            *abort = 1;
-            return false;
-        }
-    }
-    return true;
-}
-template <bool kPair>
-__device__ __forceinline__ bool fp8_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    return __all_sync(0xffffffffu, fp8_wait<kPair>(bar, parity, abort));
+// Arrive on a barrier of the pair's even CTA.  What is handed over is tensor memory that has been read, nothing in memory: with
+// release semantics at cluster scope the arrival waited for every load and store before it, a fence a block of columns.
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // 16 columns of the accumulator on their way to a thread's registers, which are theirs after tmem_arrived.
@@ -474,7 +459,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 const int atoms = (min(kFp8RowsTile, p.rows - row_tile * kFp8RowsTile) + 7) / 8;  // of 8 rows; single CTAs' tiles have a row
                 for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
                     if (issued == kStages) pdl_wait();
-                    if (issued >= kStages) ok = fp8_wait<kPair>(&sm.done[s.at], s.phase ^ 1u, abort);
+                    if (issued >= kStages) ok = wait_phase(&sm.done[s.at], s.phase ^ 1u, abort);
                     if (!ok) break;
                     uint8_t *to = smem + s.at * kStageBytes;
                     const long long code_block = static_cast<long long>(col_tile) * plan.blocks + kb;
@@ -512,7 +497,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             pdl_wait();
             while (ok && walk.next(plan, worker, seg)) {
                 for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
-                    ok = fp8_wait_warp<kPair>(&sm.full[s.at], s.phase, abort) && fp8_wait_warp<kPair>(&sm.acc_empty[acc], acc_phase, abort);
+                    ok = wait_phase_warp(&sm.full[s.at], s.phase, abort) && wait_phase_warp(&sm.acc_empty[acc], acc_phase, abort);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const uint32_t at = static_cast<uint32_t>(s.at * kStageBytes) / 16;
@@ -567,7 +552,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                     sx = __ldcg(xs);
                     sw = *ws;
                 }
-                ok = fp8_wait_warp<kPair>(&sm.acc_full[acc], acc_phase, abort);
+                ok = wait_phase_warp(&sm.acc_full[acc], acc_phase, abort);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const auto release = [&] {  // all of the accumulator is in registers
@@ -575,7 +560,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                     __syncwarp();
                     if (lane == 0) {
                         if (kPair)
-                            mbar_arrive_cluster(empty[acc]);
+                            mbar_arrive_relaxed(empty[acc]);
                         else
                             mbar_arrive(&sm.acc_empty[acc]);
                     }
