@@ -535,9 +535,9 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             const bool reads = (warp & 3) * 32 < live;                              // uniform in the warp
             const float *xs = p.x_scales + (static_cast<long long>(row_tile) * plan.blocks + seg.kb0) * kFp8RowsTile + slot;
             const float *ws = p.code_scales + (static_cast<long long>(col_tile) * plan.blocks + seg.kb0) * 2 + half;
-            f32x2 run[64];
+            float run[128];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) run[i] = pack2(0.f, 0.f);
+            for (int i = 0; i < 128; ++i) run[i] = 0.f;
             float sx = 0.f, sw = 0.f;
             if (slot < live) {
                 sx = __ldcg(xs);
@@ -545,7 +545,6 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             }
             for (int kb = seg.kb0; kb < seg.kb1 && ok; ++kb) {
                 const float f = sx * sw;
-                const f32x2 f2 = pack2(f, f);
                 xs += kFp8RowsTile;
                 ws += 2;
                 if (slot < live && kb + 1 < seg.kb1) {
@@ -577,7 +576,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                             release();
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            run[c * 8 + i] = fma2(f2, pack2(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), run[c * 8 + i]);
+                            { run[c * 16 + 2 * i] = fmaf(f, __uint_as_float(v[c & 1][2 * i]), run[c * 16 + 2 * i]); run[c * 16 + 2 * i + 1] = fmaf(f, __uint_as_float(v[c & 1][2 * i + 1]), run[c * 16 + 2 * i + 1]); }
                     }
                 } else {
                     release();
@@ -587,7 +586,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             }
             if (!ok)
 #pragma unroll
-                for (int i = 0; i < 64; ++i) run[i] = pack2(__int_as_float(0x7FFFFFFF), __int_as_float(0x7FFFFFFF));
+                for (int i = 0; i < 128; ++i) run[i] = __int_as_float(0x7FFFFFFF);
             if (seg.kb1 - seg.kb0 < plan.blocks) {
                 // part of a tile: the last of its workers adds the parts up
                 const long long part = 2ll * 32 * plan.partial_rows;  // in float4
@@ -597,9 +596,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 if (slot < live)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        float4 v;
-                        unpack2(run[2 * i], v.x, v.y);
-                        unpack2(run[2 * i + 1], v.z, v.w);
+                        const float4 v = make_float4(run[4 * i], run[4 * i + 1], run[4 * i + 2], run[4 * i + 3]);
                         mine[static_cast<long long>(i) * plan.partial_rows] = v;
                     }
                 const int w0 = fp8_worker_of(plan, seg.tail * plan.blocks), w1 = fp8_worker_of(plan, (seg.tail + 1) * plan.blocks - 1);
@@ -610,7 +607,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 if (!sm.last) continue;
                 __threadfence();
 #pragma unroll
-                for (int i = 0; i < 64; ++i) run[i] = pack2(0.f, 0.f);
+                for (int i = 0; i < 128; ++i) run[i] = 0.f;
                 if (slot < live)
                     for (int w = w0; w <= w1; ++w) {
                         const float4 *theirs = reinterpret_cast<const float4 *>(p.partials) +
@@ -619,8 +616,10 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             const float4 v = __ldcg(theirs + static_cast<long long>(i) * plan.partial_rows);
-                            run[2 * i] = add2(run[2 * i], pack2(v.x, v.y));
-                            run[2 * i + 1] = add2(run[2 * i + 1], pack2(v.z, v.w));
+                            run[4 * i] += v.x;
+                            run[4 * i + 1] += v.y;
+                            run[4 * i + 2] += v.z;
+                            run[4 * i + 3] += v.w;
                         }
                     }
             }
@@ -632,7 +631,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 for (int i = 0; i < 8; ++i) {
                     float y[16];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) unpack2(run[8 * i + j], y[2 * j], y[2 * j + 1]);
+                    for (int j = 0; j < 16; ++j) y[j] = run[16 * i + j];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) y[j] *= factor;
                     if (v0 + 16 * i < p.V) fp8_store(p, row, v0 + 16 * i, y);
