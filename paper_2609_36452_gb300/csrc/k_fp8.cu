@@ -84,31 +84,22 @@ __global__ void k_fp8_pack_scales(const float *scales, float *packed, int rows, 
 
 // ------------------------------------------------------------------------------ activations
 
-// Eight numbers over a scale as e4m3 codes: the fp32 quotient, rounded.  A product with the reciprocal is at most 2 of
-// fp32's last places off that, and the code hangs on it only where it is as close to the middle between two codes (bit 19 of
-// the number set, those below it clear); there, and where e4m3's own steps do not get smaller any more (below 2^-6), it is
-// divided.  (A division each took a head of 126464 x 4096 from 300 us to 865.)
-__device__ __forceinline__ bool fp8_close(float t) {
-    const uint32_t b = __float_as_uint(t);
-    return ((b + 3u - 0x80000u) & 0xFFFFFu) <= 6u || (fabsf(t) < 0x1p-6f && t != 0.f);
-}
+// Eight numbers over a scale as e4m3 codes: the fp32 quotient, rounded.  Of a product with the rounded reciprocal, off by a last
+// place at most, the rest x - q s is exact, and q + (rest) / s rounded once is the quotient rounded (Markstein, IBM J. Res. Dev. 34,
+// 1990): three operations where a division is some fifteen (a head of 126464 x 4096 took 865 us with these).  The rest has to
+// stay above fp32's smallest number wherever a code is not 0, which blocks of tiny numbers do not give: they are divided.
 __device__ __forceinline__ uint2 fp8_codes(const float2 (&u)[4], float scale, float inverse) {
     float2 t[4];
-    bool close = !(scale >= 0x1p-100f);
+    if (scale >= 0x1p-60f && scale <= 0x1p100f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        t[i] = make_float2(u[i].x * inverse, u[i].y * inverse);
-        close |= fp8_close(t[i].x) || fp8_close(t[i].y);
-    }
-    if (close)
-#pragma unroll 1
         for (int i = 0; i < 4; ++i) {
-            const float2 from = i == 0 ? u[0] : i == 1 ? u[1] : i == 2 ? u[2] : u[3];
-            const float2 q = make_float2(from.x / scale, from.y / scale);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (k == i) t[k] = q;
+            const float qx = __fmul_rn(u[i].x, inverse), qy = __fmul_rn(u[i].y, inverse);
+            t[i] = make_float2(__fmaf_rn(__fmaf_rn(-qx, scale, u[i].x), inverse, qx), __fmaf_rn(__fmaf_rn(-qy, scale, u[i].y), inverse, qy));
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = make_float2(u[i].x / scale, u[i].y / scale);
+    }
     uint32_t h[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = __nv_cvt_float2_to_fp8x2(t[i], __NV_SATFINITE, __NV_E4M3);
