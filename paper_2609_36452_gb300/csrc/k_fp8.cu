@@ -783,56 +783,95 @@ struct Fp8QuantizeParams {
     float *scales;
 };
 
-// Blocks of 128 columns of kHigh rows.  16 lanes have 128 columns of a row; with kHigh = 1 that is a block, with 128 a CTA
-// has a block, whose numbers stay in registers (8 rows a thread) between its maximum and its codes.
-template <typename T, int kHigh>
-__global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantizeParams p) {
-    __shared__ float red[8];
+template <typename T, int n>
+__device__ __forceinline__ float largest_of(const Eight<T> (&x)[n]) {
+    float amax = 0.f;
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+        float2 u[4];
+        x[j].get(u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(fabsf(u[k].x), fabsf(u[k].y)));
+    }
+    return amax;
+}
+
+// Blocks of 128 columns of a row: 16 lanes have one.
+template <typename T>
+__global__ void __launch_bounds__(256) k_fp8_quantize_rows(const Fp8QuantizeParams p) {
     const int lanes = threadIdx.x >> 4, col = (threadIdx.x & 15) * 8, blocks = (p.cols + kFp8Block - 1) / kFp8Block;
-    constexpr int kRows = kHigh == 1 ? 1 : 8;
+    const long long n = static_cast<long long>(p.rows) * blocks;
     pdl_trigger();
     pdl_wait();
-    const long long rows = kHigh == 1 ? p.rows : (p.rows + kHigh - 1ll) / kHigh;
-    for (long long i = kHigh == 1 ? blockIdx.x * 16ll + lanes : blockIdx.x; i - lanes * (kHigh == 1) < rows * blocks;
-         i += kHigh == 1 ? gridDim.x * 16ll : gridDim.x) {
-        const bool live = i < rows * blocks;
-        const int block = static_cast<int>(i % blocks);
-        const long long row0 = kHigh == 1 ? i / blocks : i / blocks * kHigh + lanes;
-        Eight<T> x[kRows];
-        float amax = 0.f;
+    for (long long first = blockIdx.x * 16ll; first < n; first += gridDim.x * 16ll) {
+        const long long i = first + lanes, row = i / blocks;
+        const int at = static_cast<int>(i - row * blocks) * kFp8Block + col;
+        Eight<T> x[1];
+        if (i < n)
+            x[0].load(static_cast<const T *>(p.x) + row * p.x_stride, at, p.cols, p.x_align);
+        else
+            x[0].clear();
+        float amax = largest_of(x);
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
-            const long long row = row0 + j * 16;
-            if (live && row < p.rows)
-                x[j].load(static_cast<const T *>(p.x) + row * p.x_stride, block * kFp8Block + col, p.cols, p.x_align);
+        for (int o = 8; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        const float scale = amax / kFp8Most, by = scale > 0.f ? scale : 1.f;
+        if (i < n) {
+            float2 u[4];
+            x[0].get(u);
+            if (col == 0) p.scales[i] = scale;
+            store_codes(p.codes + row * p.codes_stride, at, p.cols, p.vec, fp8_codes(u, by, 1.f / by));
+        }
+    }
+}
+
+// Blocks of 128 x 128: a CTA has one, whose numbers stay in registers (8 rows a thread, 8 columns each) between its largest
+// and its codes, while the next one's are on their way.  (Without that, at two to four CTAs an SM: 370 to 330 us for a head of
+// 126464 x 4096.)
+template <typename T>
+__global__ void __launch_bounds__(256, 2) k_fp8_quantize_blocks(const Fp8QuantizeParams p) {
+    constexpr int kRows = kFp8Block / 16;
+    __shared__ float red[2][8];
+    const int lanes = threadIdx.x >> 4, col = (threadIdx.x & 15) * 8, blocks = (p.cols + kFp8Block - 1) / kFp8Block;
+    const long long n = (p.rows + kFp8Block - 1ll) / kFp8Block * blocks;
+    const auto load = [&](Eight<T> (&x)[kRows], long long i) {
+        const long long high = i / blocks;
+        const int at = static_cast<int>(i - high * blocks) * kFp8Block + col;
+        const int row = static_cast<int>(high) * kFp8Block + lanes;
+        const T *from = static_cast<const T *>(p.x) + row * p.x_stride;
+#pragma unroll
+        for (int j = 0; j < kRows; ++j, from += 16 * p.x_stride) {
+            if (row + 16 * j < p.rows)
+                x[j].load(from, at, p.cols, p.x_align);
             else
                 x[j].clear();
         }
+    };
+    pdl_trigger();
+    pdl_wait();
+    Eight<T> x[kRows], next[kRows];
+    load(x, blockIdx.x);
+    int turn = 0;
+    for (long long i = blockIdx.x; i < n; i += gridDim.x, turn ^= 1) {
+        if (i + gridDim.x < n) load(next, i + gridDim.x);
+        float amax = largest_of(x);
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
-            float2 u[4];
-            x[j].get(u);
+        for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        if ((threadIdx.x & 31) == 0) red[turn][threadIdx.x >> 5] = amax;
+        __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(fabsf(u[k].x), fabsf(u[k].y)));
-        }
-#pragma unroll
-        for (int o = kHigh == 1 ? 8 : 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        if (kHigh != 1) {
-            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < 8; ++w) amax = fmaxf(amax, red[w]);
-            __syncthreads();
-        }
+        for (int w = 0; w < 8; ++w) amax = fmaxf(amax, red[turn][w]);
         const float scale = amax / kFp8Most, by = scale > 0.f ? scale : 1.f, inverse = 1.f / by;
-        if (live && (kHigh == 1 ? col == 0 : threadIdx.x == 0)) p.scales[i] = scale;
+        if (threadIdx.x == 0) p.scales[i] = scale;
+        const long long high = i / blocks;
+        const int at = static_cast<int>(i - high * blocks) * kFp8Block + col;
+        const int row = static_cast<int>(high) * kFp8Block + lanes;
+        uint8_t *to = p.codes + row * p.codes_stride;
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
-            const long long row = row0 + j * 16;
+        for (int j = 0; j < kRows; ++j, to += 16 * p.codes_stride) {
             float2 u[4];
             x[j].get(u);
-            if (live && row < p.rows)
-                store_codes(p.codes + row * p.codes_stride, block * kFp8Block + col, p.cols, p.vec, fp8_codes(u, by, inverse));
+            if (row + 16 * j < p.rows) store_codes(to, at, p.cols, p.vec, fp8_codes(u, by, inverse));
+            x[j] = next[j];
         }
     }
 }
@@ -840,9 +879,12 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantizeParams p)
 template <typename T>
 cudaError_t launch_quantize(const Fp8QuantizeParams &p, int high, int num_sms, cudaStream_t s) {
     const long long blocks = (p.cols + kFp8Block - 1ll) / kFp8Block;
-    const long long ctas = high == 1 ? (p.rows * blocks + 15) / 16 : (p.rows + high - 1ll) / high * blocks;
-    const dim3 grid(static_cast<unsigned>(std::min<long long>(ctas, num_sms * 32ll)));
-    return high == 1 ? launch_pdl(k_fp8_quantize<T, 1>, grid, dim3(256), 0, s, p) : launch_pdl(k_fp8_quantize<T, 128>, grid, dim3(256), 0, s, p);
+    if (high == 1)
+        return launch_pdl(k_fp8_quantize_rows<T>, dim3(static_cast<unsigned>(std::min<long long>((p.rows * blocks + 15) / 16, num_sms * 32ll))),
+                          dim3(256), 0, s, p);
+    return launch_pdl(k_fp8_quantize_blocks<T>,
+                      dim3(static_cast<unsigned>(std::min<long long>((p.rows + kFp8Block - 1ll) / kFp8Block * blocks, num_sms * 2ll))), dim3(256), 0,
+                      s, p);
 }
 
 }  // namespace
