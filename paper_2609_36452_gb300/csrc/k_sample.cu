@@ -27,6 +27,8 @@ namespace {
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleMaxCluster = 8;
+constexpr int kSampleResident = 1024;      // threads of an SM: 64 registers each
+constexpr int kSampleSteps = kSampleMaxCluster * kSampleWarps / 32;  // in which a warp looks at what every warp of the row has left
 constexpr int kSampleTable = 512;
 constexpr int kSampleBins = 4096;          // of the first histogram
 constexpr int kBinParts = 256;             // parts of a bin, of which the mean is kept
@@ -96,6 +98,48 @@ __device__ __forceinline__ uint4 keep_allowed(const uint4 &v, uint32_t bits) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Largest and smallest of a vector's numbers, pairwise for 16-bit types; the largest is NaN where one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b, __nv_bfloat16) {
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b, __half) {
+    const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b, float) {
+    return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+}
+__device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b, __nv_bfloat16) {
+    const __nv_bfloat162 r = __hmin2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+__device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b, __half) {
+    const __half2 r = __hmin2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+__device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b, float) {
+    return __float_as_uint(fminf(__uint_as_float(a), __uint_as_float(b)));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t vec_max(const uint4 &v) {
+    return pair_max(pair_max(v.x, v.y, T()), pair_max(v.z, v.w, T()), T());
+}
+template <typename T>
+__device__ __forceinline__ uint32_t vec_min(const uint4 &v) {
+    return pair_min(pair_min(v.x, v.y, T()), pair_min(v.z, v.w, T()), T());
+}
+__device__ __forceinline__ float2 pair_values(uint32_t v, float) { return make_float2(__uint_as_float(v), __uint_as_float(v)); }
+__device__ __forceinline__ float2 pair_values(uint32_t v, __nv_bfloat16) {
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+__device__ __forceinline__ float2 pair_values(uint32_t v, __half) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+
 // Tokens [v0, v0 + row.V) of a row.  Resident: a copy in shared memory, at the same distance from a 16-byte boundary, in which
 // tokens that are not allowed are -infinity.
 template <typename T, bool kResident>
@@ -125,9 +169,10 @@ struct Slice {
     }
     __device__ __forceinline__ int loose() const { return row.V - row.vecs * N; }  // tokens outside vectors
     __device__ __forceinline__ int loose_at(int i) const { return i < row.peel ? i : i + row.vecs * N; }
-    // f(logits, first token, how many) for every vector, and every token outside of them (then other logits are -infinity).
+    // f(logits, first token) for every vector with a logit of `least` or more, and every token outside of vectors (then other
+    // logits are -infinity).
     template <typename F>
-    __device__ __forceinline__ void each_vec(F f) const {
+    __device__ __forceinline__ void each_vec(float least, F f) const {
         constexpr int kAhead = kResident ? 1 : 3;  // vectors on their way from L2 meanwhile
         const int pieces = row.vecs + loose();
         uint4 raw[kAhead];
@@ -140,18 +185,24 @@ struct Slice {
         for (int i = threadIdx.x; i < pieces; i += kSampleThreads) {
             float z[N];
             int first = row.peel + i * N;
+            uint4 now;
+            if (kResident) {
+                if (i < row.vecs) now = *reinterpret_cast<const uint4 *>(buf + first * sizeof(T));
+            } else {
+                if (i < row.vecs) now = allowed_vec(raw[0], i);
+#pragma unroll
+                for (int a = 0; a + 1 < kAhead; ++a) raw[a] = raw[a + 1];
+                if (i + kAhead * kSampleThreads < row.vecs) raw[kAhead - 1] = global_vec(i + kAhead * kSampleThreads);
+            }
             if (i < row.vecs) {
-                unpack(kResident ? *reinterpret_cast<const uint4 *>(buf + first * sizeof(T)) : allowed_vec(raw[0], i), z, T());
+                const float2 most = pair_values(vec_max<T>(now), T());
+                if (fmaxf(most.x, most.y) < least) continue;
+                unpack(now, z, T());
             } else {
                 first = loose_at(i - row.vecs);
                 z[0] = at(first);
 #pragma unroll
                 for (int k = 1; k < N; ++k) z[k] = kNoLogit;
-            }
-            if (!kResident) {
-#pragma unroll
-                for (int a = 0; a + 1 < kAhead; ++a) raw[a] = raw[a + 1];
-                if (i + kAhead * kSampleThreads < row.vecs) raw[kAhead - 1] = global_vec(i + kAhead * kSampleThreads);
             }
             f(z, v0 + first);
         }
@@ -185,36 +236,51 @@ struct Slice {
 };
 static_assert(kSampleThreads >= 2 * 8, "tokens outside vectors are a thread's each");
 
-// Of a thread's part of a slice: largest and smallest logit, the number of those that are -infinity, and about the sum of
-// the weights relative to the largest (free of charge: the row is on its way from HBM meanwhile).  The sum is no number where a
-// logit is NaN or +infinity.
+// Of a thread's part of a slice: the largest allowed logit, the smallest of any (-infinity if there is one: then the finite ones
+// have to be counted), the number of tokens that are not allowed, and about the sum of the weights relative to the
+// largest.  The sum is no number where an allowed logit is NaN or +infinity.
+template <typename T>
 struct SampleRange {
-    float top = kLowest, low = -kNoLogit, sum = 0.f;
-    int gone = 0;
-    template <int n>
-    __device__ __forceinline__ void add(const float (&z)[n], float c) {
-        float most = top, least = z[0];
+    uint32_t most, least;  // of pairs
+    float top = kLowest, sum = 0.f;
+    int barred = 0;
+    __device__ SampleRange() : most(no_logit_pair(T())), least(no_logit_pair(T()) & 0x7FFF7FFFu) {
+        if (sizeof(T) == 4) least = 0x7F800000u;
+    }
+    __device__ __forceinline__ void add(const uint4 &raw, const uint4 &allowed, bool weigh, float c) {
+        constexpr int N = Row<T>::kVec;
+        const uint32_t here = vec_max<T>(allowed);
+        most = pair_max(most, here, T());
+        least = pair_min(least, vec_min<T>(raw), T());
+        if (weigh) {
+            const float2 two = pair_values(here, T());
+            const float larger = max_nan(two.x, two.y);
+            if (larger > top) {
+                sum *= ex2((top - larger) * c);
+                top = larger;
+            }
+            float z[N];
+            unpack(allowed, z, T());
 #pragma unroll
-        for (int k = 0; k < n; ++k) {
-            most = fmaxf(most, z[k]);
-            least = fminf(least, z[k]);
+            for (int k = 0; k < N; ++k) sum += ex2((z[k] - top) * c);
         }
-        if (most > top) {
-            sum *= ex2((top - most) * c);
-            top = most;
-        }
-        if (least < kLowest)
-#pragma unroll
-            for (int k = 0; k < n; ++k) gone += z[k] < kLowest;
-        low = fminf(low, least);
-#pragma unroll
-        for (int k = 0; k < n; ++k) sum += ex2((z[k] - top) * c);
+    }
+    __device__ __forceinline__ void end(bool weigh) {
+        const float2 two = pair_values(most, T());
+        const float larger = max_nan(two.x, two.y);
+        if (!(larger < -kNoLogit)) sum = __int_as_float(0x7FFFFFFF);
+        top = fmaxf(larger, kLowest);
+    }
+    __device__ __forceinline__ float low() const {
+        const float2 two = pair_values(least, T());
+        return fminf(two.x, two.y);
     }
 };
+// Goes through the slice, and copies it where it is resident.
 template <typename T, bool kResident>
-__device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s, float c) {
+__device__ __forceinline__ SampleRange<T> load_slice(const Slice<T, kResident> &s, bool weigh, float c) {
     constexpr int N = Row<T>::kVec, kUnroll = 4;
-    SampleRange r;
+    SampleRange<T> r;
     for (int i = threadIdx.x; i < s.row.vecs; i += kSampleThreads * kUnroll) {
         uint4 raw[kUnroll];
 #pragma unroll
@@ -224,24 +290,33 @@ __device__ __forceinline__ SampleRange load_slice(const Slice<T, kResident> &s, 
         for (int u = 0; u < kUnroll; ++u) {
             const int at = i + u * kSampleThreads;
             if (at < s.row.vecs) {
-                raw[u] = s.allowed_vec(raw[u], at);
-                if (kResident) *reinterpret_cast<uint4 *>(s.buf + (s.row.peel + at * N) * sizeof(T)) = raw[u];
-                float z[N];
-                unpack(raw[u], z, T());
-                r.add(z, c);
+                uint4 allowed = raw[u];
+                if (s.mask) {
+                    const uint32_t bits = allowed_bits(s.mask, s.v0 + s.row.peel + at * N, s.words);
+                    allowed = keep_allowed<T>(allowed, bits);
+                    r.barred += N - __popc(bits & ((1u << N) - 1));
+                }
+                if (kResident) *reinterpret_cast<uint4 *>(s.buf + (s.row.peel + at * N) * sizeof(T)) = allowed;
+                r.add(raw[u], allowed, weigh, c);
             }
         }
     }
     if (static_cast<int>(threadIdx.x) < s.loose()) {
         const int j = s.loose_at(threadIdx.x);
-        const float z[1] = {s.global_at(j)};
-        if (kResident) {
-            const uint32_t none = no_logit_pair(T());
-            T *to = reinterpret_cast<T *>(s.buf) + j;
-            *to = z[0] == kNoLogit ? *reinterpret_cast<const T *>(&none) : s.row.p[j];
-        }
-        r.add(z, c);
+        const uint32_t none = no_logit_pair(T());
+        const T no_logit = *reinterpret_cast<const T *>(&none), x = s.row.p[j];
+        const bool allowed = !s.mask || (s.mask[(s.v0 + j) >> 5] >> ((s.v0 + j) & 31) & 1u);
+        alignas(16) T kept[N], any[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) kept[k] = no_logit;
+        kept[0] = allowed ? x : no_logit;
+#pragma unroll
+        for (int k = 0; k < N; ++k) any[k] = x;
+        if (kResident) reinterpret_cast<T *>(s.buf)[j] = kept[0];
+        r.barred += !allowed;
+        r.add(*reinterpret_cast<const uint4 *>(any), *reinterpret_cast<const uint4 *>(kept), weigh, c);
     }
+    r.end(weigh);
     return r;
 }
 
@@ -319,19 +394,24 @@ struct SampleWeights {
         k = __float_as_int(t);
         return __float2ll_rn(__fsub_rn(y, __fsub_rn(t, kShift)) * 0x1p52f) + __float2ll_rn(fmaf(d, c_lo, fmaf(d, c_hi, -y)) * 0x1p52f);
     }
-    // The same weight with every step in 64 bits, right to some 2^-42.
-    __device__ __noinline__ uint64_t in_64_bits(float z, int bits, const SampleTable *table) const {
-        int k;
-        const int64_t r = rest64(z - A, k) - rest64_top;
-        k -= k_top;
+    // 2^(r + k mod 512 / 512) in units of 2^-52, r in these too.
+    static __device__ __forceinline__ uint64_t power(int64_t r, int k, const SampleTable *table) {
         const int64_t x = __mul64hi(r << 8, 0x58B90BFBE8E7BCD6ll) >> 7;  // r ln 2: ln 2 in units of 2^-63
         const float xf = static_cast<float>(x) * 0x1p-52f;
         const int64_t p = x + (__mul64hi(x << 6, x << 6) >> 1) + __float2ll_rn(xf * xf * xf * (0.16666667f + xf * 0.041666668f) * 0x1p52f);
         const int at = k & (kSampleTable - 1);
         const int64_t whole = (static_cast<int64_t>(table->v[at]) << 21) + table->rest[at];
-        const uint64_t m = static_cast<uint64_t>(whole + __mul64hi(whole << 5, p << 7));  // 2^52 to 2^53
+        return static_cast<uint64_t>(whole + __mul64hi(whole << 5, p << 7));
+    }
+    // The same weight with every step in 64 bits, right to some 2^-42.
+    __device__ __noinline__ uint64_t in_64_bits(float z, int bits, const SampleTable *table) const {
+        if (!(z - A > least)) return 0;
+        int k;
+        const int64_t r = rest64(z - A, k) - rest64_top;
+        k -= k_top;
+        uint64_t m = power(r, k, table);  // 2^52 to 2^53
         const int down = 52 - bits - (k >> 9);
-        return down > 0 ? (m >> (down - 1)) + 1 >> 1 : m << -down;
+        return down > 0 ? (m >> min(down - 1, 63)) + 1 >> 1 : m << -down;
     }
     // With the big ones in 64 bits.
     __device__ __forceinline__ uint64_t exact_of(float z, int bits, const SampleTable &table) const {
@@ -339,6 +419,23 @@ struct SampleWeights {
         return of(z, bits, table.v);
     }
 };
+
+// T ln m, m in (0, 1], as the sum of two floats: logf's number l, and what e^l, in 64 bits, lacks of m.
+__device__ __forceinline__ float2 scaled_log(float T, float m, const SampleTable *table) {
+    SampleWeights w;
+    w.set_temperature(1.f);
+    const float l = logf(m);
+    int k;
+    const int64_t r = w.rest64(l, k);
+    k -= __float_as_int(SampleWeights::kShift);
+    const int64_t e = static_cast<int64_t>(SampleWeights::power(r, k, table));  // times 2^((k >> 9) - 52)
+    const uint32_t b = __float_as_uint(m), field = b >> 23;
+    const int64_t whole = field ? (b & 0x7FFFFFu) | 0x800000u : b;
+    const int up = static_cast<int>(max(field, 1u)) - 150 + 52 - (k >> 9);  // some 29
+    const float off = static_cast<float>((whole << up) - e) / static_cast<float>(e);
+    const float high = T * l;
+    return make_float2(high, fmaf(T, l, -high) + T * off);
+}
 
 // ------------------------------------------------------------------------------ shared memory
 
@@ -395,7 +492,7 @@ struct SampleShared {
     uint64_t bin_mass;
     int above_count, bin_count, bin;
     int tie;                   // the token of a tie that the border falls on
-    double min_log;            // T log(min_p): min-p keeps logits from so far below the largest on
+    float edge;                // the smallest logit that min-p keeps
     // the quick way
     SampleFound found[5];
     float edges[4];            // the smallest logits before the plan's places
@@ -438,6 +535,21 @@ __device__ __forceinline__ void row_sync(int ranks) {
         cluster_sync();
     else
         __syncthreads();
+}
+
+// Of all threads of the row, in each of them.
+__device__ __forceinline__ int sum_of_row(SampleShared &sm, int ranks, int mine) {
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if ((threadIdx.x & 31) == 0) sm.binned[threadIdx.x >> 5] = mine;
+    row_sync(ranks);
+    int all = 0;
+#pragma unroll
+    for (int i = 0; i < kSampleSteps; ++i) {
+        const int lane = threadIdx.x & 31, q = 32 / kSampleWarps * i + lane / kSampleWarps;
+        if (q < ranks) all += static_cast<int>(ld_cluster_u32(peer(&sm.binned[lane % kSampleWarps], q)));
+    }
+    row_sync(ranks);
+    return __reduce_add_sync(0xffffffffu, all);
 }
 
 // ------------------------------------------------------------------------------ any border, in four passes
@@ -921,8 +1033,8 @@ __device__ __forceinline__ SampleBins make_bins(SampleShared &sm, const uint32_t
     int n_before = 0, n_all = 0;
     float m_before = 0.f, m_all = 0.f;
 #pragma unroll
-    for (int i = 0; i < kSampleMaxCluster / 2; ++i) {
-        const int q = 2 * i + lane / kSampleWarps, w = lane % kSampleWarps;
+    for (int i = 0; i < kSampleSteps; ++i) {
+        const int q = 32 / kSampleWarps * i + lane / kSampleWarps, w = lane % kSampleWarps;
         if (q < ranks) {
             const int nw = static_cast<int>(ld_cluster_u32(peer(&sm.counts[w], q)));
             const float mw = __uint_as_float(ld_cluster_u32(peer(&sm.sums[w], q)));
@@ -1050,14 +1162,6 @@ __device__ __forceinline__ void list_token(int *listed, uint64_t *list, int room
     if (at < room) list[at] = sample_entry(z, v);
 }
 
-template <int n>
-__device__ __forceinline__ float largest(const float (&z)[n]) {
-    float most = z[0];
-#pragma unroll
-    for (int k = 1; k < n; ++k) most = fmaxf(most, z[k]);
-    return most;
-}
-
 // A first histogram of the row over 4096 bins, equally wide in the logit, says in which one or two of them each border is;
 // a second pass adds the weights before these up, exactly, and lists the tokens in them; the lists go to the first CTA's shared
 // memory, which sorts them (solve_lists).  With top-k all tokens that may be kept are listed.  False: the row is not like that (so
@@ -1073,8 +1177,7 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
     const float span = fminf(fminf(kBinOctaves / c, top - fmaxf(low, least)), 3e38f);
     const float scale = span > 0.f ? fminf((kSampleBins * kBinParts - kBinParts / 2) / span, 1e38f) : 0.f;
     int binned = 0;
-    s.each_vec([&](const auto &z, int) {
-        if (largest(z) < least) return;
+    s.each_vec(least, [&](const auto &z, int) {
 #pragma unroll
         for (int k = 0; k < S::N; ++k)
             if (z[k] >= least) {
@@ -1085,16 +1188,7 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
                 }
             }
     });
-    binned = __reduce_add_sync(0xffffffffu, binned);
-    if (lane == 0) sm.binned[warp] = binned;
-    row_sync(ranks);
-    int expected = 0;
-#pragma unroll
-    for (int i = 0; i < kSampleMaxCluster / 2; ++i) {
-        const int q = 2 * i + lane / kSampleWarps;
-        if (q < ranks) expected += static_cast<int>(ld_cluster_u32(peer(&sm.binned[lane % kSampleWarps], q)));
-    }
-    expected = __reduce_add_sync(0xffffffffu, expected);
+    const int expected = sum_of_row(sm, ranks, binned);
     const SampleBins bins = make_bins(sm, hist, own, ranks, rank, scale > 0.f ? c / scale : 0.f);
     SamplePlan plan = plan_borders(sm, bins, ranks, top, edge, scale, sum, expected, top_k, top_p, u);
     if (plan.slow) {
@@ -1109,6 +1203,7 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
         sm.plan = plan;
         sm.w.set_floor(plan.bits);
         sm.w.set_big(plan.sum);
+        if (plan.gather) sm.w.big = kNoLogit;  // (few tokens: all of them in 64 bits)
     }
     __syncthreads();
     uint64_t *list = reinterpret_cast<uint64_t *>(hist), *cut_list = list + kSampleList / 2;
@@ -1128,15 +1223,13 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
         __syncthreads();
     }
     if (plan.gather) {
-        s.each_vec([&](const auto &z, int v) {
-            if (largest(z) < draw1) return;
+        s.each_vec(draw1, [&](const auto &z, int v) {
 #pragma unroll
             for (int k = 0; k < S::N; ++k)
                 if (z[k] >= draw1) list_token(&sm.listed[0], list, kSampleList, z[k], v + k);
         });
     } else if (plan.by_edge) {
-        s.each_vec([&](const auto &z, int v) {
-            if (largest(z) < edge) return;
+        s.each_vec(edge, [&](const auto &z, int v) {
             uint32_t kept = 0;
 #pragma unroll
             for (int k = 0; k < S::N; ++k)
@@ -1155,7 +1248,7 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
     } else {
         const SampleWeights w = sm.w;
         const float from = plan.by_list ? cut0 : kLowest;
-        s.each_vec([&](const auto &z, int v) {
+        s.each_vec(kNoLogit, [&](const auto &z, int v) {
             uint32_t kept = 0;
             uint32_t special = 0;  // tokens that are listed, or weighed in 64 bits
 #pragma unroll
@@ -1290,7 +1383,7 @@ __device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, u
 __device__ __forceinline__ float clamp_temperature(float T) { return fminf(fmaxf(T, 1.45e-30f), 1.44e37f); }
 
 template <typename T, bool kResident>
-__global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const SampleParams p) {
+__global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThreads) k_sample_limits(const SampleParams p) {
     extern __shared__ __align__(16) uint8_t buffer[];
     __shared__ SampleShared sm;
     const int ranks = static_cast<int>(cluster_nctarank()), rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -1317,13 +1410,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     const int top_k = p.a.top_k ? p.a.top_k[r] : 0;
     uint32_t *out = p.a.out_allowed ? reinterpret_cast<uint32_t *>(p.a.out_allowed) + r * p.words : nullptr;
     const float T_used = clamp_temperature(T_row), c = 1.44269502f / T_used;
-    if (threadIdx.x == 0) {
-        sm.w.set_temperature(T_used);
-        sm.min_log = min_p > 0.f ? T_used * log(static_cast<double>(min_p)) : 0.0;  // (on its way while the others load)
-    }
-    SampleRange range = load_slice(s, c);
-    float top = range.top, low = fmaxf(range.low, kLowest);  // (of a row with -infinities: the lowest there is)
-    float least_top = top;
+    if (threadIdx.x == 0) sm.w.set_temperature(T_used);
+    const bool weigh = T_row != 0.f && !(top_k > 0 && top_k <= kSampleList);
+    const SampleRange<T> range = load_slice(s, weigh, c);
+    float top = range.top, low = range.low(), least_top = top;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -1333,7 +1423,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
     float sum = range.sum * ex2((range.top - top) * c);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    int finite = __reduce_add_sync(0xffffffffu, range.gone);  // those that are not, here
+    int finite = __reduce_add_sync(0xffffffffu, range.barred);  // those that are not, here
     if (lane == 0) {
         sm.range[0][warp] = top;
         sm.range[1][warp] = low;
@@ -1342,14 +1432,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         sm.finite[warp] = finite;
     }
     row_sync(ranks);
-    float tops[kSampleMaxCluster / 2], sums[kSampleMaxCluster / 2], least_warp = -kNoLogit;
+    float tops[kSampleSteps], sums[kSampleSteps], least_warp = -kNoLogit;
     top = kLowest;
     low = least_top = -kNoLogit;
     finite = 0;
     sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kSampleMaxCluster / 2; ++i) {  // two CTAs' warps at a time
-        const int q = 2 * i + lane / kSampleWarps, w = lane % kSampleWarps;
+    for (int i = 0; i < kSampleSteps; ++i) {
+        const int q = 32 / kSampleWarps * i + lane / kSampleWarps, w = lane % kSampleWarps;
         tops[i] = kLowest;
         sums[i] = 0.f;
         if (q < ranks) {
@@ -1370,11 +1460,18 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         least_warp = fminf(least_warp, __shfl_xor_sync(0xffffffffu, least_warp, o));
     }
 #pragma unroll
-    for (int i = 0; i < kSampleMaxCluster / 2; ++i) sum += sums[i] * ex2((tops[i] - top) * c);
+    for (int i = 0; i < kSampleSteps; ++i) sum += sums[i] * ex2((tops[i] - top) * c);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     finite = p.a.V - __reduce_add_sync(0xffffffffu, finite);
-    static_assert(kSampleWarps == 16, "two CTAs' warps are a warp's lanes");
+    if (low == kNoLogit && sum == sum) {  // of the allowed ones some may be -infinity
+        int count = 0;
+        s.each_vec(kLowest, [&](const auto &z, int) {
+#pragma unroll
+            for (int k = 0; k < Row<T>::kVec; ++k) count += z[k] >= kLowest;
+        });
+        finite = sum_of_row(sm, ranks, count);
+    }
     const bool ok = fabsf(sum) < -kNoLogit && finite > 0 && T_row >= 0.f && (T_row == 0.f || (p.a.uniform && u >= 0.f && u < 1.f)) &&
                     top_p == top_p && min_p <= 1.f;
     bool done = false;  // the mask is written
@@ -1386,21 +1483,51 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample_limits(const Sampl
         if (threadIdx.x == 0) sm.tie = 0x7FFFFFFF;
         row_sync(ranks);
         cut = {order_key(top), 0x7FFFFFFF};
-        s.each([&](float z, int v) {
-            if (order_key(z) == cut.key) atomicMin(&sm.tie, v);
+        s.each_vec(top, [&](const auto &z, int v) {
+#pragma unroll
+            for (int k = 0; k < Row<T>::kVec; ++k)
+                if (z[k] == top) atomicMin(&sm.tie, v + k);
         });
         row_sync(ranks);
         for (int q = 0; q < ranks; ++q) cut.last = min(cut.last, static_cast<int>(ld_cluster_u32(peer(&sm.tie, q))));
         if (threadIdx.x == 0) sm.result = {0, cut, cut.last, 1, 1.f};
     } else {
-        if (threadIdx.x == 0) sm.w.set_top(top);
+        const bool by_k = top_k > 0 && top_k < finite;
+        if (threadIdx.x == 0) {
+            sm.w.set_top(top);
+            sm.edge = kNoLogit;
+            if (min_p > 0.f) {
+                // the first float from top + T ln min_p on
+                const float2 log = scaled_log(T_used, min_p, &sm.table);
+                const float near = __fadd_rn(top, log.x), part = __fsub_rn(near, top);
+                const float rest = __fadd_rn(__fsub_rn(top, __fsub_rn(near, part)), __fsub_rn(log.x, part));  // what the sum has lost
+                if (near > kNoLogit) sm.edge = __fadd_ru(near, __fadd_rn(rest, log.y));
+            }
+        }
+        if (!weigh && !by_k) {  // a k that keeps all of few tokens
+            float mine = 0.f;
+            s.each([&](float z, int) { mine += ex2((z - top) * c); });
+#pragma unroll
+            for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+            row_sync(ranks);
+            if (lane == 0) sm.range[2][warp] = mine;
+            row_sync(ranks);
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSampleSteps; ++i) {
+                const int q = 32 / kSampleWarps * i + lane / kSampleWarps;
+                if (q < ranks) sum += __uint_as_float(ld_cluster_u32(peer(&sm.range[2][lane % kSampleWarps], q)));
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        }
+        if (by_k) sum = static_cast<float>(top_k);  // more than that it is not
         __syncthreads();
-        const float edge = min_p > 0.f ? __double2float_ru(top + sm.min_log) : kNoLogit;
+        const float edge = sm.edge;
         // Logits that no border can be at.  Top-k: a warp's (or a thread's) largest logit is one of the row's, so that the least of
         // so many of them is not above the k-th.  Top-p, or the draw where there is no limit: what follows a border holds
         // 1 - q of the sum in V tokens at most, and none of these weighs more than the border's.  (2^-12 for the bins' error.)
         float least = kLowest;
-        const bool by_k = top_k > 0 && top_k < finite;
         if (by_k) {
             if (top_k <= ranks * kSampleWarps)
                 least = least_warp;

@@ -235,3 +235,31 @@ def test_random_rows():
         r = lambda lo, hi: (lo + (hi - lo) * torch.rand(rows, generator=g)).tolist()  # noqa: E731
         run_and_check(z, r(0, 1), r(0.3, 3.0), torch.randint(0, V, (rows,), generator=g).tolist() if i % 2 else None, r(0.3, 1.1),
                       (10 ** (-6 * torch.rand(rows, generator=g))).tolist() if i > 2 else None)
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+def test_min_p_at_its_border(kind):
+    """Logits one step of the type above and below the largest one plus T ln min_p, for many min_p."""
+    rows, V = 64, 300
+    g = gen(21)
+    m = torch.cat([torch.exp(-20 * torch.rand(60, generator=g)), torch.tensor([1.0, 1e-38, 1e-44, 2.0 ** -20])]).float()
+    T = 0.5 + torch.rand(rows, generator=g).float()
+    top = 10 + torch.rand(rows, generator=g)
+    z = torch.full((rows, V), -300.0, dtype=TYPES[kind])
+    z[:, 0] = top.to(z.dtype)
+    for r in range(rows):
+        edge = (z[r, 0].double() + T[r].double() * torch.log(m[r].double())).to(z.dtype)
+        step = edge
+        for i in range(1, 40):
+            z[r, i] = step
+            step = torch.nextafter(step.float(), torch.tensor(100.0)).to(z.dtype) if kind == "f32" else step + abs(step) * 2.0 ** -7
+        step = edge
+        for i in range(40, 80):
+            z[r, i] = step
+            step = torch.nextafter(step.float(), torch.tensor(-1000.0)).to(z.dtype) if kind == "f32" else step - abs(step) * 2.0 ** -7
+    z = torch.minimum(z, z[:, :1])
+    run_and_check(z, [0.999] * rows, T.tolist(), None, None, m.tolist())
+    run_and_check(z, [0.999] * rows, T.tolist(), [70] * rows, None, m.tolist())
+    run_and_check(z, [0.5] * rows, T.tolist(), [V + 5] * rows, [0.9] * rows, m.tolist())
