@@ -261,8 +261,14 @@ struct SampleRange {
             }
             float z[N];
             unpack(allowed, z, T());
+            float part[N / 2];
 #pragma unroll
-            for (int k = 0; k < N; ++k) sum += ex2((z[k] - top) * c);
+            for (int k = 0; k < N / 2; ++k) part[k] = ex2((z[k] - top) * c) + ex2((z[k + N / 2] - top) * c);
+#pragma unroll
+            for (int k = N / 4; k; k >>= 1)
+#pragma unroll
+                for (int i = 0; i < k; ++i) part[i] += part[i + k];
+            sum += part[0];
         }
     }
     __device__ __forceinline__ void end(bool weigh) {
@@ -482,7 +488,7 @@ struct SampleShared {
         uint64_t mass[256];
         uint32_t count[256];
     } *x;
-    float range[4][kSampleWarps];  // largest, smallest, sum, least of the threads' largest
+    float range[5][kSampleWarps];  // largest, smallest, sum, n-th of the threads' largest, weights of these
     int finite[kSampleWarps], binned[kSampleWarps];
     float sums[kSampleWarps];
     float sum;
@@ -504,6 +510,7 @@ struct SampleShared {
     int part_count[kSampleMaxCluster];
     uint64_t warp_sums[3][kSampleWarps];
     SampleHit hit;
+    int first;                 // whether the short way has found the token
 };
 
 __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
@@ -1378,6 +1385,107 @@ __device__ __forceinline__ bool solve_lists(SampleShared &sm, uint64_t *lists, u
     return good;
 }
 
+// ------------------------------------------------------------------------------ the short way
+
+// Lane j has the j-th largest of the warp's numbers, from 0.
+__device__ __forceinline__ float sort_warp(float x) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j; j >>= 1) {
+            const float y = __shfl_xor_sync(0xffffffffu, x, j);
+            x = (((lane & k) == 0) == ((lane & j) == 0)) ? fmaxf(x, y) : fminf(x, y);
+        }
+    return x;
+}
+
+// What the short way takes a row for.
+struct SampleShort {
+    bool by_k, by_sum;  // top-k; top-p without it.  Else min-p alone
+    bool whole;         // no kept token is below `from`
+    float from;         // logits from there on are listed
+    int room;           // for so many
+};
+
+// Every token that may be kept is among the largest few of most rows: of those that ask for the first k, or whose probable
+// tokens hold top_p, or whose min_p has few above it.  They are listed in the first CTA's shared memory.  -1: too many, or
+// they hold too little; else their number.  `mask`, which the kept ones' bits go to, is cleared.
+template <typename S>
+__device__ __forceinline__ int list_likely(const S &s, SampleShared &sm, const SampleShort &way, uint64_t *list, int ranks, int rank, float top, float c,
+                                           float sum, float top_p, uint32_t *out) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float from = way.from;
+    float mass = 0.f;
+    s.each_vec(from, [&](const auto &z, int v) {
+#pragma unroll
+        for (int k = 0; k < S::N; ++k)
+            if (z[k] >= from) {
+                mass += ex2((z[k] - top) * c);
+                const int at = atomicAdd(&sm.listed[0], 1);
+                if (at < kSampleList) list[at] = sample_entry(z[k], v + k);
+            }
+    });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+    if (lane == 0) sm.sums[warp] = mass;
+    row_sync(ranks);
+    mass = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSampleSteps; ++i) {
+        const int q = 32 / kSampleWarps * i + lane / kSampleWarps;
+        if (q < ranks) mass += __uint_as_float(ld_cluster_u32(peer(&sm.sums[lane % kSampleWarps], q)));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+    const int theirs = lane < ranks ? static_cast<int>(ld_cluster_u32(peer(&sm.listed[0], lane))) : 0;
+    const int n = __reduce_add_sync(0xffffffffu, theirs), base = __reduce_add_sync(0xffffffffu, lane < rank ? theirs : 0);
+    if (n > way.room || (way.by_sum && !way.whole && mass < (top_p + 0x1p-10f) * sum)) return -1;
+    if (rank != 0) {
+        const uint32_t to = peer(list, 0) + base * 8;
+        for (int i = threadIdx.x; i < sm.listed[0]; i += kSampleThreads) st_cluster_u64(to + i * 8, list[i]);
+    }
+    if (out)
+        for (int i = threadIdx.x; i < (s.row.V + 31) / 32; i += kSampleThreads) out[s.v0 / 32 + i] = 0;
+    return n;
+}
+
+// The token from a list of n: by the row's first CTA.  A sum of all weights that is only known to lie within `off` of `sum` decides
+// as long as both ends do the same; false where they do not.
+__device__ __forceinline__ bool solve_likely(SampleShared &sm, const SampleShort &way, uint64_t *list, int n, uint64_t *upto, float edge, int top_k,
+                                             float sum, float off, float top_p, float u, uint32_t *out) {
+    const int bits = min(54, 59 - ilogbf(way.by_sum ? sum : static_cast<float>(kSampleList)));
+    if (threadIdx.x == 0) {
+        sm.w.set_floor(bits);
+        sm.w.big = kNoLogit;  // (few tokens: all of them in 64 bits)
+    }
+    sort_entries(list, n, 0);
+    if (way.by_k) n = min(n, top_k);
+    const uint64_t mine = add_up(list, n, upto, bits, sm);
+    uint64_t low = ~0ull, high = ~0ull;
+    if (top_p < 1.f) {
+        const float unit = ldexpf(1.f, bits);
+        low = high = times_fraction(mine, fmaxf(top_p, 0.f), true);
+        if (way.by_sum) {
+            low = times_fraction(__float2ull_rd(sum * (1.f - off) * unit), fmaxf(top_p, 0.f), true);
+            high = times_fraction(__float2ull_ru(sum * (1.f + off) * unit), fmaxf(top_p, 0.f), true);
+        }
+    }
+    const SampleHit end = find_entry(list, upto, n, 0, low, false, true, edge, sm);
+    const bool below = end.at < n && key_value(~static_cast<uint32_t>(end.entry >> 32)) < edge;
+    if (way.by_sum && !below && (end.at < n ? end.before < high : !way.whole)) return false;
+    if (out)
+        for (int i = threadIdx.x; i < end.at; i += kSampleThreads) {
+            const int v = static_cast<int>(list[i] & 0xFFFFFFFFu);
+            atomicOr(&out[v >> 5], 1u << (v & 31));
+        }
+    const SampleHit hit = find_entry(list, upto, end.at, 0, times_fraction(end.before, u, false), true, false, edge, sm);
+    if (threadIdx.x == 0)
+        sm.result = {0, {}, static_cast<int>(hit.entry & 0xFFFFFFFFu), end.at, quotient(hit.w, end.before)};
+    __syncthreads();
+    return true;
+}
+
 // ------------------------------------------------------------------------------ the kernel
 
 __device__ __forceinline__ float clamp_temperature(float T) { return fminf(fmaxf(T, 1.45e-30f), 1.44e37f); }
@@ -1413,42 +1521,50 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
     if (threadIdx.x == 0) sm.w.set_temperature(T_used);
     const bool weigh = T_row != 0.f && !(top_k > 0 && top_k <= kSampleList);
     const SampleRange<T> range = load_slice(s, weigh, c);
-    float top = range.top, low = range.low(), least_top = top;
+    const int warps = ranks * kSampleWarps;
+    // so many tokens of every warp's threads, one of each, are not below the number that a warp hands on: the row has 32 or warps
+    // times as many
+    const int nth = top_k > 0 ? min(32, (top_k + warps - 1) / warps) : max(1, min(32, kSampleBins / ranks / 4 / warps));
+    float top = range.top, low = range.low(), nth_top = __shfl_sync(0xffffffffu, sort_warp(range.top), nth - 1);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-        least_top = fminf(least_top, __shfl_xor_sync(0xffffffffu, least_top, o));
     }
-    float sum = range.sum * ex2((range.top - top) * c);
+    const float part = ex2((range.top - top) * c);
+    float sum = range.sum * part, likely = part;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int o = 16; o; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        likely += __shfl_xor_sync(0xffffffffu, likely, o);
+    }
     int finite = __reduce_add_sync(0xffffffffu, range.barred);  // those that are not, here
     if (lane == 0) {
         sm.range[0][warp] = top;
         sm.range[1][warp] = low;
         sm.range[2][warp] = sum;
-        sm.range[3][warp] = least_top;
+        sm.range[3][warp] = nth_top;
+        sm.range[4][warp] = likely;
         sm.finite[warp] = finite;
     }
     row_sync(ranks);
-    float tops[kSampleSteps], sums[kSampleSteps], least_warp = -kNoLogit;
+    float tops[kSampleSteps], sums[kSampleSteps], likelies[kSampleSteps];
     top = kLowest;
-    low = least_top = -kNoLogit;
+    low = nth_top = -kNoLogit;
     finite = 0;
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kSampleSteps; ++i) {
         const int q = 32 / kSampleWarps * i + lane / kSampleWarps, w = lane % kSampleWarps;
         tops[i] = kLowest;
-        sums[i] = 0.f;
+        sums[i] = likelies[i] = 0.f;
         if (q < ranks) {
+            likelies[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[4][w], q)));
             tops[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[0][w], q)));
             sums[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[2][w], q)));
             low = fminf(low, __uint_as_float(ld_cluster_u32(peer(&sm.range[1][w], q))));
-            least_top = fminf(least_top, __uint_as_float(ld_cluster_u32(peer(&sm.range[3][w], q))));
+            nth_top = fminf(nth_top, __uint_as_float(ld_cluster_u32(peer(&sm.range[3][w], q))));
             finite += static_cast<int>(ld_cluster_u32(peer(&sm.finite[w], q)));
-            least_warp = fminf(least_warp, tops[i]);
         }
         top = fmaxf(top, tops[i]);
     }
@@ -1456,13 +1572,20 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-        least_top = fminf(least_top, __shfl_xor_sync(0xffffffffu, least_top, o));
-        least_warp = fminf(least_warp, __shfl_xor_sync(0xffffffffu, least_warp, o));
+        nth_top = fminf(nth_top, __shfl_xor_sync(0xffffffffu, nth_top, o));
+    }
+    likely = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSampleSteps; ++i) {
+        const float factor = ex2((tops[i] - top) * c);
+        sum += sums[i] * factor;
+        likely += likelies[i] * factor;
     }
 #pragma unroll
-    for (int i = 0; i < kSampleSteps; ++i) sum += sums[i] * ex2((tops[i] - top) * c);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int o = 16; o; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        likely += __shfl_xor_sync(0xffffffffu, likely, o);
+    }
     finite = p.a.V - __reduce_add_sync(0xffffffffu, finite);
     if (low == kNoLogit && sum == sum) {  // of the allowed ones some may be -infinity
         int count = 0;
@@ -1524,15 +1647,12 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
         if (by_k) sum = static_cast<float>(top_k);  // more than that it is not
         __syncthreads();
         const float edge = sm.edge;
-        // Logits that no border can be at.  Top-k: a warp's (or a thread's) largest logit is one of the row's, so that the least of
-        // so many of them is not above the k-th.  Top-p, or the draw where there is no limit: what follows a border holds
-        // 1 - q of the sum in V tokens at most, and none of these weighs more than the border's.  (2^-12 for the bins' error.)
+        // Logits that no border can be at.  Top-k: the n-th largest of a warp's threads' largest, as above.  Top-p, or the draw
+        // where there is no limit: what follows a border holds 1 - q of the sum in V tokens at most, and none of these weighs more
+        // than the border's.  (2^-12 for the bins' error.)
         float least = kLowest;
         if (by_k) {
-            if (top_k <= ranks * kSampleWarps)
-                least = least_warp;
-            else if (top_k <= ranks * kSampleThreads)
-                least = least_top;
+            if (top_k <= 32 * warps) least = nth_top;
         } else {
             const float q = top_p < 1.f ? fmaxf(top_p, 0.f) : u, rest = (1.f - q - 0x1p-12f) * sum / static_cast<float>(p.a.V);
             if (edge != kNoLogit && top_p >= 1.f)
@@ -1540,7 +1660,47 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
             else if (rest > 0.f)
                 least = fmaxf(edge, top + __fdividef(log2f(rest) - 0x1p-6f, c));
         }
-        if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out,
+        SampleShort way{by_k, !by_k && top_p < 1.f, false, 0.f, kSampleList};
+        way.from = way.by_k ? least : way.by_sum ? fmaxf(nth_top, edge) : edge;
+        way.whole = !way.by_k && way.from == edge;
+        if (way.by_sum) way.room = min(kSampleList, kSampleBins / ranks);  // (running sums lie where this CTA's bins would: the slice is needed if that fails)
+        // (with top-p only where the threads' largest, which will be listed, about hold it: listed in vain they cost a sixth)
+        if (way.by_k ? least > kLowest : way.from > kLowest && (!way.by_sum || way.whole || likely > top_p * sum)) {
+            uint64_t *list = reinterpret_cast<uint64_t *>(hist);
+            const int n = list_likely(s, sm, way, list, ranks, rank, top, c, sum, top_p, out);
+            if (n >= 0) {
+                if (ranks > 1) {
+                    cluster_arrive();
+                    if (rank != 0 && !way.by_sum) return;
+                    cluster_wait();
+                } else {
+                    __syncthreads();
+                }
+                // In units of 2^-24 of the sum: additions, one for every four of a thread's tokens; exponents of up to 40 octaves,
+                // whose product with c is two roundings off (80); ex2, 4, and a dozen such factors where larger logits turn up (128).
+                const float off = (static_cast<float>(p.slice / kSampleThreads / 4) + 256.f) * 0x1p-24f;
+                if (rank == 0) {
+                    done = solve_likely(sm, way, list, n, reinterpret_cast<uint64_t *>(way.by_sum ? own : buffer + p.upto_at), edge, top_k, sum, off,
+                                        top_p, u, out);
+                    if (threadIdx.x == 0) sm.first = done;
+                }
+                if (way.by_sum) {
+                    row_sync(ranks);
+                    done = ld_cluster_u32(peer(&sm.first, 0)) != 0;
+                    if (ranks > 1) cluster_arrive();
+                    if (done && rank != 0) return;
+                    if (ranks > 1) cluster_wait();
+                }
+            }
+            if (!done) {  // the histogram's place again
+                row_sync(ranks);
+                for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
+                if (threadIdx.x == 0) sm.listed[0] = 0;
+                row_sync(ranks);
+            }
+        }
+        if (done) {
+        } else         if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out,
                          p.bits_at ? reinterpret_cast<uint32_t *>(buffer + p.bits_at) : nullptr)) {
             // the rest is the first CTA's; the others' shared memory is not read any more
             if (ranks > 1) {
@@ -1581,13 +1741,13 @@ constexpr int kSampleSmem = 200 * 1024;
 constexpr int kSampleSlice = 80 * 1024;  // that stays in shared memory, two of them beside each other; a longer one is read again
 constexpr int kSampleBits = 48 * 1024;   // of a slice, at most
 
-// CTAs of a row, two of which an SM holds.  One row of 126464 tokens: 22.0 us with eight, 27.7 with four; 7 rows of 50021: 22.3
-// and 20.2; 128 rows of 126464: 88 with eight, 57 with four, 59 with two; 528 rows of 152064 in fp32 (no slice of a row in four
-// stays in shared memory beside another): 391 with four, 327 with two, 346 with one; one row of 4096: 12.6 with four, 13.5
-// with two, 14.3 with one.
+// CTAs of a row, two of which an SM holds: as many as run at once, but no slice shorter than some 8000 tokens.  One row of
+// 126464 tokens with top-p: 22 us with eight, 28 with four; 7 rows of 50021: 22.4 with four, 23.4 with eight; one row of 4096: 9.3
+// with one, 10.2 with two, 14 with four; 128 rows of 126464 with top-k: 36.6 with two, 48 with four, 52 with one; 528
+// rows of 152064 in fp32 with top-p: 330 with two, 349 with four, 521 with one.
 int sample_ranks(long long rows, int V, int num_sms) {
-    int ranks = rows * 8 <= 2 * num_sms && V >= 8 * 8192 ? 8 : rows * 4 <= 4 * num_sms ? 4 : 2;
-    while (ranks > 1 && V < ranks * 1024) ranks >>= 1;
+    int ranks = rows * 8 <= 2 * num_sms ? 8 : rows * 4 <= 2 * num_sms ? 4 : 2;
+    while (ranks > 1 && V < ranks * 8192) ranks >>= 1;
     return ranks;
 }
 
