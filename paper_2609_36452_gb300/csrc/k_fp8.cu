@@ -41,6 +41,8 @@ constexpr int kFp8RowsBytes = kFp8RowsTile * kFp8Block;
 constexpr int kFp8Threads = 12 * 32;        // three warpgroups, between which the registers are divided anew
 constexpr int kFp8EpilogueRegs = 224, kFp8OtherRegs = 56;  // 256 * 224 + 128 * 56 of the launch's 384 * 168
 constexpr int kFp8TmaCodes = 8, kFp8TmaRows = 9, kFp8Mma = 10;  // warps; 0 - 7 are the epilogue
+constexpr int kFp8FewRows = 24;             // activations whose logits are handed to all of the epilogue's threads, a column each
+constexpr int kFp8FewPitch = kFp8ColsTile + 1;
 constexpr int kFp8Smem = 226 * 1024;
 constexpr int kFp8MaxRows = 1 << 14;         // of a launch
 
@@ -393,7 +395,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
     k_fp8_head(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x, const Fp8Params p) {
     constexpr int kCtas = kPair ? 2 : 1;
     constexpr int kCodeBytes = kFp8TileBytes / kCtas, kStageBytes = kFp8RowsBytes + kCodeBytes;
-    constexpr int kStages = (kFp8Smem - 2048) / kStageBytes;
+    constexpr int kStages = (kFp8Smem - 2048 - (kPair ? 0 : kFp8FewRows * kFp8FewPitch * 4)) / kStageBytes;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Fp8Shared<kStages> sm;
     volatile int *abort = sm.give_up;
@@ -591,18 +593,46 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                         mine[static_cast<long long>(i) * plan.partial_rows] = v;
                     }
                 const int w0 = fp8_worker_of(plan, seg.tail * plan.blocks), w1 = fp8_worker_of(plan, (seg.tail + 1) * plan.blocks - 1);
+                const int slot0 = fp8_slot_of(plan, w0, seg.tail);  // the others' shares begin in this tile: theirs is 0
                 __threadfence();
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (threadIdx.x == 0) sm.last = counter_add_acq_rel(&p.counters[seg.tail * kCtas + rank], 1) == w1 - w0;
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (!sm.last) continue;
                 __threadfence();
+                if (!kPair && p.rows <= kFp8FewRows) {
+                    // a thread a column: the parts of four rows are on their way at once
+                    const int v = col_tile * kFp8ColsTile + threadIdx.x;
+                    const float *from = p.partials + static_cast<long long>(threadIdx.x >> 2) * plan.partial_rows * 4 + (threadIdx.x & 3);
+                    for (int r = 0; r < p.rows; r += 4) {
+                        float y[4] = {0.f, 0.f, 0.f, 0.f};
+                        for (int w = w0; w <= w1; w += 8) {
+                            float x[8][4];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    x[i][j] = w + i <= w1 && r + j < p.rows
+                                                  ? __ldcg(from + (2ll * (w + i) + (w + i == w0 ? slot0 : 0)) * part * 4 + (r + j) * 4)
+                                                  : 0.f;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) y[j] += x[i][j];
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (r + j < p.rows && v < p.V)
+                                store_out(p.out, p.out_type, (r + j) * p.out_stride + v, y[j] * __ldcg(p.factor + r + j));
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int i = 0; i < 128; ++i) run[i] = 0.f;
                 if (slot < live)
                     for (int w = w0; w <= w1; ++w) {
                         const float4 *theirs = reinterpret_cast<const float4 *>(p.partials) +
-                                               ((w * 2 + fp8_slot_of(plan, w, seg.tail)) * kCtas + rank) * part +
+                                               ((w * 2 + (w == w0 ? slot0 : 0)) * kCtas + rank) * part +
                                                half * 32ll * plan.partial_rows + slot;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
@@ -613,6 +643,21 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                             run[4 * i + 3] += v.w;
                         }
                     }
+            }
+            if (!kPair && p.rows <= kFp8FewRows) {
+                // by way of shared memory: a thread has one row, of which it would write 128 columns by itself
+                float *stage = reinterpret_cast<float *>(smem + kStages * kStageBytes);
+                if (slot < live) {
+                    const float factor = __ldcg(p.factor + slot);
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) stage[slot * kFp8FewPitch + half * 128 + i] = run[i] * factor;
+                }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                const int v = col_tile * kFp8ColsTile + threadIdx.x;
+                if (v < p.V)
+                    for (int r = 0; r < p.rows; ++r) store_out(p.out, p.out_type, r * p.out_stride + v, stage[r * kFp8FewPitch + threadIdx.x]);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                continue;
             }
             if (slot < live) {
                 const long long row = static_cast<long long>(row_tile) * kFp8RowsTile + slot;
@@ -682,7 +727,9 @@ struct Fp8Layout {
         partials = counters + (plan.tail * ctas * 4 + 255) / 256 * 256;
         bytes = partials + (plan.tail ? static_cast<long long>(plan.tail_workers) * 2 * ctas * kFp8ColsTile * plan.partial_rows * 4 : 0);
     }
-    static constexpr int kLeast = 4;  // blocks of shared tiles that a worker has at least (as long as every tile has a worker)
+    // Blocks of shared tiles that a worker has at least (as long as every tile has a worker): 50021 x 1001, 13 rows take 15.5 us
+    // with 8, 20 with 4; 4096 x 4096, one row 11.4 with 8, 10.2 with 4, 14.1 with 16, 128 rows 21.7, 29.0 and 22.4.
+    static constexpr int kLeast = 8;
 };
 
 // Of a call: more rows than a launch takes are several launches, one after the other.

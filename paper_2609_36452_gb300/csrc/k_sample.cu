@@ -1669,13 +1669,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
             uint64_t *list = reinterpret_cast<uint64_t *>(hist);
             const int n = list_likely(s, sm, way, list, ranks, rank, top, c, sum, top_p, out);
             if (n >= 0) {
-                if (ranks > 1) {
-                    cluster_arrive();
-                    if (rank != 0 && !way.by_sum) return;
-                    cluster_wait();
-                } else {
-                    __syncthreads();
-                }
+                row_sync(ranks);  // (all have looked at the others' numbers, and the list is there)
+                if (rank != 0 && !way.by_sum) return;
                 // In units of 2^-24 of the sum: additions, one for every four of a thread's tokens; exponents of up to 40 octaves,
                 // whose product with c is two roundings off (80); ex2, 4, and a dozen such factors where larger logits turn up (128).
                 const float off = (static_cast<float>(p.slice / kSampleThreads / 4) + 256.f) * 0x1p-24f;
