@@ -43,6 +43,7 @@ constexpr int kFp8EpilogueRegs = 224, kFp8OtherRegs = 56;  // 256 * 224 + 128 * 
 constexpr int kFp8TmaCodes = 8, kFp8TmaRows = 9, kFp8Mma = 10;  // warps; 0 - 7 are the epilogue
 constexpr int kFp8FewRows = 24;             // activations whose logits are handed to all of the epilogue's threads, a column each
 constexpr int kFp8FewPitch = kFp8ColsTile + 1;
+constexpr int kFp8StageOut = 64 * 1024;      // a tile's 16-bit logits on their way out: boxes of 64 columns x 128 rows
 constexpr int kFp8Smem = 226 * 1024;
 constexpr int kFp8MaxRows = 1 << 14;         // of a launch
 
@@ -209,7 +210,7 @@ struct Fp8Params {
     float *partials;          // [worker][2][CTA of a pair][2][32][partial rows][4]
     void *out;
     long long out_stride;
-    int out_type, out_vec;    // out_vec: 32-byte stores fit
+    int out_type, out_vec;    // out_vec: 32-byte stores fit, 2: and map_out is there
     int rows, V;
     long long wait_cycles;
     int stall;
@@ -392,10 +393,12 @@ __device__ __noinline__ void fp8_drain(Fp8Shared<kStages> &sm, const int (&codes
 
 template <bool kPair>
 __global__ void __launch_bounds__(kFp8Threads, 1)
-    k_fp8_head(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x, const Fp8Params p) {
+    k_fp8_head(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x,
+               const __grid_constant__ CUtensorMap map_out, const Fp8Params p) {
     constexpr int kCtas = kPair ? 2 : 1;
     constexpr int kCodeBytes = kFp8TileBytes / kCtas, kStageBytes = kFp8RowsBytes + kCodeBytes;
-    constexpr int kStages = (kFp8Smem - 2048 - (kPair ? 0 : kFp8FewRows * kFp8FewPitch * 4)) / kStageBytes;
+    constexpr int kStages = (kFp8Smem - 2048 - kFp8StageOut) / kStageBytes;
+    static_assert(kFp8FewRows * kFp8FewPitch * 4 <= kFp8StageOut, "few rows' logits fit there too");
     extern __shared__ uint8_t smem_raw[];
     __shared__ Fp8Shared<kStages> sm;
     volatile int *abort = sm.give_up;
@@ -659,6 +662,38 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 continue;
             }
+            if (p.out_vec == 2) {
+                // 16-bit logits by way of shared memory and TMA, which goes on while the next tile is added up.  (Stores of 32 bytes
+                // a thread, of all CTAs at about the same time, held the next tile up: 1024 rows of 152064 x 3584 took 537 us.)
+                uint8_t *stage = smem + kStages * kStageBytes + half * (kFp8StageOut / 2);
+                const bool first = threadIdx.x % 128 == 0;
+                if (first) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
+                const float factor = slot < live ? __ldcg(p.factor + static_cast<long long>(row_tile) * kFp8RowsTile + slot) : 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = pair_of(run[8 * i + 2 * j] * factor, run[8 * i + 2 * j + 1] * factor, p.out_type);
+                    *reinterpret_cast<uint4 *>(stage + (i >> 3) * (kFp8RowsTile * 128) + slot * 128 + (((i & 7) ^ (slot & 7)) * 16)) =
+                        make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
+                if (first && live > 0) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int v0 = col_tile * kFp8ColsTile + half * 128 + b * 64;
+                        if (v0 < p.V)
+                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                                             reinterpret_cast<uint64_t>(&map_out)),
+                                         "r"(v0), "r"(row_tile * kFp8RowsTile), "r"(smem_u32(stage + b * (kFp8RowsTile * 128)))
+                                         : "memory");
+                    }
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+                continue;
+            }
             if (slot < live) {
                 const long long row = static_cast<long long>(row_tile) * kFp8RowsTile + slot;
                 const int v0 = col_tile * kFp8ColsTile + half * 128;
@@ -674,6 +709,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 }
             }
         }
+        if (threadIdx.x % 128 == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -752,8 +788,19 @@ int fp8_encode(const void *base, long long rows, CUtensorMap *map) {
     return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
 }
 
+// Boxes of 128 rows x 64 of 16-bit logits, swizzled as the epilogue writes them.
+int fp8_encode_out(void *out, int rows, int V, long long stride, CUtensorMap *map) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(V), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(stride) * 2};
+    cuuint32_t box[2] = {64, 128}, step[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, out, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+}
+
 template <bool kPair>
-cudaError_t launch_fp8(const CUtensorMap &codes, const CUtensorMap &x, const Fp8Params &p, int grid, cudaStream_t s) {
+cudaError_t launch_fp8(const CUtensorMap &codes, const CUtensorMap &x, const CUtensorMap &out, const Fp8Params &p, int grid, cudaStream_t s) {
     cudaError_t e = cudaFuncSetAttribute(k_fp8_head<kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFp8Smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -769,7 +816,7 @@ cudaError_t launch_fp8(const CUtensorMap &codes, const CUtensorMap &x, const Fp8
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_fp8_head<kPair>, codes, x, p);
+    return cudaLaunchKernelEx(&cfg, k_fp8_head<kPair>, codes, x, out, p);
 }
 
 // ------------------------------------------------------------------------------ the quantiser
@@ -1104,13 +1151,19 @@ int rpd_fp8_logits(const rpd_fp8 *h, const void *x, int x_type, int64_t x_stride
         p.V = h->V;
         p.wait_cycles = h->wait_us * kWaitCyclesPerUs;
         p.stall = h->stall ? 1 : 0;
-        CUtensorMap map = h->map;
+        CUtensorMap map = h->map, map_out = h->map;
+        // more rows than few, 16-bit logits and addresses that TMA takes
+        if (n > kFp8FewRows && type_size(out_type) == 2 && aligned_to(p.out, 16) && (rows == 1 || out_stride % 8 == 0)) {
+            const int code = fp8_encode_out(p.out, n, h->V, out_stride, &map_out);
+            if (code != RPD_OK) return code;
+            p.out_vec = 2;
+        }
         if (fp8_pairs(n)) {
             const int code = fp8_encode(q.codes, (at.scales - at.codes) / 128, &map);
             if (code != RPD_OK) return code;
-            e = launch_fp8<true>(h->map, map, p, at.grid, s);
+            e = launch_fp8<true>(h->map, map, map_out, p, at.grid, s);
         } else {
-            e = launch_fp8<false>(h->map, map, p, at.grid, s);
+            e = launch_fp8<false>(h->map, map, map_out, p, at.grid, s);
         }
         if (e != cudaSuccess) return op_cuda_fail(e, "8-bit head launch");
     }
