@@ -294,20 +294,18 @@ __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-// 16 columns of the accumulator on their way to a thread's registers, which are theirs after tmem_arrived.
-__device__ __forceinline__ void tmem_ask_x16(uint32_t taddr, uint32_t (&r)[16]) {
+// 32 columns of the accumulator on their way to a thread's registers, which are theirs after tmem_arrived.
+__device__ __forceinline__ void tmem_ask_x32(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32"
-        " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32"
+        " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;\n"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
                  :
                  : "memory");
 }
@@ -561,18 +559,17 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                     }
                 };
                 if (reads) {
-                    uint32_t v[2][16];  // one half is multiplied while the next is on its way
-                    tmem_ask_x16(from + acc * 256, v[0]);
+                    uint32_t v[2][32];  // one part is multiplied while the next is on its way
+                    tmem_ask_x32(from + acc * 256, v[0]);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < 4; ++c) {
                         tmem_arrived(v[c & 1]);
-                        if (c < 7)
-                            tmem_ask_x16(from + acc * 256 + (c + 1) * 16, v[(c + 1) & 1]);
+                        if (c < 3)
+                            tmem_ask_x32(from + acc * 256 + (c + 1) * 32, v[(c + 1) & 1]);
                         else
                             release();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            { run[c * 16 + 2 * i] = fmaf(f, __uint_as_float(v[c & 1][2 * i]), run[c * 16 + 2 * i]); run[c * 16 + 2 * i + 1] = fmaf(f, __uint_as_float(v[c & 1][2 * i + 1]), run[c * 16 + 2 * i + 1]); }
+                        for (int i = 0; i < 32; ++i) run[c * 32 + i] = fmaf(f, __uint_as_float(v[c & 1][i]), run[c * 32 + i]);
                     }
                 } else {
                     release();
