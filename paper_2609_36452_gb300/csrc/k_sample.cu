@@ -173,7 +173,7 @@ struct Slice {
     // logits are -infinity).
     template <typename F>
     __device__ __forceinline__ void each_vec(float least, F f) const {
-        constexpr int kAhead = kResident ? 1 : 3;  // vectors on their way from L2 meanwhile
+        constexpr int kAhead = kResident ? 1 : 4;  // vectors on their way from L2 meanwhile
         const int pieces = row.vecs + loose();
         uint4 raw[kAhead];
 #pragma unroll
@@ -488,7 +488,7 @@ struct SampleShared {
         uint64_t mass[256];
         uint32_t count[256];
     } *x;
-    float range[5][kSampleWarps];  // largest, smallest, sum, n-th of the threads' largest, weights of these
+    float range[5][kSampleWarps];  // largest, smallest, sum, n-th of the threads' largest, weights of the n largest
     int finite[kSampleWarps], binned[kSampleWarps];
     float sums[kSampleWarps];
     float sum;
@@ -1525,14 +1525,15 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
     // so many tokens of every warp's threads, one of each, are not below the number that a warp hands on: the row has 32 or warps
     // times as many
     const int nth = top_k > 0 ? min(32, (top_k + warps - 1) / warps) : max(1, min(32, kSampleBins / ranks / 4 / warps));
-    float top = range.top, low = range.low(), nth_top = __shfl_sync(0xffffffffu, sort_warp(range.top), nth - 1);
+    const float sorted = sort_warp(range.top);
+    float top = range.top, low = range.low(), nth_top = __shfl_sync(0xffffffffu, sorted, nth - 1);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
     }
-    const float part = ex2((range.top - top) * c);
-    float sum = range.sum * part, likely = part;
+    float sum = range.sum * ex2((range.top - top) * c);
+    float likely = lane < nth ? ex2((sorted - top) * c) : 0.f;  // of tokens that are not below what the warp hands on
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -1664,7 +1665,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
         way.from = way.by_k ? least : way.by_sum ? fmaxf(nth_top, edge) : edge;
         way.whole = !way.by_k && way.from == edge;
         if (way.by_sum) way.room = min(kSampleList, kSampleBins / ranks);  // (running sums lie where this CTA's bins would: the slice is needed if that fails)
-        // (with top-p only where the threads' largest, which will be listed, about hold it: listed in vain they cost a sixth)
+        // (with top-p only where tokens that will be listed are known to hold it: listed in vain they cost a sixth)
         if (way.by_k ? least > kLowest : way.from > kLowest && (!way.by_sum || way.whole || likely > top_p * sum)) {
             uint64_t *list = reinterpret_cast<uint64_t *>(hist);
             const int n = list_likely(s, sm, way, list, ranks, rank, top, c, sum, top_p, out);
