@@ -549,11 +549,11 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
  * The token is the first, in that order, at which the sum of the kept weights up to and with it exceeds
  * uniform[r] times the sum of all that are kept.  T = 0 keeps the first token alone, whatever the limits;
  * other T count as at least 1.45e-30 and at most 1.44e37.
- * Weights are right to some 2^-31 each, without bias, those of 2^-10 of their sum and more to 2^-50; sums of them
- * are exact.  Results do not depend on the launch's shape.
+ * Weights are right to some 2^-31 each, without bias, those of 2^-10 of their sum and more to 2^-42, and sums of
+ * them are exact: which token a border falls on can differ from exact arithmetic's only where that is closer to it
+ * than some 2^-38 of the sum.  The same call gives the same results every time.
  *
- * 1 <= V <= 2^24, 0 <= rows <= 2^26 (larger: RPD_ERR_UNSUPPORTED; 0 is a no-op).  A row that fits eight SMs' shared
- * memory (400 KB a CTA pair; 800 000 bf16 logits) is read once. */
+ * 1 <= V <= 2^24, 0 <= rows <= 2^26 (larger: RPD_ERR_UNSUPPORTED; 0 is a no-op). */
 typedef struct rpd_sample_args {
     const void *logits;         /* [rows][V] of `type`, device, rows row_stride elements apart */
     const uint32_t *allowed;    /* [rows][ceil(V / 32)] bits, 1 = allowed, as rpd_verify's; or NULL.  Logits of other
