@@ -48,7 +48,8 @@ constexpr int kFp8EpilogueRegs = 224, kFp8OtherRegs = 56;  // 256 * 224 + 128 * 
 constexpr int kFp8TmaCodes = 8, kFp8TmaRows = 9, kFp8Mma = 10;  // warps; 0 - 7 are the epilogue
 constexpr int kFp8FewRows = 24;             // activations whose logits are handed to all of the epilogue's threads, a column each
 constexpr int kFp8FewPitch = kFp8ColsTile + 1;
-constexpr int kFp8StageOut = 64 * 1024;      // a tile's 16-bit logits on their way out: boxes of 64 columns x 128 rows
+constexpr int kFp8BoxBytes = kFp8RowsTile * 128;  // of logits on their way out: 64 (32 in fp32) columns x 128 rows
+constexpr int kFp8StageOut = 4 * kFp8BoxBytes;
 constexpr int kFp8Smem = 226 * 1024;
 constexpr int kFp8MaxRows = 1 << 14;         // of a launch
 
@@ -215,7 +216,8 @@ struct Fp8Params {
     float *partials;          // [worker][2][CTA of a pair][2][32][partial rows][4]
     void *out;
     long long out_stride;
-    int out_type, out_vec;    // out_vec: 32-byte stores fit, 2: and map_out is there
+    int out_type;
+    bool out_tma;             // there is a map_out
     int rows, V;
     long long wait_cycles;
     int stall;
@@ -324,11 +326,6 @@ __device__ __forceinline__ void mbar_complete_tx(uint64_t *bar, uint32_t bytes) 
     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
 
-__device__ __forceinline__ void store_256(void *to, const uint32_t (&w)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-                 "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-}
 __device__ __forceinline__ uint32_t pair_of(float a, float b, int type) {
     if (type == RPD_TYPE_BF16) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -338,30 +335,23 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b, int type) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// Sixteen neighbouring logits of a row from column v on, 32 bytes a store where that fits (a whole sector: stores of half
-// a sector were read and written twice).
-__device__ __forceinline__ void fp8_store(const Fp8Params &p, long long row, int v, const float (&y)[16]) {
-    const long long at = row * p.out_stride + v;
-    if (p.out_vec && v + 16 <= p.V) {
-        uint32_t w[8];
-        if (p.out_type == RPD_TYPE_F32) {
-            float *to = static_cast<float *>(p.out) + at;
+// Logits from shared memory to their rows, a warp a row: 256 bytes, of which `cols` numbers are there.  545 rows of
+// 126464 x 4096 in bf16 at an odd stride take 356 us so, 920 where every thread wrote its own row's; two numbers a store,
+// from the row's first whole word on, took 404.
+template <typename T>
+__device__ __forceinline__ void fp8_store_rows(const uint8_t *stage, T *out, long long stride, int rows, int cols) {
+    constexpr int kBytes = sizeof(T), kBox = 128 / kBytes;  // columns of a box
+    const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+#pragma unroll 4
+    for (int r = warp; r < rows; r += 4) {
+        T *to = out + r * stride;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(y[8 * h + i]);
-                store_256(to + 8 * h, w);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = pair_of(y[2 * i], y[2 * i + 1], p.out_type);
-            store_256(static_cast<uint16_t *>(p.out) + at, w);
+        for (int j = 0; j < 256 / kBytes / 32; ++j) {
+            const int c = j * 32 + lane, byte = c % kBox * kBytes;
+            if (c < cols)
+                to[c] = *reinterpret_cast<const T *>(stage + c / kBox * kFp8BoxBytes + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
         }
-        return;
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (v + i < p.V) store_out(p.out, p.out_type, at + i, y[i]);
 }
 
 // Shared by a CTA's roles.
@@ -664,50 +654,50 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 continue;
             }
-            if (p.out_vec == 2) {
-                // 16-bit logits by way of shared memory and TMA, which goes on while the next tile is added up.  (Stores of 32 bytes
-                // a thread, of all CTAs at about the same time, held the next tile up: 1024 rows of 152064 x 3584 took 537 us.)
-                uint8_t *stage = smem + kStages * kStageBytes + half * (kFp8StageOut / 2);
-                const bool first = threadIdx.x % 128 == 0;
+            // Logits leave by way of shared memory, 256 bytes of each row at a time: by TMA, which goes on while the next tile is
+            // added up, or a warp a row, where addresses do not fit that or the row ends in them (TMA writes 16 bytes at
+            // least, and what follows a row is the caller's).  With stores of 32 bytes a thread 1024 rows of 152064 x 3584 took 537
+            // us, by TMA 443.
+            uint8_t *stage = smem + kStages * kStageBytes + half * (kFp8StageOut / 2);
+            const bool first = threadIdx.x % 128 == 0, wide = p.out_type == RPD_TYPE_F32;
+            const float factor = slot < live ? __ldcg(p.factor + static_cast<long long>(row_tile) * kFp8RowsTile + slot) : 0.f;
+#pragma unroll
+            for (int pass = 0; pass < 2; ++pass) {
+                if (pass && !wide) break;
                 if (first) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
-                const float factor = slot < live ? __ldcg(p.factor + static_cast<long long>(row_tile) * kFp8RowsTile + slot) : 0.f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     uint32_t w[4];
+                    if (wide)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = pair_of(run[8 * i + 2 * j] * factor, run[8 * i + 2 * j + 1] * factor, p.out_type);
-                    *reinterpret_cast<uint4 *>(stage + (i >> 3) * (kFp8RowsTile * 128) + slot * 128 + (((i & 7) ^ (slot & 7)) * 16)) =
+                        for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(run[64 * pass + 4 * i + j] * factor);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = pair_of(run[8 * i + 2 * j] * factor, run[8 * i + 2 * j + 1] * factor, p.out_type);
+                    *reinterpret_cast<uint4 *>(stage + (i >> 3) * kFp8BoxBytes + slot * 128 + (((i & 7) ^ (slot & 7)) * 16)) =
                         make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
-                if (first && live > 0) {
+                const int v0 = col_tile * kFp8ColsTile + half * 128 + pass * 64;
+                if (p.out_tma && v0 + (wide ? 64 : 128) <= p.V) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
+                    if (first && live > 0) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const int v0 = col_tile * kFp8ColsTile + half * 128 + b * 64;
-                        if (v0 < p.V)
+                        for (int b = 0; b < 2; ++b)
                             asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
                                              reinterpret_cast<uint64_t>(&map_out)),
-                                         "r"(v0), "r"(row_tile * kFp8RowsTile), "r"(smem_u32(stage + b * (kFp8RowsTile * 128)))
+                                         "r"(v0 + b * (wide ? 32 : 64)), "r"(row_tile * kFp8RowsTile), "r"(smem_u32(stage + b * kFp8BoxBytes))
                                          : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                }
-                continue;
-            }
-            if (slot < live) {
-                const long long row = static_cast<long long>(row_tile) * kFp8RowsTile + slot;
-                const int v0 = col_tile * kFp8ColsTile + half * 128;
-                const float factor = __ldcg(p.factor + row);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float y[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) y[j] = run[16 * i + j];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) y[j] *= factor;
-                    if (v0 + 16 * i < p.V) fp8_store(p, row, v0 + 16 * i, y);
+                } else {
+                    asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
+                    const long long at = static_cast<long long>(row_tile) * kFp8RowsTile * p.out_stride + v0;
+                    if (wide)
+                        fp8_store_rows(stage, static_cast<uint32_t *>(p.out) + at, p.out_stride, live, p.V - v0);
+                    else
+                        fp8_store_rows(stage, static_cast<uint16_t *>(p.out) + at, p.out_stride, live, p.V - v0);
                 }
             }
         }
@@ -790,14 +780,15 @@ int fp8_encode(const void *base, long long rows, CUtensorMap *map) {
     return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
 }
 
-// Boxes of 128 rows x 64 of 16-bit logits, swizzled as the epilogue writes them.
-int fp8_encode_out(void *out, int rows, int V, long long stride, CUtensorMap *map) {
+// Boxes of 128 rows x 128 bytes of logits, swizzled as the epilogue writes them.
+int fp8_encode_out(void *out, int size, int rows, int V, long long stride, CUtensorMap *map) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
-    cuuint64_t dims[2] = {static_cast<cuuint64_t>(V), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(stride) * 2};
-    cuuint32_t box[2] = {64, 128}, step[2] = {1, 1};
-    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, out, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(V), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(stride) * size};
+    cuuint32_t box[2] = {128u / size, 128}, step[2] = {1, 1};
+    const CUresult r = fn(map, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, out, dims, strides, box, step,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? RPD_OK : op_fail(RPD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
 }
 
@@ -1148,17 +1139,16 @@ int rpd_fp8_logits(const rpd_fp8 *h, const void *x, int x_type, int64_t x_stride
         p.out = static_cast<uint8_t *>(out) + first * out_stride * type_size(out_type);
         p.out_stride = out_stride;
         p.out_type = out_type;
-        p.out_vec = aligned_to(out, 32) && (rows == 1 || out_stride * type_size(out_type) % 32 == 0);
         p.rows = n;
         p.V = h->V;
         p.wait_cycles = h->wait_us * kWaitCyclesPerUs;
         p.stall = h->stall ? 1 : 0;
         CUtensorMap map = h->map, map_out = h->map;
-        // more rows than few, 16-bit logits and addresses that TMA takes
-        if (n > kFp8FewRows && type_size(out_type) == 2 && aligned_to(p.out, 16) && (rows == 1 || out_stride % 8 == 0)) {
-            const int code = fp8_encode_out(p.out, n, h->V, out_stride, &map_out);
+        // more rows than few, and addresses that TMA takes
+        if (n > kFp8FewRows && aligned_to(p.out, 16) && out_stride * type_size(out_type) % 16 == 0) {
+            const int code = fp8_encode_out(p.out, type_size(out_type), n, h->V, out_stride, &map_out);
             if (code != RPD_OK) return code;
-            p.out_vec = 2;
+            p.out_tma = true;
         }
         if (fp8_pairs(n)) {
             const int code = fp8_encode(q.codes, (at.scales - at.codes) / 128, &map);

@@ -143,6 +143,30 @@ def test_rows_of_every_count_between_tiles():
 
 @gpu
 @needs_gpu
+@pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows", [25, 128, 200])
+def test_rows_of_logits_at_any_address(rows, out):
+    """Strides and first columns of every alignment, V that ends anywhere in a tile; what lies around the logits stays."""
+    for V in (1, 63, 128, 193, 383, 513):
+        c = make(200, V, rows, True, out=out)
+        h = head_of(c)
+        for apart in range(9):
+            for first in (0, 1, 2, 4, 8):
+                buffer = torch.full((rows, first + V + apart), 77.0, dtype=TYPES[out], device="cuda")
+                c["out"] = buffer[:, first:first + V]
+                c["buffer"] = buffer[:, first:]
+                h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+                torch.cuda.synchronize()
+                if apart == first == 0:
+                    check(c)
+                    want = c["out"].clone()
+                assert torch.equal(c["out"], want), (V, apart, first)
+                assert (buffer[:, :first] == 77).all() and (buffer[:, first + V:] == 77).all(), (V, apart, first)
+        h.close()
+
+
+@gpu
+@needs_gpu
 def test_two_streams_and_threads():
     cases = [make(512, 20000, r, True, seed=r) for r in (5, 200)]
     h = head_of(cases[0])
