@@ -152,8 +152,8 @@ def test_rows_of_logits_at_any_address(rows, out):
         h = head_of(c)
         for apart in range(9):
             for first in (0, 1, 2, 4, 8):
-                buffer = torch.full((rows, first + V + apart), 77.0, dtype=TYPES[out], device="cuda")
-                c["out"] = buffer[:, first:first + V]
+                buffer = torch.full((rows + 2, first + V + apart), 77.0, dtype=TYPES[out], device="cuda")
+                c["out"] = buffer[:rows, first:first + V]
                 c["buffer"] = buffer[:, first:]
                 h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
                 torch.cuda.synchronize()
@@ -162,7 +162,27 @@ def test_rows_of_logits_at_any_address(rows, out):
                     want = c["out"].clone()
                 assert torch.equal(c["out"], want), (V, apart, first)
                 assert (buffer[:, :first] == 77).all() and (buffer[:, first + V:] == 77).all(), (V, apart, first)
+                assert (buffer[rows:] == 77).all(), (V, apart, first)
         h.close()
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("more,out,pad", [(1, "bf16", 0), (24, "f32", 1), (25, "f16", 2), (200, "bf16", 5)])
+def test_more_rows_than_a_launch_takes(more, out, pad):
+    most = 1 << 14
+    c = make(130, 70, most + more, True, out=out, pad=pad)
+    h = head_of(c)
+    h.logits(c["x"], c["out"], gain=c["gain"], eps=c["eps"])
+    torch.cuda.synchronize()
+    check(c)
+    whole = c["out"].clone()
+    for rows in (slice(0, most), slice(most, None)):
+        c["out"].fill_(3)
+        h.logits(c["x"][rows], c["out"][rows], gain=c["gain"], eps=c["eps"])
+        torch.cuda.synchronize()
+        assert torch.equal(c["out"][rows], whole[rows])
+    h.close()
 
 
 @gpu
