@@ -843,6 +843,54 @@ __device__ __forceinline__ void sort_in_registers(uint64_t *list, int apart, int
     __syncthreads();
 }
 
+// kPer entries a thread, kSampleThreads apart: those exchange in its registers, neighbours by shuffles, the others in shared
+// memory.  (All steps there, 66 of them with a barrier each, took 900 rows of 2000 tokens from 112 to 129 us.)
+template <int kPer>
+__device__ __forceinline__ void sort_long(uint64_t *list) {
+    const int t = threadIdx.x;
+    uint64_t x[kPer];
+#pragma unroll
+    for (int l = 0; l < kPer; ++l) x[l] = list[l * kSampleThreads + t];
+#pragma unroll 1
+    for (int k = 2; k <= kPer * kSampleThreads; k <<= 1) {
+#pragma unroll
+        for (int d = kPer / 2; d; d >>= 1)
+            if (k > d * kSampleThreads)
+#pragma unroll
+                for (int l = 0; l < kPer; ++l) {
+                    if (l & d) continue;
+                    const uint64_t a = x[l], b = x[l | d];
+                    const bool swap = (b < a) == (((l * kSampleThreads) & k) == 0);
+                    x[l] = swap ? b : a;
+                    x[l | d] = swap ? a : b;
+                }
+#pragma unroll 1
+        for (int j = min(k, kSampleThreads) >> 1; j; j >>= 1) {
+            uint64_t y[kPer];
+            if (j >= 32) {
+                __syncthreads();
+#pragma unroll
+                for (int l = 0; l < kPer; ++l) list[l * kSampleThreads + t] = x[l];
+                __syncthreads();
+#pragma unroll
+                for (int l = 0; l < kPer; ++l) y[l] = list[l * kSampleThreads + (t ^ j)];
+            } else {
+#pragma unroll
+                for (int l = 0; l < kPer; ++l) y[l] = __shfl_xor_sync(0xffffffffu, x[l], j);
+            }
+#pragma unroll
+            for (int l = 0; l < kPer; ++l) {
+                const bool low = (((l * kSampleThreads + t) & k) == 0) == ((t & j) == 0);
+                if ((y[l] < x[l]) == low) x[l] = y[l];
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int l = 0; l < kPer; ++l) list[l * kSampleThreads + t] = x[l];
+    __syncthreads();
+}
+
 // n0 entries, and n1 from kSampleList / 2 on, by the CTA; each padded to `size`, a power of two (returned).
 __device__ __noinline__ int sort_entries(uint64_t *list, int n0, int n1) {
     int size = 32;
@@ -858,19 +906,12 @@ __device__ __noinline__ int sort_entries(uint64_t *list, int n0, int n1) {
             sort_in_registers<1>(list, 0, size);
         return size;
     }
-    for (int l = 0; l < (n1 ? 2 : 1); ++l, list += kSampleList / 2)
-        for (int k = 2; k <= size; k <<= 1)
-            for (int j = k >> 1; j; j >>= 1) {
-                for (int i = threadIdx.x; i < size / 2; i += kSampleThreads) {
-                    const int a = 2 * i - (i & (j - 1)), b = a + j;
-                    const uint64_t x = list[a], y = list[b];
-                    if ((x > y) == ((a & k) == 0)) {
-                        list[a] = y;
-                        list[b] = x;
-                    }
-                }
-                __syncthreads();
-            }
+    for (int l = 0; l < (n1 ? 2 : 1); ++l) {
+        if (size == 2 * kSampleThreads)
+            sort_long<2>(list + l * (kSampleList / 2));
+        else
+            sort_long<kSampleList / kSampleThreads>(list);
+    }
     return size;
 }
 
@@ -1410,6 +1451,7 @@ __device__ __forceinline__ float sort_warp(float x) {
 struct SampleShort {
     bool by_k, by_sum;  // top-k; top-p without it.  Else min-p alone
     bool whole;         // no kept token is below `from`
+    bool all;           // every token is listed: V of them are sorted
     float from;         // logits from there on are listed
     int room;           // for so many
 };
@@ -1456,16 +1498,24 @@ __device__ __forceinline__ int list_likely(const S &s, SampleShared &sm, const S
     return n;
 }
 
+// Every token of a row that the list has room for, at its own place: those that are none sort behind the others.
+template <typename S>
+__device__ __forceinline__ void list_all(const S &s, uint64_t *list, uint32_t *out) {
+    s.each([&](float z, int v) { list[v] = z >= kLowest ? sample_entry(z, v) : ~0ull; });
+    if (out)
+        for (int i = threadIdx.x; i < (s.row.V + 31) / 32; i += kSampleThreads) out[i] = 0;
+}
+
 // The token from a list of n: by the row's first CTA.  A sum of all weights that is only known to lie within `off` of `sum` decides
 // as long as both ends do the same; false where they do not.
-__device__ __forceinline__ bool solve_likely(SampleShared &sm, const SampleShort &way, uint64_t *list, int n, uint64_t *upto, float edge, int top_k,
+__device__ __forceinline__ bool solve_likely(SampleShared &sm, const SampleShort &way, uint64_t *list, int n, int V, uint64_t *upto, float edge, int top_k,
                                              float sum, float off, float top_p, float u, uint32_t *out) {
-    const int bits = min(54, 59 - ilogbf(way.by_sum ? sum : static_cast<float>(kSampleList)));
+    const int bits = min(54, 59 - ilogbf(way.by_sum || way.all ? fmaxf(sum, 1.f) : static_cast<float>(kSampleList)));
     if (threadIdx.x == 0) {
         sm.w.set_floor(bits);
         sm.w.big = kNoLogit;  // (few tokens: all of them in 64 bits)
     }
-    sort_entries(list, n, 0);
+    sort_entries(list, way.all ? V : n, 0);
     if (way.by_k) n = min(n, top_k);
     const uint64_t mine = add_up(list, n, upto, bits, sm);
     uint64_t low = ~0ull, high = ~0ull;
@@ -1667,14 +1717,24 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
             else if (rest > 0.f)
                 least = fmaxf(edge, top + __fdividef(log2f(rest) - 0x1p-6f, c));
         }
-        SampleShort way{by_k, !by_k && top_p < 1.f, false, 0.f, kSampleList};
+        SampleShort way{by_k, !by_k && top_p < 1.f, false, false, 0.f, kSampleList};
         way.from = way.by_k ? least : way.by_sum ? fmaxf(nth_top, edge) : edge;
         way.whole = !way.by_k && way.from == edge;
         if (way.by_sum) way.room = min(kSampleList, kSampleBins / ranks);  // (running sums lie where this CTA's bins would: the slice is needed if that fails)
         // (with top-p only where tokens that will be listed are known to hold it: listed in vain they cost a sixth)
-        if (way.by_k ? least > kLowest : way.from > kLowest && (!way.by_sum || way.whole || likely > top_p * sum)) {
+        const bool few = way.by_k ? least > kLowest : way.from > kLowest && (!way.by_sum || way.whole || likely > top_p * sum);
+        // Short rows are listed whole (one CTA has them): 136 rows of 300 tokens take 16.4 us so, 24.6 to 30.8 by the histogram; of 1000
+        // 20.5 and 24.6 to 32.8; of 2000, as many as there is room for, 30.7 and 41.0 where top-k keeps most of them, else 26.6.
+        way.all = !few && (p.a.V <= kSampleList / 2 || (by_k && p.a.V <= kSampleList && top_k >= p.a.V / 2));
+        if (few || way.all) {
             uint64_t *list = reinterpret_cast<uint64_t *>(hist);
-            const int n = list_likely(s, sm, way, list, ranks, rank, top, c, sum, top_p, out);
+            int n = finite;
+            if (way.all) {
+                way.by_sum = false;
+                list_all(s, list, out);
+            } else {
+                n = list_likely(s, sm, way, list, ranks, rank, top, c, sum, top_p, out);
+            }
             if (n >= 0) {
                 row_sync(ranks);  // (all have looked at the others' numbers, and the list is there)
                 if (rank != 0 && !way.by_sum) return;
@@ -1682,7 +1742,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
                 // whose product with c is two roundings off (80); ex2, 4, and a dozen such factors where larger logits turn up (128).
                 const float off = (static_cast<float>(p.slice / kSampleThreads / 4) + 256.f) * 0x1p-24f;
                 if (rank == 0) {
-                    done = solve_likely(sm, way, list, n, reinterpret_cast<uint64_t *>(way.by_sum ? own : buffer + p.upto_at), edge, top_k, sum, off,
+                    done = solve_likely(sm, way, list, n, p.a.V, reinterpret_cast<uint64_t *>(way.by_sum ? own : buffer + p.upto_at), edge, top_k, sum, off,
                                         top_p, u, out);
                     if (threadIdx.x == 0) sm.first = done;
                 }
@@ -1702,7 +1762,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
             }
         }
         if (done) {
-        } else         if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out,
+        } else if (list_borders(s, sm, hist, own, ranks, rank, top, low, least, sum, finite, edge, by_k ? top_k : 0, top_p, u, out,
                          p.bits_at ? reinterpret_cast<uint32_t *>(buffer + p.bits_at) : nullptr)) {
             // the rest is the first CTA's; the others' shared memory is not read any more
             if (ranks > 1) {

@@ -165,6 +165,27 @@ def test_sizes(rows, V, kind):
 
 @gpu
 @needs_gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [31, 257, 512, 513, 1025, 2047, 2048, 2049])
+def test_short_rows(V, kind):
+    g = gen(V)
+    for stride in (V, V + 3):
+        z = logits(24, V, kind, V, spread=0.7, peaks=1)
+        on = torch.rand(24, V, generator=g) < 0.8
+        on[0], on[1] = False, True
+        z[2:5, ::3] = -INF
+        z[(torch.rand(24, V, generator=g) < 0.1) & ~on] = NAN
+        z[5] = torch.finfo(TYPES[kind]).min
+        u = torch.rand(24, generator=g).tolist()
+        k = torch.randint(V // 2, V + 2, (24,), generator=g).tolist()
+        p = torch.rand(24, generator=g).tolist()
+        for kw in (dict(), dict(p=p), dict(k=k), dict(k=k, p=p, m=[1e-3] * 24), dict(p=p, m=[1e-2] * 24), dict(p=[0.999] * 24, T=[3.0] * 24),
+                   dict(p=[-INF] * 24, m=[-INF] * 24)):
+            run_and_check(z, u, on=on, stride=stride, **kw)
+
+
+@gpu
+@needs_gpu
 @pytest.mark.parametrize("V", [5, 2048, 40000, 152064])
 def test_equal_logits_and_exact_borders(V):
     z = torch.full((8, V), 3.25)
