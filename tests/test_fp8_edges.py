@@ -228,6 +228,28 @@ def test_quantise_strides_and_magnitudes(kind):
 
 @gpu
 @needs_gpu
+@pytest.mark.parametrize("high", [1, 128])
+@pytest.mark.parametrize("cols", [8, 127, 128, 300, 384])
+def test_codes_at_any_address(cols, high):
+    """First columns and strides of every alignment; what lies around the codes stays."""
+    rows = 150
+    x = torch.randn(rows, cols, generator=torch.Generator().manual_seed(cols)).cuda().bfloat16()
+    want = torch.zeros(rows, cols, dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(-(-rows // high), -(-cols // 128), device="cuda")
+    rpd.quantize_fp8(x, want, scales, block_rows=high)
+    q, s = to_codes(x.float(), high)
+    assert torch.equal(want, q.view(torch.uint8)) and torch.equal(scales, s)
+    for first in range(9):
+        for apart in range(5):
+            buffer = torch.full((rows + 2, first + cols + apart), 0x55, dtype=torch.uint8, device="cuda")
+            again = torch.zeros_like(scales)
+            rpd.quantize_fp8(x, buffer[:rows, first:first + cols], again, block_rows=high)
+            assert torch.equal(buffer[:rows, first:first + cols], want) and torch.equal(again, scales), (first, apart)
+            assert (buffer[:, :first] == 0x55).all() and (buffer[:, first + cols:] == 0x55).all() and (buffer[rows:] == 0x55).all()
+
+
+@gpu
+@needs_gpu
 def test_quantise_every_quotient_of_8_bit_mantissas():
     """All pairs of bf16 mantissas as a block's largest number and another one: where ties are."""
     m = torch.arange(128, 256, device="cuda").float()
