@@ -95,15 +95,16 @@ __global__ void k_fp8_pack_scales(const float *scales, float *packed, int rows, 
 
 // Eight numbers over a scale as e4m3 codes: the fp32 quotient, rounded.  Of a product with the rounded reciprocal, off by a last
 // place at most, the rest x - q s is exact, and q + (rest) / s rounded once is the quotient rounded (Markstein, IBM J. Res. Dev. 34,
-// 1990): three operations where a division is some fifteen (a head of 126464 x 4096 took 865 us with these).  The rest has to
-// stay above fp32's smallest number wherever a code is not 0, which blocks of tiny numbers do not give: they are divided.
+// 1990): three operations where a division is some fifteen (a head of 126464 x 4096 took 865 us with these).  (q s - x taken away,
+// not x - q s added: so that -0 stays -0.)  The rest has to stay above fp32's smallest number wherever a code is not 0, which blocks of
+// tiny numbers do not give: they are divided.
 __device__ __forceinline__ uint2 fp8_codes(const float2 (&u)[4], float scale, float inverse) {
     float2 t[4];
     if (scale >= 0x1p-60f && scale <= 0x1p100f) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float qx = __fmul_rn(u[i].x, inverse), qy = __fmul_rn(u[i].y, inverse);
-            t[i] = make_float2(__fmaf_rn(__fmaf_rn(-qx, scale, u[i].x), inverse, qx), __fmaf_rn(__fmaf_rn(-qy, scale, u[i].y), inverse, qy));
+            t[i] = make_float2(__fmaf_rn(-__fmaf_rn(qx, scale, -u[i].x), inverse, qx), __fmaf_rn(-__fmaf_rn(qy, scale, -u[i].y), inverse, qy));
         }
     } else {
 #pragma unroll

@@ -250,6 +250,20 @@ def test_codes_at_any_address(cols, high):
 
 @gpu
 @needs_gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("high", [1, 128])
+def test_zeros_keep_their_sign(high, kind):
+    x = torch.tensor([0.0, -0.0, 1.5, -1e-6, 1e-6, -2.0, -0.0, 0.0]).repeat(130, 20).to(TYPES[kind]).cuda()
+    x[:, 128:] *= 0.0  # a block of zeros of both signs
+    q, s = to_codes(x, high)
+    codes = torch.full((130, 160), 0x55, dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(s.shape, device="cuda")
+    rpd.quantize_fp8(x, codes, scales, block_rows=high)
+    assert torch.equal(codes, q.view(torch.uint8)) and torch.equal(scales, s)
+
+
+@gpu
+@needs_gpu
 def test_quantise_every_quotient_of_8_bit_mantissas():
     """All pairs of bf16 mantissas as a block's largest number and another one: where ties are."""
     m = torch.arange(128, 256, device="cuda").float()
