@@ -550,8 +550,9 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
  * uniform[r] times the sum of all that are kept.  T = 0 keeps the first token alone, whatever the limits;
  * other T count as at least 1.45e-30 and at most 1.44e37.
  * Weights are right to some 2^-31 each, without bias, those of 2^-10 of their sum and more to 2^-42, and sums of
- * them are exact: which token a border falls on can differ from exact arithmetic's only where that is closer to it
- * than some 2^-38 of the sum.  The same call gives the same results every time.
+ * them are exact, in units of 2^-54 of the largest or finer than a 2^59th of the sum: which token a border falls on can
+ * differ from exact arithmetic's only where that is closer to it than some V 2^-55 of the sum, 2^-38 for V = 150000 (or
+ * 2^-31 of what weighs less than 2^-10 each, where that is more).  The same call gives the same results every time.
  *
  * 1 <= V <= 2^24, 0 <= rows <= 2^26 (larger: RPD_ERR_UNSUPPORTED; 0 is a no-op). */
 typedef struct rpd_sample_args {

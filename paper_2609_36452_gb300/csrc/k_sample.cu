@@ -48,7 +48,6 @@ struct SampleParams {
     rpd_sample_args a;
     int words;       // 32-bit words of a row of masks
     int slice;       // tokens of a CTA, a multiple of 32
-    int sum_bits;    // units of a row's sum of weights: 2^-sum_bits of the largest
     int list_at;     // in shared memory, where the histogram and then the lists are; behind them this CTA's bins of the row
     int upto_at;     // room for running sums of a list
     int bits_at;     // a slice's bits of the mask that goes out; 0 where these are too many
@@ -763,11 +762,9 @@ __device__ __forceinline__ void write_bits(const S &s, uint32_t *out, bool none,
 
 // Every border in four passes.  Leaves the result in every CTA.
 template <typename S>
-__device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ranks, int rank, int bits, float top, float edge, int top_k,
+__device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ranks, int rank, float top, float edge, int top_k,
                                            float top_p, float u) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) sm.w.set_floor(bits);
-    __syncthreads();
     float sum = 0.f;
     s.each([&](float z, int) { sum += ex2((z - top) * sm.w.c); });
 #pragma unroll
@@ -783,9 +780,13 @@ __device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ran
     if (threadIdx.x == 0) {
         sum = 0.f;
         for (int q = 0; q < ranks; ++q) sum += __uint_as_float(ld_cluster_u32(peer(&sm.sum, q)));
-        sm.w.set_big(fmaxf(sum, 1.f));
+        sum = fmaxf(sum, 1.f);
+        sm.plan.bits = min(54, 59 - ilogbf(sum));
+        sm.w.set_floor(sm.plan.bits);
+        sm.w.set_big(sum);
     }
     row_sync(ranks);
+    const int bits = sm.plan.bits;
     SampleCut cut{0u, 0x7FFFFFFF};
     int n, place;
     double mass = kept_mass(s, sm, ranks, bits, cut, n), weight, upto;
@@ -1777,13 +1778,13 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
                 SampleParams whole = p;
                 whole.slice = p.words * 32;
                 const Slice<T, false> row(whole, r, 0, buffer);
-                sample_slowly(row, sm, 1, 0, p.sum_bits, top, edge, top_k, top_p, u);
+                sample_slowly(row, sm, 1, 0, top, edge, top_k, top_p, u);
                 cut = sm.result.cut;
                 if (out) write_bits(row, out, false, [&](float z, int v) { return z >= kLowest && cut.keeps(order_key(z), v); });
                 done = true;
             }
         } else {
-            sample_slowly(s, sm, ranks, rank, p.sum_bits, top, edge, top_k, top_p, u);
+            sample_slowly(s, sm, ranks, rank, top, edge, top_k, top_p, u);
             cut = sm.result.cut;
         }
     }
@@ -1895,9 +1896,6 @@ extern "C" int rpd_sample(const rpd_sample_args *args, void *stream_ptr) {
     SampleParams p{};
     p.a = a;
     p.words = (a.V + 31) / 32;
-    int bits = 0;
-    while (1 << bits < a.V) ++bits;
-    p.sum_bits = std::min(54, 62 - bits);
     cudaStream_t s = static_cast<cudaStream_t>(stream_ptr);
     e = a.type == RPD_TYPE_F32    ? launch_sample<float>(p, num_sms, s)
         : a.type == RPD_TYPE_BF16 ? launch_sample<__nv_bfloat16>(p, num_sms, s)

@@ -260,6 +260,30 @@ def test_random_rows():
 
 @gpu
 @needs_gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_draws_from_the_tail(kind):
+    """Tokens that weigh 2^-24 of the sum and less.  Units of 2^-54 of the largest weight, cut off, take 152064 / 2 of them, 2^-37.8, at
+    most; weights that are 2^-31 off take 2^-35.3 if all of a tail of 0.05 were off alike.  Together less than 2^-35 of the sum."""
+    rows, V = 197, 152064
+    z = logits(rows, V, kind, 41, spread=1.0).cuda()
+    T = (0.4 + 0.6 * torch.rand(rows, generator=gen(42))).float().cuda()
+    zd, order = torch.sort(z.double(), dim=1, descending=True, stable=True)
+    C = torch.exp((zd - zd[:, :1]) / T.double()[:, None]).cumsum(1)
+    S = C[:, -1]
+    token, status = (torch.full((rows,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    for seed in range(20):
+        u = (1 - 0.02 * torch.rand(rows, generator=gen(100 + seed))).float().clamp(max=1 - 2.0 ** -24).cuda()
+        rpd.sample(z, u, token, status, temperature=T)
+        at = (order == token[:, None]).int().argmax(1)
+        with_it = C.gather(1, at[:, None])[:, 0]
+        before = torch.where(at > 0, C.gather(1, (at - 1).clamp(min=0)[:, None])[:, 0], torch.zeros_like(S))
+        target = u.double() * S
+        assert (status == 0).all()
+        assert (target < with_it + 2.0 ** -35 * S).all() and (target > before - 2.0 ** -35 * S).all()
+
+
+@gpu
+@needs_gpu
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 def test_min_p_at_its_border(kind):
     """Logits one step of the type above and below the largest one plus T ln min_p, for many min_p."""
