@@ -550,7 +550,7 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
  * uniform[r] times the sum of all that are kept.  T = 0 keeps the first token alone, whatever the limits;
  * other T count as at least 1.45e-30 and at most 1.44e37.
  * Weights are right to some 2^-31 each, without bias, those of 2^-10 of their sum and more to 2^-42, and sums of
- * them are exact, in units of 2^-54 of the largest or finer than a 2^59th of the sum: which token a border falls on can
+ * them are exact, in units of 2^-54 of the largest or some 2^-59 of the sum, whichever is more: which token a border falls on can
  * differ from exact arithmetic's only where that is closer to it than some V 2^-55 of the sum, 2^-38 for V = 150000 (or
  * 2^-31 of what weighs less than 2^-10 each, where that is more).  The same call gives the same results every time.
  *
