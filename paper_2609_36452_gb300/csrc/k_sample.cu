@@ -26,6 +26,7 @@
 #include "logits_row.cuh"
 #include "op_host.h"
 #include "ptx.cuh"
+#include "sample_bins.h"
 
 namespace rpd {
 namespace {
@@ -40,7 +41,7 @@ constexpr int kSampleBins = 4096;          // of the first histogram
 constexpr int kBinParts = 256;             // parts of a bin, of which the mean is kept
 constexpr int kBinOctaves = 64;            // what the bins span at most: a bin is a 64th of an octave of weights, or less
 constexpr float kBinError = 0x1p-14f;      // of a sum of bins' weights, taken at their tokens' mean places: at most 2^-16 for
-                                           // the spread around the mean and 2^-15.5 for the parts
+                                           // the spread around the mean, 2^-15.5 for the parts and 2^-19 for the units
 constexpr int kSampleList = 2048;          // tokens that are sorted
 constexpr float kLowest = -3.402823466e38f;
 
@@ -496,6 +497,7 @@ struct SampleShared {
     float range[5][kSampleWarps];  // largest, smallest, sum, n-th of the threads' largest, weights of the n largest
     int finite[kSampleWarps], binned[kSampleWarps];
     float sums[kSampleWarps];
+    uint32_t units[kSampleWarps];
     float sum;
     int counts[kSampleWarps];
     // what the first CTA of the cluster has found
@@ -992,41 +994,42 @@ __device__ __forceinline__ SampleHit find_entry(const uint64_t *list, const uint
     return sm.hit;
 }
 
-// A CTA's bins of the row's histogram: counts and sums of weights, kPer neighbours a thread; and the running ones before each
+// A CTA's bins of the row's histogram: counts and weights in units, kPer neighbours a thread; and the running ones before each
 // thread's, of the row.
 struct SampleBins {
     const uint2 *own;
     int per, first;    // bins of a thread, and the first of this one's among the row's
     int count0, count1, all_count;  // before and behind this thread's, and of the row
-    float sum0, sum1, all_sum;
-    // The first bin up to whose end there are `least` tokens (by_count), or a sum of `least` or more (or of more), in every CTA's
-    // found[slot]; what was there stays where there is none.
+    uint32_t units0, units1;
+    float unit;        // weight of one
+    // The first bin for which the border's condition holds, in every CTA's found[slot] (one thread of the row has it; see
+    // BinBorder); what was there stays where it holds for none.
     __device__ __forceinline__ void find(SampleShared &sm, int slot, int ranks, bool by_count, float least, bool more) const {
-        const auto f = [&](int n, float m) { return by_count ? n >= static_cast<int>(least) : more ? m > least : m >= least; };
-        if ((first && f(count0, sum0)) || !f(count1, sum1)) return;
+        const BinBorder border{by_count, more, least, unit};
+        if (!border.within(first == 0, count0, units0, count1, units1)) return;
         int i = 0, n = count0, n1 = n;
-        float m = sum0, m1 = m;
+        uint32_t m = units0, m1 = m;
         for (;; ++i) {
             const uint2 v = own[i];
             n1 = n + static_cast<int>(v.x);
-            m1 = m + __uint_as_float(v.y);
-            if (i == per - 1 || f(n1, m1)) break;
+            m1 = m + v.y;
+            if (i == per - 1 || border.holds(n1, m1)) break;
             n = n1;
             m = m1;
         }
-        tell(sm, slot, ranks, {first + i, n, n1, m, m1});
+        tell(sm, slot, ranks, {first + i, n, n1, border.weight(m), border.weight(m1)});
     }
     // The same for a bin that is known.
     __device__ __forceinline__ void find_bin(SampleShared &sm, int slot, int ranks, int bin) const {
         if (bin < first || bin >= first + per) return;
         int n = count0;
-        float m = sum0;
+        uint32_t m = units0;
         for (int i = 0; i < bin - first; ++i) {
             n += static_cast<int>(own[i].x);
-            m += __uint_as_float(own[i].y);
+            m += own[i].y;
         }
         const uint2 v = own[bin - first];
-        tell(sm, slot, ranks, {bin, n, n + static_cast<int>(v.x), m, m + __uint_as_float(v.y)});
+        tell(sm, slot, ranks, {bin, n, n + static_cast<int>(v.x), static_cast<float>(m) * unit, static_cast<float>(m + v.y) * unit});
     }
     __device__ __forceinline__ void tell(SampleShared &sm, int slot, int ranks, const SampleFound &f) const {
         for (int q = 0; q < ranks; ++q) {
@@ -1040,8 +1043,9 @@ struct SampleBins {
     }
 };
 
-// The slices' histograms become the row's, a part of the bins a CTA.
-__device__ __forceinline__ SampleBins make_bins(SampleShared &sm, const uint32_t *hist, uint8_t *own, int ranks, int rank, float octaves) {
+// The slices' histograms become the row's, a part of the bins a CTA.  `sum`: about that of the row's weights, 1 at least.
+__device__ __forceinline__ SampleBins make_bins(SampleShared &sm, const uint32_t *hist, uint8_t *own, int ranks, int rank, float octaves, float sum) {
+    const float units = kBinUnits / sum;
     const int per_rank = kSampleBins / ranks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint2 *mine = reinterpret_cast<uint2 *>(own);
     for (int i = threadIdx.x; i < per_rank; i += kSampleThreads) {
@@ -1055,25 +1059,26 @@ __device__ __forceinline__ SampleBins make_bins(SampleShared &sm, const uint32_t
             parts += v[q] & 0xFFFFFu;
         }
         const float mean = n ? __fdividef(static_cast<float>(parts), static_cast<float>(n)) + 0.5f : 0.f;
-        mine[i] = make_uint2(n, __float_as_uint(static_cast<float>(n) * ex2(-(static_cast<float>(b * kBinParts) + mean) * octaves)));
+        mine[i] = make_uint2(n, bin_units(static_cast<float>(n) * ex2(-(static_cast<float>(b * kBinParts) + mean) * octaves), units));
     }
     __syncthreads();
     SampleBins bins;
     bins.per = per_rank / kSampleThreads;
     bins.own = mine + threadIdx.x * bins.per;
     bins.first = rank * per_rank + static_cast<int>(threadIdx.x) * bins.per;
+    bins.unit = sum / kBinUnits;
     int n = 0;
-    float m = 0.f;
+    uint32_t m = 0;
     for (int i = 0; i < bins.per; ++i) {
         n += static_cast<int>(bins.own[i].x);
-        m += __uint_as_float(bins.own[i].y);
+        m += bins.own[i].y;
     }
     int n_upto = n;
-    float m_upto = m;
+    uint32_t m_upto = m;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int nu = __shfl_up_sync(0xffffffffu, n_upto, o);
-        const float mu = __shfl_up_sync(0xffffffffu, m_upto, o);
+        const uint32_t mu = __shfl_up_sync(0xffffffffu, m_upto, o);
         if (lane >= o) {
             n_upto += nu;
             m_upto += mu;
@@ -1081,44 +1086,32 @@ __device__ __forceinline__ SampleBins make_bins(SampleShared &sm, const uint32_t
     }
     if (lane == 31) {
         sm.counts[warp] = n_upto;
-        sm.sums[warp] = m_upto;
+        sm.units[warp] = m_upto;
     }
     row_sync(ranks);
     // totals of all warps before this one, in this CTA and those before
     int n_before = 0, n_all = 0;
-    float m_before = 0.f, m_all = 0.f;
+    uint32_t m_before = 0;
 #pragma unroll
     for (int i = 0; i < kSampleSteps; ++i) {
         const int q = 32 / kSampleWarps * i + lane / kSampleWarps, w = lane % kSampleWarps;
         if (q < ranks) {
             const int nw = static_cast<int>(ld_cluster_u32(peer(&sm.counts[w], q)));
-            const float mw = __uint_as_float(ld_cluster_u32(peer(&sm.sums[w], q)));
             n_all += nw;
-            m_all += mw;
             if (q < rank || (q == rank && w < warp)) {
                 n_before += nw;
-                m_before += mw;
+                m_before += ld_cluster_u32(peer(&sm.units[w], q));
             }
         }
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        m_all += __shfl_xor_sync(0xffffffffu, m_all, o);
-        m_before += __shfl_xor_sync(0xffffffffu, m_before, o);
-    }
     n_all = __reduce_add_sync(0xffffffffu, n_all);
     n_before = __reduce_add_sync(0xffffffffu, n_before);
+    m_before = __reduce_add_sync(0xffffffffu, m_before);
     bins.count1 = n_before + n_upto;
-    bins.sum1 = m_before + m_upto;
-    // (what is before a thread is what is behind the one before it: the same number, so that one of them has a border)
-    bins.count0 = __shfl_up_sync(0xffffffffu, bins.count1, 1);
-    bins.sum0 = __shfl_up_sync(0xffffffffu, bins.sum1, 1);
-    if (lane == 0) {
-        bins.count0 = n_before;
-        bins.sum0 = m_before;
-    }
+    bins.units1 = m_before + m_upto;
+    bins.count0 = bins.count1 - n;
+    bins.units0 = bins.units1 - m;
     bins.all_count = n_all;
-    bins.all_sum = m_all;
     return bins;
 }
 
@@ -1128,7 +1121,6 @@ __device__ __forceinline__ SamplePlan plan_borders(SampleShared &sm, const Sampl
                                                    int expected, int top_k, float top_p, float u) {
     constexpr float kEnd = static_cast<float>(kSampleBins) * kBinParts;
     const auto place_of = [](int bin) { return static_cast<float>(bin) * kBinParts; };
-    sum = fmaxf(sum, 1.f);
     const float error = kBinError * sum;
     const float edge_place = edge == kNoLogit ? kEnd : fminf(sample_place(edge, top, scale), kEnd);
     SamplePlan plan{};
@@ -1244,7 +1236,8 @@ __device__ __forceinline__ bool list_borders(const S &s, SampleShared &sm, uint3
             }
     });
     const int expected = sum_of_row(sm, ranks, binned);
-    const SampleBins bins = make_bins(sm, hist, own, ranks, rank, scale > 0.f ? c / scale : 0.f);
+    sum = fmaxf(sum, 1.f);
+    const SampleBins bins = make_bins(sm, hist, own, ranks, rank, scale > 0.f ? c / scale : 0.f, sum);
     SamplePlan plan = plan_borders(sm, bins, ranks, top, edge, scale, sum, expected, top_k, top_p, u);
     if (plan.slow) {
         row_sync(ranks);
