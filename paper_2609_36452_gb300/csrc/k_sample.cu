@@ -337,9 +337,13 @@ __device__ __forceinline__ SampleRange<T> load_slice(const Slice<T, kResident> &
 // 2^((z - top) c) in units of 2^-bits, c = log2 e / T as the sum of two floats.  y = (z - A) c is a product and its
 // error; k is y to the nearest 1/512, the rest |r| <= 2^-9 (after that of the largest logit is taken off), and 2^y =
 // 2^(whole part of k) table[k mod 512] (1 + r ln 2 + ...).  A = 0, or the largest logit where that times c leaves
-// the range of k: logits that count are then within a factor of two of it, and the difference is exact.
+// the range of k: logits that count are then within a factor of two of it, and the difference is exact.  From T = 2^96 on logits and
+// T are taken 2^-32 times, which is exact for all that counts beside such a T: the floor of the weights, 54 octaves and more
+// below the largest logit, is then an fp32 number for every T and logit, and a logit of -infinity, below it, weighs 0; and c_lo
+// keeps its digits.
 struct SampleWeights {
-    float A, c_hi, c_lo, rest_top, least, big;
+    float A, c_hi, c_lo, rest_top, least, big;  // A and least as z times shrink
+    float shrink;
     int k_top;  // as the bits of the shifted product
     int64_t rest64_top;
     float c, top, temperature;
@@ -355,20 +359,26 @@ struct SampleWeights {
     __device__ void set_temperature(float T) {
         constexpr float kHigh = 1.44269502f, kLow = 1.92596303e-8f;  // log2 e
         temperature = T;
+        c = __fdiv_rn(kHigh, T);
+        shrink = T < 0x1p96f ? 1.f : 0x1p-32f;
+        T *= shrink;
         c_hi = __fdiv_rn(kHigh, T);
         c_lo = __fdiv_rn(fmaf(-c_hi, T, kHigh) + kLow, T);
-        c = c_hi;
     }
+    // z times shrink, from A on.
+    __device__ __forceinline__ float from_A(float z) const { return fmaf(z, shrink, -A); }
     __device__ void set_top(float top_logit) {
         top = top_logit;
-        A = fabsf(top_logit) * c < 0x1p12f ? 0.f : top_logit;
-        k_top = split(top_logit - A, rest_top);
-        rest64_top = rest64(top_logit - A, k_top);
+        A = 0.f;
+        const float shrunk = from_A(top_logit);
+        if (!(fabsf(shrunk) * c_hi < 0x1p12f)) A = shrunk;
+        k_top = split(shrunk - A, rest_top);
+        rest64_top = rest64(shrunk - A, k_top);
         big = -kNoLogit;
     }
     // Logits so far below weigh nothing: under 2^-bits.
     __device__ void set_floor(int bits) {
-        least = (top - A) - (static_cast<float>(bits) + 0.5f) / c;
+        least = from_A(top) - (static_cast<float>(bits) + 0.5f) / c_hi;
     }
     // Of a sum of about `sum` times the largest weight, those that hold 2^-10 and more.
     __device__ void set_big(float sum) { big = top - (10.f - log2f(sum)) / c; }
@@ -380,7 +390,7 @@ struct SampleWeights {
     // Two at a time.  A logit at the floor and below gets the weight 0: its difference is taken for one of bits + 1/2 octaves,
     // and the shift leaves nothing.
     __device__ __forceinline__ void two_of(float z0, float z1, int bits, const uint32_t *table, uint64_t (&m)[2]) const {
-        const f32x2 d = pack2(fmaxf(z0 - A, least), fmaxf(z1 - A, least)), c2 = pack2(c_hi, c_hi), shift = pack2(kShift, kShift);
+        const f32x2 d = pack2(fmaxf(from_A(z0), least), fmaxf(from_A(z1), least)), c2 = pack2(c_hi, c_hi), shift = pack2(kShift, kShift);
         const f32x2 minus = pack2(-1.f, -1.f);
         const f32x2 y = mul2(d, c2), t = add2(y, shift);
         // (y - (t - shift)) + (d c_lo + (d c_hi - y)) - rest_top
@@ -417,9 +427,10 @@ struct SampleWeights {
     }
     // The same weight with every step in 64 bits, right to some 2^-42.
     __device__ __noinline__ uint64_t in_64_bits(float z, int bits, const SampleTable *table) const {
-        if (!(z - A > least)) return 0;
+        const float d = from_A(z);
+        if (!(d > least)) return 0;
         int k;
-        const int64_t r = rest64(z - A, k) - rest64_top;
+        const int64_t r = rest64(d, k) - rest64_top;
         k -= k_top;
         uint64_t m = power(r, k, table);  // 2^52 to 2^53
         const int down = 52 - bits - (k >> 9);
@@ -1734,7 +1745,9 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
                 if (rank != 0 && !way.by_sum) return;
                 // In units of 2^-24 of the sum: additions, one for every four of a thread's tokens; exponents of up to 40 octaves,
                 // whose product with c is two roundings off (80); ex2, 4, and a dozen such factors where larger logits turn up (128).
-                const float off = (static_cast<float>(p.slice / kSampleThreads / 4) + 256.f) * 0x1p-24f;
+                // Logits more than fp32's largest number below the top are taken for -infinity: where T is as large, they weigh up to
+                // 2^-34 each.
+                const float off = (static_cast<float>(p.slice / kSampleThreads / 4) + 256.f) * 0x1p-24f + (T_used < 0x1p118f ? 0.f : p.a.V * 0x1p-34f);
                 if (rank == 0) {
                     done = solve_likely(sm, way, list, n, p.a.V, reinterpret_cast<uint64_t *>(way.by_sum ? own : buffer + p.upto_at), edge, top_k, sum, off,
                                         top_p, u, out);
