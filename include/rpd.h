@@ -549,10 +549,11 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
  * The token is the first, in that order, at which the sum of the kept weights up to and with it exceeds
  * uniform[r] times the sum of all that are kept.  T = 0 keeps the first token alone, whatever the limits;
  * other T count as at least 1.45e-30 and at most 1.44e37.
- * Weights are right to some 2^-31 each, without bias, those of 2^-10 of their sum and more to 2^-42, and sums of
- * them are exact, in units of 2^-54 of the largest or some 2^-59 of the sum, whichever is more: which token a border falls on can
- * differ from exact arithmetic's only where that is closer to it than some V 2^-55 of the sum, 2^-38 for V = 150000 (or
- * 2^-31 of what weighs less than 2^-10 each, where that is more).  The same call gives the same results every time.
+ * Weights are right to some 2^-31 each, without bias, those of 2^-10 of the row's sum and more to 2^-42.  Sums of them are exact, in
+ * units of 2^-54 of the largest or some 2^-59 of the sum of all of the row's, whichever is more, and of 2^-52 of the largest at
+ * most where no more than 2048 tokens can be kept: which token a border falls on can differ from exact arithmetic's only where that is closer
+ * to it than some V 2^-55 of that sum, 2^-38 for V = 150000 (2^-42 for V < 8192; or 2^-31 of what weighs less than 2^-10 each,
+ * where that is more).  The same call gives the same results every time.
  *
  * 1 <= V <= 2^24, 0 <= rows <= 2^26 (larger: RPD_ERR_UNSUPPORTED; 0 is a no-op). */
 typedef struct rpd_sample_args {

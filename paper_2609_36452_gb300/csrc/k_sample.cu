@@ -43,6 +43,7 @@ constexpr int kBinOctaves = 64;            // what the bins span at most: a bin 
 constexpr float kBinError = 0x1p-14f;      // of a sum of bins' weights, taken at their tokens' mean places: at most 2^-16 for
                                            // the spread around the mean, 2^-15.5 for the parts and 2^-19 for the units
 constexpr int kSampleList = 2048;          // tokens that are sorted
+constexpr int kSampleBits = 54;            // sums are in units of 2^-54 of the largest weight, or of more where they would not fit
 constexpr float kLowest = -3.402823466e38f;
 
 struct SampleParams {
@@ -334,6 +335,12 @@ __device__ __forceinline__ SampleRange<T> load_slice(const Slice<T, kResident> &
 
 // ------------------------------------------------------------------------------ weights
 
+// Units of a sum of about `sum` times the largest weight, 1 at least: 2^-54 of the largest weight, or some 2^-59 of the sum.
+__device__ __forceinline__ int units_of(float sum) { return min(kSampleBits, 59 - ilogbf(sum)); }
+// For n tokens of a list, whose sum is n at most: it fits 2^63 (2^-54 for 512, 2^-52 for 2048).  (An estimate of the sum gave 2048 the
+// smaller units too, and every row that is decided by a list 0.2 us more.)
+__device__ __forceinline__ int list_units(int n) { return min(kSampleBits, 31 + __clz(n - 1)); }
+
 // 2^((z - top) c) in units of 2^-bits, c = log2 e / T as the sum of two floats.  y = (z - A) c is a product and its
 // error; k is y to the nearest 1/512, the rest |r| <= 2^-9 (after that of the largest logit is taken off), and 2^y =
 // 2^(whole part of k) table[k mod 512] (1 + r ln 2 + ...).  A = 0, or the largest logit where that times c leaves
@@ -483,7 +490,7 @@ struct SamplePlan {
     float draw0, draw1, cut0, cut1;  // places, in parts of bins
     int cut_count;          // tokens before cut0
     float sum;              // about that of all weights
-    int bits;               // units of sums: 2^-bits of the largest weight; all of them fit 62 bits
+    int bits;               // units of sums: 2^-bits of the largest weight
 };
 // An entry of a sorted list, and the weights before it.
 struct SampleHit {
@@ -794,7 +801,7 @@ __device__ __noinline__ void sample_slowly(const S &s, SampleShared &sm, int ran
         sum = 0.f;
         for (int q = 0; q < ranks; ++q) sum += __uint_as_float(ld_cluster_u32(peer(&sm.sum, q)));
         sum = fmaxf(sum, 1.f);
-        sm.plan.bits = min(54, 59 - ilogbf(sum));
+        sm.plan.bits = units_of(sum);
         sm.w.set_floor(sm.plan.bits);
         sm.w.set_big(sum);
     }
@@ -1136,7 +1143,7 @@ __device__ __forceinline__ SamplePlan plan_borders(SampleShared &sm, const Sampl
     const float edge_place = edge == kNoLogit ? kEnd : fminf(sample_place(edge, top, scale), kEnd);
     SamplePlan plan{};
     plan.sum = sum;
-    plan.bits = min(54, 59 - ilogbf(plan.sum));
+    plan.bits = top_k > 0 ? list_units(top_k) : units_of(sum);
     plan.cut0 = plan.cut1 = -1.f;
     plan.slow = bins.all_count != expected;  // a bin had more tokens than it can count
     if (top_k > 0) {
@@ -1515,13 +1522,14 @@ __device__ __forceinline__ void list_all(const S &s, uint64_t *list, uint32_t *o
 // as long as both ends do the same; false where they do not.
 __device__ __forceinline__ bool solve_likely(SampleShared &sm, const SampleShort &way, uint64_t *list, int n, int V, uint64_t *upto, float edge, int top_k,
                                              float sum, float off, float top_p, float u, uint32_t *out) {
-    const int bits = min(54, 59 - ilogbf(way.by_sum || way.all ? fmaxf(sum, 1.f) : static_cast<float>(kSampleList)));
+    const int listed = n;
+    if (way.by_k) n = min(n, top_k);
+    const int bits = way.by_sum ? units_of(fmaxf(sum, 1.f)) : list_units(n);  // (the sum of all has to fit too)
     if (threadIdx.x == 0) {
         sm.w.set_floor(bits);
         sm.w.big = kNoLogit;  // (few tokens: all of them in 64 bits)
     }
-    sort_entries(list, way.all ? V : n, 0);
-    if (way.by_k) n = min(n, top_k);
+    sort_entries(list, way.all ? V : listed, 0);
     const uint64_t mine = add_up(list, n, upto, bits, sm);
     uint64_t low = ~0ull, high = ~0ull;
     if (top_p < 1.f) {
@@ -1808,7 +1816,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
 
 constexpr int kSampleSmem = 200 * 1024;
 constexpr int kSampleSlice = 80 * 1024;  // that stays in shared memory, two of them beside each other; a longer one is read again
-constexpr int kSampleBits = 48 * 1024;   // of a slice, at most
+constexpr int kSampleMask = 48 * 1024;   // of a slice's bits, at most
 
 // CTAs of a row, two of which an SM holds: as many as run at once, but no slice shorter than some 8000 tokens.  One row of
 // 126464 tokens with top-p: 22 us with eight, 28 with four; 7 rows of 50021: 22.4 with four, 23.4 with eight; one row of 4096: 9.3
@@ -1832,7 +1840,7 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t s) {
     p.upto_at = p.list_at >= kSampleList * 8 ? 0 : p.list_at + kSampleList * 8;
     p.bits_at = p.list_at + kSampleList * 8 + (p.upto_at ? std::max(own_bytes, kSampleList * 8) : own_bytes);
     long long bytes = p.bits_at;
-    if (p.a.out_allowed && p.slice / 8 <= kSampleBits)
+    if (p.a.out_allowed && p.slice / 8 <= kSampleMask)
         bytes += p.slice / 8;
     else
         p.bits_at = 0;

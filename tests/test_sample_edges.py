@@ -2,6 +2,8 @@
 equal, probabilities as close as in test_sample.py."""
 import pytest
 import torch
+
+import paper_2609_36452_gb300 as rpd
 from test_sample import INF, NAN, TYPES, gen, gpu, logits, needs_gpu, run_and_check
 
 # from where the largest logit less 54 octaves of weights still is an fp32 number to the largest temperature there is
@@ -49,3 +51,40 @@ def test_logits_as_large_as_the_temperature(T, V, kind):
     p = [0.9, 0.5, 0.99] * 3
     for kw in (dict(), dict(p=p), dict(p=p, m=[1e-4] * rows), dict(m=[1e-4] * rows), dict(k=[30, 300, V // 2] * 3, p=p)):
         run_and_check(z, u, [T] * rows, stride=V + 1, **kw)
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("V,count,limits", [
+    (5000, 40, "k"), (5000, 500, "k"), (5000, 1000, "k"), (5000, 2048, "k"), (900, 600, "k"), (2000, 1500, "k"), (300, 300, ""), (1024, 1000, ""),
+    (5000, 40, "m"), (5000, 500, "m"), (5000, 1500, "m"), (126464, 2048, "k"), (126464, 1500, "m")])
+def test_light_tokens_beside_a_heavy_one(V, count, limits):
+    """Probabilities of tokens of 2^-21 of the sum altogether.  Sums are in units of 2^-54 of the largest weight, lists of more than 512
+    tokens in units of 2^-52: a token's weight is one of them off at most (a weight that is a product of 32-bit numbers is cut off to
+    whole units: rows whose other tokens overflow a bin, 126464 of them here; one made in 64 bits is rounded), and their
+    sum, of which the quotient is taken, count of them.  Weights themselves are right to 2^-30, the quotient to 2^-29, and half of
+    fp32's eps comes with the result."""
+    rows, g = 40, gen(V + count)
+    T = 0.5 + torch.rand(rows, generator=g)
+    light = 2.0 ** -21 / count * torch.exp2(torch.rand(rows, count, generator=g, dtype=torch.float64) - 0.5)
+    z = torch.full((rows, V), -60.0)
+    z[:, :count] = (T.double()[:, None] * torch.log(light)).float()
+    z[:, 7] = 0.0
+    z = z[:, torch.randperm(V, generator=g)]
+    u = 1 - 2.0 ** -24 * torch.tensor([1.0, 2.0, 3.0, 4.0]).repeat(rows // 4)
+    w = torch.where(z < -50.0, 0.0, torch.exp(z.double() / T.double()[:, None]))
+    if not limits:
+        w = torch.exp(z.double() / T.double()[:, None])
+    dev = z.cuda()
+    token, status = (torch.full((rows,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    prob = torch.zeros(rows, device="cuda")
+    rpd.sample(dev, u.cuda(), token, status, temperature=T.cuda(), out_prob=prob,
+               top_k=torch.full((rows,), count, dtype=torch.int32, device="cuda") if limits == "k" else None,
+               min_p=torch.full((rows,), 2.0 ** -50, device="cuda") if limits == "m" else None)
+    assert (status == 0).all()
+    want = w.gather(1, token.long().cpu()[:, None])[:, 0] / w.sum(1)
+    assert (want < 2.0 ** -20 / count).all()
+    off = (prob.cpu().double() - want).abs()
+    unit = 2.0 ** -54 if count <= 512 else 2.0 ** -52
+    most = want * (2.0 ** -24 + 2.0 ** -28 + count * unit) + unit
+    assert (off <= most).all(), float((off / most).max())
