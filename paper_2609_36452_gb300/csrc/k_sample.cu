@@ -1618,22 +1618,28 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
         sm.finite[warp] = finite;
     }
     row_sync(ranks);
-    float tops[kSampleSteps], sums[kSampleSteps], likelies[kSampleSteps];
+    // Under top-p eight CTAs hand on their warps' largest logits, of 128 warps: above the least of them are some 700 tokens (128 times 1 + 1/2 +
+    // ... + 1/128), more than a list has room for then, and listing them in vain took a row of 126464 from 25 to 29 us.  Of the
+    // largest of each lane's four the least has some 130 above it.
+    const bool by_four = top_k <= 0 && ranks == kSampleMaxCluster;
+    float tops[kSampleSteps], sums[kSampleSteps], likelies[kSampleSteps], nth_tops[kSampleSteps];
     top = kLowest;
-    low = nth_top = -kNoLogit;
+    low = -kNoLogit;
+    nth_top = by_four ? kNoLogit : -kNoLogit;
     finite = 0;
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kSampleSteps; ++i) {
         const int q = 32 / kSampleWarps * i + lane / kSampleWarps, w = lane % kSampleWarps;
         tops[i] = kLowest;
-        sums[i] = likelies[i] = 0.f;
+        sums[i] = likelies[i] = nth_tops[i] = 0.f;
         if (q < ranks) {
             likelies[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[4][w], q)));
             tops[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[0][w], q)));
             sums[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[2][w], q)));
             low = fminf(low, __uint_as_float(ld_cluster_u32(peer(&sm.range[1][w], q))));
-            nth_top = fminf(nth_top, __uint_as_float(ld_cluster_u32(peer(&sm.range[3][w], q))));
+            nth_tops[i] = __uint_as_float(ld_cluster_u32(peer(&sm.range[3][w], q)));
+            nth_top = by_four ? fmaxf(nth_top, nth_tops[i]) : fminf(nth_top, nth_tops[i]);
             finite += static_cast<int>(ld_cluster_u32(peer(&sm.finite[w], q)));
         }
         top = fmaxf(top, tops[i]);
@@ -1649,7 +1655,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
     for (int i = 0; i < kSampleSteps; ++i) {
         const float factor = ex2((tops[i] - top) * c);
         sum += sums[i] * factor;
-        likely += likelies[i] * factor;
+        if (nth_tops[i] >= nth_top) likely += likelies[i] * factor;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {

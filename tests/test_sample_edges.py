@@ -88,3 +88,21 @@ def test_light_tokens_beside_a_heavy_one(V, count, limits):
     unit = 2.0 ** -54 if count <= 512 else 2.0 ** -52
     most = want * (2.0 ** -24 + 2.0 ** -28 + count * unit) + unit
     assert (off <= most).all(), float((off / most).max())
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,V", [(1, 65536), (24, 70001), (5, 130000)])
+def test_few_rows_under_top_p(rows, V, kind):
+    """Eight CTAs a row: top-p's tokens from one to thousands, likely ones beside each other, in one CTA's slice or over all of them."""
+    g = gen(V)
+    for spread, peaks in ((0.3, 6), (1.5, 6), (2.5, 1), (1.0, 300), (1.0, 900)):
+        z = logits(rows, V, kind, V + peaks, spread=spread, peaks=peaks)
+        z[::3, 100:100 + 2 * peaks] = (8 + 2 * torch.randn(len(z[::3]), 2 * peaks, generator=g)).to(z.dtype)
+        for low, high in ((0.2, 0.9), (0.9, 0.999), (0.9999, 1.0)):
+            p = (low + (high - low) * torch.rand(rows, generator=g)).tolist()
+            T = (0.5 + torch.rand(rows, generator=g)).tolist()
+            u = torch.rand(rows, generator=g).tolist()
+            run_and_check(z, u, T, None, p, None, stride=V + 3)
+            run_and_check(z, u, T, None, p, [10.0 ** -i for i in range(rows)] if rows < 24 else None)
