@@ -431,7 +431,9 @@ void rpd_quant_destroy(rpd_quant *head);
  * |u[r][k]| of the block / 448, qx = u / sx, both divisions in fp32, the quotient rounded to the nearest
  * e4m3 number (ties to even; a block whose scale is 0 has codes of 0).  Sums are fp32; the logits are
  * rounded once, to the type of `out`.  Inputs and u must be finite, codes no NaN, scales 0 or within
- * 2^-100 .. 2^110 in size.
+ * 2^-100 .. 2^100 in size: sums are kept relative to the power of two E at the row's largest |u|, and 32768 columns then stay
+ * below 2^125.  A block counts with all of fp32's digits where sx and sx sw are at least 2^-126 E (its activations, at scales of
+ * 2^-100, at least 2^-16 of the row's largest).
  *
  * rpd_fp8_create: a head of d columns and V rows on the current device; 1 <= d <= 32768, 1 <= V <= 2^24 and
  * fewer than 256 GB of codes.  NULL on failure. */
