@@ -936,7 +936,7 @@ __device__ __noinline__ int sort_entries(uint64_t *list, int n0, int n1) {
     return size;
 }
 
-// a f, f in [0, 1), rounded down or up.
+// a f, f in [0, 1) and not -0, rounded down or up.
 __device__ __forceinline__ uint64_t times_fraction(uint64_t a, float f, bool up) {
     const uint32_t b = __float_as_uint(f), e = b >> 23;
     const uint64_t m = e ? (b & 0x7FFFFFu) | 0x800000u : b & 0x7FFFFFu;
@@ -1582,8 +1582,9 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleResident / kSampleThrea
     }
     pdl_wait();
     const Slice<T, kResident> s(p, r, rank, buffer);
-    const float T_row = p.a.temperature ? p.a.temperature[r] : 1.f, u = p.a.uniform ? p.a.uniform[r] : 0.f;
-    const float top_p = p.a.top_p ? p.a.top_p[r] : 1.f, min_p = p.a.min_p ? p.a.min_p[r] : 0.f;
+    // (+ 0: -0 becomes 0, whose bits times_fraction takes)
+    const float T_row = p.a.temperature ? p.a.temperature[r] : 1.f, u = p.a.uniform ? p.a.uniform[r] + 0.f : 0.f;
+    const float top_p = p.a.top_p ? p.a.top_p[r] + 0.f : 1.f, min_p = p.a.min_p ? p.a.min_p[r] : 0.f;
     const int top_k = p.a.top_k ? p.a.top_k[r] : 0;
     uint32_t *out = p.a.out_allowed ? reinterpret_cast<uint32_t *>(p.a.out_allowed) + r * p.words : nullptr;
     const float T_used = clamp_temperature(T_row), c = 1.44269502f / T_used;

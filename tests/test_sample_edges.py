@@ -106,3 +106,16 @@ def test_few_rows_under_top_p(rows, V, kind):
             u = torch.rand(rows, generator=g).tolist()
             run_and_check(z, u, T, None, p, None, stride=V + 3)
             run_and_check(z, u, T, None, p, [10.0 ** -i for i in range(rows)] if rows < 24 else None)
+
+
+@gpu
+@needs_gpu
+@pytest.mark.parametrize("V", [300, 1500, 5000, 70001])
+def test_zeros_of_either_sign(V):
+    """A number, limits and a temperature of -0 are 0."""
+    z = logits(6, V, "f32", V)
+    u, zero = [-0.0] * 6, [-0.0] * 6
+    for kw in (dict(), dict(p=[0.9] * 6), dict(k=[20] * 6), dict(k=[20] * 6, p=[0.9] * 6), dict(k=[V // 2 + 1] * 6), dict(m=[0.1] * 6), dict(p=zero),
+               dict(k=[20] * 6, p=zero), dict(m=zero), dict(T=zero), dict(p=[0.999] * 6, T=[4.0] * 6)):
+        run_and_check(z, u, **kw)
+    run_and_check(z, [0.3, 0.99, 0.0] * 2, p=zero, m=zero)
