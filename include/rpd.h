@@ -556,6 +556,8 @@ int rpd_verify(const rpd_verify_args *args, void *workspace, int64_t workspace_b
  * most where no more than 2048 tokens can be kept: which token a border falls on can differ from exact arithmetic's only where that is closer
  * to it than some V 2^-55 of that sum, 2^-38 for V = 150000 (2^-42 for V < 8192; or 2^-31 of what weighs less than 2^-10 each,
  * where that is more).  The same call gives the same results every time.
+ * Up to some 2000 tokens are put in order at once.  A larger k, or thousands of equal logits at a border, needs passes over the row
+ * for every eight bits of a logit: 22 rows of 126464 bf16 logits take 47 us with k = 1000, 60 with 1800 and 245 with 2900.
  *
  * 1 <= V <= 2^24, 0 <= rows <= 2^26 (larger: RPD_ERR_UNSUPPORTED; 0 is a no-op). */
 typedef struct rpd_sample_args {

@@ -17,8 +17,9 @@
 // too; more than 128 go to pairs of CTAs, each of which keeps half of the matrix rows' stage and its own activations.
 //
 // What bounds it.  Few rows: reading the codes.  126464 x 4096 is 518 MB, 77.6 us at 6683 GB/s: one row takes 83.0, 128 rows (32 MB
-// of logits) 103.  Many: the accumulators' way from the tensor core to the epilogue and back.  1024 rows of 152064 x 3584 are 1116
-// GFLOP in 443 to 480 us; an MMA of 256 x 256 x 128 is 528 cycles, an accumulator's turn 910.
+// of logits) 103.  Many: no one thing.  1024 rows of 152064 x 3584 are 1116 GFLOP in 447 to 491 us, some 940 cycles for every 256 x 256
+// x 128, of which the MMAs are 528; the warp that issues them waits 261 for a stage and 253 for an accumulator (time stamps around its
+// waits).  Without the epilogue's reads of accumulators a launch of 447 us took 349, without its stores 421, without both 325.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -7,15 +7,15 @@
 // Precision.  Borders of a running sum over 10^5 tokens lie some 10^-6 of it apart, and closer: sums that carry fp32's
 // errors find another token in one row of a thousand.  Weights are therefore integers: 2^y by a table of 512 values and
 // a cubic, right to 2^-31 relative and without bias, in units of 2^-54 (and more) of the largest; the few that
-// hold more than 2^-10 of the sum are made in 64 bits.  Sums of integers do not depend on their order.
+// hold more than 2^-10 of the sum, and those of a list that decides a row, are made in 64 bits.  Sums of integers do not depend on their order.
 //
 // A cluster of up to eight CTAs has a row.  One pass brings it from HBM; later ones read it from shared memory, or from L2
 // where two slices do not fit an SM.  Most rows are decided by a list of their likeliest tokens (list_likely), others by a
 // histogram and a second pass (list_borders), the rest in passes of eight bits (sample_slowly).
 //
-// What bounds it: not HBM (128 rows of 126464 bf16 logits under top-k, top-p, min-p and a mask, 34 MB, take 33.5 us, 5.1 by bytes; 528 rows
-// of 152064 in fp32 under top-p, with the kept tokens' mask, 310 us, 49.6 by bytes), but some twenty phases with a barrier
-// of the row between them, and for rows that need all three passes their arithmetic: 63 instructions a token, at half of the
+// What bounds it: not HBM (128 rows of 126464 bf16 logits under top-k, top-p, min-p and a mask, 34 MB, take 33.6 us, 5.1 by bytes; 528 rows
+// of 152064 in fp32 under top-p, with the kept tokens' mask, 302 to 319 us, 49.6 by bytes), but some twenty phases with a barrier
+// of the row between them, and for rows that need all three passes their arithmetic: 67 instructions a token, at half of the
 // issue slots.  Four passes of a 64-bit histogram for every border, the first form, took 956 and 4982 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1826,9 +1826,9 @@ constexpr int kSampleSlice = 80 * 1024;  // that stays in shared memory, two of 
 constexpr int kSampleMask = 48 * 1024;   // of a slice's bits, at most
 
 // CTAs of a row, two of which an SM holds: as many as run at once, but no slice shorter than some 8000 tokens.  One row of
-// 126464 tokens with top-p: 22 us with eight, 28 with four; 7 rows of 50021: 22.4 with four, 23.4 with eight; one row of 4096: 9.3
-// with one, 10.2 with two, 14 with four; 128 rows of 126464 with top-k: 36.6 with two, 48 with four, 52 with one; 528
-// rows of 152064 in fp32 with top-p: 330 with two, 349 with four, 521 with one.
+// 126464 tokens with top-p: 15 to 17 us with eight, 22 with four, 36 with two; 7 rows of 50021: 22.8 with four, 23.0 with eight,
+// 28.4 with two; one row of 4096: 9.7 with one, 10.7 with two, 14.3 with four; 128 rows of 126464 with top-k: 33.5 with two, 44.5
+// with four, 45 with one; 528 rows of 152064 in fp32 with top-p: 313 with two, 330 with four, 528 with one.
 int sample_ranks(long long rows, int V, int num_sms) {
     int ranks = rows * 8 <= 2 * num_sms ? 8 : rows * 4 <= 2 * num_sms ? 4 : 2;
     while (ranks > 1 && V < ranks * 8192) ranks >>= 1;
