@@ -433,84 +433,84 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
     Fp8Segment seg;
 
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFp8OtherRegs));
-    if (warp == kFp8TmaCodes || warp == kFp8TmaRows) {
-        // ---- TMA, a warp for the codes and one for the activations
-        if (lane == 0) {
-            const bool codes = warp == kFp8TmaCodes;
-            if (!codes) {  // codes were laid out long ago: theirs need not wait
-                pdl_wait();
-                proxy_fence_global();
-            }
-            Cursor s;
-            int issued = 0;
-            bool ok = codes || !p.stall;
-            while (ok && walk.next(plan, worker, seg)) {
-                const int col_tile = seg.tile / plan.row_tiles, row_tile = (seg.tile % plan.row_tiles) * kCtas + rank;
-                const int atoms = (min(kFp8RowsTile, p.rows - row_tile * kFp8RowsTile) + 7) / 8;  // of 8 rows; single CTAs' tiles have a row
-                for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
-                    if (issued == kStages) pdl_wait();
-                    if (issued >= kStages) ok = wait_phase(&sm.done[s.at], s.phase ^ 1u, abort);
-                    if (!ok) break;
-                    uint8_t *to = smem + s.at * kStageBytes;
-                    const long long code_block = static_cast<long long>(col_tile) * plan.blocks + kb;
-                    const long long row_block = static_cast<long long>(row_tile) * plan.blocks + kb;
-                    if (kPair) {
-                        // the even CTA's barrier counts both CTAs' bytes
-                        if (rank == 0) mbar_arrive_expect_tx(&sm.full[s.at], 2 * (codes ? kCodeBytes : kFp8RowsBytes));
-                        const uint32_t bar = mapa_shared(smem_u32(&sm.full[s.at]), 0);
-                        if (codes)
-                            tma_load_2d_pair(to + kFp8RowsBytes, &map_codes, bar, 0, static_cast<int>(code_block * kFp8ColsTile) + rank * 128);
-                        else
-                            tma_load_2d_pair(to, &map_x, bar, 0, static_cast<int>(row_block * kFp8RowsTile));
-                    } else if (codes) {
-                        mbar_arrive_expect_tx(&sm.full[s.at], kFp8TileBytes);
-                        bulk_copy(to + kFp8RowsBytes, p.codes + code_block * kFp8TileBytes, kFp8TileBytes, &sm.full[s.at]);
-                    } else {  // (rows behind the last stay whatever they are: a row of A is a row of D)
-                        mbar_arrive_expect_tx(&sm.full[s.at], atoms * 1024);
-                        bulk_copy(to, p.x + row_block * kFp8RowsBytes, atoms * 1024, &sm.full[s.at]);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFp8OtherRegs));
+        if (warp == kFp8TmaCodes || warp == kFp8TmaRows) {
+            // ---- TMA, a warp for the codes and one for the activations
+            if (lane == 0) {
+                const bool codes = warp == kFp8TmaCodes;
+                if (!codes) {  // codes were laid out long ago: theirs need not wait
+                    pdl_wait();
+                    proxy_fence_global();
+                }
+                Cursor s;
+                int issued = 0;
+                bool ok = codes || !p.stall;
+                while (ok && walk.next(plan, worker, seg)) {
+                    const int col_tile = seg.tile / plan.row_tiles, row_tile = (seg.tile % plan.row_tiles) * kCtas + rank;
+                    const int atoms = (min(kFp8RowsTile, p.rows - row_tile * kFp8RowsTile) + 7) / 8;  // of 8 rows; single CTAs' tiles have a row
+                    for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
+                        if (issued == kStages) pdl_wait();
+                        if (issued >= kStages) ok = wait_phase(&sm.done[s.at], s.phase ^ 1u, abort);
+                        if (!ok) break;
+                        uint8_t *to = smem + s.at * kStageBytes;
+                        const long long code_block = static_cast<long long>(col_tile) * plan.blocks + kb;
+                        const long long row_block = static_cast<long long>(row_tile) * plan.blocks + kb;
+                        if (kPair) {
+                            // the even CTA's barrier counts both CTAs' bytes
+                            if (rank == 0) mbar_arrive_expect_tx(&sm.full[s.at], 2 * (codes ? kCodeBytes : kFp8RowsBytes));
+                            const uint32_t bar = mapa_shared(smem_u32(&sm.full[s.at]), 0);
+                            if (codes)
+                                tma_load_2d_pair(to + kFp8RowsBytes, &map_codes, bar, 0, static_cast<int>(code_block * kFp8ColsTile) + rank * 128);
+                            else
+                                tma_load_2d_pair(to, &map_x, bar, 0, static_cast<int>(row_block * kFp8RowsTile));
+                        } else if (codes) {
+                            mbar_arrive_expect_tx(&sm.full[s.at], kFp8TileBytes);
+                            bulk_copy(to + kFp8RowsBytes, p.codes + code_block * kFp8TileBytes, kFp8TileBytes, &sm.full[s.at]);
+                        } else {  // (rows behind the last stay whatever they are: a row of A is a row of D)
+                            mbar_arrive_expect_tx(&sm.full[s.at], atoms * 1024);
+                            bulk_copy(to, p.x + row_block * kFp8RowsBytes, atoms * 1024, &sm.full[s.at]);
+                        }
+                        ++issued;
+                        s.next(kStages);
                     }
-                    ++issued;
-                    s.next(kStages);
                 }
+                sm.issued_of[codes ? 0 : 1] = issued;
             }
-            sm.issued_of[codes ? 0 : 1] = issued;
-        }
-        __syncwarp();
-    } else if (warp == kFp8Mma) {
-        // ---- MMA issue, in a pair by the even CTA (every branch is warp-uniform)
-        if (rank == 0) {
-            const uint32_t idesc = idesc_e4m3(kFp8RowsTile * kCtas, kFp8ColsTile), base = __shfl_sync(0xffffffffu, tmem, 0);
-            const uint64_t a_base = smem_desc_sw128(smem_u32(smem)), b_base = smem_desc_sw128(smem_u32(smem) + kFp8RowsBytes);
-            Cursor s;
-            uint32_t acc = 0, acc_phase = 1;  // of the two accumulators: they are used in turn
-            bool ok = true;
-            pdl_wait();
-            while (ok && walk.next(plan, worker, seg)) {
-                for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
-                    ok = wait_phase_warp(&sm.full[s.at], s.phase, abort) && wait_phase_warp(&sm.acc_empty[acc], acc_phase, abort);
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                    const uint32_t at = static_cast<uint32_t>(s.at * kStageBytes) / 16;
+            __syncwarp();
+        } else if (warp == kFp8Mma) {
+            // ---- MMA issue, in a pair by the even CTA (every branch is warp-uniform)
+            if (rank == 0) {
+                const uint32_t idesc = idesc_e4m3(kFp8RowsTile * kCtas, kFp8ColsTile), base = __shfl_sync(0xffffffffu, tmem, 0);
+                const uint64_t a_base = smem_desc_sw128(smem_u32(smem)), b_base = smem_desc_sw128(smem_u32(smem) + kFp8RowsBytes);
+                Cursor s;
+                uint32_t acc = 0, acc_phase = 1;  // of the two accumulators: they are used in turn
+                bool ok = true;
+                pdl_wait();
+                while (ok && walk.next(plan, worker, seg)) {
+                    for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
+                        ok = wait_phase_warp(&sm.full[s.at], s.phase, abort) && wait_phase_warp(&sm.acc_empty[acc], acc_phase, abort);
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                        const uint32_t at = static_cast<uint32_t>(s.at * kStageBytes) / 16;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        umma_f8_warp<kPair>(base + acc * 256, a_base + at + k * 2, b_base + at + k * 2, idesc, k != 0);
-                    fp8_commit<kPair>(&sm.done[s.at]);
-                    fp8_commit<kPair>(&sm.acc_full[acc]);
-                    acc_phase ^= acc;
-                    acc ^= 1;
-                    s.next(kStages);
+                        for (int k = 0; k < 4; ++k)
+                            umma_f8_warp<kPair>(base + acc * 256, a_base + at + k * 2, b_base + at + k * 2, idesc, k != 0);
+                        fp8_commit<kPair>(&sm.done[s.at]);
+                        fp8_commit<kPair>(&sm.acc_full[acc]);
+                        acc_phase ^= acc;
+                        acc ^= 1;
+                        s.next(kStages);
+                    }
                 }
+                // everything issued has to be done before TMEM is given back
+                if (kPair)
+                    umma_commit_pair_multicast_warp(&sm.drained, 1);
+                else
+                    umma_commit_warp(&sm.drained);
+                wait_drained(&sm.drained, 0, abort);
             }
-            // everything issued has to be done before TMEM is given back
-            if (kPair)
-                umma_commit_pair_multicast_warp(&sm.drained, 1);
-            else
-                umma_commit_warp(&sm.drained);
-            wait_drained(&sm.drained, 0, abort);
+            __syncwarp();
         }
-        __syncwarp();
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFp8EpilogueRegs));
         // ---- epilogue: a thread a row of activations and 128 of the tile's columns
